@@ -381,6 +381,116 @@ int mnmt_attention_decode(const int8_t *q, const int8_t *Kc, const int8_t *Vc, c
 int mnmt_layernorm(const float *r, const float *g, const float *b, int32_t M, int32_t d, float inv,
                    float *out_f, int8_t *out_q, int32_t *status, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * Microscaled 4-bit floating point (quantising to lower bits, Sec. 3.3, in the
+ * formats that the GB300 tensor cores multiply) and the dropout of training.
+ * As above: device pointers, queued on `cuda_stream`, nothing allocated, no
+ * synchronisation.  Sizes of zero rows are valid and write only what a sum over
+ * nothing gives.  Matrices are row-major with a row stride (ld*, in elements,
+ * >= the columns) and any alignment of their element type.  rows and columns
+ * are at most 2^30.
+ * ------------------------------------------------------------------------- */
+enum { MNMT_F32 = 0, MNMT_BF16 = 1, MNMT_F16 = 2 }; /* element types (bf16 / fp16 bit patterns) */
+
+/* A matrix of E2M1 codes (0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign bit, 4 bits)
+ * with a scale per block of consecutive elements of a row:
+ *   MNMT_FP4_MX  blocks of 32, scale 2^(byte - 127), byte 255 = NaN;
+ *   MNMT_FP4_NV  blocks of 16, scale E4M3(byte), byte 0x7F = NaN, and one fp32
+ *                scale g = tensor_scale of the whole matrix, in [2^-100, 2^100]
+ *                (unused by MX).
+ * codes: [rows][mnmt_fp4_pitch(cols)] bytes, element 2j of a row in the low half
+ *   of byte j.  scales: tiles of 128 rows x 4 blocks, 512 bytes each, tile
+ *   (row / 128, block / 4) row-major; the byte of (row, block) is byte
+ *   16 (row % 32) + 4 (row % 128 / 32) + block % 4 of its tile (the order in
+ *   which the tensor cores read them).  Codes and scales beyond cols and rows
+ *   are zero: mnmt_fp4_quantize writes them so.  Both 16-byte aligned.
+ * Quantisation of a block with a = max |x|:
+ *   MX  e = max(floor(log2 a) - 2, -127) (a = 0: -127), S = 2^e, r = 2^-e
+ *   NV  s = E4M3(fl(a fl(1 / fl(6 g)))) (nearest even, at most 448),
+ *       S = fl(s g), r = fl(1 / S), 0 where S = 0
+ *   code = E2M1(fl(x r)) (nearest even, magnitude at most 6), value = fl(code S).
+ * A block that holds an infinity or a NaN has the scale NaN and codes 0. */
+enum { MNMT_FP4_MX = 0, MNMT_FP4_NV = 1 };
+typedef struct {
+    uint8_t *codes, *scales;
+    int32_t rows, cols, format;
+    float tensor_scale;
+} mnmt_fp4;
+
+/* Bytes of a row's codes (16 per 32 elements) and of a matrix's scales. */
+size_t mnmt_fp4_pitch(int32_t cols);
+size_t mnmt_fp4_scale_bytes(int32_t rows, int32_t cols, int32_t format);
+
+/* Quantises x [q->rows][q->cols] of type dtype in one pass into q's codes and
+ * scales (both given, or both NULL) and into `values` (the value of each code,
+ * rounded to dtype; may be NULL, may be x).  At least one of the two outputs. */
+int mnmt_fp4_quantize(const mnmt_fp4 *q, const void *x, int32_t dtype, int64_t ldx, void *values, int64_t ldv,
+                      void *cuda_stream);
+
+/* values = the values of q's codes, rounded to dtype. */
+int mnmt_fp4_dequantize(const mnmt_fp4 *q, void *values, int32_t dtype, int64_t ldv, void *cuda_stream);
+
+/* Straight-through gradient of the values of mnmt_fp4_quantize: gx = g where
+ * |fl(x r)| <= 6 (r as above, found again from x), 0 where the code was held at
+ * 6 and in blocks with an infinity or a NaN.  x, g and gx of type dtype; of q only
+ * rows, cols, format and tensor_scale are used.  gx may be x or g. */
+int mnmt_fp4_quantize_backward(const mnmt_fp4 *q, const void *x, int32_t dtype, int64_t ldx, const void *g, int64_t ldg,
+                               void *gx, int64_t ldgx, void *cuda_stream);
+
+/* Linear on 4-bit floating-point operands:
+ *   y[m][n] = act(alpha sum_k X[m][k] W[n][k] + bias[n])
+ * with X, W the codes times their block scales (products exact, sums in fp32),
+ * alpha = fl(g_x g_w) for NV and 1 for MX, bias [N] fp32 or NULL, act = ReLU if
+ * relu != 0, y rounded once to ydtype.  X is quantised from x (type xdtype) into
+ * xq's buffers, which hold it afterwards (for the backward pass); with x = NULL
+ * xq holds it already.  xq and w have the same cols and format.  *status (device
+ * int32, may be NULL) receives MNMT_ETIMEOUT if a bounded wait of the kernel
+ * gave up (affected tiles are then not written). */
+int mnmt_fp4_linear(const mnmt_fp4 *xq, const mnmt_fp4 *w, const void *x, int32_t xdtype, int64_t ldx, const float *bias,
+                    int32_t relu, void *y, int32_t ydtype, int64_t ldy, int32_t *status, void *cuda_stream);
+
+/* Gradients of that linear (before ReLU) for output gradients G [M][N] in bf16:
+ *   gx[m][k] = in_x alpha_w sum_n G[m][n] W[n][k]      type xdtype
+ *   gw[n][k] = in_w alpha_x sum_m G[m][n] X[m][k]      fp32
+ *   gb[n]    = sum_m G[m][n]                           fp32
+ * (alpha_w, alpha_x: the tensor scales for NV, else 1; products exact, sums in
+ * fp32 in a fixed order).  in_x, in_w: the straight-through masks, |fl(x r)| <= 6,
+ * from the float originals x [M][K] and w [N][K] (types xdtype and wdtype) and the
+ * scales of xq and wq; a NULL original means no mask.  gx, gw and gb may each be
+ * NULL.  workspace: mnmt_fp4_linear_backward_workspace(M, N, K) bytes of device
+ * scratch, 16-byte aligned. */
+size_t mnmt_fp4_linear_backward_workspace(int32_t M, int32_t N, int32_t K);
+int mnmt_fp4_linear_backward(const mnmt_fp4 *xq, const mnmt_fp4 *wq, const void *G, int64_t ldg, const void *x,
+                             int32_t xdtype, int64_t ldx, const void *w, int32_t wdtype, int64_t ldw, void *workspace,
+                             void *gx, int64_t ldgx, float *gw, int64_t ldgw, float *gb, int32_t *status,
+                             void *cuda_stream);
+
+/* Dropout of a sublayer, with the gamma residual of Fig. 5 (r may be NULL: none)
+ * and an optional ReLU in front:
+ *   out[m][c] = fl(fl(gamma r[m][c]) + D(act(x[m][c]))),  D(v) = keep ? fl(v s) : 0
+ * keep: the 16-bit field c % 8 (the low half of a word first) of Philox4x32-10 with
+ * counter {c / 8, m, offset low, offset high} and key seed is >= t, where
+ * t = rne(65536 p) and s = fl(65536 / (65536 - t)); p = 1 drops everything.  p in
+ * [0, 1].  No mask is stored: calls with one (seed, offset) draw the same numbers,
+ * so a program gives each dropout of each step an offset of its own.  x of type
+ * dtype; r and out of type otype.  out may be x (if the types are equal) or r. */
+int mnmt_dropout(const void *x, int32_t dtype, int64_t ldx, const void *r, int64_t ldr, float gamma, float p, uint64_t seed,
+                 uint64_t offset, int32_t relu, int32_t M, int32_t d, void *out, int32_t otype, int64_t ldo,
+                 void *cuda_stream);
+
+/* Its backward pass for the gradient g [M][d] of out (type otype):
+ *   gx = keep and (relu: x > 0) ? fl(g s) : 0   type dtype (x is read only if relu)
+ *   gr = fl(gamma g)                            type otype
+ *   *ggamma = sum g r                           fp32, summed in a fixed order
+ * Each output may be NULL; ggamma needs r and workspace (MNMT_DROPOUT_WORKSPACE
+ * bytes of device scratch, 8-byte aligned).  gx may be x or g, gr may be g (gx and gr are
+ * then not the same). */
+#define MNMT_DROPOUT_WORKSPACE 16384
+int mnmt_dropout_backward(const void *g, int32_t otype, int64_t ldg, const void *x, int32_t dtype, int64_t ldx, const void *r,
+                          int64_t ldr, float gamma, float p, uint64_t seed, uint64_t offset, int32_t relu, int32_t M,
+                          int32_t d, void *gx, int64_t ldgx, void *gr, int64_t ldgr, float *ggamma, void *workspace,
+                          void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

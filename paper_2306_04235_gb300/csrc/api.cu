@@ -1703,6 +1703,7 @@ extern "C" int mnmt_session_decode_path(mnmt_session *s) {
 }
 
 int mnmt::set_error(int code, const char *msg) { return fail(code, "%s", msg); }
+int mnmt::ensure_device() { return lib_init(); }
 
 // ---------------------------------------------------------------------------
 // kernel-level entry points

@@ -18,6 +18,9 @@ from . import build as _build
 
 OK, EINVAL, ENOMEM, ECUDA, ETIMEOUT, EFORMAT, EOVERFLOW = 0, -1, -2, -3, -4, -5, -6
 DEVICE_PTRS = 1
+F32, BF16, F16 = 0, 1, 2
+FP4_MX, FP4_NV = 0, 1
+DROPOUT_WORKSPACE = 16384
 EPI_Q8, EPI_RELU_Q8, EPI_RESID, EPI_F32, EPI_ARGMAX = 0, 1, 2, 3, 4
 (TAP_ENC_OUT, TAP_CROSS_K, TAP_CROSS_V, TAP_SELF_K, TAP_SELF_V, TAP_DEC_OUT, TAP_LOGITS, TAP_RESID,
  TAP_HISTORY, TAP_PARENTS, TAP_ANCESTRY, TAP_STEP) = range(1, 13)
@@ -35,6 +38,17 @@ class MnmtError(RuntimeError):
 class _Config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ["n_enc", "n_dec", "d_model", "n_heads", "d_ffn", "vocab", "d_embed",
                                          "pre_ln", "tied_output", "max_pos", "pad_id", "bos_id", "eos_id"]]
+
+
+class Fp4(C.Structure):
+    """A matrix in microscaled 4-bit floating point (mnmt_fp4): where its codes
+    and scales are (device buffers, kept alive by this object; None: none)."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int32), ("cols", C.c_int32),
+                ("format", C.c_int32), ("tensor_scale", C.c_float)]
+
+    def __init__(self, rows, cols, format, tensor_scale=1.0, codes=None, scales=None):
+        super().__init__(_ptr(codes), _ptr(scales), rows, cols, format, tensor_scale)
+        self.buffers = codes, scales
 
 
 def lib_path() -> str:
@@ -87,6 +101,22 @@ def _declare(L):
     L.mnmt_fake_quant.argtypes = [p, sz, f, f, i32, i32, p, p, p]
     L.mnmt_fake_quant_backward.argtypes = [p, p, sz, f, f, i32, i32, p, p, p, p]
     L.mnmt_fake_quant_linear.argtypes = [p, p, f, p, p, i32, i32, i32, i32, p, p, p]
+    fp4, i64, u64 = C.POINTER(Fp4), C.c_int64, C.c_uint64
+    L.mnmt_fp4_pitch.argtypes = [i32]; L.mnmt_fp4_pitch.restype = sz
+    L.mnmt_fp4_scale_bytes.argtypes = [i32, i32, i32]; L.mnmt_fp4_scale_bytes.restype = sz
+    L.mnmt_fp4_quantize.argtypes = [fp4, p, i32, i64, p, i64, p]
+    L.mnmt_fp4_dequantize.argtypes = [fp4, p, i32, i64, p]
+    L.mnmt_fp4_quantize_backward.argtypes = [fp4, p, i32, i64, p, i64, p, i64, p]
+    L.mnmt_fp4_linear.argtypes = [fp4, fp4, p, i32, i64, p, i32, p, i32, i64, p, p]
+    L.mnmt_fp4_linear_backward_workspace.argtypes = [i32, i32, i32]
+    L.mnmt_fp4_linear_backward_workspace.restype = sz
+    L.mnmt_fp4_linear_backward.argtypes = [fp4, fp4, p, i64, p, i32, i64, p, i32, i64, p, p, i64, p, i64, p, p, p]
+    L.mnmt_dropout.argtypes = [p, i32, i64, p, i64, f, f, u64, u64, i32, i32, i32, p, i32, i64, p]
+    L.mnmt_dropout_backward.argtypes = [p, i32, i64, p, i32, i64, p, i64, f, f, u64, u64, i32, i32, i32, p, i64, p, i64,
+                                        p, p, p]
+    for n in ["mnmt_fp4_quantize", "mnmt_fp4_dequantize", "mnmt_fp4_quantize_backward", "mnmt_fp4_linear",
+              "mnmt_fp4_linear_backward", "mnmt_dropout", "mnmt_dropout_backward"]:
+        getattr(L, n).restype = C.c_int
     for n in ["mnmt_fake_quant", "mnmt_fake_quant_backward", "mnmt_fake_quant_linear"]:
         getattr(L, n).restype = C.c_int
     L.mnmt_wait_timeout_selftest.argtypes = [p, p]
@@ -275,6 +305,59 @@ def mnmt_fake_quant_linear(X, W, s_x, s_w, bias, M, N, K, wbits, workspace, y, s
     """QAT forward of a linear from fp32 input and weights (learnable scales)."""
     _chk(lib().mnmt_fake_quant_linear(_ptr(X), _ptr(W), float(s_x), _ptr(s_w), _ptr(bias), M, N, K, wbits,
                                       _ptr(workspace), _ptr(y), _stream_handle(stream)))
+
+
+def mnmt_fp4_pitch(cols: int) -> int:
+    return lib().mnmt_fp4_pitch(cols)
+
+
+def mnmt_fp4_scale_bytes(rows: int, cols: int, format: int) -> int:
+    return lib().mnmt_fp4_scale_bytes(rows, cols, format)
+
+
+def mnmt_fp4_quantize(q: Fp4, x, dtype, ldx, values=None, ldv=0, stream=None):
+    """x into q's codes and scales (where it has them) and into values (device buffers)."""
+    _chk(lib().mnmt_fp4_quantize(q, _ptr(x), dtype, ldx, _ptr(values), ldv, _stream_handle(stream)))
+
+
+def mnmt_fp4_dequantize(q: Fp4, values, dtype, ldv, stream=None):
+    _chk(lib().mnmt_fp4_dequantize(q, _ptr(values), dtype, ldv, _stream_handle(stream)))
+
+
+def mnmt_fp4_quantize_backward(q: Fp4, x, dtype, ldx, g, ldg, gx, ldgx, stream=None):
+    """Straight-through gradient of mnmt_fp4_quantize's values."""
+    _chk(lib().mnmt_fp4_quantize_backward(q, _ptr(x), dtype, ldx, _ptr(g), ldg, _ptr(gx), ldgx, _stream_handle(stream)))
+
+
+def mnmt_fp4_linear(xq: Fp4, w: Fp4, x, xdtype, ldx, bias, relu, y, ydtype, ldy, status=None, stream=None):
+    """Linear on 4-bit floating-point operands; x (None: xq holds it already) is quantised into xq first."""
+    _chk(lib().mnmt_fp4_linear(xq, w, _ptr(x), xdtype, ldx, _ptr(bias), int(relu), _ptr(y), ydtype, ldy, _ptr(status),
+                               _stream_handle(stream)))
+
+
+def mnmt_fp4_linear_backward_workspace(M: int, N: int, K: int) -> int:
+    return lib().mnmt_fp4_linear_backward_workspace(M, N, K)
+
+
+def mnmt_fp4_linear_backward(xq: Fp4, wq: Fp4, g, ldg, x, xdtype, ldx, w, wdtype, ldw, workspace, gx=None, ldgx=0, gw=None,
+                             ldgw=0, gb=None, status=None, stream=None):
+    """Gradients of mnmt_fp4_linear for bf16 output gradients g (x, w: the originals, None: no straight-through mask)."""
+    _chk(lib().mnmt_fp4_linear_backward(xq, wq, _ptr(g), ldg, _ptr(x), xdtype, ldx, _ptr(w), wdtype, ldw, _ptr(workspace),
+                                        _ptr(gx), ldgx, _ptr(gw), ldgw, _ptr(gb), _ptr(status), _stream_handle(stream)))
+
+
+def mnmt_dropout(x, dtype, ldx, r, ldr, gamma, p, seed, offset, relu, M, d, out, otype, ldo, stream=None):
+    """out = gamma r + dropout(relu?(x)) (r None: no residual)."""
+    _chk(lib().mnmt_dropout(_ptr(x), dtype, ldx, _ptr(r), ldr, gamma, p, seed, offset, int(relu), M, d, _ptr(out), otype,
+                            ldo, _stream_handle(stream)))
+
+
+def mnmt_dropout_backward(g, otype, ldg, x, dtype, ldx, r, ldr, gamma, p, seed, offset, relu, M, d, gx=None, ldgx=0, gr=None,
+                          ldgr=0, ggamma=None, workspace=None, stream=None):
+    """Gradients of mnmt_dropout: gx, gr and the scalar ggamma, each where given."""
+    _chk(lib().mnmt_dropout_backward(_ptr(g), otype, ldg, _ptr(x), dtype, ldx, _ptr(r), ldr, gamma, p, seed, offset,
+                                     int(relu), M, d, _ptr(gx), ldgx, _ptr(gr), ldgr, _ptr(ggamma), _ptr(workspace),
+                                     _stream_handle(stream)))
 
 
 def mnmt_codes_to_f16(src, dst, n, stream=None):
