@@ -4,6 +4,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <mutex>
 
 #include "fp4.cuh"
 #include "internal.h"
@@ -34,6 +35,23 @@ bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 bool matrix_ok(const void *p, int32_t dtype, int64_t ld, int32_t cols) {
     const int e = type_size(dtype);
     return e && p && aligned(p, e) && ld >= cols && ld <= ((int64_t)1 << 40);
+}
+
+// one-time set-up of the product kernels, apart from the library's own so that
+// programs that only translate do not load them
+int fp4_ready() {
+    if (int rc = ensure_device()) return rc;
+    static std::mutex mu;
+    static bool ready[64] = {false};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return fail(MNMT_ECUDA, "fp4: no usable current device");
+    std::lock_guard<std::mutex> lk(mu);
+    if (!ready[dev]) {
+        const cudaError_t e = fp4_init();
+        if (e != cudaSuccess) return fail(MNMT_ECUDA, "fp4 kernel set-up failed: %s", cudaGetErrorString(e));
+        ready[dev] = true;
+    }
+    return MNMT_OK;
 }
 
 // 0 if q's sizes and format are valid (and, with buffers, its pointers)
@@ -118,7 +136,7 @@ extern "C" int mnmt_fp4_quantize_backward(const mnmt_fp4 *q, const void *x, int3
 
 extern "C" int mnmt_fp4_linear(const mnmt_fp4 *xq, const mnmt_fp4 *w, const void *x, int32_t xdtype, int64_t ldx, const float *bias, int32_t relu,
                                void *y, int32_t ydtype, int64_t ldy, int32_t *status, void *cuda_stream) {
-    int rc = ensure_device();
+    int rc = fp4_ready();
     if (rc) return rc;
     if ((rc = check_fp4("fp4_linear", xq, true)) || (rc = check_fp4("fp4_linear", w, true))) return rc;
     if (xq->cols != w->cols || xq->format != w->format) return fail(MNMT_EINVAL, "fp4_linear: operands of different depth or format");
@@ -144,7 +162,7 @@ extern "C" size_t mnmt_fp4_linear_backward_workspace(int32_t M, int32_t N, int32
 extern "C" int mnmt_fp4_linear_backward(const mnmt_fp4 *xq, const mnmt_fp4 *wq, const void *G, int64_t ldg, const void *x, int32_t xdtype,
                                         int64_t ldx, const void *w, int32_t wdtype, int64_t ldw, void *workspace, void *gx, int64_t ldgx,
                                         float *gw, int64_t ldgw, float *gb, int32_t *status, void *cuda_stream) {
-    int rc = ensure_device();
+    int rc = fp4_ready();
     if (rc) return rc;
     if ((rc = check_fp4("fp4_linear_backward", xq, true)) || (rc = check_fp4("fp4_linear_backward", wq, true))) return rc;
     const int M = xq->rows, N = wq->rows, K = xq->cols;

@@ -50,23 +50,6 @@ MNMT_DEV void tile_product(float (&acc)[4][4], int K, A &&a, B &&b) {
     }
 }
 
-template <bool NV, typename Y>
-__global__ void __launch_bounds__(256) fp4_product_kernel(Fp4Args x, Fp4Args w, float alpha, const float *bias, int relu, Y *y, long ldy) {
-    pdl_grid_wait();
-    float acc[4][4] = {};
-    tile_product(acc, x.cols, [&](int m, int k) { return fp4_at<NV>(x, m, k); }, [&](int n, int k) { return fp4_at<NV>(w, n, k); });
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int i = 0; i < 4; i++)
-        for (int j = 0; j < 4; j++) {
-            const int m = blockIdx.y * PT + ty + 16 * i, n = blockIdx.x * PT + tx + 16 * j;
-            if (m >= x.rows || n >= w.rows) continue;
-            float v = __fmul_rn(alpha, acc[i][j]);
-            if (bias) v = __fadd_rn(v, bias[n]);
-            if (relu && v <= 0.0f) v = 0.0f;
-            y[m * ldy + n] = from_f32<Y>(v);
-        }
-}
-
 // whether fp32 x lies within the range of its block
 template <bool NV>
 MNMT_DEV bool fp4_inside(const Fp4Args &q, int row, int k, float x) {
@@ -124,16 +107,6 @@ void by_type(int dtype, F &&f) {
 dim3 tiles(int rows, int cols) { return dim3((cols + PT - 1) / PT, (rows + PT - 1) / PT); }
 
 }  // namespace
-
-cudaError_t launch_fp4_product(const Fp4Args &x, const Fp4Args &w, bool nv, float alpha, const float *bias, int relu, void *y, int ydtype,
-                               long ldy, int *, cudaStream_t st) {
-    by_type(ydtype, [&](auto t) {
-        using Y = decltype(t);
-        launch_pdl(nv ? fp4_product_kernel<true, Y> : fp4_product_kernel<false, Y>, tiles(x.rows, w.rows), 256, 0, st, x, w, alpha, bias, relu,
-                   static_cast<Y *>(y), ldy);
-    });
-    return cudaGetLastError();
-}
 
 size_t fp4_backward_workspace(int, int, int) { return 16; }
 

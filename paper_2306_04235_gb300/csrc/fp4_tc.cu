@@ -1,0 +1,513 @@
+// fp4_tc.cu -- product of two microscaled 4-bit floating-point matrices on the
+// fifth-generation tensor cores (mnmt_fp4_linear):
+//   y[m][n] = act(alpha sum_k X[m][k] W[n][k] + bias[n]).
+//
+// tcgen05.mma kind::mxf4 / mxf4nvf4 multiplies packed E2M1 codes and applies the
+// block scales itself: 64 codes of K per instruction, scales in TMEM, sums in
+// fp32.  So the kernel moves the codes as they are stored (128-byte-swizzled TMA
+// tiles of 256 codes) and the scales as they are stored: a 512-byte tile of 128
+// rows x 4 blocks goes to four TMEM columns with one tcgen05.cp.
+//
+// Persistent, 320 threads per CTA:
+//   warp 0 lane 0   TMA producer: codes and scales of a k-block of 256 into a ring;
+//   warp 1 lane 0   copies a k-block's scales to TMEM (tcgen05.cp and .mma run in
+//                   the order in which they are issued, so one set of columns
+//                   serves every k-block), issues its four MMAs, frees the slot;
+//   warps 2..9      drain a finished accumulator (TMEM holds two), apply alpha,
+//                   bias and ReLU, round, and store through shared memory by TMA.
+// CG = 2: a pair of CTAs computes 256 x 192 tiles, each CTA half of the rows of
+// both operands; CG = 1: 128 x 128 or 128 x 64 tiles for smaller grids.
+// Every wait is bounded; one that runs out records MNMT_ETIMEOUT in *status, and
+// the CTA stops issuing work, waits (bounded) for what it has in flight, frees
+// its TMEM and returns.
+#include <type_traits>
+
+#include "fp4.cuh"
+#include "internal.h"
+#include "mbarrier.cuh"
+#include "tcgen05.cuh"
+
+namespace mnmt {
+namespace {
+
+constexpr int F4_BM = 128;
+constexpr int F4_BK = 256;  // codes per k-block: 128 bytes
+constexpr int F4_EPI_WARPS = 8;
+constexpr int F4_THREADS = 64 + F4_EPI_WARPS * 32;
+constexpr int F4_BLK = 2048;  // a staging block: 32 rows of 64 bytes
+
+template <int CG, int BN, bool NV>
+struct F4Layout {
+    static constexpr int T = NV ? 4 : 2;                // scale tiles along a k-block
+    static constexpr int R = BN > 128 ? 2 : 1;          // row tiles of W's scales that a tile touches
+    static constexpr uint32_t A_BYTES = F4_BM * 128;
+    static constexpr uint32_t B_BYTES = BN / CG * 128;
+    static constexpr uint32_t OFF_SFA = A_BYTES + B_BYTES, OFF_SFB = OFF_SFA + T * 512;
+    static constexpr uint32_t STAGE = OFF_SFB + R * T * 512;
+    static constexpr uint32_t OFF_AFTER = F4_EPI_WARPS * 2 * F4_BLK + 2 * BN * 4 + 512;  // staging, bias, barriers
+    static constexpr int FIT = (int)((227 * 1024 - 1024 - OFF_AFTER) / STAGE);
+    static constexpr int STAGES = FIT > 8 ? 8 : FIT;
+    static constexpr uint32_t OFF_STG = STAGES * STAGE;
+    static constexpr uint32_t OFF_COLS = OFF_STG + F4_EPI_WARPS * 2 * F4_BLK;  // [2][BN] fp32
+    static constexpr uint32_t OFF_BARS = OFF_COLS + 2 * BN * 4;
+    static constexpr int NBARS = 2 * STAGES + 5;  // full, empty, acc_full[2], acc_empty[2], done
+    static constexpr uint32_t OFF_MISC = OFF_BARS + NBARS * 8;
+    static constexpr size_t SMEM = 1024 + OFF_MISC + 16;
+    static constexpr int COL_SFA = 2 * BN, COL_SFB = COL_SFA + 4 * T;  // TMEM columns
+    static constexpr int COLS = COL_SFB + 4 * R * T <= 256 ? 256 : 512;
+    static_assert(COL_SFB + 4 * R * T <= 512, "TMEM holds 512 columns");
+    static_assert(STAGE % 1024 == 0, "swizzled tiles start on 1024 bytes");
+    static_assert(OFF_MISC + 16 - OFF_STG <= OFF_AFTER, "barriers fit");
+};
+
+// instruction descriptor of the block-scaled kinds: E2M1 operands, both K-major,
+// scales UE8M0 or UE4M3, K = 64; id: which bytes of a scale word apply
+__host__ __device__ constexpr uint32_t f4_idesc(int m, int n, bool nv, int id) {
+    return ((uint32_t)id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((nv ? 0u : 1u) << 23) | ((uint32_t)(m >> 7) << 27) |
+           ((uint32_t)id << 29);
+}
+
+// a 512-byte scale tile: no swizzle, 8-row groups of 128 bytes
+__device__ __forceinline__ uint64_t f4_scale_desc(uint32_t saddr) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)8 << 16) | ((uint64_t)8 << 32) | ((uint64_t)1 << 46);
+}
+
+template <int CG, bool NV>
+__device__ __forceinline__ void f4_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+#define F4_MMA(G, KIND)                                                                                            \
+    asm volatile(                                                                                                  \
+        "{\n\t.reg .pred p;\n\t"                                                                                   \
+        "setp.ne.b32 p, %4, 0;\n\t"                                                                                \
+        "tcgen05.mma.cta_group::" G ".kind::" KIND " [%0], %1, %2, %3, [%5], [%6], p;\n\t}" ::"r"(d),              \
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)                                            \
+        : "memory")
+    if constexpr (CG == 1 && NV) F4_MMA("1", "mxf4nvf4.block_scale.scale_vec::4X");
+    else if constexpr (CG == 1) F4_MMA("1", "mxf4.block_scale.scale_vec::2X");
+    else if constexpr (NV) F4_MMA("2", "mxf4nvf4.block_scale.scale_vec::4X");
+    else F4_MMA("2", "mxf4.block_scale.scale_vec::2X");
+#undef F4_MMA
+}
+
+// scale tile -> four TMEM columns, repeated in the four lane quarters (of both CTAs of a pair)
+template <int CG>
+__device__ __forceinline__ void f4_copy_scales(uint32_t taddr, uint64_t desc) {
+    if constexpr (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+template <int CG>
+__device__ __forceinline__ void f4_load(uint32_t dst, const CUtensorMap *tm, int x, int y, uint32_t bar) {
+    if constexpr (CG == 1) tma_load_2d(dst, tm, x, y, bar);
+    else t2_load(dst, tm, x, y, bar);
+}
+template <int CG>
+__device__ __forceinline__ void f4_commit(uint32_t bar) {
+    if constexpr (CG == 1) mma_commit(bar);
+    else t2_commit(bar);
+}
+
+__device__ __forceinline__ void f4_epi_sync() { asm volatile("bar.sync 1, %0;" ::"n"(F4_EPI_WARPS * 32) : "memory"); }
+
+struct F4Out {
+    void *y;
+    long ldy;
+    int type;   // MNMT_F32 / BF16 / F16
+    int tma;    // tmY describes y
+    int relu;
+    float alpha;
+    const float *bias;
+};
+
+// 32 outputs of a row, rounded, into staging blocks (row = lane): one of 32
+// 16-bit outputs, or half h of 32 fp32 ones
+__device__ __forceinline__ void f4_stage16(uint8_t *blk, const float (&v)[32], int type) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float lo = v[8 * c + 2 * i], hi = v[8 * c + 2 * i + 1];
+            if (type == MNMT_BF16) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                const __half2 h = __floats2half2_rn(lo, hi);
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+        }
+        *reinterpret_cast<uint4 *>(blk + lane * 64 + t2_chunk<64>(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <int H>
+__device__ __forceinline__ void f4_stage32(uint8_t *blk, const float (&v)[32]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int c = 0; c < 4; c++)
+        *reinterpret_cast<float4 *>(blk + lane * 64 + t2_chunk<64>(lane, c)) =
+            make_float4(v[16 * H + 4 * c], v[16 * H + 4 * c + 1], v[16 * H + 4 * c + 2], v[16 * H + 4 * c + 3]);
+}
+
+// a staged block to y where no tensor map describes it: coalesced single elements
+__device__ __forceinline__ void f4_store_plain(const F4Out &o, const uint8_t *blk, int row0, int col0, int M, int N) {
+    const int lane = threadIdx.x & 31;
+    if (o.type == MNMT_F32) {
+        const int c = lane & 15;
+        for (int r = lane >> 4; r < 32; r += 2)
+            if (row0 + r < M && col0 + c < N)
+                static_cast<float *>(o.y)[(row0 + r) * o.ldy + col0 + c] =
+                    *reinterpret_cast<const float *>(blk + r * 64 + t2_chunk<64>(r, c >> 2) + 4 * (c & 3));
+    } else {
+        for (int r = 0; r < 32; r++)
+            if (row0 + r < M && col0 + lane < N)
+                static_cast<uint16_t *>(o.y)[(row0 + r) * o.ldy + col0 + lane] =
+                    *reinterpret_cast<const uint16_t *>(blk + r * 64 + t2_chunk<64>(r, lane >> 3) + 2 * (lane & 7));
+    }
+}
+
+template <int CG, int BN, bool NV>
+__global__ void __launch_bounds__(F4_THREADS, 1)
+    fp4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmSA,
+             const __grid_constant__ CUtensorMap tmSB, const __grid_constant__ CUtensorMap tmY, F4Out o, int M, int N, int K, int *status) {
+    pdl_grid_wait();
+    using L = F4Layout<CG, BN, NV>;
+    constexpr int STAGES = L::STAGES, T = L::T, R = L::R;
+
+    extern __shared__ uint8_t f4_raw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(f4_raw) + 1023) & ~(uintptr_t)1023);
+    float *cols = reinterpret_cast<float *>(sm + L::OFF_COLS);
+    const uint32_t bars = s_addr(sm + L::OFF_BARS);
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
+    auto accf_bar = [&](int b) { return bars + 8u * (2 * STAGES + b); };
+    auto acce_bar = [&](int b) { return bars + 8u * (2 * STAGES + 2 + b); };
+    const uint32_t done_bar = bars + 8u * (2 * STAGES + 4);
+    uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);  // [0] tmem base, [1] abort, [2] consumed
+    volatile uint32_t *abort_flag = misc + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t rank = 0;
+    if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
+    const int mt = (M + CG * F4_BM - 1) / (CG * F4_BM), nt = (N + BN - 1) / BN;
+    const long tiles = (long)mt * nt;
+    // the dimension of fewer tiles runs fastest: the larger operand is then read
+    // by CTAs that run at the same time
+    auto tile_m = [&](long t) { return (int)(mt <= nt ? t % mt : t / nt) * CG * F4_BM; };
+    auto tile_n = [&](long t) { return (int)(mt <= nt ? t / mt : t % nt) * BN; };
+    const int steps = (K + 63) / 64, nkb = (K + F4_BK - 1) / F4_BK, tiles_k = fp4_tiles_k(K, NV);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; s++) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int b = 0; b < 2; b++) {
+            mbar_init(accf_bar(b), 1);
+            mbar_init(acce_bar(b), CG * F4_EPI_WARPS);
+        }
+        mbar_init(done_bar, 1);
+        misc[1] = 0;
+        misc[2] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        if constexpr (CG == 1) {
+            tmem_alloc<L::COLS>(s_addr(misc));
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s_addr(misc)), "r"(L::COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+        tc_fence_before();
+    }
+    // barriers and accumulators are set up, in both CTAs of a pair
+    if constexpr (CG == 2) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tbase = misc[0];
+
+    uint32_t issued = 0;
+    if (warp == 0 && lane == 0) {
+        // ---- TMA producer: this CTA's rows of all its tiles ----
+        uint32_t it = 0;
+        bool failed = false;
+        const uint32_t ring = s_addr(sm);
+        for (long tile = unit; tile < tiles && !failed && !*abort_flag; tile += units) {
+            const int m0 = tile_m(tile) + (int)rank * F4_BM, nb = tile_n(tile), n0 = nb + (int)rank * (BN / CG);
+            for (int kb = 0; kb < nkb; kb++, it++) {
+                const int s = (int)(it % STAGES);
+                if (it >= STAGES && !mbar_wait(empty_bar(s), (it / STAGES - 1) & 1)) {
+                    *abort_flag = 1;
+                    set_status(status, MNMT_ETIMEOUT);
+                    failed = true;
+                    break;
+                }
+                // the leader's barrier takes the bytes of both CTAs of a pair
+                if (rank == 0) mbar_expect_tx(full_bar(s), CG * L::STAGE);
+                const uint32_t bar = CG == 1 ? full_bar(s) : t2_mapa(full_bar(s), 0), base = ring + s * L::STAGE;
+                f4_load<CG>(base, &tmA, kb * 128, m0, bar);
+                f4_load<CG>(base + L::A_BYTES, &tmB, kb * 128, n0, bar);
+                // scale tiles kb T .. of the rows' tile rows (tiles past the row's
+                // end belong to k-steps that are not issued)
+                f4_load<CG>(base + L::OFF_SFA, &tmSA, 0, (m0 >> 7) * tiles_k + kb * T, bar);
+#pragma unroll
+                for (int r = 0; r < R; r++)
+                    f4_load<CG>(base + L::OFF_SFB + r * T * 512, &tmSB, 0, ((nb >> 7) + r) * tiles_k + kb * T, bar);
+                issued = it + 1;
+            }
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        // ---- scales to TMEM and MMAs ----
+        uint32_t it = 0, lt = 0;
+        bool failed = false;
+        const uint32_t ring = s_addr(sm);
+        const uint64_t a_desc = sw128_desc(ring), b_desc = sw128_desc(ring + L::A_BYTES);
+        const uint64_t sa_desc = f4_scale_desc(ring + L::OFF_SFA), sb_desc = f4_scale_desc(ring + L::OFF_SFB);
+        for (long tile = unit; tile < tiles && !failed; tile += units, lt++) {
+            const int buf = (int)(lt & 1);
+            if (lt >= 2 && !mbar_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
+                failed = true;
+                break;
+            }
+            tc_fence_after();
+            const uint32_t d = tbase + (uint32_t)(buf * BN);
+            // scale columns of the tile's first row of W (a tile that starts inside a row tile: two columns per 64 rows)
+            const uint32_t sfa = tbase + L::COL_SFA, sfb = tbase + L::COL_SFB, shift = (uint32_t)((tile_n(tile) & 127) >> 5);
+            for (int kb = 0; kb < nkb; kb++, it++) {
+                const int s = (int)(it % STAGES);
+                if (!mbar_wait(full_bar(s), (it / STAGES) & 1)) {
+                    failed = true;
+                    break;
+                }
+                tc_fence_after();
+                const uint64_t off = (uint64_t)((s * L::STAGE) >> 4);
+#pragma unroll
+                for (int t = 0; t < T; t++) {
+                    f4_copy_scales<CG>(sfa + 4 * t, sa_desc + off + (uint64_t)(t * 32));
+#pragma unroll
+                    for (int r = 0; r < R; r++) f4_copy_scales<CG>(sfb + 4 * (R * t + r), sb_desc + off + (uint64_t)((r * T + t) * 32));
+                }
+                const int n = min(4, steps - 4 * kb);
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    if (k < n) {
+                        const int t = NV ? k : k >> 1, id = NV ? 0 : 2 * (k & 1);
+                        f4_mma<CG, NV>(d, a_desc + off + (uint64_t)(2 * k), b_desc + off + (uint64_t)(2 * k), f4_idesc(CG * F4_BM, BN, NV, id),
+                                       sfa + 4 * t, sfb + 4 * R * t + shift, (uint32_t)(kb | k));
+                    }
+                }
+                f4_commit<CG>(empty_bar(s));
+            }
+            if (!failed) f4_commit<CG>(accf_bar(buf));
+        }
+        if (failed) {
+            *abort_flag = 1;
+            set_status(status, MNMT_ETIMEOUT);
+        }
+        pdl_allow_next();  // every MMA of this CTA (pair) is issued
+        misc[2] = it;      // k-blocks whose copies this thread saw land
+        f4_commit<CG>(done_bar);
+    } else if (warp == 1 && lane == 0) {
+        pdl_allow_next();  // the leader's trigger decides
+    } else if (warp >= 2) {
+        // ---- epilogue of this CTA's 128 rows: warp half h takes columns h BN/2 .. ----
+        constexpr int NB = BN / 64;
+        const int ew = warp - 2, q = warp & 3, cw = (BN / 2) * (ew >> 2);
+        uint8_t *stg = sm + L::OFF_STG + ew * 2 * F4_BLK;
+        const uint32_t stg_s = s_addr(stg);
+        const int ti = ew * 32 + lane;
+        uint32_t lt = 0, blocks = 0;  // blocks staged so far: they alternate between the two buffers
+        for (long tile = unit; tile < tiles; tile += units, lt++) {
+            const int buf = (int)(lt & 1);
+            const int n0 = tile_n(tile), row0 = tile_m(tile) + (int)rank * F4_BM + 32 * q, col0 = n0 + cw;
+            float *bias = cols + (lt & 1) * BN;
+            if (ti < BN) bias[ti] = o.bias && n0 + ti < N ? o.bias[n0 + ti] : 0.0f;
+            f4_epi_sync();
+            bool ok = *abort_flag == 0 && mbar_wait(accf_bar(buf), (lt >> 1) & 1);
+            if (!ok && *abort_flag == 0) {
+                *abort_flag = 1;
+                set_status(status, MNMT_ETIMEOUT);
+            }
+            tc_fence_after();
+            ok = __all_sync(0xFFFFFFFFu, ok && *abort_flag == 0);
+            const uint32_t taddr = tbase + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * BN + cw);
+            const bool mine = ok && row0 < M;
+#pragma unroll 1
+            for (int b = 0; b < NB; b++) {
+                float v[32];
+                if (mine && col0 + 32 * b < N) {
+                    uint32_t r[32];
+                    tmem_ld32(taddr + 32 * b, r);
+                    tmem_wait_ld();
+                    const float *bb = bias + cw + 32 * b;
+#pragma unroll
+                    for (int i = 0; i < 32; i++) {
+                        v[i] = __fadd_rn(__fmul_rn(__uint_as_float(r[i]), o.alpha), bb[i]);
+                        if (o.relu && v[i] <= 0.0f) v[i] = 0.0f;  // a NaN stays
+                    }
+                }
+                if (b == NB - 1) {  // this warp is done with the accumulator buffer
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (CG == 1) mbar_arrive(acce_bar(buf));
+                        else t2_arrive_remote(t2_mapa(acce_bar(buf), 0));
+                    }
+                }
+                if (!mine || col0 + 32 * b >= N) continue;
+                const bool f32 = o.type == MNMT_F32;
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    if (h == 1 && !f32) break;
+                    uint8_t *blk = stg + (blocks & 1) * F4_BLK;
+                    if (o.tma) {
+                        if (lane == 0) t2_store_wait_read<1>();  // the store before the last has read this block
+                        __syncwarp();
+                    }
+                    if (!f32) f4_stage16(blk, v, o.type);
+                    else if (h == 0) f4_stage32<0>(blk, v);
+                    else f4_stage32<1>(blk, v);
+                    const int col = col0 + 32 * b + 16 * h;
+                    if (o.tma) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (col < N) t2_store(&tmY, col, row0, stg_s + (blocks & 1) * F4_BLK);
+                            t2_store_commit();
+                        }
+                    } else {
+                        __syncwarp();
+                        f4_store_plain(o, blk, row0, col, M, N);
+                        __syncwarp();
+                    }
+                    blocks++;
+                }
+            }
+        }
+        if (lane == 0) t2_store_wait();
+    }
+
+    // ---- teardown: every MMA and copy has completed before a CTA ends ----
+    __syncthreads();
+    if (warp == 0 && lane == 0 && rank == 0 && *abort_flag)
+        for (uint32_t it = misc[2]; it < issued; it++) mbar_wait(full_bar((int)(it % STAGES)), (it / STAGES) & 1);
+    if (warp == 1) {
+        if (lane == 0) mbar_wait(done_bar, 0);
+        __syncwarp();
+        tc_fence_after();
+    }
+    if constexpr (CG == 2) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    if (warp == 1) {
+        if constexpr (CG == 1) tmem_free<L::COLS>(tbase);
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(L::COLS) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+int g_f4_pairs = 0;  // CTA pairs that fit at once
+
+bool encode(CUtensorMap *tm, CUtensorMapDataType type, const void *p, cuuint64_t w, cuuint64_t h, cuuint64_t stride, cuuint32_t bw, cuuint32_t bh,
+            CUtensorMapSwizzle sw, bool load) {
+    cuuint64_t dims[2] = {w, h}, strides[1] = {stride};
+    cuuint32_t box[2] = {bw, bh}, estr[2] = {1, 1};
+    return tma_encoder()(tm, type, 2, const_cast<void *>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
+                         load ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool encode_codes(CUtensorMap *tm, const Fp4Args &q, int box_rows) {
+    const size_t pitch = fp4_pitch(q.cols);
+    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, q.codes, pitch, q.rows, pitch, 128, box_rows, CU_TENSOR_MAP_SWIZZLE_128B, true);
+}
+// the scale tiles as a matrix of 128 words each
+bool encode_scales(CUtensorMap *tm, const Fp4Args &q, bool nv) {
+    const size_t n = fp4_scale_bytes(q.rows, q.cols, nv) / 512;
+    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT32, q.scales, 128, n, 512, 128, nv ? 4 : 2, CU_TENSOR_MAP_SWIZZLE_NONE, true);
+}
+
+template <int CG, int BN, bool NV>
+cudaLaunchConfig_t f4_config(int units, cudaStream_t st, cudaLaunchAttribute (&attr)[2], bool pdl) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(CG * units));
+    cfg.blockDim = dim3(F4_THREADS);
+    cfg.dynamicSmemBytes = F4Layout<CG, BN, NV>::SMEM;
+    cfg.stream = st;
+    int n = 0;
+    if (CG == 2) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = 2;
+        attr[n].val.clusterDim.y = 1;
+        attr[n++].val.clusterDim.z = 1;
+    }
+    if (pdl) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cfg;
+}
+
+template <int CG, int BN, bool NV>
+cudaError_t f4_init() {
+    cudaError_t err = cudaFuncSetAttribute(fp4_gemm<CG, BN, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F4Layout<CG, BN, NV>::SMEM);
+    if (err != cudaSuccess || CG == 1) return err;
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = f4_config<CG, BN, NV>(64, nullptr, attr, false);
+    int n = 0;
+    err = cudaOccupancyMaxActiveClusters(&n, fp4_gemm<CG, BN, NV>, &cfg);
+    if (err == cudaSuccess && (g_f4_pairs == 0 || n < g_f4_pairs)) g_f4_pairs = n;
+    return err;
+}
+
+template <int CG, int BN, bool NV>
+cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &out, int *status, cudaStream_t st) {
+    const int M = x.rows, N = w.rows, K = x.cols;
+    CUtensorMap ta, tb, tsa, tsb, ty;
+    F4Out o = out;
+    if (!encode_codes(&ta, x, F4_BM) || !encode_codes(&tb, w, BN / CG) || !encode_scales(&tsa, x, NV) || !encode_scales(&tsb, w, NV))
+        return cudaErrorInvalidValue;
+    const int es = o.type == MNMT_F32 ? 4 : 2;
+    const CUtensorMapDataType yt = o.type == MNMT_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : o.type == MNMT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                         : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    o.tma = (reinterpret_cast<uintptr_t>(o.y) & 15) == 0 && o.ldy * es % 16 == 0 &&
+            encode(&ty, yt, o.y, N, M, (cuuint64_t)o.ldy * es, 64 / es, 32, CU_TENSOR_MAP_SWIZZLE_64B, false);
+    if (!o.tma) ty = ta;
+    const long tiles = (long)((M + CG * F4_BM - 1) / (CG * F4_BM)) * ((N + BN - 1) / BN);
+    const long fit = CG == 2 ? g_f4_pairs : device_sm_count();
+    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &cs) != cudaSuccess) cs = cudaStreamCaptureStatusNone;
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = f4_config<CG, BN, NV>((int)(tiles < fit ? tiles : fit), st, attr, cs != cudaStreamCaptureStatusActive);
+    return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV>, ta, tb, tsa, tsb, ty, o, M, N, K, status);
+}
+
+}  // namespace
+
+cudaError_t fp4_init() {
+    cudaError_t err = f4_init<2, 192, false>();
+    if (err == cudaSuccess) err = f4_init<2, 192, true>();
+    if (err == cudaSuccess) err = f4_init<1, 128, false>();
+    if (err == cudaSuccess) err = f4_init<1, 128, true>();
+    if (err == cudaSuccess) err = f4_init<1, 64, false>();
+    if (err == cudaSuccess) err = f4_init<1, 64, true>();
+    return err;
+}
+
+cudaError_t launch_fp4_product(const Fp4Args &x, const Fp4Args &w, bool nv, float alpha, const float *bias, int relu, void *y, int ydtype,
+                               long ldy, int *status, cudaStream_t st) {
+    const F4Out o{y, ldy, ydtype, 0, relu, alpha, bias};
+    auto go = [&](auto n) {
+        constexpr bool NV = decltype(n)::value;
+        const long mt = (x.rows + 127) / 128, sms = device_sm_count();
+        if (mt * ((w.rows + 63) / 64) <= sms) return f4_launch<1, 64, NV>(x, w, o, status, st);
+        if (mt * ((w.rows + 127) / 128) <= sms) return f4_launch<1, 128, NV>(x, w, o, status, st);
+        return f4_launch<2, 192, NV>(x, w, o, status, st);
+    };
+    return nv ? go(std::true_type{}) : go(std::false_type{});
+}
+
+}  // namespace mnmt

@@ -192,6 +192,29 @@ def test_linear(fmt, M, N, K, ty, out, relu, bias, pad):
     assert np.array_equal(host(y2), host(y))
 
 
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M,N,K,out,pad", [(2100, 2500, 320, "bf16", 0), (2100, 2500, 320, "f32", 3), (4096, 1536, 1100, "f16", 0), (385, 9000, 64, "f32", 0),
+                                           (9000, 385, 544, "bf16", 1)])
+def test_linear_of_many_tiles(fmt, M, N, K, out, pad):
+    """Grids of more tiles than SMs: several tiles per CTA, on CTA pairs."""
+    rng = np.random.default_rng(M + N + K)
+    yt, ydt = TYPES[out]
+    wq, w, _ = packed(rng.standard_normal((N, K)).astype(np.float32) * np.float32(0.05), fmt)
+    x = strided(rng.standard_normal((M, K)).astype(np.float32), torch.bfloat16, 0)
+    b = rng.standard_normal(N).astype(np.float32)
+    c, s = buffers(M, K, fmt)
+    y = strided(np.full((M, N), 3.0, np.float32), ydt, pad)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    mnmt.mnmt_fp4_linear(mnmt.Fp4(M, K, FMT[fmt], G[fmt], c, s), wq, x, mnmt.BF16, K, torch.from_numpy(b).cuda(), True, y, yt, N + pad, status)
+    v = P.quantize(host(x), fmt, G[fmt])[2].astype(np.float64)
+    want = np.maximum(v @ w.T + b, 0)
+    mag = np.abs(v) @ np.abs(w).T + np.abs(b)
+    tol = (K / 16 + 16) * 2.0 ** -23 * mag + UNIT[out] * np.abs(want) + (2.0 ** -24 if out == "f16" else 0)
+    assert (np.abs(host(y).astype(np.float64) - want) <= tol).all() and int(status.item()) == 0
+    if pad:
+        assert (host(torch.as_strided(y, (M, N + pad), (N + pad, 1)))[:, N:] == 7.0).all()
+
+
 def gradient_case(fmt, M, N, K, ty, wty, pad, seed=0):
     rng = np.random.default_rng(seed + M + 7 * N + 13 * K)
     x = strided(rng.standard_normal((M, K)).astype(np.float32), TYPES[ty][1], pad)
