@@ -47,7 +47,8 @@ int fp4_ready() {
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return fail(MNMT_ECUDA, "fp4: no usable current device");
     std::lock_guard<std::mutex> lk(mu);
     if (!ready[dev]) {
-        const cudaError_t e = fp4_init();
+        cudaError_t e = fp4_init();
+        if (e == cudaSuccess) e = fp4_backward_init();
         if (e != cudaSuccess) return fail(MNMT_ECUDA, "fp4 kernel set-up failed: %s", cudaGetErrorString(e));
         ready[dev] = true;
     }

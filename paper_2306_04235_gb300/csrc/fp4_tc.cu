@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "fp4.cuh"
+#include "fp4_tile.cuh"
 #include "internal.h"
 #include "mbarrier.cuh"
 #include "tcgen05.cuh"
@@ -30,11 +31,7 @@
 namespace mnmt {
 namespace {
 
-constexpr int F4_BM = 128;
 constexpr int F4_BK = 256;  // codes per k-block: 128 bytes
-constexpr int F4_EPI_WARPS = 8;
-constexpr int F4_THREADS = 64 + F4_EPI_WARPS * 32;
-constexpr int F4_BLK = 2048;  // a staging block: 32 rows of 64 bytes
 
 template <int CG, int BN, bool NV>
 struct F4Layout {
@@ -93,76 +90,6 @@ template <int CG>
 __device__ __forceinline__ void f4_copy_scales(uint32_t taddr, uint64_t desc) {
     if constexpr (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
     else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-}
-
-template <int CG>
-__device__ __forceinline__ void f4_load(uint32_t dst, const CUtensorMap *tm, int x, int y, uint32_t bar) {
-    if constexpr (CG == 1) tma_load_2d(dst, tm, x, y, bar);
-    else t2_load(dst, tm, x, y, bar);
-}
-template <int CG>
-__device__ __forceinline__ void f4_commit(uint32_t bar) {
-    if constexpr (CG == 1) mma_commit(bar);
-    else t2_commit(bar);
-}
-
-__device__ __forceinline__ void f4_epi_sync() { asm volatile("bar.sync 1, %0;" ::"n"(F4_EPI_WARPS * 32) : "memory"); }
-
-struct F4Out {
-    void *y;
-    long ldy;
-    int type;   // MNMT_F32 / BF16 / F16
-    int tma;    // tmY describes y
-    int relu;
-    float alpha;
-    const float *bias;
-};
-
-// 32 outputs of a row, rounded, into staging blocks (row = lane): one of 32
-// 16-bit outputs, or half h of 32 fp32 ones
-__device__ __forceinline__ void f4_stage16(uint8_t *blk, const float (&v)[32], int type) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int c = 0; c < 4; c++) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const float lo = v[8 * c + 2 * i], hi = v[8 * c + 2 * i + 1];
-            if (type == MNMT_BF16) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-                w[i] = *reinterpret_cast<const uint32_t *>(&h);
-            } else {
-                const __half2 h = __floats2half2_rn(lo, hi);
-                w[i] = *reinterpret_cast<const uint32_t *>(&h);
-            }
-        }
-        *reinterpret_cast<uint4 *>(blk + lane * 64 + t2_chunk<64>(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-}
-template <int H>
-__device__ __forceinline__ void f4_stage32(uint8_t *blk, const float (&v)[32]) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int c = 0; c < 4; c++)
-        *reinterpret_cast<float4 *>(blk + lane * 64 + t2_chunk<64>(lane, c)) =
-            make_float4(v[16 * H + 4 * c], v[16 * H + 4 * c + 1], v[16 * H + 4 * c + 2], v[16 * H + 4 * c + 3]);
-}
-
-// a staged block to y where no tensor map describes it: coalesced single elements
-__device__ __forceinline__ void f4_store_plain(const F4Out &o, const uint8_t *blk, int row0, int col0, int M, int N) {
-    const int lane = threadIdx.x & 31;
-    if (o.type == MNMT_F32) {
-        const int c = lane & 15;
-        for (int r = lane >> 4; r < 32; r += 2)
-            if (row0 + r < M && col0 + c < N)
-                static_cast<float *>(o.y)[(row0 + r) * o.ldy + col0 + c] =
-                    *reinterpret_cast<const float *>(blk + r * 64 + t2_chunk<64>(r, c >> 2) + 4 * (c & 3));
-    } else {
-        for (int r = 0; r < 32; r++)
-            if (row0 + r < M && col0 + lane < N)
-                static_cast<uint16_t *>(o.y)[(row0 + r) * o.ldy + col0 + lane] =
-                    *reinterpret_cast<const uint16_t *>(blk + r * 64 + t2_chunk<64>(r, lane >> 3) + 2 * (lane & 7));
-    }
 }
 
 template <int CG, int BN, bool NV>
@@ -315,7 +242,6 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
         constexpr int NB = BN / 64;
         const int ew = warp - 2, q = warp & 3, cw = (BN / 2) * (ew >> 2);
         uint8_t *stg = sm + L::OFF_STG + ew * 2 * F4_BLK;
-        const uint32_t stg_s = s_addr(stg);
         const int ti = ew * 32 + lane;
         uint32_t lt = 0, blocks = 0;  // blocks staged so far: they alternate between the two buffers
         for (long tile = unit; tile < tiles; tile += units, lt++) {
@@ -356,33 +282,7 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
                     }
                 }
                 if (!mine || col0 + 32 * b >= N) continue;
-                const bool f32 = o.type == MNMT_F32;
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    if (h == 1 && !f32) break;
-                    uint8_t *blk = stg + (blocks & 1) * F4_BLK;
-                    if (o.tma) {
-                        if (lane == 0) t2_store_wait_read<1>();  // the store before the last has read this block
-                        __syncwarp();
-                    }
-                    if (!f32) f4_stage16(blk, v, o.type);
-                    else if (h == 0) f4_stage32<0>(blk, v);
-                    else f4_stage32<1>(blk, v);
-                    const int col = col0 + 32 * b + 16 * h;
-                    if (o.tma) {
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (col < N) t2_store(&tmY, col, row0, stg_s + (blocks & 1) * F4_BLK);
-                            t2_store_commit();
-                        }
-                    } else {
-                        __syncwarp();
-                        f4_store_plain(o, blk, row0, col, M, N);
-                        __syncwarp();
-                    }
-                    blocks++;
-                }
+                f4_store_block(o, &tmY, stg, blocks, v, row0, col0 + 32 * b, M, N);
             }
         }
         if (lane == 0) t2_store_wait();
@@ -409,14 +309,6 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
 // ---------------------------------------------------------------------------
 int g_f4_pairs = 0;  // CTA pairs that fit at once
 
-bool encode(CUtensorMap *tm, CUtensorMapDataType type, const void *p, cuuint64_t w, cuuint64_t h, cuuint64_t stride, cuuint32_t bw, cuuint32_t bh,
-            CUtensorMapSwizzle sw, bool load) {
-    cuuint64_t dims[2] = {w, h}, strides[1] = {stride};
-    cuuint32_t box[2] = {bw, bh}, estr[2] = {1, 1};
-    return tma_encoder()(tm, type, 2, const_cast<void *>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
-                         load ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 bool encode_codes(CUtensorMap *tm, const Fp4Args &q, int box_rows) {
     const size_t pitch = fp4_pitch(q.cols);
     return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, q.codes, pitch, q.rows, pitch, 128, box_rows, CU_TENSOR_MAP_SWIZZLE_128B, true);
@@ -428,34 +320,11 @@ bool encode_scales(CUtensorMap *tm, const Fp4Args &q, bool nv) {
 }
 
 template <int CG, int BN, bool NV>
-cudaLaunchConfig_t f4_config(int units, cudaStream_t st, cudaLaunchAttribute (&attr)[2], bool pdl) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(CG * units));
-    cfg.blockDim = dim3(F4_THREADS);
-    cfg.dynamicSmemBytes = F4Layout<CG, BN, NV>::SMEM;
-    cfg.stream = st;
-    int n = 0;
-    if (CG == 2) {
-        attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = 2;
-        attr[n].val.clusterDim.y = 1;
-        attr[n++].val.clusterDim.z = 1;
-    }
-    if (pdl) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n++].val.programmaticStreamSerializationAllowed = 1;
-    }
-    cfg.attrs = attr;
-    cfg.numAttrs = n;
-    return cfg;
-}
-
-template <int CG, int BN, bool NV>
 cudaError_t f4_init() {
     cudaError_t err = cudaFuncSetAttribute(fp4_gemm<CG, BN, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F4Layout<CG, BN, NV>::SMEM);
     if (err != cudaSuccess || CG == 1) return err;
     cudaLaunchAttribute attr[2];
-    cudaLaunchConfig_t cfg = f4_config<CG, BN, NV>(64, nullptr, attr, false);
+    cudaLaunchConfig_t cfg = f4_config(CG, 64, F4Layout<CG, BN, NV>::SMEM, nullptr, attr);
     int n = 0;
     err = cudaOccupancyMaxActiveClusters(&n, fp4_gemm<CG, BN, NV>, &cfg);
     if (err == cudaSuccess && (g_f4_pairs == 0 || n < g_f4_pairs)) g_f4_pairs = n;
@@ -469,19 +338,12 @@ cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &out, int 
     F4Out o = out;
     if (!encode_codes(&ta, x, F4_BM) || !encode_codes(&tb, w, BN / CG) || !encode_scales(&tsa, x, NV) || !encode_scales(&tsb, w, NV))
         return cudaErrorInvalidValue;
-    const int es = o.type == MNMT_F32 ? 4 : 2;
-    const CUtensorMapDataType yt = o.type == MNMT_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                   : o.type == MNMT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
-                                                         : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    o.tma = (reinterpret_cast<uintptr_t>(o.y) & 15) == 0 && o.ldy * es % 16 == 0 &&
-            encode(&ty, yt, o.y, N, M, (cuuint64_t)o.ldy * es, 64 / es, 32, CU_TENSOR_MAP_SWIZZLE_64B, false);
+    encode_out(&ty, o, M, N);
     if (!o.tma) ty = ta;
     const long tiles = (long)((M + CG * F4_BM - 1) / (CG * F4_BM)) * ((N + BN - 1) / BN);
     const long fit = CG == 2 ? g_f4_pairs : device_sm_count();
-    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(st, &cs) != cudaSuccess) cs = cudaStreamCaptureStatusNone;
     cudaLaunchAttribute attr[2];
-    cudaLaunchConfig_t cfg = f4_config<CG, BN, NV>((int)(tiles < fit ? tiles : fit), st, attr, cs != cudaStreamCaptureStatusActive);
+    cudaLaunchConfig_t cfg = f4_config(CG, (int)(tiles < fit ? tiles : fit), F4Layout<CG, BN, NV>::SMEM, st, attr);
     return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV>, ta, tb, tsa, tsb, ty, o, M, N, K, status);
 }
 

@@ -234,6 +234,7 @@ cudaError_t launch_fp4_quantize_backward(const void *x, int dtype, long ldx, con
 cudaError_t launch_fp4_product(const Fp4Args &x, const Fp4Args &w, bool nv, float alpha, const float *bias, int relu,
                                void *y, int ydtype, long ldy, int *status, cudaStream_t st);
 cudaError_t fp4_init();  // set-up of the product kernels on the current device
+cudaError_t fp4_backward_init();
 size_t fp4_backward_workspace(int M, int N, int K);
 
 constexpr int DROPOUT_PARTIALS = MNMT_DROPOUT_WORKSPACE / 8;  // blocks of a backward pass, at most

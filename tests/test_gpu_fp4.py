@@ -268,6 +268,31 @@ def test_linear_backward(fmt, M, N, K, ty, wty, pad):
 
 
 @pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M,N,K,pad", [(3000, 1100, 1300, 0), (700, 5003, 2056, 3), (20000, 520, 264, 8)])
+def test_linear_backward_of_many_tiles(fmt, M, N, K, pad):
+    """Grids of CTA pairs and long sums, against float64."""
+    x, w, g, xq, xv, xin, wq, wv, win = gradient_case(fmt, M, N, K, "bf16", "f32", pad)
+    gx = strided(np.full((M, K), 3.0, np.float32), torch.bfloat16, pad)
+    gw = strided(np.full((N, K), 3.0, np.float32), torch.float32, pad)
+    gb = torch.full((N,), 3.0, device="cuda")
+    ws = torch.empty(mnmt.mnmt_fp4_linear_backward_workspace(M, N, K), dtype=torch.uint8, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    mnmt.mnmt_fp4_linear_backward(xq, wq, g, N + pad, x, mnmt.BF16, K + pad, w, mnmt.F32, K + pad, ws, gx, K + pad, gw, K + pad, gb, status)
+    d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda().double()
+    G64, X64, W64 = g.double(), d(xv), d(wv)
+    for got, want, mag, inside, n, unit in ((gx, G64 @ W64, G64.abs() @ W64.abs(), xin, N, UNIT["bf16"]),
+                                            (gw, G64.t() @ X64, G64.abs().t() @ X64.abs(), win, M, UNIT["f32"])):
+        want = want * d(inside)
+        assert ((got.double() - want).abs() <= (n / 16 + 16) * 2.0 ** -23 * mag + unit * want.abs()).all()
+        rel = ((got.double() - want).norm() / want.norm()).item()
+        assert rel <= unit + n / 16 * 2.0 ** -24
+        if pad:
+            full = torch.as_strided(got, (got.shape[0], K + pad), (K + pad, 1))
+            assert (full[:, K:] == 7.0).all()
+    assert ((gb.double() - G64.sum(0)).abs() <= (M / 16 + 16) * 2.0 ** -23 * G64.abs().sum(0)).all() and int(status.item()) == 0
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
 def test_linear_gradient_by_differences(fmt):
     """The linear is linear in each operand: changing one code by one step changes sum(G y) by the gradient times
     the step (no masks, fp32)."""
