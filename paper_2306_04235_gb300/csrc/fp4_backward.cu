@@ -7,15 +7,15 @@
 // code times its block scale (a power of two, or an E4M3 number) has at most six
 // significant bits and is exact in bf16, products are exact in fp32.
 //
-// fp4_backward_prepare, one pass over the operands (memory): W and X decoded to
-// bf16 in their stored order, column sums of G over 256 rows at a time, and a
-// copy of G where TMA cannot read it (rows not 16-byte aligned).
+// fp4_backward_prepare (memory): W and X decoded to bf16 in their stored order, a
+// copy of G where TMA cannot read it (rows not 16-byte aligned), tickets zeroed.
 // fp4_backward_gemm, both products in one persistent launch (tensor cores): the
 // reduction index is the row of a stored operand, so the MMAs read W, X and (for
 // gW) G "MN-major" from tiles as they lie in memory: no transposed copies.  The
-// epilogue warps sum the bias gradient while the first tile is multiplied,
-// gather the straight-through masks of a tile before its sums are ready, and
-// store through shared memory by TMA.
+// epilogue warps gather the straight-through masks of a tile before its sums are
+// ready and store through shared memory by TMA; two warps sum the bias gradient
+// meanwhile.  Grids of few tiles split the reduction; the parts are added in
+// their order by the CTA that finishes last.
 #include <type_traits>
 
 #include "fp4.cuh"
@@ -25,16 +25,14 @@
 namespace mnmt {
 namespace {
 
-constexpr int GB_ROWS = 256;  // rows of G per partial column sum
-
 struct PrepArgs {
     Fp4Args w, x;
     const __nv_bfloat16 *g;
     long ldg;
     __nv_bfloat16 *w16, *x16, *g16;  // each may be null
-    float *part;                     // [ceil(M / 256)][N], may be null
-    int M, N, K, pk, pn;
-    int bw, bx;                      // blocks of W, of X; the rest take G
+    int *tickets;
+    int n_tickets, M, N, pk, pn;
+    int bw, bx;  // blocks of W, of X; the rest take G
 };
 
 // rows of a packed matrix as bf16 (without the tensor scale); a thread takes 32 elements of a row
@@ -76,35 +74,15 @@ __global__ void __launch_bounds__(256) fp4_backward_prepare(PrepArgs a) {
         decode_rows<NV>(a.x, a.x16, a.pk, (long)(blockIdx.x - a.bw) * 256 + threadIdx.x, (long)a.bx * 256);
         return;
     }
-    // 256 rows x 256 columns of G per block and step: a thread takes eight columns of every eighth row
-    __shared__ float red[8][257];
-    const int strips = fp4_div_up(a.N, 256), chunks = fp4_div_up(a.M, GB_ROWS);
-    const bool vec = (reinterpret_cast<uintptr_t>(a.g) & 15) == 0 && a.ldg % 8 == 0;
-    const int cg = (threadIdx.x & 31) * 8, rr = threadIdx.x >> 5;
-    for (long i = (int)blockIdx.x - a.bw - a.bx; i < (long)strips * chunks; i += (int)gridDim.x - a.bw - a.bx) {
-        const int chunk = (int)(i / strips), c = (int)(i - (long)chunk * strips) * 256 + cg;
-        float s[8] = {};
-        const int r1 = min(a.M, (chunk + 1) * GB_ROWS);
-#pragma unroll 4
-        for (int r = chunk * GB_ROWS + rr; r < r1; r += 8) {
-            if (c >= a.N) break;
-            float v[8];
-            const __nv_bfloat16 *p = a.g + r * a.ldg + c;
-            if (vec && c + 8 <= a.N) load8<__nv_bfloat16, true>(p, 8, v);
-            else load8<__nv_bfloat16, false>(p, a.N - c, v);
-            if (a.g16) store8<__nv_bfloat16, true>(a.g16 + (size_t)r * a.pn + c, 8, v);
-#pragma unroll
-            for (int k = 0; k < 8; k++) s[k] = __fadd_rn(s[k], v[k]);
-        }
-        if (!a.part) continue;
-#pragma unroll
-        for (int k = 0; k < 8; k++) red[rr][cg + k] = s[k];
-        __syncthreads();
-        float t = red[0][threadIdx.x];
-        for (int w = 1; w < 8; w++) t = __fadd_rn(t, red[w][threadIdx.x]);
-        const int n = c - cg + (int)threadIdx.x;
-        if (n < a.N) a.part[(size_t)chunk * a.N + n] = t;
-        __syncthreads();
+    const int first = ((int)blockIdx.x - a.bw - a.bx) * 256 + threadIdx.x, step = ((int)gridDim.x - a.bw - a.bx) * 256;
+    for (int i = first; i < a.n_tickets; i += step) a.tickets[i] = 0;
+    if (!a.g16) return;
+    const int groups = a.pn / 8;
+    for (long i = first; i < (long)a.M * groups; i += step) {
+        const int r = (int)(i / groups), c = (int)(i - (long)r * groups) * 8;
+        float v[8];
+        load8<__nv_bfloat16, false>(a.g + r * a.ldg + c, a.N - c, v);
+        store8<__nv_bfloat16, true>(a.g16 + (size_t)r * a.pn + c, 8, v);
     }
 }
 
@@ -112,6 +90,14 @@ __global__ void __launch_bounds__(256) fp4_backward_prepare(PrepArgs a) {
 // the two products
 // ---------------------------------------------------------------------------
 constexpr int BW_BK = 64;  // reduction indices per stage
+// The tensor core's fp32 accumulator drops bits at every MMA (its relative error
+// grows by about 3e-8 per MMA of 16 terms, always towards zero: 3e-5 measured
+// after 16384 terms).  fp32 results are therefore accumulated there over 1024
+// terms and added up in registers (16384 terms: 5e-7 off); 16-bit results, whose
+// rounding is 2^-9 or 2^-11, are not.
+constexpr int BW_CHUNK = 16;  // stages
+constexpr int BW_GB_WARPS = 2, BW_THREADS = F4_THREADS + 32 * BW_GB_WARPS;
+constexpr int GB_ROWS = 128, GB_COLS = 256;  // rows and columns of G that a warp sums at a time
 
 template <int CG, int BN>
 struct BwLayout {
@@ -133,6 +119,10 @@ struct BwLayout {
 // one of the products: rows x cols outputs, sums over red indices
 struct BwProduct {
     int rows, cols, red, a_mn;  // a_mn: A is stored [red][rows] (gW), else [rows][red]
+    int chunk;                  // stages per accumulator
+    int parts, len;             // parts of the reduction, stages of a part
+    float *partial;             // parts > 1: fp32 sums of each tile and part
+    int *tickets;               // and how many parts of a tile (of each CTA of a pair) are done
     F4Out out;
     // straight-through mask: the float original and the scales of its packed form
     const void *orig;
@@ -142,10 +132,13 @@ struct BwProduct {
 };
 struct BwArgs {
     BwProduct p[2];
-    int n;               // products
-    const float *part;   // partial column sums of G [chunks][N], or null
-    float *gb;
-    int chunks, N;
+    int n;  // products
+    // bias gradient: G, partial column sums [ceil(M / 128)][N], done per 256 columns; gb may be null
+    const __nv_bfloat16 *g;
+    long ldg;
+    float *gb, *gb_part;
+    int *gb_tickets;
+    int M, N;
 };
 
 // MN-major operand tile as TMA leaves it: boxes of 64 (M or N) x 64 (reduction),
@@ -163,7 +156,7 @@ __host__ __device__ constexpr uint32_t bw_idesc(int m, int n, bool a_mn) {
 
 // bit i: element (row, col + i) of the original lies within the range of its block
 template <bool NV>
-MNMT_DEV uint32_t inside32(const BwProduct &p, int row, int col) {
+__device__ __noinline__ uint32_t inside32(const BwProduct &p, int row, int col) {
     if (!p.orig) return 0xFFFFFFFFu;
     const uint8_t *sp = p.q.scales + fp4_scale_at(row, col / fp4_block(NV), fp4_tiles_k(p.cols, NV));
     const float r0 = fp4_scale_of<NV>(sp[0], p.q.g).r, r1 = NV && col + 16 < p.cols ? fp4_scale_of<NV>(sp[1], p.q.g).r : r0;
@@ -188,11 +181,67 @@ MNMT_DEV uint32_t inside32(const BwProduct &p, int row, int col) {
     return m;
 }
 
-// Persistent, 320 threads per CTA: warp 0 lane 0 loads tiles by TMA, warp 1 lane
-// 0 issues MMAs into two TMEM accumulators, warps 2..9 drain them.  Tiles of
-// product 0 come before those of product 1.
+// The bias gradient by warps w of n: 128 rows x 256 columns at a time, eight
+// columns per lane; the warp that finishes the last row block of 256 columns adds
+// the blocks' sums in their order.
+__device__ __noinline__ void bias_gradient(const BwArgs &a, int w, int n) {
+    const int lane = threadIdx.x & 31;
+    const int strips = fp4_div_up(a.N, GB_COLS), blocks = fp4_div_up(a.M, GB_ROWS);
+    const bool vec = (reinterpret_cast<uintptr_t>(a.g) & 15) == 0 && a.ldg % 8 == 0;
+    for (long i = w; i < (long)strips * blocks; i += n) {
+        const int block = (int)(i / strips), strip = (int)(i - (long)block * strips), c = strip * GB_COLS + 8 * lane;
+        const int r1 = min(a.M, (block + 1) * GB_ROWS);
+        float s[8] = {};
+        if (c < a.N) {
+            const __nv_bfloat16 *p = a.g + c;
+            if (vec && c + 8 <= a.N) {
+#pragma unroll 8
+                for (int r = block * GB_ROWS; r < r1; r++) {
+                    float v[8];
+                    load8<__nv_bfloat16, true>(p + r * a.ldg, 8, v);
+#pragma unroll
+                    for (int k = 0; k < 8; k++) s[k] = __fadd_rn(s[k], v[k]);
+                }
+            } else {
+                for (int r = block * GB_ROWS; r < r1; r++) {
+                    float v[8];
+                    load8<__nv_bfloat16, false>(p + r * a.ldg, a.N - c, v);
+#pragma unroll
+                    for (int k = 0; k < 8; k++) s[k] = __fadd_rn(s[k], v[k]);
+                }
+            }
+        }
+        if (blocks > 1) {
+            float *out = a.gb_part + (size_t)block * strips * GB_COLS + c;
+            reinterpret_cast<float4 *>(out)[0] = make_float4(s[0], s[1], s[2], s[3]);
+            reinterpret_cast<float4 *>(out)[1] = make_float4(s[4], s[5], s[6], s[7]);
+            __threadfence();
+            __syncwarp();
+            int old = 0;
+            if (lane == 0) old = atomicAdd(a.gb_tickets + strip, 1);
+            if (__shfl_sync(0xFFFFFFFFu, old, 0) != blocks - 1) continue;
+            __threadfence();
+            const float4 *in = reinterpret_cast<const float4 *>(a.gb_part + c);
+            float4 lo = make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi = lo;
+#pragma unroll 4
+            for (int b = 0; b < blocks; b++) {
+                const float4 x = __ldcg(in + (size_t)b * strips * (GB_COLS / 4)), y = __ldcg(in + (size_t)b * strips * (GB_COLS / 4) + 1);
+                lo.x = __fadd_rn(lo.x, x.x), lo.y = __fadd_rn(lo.y, x.y), lo.z = __fadd_rn(lo.z, x.z), lo.w = __fadd_rn(lo.w, x.w);
+                hi.x = __fadd_rn(hi.x, y.x), hi.y = __fadd_rn(hi.y, y.y), hi.z = __fadd_rn(hi.z, y.z), hi.w = __fadd_rn(hi.w, y.w);
+            }
+            s[0] = lo.x, s[1] = lo.y, s[2] = lo.z, s[3] = lo.w, s[4] = hi.x, s[5] = hi.y, s[6] = hi.z, s[7] = hi.w;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+            if (c + k < a.N) a.gb[c + k] = s[k];
+    }
+}
+
+// Persistent, 384 threads per CTA: warp 0 lane 0 loads tiles by TMA, warp 1 lane
+// 0 issues MMAs into two TMEM accumulators, warps 2..9 drain them, warps 10 and
+// 11 sum the bias gradient.  An item is a part of a tile.
 template <int CG, int BN, bool NV>
-__global__ void __launch_bounds__(F4_THREADS, 1)
+__global__ void __launch_bounds__(BW_THREADS, 1)
     fp4_backward_gemm(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmY0,
                       const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ CUtensorMap tmY1,
                       const __grid_constant__ BwArgs a, int *status) {
@@ -208,7 +257,7 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
     auto accf_bar = [&](int b) { return bars + 8u * (2 * STAGES + b); };
     auto acce_bar = [&](int b) { return bars + 8u * (2 * STAGES + 2 + b); };
     const uint32_t done_bar = bars + 8u * (2 * STAGES + 4);
-    uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);  // [0] tmem base, [1] abort, [2] consumed
+    uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);  // [0] tmem base, [1] abort, [2] consumed, [3] last part
     volatile uint32_t *abort_flag = misc + 1;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -217,18 +266,35 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
     const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
     auto mt = [&](int i) { return (a.p[i].rows + CG * F4_BM - 1) / (CG * F4_BM); };
     auto nt = [&](int i) { return (a.p[i].cols + BN - 1) / BN; };
-    const long t0 = (long)mt(0) * nt(0), tiles = t0 + (a.n > 1 ? (long)mt(1) * nt(1) : 0);
-    // product and corner of a tile: the dimension of fewer tiles runs fastest
-    struct At {
-        int p, m, n;
+    const long n0 = (long)mt(0) * nt(0) * a.p[0].parts, n1 = a.n > 1 ? (long)mt(1) * nt(1) * a.p[1].parts : 0;
+    // A unit (CTA or pair) takes every units-th item of product 0; the units that
+    // then have one item less take as many more of product 1 as fit that item's
+    // time, then all of them take turns.
+    const int heavy = (int)(n0 % units);
+    const long extra = heavy ? (long)(units - heavy) * (a.p[0].len / max(1, a.p[1].len)) : 0;
+    struct Range {
+        long first, step, end;
     };
-    auto at = [&](long t) {
+    auto range = [&](int phase) {
+        if (phase == 0) return Range{unit, units, n0};
+        if (phase == 1) return Range{unit >= heavy ? unit - heavy : n1, units - heavy, extra < n1 ? extra : n1};
+        return Range{extra + (unit >= heavy ? unit - heavy : units - heavy + unit), units, n1};
+    };
+    // tile, part and corner of an item: the dimension of fewer tiles runs fastest
+    struct At {
+        int p, m, n, k0, k1;
+        long tile;
+    };
+    auto at = [&](int phase, long item) {
         At r;
-        r.p = t >= t0;
-        if (r.p) t -= t0;
+        r.p = phase > 0;
+        const BwProduct &p = a.p[r.p];
+        r.tile = item / p.parts;
+        r.k0 = (int)(item - r.tile * p.parts) * p.len;
+        r.k1 = min((p.red + BW_BK - 1) / BW_BK, r.k0 + p.len);
         const int m = mt(r.p), n = nt(r.p);
-        r.m = (int)(m <= n ? t % m : t / n) * CG * F4_BM;
-        r.n = (int)(m <= n ? t / m : t % n) * BN;
+        r.m = (int)(m <= n ? r.tile % m : r.tile / n) * CG * F4_BM;
+        r.n = (int)(m <= n ? r.tile / m : r.tile % n) * BN;
         return r;
     };
 
@@ -267,68 +333,77 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
         uint32_t it = 0;
         bool failed = false;
         const uint32_t ring = s_addr(sm);
-        for (long tile = unit; tile < tiles && !failed && !*abort_flag; tile += units) {
-            const At t = at(tile);
-            const CUtensorMap *ta = t.p ? &tmA1 : &tmA0, *tb = t.p ? &tmB1 : &tmB0;
-            const int m0 = t.m + (int)rank * F4_BM, n0 = t.n + (int)rank * (BN / CG), nkb = (a.p[t.p].red + BW_BK - 1) / BW_BK;
-            const bool a_mn = a.p[t.p].a_mn;
-            for (int kb = 0; kb < nkb; kb++, it++) {
-                const int s = (int)(it % STAGES);
-                if (it >= STAGES && !mbar_wait(empty_bar(s), (it / STAGES - 1) & 1)) {
-                    *abort_flag = 1;
-                    set_status(status, MNMT_ETIMEOUT);
-                    failed = true;
-                    break;
-                }
-                if (rank == 0) mbar_expect_tx(full_bar(s), CG * L::STAGE);
-                const uint32_t bar = CG == 1 ? full_bar(s) : t2_mapa(full_bar(s), 0), base = ring + s * L::STAGE;
-                if (a_mn) {
-                    f4_load<CG>(base, ta, m0, kb * BW_BK, bar);
-                    f4_load<CG>(base + 8192, ta, m0 + 64, kb * BW_BK, bar);
-                } else {
-                    f4_load<CG>(base, ta, kb * BW_BK, m0, bar);
-                }
+        for (int phase = 0; phase < 3; phase++) {
+            const Range r = range(phase);
+            for (long item = r.first; item < r.end && !failed && !*abort_flag; item += r.step) {
+                const At t = at(phase, item);
+                const CUtensorMap *ta = t.p ? &tmA1 : &tmA0, *tb = t.p ? &tmB1 : &tmB0;
+                const int m0 = t.m + (int)rank * F4_BM, n0 = t.n + (int)rank * (BN / CG);
+                const bool a_mn = a.p[t.p].a_mn;
+                for (int kb = t.k0; kb < t.k1; kb++, it++) {
+                    const int s = (int)(it % STAGES);
+                    if (it >= STAGES && !mbar_wait(empty_bar(s), (it / STAGES - 1) & 1)) {
+                        *abort_flag = 1;
+                        set_status(status, MNMT_ETIMEOUT);
+                        failed = true;
+                        break;
+                    }
+                    if (rank == 0) mbar_expect_tx(full_bar(s), CG * L::STAGE);
+                    const uint32_t bar = CG == 1 ? full_bar(s) : t2_mapa(full_bar(s), 0), base = ring + s * L::STAGE;
+                    if (a_mn) {
+                        f4_load<CG>(base, ta, m0, kb * BW_BK, bar);
+                        f4_load<CG>(base + 8192, ta, m0 + 64, kb * BW_BK, bar);
+                    } else {
+                        f4_load<CG>(base, ta, kb * BW_BK, m0, bar);
+                    }
 #pragma unroll
-                for (int j = 0; j < BOXES; j++) f4_load<CG>(base + L::A_BYTES + j * 8192, tb, n0 + 64 * j, kb * BW_BK, bar);
-                issued = it + 1;
+                    for (int j = 0; j < BOXES; j++) f4_load<CG>(base + L::A_BYTES + j * 8192, tb, n0 + 64 * j, kb * BW_BK, bar);
+                    issued = it + 1;
+                }
             }
         }
     } else if (warp == 1 && lane == 0 && rank == 0) {
         // ---- MMA issuer ----
-        uint32_t it = 0, lt = 0;
+        uint32_t it = 0, lt = 0;  // k-blocks and accumulators so far
         bool failed = false;
         const uint32_t ring = s_addr(sm);
         const uint64_t b_desc = mn128_desc(ring + L::A_BYTES);
-        for (long tile = unit; tile < tiles && !failed; tile += units, lt++) {
-            const int buf = (int)(lt & 1), p = tile >= t0;
-            if (lt >= 2 && !mbar_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
-                failed = true;
-                break;
-            }
-            tc_fence_after();
-            const uint32_t d = tbase + (uint32_t)(buf * BN);
-            const bool a_mn = a.p[p].a_mn;
+        for (int phase = 0; phase < 3; phase++) {
+            const Range r = range(phase);
+            const bool a_mn = a.p[phase > 0].a_mn;
             const uint64_t a_desc = a_mn ? mn128_desc(ring) : sw128_desc(ring);
             const uint64_t a_step = a_mn ? 2048 >> 4 : 32 >> 4;  // 16 reduction indices
             const uint32_t idesc = bw_idesc(CG * F4_BM, BN, a_mn);
-            const int nkb = (a.p[p].red + BW_BK - 1) / BW_BK;
-            for (int kb = 0; kb < nkb; kb++, it++) {
-                const int s = (int)(it % STAGES);
-                if (!mbar_wait(full_bar(s), (it / STAGES) & 1)) {
-                    failed = true;
-                    break;
-                }
-                tc_fence_after();
-                const uint64_t off = (uint64_t)((s * L::STAGE) >> 4);
+            const int chunk = a.p[phase > 0].chunk;
+            for (long item = r.first; item < r.end && !failed; item += r.step) {
+                const At t = at(phase, item);
+                for (int k0 = t.k0; k0 < t.k1 && !failed; k0 += chunk, lt++) {
+                    const int buf = (int)(lt & 1), k1 = min(t.k1, k0 + chunk);
+                    if (lt >= 2 && !mbar_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
+                        failed = true;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t d = tbase + (uint32_t)(buf * BN);
+                    for (int kb = k0; kb < k1; kb++, it++) {
+                        const int s = (int)(it % STAGES);
+                        if (!mbar_wait(full_bar(s), (it / STAGES) & 1)) {
+                            failed = true;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint64_t off = (uint64_t)((s * L::STAGE) >> 4);
 #pragma unroll
-                for (int k = 0; k < BW_BK / 16; k++) {
-                    const uint64_t ad = a_desc + off + a_step * k, bd = b_desc + off + (uint64_t)(k * (2048 >> 4));
-                    if constexpr (CG == 1) mma_f16(d, ad, bd, idesc, (uint32_t)(kb | k));
-                    else t2_mma(d, ad, bd, idesc, (uint32_t)(kb | k));
+                        for (int k = 0; k < BW_BK / 16; k++) {
+                            const uint64_t ad = a_desc + off + a_step * k, bd = b_desc + off + (uint64_t)(k * (2048 >> 4));
+                            if constexpr (CG == 1) mma_f16(d, ad, bd, idesc, (uint32_t)((kb - k0) | k));
+                            else t2_mma(d, ad, bd, idesc, (uint32_t)((kb - k0) | k));
+                        }
+                        f4_commit<CG>(empty_bar(s));
+                    }
+                    if (!failed) f4_commit<CG>(accf_bar(buf));
                 }
-                f4_commit<CG>(empty_bar(s));
             }
-            if (!failed) f4_commit<CG>(accf_bar(buf));
         }
         if (failed) {
             *abort_flag = 1;
@@ -339,48 +414,49 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
         f4_commit<CG>(done_bar);
     } else if (warp == 1 && lane == 0) {
         pdl_allow_next();  // the leader's trigger decides
+    } else if (warp >= 2 + F4_EPI_WARPS) {
+        if (a.gb) bias_gradient(a, (int)blockIdx.x * BW_GB_WARPS + warp - 2 - F4_EPI_WARPS, (int)gridDim.x * BW_GB_WARPS);
     } else if (warp >= 2) {
         // ---- epilogue ----
         constexpr int NB = BN / 64;
         const int ew = warp - 2, q = warp & 3, cw = (BN / 2) * (ew >> 2);
-        if (a.gb)  // the bias gradient, always in the same order
-            for (long n = (long)blockIdx.x * F4_EPI_WARPS * 32 + ew * 32 + lane; n < a.N; n += (long)gridDim.x * F4_EPI_WARPS * 32) {
-                float s = 0.0f;
-#pragma unroll 8
-                for (int c = 0; c < a.chunks; c++) s = __fadd_rn(s, a.part[(size_t)c * a.N + n]);
-                a.gb[n] = s;
-            }
         uint8_t *stg = sm + L::OFF_STG + ew * 2 * F4_BLK;
         uint32_t lt = 0, blocks = 0;
-        for (long tile = unit; tile < tiles; tile += units, lt++) {
-            const int buf = (int)(lt & 1);
-            const At t = at(tile);
-            const BwProduct &p = a.p[t.p];
-            const CUtensorMap *ty = t.p ? &tmY1 : &tmY0;
-            const int row0 = t.m + (int)rank * F4_BM + 32 * q, col0 = t.n + cw;
-            uint32_t in[NB];
+        for (int phase = 0; phase < 3; phase++) {
+            const Range rg = range(phase);
+            const BwProduct &p = a.p[phase > 0];
+            const CUtensorMap *ty = phase ? &tmY1 : &tmY0;
+            for (long item = rg.first; item < rg.end; item += rg.step) {
+                const At t = at(phase, item);
+                const int row0 = t.m + (int)rank * F4_BM + 32 * q, col0 = t.n + cw;
+                uint32_t in[NB];
 #pragma unroll
-            for (int b = 0; b < NB; b++) in[b] = row0 + lane < p.rows && col0 + 32 * b < p.cols ? inside32<NV>(p, row0 + lane, col0 + 32 * b) : 0;
-            bool ok = *abort_flag == 0 && mbar_wait(accf_bar(buf), (lt >> 1) & 1);
-            if (!ok && *abort_flag == 0) {
-                *abort_flag = 1;
-                set_status(status, MNMT_ETIMEOUT);
-            }
-            tc_fence_after();
-            ok = __all_sync(0xFFFFFFFFu, ok && *abort_flag == 0);
-            const uint32_t taddr = tbase + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * BN + cw);
-            const bool mine = ok && row0 < p.rows;
+                for (int b = 0; b < NB; b++) in[b] = row0 + lane < p.rows && col0 + 32 * b < p.cols ? inside32<NV>(p, row0 + lane, col0 + 32 * b) : 0;
+                float acc[NB][32];
 #pragma unroll
-            for (int b = 0; b < NB; b++) {
-                float v[32];
-                if (mine && col0 + 32 * b < p.cols) {
-                    uint32_t r[32];
-                    tmem_ld32(taddr + 32 * b, r);
-                    tmem_wait_ld();
+                for (int b = 0; b < NB; b++)
 #pragma unroll
-                    for (int i = 0; i < 32; i++) v[i] = (in[b] >> i) & 1u ? __fmul_rn(__uint_as_float(r[i]), p.out.alpha) : 0.0f;
-                }
-                if (b == NB - 1) {
+                    for (int i = 0; i < 32; i++) acc[b][i] = 0.0f;
+                bool ok = true;
+                for (int k0 = t.k0; k0 < t.k1; k0 += p.chunk, lt++) {
+                    const int buf = (int)(lt & 1);
+                    ok = *abort_flag == 0 && mbar_wait(accf_bar(buf), (lt >> 1) & 1);
+                    if (!ok && *abort_flag == 0) {
+                        *abort_flag = 1;
+                        set_status(status, MNMT_ETIMEOUT);
+                    }
+                    tc_fence_after();
+                    ok = __all_sync(0xFFFFFFFFu, ok && *abort_flag == 0);
+                    const uint32_t taddr = tbase + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * BN + cw);
+#pragma unroll
+                    for (int b = 0; b < NB; b++) {
+                        if (!ok || row0 >= p.rows) break;
+                        uint32_t r[32];
+                        tmem_ld32(taddr + 32 * b, r);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; i++) acc[b][i] = __fadd_rn(acc[b][i], __uint_as_float(r[i]));
+                    }
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) {
@@ -388,7 +464,49 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
                         else t2_arrive_remote(t2_mapa(acce_bar(buf), 0));
                     }
                 }
-                if (mine && col0 + 32 * b < p.cols) f4_store_block(p.out, ty, stg, blocks, v, row0, col0 + 32 * b, p.rows, p.cols);
+                bool store = ok && row0 < p.rows;
+                if (p.parts > 1) {
+                    // this part's sums to memory, 16 bytes per lane; the last part to finish adds all of them in order
+                    const size_t unit_f = (size_t)F4_BM * BN, at_f = ((size_t)ew * NB * 8 * 32 + lane) * 4;
+                    float *tile = p.partial + ((size_t)t.tile * CG + rank) * p.parts * unit_f;
+                    if (store) {
+                        float4 *o = reinterpret_cast<float4 *>(tile + (size_t)(t.k0 / p.len) * unit_f + at_f);
+#pragma unroll
+                        for (int b = 0; b < NB; b++)
+#pragma unroll
+                            for (int g = 0; g < 8; g++) o[(b * 8 + g) * 32] = make_float4(acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]);
+                    }
+                    __threadfence();
+                    f4_epi_sync();
+                    if (ew == 0 && lane == 0) misc[3] = *abort_flag == 0 && atomicAdd(p.tickets + t.tile * CG + rank, 1) == p.parts - 1;
+                    f4_epi_sync();
+                    store = store && misc[3];
+                    if (store) {
+                        __threadfence();
+#pragma unroll
+                        for (int b = 0; b < NB; b++)
+#pragma unroll
+                            for (int i = 0; i < 32; i++) acc[b][i] = 0.0f;
+                        const float4 *in4 = reinterpret_cast<const float4 *>(tile + at_f);
+                        for (int s = 0; s < p.parts; s++, in4 += unit_f / 4) {
+#pragma unroll
+                            for (int b = 0; b < NB; b++)
+#pragma unroll
+                                for (int g = 0; g < 8; g++) {
+                                    const float4 v = __ldcg(in4 + (b * 8 + g) * 32);
+                                    acc[b][4 * g] = __fadd_rn(acc[b][4 * g], v.x), acc[b][4 * g + 1] = __fadd_rn(acc[b][4 * g + 1], v.y);
+                                    acc[b][4 * g + 2] = __fadd_rn(acc[b][4 * g + 2], v.z), acc[b][4 * g + 3] = __fadd_rn(acc[b][4 * g + 3], v.w);
+                                }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int b = 0; b < NB; b++) {
+                    if (!store || col0 + 32 * b >= p.cols) continue;
+#pragma unroll
+                    for (int i = 0; i < 32; i++) acc[b][i] = (in[b] >> i) & 1u ? __fmul_rn(acc[b][i], p.out.alpha) : 0.0f;
+                    f4_store_block(p.out, ty, stg, blocks, acc[b], row0, col0 + 32 * b, p.rows, p.cols);
+                }
             }
         }
         if (lane == 0) t2_store_wait();
@@ -427,38 +545,89 @@ cudaError_t bw_init() {
     cudaError_t err = cudaFuncSetAttribute(fp4_backward_gemm<CG, BN, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)BwLayout<CG, BN>::SMEM);
     if (err != cudaSuccess || CG == 1) return err;
     cudaLaunchAttribute attr[2];
-    cudaLaunchConfig_t cfg = f4_config(CG, 64, BwLayout<CG, BN>::SMEM, nullptr, attr);
+    cudaLaunchConfig_t cfg = f4_config(CG, 64, BW_THREADS, BwLayout<CG, BN>::SMEM, nullptr, attr);
     int n = 0;
     err = cudaOccupancyMaxActiveClusters(&n, fp4_backward_gemm<CG, BN, NV>, &cfg);
     if (err == cudaSuccess && (g_bw_pairs == 0 || n < g_bw_pairs)) g_bw_pairs = n;
     return err;
 }
 
-template <int CG, int BN, bool NV>
-cudaError_t bw_launch(const CUtensorMap (&tm)[6], const BwArgs &a, int *status, cudaStream_t st) {
-    long tiles = 0;
-    for (int i = 0; i < a.n; i++) tiles += (long)fp4_div_up(a.p[i].rows, CG * F4_BM) * fp4_div_up(a.p[i].cols, BN);
-    if (tiles == 0) tiles = 1;  // the bias gradient alone
-    const long fit = CG == 2 ? g_bw_pairs : device_sm_count();
-    cudaLaunchAttribute attr[2];
-    cudaLaunchConfig_t cfg = f4_config(CG, (int)(tiles < fit ? tiles : fit), BwLayout<CG, BN>::SMEM, st, attr);
-    return cudaLaunchKernelEx(&cfg, fp4_backward_gemm<CG, BN, NV>, tm[0], tm[1], tm[2], tm[3], tm[4], tm[5], a, status);
+// Tiles and parts of the two products (index 0: gX, 1: gW), by sizes alone (the
+// workspace's size is asked for before any device is set up): for 152 SMs.
+struct Plan {
+    bool pair;
+    int units;
+    int parts[2], len[2];  // of the reduction; stages of a part
+    long tiles[2], items;
+};
+Plan plan(int M, int N, int K, bool gx, bool gw) {
+    Plan best = {};
+    const int rows[2] = {M, N}, red[2] = {N, M};
+    const bool want[2] = {gx, gw};
+    for (int pair = 1; pair >= 0; pair--) {
+        Plan p = {};
+        p.pair = pair;
+        p.units = pair ? 76 : 152;
+        const int least = pair ? 8 : 4;  // stages of a part, at least
+        double work = 0.0;
+        for (int i = 0; i < 2; i++) {
+            if (!want[i]) continue;
+            p.tiles[i] = (long)fp4_div_up(rows[i], pair ? 2 * F4_BM : F4_BM) * fp4_div_up(K, pair ? 256 : 64);
+            work += (double)p.tiles[i] * fp4_div_up(red[i], BW_BK);
+        }
+        const double share = work / p.units;  // stages of a unit
+        for (int i = 0; i < 2; i++) {
+            const int nkb = fp4_div_up(red[i], BW_BK);
+            // parts of about a unit's share; whole reductions where there is a tile for every unit
+            int parts = want[i] && p.tiles[0] + p.tiles[1] < p.units ? (int)(nkb / (share > least ? share : least) + 0.5) : 1;
+            if (parts > 64) parts = 64;
+            if (parts < 1) parts = 1;
+            p.len[i] = fp4_div_up(nkb, parts);
+            p.parts[i] = fp4_div_up(nkb, p.len[i]);
+            p.items += p.tiles[i] * p.parts[i];
+        }
+        best = p;
+        if (pair && share >= 12) break;
+    }
+    return best;
+}
+size_t partial_bytes(const Plan &p, int i) {
+    return p.parts[i] > 1 ? (size_t)p.tiles[i] * p.parts[i] * (p.pair ? 2 * F4_BM * 256 : F4_BM * 64) * 4 : 0;
 }
 
-// scratch: W and X in bf16, a copy of G, partial column sums
+// scratch: W and X in bf16, a copy of G, sums of the bias gradient, of split tiles, tickets
 struct Scratch {
-    size_t w, x, g, part, bytes;
-    int pk, pn;
+    size_t w, x, g, gb, partial, tickets, bytes;
+    int pk, pn, strips;
 };
 Scratch scratch(int M, int N, int K) {
     Scratch s;
-    s.pk = up8(K), s.pn = up8(N);
+    s.pk = up8(K), s.pn = up8(N), s.strips = fp4_div_up(N, GB_COLS);
     s.w = 0;
     s.x = up16((size_t)N * s.pk * 2);
     s.g = s.x + up16((size_t)M * s.pk * 2);
-    s.part = s.g + up16((size_t)M * s.pn * 2);
-    s.bytes = s.part + up16((size_t)fp4_div_up(M, GB_ROWS) * N * 4) + 16;
+    s.gb = s.g + up16((size_t)M * s.pn * 2);
+    s.partial = s.gb + (size_t)fp4_div_up(M, GB_ROWS) * s.strips * GB_COLS * 4;
+    size_t most = 0;
+    for (int w = 1; w < 4; w++) {
+        const Plan p = plan(M, N, K, w & 1, w & 2);
+        const size_t n = partial_bytes(p, 0) + partial_bytes(p, 1);
+        if (n > most) most = n;
+    }
+    s.tickets = s.partial + most;
+    s.bytes = s.tickets + up16((size_t)(s.strips + 4 * 2 * 152) * 4) + 16;
     return s;
+}
+
+template <int CG, int BN, bool NV>
+cudaError_t bw_launch(const CUtensorMap (&tm)[6], const BwArgs &a, long items, int *status, cudaStream_t st) {
+    const long fit = CG == 2 ? g_bw_pairs : device_sm_count();
+    // the bias gradient's warps take the whole GPU where the products do not
+    const long gb = a.gb ? ((long)fp4_div_up(a.N, GB_COLS) * fp4_div_up(a.M, GB_ROWS) + CG * BW_GB_WARPS - 1) / (CG * BW_GB_WARPS) : 0;
+    if (items < gb) items = gb;
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = f4_config(CG, (int)(items < fit ? items : fit), BW_THREADS, BwLayout<CG, BN>::SMEM, st, attr);
+    return cudaLaunchKernelEx(&cfg, fp4_backward_gemm<CG, BN, NV>, tm[0], tm[1], tm[2], tm[3], tm[4], tm[5], a, status);
 }
 
 }  // namespace
@@ -484,7 +653,9 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
     }
     if (!b.gx && !b.gw && !b.gb) return cudaSuccess;
     const Scratch s = scratch(M, N, K);
+    const Plan pl = plan(M, N, K, b.gx, b.gw);
     uint8_t *ws = static_cast<uint8_t *>(b.workspace);
+    int *tickets = reinterpret_cast<int *>(ws + s.tickets);
     const bool products = b.gx || b.gw;
     const bool copy = products && ((reinterpret_cast<uintptr_t>(b.g) & 15) || b.ldg % 8);
     PrepArgs p;
@@ -493,48 +664,52 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
     p.w16 = b.gx ? reinterpret_cast<__nv_bfloat16 *>(ws + s.w) : nullptr;
     p.x16 = b.gw ? reinterpret_cast<__nv_bfloat16 *>(ws + s.x) : nullptr;
     p.g16 = copy ? reinterpret_cast<__nv_bfloat16 *>(ws + s.g) : nullptr;
-    p.part = b.gb ? reinterpret_cast<float *>(ws + s.part) : nullptr;
-    p.M = M, p.N = N, p.K = K, p.pk = s.pk, p.pn = s.pn;
-    // blocks in proportion to the bytes each part moves, eight per SM at most
-    const long groups = fp4_div_up(K, 32), strips = (long)fp4_div_up(N, 256) * fp4_div_up(M, GB_ROWS), cap = 4L * device_sm_count();
-    auto part = [&](long blocks) { return (int)(blocks < cap ? blocks : cap); };
-    p.bw = p.w16 ? part((N * groups + 255) / 256) : 0;
-    p.bx = p.x16 ? part((M * groups + 255) / 256) : 0;
-    const int bg = p.g16 || p.part ? part(strips) : 0;
-    launch_pdl(b.nv ? fp4_backward_prepare<true> : fp4_backward_prepare<false>, p.bw + p.bx + bg, 256, 0, st, p);
-    if ((err = cudaGetLastError()) != cudaSuccess) return err;
+    p.tickets = tickets, p.n_tickets = s.strips;
+    p.M = M, p.N = N, p.pk = s.pk, p.pn = s.pn;
 
     BwArgs a;
-    a.n = 0;
-    a.part = p.part, a.gb = b.gb, a.chunks = fp4_div_up(M, GB_ROWS), a.N = N;
+    memset(&a, 0, sizeof(a));
+    a.M = M, a.N = N;
+    a.g = copy ? p.g16 : p.g, a.ldg = copy ? s.pn : b.ldg;
+    a.gb = b.gb, a.gb_part = reinterpret_cast<float *>(ws + s.gb), a.gb_tickets = tickets;
+    a.p[0].parts = a.p[1].parts = 1;
     CUtensorMap tm[6];
     memset(tm, 0, sizeof(tm));
-    const void *g = copy ? static_cast<const void *>(p.g16) : b.g;
-    const long ldg = copy ? s.pn : b.ldg;
-    long blocks64 = 0, pairs = 0;
-    auto add = [&](bool input) {
+    float *partial = reinterpret_cast<float *>(ws + s.partial);
+    // the longer part first
+    const bool input_first = pl.len[0] >= pl.len[1];
+    for (int i = 0; i < 2; i++) {
+        const bool input = (i == 0) == input_first;
+        if (input ? !b.gx : !b.gw) continue;
         BwProduct &r = a.p[a.n];
+        CUtensorMap *t = tm + 3 * a.n;
+        a.n++;
         r.rows = input ? M : N, r.cols = K, r.red = input ? N : M, r.a_mn = !input;
         r.out = input ? F4Out{b.gx, b.ldgx, b.xdtype, 0, 0, b.nv ? b.w.g : 1.0f, nullptr} : F4Out{b.gw, b.ldgw, MNMT_F32, 0, 0, b.nv ? b.x.g : 1.0f, nullptr};
         r.orig = input ? b.xo : b.wo, r.ldo = input ? b.ldx : b.ldw, r.otype = input ? b.xdtype : b.wdtype;
         r.q = input ? b.x : b.w;
-        CUtensorMap *t = tm + 3 * a.n;
+        r.chunk = r.out.type == MNMT_F32 ? BW_CHUNK : 1 << 24;
+        r.parts = pl.parts[!input], r.len = pl.len[!input];
+        if (r.parts > 1) {
+            r.partial = partial;
+            partial += partial_bytes(pl, !input) / 4;
+            r.tickets = tickets + p.n_tickets;
+            p.n_tickets += (int)pl.tiles[!input] * (pl.pair ? 2 : 1);
+        }
         encode_out(t + 2, r.out, r.rows, r.cols);
-        blocks64 += (long)fp4_div_up(r.rows, F4_BM) * fp4_div_up(K, 64);
-        pairs += (long)fp4_div_up(r.rows, 2 * F4_BM) * fp4_div_up(K, 256);
-        a.n++;
-        return encode_bf16(t, g, N, M, ldg, input ? F4_BM : 64) && encode_bf16(t + 1, input ? p.w16 : p.x16, K, input ? N : M, s.pk, 64);
-    };
-    // the longer reduction first: its tiles take longest
-    const bool input_first = N >= M;
-    for (int i = 0; i < 2; i++) {
-        const bool input = (i == 0) == input_first;
-        if ((input ? b.gx != nullptr : b.gw != nullptr) && !add(input)) return cudaErrorInvalidValue;
+        if (!encode_bf16(t, a.g, N, M, a.ldg, input ? F4_BM : 64) || !encode_bf16(t + 1, input ? p.w16 : p.x16, K, input ? N : M, s.pk, 64))
+            return cudaErrorInvalidValue;
     }
-    if (a.n == 0) a.p[0] = BwProduct{};
-    const bool small = blocks64 <= 2L * device_sm_count();
-    if (small) return b.nv ? bw_launch<1, 64, true>(tm, a, b.status, st) : bw_launch<1, 64, false>(tm, a, b.status, st);
-    return b.nv ? bw_launch<2, 256, true>(tm, a, b.status, st) : bw_launch<2, 256, false>(tm, a, b.status, st);
+
+    // blocks in proportion to the bytes each part moves, four per SM of each at most
+    const long groups = fp4_div_up(K, 32), cap = 4L * device_sm_count();
+    auto blocks = [&](long threads) { return (int)((threads + 255) / 256 < cap ? (threads + 255) / 256 : cap); };
+    p.bw = p.w16 ? blocks(N * groups) : 0;
+    p.bx = p.x16 ? blocks(M * groups) : 0;
+    launch_pdl(b.nv ? fp4_backward_prepare<true> : fp4_backward_prepare<false>, p.bw + p.bx + (copy ? blocks((long)M * s.pn / 8) : 1), 256, 0, st, p);
+    if ((err = cudaGetLastError()) != cudaSuccess) return err;
+    if (pl.pair) return b.nv ? bw_launch<2, 256, true>(tm, a, pl.items, b.status, st) : bw_launch<2, 256, false>(tm, a, pl.items, b.status, st);
+    return b.nv ? bw_launch<1, 64, true>(tm, a, pl.items, b.status, st) : bw_launch<1, 64, false>(tm, a, pl.items, b.status, st);
 }
 
 }  // namespace mnmt

@@ -324,7 +324,7 @@ cudaError_t f4_init() {
     cudaError_t err = cudaFuncSetAttribute(fp4_gemm<CG, BN, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F4Layout<CG, BN, NV>::SMEM);
     if (err != cudaSuccess || CG == 1) return err;
     cudaLaunchAttribute attr[2];
-    cudaLaunchConfig_t cfg = f4_config(CG, 64, F4Layout<CG, BN, NV>::SMEM, nullptr, attr);
+    cudaLaunchConfig_t cfg = f4_config(CG, 64, F4_THREADS, F4Layout<CG, BN, NV>::SMEM, nullptr, attr);
     int n = 0;
     err = cudaOccupancyMaxActiveClusters(&n, fp4_gemm<CG, BN, NV>, &cfg);
     if (err == cudaSuccess && (g_f4_pairs == 0 || n < g_f4_pairs)) g_f4_pairs = n;
@@ -343,7 +343,7 @@ cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &out, int 
     const long tiles = (long)((M + CG * F4_BM - 1) / (CG * F4_BM)) * ((N + BN - 1) / BN);
     const long fit = CG == 2 ? g_f4_pairs : device_sm_count();
     cudaLaunchAttribute attr[2];
-    cudaLaunchConfig_t cfg = f4_config(CG, (int)(tiles < fit ? tiles : fit), F4Layout<CG, BN, NV>::SMEM, st, attr);
+    cudaLaunchConfig_t cfg = f4_config(CG, (int)(tiles < fit ? tiles : fit), F4_THREADS, F4Layout<CG, BN, NV>::SMEM, st, attr);
     return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV>, ta, tb, tsa, tsb, ty, o, M, N, K, status);
 }
 

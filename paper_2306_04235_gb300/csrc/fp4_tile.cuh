@@ -138,10 +138,10 @@ inline void encode_out(CUtensorMap *tm, F4Out &o, int M, int N) {
 }
 
 // cluster and launch attributes of a tile kernel (programmatic launch outside stream captures, as launch_pdl)
-inline cudaLaunchConfig_t f4_config(int cg, int units, size_t smem, cudaStream_t st, cudaLaunchAttribute (&attr)[2]) {
+inline cudaLaunchConfig_t f4_config(int cg, int units, int threads, size_t smem, cudaStream_t st, cudaLaunchAttribute (&attr)[2]) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(cg * units));
-    cfg.blockDim = dim3(F4_THREADS);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     int n = 0;
