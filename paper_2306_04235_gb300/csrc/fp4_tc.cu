@@ -70,13 +70,15 @@ __device__ __forceinline__ uint64_t f4_scale_desc(uint32_t saddr) {
 }
 
 template <int CG, bool NV>
-__device__ __forceinline__ void f4_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+__device__ __forceinline__ void f4_mma_on(uint32_t on, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                          uint32_t accumulate) {
 #define F4_MMA(G, KIND)                                                                                            \
     asm volatile(                                                                                                  \
-        "{\n\t.reg .pred p;\n\t"                                                                                   \
+        "{\n\t.reg .pred p, q;\n\t"                                                                                \
         "setp.ne.b32 p, %4, 0;\n\t"                                                                                \
-        "tcgen05.mma.cta_group::" G ".kind::" KIND " [%0], %1, %2, %3, [%5], [%6], p;\n\t}" ::"r"(d),              \
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)                                            \
+        "setp.ne.b32 q, %7, 0;\n\t"                                                                                \
+        "@q tcgen05.mma.cta_group::" G ".kind::" KIND " [%0], %1, %2, %3, [%5], [%6], p;\n\t}" ::"r"(d),           \
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb), "r"(on)                                   \
         : "memory")
     if constexpr (CG == 1 && NV) F4_MMA("1", "mxf4nvf4.block_scale.scale_vec::4X");
     else if constexpr (CG == 1) F4_MMA("1", "mxf4.block_scale.scale_vec::2X");
@@ -87,9 +89,15 @@ __device__ __forceinline__ void f4_mma(uint32_t d, uint64_t a, uint64_t b, uint3
 
 // scale tile -> four TMEM columns, repeated in the four lane quarters (of both CTAs of a pair)
 template <int CG>
-__device__ __forceinline__ void f4_copy_scales(uint32_t taddr, uint64_t desc) {
-    if constexpr (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+__device__ __forceinline__ void f4_copy_scales_on(uint32_t on, uint32_t taddr, uint64_t desc) {
+    if constexpr (CG == 1)
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr),
+                     "l"(desc), "r"(on)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr),
+                     "l"(desc), "r"(on)
+                     : "memory");
 }
 
 template <int CG, int BN, bool NV>
@@ -112,7 +120,7 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
     uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);  // [0] tmem base, [1] abort, [2] consumed
     volatile uint32_t *abort_flag = misc + 1;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     uint32_t rank = 0;
     if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
@@ -155,55 +163,57 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
     const uint32_t tbase = misc[0];
 
     uint32_t issued = 0;
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         // ---- TMA producer: this CTA's rows of all its tiles ----
-        uint32_t it = 0;
+        const uint32_t on = elect_one();
+        uint32_t s = 0, phase = 1;  // slot, and the parity its release completes
         bool failed = false;
-        const uint32_t ring = s_addr(sm);
+        const uint32_t ring = s_addr(sm), lead = CG == 1 ? bars : t2_mapa(bars, 0);
         for (long tile = unit; tile < tiles && !failed && !*abort_flag; tile += units) {
             const int m0 = tile_m(tile) + (int)rank * F4_BM, nb = tile_n(tile), n0 = nb + (int)rank * (BN / CG);
-            for (int kb = 0; kb < nkb; kb++, it++) {
-                const int s = (int)(it % STAGES);
-                if (it >= STAGES && !mbar_wait(empty_bar(s), (it / STAGES - 1) & 1)) {
+            // scale tiles of the rows' tile rows (tiles past the row's end belong
+            // to k-steps that are not issued)
+            int sa = (m0 >> 7) * tiles_k, sb = (nb >> 7) * tiles_k;
+            for (int kb = 0; kb < nkb; kb++) {
+                if (!mbar_wait(empty_bar(s), phase)) {  // a fresh barrier passes
                     *abort_flag = 1;
                     set_status(status, MNMT_ETIMEOUT);
                     failed = true;
                     break;
                 }
                 // the leader's barrier takes the bytes of both CTAs of a pair
-                if (rank == 0) mbar_expect_tx(full_bar(s), CG * L::STAGE);
-                const uint32_t bar = CG == 1 ? full_bar(s) : t2_mapa(full_bar(s), 0), base = ring + s * L::STAGE;
-                f4_load<CG>(base, &tmA, kb * 128, m0, bar);
-                f4_load<CG>(base + L::A_BYTES, &tmB, kb * 128, n0, bar);
-                // scale tiles kb T .. of the rows' tile rows (tiles past the row's
-                // end belong to k-steps that are not issued)
-                f4_load<CG>(base + L::OFF_SFA, &tmSA, 0, (m0 >> 7) * tiles_k + kb * T, bar);
+                expect_tx_on(on && rank == 0, full_bar(s), CG * L::STAGE);
+                const uint32_t bar = lead + 8u * s, base = ring + s * L::STAGE;
+                f4_load_on<CG>(on, base, &tmA, kb * 128, m0, bar);
+                f4_load_on<CG>(on, base + L::A_BYTES, &tmB, kb * 128, n0, bar);
+                f4_load_on<CG>(on, base + L::OFF_SFA, &tmSA, 0, sa, bar);
 #pragma unroll
-                for (int r = 0; r < R; r++)
-                    f4_load<CG>(base + L::OFF_SFB + r * T * 512, &tmSB, 0, ((nb >> 7) + r) * tiles_k + kb * T, bar);
-                issued = it + 1;
+                for (int r = 0; r < R; r++) f4_load_on<CG>(on, base + L::OFF_SFB + r * T * 512, &tmSB, 0, sb + r * tiles_k, bar);
+                sa += T, sb += T;
+                issued++;
+                if (++s == STAGES) s = 0, phase ^= 1;
             }
         }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
         // ---- scales to TMEM and MMAs ----
-        uint32_t it = 0, lt = 0;
+        const uint32_t on = elect_one();
+        uint32_t s = 0, phase = 0, lt = 0, seen = 0;
         bool failed = false;
         const uint32_t ring = s_addr(sm);
         const uint64_t a_desc = sw128_desc(ring), b_desc = sw128_desc(ring + L::A_BYTES);
         const uint64_t sa_desc = f4_scale_desc(ring + L::OFF_SFA), sb_desc = f4_scale_desc(ring + L::OFF_SFB);
         for (long tile = unit; tile < tiles && !failed; tile += units, lt++) {
-            const int buf = (int)(lt & 1);
+            const uint32_t buf = lt & 1;
             if (lt >= 2 && !mbar_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
                 failed = true;
                 break;
             }
             tc_fence_after();
-            const uint32_t d = tbase + (uint32_t)(buf * BN);
+            const uint32_t d = tbase + buf * BN;
             // scale columns of the tile's first row of W (a tile that starts inside a row tile: two columns per 64 rows)
             const uint32_t sfa = tbase + L::COL_SFA, sfb = tbase + L::COL_SFB, shift = (uint32_t)((tile_n(tile) & 127) >> 5);
-            for (int kb = 0; kb < nkb; kb++, it++) {
-                const int s = (int)(it % STAGES);
-                if (!mbar_wait(full_bar(s), (it / STAGES) & 1)) {
+            for (int kb = 0; kb < nkb; kb++) {
+                if (!mbar_wait(full_bar(s), phase)) {
                     failed = true;
                     break;
                 }
@@ -211,31 +221,31 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
                 const uint64_t off = (uint64_t)((s * L::STAGE) >> 4);
 #pragma unroll
                 for (int t = 0; t < T; t++) {
-                    f4_copy_scales<CG>(sfa + 4 * t, sa_desc + off + (uint64_t)(t * 32));
+                    f4_copy_scales_on<CG>(on, sfa + 4 * t, sa_desc + off + (uint64_t)(t * 32));
 #pragma unroll
-                    for (int r = 0; r < R; r++) f4_copy_scales<CG>(sfb + 4 * (R * t + r), sb_desc + off + (uint64_t)((r * T + t) * 32));
+                    for (int r = 0; r < R; r++) f4_copy_scales_on<CG>(on, sfb + 4 * (R * t + r), sb_desc + off + (uint64_t)((r * T + t) * 32));
                 }
                 const int n = min(4, steps - 4 * kb);
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
-                    if (k < n) {
-                        const int t = NV ? k : k >> 1, id = NV ? 0 : 2 * (k & 1);
-                        f4_mma<CG, NV>(d, a_desc + off + (uint64_t)(2 * k), b_desc + off + (uint64_t)(2 * k), f4_idesc(CG * F4_BM, BN, NV, id),
-                                       sfa + 4 * t, sfb + 4 * R * t + shift, (uint32_t)(kb | k));
-                    }
+                    const int t = NV ? k : k >> 1, id = NV ? 0 : 2 * (k & 1);
+                    f4_mma_on<CG, NV>(k < n ? on : 0, d, a_desc + off + (uint64_t)(2 * k), b_desc + off + (uint64_t)(2 * k),
+                                      f4_idesc(CG * F4_BM, BN, NV, id), sfa + 4 * t, sfb + 4 * R * t + shift, (uint32_t)(kb | k));
                 }
-                f4_commit<CG>(empty_bar(s));
+                f4_commit_on<CG>(on, empty_bar(s));
+                seen++;
+                if (++s == STAGES) s = 0, phase ^= 1;
             }
-            if (!failed) f4_commit<CG>(accf_bar(buf));
+            if (!failed) f4_commit_on<CG>(on, accf_bar(buf));
         }
         if (failed) {
             *abort_flag = 1;
             set_status(status, MNMT_ETIMEOUT);
         }
         pdl_allow_next();  // every MMA of this CTA (pair) is issued
-        misc[2] = it;      // k-blocks whose copies this thread saw land
-        f4_commit<CG>(done_bar);
-    } else if (warp == 1 && lane == 0) {
+        misc[2] = seen;    // k-blocks whose copies this warp saw land
+        f4_commit_on<CG>(on, done_bar);
+    } else if (warp == 1) {
         pdl_allow_next();  // the leader's trigger decides
     } else if (warp >= 2) {
         // ---- epilogue of this CTA's 128 rows: warp half h takes columns h BN/2 .. ----

@@ -15,6 +15,52 @@ constexpr int F4_EPI_WARPS = 8;
 constexpr int F4_THREADS = 64 + F4_EPI_WARPS * 32;  // producer warp, MMA warp, epilogue warps
 constexpr int F4_BLK = 2048;  // a staging block: 32 rows of 64 bytes
 
+// One lane of a converged warp.  The producer and MMA warps of a fast kernel run
+// their loops with all lanes and issue from this one by predicate (on): operands
+// that every lane computes alike stay in uniform registers, where a branch on the
+// lane costs a move per operand and instruction.
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t on;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+    return on;
+}
+template <int CG>
+__device__ __forceinline__ void f4_load_on(uint32_t on, uint32_t dst, const CUtensorMap *tm, int x, int y, uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+            "@q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}" ::"r"(dst),
+            "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(bar), "r"(on)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+            "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}" ::"r"(
+                dst),
+            "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(bar), "r"(on)
+            : "memory");
+}
+__device__ __forceinline__ void expect_tx_on(uint32_t on, uint32_t bar, uint32_t bytes) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar),
+                 "r"(bytes), "r"(on)
+                 : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void f4_commit_on(uint32_t on, uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+            "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+            "r"(on)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+            "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(bar),
+            "h"((uint16_t)3), "r"(on)
+            : "memory");
+}
+
 template <int CG>
 __device__ __forceinline__ void f4_load(uint32_t dst, const CUtensorMap *tm, int x, int y, uint32_t bar) {
     if constexpr (CG == 1) tma_load_2d(dst, tm, x, y, bar);
