@@ -13,7 +13,7 @@
 // reduction index is the row of a stored operand, so the MMAs read W, X and (for
 // gW) G "MN-major" from tiles as they lie in memory: no transposed copies.  The
 // epilogue warps gather the straight-through masks of a tile before its sums are
-// ready and store through shared memory by TMA; two warps sum the bias gradient
+// ready and store through shared memory; two warps sum the bias gradient
 // meanwhile.  Grids of few tiles split the reduction; the parts are added in
 // their order by the CTA that finishes last.
 #include <type_traits>
@@ -96,7 +96,7 @@ constexpr int BW_BK = 64;  // reduction indices per stage
 // terms and added up in registers (16384 terms: 5e-7 off); 16-bit results, whose
 // rounding is 2^-9 or 2^-11, are not.
 constexpr int BW_CHUNK = 16;  // stages
-constexpr int BW_GB_WARPS = 2, BW_THREADS = F4_THREADS + 32 * BW_GB_WARPS;
+constexpr int BW_EPI_WARPS = 8, BW_GB_WARPS = 2, BW_THREADS = 64 + 32 * (BW_EPI_WARPS + BW_GB_WARPS);
 constexpr int GB_ROWS = 128, GB_COLS = 256;  // rows and columns of G that a warp sums at a time
 
 template <int CG, int BN>
@@ -104,7 +104,7 @@ struct BwLayout {
     static constexpr uint32_t A_BYTES = F4_BM * BW_BK * 2;
     static constexpr uint32_t B_BYTES = BN / CG * BW_BK * 2;
     static constexpr uint32_t STAGE = A_BYTES + B_BYTES;
-    static constexpr uint32_t STG = F4_EPI_WARPS * 2 * F4_BLK;
+    static constexpr uint32_t STG = BW_EPI_WARPS * F4_BLK;
     static constexpr int FIT = (int)((227 * 1024 - 1024 - STG - 512) / STAGE);
     static constexpr int STAGES = FIT > 8 ? 8 : FIT;
     static constexpr uint32_t OFF_STG = STAGES * STAGE;
@@ -242,8 +242,8 @@ __device__ __noinline__ void bias_gradient(const BwArgs &a, int w, int n) {
 // 11 sum the bias gradient.  An item is a part of a tile.
 template <int CG, int BN, bool NV>
 __global__ void __launch_bounds__(BW_THREADS, 1)
-    fp4_backward_gemm(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmY0,
-                      const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ CUtensorMap tmY1,
+    fp4_backward_gemm(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0,
+                      const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1,
                       const __grid_constant__ BwArgs a, int *status) {
     pdl_grid_wait();
     using L = BwLayout<CG, BN>;
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
         }
         for (int b = 0; b < 2; b++) {
             mbar_init(accf_bar(b), 1);
-            mbar_init(acce_bar(b), CG * F4_EPI_WARPS);
+            mbar_init(acce_bar(b), CG * BW_EPI_WARPS);
         }
         mbar_init(done_bar, 1);
         misc[1] = 0;
@@ -414,18 +414,17 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
         f4_commit<CG>(done_bar);
     } else if (warp == 1 && lane == 0) {
         pdl_allow_next();  // the leader's trigger decides
-    } else if (warp >= 2 + F4_EPI_WARPS) {
-        if (a.gb) bias_gradient(a, (int)blockIdx.x * BW_GB_WARPS + warp - 2 - F4_EPI_WARPS, (int)gridDim.x * BW_GB_WARPS);
+    } else if (warp >= 2 + BW_EPI_WARPS) {
+        if (a.gb) bias_gradient(a, (int)blockIdx.x * BW_GB_WARPS + warp - 2 - BW_EPI_WARPS, (int)gridDim.x * BW_GB_WARPS);
     } else if (warp >= 2) {
         // ---- epilogue ----
         constexpr int NB = BN / 64;
         const int ew = warp - 2, q = warp & 3, cw = (BN / 2) * (ew >> 2);
-        uint8_t *stg = sm + L::OFF_STG + ew * 2 * F4_BLK;
-        uint32_t lt = 0, blocks = 0;
+        uint8_t *stg = sm + L::OFF_STG + ew * F4_BLK;
+        uint32_t lt = 0;
         for (int phase = 0; phase < 3; phase++) {
             const Range rg = range(phase);
             const BwProduct &p = a.p[phase > 0];
-            const CUtensorMap *ty = phase ? &tmY1 : &tmY0;
             for (long item = rg.first; item < rg.end; item += rg.step) {
                 const At t = at(phase, item);
                 const int row0 = t.m + (int)rank * F4_BM + 32 * q, col0 = t.n + cw;
@@ -477,9 +476,9 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                             for (int g = 0; g < 8; g++) o[(b * 8 + g) * 32] = make_float4(acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]);
                     }
                     __threadfence();
-                    f4_epi_sync();
+                    asm volatile("bar.sync 1, %0;" ::"n"(BW_EPI_WARPS * 32) : "memory");
                     if (ew == 0 && lane == 0) misc[3] = *abort_flag == 0 && atomicAdd(p.tickets + t.tile * CG + rank, 1) == p.parts - 1;
-                    f4_epi_sync();
+                    asm volatile("bar.sync 1, %0;" ::"n"(BW_EPI_WARPS * 32) : "memory");
                     store = store && misc[3];
                     if (store) {
                         __threadfence();
@@ -505,11 +504,10 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                     if (!store || col0 + 32 * b >= p.cols) continue;
 #pragma unroll
                     for (int i = 0; i < 32; i++) acc[b][i] = (in[b] >> i) & 1u ? __fmul_rn(acc[b][i], p.out.alpha) : 0.0f;
-                    f4_store_block(p.out, ty, stg, blocks, acc[b], row0, col0 + 32 * b, p.rows, p.cols);
+                    f4_store_block(p.out, stg, acc[b], row0, col0 + 32 * b, p.rows, p.cols);
                 }
             }
         }
-        if (lane == 0) t2_store_wait();
     }
 
     // ---- teardown: every MMA and copy has completed before a CTA ends ----
@@ -537,7 +535,7 @@ size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 int up8(int n) { return (n + 7) & ~7; }
 
 bool encode_bf16(CUtensorMap *tm, const void *p, int cols, int rows, long ld, int box_rows) {
-    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p, cols, rows, (cuuint64_t)ld * 2, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B, true);
+    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p, cols, rows, (cuuint64_t)ld * 2, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 template <int CG, int BN, bool NV>
@@ -620,14 +618,14 @@ Scratch scratch(int M, int N, int K) {
 }
 
 template <int CG, int BN, bool NV>
-cudaError_t bw_launch(const CUtensorMap (&tm)[6], const BwArgs &a, long items, int *status, cudaStream_t st) {
+cudaError_t bw_launch(const CUtensorMap (&tm)[4], const BwArgs &a, long items, int *status, cudaStream_t st) {
     const long fit = CG == 2 ? g_bw_pairs : device_sm_count();
     // the bias gradient's warps take the whole GPU where the products do not
     const long gb = a.gb ? ((long)fp4_div_up(a.N, GB_COLS) * fp4_div_up(a.M, GB_ROWS) + CG * BW_GB_WARPS - 1) / (CG * BW_GB_WARPS) : 0;
     if (items < gb) items = gb;
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, (int)(items < fit ? items : fit), BW_THREADS, BwLayout<CG, BN>::SMEM, st, attr);
-    return cudaLaunchKernelEx(&cfg, fp4_backward_gemm<CG, BN, NV>, tm[0], tm[1], tm[2], tm[3], tm[4], tm[5], a, status);
+    return cudaLaunchKernelEx(&cfg, fp4_backward_gemm<CG, BN, NV>, tm[0], tm[1], tm[2], tm[3], a, status);
 }
 
 }  // namespace
@@ -673,7 +671,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
     a.g = copy ? p.g16 : p.g, a.ldg = copy ? s.pn : b.ldg;
     a.gb = b.gb, a.gb_part = reinterpret_cast<float *>(ws + s.gb), a.gb_tickets = tickets;
     a.p[0].parts = a.p[1].parts = 1;
-    CUtensorMap tm[6];
+    CUtensorMap tm[4];
     memset(tm, 0, sizeof(tm));
     float *partial = reinterpret_cast<float *>(ws + s.partial);
     // the longer part first
@@ -682,7 +680,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
         const bool input = (i == 0) == input_first;
         if (input ? !b.gx : !b.gw) continue;
         BwProduct &r = a.p[a.n];
-        CUtensorMap *t = tm + 3 * a.n;
+        CUtensorMap *t = tm + 2 * a.n;
         a.n++;
         r.rows = input ? M : N, r.cols = K, r.red = input ? N : M, r.a_mn = !input;
         r.out = input ? F4Out{b.gx, b.ldgx, b.xdtype, 0, 0, b.nv ? b.w.g : 1.0f, nullptr} : F4Out{b.gw, b.ldgw, MNMT_F32, 0, 0, b.nv ? b.x.g : 1.0f, nullptr};
@@ -696,7 +694,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
             r.tickets = tickets + p.n_tickets;
             p.n_tickets += (int)pl.tiles[!input] * (pl.pair ? 2 : 1);
         }
-        encode_out(t + 2, r.out, r.rows, r.cols);
+        r.out.vec = out_vec(r.out.y, r.out.ldy, r.out.type);
         if (!encode_bf16(t, a.g, N, M, a.ldg, input ? F4_BM : 64) || !encode_bf16(t + 1, input ? p.w16 : p.x16, K, input ? N : M, s.pk, 64))
             return cudaErrorInvalidValue;
     }

@@ -8,13 +8,13 @@
 // tiles of 256 codes) and the scales as they are stored: a 512-byte tile of 128
 // rows x 4 blocks goes to four TMEM columns with one tcgen05.cp.
 //
-// Persistent, 320 threads per CTA:
+// Persistent, 10 or 14 warps per CTA:
 //   warp 0 lane 0   TMA producer: codes and scales of a k-block of 256 into a ring;
 //   warp 1 lane 0   copies a k-block's scales to TMEM (tcgen05.cp and .mma run in
 //                   the order in which they are issued, so one set of columns
 //                   serves every k-block), issues its four MMAs, frees the slot;
-//   warps 2..9      drain a finished accumulator (TMEM holds two), apply alpha,
-//                   bias and ReLU, round, and store through shared memory by TMA.
+//   the others      drain a finished accumulator (TMEM holds two), apply alpha,
+//                   bias and ReLU, round, and store through shared memory.
 // CG = 2: a pair of CTAs computes 256 x 192 tiles, each CTA half of the rows of
 // both operands; CG = 1: 128 x 128 or 128 x 64 tiles for smaller grids.
 // Every wait is bounded; one that runs out records MNMT_ETIMEOUT in *status, and
@@ -41,12 +41,14 @@ struct F4Layout {
     static constexpr uint32_t B_BYTES = BN / CG * 128;
     static constexpr uint32_t OFF_SFA = A_BYTES + B_BYTES, OFF_SFB = OFF_SFA + T * 512;
     static constexpr uint32_t STAGE = OFF_SFB + R * T * 512;
-    static constexpr uint32_t OFF_AFTER = F4_EPI_WARPS * 2 * F4_BLK + 2 * BN * 4 + 512;  // staging, bias, barriers
+    static constexpr int EPI = BN == 64 ? 8 : BN / 16, CW = 4 * BN / EPI;  // epilogue warps, columns of each (its 32 rows)
+    static constexpr int THREADS = 64 + 32 * EPI;
+    static constexpr uint32_t OFF_AFTER = EPI * (F4_BLK + CW * 4) + 512;  // staging, bias, barriers
     static constexpr int FIT = (int)((227 * 1024 - 1024 - OFF_AFTER) / STAGE);
     static constexpr int STAGES = FIT > 8 ? 8 : FIT;
     static constexpr uint32_t OFF_STG = STAGES * STAGE;
-    static constexpr uint32_t OFF_COLS = OFF_STG + F4_EPI_WARPS * 2 * F4_BLK;  // [2][BN] fp32
-    static constexpr uint32_t OFF_BARS = OFF_COLS + 2 * BN * 4;
+    static constexpr uint32_t OFF_COLS = OFF_STG + EPI * F4_BLK;  // [EPI][CW] fp32
+    static constexpr uint32_t OFF_BARS = OFF_COLS + EPI * CW * 4;
     static constexpr int NBARS = 2 * STAGES + 5;  // full, empty, acc_full[2], acc_empty[2], done
     static constexpr uint32_t OFF_MISC = OFF_BARS + NBARS * 8;
     static constexpr size_t SMEM = 1024 + OFF_MISC + 16;
@@ -101,16 +103,15 @@ __device__ __forceinline__ void f4_copy_scales_on(uint32_t on, uint32_t taddr, u
 }
 
 template <int CG, int BN, bool NV>
-__global__ void __launch_bounds__(F4_THREADS, 1)
+__global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
     fp4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmSA,
-             const __grid_constant__ CUtensorMap tmSB, const __grid_constant__ CUtensorMap tmY, F4Out o, int M, int N, int K, int *status) {
+             const __grid_constant__ CUtensorMap tmSB, F4Out o, int M, int N, int K, int *status) {
     pdl_grid_wait();
     using L = F4Layout<CG, BN, NV>;
     constexpr int STAGES = L::STAGES, T = L::T, R = L::R;
 
     extern __shared__ uint8_t f4_raw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(f4_raw) + 1023) & ~(uintptr_t)1023);
-    float *cols = reinterpret_cast<float *>(sm + L::OFF_COLS);
     const uint32_t bars = s_addr(sm + L::OFF_BARS);
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
         }
         for (int b = 0; b < 2; b++) {
             mbar_init(accf_bar(b), 1);
-            mbar_init(acce_bar(b), CG * F4_EPI_WARPS);
+            mbar_init(acce_bar(b), CG * L::EPI);
         }
         mbar_init(done_bar, 1);
         misc[1] = 0;
@@ -248,18 +249,21 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
     } else if (warp == 1) {
         pdl_allow_next();  // the leader's trigger decides
     } else if (warp >= 2) {
-        // ---- epilogue of this CTA's 128 rows: warp half h takes columns h BN/2 .. ----
-        constexpr int NB = BN / 64;
-        const int ew = warp - 2, q = warp & 3, cw = (BN / 2) * (ew >> 2);
-        uint8_t *stg = sm + L::OFF_STG + ew * 2 * F4_BLK;
-        const int ti = ew * 32 + lane;
-        uint32_t lt = 0, blocks = 0;  // blocks staged so far: they alternate between the two buffers
+        // ---- epilogue: warp ew takes 32 of this CTA's rows, CW columns of the tile ----
+        constexpr int CW = L::CW, NB = CW / 32;
+        const int ew = warp - 2, q = warp & 3, cw = CW * (ew >> 2);
+        uint8_t *stg = sm + L::OFF_STG + ew * F4_BLK;
+        float *bias = reinterpret_cast<float *>(sm + L::OFF_COLS) + ew * CW;
+        uint32_t lt = 0;
         for (long tile = unit; tile < tiles; tile += units, lt++) {
             const int buf = (int)(lt & 1);
-            const int n0 = tile_n(tile), row0 = tile_m(tile) + (int)rank * F4_BM + 32 * q, col0 = n0 + cw;
-            float *bias = cols + (lt & 1) * BN;
-            if (ti < BN) bias[ti] = o.bias && n0 + ti < N ? o.bias[n0 + ti] : 0.0f;
-            f4_epi_sync();
+            const int row0 = tile_m(tile) + (int)rank * F4_BM + 32 * q, col0 = tile_n(tile) + cw;
+            __syncwarp();
+#pragma unroll
+            for (int b = 0; b < NB; b++) {
+                const int n = col0 + 32 * b + lane;
+                bias[32 * b + lane] = o.bias && n < N ? o.bias[n] : 0.0f;
+            }
             bool ok = *abort_flag == 0 && mbar_wait(accf_bar(buf), (lt >> 1) & 1);
             if (!ok && *abort_flag == 0) {
                 *abort_flag = 1;
@@ -268,34 +272,37 @@ __global__ void __launch_bounds__(F4_THREADS, 1)
             tc_fence_after();
             ok = __all_sync(0xFFFFFFFFu, ok && *abort_flag == 0);
             const uint32_t taddr = tbase + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * BN + cw);
-            const bool mine = ok && row0 < M;
-#pragma unroll 1
-            for (int b = 0; b < NB; b++) {
-                float v[32];
-                if (mine && col0 + 32 * b < N) {
-                    uint32_t r[32];
-                    tmem_ld32(taddr + 32 * b, r);
-                    tmem_wait_ld();
-                    const float *bb = bias + cw + 32 * b;
+            uint32_t r[NB][32];
 #pragma unroll
-                    for (int i = 0; i < 32; i++) {
-                        v[i] = __fadd_rn(__fmul_rn(__uint_as_float(r[i]), o.alpha), bb[i]);
-                        if (o.relu && v[i] <= 0.0f) v[i] = 0.0f;  // a NaN stays
+            for (int b = 0; b < NB; b++) tmem_ld32(taddr + 32 * b, r[b]);
+            tmem_wait_ld();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {  // this warp is done with the accumulator buffer
+                if constexpr (CG == 1) mbar_arrive(acce_bar(buf));
+                else t2_arrive_remote(t2_mapa(acce_bar(buf), 0));
+            }
+            if (!ok || row0 >= M) continue;
+#pragma unroll
+            for (int b = 0; b < NB; b++) {
+                if (col0 + 32 * b >= N) break;
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const float4 c = *reinterpret_cast<const float4 *>(bias + 32 * b + i);
+                    const float cc[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        const float a = __uint_as_float(r[b][i + k]);
+                        v[i + k] = __fadd_rn(NV ? __fmul_rn(a, o.alpha) : a, cc[k]);
                     }
                 }
-                if (b == NB - 1) {  // this warp is done with the accumulator buffer
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (CG == 1) mbar_arrive(acce_bar(buf));
-                        else t2_arrive_remote(t2_mapa(acce_bar(buf), 0));
-                    }
-                }
-                if (!mine || col0 + 32 * b >= N) continue;
-                f4_store_block(o, &tmY, stg, blocks, v, row0, col0 + 32 * b, M, N);
+                if (o.relu)
+#pragma unroll
+                    for (int i = 0; i < 32; i++) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v[i]));
+                f4_store_block(o, stg, v, row0, col0 + 32 * b, M, N);
             }
         }
-        if (lane == 0) t2_store_wait();
     }
 
     // ---- teardown: every MMA and copy has completed before a CTA ends ----
@@ -321,12 +328,12 @@ int g_f4_pairs = 0;  // CTA pairs that fit at once
 
 bool encode_codes(CUtensorMap *tm, const Fp4Args &q, int box_rows) {
     const size_t pitch = fp4_pitch(q.cols);
-    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, q.codes, pitch, q.rows, pitch, 128, box_rows, CU_TENSOR_MAP_SWIZZLE_128B, true);
+    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, q.codes, pitch, q.rows, pitch, 128, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 // the scale tiles as a matrix of 128 words each
 bool encode_scales(CUtensorMap *tm, const Fp4Args &q, bool nv) {
     const size_t n = fp4_scale_bytes(q.rows, q.cols, nv) / 512;
-    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT32, q.scales, 128, n, 512, 128, nv ? 4 : 2, CU_TENSOR_MAP_SWIZZLE_NONE, true);
+    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT32, q.scales, 128, n, 512, 128, nv ? 4 : 2, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 template <int CG, int BN, bool NV>
@@ -334,7 +341,7 @@ cudaError_t f4_init() {
     cudaError_t err = cudaFuncSetAttribute(fp4_gemm<CG, BN, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F4Layout<CG, BN, NV>::SMEM);
     if (err != cudaSuccess || CG == 1) return err;
     cudaLaunchAttribute attr[2];
-    cudaLaunchConfig_t cfg = f4_config(CG, 64, F4_THREADS, F4Layout<CG, BN, NV>::SMEM, nullptr, attr);
+    cudaLaunchConfig_t cfg = f4_config(CG, 64, F4Layout<CG, BN, NV>::THREADS, F4Layout<CG, BN, NV>::SMEM, nullptr, attr);
     int n = 0;
     err = cudaOccupancyMaxActiveClusters(&n, fp4_gemm<CG, BN, NV>, &cfg);
     if (err == cudaSuccess && (g_f4_pairs == 0 || n < g_f4_pairs)) g_f4_pairs = n;
@@ -342,19 +349,16 @@ cudaError_t f4_init() {
 }
 
 template <int CG, int BN, bool NV>
-cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &out, int *status, cudaStream_t st) {
+cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &o, int *status, cudaStream_t st) {
     const int M = x.rows, N = w.rows, K = x.cols;
-    CUtensorMap ta, tb, tsa, tsb, ty;
-    F4Out o = out;
+    CUtensorMap ta, tb, tsa, tsb;
     if (!encode_codes(&ta, x, F4_BM) || !encode_codes(&tb, w, BN / CG) || !encode_scales(&tsa, x, NV) || !encode_scales(&tsb, w, NV))
         return cudaErrorInvalidValue;
-    encode_out(&ty, o, M, N);
-    if (!o.tma) ty = ta;
     const long tiles = (long)((M + CG * F4_BM - 1) / (CG * F4_BM)) * ((N + BN - 1) / BN);
     const long fit = CG == 2 ? g_f4_pairs : device_sm_count();
     cudaLaunchAttribute attr[2];
-    cudaLaunchConfig_t cfg = f4_config(CG, (int)(tiles < fit ? tiles : fit), F4_THREADS, F4Layout<CG, BN, NV>::SMEM, st, attr);
-    return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV>, ta, tb, tsa, tsb, ty, o, M, N, K, status);
+    cudaLaunchConfig_t cfg = f4_config(CG, (int)(tiles < fit ? tiles : fit), F4Layout<CG, BN, NV>::THREADS, F4Layout<CG, BN, NV>::SMEM, st, attr);
+    return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV>, ta, tb, tsa, tsb, o, M, N, K, status);
 }
 
 }  // namespace
@@ -371,7 +375,7 @@ cudaError_t fp4_init() {
 
 cudaError_t launch_fp4_product(const Fp4Args &x, const Fp4Args &w, bool nv, float alpha, const float *bias, int relu, void *y, int ydtype,
                                long ldy, int *status, cudaStream_t st) {
-    const F4Out o{y, ldy, ydtype, 0, relu, alpha, bias};
+    const F4Out o{y, ldy, ydtype, out_vec(y, ldy, ydtype), relu, alpha, bias};
     auto go = [&](auto n) {
         constexpr bool NV = decltype(n)::value;
         const long mt = (x.rows + 127) / 128, sms = device_sm_count();

@@ -11,9 +11,7 @@
 namespace mnmt {
 
 constexpr int F4_BM = 128;  // rows of a tile per CTA
-constexpr int F4_EPI_WARPS = 8;
-constexpr int F4_THREADS = 64 + F4_EPI_WARPS * 32;  // producer warp, MMA warp, epilogue warps
-constexpr int F4_BLK = 2048;  // a staging block: 32 rows of 64 bytes
+constexpr int F4_BLK = 2048;  // a warp's staging block: 32 rows of 64 bytes
 
 // One lane of a converged warp.  The producer and MMA warps of a fast kernel run
 // their loops with all lanes and issue from this one by predicate (on): operands
@@ -72,13 +70,11 @@ __device__ __forceinline__ void f4_commit(uint32_t bar) {
     else t2_commit(bar);
 }
 
-__device__ __forceinline__ void f4_epi_sync() { asm volatile("bar.sync 1, %0;" ::"n"(F4_EPI_WARPS * 32) : "memory"); }
-
 struct F4Out {
     void *y;
     long ldy;
     int type;   // MNMT_F32 / BF16 / F16
-    int tma;    // tmY describes y
+    int vec;    // 16-byte stores are aligned
     int relu;
     float alpha;
     const float *bias;
@@ -114,73 +110,57 @@ __device__ __forceinline__ void f4_stage32(uint8_t *blk, const float (&v)[32]) {
             make_float4(v[16 * H + 4 * c], v[16 * H + 4 * c + 1], v[16 * H + 4 * c + 2], v[16 * H + 4 * c + 3]);
 }
 
-// a staged block to y where no tensor map describes it: coalesced single elements
-__device__ __forceinline__ void f4_store_plain(const F4Out &o, const uint8_t *blk, int row0, int col0, int M, int N) {
-    const int lane = threadIdx.x & 31;
-    if (o.type == MNMT_F32) {
-        const int c = lane & 15;
-        for (int r = lane >> 4; r < 32; r += 2)
-            if (row0 + r < M && col0 + c < N)
-                static_cast<float *>(o.y)[(row0 + r) * o.ldy + col0 + c] =
-                    *reinterpret_cast<const float *>(blk + r * 64 + t2_chunk<64>(r, c >> 2) + 4 * (c & 3));
-    } else {
-        for (int r = 0; r < 32; r++)
-            if (row0 + r < M && col0 + lane < N)
-                static_cast<uint16_t *>(o.y)[(row0 + r) * o.ldy + col0 + lane] =
-                    *reinterpret_cast<const uint16_t *>(blk + r * 64 + t2_chunk<64>(r, lane >> 3) + 2 * (lane & 7));
-    }
-}
-
-// 32 columns of a warp's 32 rows (a row per lane) from column col on: one block
-// of 16-bit outputs or two of fp32, staged in the two blocks at stg by turns
-__device__ __forceinline__ void f4_store_block(const F4Out &o, const CUtensorMap *tmY, uint8_t *stg, uint32_t &blocks, const float (&v)[32], int row0,
-                                               int col, int M, int N) {
-    const int lane = threadIdx.x & 31;
+// 32 columns of a warp's 32 rows (a row per lane) from column col on: through the
+// staging block (32 x 16-bit or 16 x fp32 columns) so that the stores write whole
+// 64-byte runs, eight rows at a time.
+__device__ __forceinline__ void f4_store_block(const F4Out &o, uint8_t *blk, const float (&v)[32], int row0, int col, int M, int N) {
+    const int lane = threadIdx.x & 31, c = lane & 3;
     const bool f32 = o.type == MNMT_F32;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
         if (h == 1 && !f32) break;
-        uint8_t *blk = stg + (blocks & 1) * F4_BLK;
-        if (o.tma) {
-            if (lane == 0) t2_store_wait_read<1>();  // the store before the last has read this block
-            __syncwarp();
-        }
+        __syncwarp();  // the block has been read
         if (!f32) f4_stage16(blk, v, o.type);
         else if (h == 0) f4_stage32<0>(blk, v);
         else f4_stage32<1>(blk, v);
-        if (o.tma) {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-                if (col + 16 * h < N) t2_store(tmY, col + 16 * h, row0, s_addr(blk));
-                t2_store_commit();
+        __syncwarp();
+        const int es = f32 ? 4 : 2, per = 16 / es, col0 = col + 16 * h + per * c, n = N - col0;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int r = 8 * i + (lane >> 2), row = row0 + r;
+            const uint4 w = *reinterpret_cast<const uint4 *>(blk + r * 64 + t2_chunk<64>(r, c));
+            if (row >= M || n <= 0) continue;
+            uint8_t *dst = static_cast<uint8_t *>(o.y) + ((long)row * o.ldy + col0) * es;
+            if (o.vec && n >= per) {
+                *reinterpret_cast<uint4 *>(dst) = w;
+            } else {
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                if (f32) {
+#pragma unroll
+                    for (int k = 0; k < 4; k++)
+                        if (k < n) reinterpret_cast<uint32_t *>(dst)[k] = u[k];
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; k++)
+                        if (k < n) reinterpret_cast<uint16_t *>(dst)[k] = (uint16_t)(u[k >> 1] >> (16 * (k & 1)));
+                }
             }
-        } else {
-            __syncwarp();
-            f4_store_plain(o, blk, row0, col + 16 * h, M, N);
-            __syncwarp();
         }
-        blocks++;
     }
 }
 
 // two-dimensional tensor map: w x h elements, rows `stride` bytes apart, boxes of bw x bh
 inline bool encode(CUtensorMap *tm, CUtensorMapDataType type, const void *p, cuuint64_t w, cuuint64_t h, cuuint64_t stride, cuuint32_t bw, cuuint32_t bh,
-            CUtensorMapSwizzle sw, bool load) {
+            CUtensorMapSwizzle sw) {
     cuuint64_t dims[2] = {w, h}, strides[1] = {stride};
     cuuint32_t box[2] = {bw, bh}, estr[2] = {1, 1};
     return tma_encoder()(tm, type, 2, const_cast<void *>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
-                         load ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// the map of an output matrix in the epilogue's boxes; o.tma: whether there is one
-inline void encode_out(CUtensorMap *tm, F4Out &o, int M, int N) {
-    const int es = o.type == MNMT_F32 ? 4 : 2;
-    const CUtensorMapDataType t = o.type == MNMT_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                  : o.type == MNMT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
-                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    o.tma = (reinterpret_cast<uintptr_t>(o.y) & 15) == 0 && o.ldy * es % 16 == 0 && o.ldy * es < ((long)1 << 40) &&
-            encode(tm, t, o.y, N, M, (cuuint64_t)o.ldy * es, 64 / es, 32, CU_TENSOR_MAP_SWIZZLE_64B, false);
+// whether every 16-byte store of the epilogue is aligned
+inline bool out_vec(const void *y, long ldy, int type) {
+    return (reinterpret_cast<uintptr_t>(y) & 15) == 0 && ldy * (type == MNMT_F32 ? 4 : 2) % 16 == 0;
 }
 
 // cluster and launch attributes of a tile kernel (programmatic launch outside stream captures, as launch_pdl)
