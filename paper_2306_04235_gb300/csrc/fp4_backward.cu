@@ -458,10 +458,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (CG == 1) mbar_arrive(acce_bar(buf));
-                        else t2_arrive_remote(t2_mapa(acce_bar(buf), 0));
-                    }
+                    if (lane == 0) f4_release<CG>(acce_bar(buf));
                 }
                 bool store = ok && row0 < p.rows;
                 if (p.parts > 1) {

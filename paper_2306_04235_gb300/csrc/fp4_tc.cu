@@ -131,7 +131,7 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
     // by CTAs that run at the same time
     auto tile_m = [&](long t) { return (int)(mt <= nt ? t % mt : t / nt) * CG * F4_BM; };
     auto tile_n = [&](long t) { return (int)(mt <= nt ? t / mt : t % nt) * BN; };
-    const int steps = (K + 63) / 64, nkb = (K + F4_BK - 1) / F4_BK, tiles_k = fp4_tiles_k(K, NV);
+    const int steps = (K + 63) / 64, full = steps / 4, nkb = (K + F4_BK - 1) / F4_BK, tiles_k = fp4_tiles_k(K, NV);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; s++) {
@@ -210,9 +210,14 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
                 break;
             }
             tc_fence_after();
-            const uint32_t d = tbase + buf * BN;
-            // scale columns of the tile's first row of W (a tile that starts inside a row tile: two columns per 64 rows)
-            const uint32_t sfa = tbase + L::COL_SFA, sfb = tbase + L::COL_SFB, shift = (uint32_t)((tile_n(tile) & 127) >> 5);
+            // Through a shuffle: every lane has the same value, and says so.  (Operands
+            // that the compiler cannot see to be uniform, or a test per MMA for the
+            // last k-block, cost more than the MMA: 8192^3 191 -> 157 us.)
+            const uint32_t d = __shfl_sync(0xFFFFFFFFu, tbase + buf * BN, 0);
+            // scale columns of the tile's first row of W: a tile may start in the middle of a row tile, two columns on
+            const uint32_t sfa = __shfl_sync(0xFFFFFFFFu, tbase + L::COL_SFA, 0);
+            const uint32_t sfb = __shfl_sync(0xFFFFFFFFu, tbase + L::COL_SFB + ((uint32_t)(tile_n(tile) & 127) >> 5), 0);
+            const uint32_t cfb = __shfl_sync(0xFFFFFFFFu, tbase + L::COL_SFB, 0);
             for (int kb = 0; kb < nkb; kb++) {
                 if (!mbar_wait(full_bar(s), phase)) {
                     failed = true;
@@ -224,14 +229,19 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
                 for (int t = 0; t < T; t++) {
                     f4_copy_scales_on<CG>(on, sfa + 4 * t, sa_desc + off + (uint64_t)(t * 32));
 #pragma unroll
-                    for (int r = 0; r < R; r++) f4_copy_scales_on<CG>(on, sfb + 4 * (R * t + r), sb_desc + off + (uint64_t)((r * T + t) * 32));
+                    for (int r = 0; r < R; r++) f4_copy_scales_on<CG>(on, cfb + 4 * (R * t + r), sb_desc + off + (uint64_t)((r * T + t) * 32));
                 }
-                const int n = min(4, steps - 4 * kb);
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
+                auto mma = [&](int k) {
                     const int t = NV ? k : k >> 1, id = NV ? 0 : 2 * (k & 1);
-                    f4_mma_on<CG, NV>(k < n ? on : 0, d, a_desc + off + (uint64_t)(2 * k), b_desc + off + (uint64_t)(2 * k),
-                                      f4_idesc(CG * F4_BM, BN, NV, id), sfa + 4 * t, sfb + 4 * R * t + shift, (uint32_t)(kb | k));
+                    f4_mma_on<CG, NV>(on, d, a_desc + off + (uint64_t)(2 * k), b_desc + off + (uint64_t)(2 * k), f4_idesc(CG * F4_BM, BN, NV, id),
+                                      sfa + 4 * t, sfb + 4 * R * t, (uint32_t)(kb | k));
+                };
+                if (kb < full) {
+                    mma(0), mma(1), mma(2), mma(3);
+                } else {
+                    mma(0);
+                    if (steps - 4 * kb > 1) mma(1);
+                    if (steps - 4 * kb > 2) mma(2);
                 }
                 f4_commit_on<CG>(on, empty_bar(s));
                 seen++;
@@ -278,10 +288,7 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
             tmem_wait_ld();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {  // this warp is done with the accumulator buffer
-                if constexpr (CG == 1) mbar_arrive(acce_bar(buf));
-                else t2_arrive_remote(t2_mapa(acce_bar(buf), 0));
-            }
+            if (lane == 0) f4_release<CG>(acce_bar(buf));  // this warp is done with the accumulator buffer
             if (!ok || row0 >= M) continue;
 #pragma unroll
             for (int b = 0; b < NB; b++) {

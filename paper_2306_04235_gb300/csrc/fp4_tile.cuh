@@ -13,6 +13,14 @@ namespace mnmt {
 constexpr int F4_BM = 128;  // rows of a tile per CTA
 constexpr int F4_BLK = 2048;  // a warp's staging block: 32 rows of 64 bytes
 
+// An epilogue warp has read an accumulator (tcgen05.wait::ld): the leader's MMAs
+// may overwrite it.  Relaxed: nothing in memory is handed over, and a release
+// would wait for the warp's own stores of the tile before (16384 x 8192 x 2048: 142 us).
+template <int CG>
+__device__ __forceinline__ void f4_release(uint32_t bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(CG == 1 ? bar : t2_mapa(bar, 0)) : "memory");
+}
+
 // One lane of a converged warp.  The producer and MMA warps of a fast kernel run
 // their loops with all lanes and issue from this one by predicate (on): operands
 // that every lane computes alike stay in uniform registers, where a branch on the
