@@ -14,8 +14,9 @@
 // gW) G "MN-major" from tiles as they lie in memory: no transposed copies.  The
 // epilogue warps gather the straight-through masks of a tile before its sums are
 // ready and store through shared memory; two warps sum the bias gradient
-// meanwhile.  Grids of few tiles split the reduction; the parts are added in
-// their order by the CTA that finishes last.
+// meanwhile.
+// fp4_backward_finish: where the reduction of a product was split (few tiles, long
+// sums), adds the parts' sums in their order and applies masks.
 #include <type_traits>
 
 #include "fp4.cuh"
@@ -121,9 +122,7 @@ struct BwProduct {
     int rows, cols, red, a_mn;  // a_mn: A is stored [red][rows] (gW), else [rows][red]
     int chunk;                  // stages per accumulator
     int parts, len;             // parts of the reduction, stages of a part
-    float *partial;             // parts > 1: fp32 sums of each tile and part
-    int *tickets;               // and how many parts of a tile (of each CTA of a pair) are done
-    F4Out out;
+    F4Out out;                  // parts > 1: fp32 sums [parts][rows][ldy], without masks
     // straight-through mask: the float original and the scales of its packed form
     const void *orig;
     long ldo;
@@ -257,7 +256,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
     auto accf_bar = [&](int b) { return bars + 8u * (2 * STAGES + b); };
     auto acce_bar = [&](int b) { return bars + 8u * (2 * STAGES + 2 + b); };
     const uint32_t done_bar = bars + 8u * (2 * STAGES + 4);
-    uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);  // [0] tmem base, [1] abort, [2] consumed, [3] last part
+    uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);  // [0] tmem base, [1] abort, [2] consumed
     volatile uint32_t *abort_flag = misc + 1;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -283,18 +282,17 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
     // tile, part and corner of an item: the dimension of fewer tiles runs fastest
     struct At {
         int p, m, n, k0, k1;
-        long tile;
     };
     auto at = [&](int phase, long item) {
         At r;
         r.p = phase > 0;
         const BwProduct &p = a.p[r.p];
-        r.tile = item / p.parts;
-        r.k0 = (int)(item - r.tile * p.parts) * p.len;
+        const long tile = item / p.parts;
+        r.k0 = (int)(item - tile * p.parts) * p.len;
         r.k1 = min((p.red + BW_BK - 1) / BW_BK, r.k0 + p.len);
         const int m = mt(r.p), n = nt(r.p);
-        r.m = (int)(m <= n ? r.tile % m : r.tile / n) * CG * F4_BM;
-        r.n = (int)(m <= n ? r.tile / m : r.tile % n) * BN;
+        r.m = (int)(m <= n ? tile % m : tile / n) * CG * F4_BM;
+        r.n = (int)(m <= n ? tile / m : tile % n) * BN;
         return r;
     };
 
@@ -414,8 +412,9 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
         f4_commit<CG>(done_bar);
     } else if (warp == 1 && lane == 0) {
         pdl_allow_next();  // the leader's trigger decides
-    } else if (warp >= 2 + BW_EPI_WARPS) {
-        if (a.gb) bias_gradient(a, (int)blockIdx.x * BW_GB_WARPS + warp - 2 - BW_EPI_WARPS, (int)gridDim.x * BW_GB_WARPS);
+    } else if (warp >= 2 + BW_EPI_WARPS || a.n == 0) {
+        const int w = a.n == 0 ? BW_EPI_WARPS + BW_GB_WARPS : BW_GB_WARPS, first = 2 + BW_EPI_WARPS + BW_GB_WARPS - w;
+        if (a.gb && warp >= first) bias_gradient(a, (int)blockIdx.x * w + warp - first, (int)gridDim.x * w);
     } else if (warp >= 2) {
         // ---- epilogue ----
         constexpr int NB = BN / 64;
@@ -460,48 +459,15 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                     __syncwarp();
                     if (lane == 0) f4_release<CG>(acce_bar(buf));
                 }
-                bool store = ok && row0 < p.rows;
-                if (p.parts > 1) {
-                    // this part's sums to memory, 16 bytes per lane; the last part to finish adds all of them in order
-                    const size_t unit_f = (size_t)F4_BM * BN, at_f = ((size_t)ew * NB * 8 * 32 + lane) * 4;
-                    float *tile = p.partial + ((size_t)t.tile * CG + rank) * p.parts * unit_f;
-                    if (store) {
-                        float4 *o = reinterpret_cast<float4 *>(tile + (size_t)(t.k0 / p.len) * unit_f + at_f);
-#pragma unroll
-                        for (int b = 0; b < NB; b++)
-#pragma unroll
-                            for (int g = 0; g < 8; g++) o[(b * 8 + g) * 32] = make_float4(acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]);
-                    }
-                    __threadfence();
-                    asm volatile("bar.sync 1, %0;" ::"n"(BW_EPI_WARPS * 32) : "memory");
-                    if (ew == 0 && lane == 0) misc[3] = *abort_flag == 0 && atomicAdd(p.tickets + t.tile * CG + rank, 1) == p.parts - 1;
-                    asm volatile("bar.sync 1, %0;" ::"n"(BW_EPI_WARPS * 32) : "memory");
-                    store = store && misc[3];
-                    if (store) {
-                        __threadfence();
-#pragma unroll
-                        for (int b = 0; b < NB; b++)
-#pragma unroll
-                            for (int i = 0; i < 32; i++) acc[b][i] = 0.0f;
-                        const float4 *in4 = reinterpret_cast<const float4 *>(tile + at_f);
-                        for (int s = 0; s < p.parts; s++, in4 += unit_f / 4) {
-#pragma unroll
-                            for (int b = 0; b < NB; b++)
-#pragma unroll
-                                for (int g = 0; g < 8; g++) {
-                                    const float4 v = __ldcg(in4 + (b * 8 + g) * 32);
-                                    acc[b][4 * g] = __fadd_rn(acc[b][4 * g], v.x), acc[b][4 * g + 1] = __fadd_rn(acc[b][4 * g + 1], v.y);
-                                    acc[b][4 * g + 2] = __fadd_rn(acc[b][4 * g + 2], v.z), acc[b][4 * g + 3] = __fadd_rn(acc[b][4 * g + 3], v.w);
-                                }
-                        }
-                    }
-                }
+                if (!ok || row0 >= p.rows) continue;
+                F4Out o = p.out;
+                o.y = static_cast<uint8_t *>(o.y) + (p.parts > 1 ? (size_t)(t.k0 / p.len) * p.rows * o.ldy * 4 : 0);
 #pragma unroll
                 for (int b = 0; b < NB; b++) {
-                    if (!store || col0 + 32 * b >= p.cols) continue;
+                    if (col0 + 32 * b >= p.cols) continue;
 #pragma unroll
                     for (int i = 0; i < 32; i++) acc[b][i] = (in[b] >> i) & 1u ? __fmul_rn(acc[b][i], p.out.alpha) : 0.0f;
-                    f4_store_block(p.out, stg, acc[b], row0, col0 + 32 * b, p.rows, p.cols);
+                    f4_store_block(o, stg, acc[b], row0, col0 + 32 * b, p.rows, p.cols);
                 }
             }
         }
@@ -520,6 +486,72 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
     if (warp == 1) {
         if constexpr (CG == 1) tmem_free<L::COLS>(tbase);
         else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(L::COLS) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------
+// the parts of split products
+// ---------------------------------------------------------------------------
+struct FinishProduct {
+    const float *sums;  // [parts][rows][ld]
+    int parts, rows, cols, ld, blocks;
+    F4Out out;
+    const void *orig;
+    long ldo;
+    int otype;
+    Fp4Args q;
+};
+struct FinishArgs {
+    FinishProduct p[2];
+};
+
+// eight columns of a row per thread and step
+template <bool NV>
+__global__ void __launch_bounds__(256) fp4_backward_finish(FinishArgs a) {
+    pdl_grid_wait();
+    const bool second = (int)blockIdx.x >= a.p[0].blocks;
+    const FinishProduct &p = a.p[second];
+    const int groups = fp4_div_up(p.cols, 8), tiles_k = fp4_tiles_k(p.cols, NV);
+    const long total = (long)p.rows * groups, part = (long)p.rows * p.ld;
+    for (long i = ((int)blockIdx.x - (second ? a.p[0].blocks : 0)) * 256L + threadIdx.x; i < total; i += p.blocks * 256L) {
+        const int row = (int)(i / groups), c = (int)(i - (long)row * groups) * 8, n = p.cols - c;
+        const float *src = p.sums + (long)row * p.ld + c;
+        float s[8] = {};
+#pragma unroll 4
+        for (int k = 0; k < p.parts; k++) {
+            float v[8];
+            load8<float, true>(src + k * part, 8, v);  // rows are padded to eight columns
+#pragma unroll
+            for (int j = 0; j < 8; j++) s[j] = __fadd_rn(s[j], v[j]);
+        }
+        uint32_t in = 0xFFu;
+        if (p.orig) {
+            const float r = fp4_scale_of<NV>(p.q.scales[fp4_scale_at(row, c / fp4_block(NV), tiles_k)], p.q.g).r;
+            float v[8];
+            auto gather = [&](auto t) {
+                using T = decltype(t);
+                const T *o = static_cast<const T *>(p.orig) + row * p.ldo + c;
+                if ((reinterpret_cast<uintptr_t>(o) & 15) == 0 && n >= 8) load8<T, true>(o, 8, v);
+                else load8<T, false>(o, n, v);
+            };
+            if (p.otype == MNMT_F32) gather(float{});
+            else if (p.otype == MNMT_BF16) gather(__nv_bfloat16{});
+            else gather(__half{});
+            in = 0;
+#pragma unroll
+            for (int j = 0; j < 8; j++) in |= (uint32_t)(fabsf(__fmul_rn(v[j], r)) <= 6.0f) << j;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) s[j] = (in >> j) & 1u ? __fmul_rn(s[j], p.out.alpha) : 0.0f;
+        auto put = [&](auto t) {
+            using T = decltype(t);
+            T *o = static_cast<T *>(p.out.y) + row * p.out.ldy + c;
+            if (p.out.vec && n >= 8) store8<T, true>(o, 8, s);
+            else store8<T, false>(o, n, s);
+        };
+        if (p.out.type == MNMT_F32) put(float{});
+        else if (p.out.type == MNMT_BF16) put(__nv_bfloat16{});
+        else put(__half{});
     }
 }
 
@@ -571,13 +603,13 @@ Plan plan(int M, int N, int K, bool gx, bool gw) {
             work += (double)p.tiles[i] * fp4_div_up(red[i], BW_BK);
         }
         const double share = work / p.units;  // stages of a unit
+        const bool few = p.tiles[0] + p.tiles[1] < p.units;
         for (int i = 0; i < 2; i++) {
+            // a reduction longer than a unit's share is split into parts of about that
             const int nkb = fp4_div_up(red[i], BW_BK);
-            // parts of about a unit's share; whole reductions where there is a tile for every unit
-            int parts = want[i] && p.tiles[0] + p.tiles[1] < p.units ? (int)(nkb / (share > least ? share : least) + 0.5) : 1;
-            if (parts > 64) parts = 64;
-            if (parts < 1) parts = 1;
-            p.len[i] = fp4_div_up(nkb, parts);
+            double parts = want[i] && nkb > share ? nkb / (share > least ? share : least) + (few ? 0.5 : 0.99) : 1.0;
+            if (parts > 64.0) parts = 64.0;
+            p.len[i] = fp4_div_up(nkb, parts < 1.0 ? 1 : (int)parts);
             p.parts[i] = fp4_div_up(nkb, p.len[i]);
             p.items += p.tiles[i] * p.parts[i];
         }
@@ -586,11 +618,9 @@ Plan plan(int M, int N, int K, bool gx, bool gw) {
     }
     return best;
 }
-size_t partial_bytes(const Plan &p, int i) {
-    return p.parts[i] > 1 ? (size_t)p.tiles[i] * p.parts[i] * (p.pair ? 2 * F4_BM * 256 : F4_BM * 64) * 4 : 0;
-}
+size_t partial_bytes(const Plan &p, int i, int rows, int K) { return p.parts[i] > 1 ? (size_t)p.parts[i] * rows * up8(K) * 4 : 0; }
 
-// scratch: W and X in bf16, a copy of G, sums of the bias gradient, of split tiles, tickets
+// scratch: W and X in bf16, a copy of G, sums of the bias gradient, of split products, tickets
 struct Scratch {
     size_t w, x, g, gb, partial, tickets, bytes;
     int pk, pn, strips;
@@ -606,11 +636,11 @@ Scratch scratch(int M, int N, int K) {
     size_t most = 0;
     for (int w = 1; w < 4; w++) {
         const Plan p = plan(M, N, K, w & 1, w & 2);
-        const size_t n = partial_bytes(p, 0) + partial_bytes(p, 1);
+        const size_t n = partial_bytes(p, 0, M, K) + partial_bytes(p, 1, N, K);
         if (n > most) most = n;
     }
     s.tickets = s.partial + most;
-    s.bytes = s.tickets + up16((size_t)(s.strips + 4 * 2 * 152) * 4) + 16;
+    s.bytes = s.tickets + up16((size_t)s.strips * 4) + 16;
     return s;
 }
 
@@ -618,8 +648,9 @@ template <int CG, int BN, bool NV>
 cudaError_t bw_launch(const CUtensorMap (&tm)[4], const BwArgs &a, long items, int *status, cudaStream_t st) {
     const long fit = CG == 2 ? g_bw_pairs : device_sm_count();
     // the bias gradient's warps take the whole GPU where the products do not
-    const long gb = a.gb ? ((long)fp4_div_up(a.N, GB_COLS) * fp4_div_up(a.M, GB_ROWS) + CG * BW_GB_WARPS - 1) / (CG * BW_GB_WARPS) : 0;
+    const long gb = a.gb ? (long)fp4_div_up(a.N, GB_COLS) * fp4_div_up(a.M, GB_ROWS) / (CG * BW_GB_WARPS) : 0;
     if (items < gb) items = gb;
+    if (items < 1) items = 1;
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, (int)(items < fit ? items : fit), BW_THREADS, BwLayout<CG, BN>::SMEM, st, attr);
     return cudaLaunchKernelEx(&cfg, fp4_backward_gemm<CG, BN, NV>, tm[0], tm[1], tm[2], tm[3], a, status);
@@ -670,7 +701,10 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
     a.p[0].parts = a.p[1].parts = 1;
     CUtensorMap tm[4];
     memset(tm, 0, sizeof(tm));
-    float *partial = reinterpret_cast<float *>(ws + s.partial);
+    FinishArgs f;
+    memset(&f, 0, sizeof(f));
+    int split = 0;
+    uint8_t *partial = ws + s.partial;
     // the longer part first
     const bool input_first = pl.len[0] >= pl.len[1];
     for (int i = 0; i < 2; i++) {
@@ -681,17 +715,22 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
         a.n++;
         r.rows = input ? M : N, r.cols = K, r.red = input ? N : M, r.a_mn = !input;
         r.out = input ? F4Out{b.gx, b.ldgx, b.xdtype, 0, 0, b.nv ? b.w.g : 1.0f, nullptr} : F4Out{b.gw, b.ldgw, MNMT_F32, 0, 0, b.nv ? b.x.g : 1.0f, nullptr};
+        r.out.vec = out_vec(r.out.y, r.out.ldy, r.out.type);
         r.orig = input ? b.xo : b.wo, r.ldo = input ? b.ldx : b.ldw, r.otype = input ? b.xdtype : b.wdtype;
         r.q = input ? b.x : b.w;
-        r.chunk = r.out.type == MNMT_F32 ? BW_CHUNK : 1 << 24;
         r.parts = pl.parts[!input], r.len = pl.len[!input];
         if (r.parts > 1) {
-            r.partial = partial;
-            partial += partial_bytes(pl, !input) / 4;
-            r.tickets = tickets + p.n_tickets;
-            p.n_tickets += (int)pl.tiles[!input] * (pl.pair ? 2 : 1);
+            FinishProduct &q = f.p[split++];
+            q.sums = reinterpret_cast<const float *>(partial);
+            q.parts = r.parts, q.rows = r.rows, q.cols = K, q.ld = s.pk;
+            q.out = r.out, q.orig = r.orig, q.ldo = r.ldo, q.otype = r.otype, q.q = r.q;
+            const long n = ((long)r.rows * fp4_div_up(K, 8) + 255) / 256, most = 8L * device_sm_count();
+            q.blocks = (int)(n < most ? n : most);
+            r.out = F4Out{partial, s.pk, MNMT_F32, 1, 0, 1.0f, nullptr};
+            r.orig = nullptr;
+            partial += partial_bytes(pl, !input, r.rows, K);
         }
-        r.out.vec = out_vec(r.out.y, r.out.ldy, r.out.type);
+        r.chunk = r.out.type == MNMT_F32 ? BW_CHUNK : 1 << 24;
         if (!encode_bf16(t, a.g, N, M, a.ldg, input ? F4_BM : 64) || !encode_bf16(t + 1, input ? p.w16 : p.x16, K, input ? N : M, s.pk, 64))
             return cudaErrorInvalidValue;
     }
@@ -703,8 +742,11 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
     p.bx = p.x16 ? blocks(M * groups) : 0;
     launch_pdl(b.nv ? fp4_backward_prepare<true> : fp4_backward_prepare<false>, p.bw + p.bx + (copy ? blocks((long)M * s.pn / 8) : 1), 256, 0, st, p);
     if ((err = cudaGetLastError()) != cudaSuccess) return err;
-    if (pl.pair) return b.nv ? bw_launch<2, 256, true>(tm, a, pl.items, b.status, st) : bw_launch<2, 256, false>(tm, a, pl.items, b.status, st);
-    return b.nv ? bw_launch<1, 64, true>(tm, a, pl.items, b.status, st) : bw_launch<1, 64, false>(tm, a, pl.items, b.status, st);
+    if (pl.pair) err = b.nv ? bw_launch<2, 256, true>(tm, a, pl.items, b.status, st) : bw_launch<2, 256, false>(tm, a, pl.items, b.status, st);
+    else err = b.nv ? bw_launch<1, 64, true>(tm, a, pl.items, b.status, st) : bw_launch<1, 64, false>(tm, a, pl.items, b.status, st);
+    if (err != cudaSuccess || !split) return err;
+    launch_pdl(b.nv ? fp4_backward_finish<true> : fp4_backward_finish<false>, f.p[0].blocks + f.p[1].blocks, 256, 0, st, f);
+    return cudaGetLastError();
 }
 
 }  // namespace mnmt

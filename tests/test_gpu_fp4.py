@@ -268,7 +268,8 @@ def test_linear_backward(fmt, M, N, K, ty, wty, pad):
 
 
 @pytest.mark.parametrize("fmt", ["mx", "nv"])
-@pytest.mark.parametrize("M,N,K,pad", [(3000, 1100, 1300, 0), (700, 5003, 2056, 3), (20000, 520, 264, 8)])
+@pytest.mark.parametrize("M,N,K,pad", [(3000, 1100, 1300, 0), (700, 5003, 2056, 3), (20000, 520, 264, 8), (300, 16000, 500, 0),
+                                       (9001, 200, 72, 3)])
 def test_linear_backward_of_many_tiles(fmt, M, N, K, pad):
     """Grids of CTA pairs and long sums, against float64."""
     x, w, g, xq, xv, xin, wq, wv, win = gradient_case(fmt, M, N, K, "bf16", "f32", pad)
