@@ -7,14 +7,15 @@
 // code times its block scale (a power of two, or an E4M3 number) has at most six
 // significant bits and is exact in bf16, products are exact in fp32.
 //
-// fp4_backward_prepare (memory): W and X decoded to bf16 in their stored order, a
-// copy of G where TMA cannot read it (rows not 16-byte aligned), tickets zeroed.
+// fp4_backward_prepare (memory): W and X decoded to bf16 in their stored order, the
+// straight-through masks as bits, a copy of G where TMA cannot read it (rows not
+// 16-byte aligned), tickets zeroed.
 // fp4_backward_gemm, both products in one persistent launch (tensor cores): the
 // reduction index is the row of a stored operand, so the MMAs read W, X and (for
 // gW) G "MN-major" from tiles as they lie in memory: no transposed copies.  The
-// epilogue warps gather the straight-through masks of a tile before its sums are
-// ready and store through shared memory; two warps sum the bias gradient
-// meanwhile.
+// epilogue warps apply masks and store through shared memory (masks from the float
+// originals there, a row per lane, waited for memory: gX of 16384 x 512 x 2048 130
+// us, without masks 64); two warps sum the bias gradient meanwhile.
 // fp4_backward_finish: where the reduction of a product was split (few tiles, long
 // sums), adds the parts' sums in their order and applies masks.
 #include <type_traits>
@@ -26,40 +27,59 @@
 namespace mnmt {
 namespace {
 
+// what is made of a packed matrix: its values in bf16 (without the tensor scale),
+// rows pk apart, and a bit per element, set where the float original lies within
+// the range of its block, rows of mp bytes; each may be null
+struct PrepMatrix {
+    Fp4Args q;
+    __nv_bfloat16 *values;
+    uint8_t *mask;
+    const void *orig;
+    long ldo;
+    int otype, blocks;
+};
 struct PrepArgs {
-    Fp4Args w, x;
+    PrepMatrix m[2];
     const __nv_bfloat16 *g;
     long ldg;
-    __nv_bfloat16 *w16, *x16, *g16;  // each may be null
+    __nv_bfloat16 *g16;  // may be null
     int *tickets;
-    int n_tickets, M, N, pk, pn;
-    int bw, bx;  // blocks of W, of X; the rest take G
+    int n_tickets, M, N, pk, mp, pn;
 };
 
-// rows of a packed matrix as bf16 (without the tensor scale); a thread takes 32 elements of a row
-template <bool NV>
-MNMT_DEV void decode_rows(const Fp4Args &q, __nv_bfloat16 *out, int ld, long first, long step) {
-    const int groups = fp4_div_up(q.cols, 32), tiles_k = fp4_tiles_k(q.cols, NV);
-    const long total = (long)q.rows * groups;
-    for (long i = first; i < total; i += step) {
-        const int row = (int)(i / groups), c = (int)(i - (long)row * groups) * 32;
-        const uint4 codes = *reinterpret_cast<const uint4 *>(q.codes + (size_t)row * fp4_pitch(q.cols) + (c >> 1));
-        const uint32_t cw[4] = {codes.x, codes.y, codes.z, codes.w};
-        float S[2];
-        const uint8_t *sp = q.scales + fp4_scale_at(row, c / fp4_block(NV), tiles_k);
-        S[0] = fp4_scale_of<NV>(sp[0], 1.0f).S;
-        S[1] = NV ? fp4_scale_of<NV>(sp[1], 1.0f).S : S[0];
-        __nv_bfloat16 *o = out + (size_t)row * ld + c;
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            uint32_t w[4];
+// eight elements of a row per thread and step
+template <bool NV, typename T>
+MNMT_DEV void prepare_rows(const PrepMatrix &m, int pk, int mp, int block) {
+    const int groups = pk / 8, tiles_k = fp4_tiles_k(m.q.cols, NV);
+    const size_t pitch = fp4_pitch(m.q.cols);
+    const long total = (long)m.q.rows * groups, step = m.blocks * 256L;
+    const T *orig = static_cast<const T *>(m.orig);
+    const bool vec = ((reinterpret_cast<uintptr_t>(orig) | (uintptr_t)m.ldo * sizeof(T)) & 15) == 0;
+#pragma unroll 2
+    for (long i = block * 256L + threadIdx.x; i < total; i += step) {
+        const int row = (int)(i / groups), c = (int)(i - (long)row * groups) * 8;
+        const uint32_t byte = m.q.scales[fp4_scale_at(row, c / fp4_block(NV), tiles_k)];
+        if (m.values) {
+            const uint32_t codes = *reinterpret_cast<const uint32_t *>(m.q.codes + row * pitch + (c >> 1));
+            const float S = fp4_scale_of<NV>(byte, 1.0f).S;
+            float v[8];
 #pragma unroll
             for (int b = 0; b < 4; b++) {
-                const float2 f = fp4_float2((cw[j] >> (8 * b)) & 0xFFu);
-                const __nv_bfloat162 h = __floats2bfloat162_rn(__fmul_rn(f.x, S[j >> 1]), __fmul_rn(f.y, S[j >> 1]));
-                w[b] = *reinterpret_cast<const uint32_t *>(&h);
+                const float2 f = fp4_float2((codes >> (8 * b)) & 0xFFu);
+                v[2 * b] = __fmul_rn(f.x, S), v[2 * b + 1] = __fmul_rn(f.y, S);
             }
-            if (c + 8 * j < ld) *reinterpret_cast<uint4 *>(o + 8 * j) = make_uint4(w[0], w[1], w[2], w[3]);
+            store8<__nv_bfloat16, true>(m.values + (size_t)row * pk + c, 8, v);
+        }
+        if (m.mask) {
+            const float r = fp4_scale_of<NV>(byte, m.q.g).r;
+            const T *src = orig + row * m.ldo + c;
+            float v[8];
+            if (vec && c + 8 <= m.q.cols) load8<T, true>(src, 8, v);
+            else load8<T, false>(src, m.q.cols - c, v);
+            uint32_t in = 0;
+#pragma unroll
+            for (int k = 0; k < 8; k++) in |= (uint32_t)(fabsf(__fmul_rn(v[k], r)) <= 6.0f) << k;
+            m.mask[(size_t)row * mp + (c >> 3)] = (uint8_t)in;
         }
     }
 }
@@ -67,15 +87,19 @@ MNMT_DEV void decode_rows(const Fp4Args &q, __nv_bfloat16 *out, int ld, long fir
 template <bool NV>
 __global__ void __launch_bounds__(256) fp4_backward_prepare(PrepArgs a) {
     pdl_grid_wait();
-    if ((int)blockIdx.x < a.bw) {
-        decode_rows<NV>(a.w, a.w16, a.pk, (long)blockIdx.x * 256 + threadIdx.x, (long)a.bw * 256);
-        return;
+    int block = blockIdx.x;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const PrepMatrix &m = a.m[i];
+        if (block < m.blocks) {
+            if (m.otype == MNMT_F32) prepare_rows<NV, float>(m, a.pk, a.mp, block);
+            else if (m.otype == MNMT_BF16) prepare_rows<NV, __nv_bfloat16>(m, a.pk, a.mp, block);
+            else prepare_rows<NV, __half>(m, a.pk, a.mp, block);
+            return;
+        }
+        block -= m.blocks;
     }
-    if ((int)blockIdx.x < a.bw + a.bx) {
-        decode_rows<NV>(a.x, a.x16, a.pk, (long)(blockIdx.x - a.bw) * 256 + threadIdx.x, (long)a.bx * 256);
-        return;
-    }
-    const int first = ((int)blockIdx.x - a.bw - a.bx) * 256 + threadIdx.x, step = ((int)gridDim.x - a.bw - a.bx) * 256;
+    const int first = block * 256 + threadIdx.x, step = ((int)gridDim.x - a.m[0].blocks - a.m[1].blocks) * 256;
     for (int i = first; i < a.n_tickets; i += step) a.tickets[i] = 0;
     if (!a.g16) return;
     const int groups = a.pn / 8;
@@ -123,11 +147,8 @@ struct BwProduct {
     int chunk;                  // stages per accumulator
     int parts, len;             // parts of the reduction, stages of a part
     F4Out out;                  // parts > 1: fp32 sums [parts][rows][ldy], without masks
-    // straight-through mask: the float original and the scales of its packed form
-    const void *orig;
-    long ldo;
-    int otype;
-    Fp4Args q;
+    const uint8_t *mask;        // straight-through bits, rows of mp bytes, or null
+    int mp;
 };
 struct BwArgs {
     BwProduct p[2];
@@ -151,33 +172,6 @@ __device__ __forceinline__ uint64_t mn128_desc(uint32_t saddr) {
 // kind::f16, D fp32, A and B bf16, B MN-major
 __host__ __device__ constexpr uint32_t bw_idesc(int m, int n, bool a_mn) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
-}
-
-// bit i: element (row, col + i) of the original lies within the range of its block
-template <bool NV>
-__device__ __noinline__ uint32_t inside32(const BwProduct &p, int row, int col) {
-    if (!p.orig) return 0xFFFFFFFFu;
-    const uint8_t *sp = p.q.scales + fp4_scale_at(row, col / fp4_block(NV), fp4_tiles_k(p.cols, NV));
-    const float r0 = fp4_scale_of<NV>(sp[0], p.q.g).r, r1 = NV && col + 16 < p.cols ? fp4_scale_of<NV>(sp[1], p.q.g).r : r0;
-    uint32_t m = 0;
-    auto gather = [&](auto t) {
-        using T = decltype(t);
-        const T *src = static_cast<const T *>(p.orig) + row * p.ldo + col;
-        const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            if (col + 8 * j >= p.cols) break;
-            float v[8];
-            if (vec && col + 8 * j + 8 <= p.cols) load8<T, true>(src + 8 * j, 8, v);
-            else load8<T, false>(src + 8 * j, p.cols - col - 8 * j, v);
-#pragma unroll
-            for (int k = 0; k < 8; k++) m |= (uint32_t)(fabsf(__fmul_rn(v[k], j < 2 ? r0 : r1)) <= 6.0f) << (8 * j + k);
-        }
-    };
-    if (p.otype == MNMT_F32) gather(float{});
-    else if (p.otype == MNMT_BF16) gather(__nv_bfloat16{});
-    else gather(__half{});
-    return m;
 }
 
 // The bias gradient by warps w of n: 128 rows x 256 columns at a time, eight
@@ -239,7 +233,7 @@ __device__ __noinline__ void bias_gradient(const BwArgs &a, int w, int n) {
 // Persistent, 384 threads per CTA: warp 0 lane 0 loads tiles by TMA, warp 1 lane
 // 0 issues MMAs into two TMEM accumulators, warps 2..9 drain them, warps 10 and
 // 11 sum the bias gradient.  An item is a part of a tile.
-template <int CG, int BN, bool NV>
+template <int CG, int BN>
 __global__ void __launch_bounds__(BW_THREADS, 1)
     fp4_backward_gemm(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0,
                       const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1,
@@ -429,7 +423,20 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                 const int row0 = t.m + (int)rank * F4_BM + 32 * q, col0 = t.n + cw;
                 uint32_t in[NB];
 #pragma unroll
-                for (int b = 0; b < NB; b++) in[b] = row0 + lane < p.rows && col0 + 32 * b < p.cols ? inside32<NV>(p, row0 + lane, col0 + 32 * b) : 0;
+                for (int b = 0; b < NB; b++) in[b] = 0xFFFFFFFFu;
+                if (p.mask && row0 + lane < p.rows) {
+                    const uint8_t *src = p.mask + (size_t)(row0 + lane) * p.mp + (col0 >> 3);
+                    if constexpr (NB == 4) {
+                        if (col0 < p.cols) {
+                            const uint4 w = *reinterpret_cast<const uint4 *>(src);
+                            in[0] = w.x, in[1] = w.y, in[2] = w.z, in[3] = w.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < NB; b++)
+                            if (col0 + 32 * b < p.cols) in[b] = reinterpret_cast<const uint32_t *>(src)[b];
+                    }
+                }
                 float acc[NB][32];
 #pragma unroll
                 for (int b = 0; b < NB; b++)
@@ -496,22 +503,19 @@ struct FinishProduct {
     const float *sums;  // [parts][rows][ld]
     int parts, rows, cols, ld, blocks;
     F4Out out;
-    const void *orig;
-    long ldo;
-    int otype;
-    Fp4Args q;
+    const uint8_t *mask;
+    int mp;
 };
 struct FinishArgs {
     FinishProduct p[2];
 };
 
 // eight columns of a row per thread and step
-template <bool NV>
 __global__ void __launch_bounds__(256) fp4_backward_finish(FinishArgs a) {
     pdl_grid_wait();
     const bool second = (int)blockIdx.x >= a.p[0].blocks;
     const FinishProduct &p = a.p[second];
-    const int groups = fp4_div_up(p.cols, 8), tiles_k = fp4_tiles_k(p.cols, NV);
+    const int groups = fp4_div_up(p.cols, 8);
     const long total = (long)p.rows * groups, part = (long)p.rows * p.ld;
     for (long i = ((int)blockIdx.x - (second ? a.p[0].blocks : 0)) * 256L + threadIdx.x; i < total; i += p.blocks * 256L) {
         const int row = (int)(i / groups), c = (int)(i - (long)row * groups) * 8, n = p.cols - c;
@@ -524,23 +528,7 @@ __global__ void __launch_bounds__(256) fp4_backward_finish(FinishArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; j++) s[j] = __fadd_rn(s[j], v[j]);
         }
-        uint32_t in = 0xFFu;
-        if (p.orig) {
-            const float r = fp4_scale_of<NV>(p.q.scales[fp4_scale_at(row, c / fp4_block(NV), tiles_k)], p.q.g).r;
-            float v[8];
-            auto gather = [&](auto t) {
-                using T = decltype(t);
-                const T *o = static_cast<const T *>(p.orig) + row * p.ldo + c;
-                if ((reinterpret_cast<uintptr_t>(o) & 15) == 0 && n >= 8) load8<T, true>(o, 8, v);
-                else load8<T, false>(o, n, v);
-            };
-            if (p.otype == MNMT_F32) gather(float{});
-            else if (p.otype == MNMT_BF16) gather(__nv_bfloat16{});
-            else gather(__half{});
-            in = 0;
-#pragma unroll
-            for (int j = 0; j < 8; j++) in |= (uint32_t)(fabsf(__fmul_rn(v[j], r)) <= 6.0f) << j;
-        }
+        const uint32_t in = p.mask ? p.mask[(size_t)row * p.mp + (c >> 3)] : 0xFFu;
 #pragma unroll
         for (int j = 0; j < 8; j++) s[j] = (in >> j) & 1u ? __fmul_rn(s[j], p.out.alpha) : 0.0f;
         auto put = [&](auto t) {
@@ -567,14 +555,14 @@ bool encode_bf16(CUtensorMap *tm, const void *p, int cols, int rows, long ld, in
     return encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p, cols, rows, (cuuint64_t)ld * 2, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int CG, int BN, bool NV>
+template <int CG, int BN>
 cudaError_t bw_init() {
-    cudaError_t err = cudaFuncSetAttribute(fp4_backward_gemm<CG, BN, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)BwLayout<CG, BN>::SMEM);
+    cudaError_t err = cudaFuncSetAttribute(fp4_backward_gemm<CG, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)BwLayout<CG, BN>::SMEM);
     if (err != cudaSuccess || CG == 1) return err;
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, 64, BW_THREADS, BwLayout<CG, BN>::SMEM, nullptr, attr);
     int n = 0;
-    err = cudaOccupancyMaxActiveClusters(&n, fp4_backward_gemm<CG, BN, NV>, &cfg);
+    err = cudaOccupancyMaxActiveClusters(&n, fp4_backward_gemm<CG, BN>, &cfg);
     if (err == cudaSuccess && (g_bw_pairs == 0 || n < g_bw_pairs)) g_bw_pairs = n;
     return err;
 }
@@ -607,7 +595,7 @@ Plan plan(int M, int N, int K, bool gx, bool gw) {
         for (int i = 0; i < 2; i++) {
             // a reduction longer than a unit's share is split into parts of about that
             const int nkb = fp4_div_up(red[i], BW_BK);
-            double parts = want[i] && nkb > share ? nkb / (share > least ? share : least) + (few ? 0.5 : 0.99) : 1.0;
+            double parts = want[i] && nkb > share ? nkb / (share > least ? share : least) + (few ? 0.0 : 0.99) : 1.0;
             if (parts > 64.0) parts = 64.0;
             p.len[i] = fp4_div_up(nkb, parts < 1.0 ? 1 : (int)parts);
             p.parts[i] = fp4_div_up(nkb, p.len[i]);
@@ -620,17 +608,19 @@ Plan plan(int M, int N, int K, bool gx, bool gw) {
 }
 size_t partial_bytes(const Plan &p, int i, int rows, int K) { return p.parts[i] > 1 ? (size_t)p.parts[i] * rows * up8(K) * 4 : 0; }
 
-// scratch: W and X in bf16, a copy of G, sums of the bias gradient, of split products, tickets
+// scratch: W and X in bf16, their masks, a copy of G, sums of the bias gradient, of split products, tickets
 struct Scratch {
-    size_t w, x, g, gb, partial, tickets, bytes;
-    int pk, pn, strips;
+    size_t w, x, mw, mx, g, gb, partial, tickets, bytes;
+    int pk, mp, pn, strips;
 };
 Scratch scratch(int M, int N, int K) {
     Scratch s;
-    s.pk = up8(K), s.pn = up8(N), s.strips = fp4_div_up(N, GB_COLS);
+    s.pk = up8(K), s.mp = (int)up16(fp4_div_up(K, 8)), s.pn = up8(N), s.strips = fp4_div_up(N, GB_COLS);
     s.w = 0;
     s.x = up16((size_t)N * s.pk * 2);
-    s.g = s.x + up16((size_t)M * s.pk * 2);
+    s.mw = s.x + up16((size_t)M * s.pk * 2);
+    s.mx = s.mw + (size_t)N * s.mp;
+    s.g = s.mx + (size_t)M * s.mp;
     s.gb = s.g + up16((size_t)M * s.pn * 2);
     s.partial = s.gb + (size_t)fp4_div_up(M, GB_ROWS) * s.strips * GB_COLS * 4;
     size_t most = 0;
@@ -644,7 +634,7 @@ Scratch scratch(int M, int N, int K) {
     return s;
 }
 
-template <int CG, int BN, bool NV>
+template <int CG, int BN>
 cudaError_t bw_launch(const CUtensorMap (&tm)[4], const BwArgs &a, long items, int *status, cudaStream_t st) {
     const long fit = CG == 2 ? g_bw_pairs : device_sm_count();
     // the bias gradient's warps take the whole GPU where the products do not
@@ -653,16 +643,14 @@ cudaError_t bw_launch(const CUtensorMap (&tm)[4], const BwArgs &a, long items, i
     if (items < 1) items = 1;
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, (int)(items < fit ? items : fit), BW_THREADS, BwLayout<CG, BN>::SMEM, st, attr);
-    return cudaLaunchKernelEx(&cfg, fp4_backward_gemm<CG, BN, NV>, tm[0], tm[1], tm[2], tm[3], a, status);
+    return cudaLaunchKernelEx(&cfg, fp4_backward_gemm<CG, BN>, tm[0], tm[1], tm[2], tm[3], a, status);
 }
 
 }  // namespace
 
 cudaError_t fp4_backward_init() {
-    cudaError_t err = bw_init<2, 256, false>();
-    if (err == cudaSuccess) err = bw_init<2, 256, true>();
-    if (err == cudaSuccess) err = bw_init<1, 64, false>();
-    if (err == cudaSuccess) err = bw_init<1, 64, true>();
+    cudaError_t err = bw_init<2, 256>();
+    if (err == cudaSuccess) err = bw_init<1, 64>();
     return err;
 }
 
@@ -685,13 +673,16 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
     const bool products = b.gx || b.gw;
     const bool copy = products && ((reinterpret_cast<uintptr_t>(b.g) & 15) || b.ldg % 8);
     PrepArgs p;
-    p.w = b.w, p.x = b.x;
+    memset(&p, 0, sizeof(p));
+    p.m[0].q = b.w, p.m[1].q = b.x;
+    if (b.gx) p.m[0].values = reinterpret_cast<__nv_bfloat16 *>(ws + s.w);
+    if (b.gw) p.m[1].values = reinterpret_cast<__nv_bfloat16 *>(ws + s.x);
+    if (b.gw && b.wo) p.m[0].mask = ws + s.mw, p.m[0].orig = b.wo, p.m[0].ldo = b.ldw, p.m[0].otype = b.wdtype;
+    if (b.gx && b.xo) p.m[1].mask = ws + s.mx, p.m[1].orig = b.xo, p.m[1].ldo = b.ldx, p.m[1].otype = b.xdtype;
     p.g = static_cast<const __nv_bfloat16 *>(b.g), p.ldg = b.ldg;
-    p.w16 = b.gx ? reinterpret_cast<__nv_bfloat16 *>(ws + s.w) : nullptr;
-    p.x16 = b.gw ? reinterpret_cast<__nv_bfloat16 *>(ws + s.x) : nullptr;
     p.g16 = copy ? reinterpret_cast<__nv_bfloat16 *>(ws + s.g) : nullptr;
     p.tickets = tickets, p.n_tickets = s.strips;
-    p.M = M, p.N = N, p.pk = s.pk, p.pn = s.pn;
+    p.M = M, p.N = N, p.pk = s.pk, p.mp = s.mp, p.pn = s.pn;
 
     BwArgs a;
     memset(&a, 0, sizeof(a));
@@ -716,36 +707,33 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
         r.rows = input ? M : N, r.cols = K, r.red = input ? N : M, r.a_mn = !input;
         r.out = input ? F4Out{b.gx, b.ldgx, b.xdtype, 0, 0, b.nv ? b.w.g : 1.0f, nullptr} : F4Out{b.gw, b.ldgw, MNMT_F32, 0, 0, b.nv ? b.x.g : 1.0f, nullptr};
         r.out.vec = out_vec(r.out.y, r.out.ldy, r.out.type);
-        r.orig = input ? b.xo : b.wo, r.ldo = input ? b.ldx : b.ldw, r.otype = input ? b.xdtype : b.wdtype;
-        r.q = input ? b.x : b.w;
+        r.mask = p.m[input].mask, r.mp = s.mp;
         r.parts = pl.parts[!input], r.len = pl.len[!input];
         if (r.parts > 1) {
             FinishProduct &q = f.p[split++];
             q.sums = reinterpret_cast<const float *>(partial);
             q.parts = r.parts, q.rows = r.rows, q.cols = K, q.ld = s.pk;
-            q.out = r.out, q.orig = r.orig, q.ldo = r.ldo, q.otype = r.otype, q.q = r.q;
+            q.out = r.out, q.mask = r.mask, q.mp = s.mp;
             const long n = ((long)r.rows * fp4_div_up(K, 8) + 255) / 256, most = 8L * device_sm_count();
             q.blocks = (int)(n < most ? n : most);
             r.out = F4Out{partial, s.pk, MNMT_F32, 1, 0, 1.0f, nullptr};
-            r.orig = nullptr;
+            r.mask = nullptr;
             partial += partial_bytes(pl, !input, r.rows, K);
         }
         r.chunk = r.out.type == MNMT_F32 ? BW_CHUNK : 1 << 24;
-        if (!encode_bf16(t, a.g, N, M, a.ldg, input ? F4_BM : 64) || !encode_bf16(t + 1, input ? p.w16 : p.x16, K, input ? N : M, s.pk, 64))
+        if (!encode_bf16(t, a.g, N, M, a.ldg, input ? F4_BM : 64) || !encode_bf16(t + 1, p.m[!input].values, K, input ? N : M, s.pk, 64))
             return cudaErrorInvalidValue;
     }
 
-    // blocks in proportion to the bytes each part moves, four per SM of each at most
-    const long groups = fp4_div_up(K, 32), cap = 4L * device_sm_count();
+    const long cap = 8L * device_sm_count();
     auto blocks = [&](long threads) { return (int)((threads + 255) / 256 < cap ? (threads + 255) / 256 : cap); };
-    p.bw = p.w16 ? blocks(N * groups) : 0;
-    p.bx = p.x16 ? blocks(M * groups) : 0;
-    launch_pdl(b.nv ? fp4_backward_prepare<true> : fp4_backward_prepare<false>, p.bw + p.bx + (copy ? blocks((long)M * s.pn / 8) : 1), 256, 0, st, p);
+    for (PrepMatrix &m : p.m) m.blocks = m.values || m.mask ? blocks((long)m.q.rows * s.pk / 8) : 0;
+    const int rest = copy ? blocks((long)M * s.pn / 8) : 1;
+    launch_pdl(b.nv ? fp4_backward_prepare<true> : fp4_backward_prepare<false>, p.m[0].blocks + p.m[1].blocks + rest, 256, 0, st, p);
     if ((err = cudaGetLastError()) != cudaSuccess) return err;
-    if (pl.pair) err = b.nv ? bw_launch<2, 256, true>(tm, a, pl.items, b.status, st) : bw_launch<2, 256, false>(tm, a, pl.items, b.status, st);
-    else err = b.nv ? bw_launch<1, 64, true>(tm, a, pl.items, b.status, st) : bw_launch<1, 64, false>(tm, a, pl.items, b.status, st);
+    err = pl.pair ? bw_launch<2, 256>(tm, a, pl.items, b.status, st) : bw_launch<1, 64>(tm, a, pl.items, b.status, st);
     if (err != cudaSuccess || !split) return err;
-    launch_pdl(b.nv ? fp4_backward_finish<true> : fp4_backward_finish<false>, f.p[0].blocks + f.p[1].blocks, 256, 0, st, f);
+    launch_pdl(fp4_backward_finish, f.p[0].blocks + f.p[1].blocks, 256, 0, st, f);
     return cudaGetLastError();
 }
 
