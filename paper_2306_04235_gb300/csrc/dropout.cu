@@ -48,72 +48,83 @@ MNMT_DEV uint32_t keep8(const uint4 w, uint32_t thr) {
     return k;
 }
 
-template <typename T, bool VEC>
-MNMT_DEV void load_at(const T *row, int c, int cols, float (&v)[8]) {
-    if (VEC && c + 8 <= cols) load8<T, true>(row + c, 8, v);
-    else load8<T, false>(row + c, cols - c, v);
-}
-template <typename T, bool VEC>
-MNMT_DEV void store_at(T *row, int c, int cols, const float (&v)[8]) {
-    if (VEC && c + 8 <= cols) store8<T, true>(row + c, 8, v);
-    else store8<T, false>(row + c, cols - c, v);
-}
-
 // T: type of x and gx; O: type of out, r, g and gr
 template <typename T, typename O, bool VEC>
-__global__ void __launch_bounds__(256) dropout_kernel(const T *x, long ldx, const O *r, long ldr, float gamma, uint32_t thr,
-                                                      float scale, Philox ph, int relu, int M, int d, O *out, long ldo) {
+__global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_kernel(const T *x, long ldx, bool alx, const O *r, long ldr, bool alr, float gamma,
+                                                                  uint32_t thr, float scale, Philox ph, int relu, int M, int d, O *out, long ldo,
+                                                                  bool alo) {
     pdl_grid_wait();
-    const int groups = (d + 7) >> 3;
-    const long total = (long)M * groups;
-    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long)gridDim.x * 256) {
-        const int row = (int)(i / groups), cg = (int)(i - (long)row * groups);
-        float v[8], u[8];
-        load_at<T, VEC>(x + row * ldx, cg * 8, d, v);
-        if (r) load_at<O, VEC>(r + row * ldr, cg * 8, d, u);
-        const uint32_t keep = keep8(ph((uint32_t)cg, (uint32_t)row), thr);
+    MNMT_ROW_BUF(buf, VEC);
+    constexpr int U = 2;  // chunks in flight
+    for (Walk w(d); w.row < M;) {
+        Raw8<T> rx[U];
+        Raw8<O> rr[U];
+        long row[U];
+        int c0[U];
 #pragma unroll
-        for (int k = 0; k < 8; k++) {
-            float y = relu && v[k] <= 0.0f ? 0.0f : v[k];  // a NaN stays
-            y = (keep >> k) & 1u ? __fmul_rn(y, scale) : 0.0f;
-            v[k] = r ? __fadd_rn(__fmul_rn(gamma, u[k]), y) : y;
+        for (int u = 0; u < U; u++) {
+            row[u] = w.row, c0[u] = w.chunk * ROW_CHUNK;
+            if (row[u] < M) {
+                fetch8<T, VEC>(x + row[u] * ldx, c0[u], d, alx, rx[u]);
+                if (r) fetch8<O, VEC>(r + row[u] * ldr, c0[u], d, alr, rr[u]);
+            }
+            w.next();
         }
-        store_at<O, VEC>(out + row * ldo, cg * 8, d, v);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (row[u] >= M) break;
+            const uint32_t keep = keep8(ph((uint32_t)(c0[u] >> 3) + (threadIdx.x & 31), (uint32_t)row[u]), thr);
+            float v[8], s[8];
+            settle8<T, VEC>(rx[u], alx, buf, v);
+            if (r) settle8<O, VEC>(rr[u], alr, buf, s);
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                float y = relu && v[k] <= 0.0f ? 0.0f : v[k];  // a NaN stays
+                y = (keep >> k) & 1u ? __fmul_rn(y, scale) : 0.0f;
+                v[k] = r ? __fadd_rn(__fmul_rn(gamma, s[k]), y) : y;
+            }
+            put8<O, VEC>(out + row[u] * ldo, c0[u], d, alo, buf, v);
+        }
     }
 }
 
 template <typename T, typename O, bool VEC>
-__global__ void __launch_bounds__(256) dropout_backward_kernel(const O *g, long ldg, const T *x, long ldx, const O *r, long ldr, float gamma,
-                                                               uint32_t thr, float scale, Philox ph, int M, int d, T *gx, long ldgx, O *gr,
-                                                               long ldgr, double *partial) {
+__global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_backward_kernel(const O *g, long ldg, bool alg, const T *x, long ldx, bool alx, const O *r,
+                                                                           long ldr, bool alr, float gamma, uint32_t thr, float scale, Philox ph, int M,
+                                                                           int d, T *gx, long ldgx, bool algx, O *gr, long ldgr, bool algr,
+                                                                           double *partial) {
     pdl_grid_wait();
-    const int groups = (d + 7) >> 3;
-    const long total = (long)M * groups;
+    MNMT_ROW_BUF(buf, VEC);
     float sum = 0.0f;
-    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long)gridDim.x * 256) {
-        const int row = (int)(i / groups), cg = (int)(i - (long)row * groups);
+    for (Walk w(d); w.row < M; w.next()) {
+        const int c0 = w.chunk * ROW_CHUNK;
+        Raw8<O> rg, rr;
+        Raw8<T> rx;
+        fetch8<O, VEC>(g + w.row * ldg, c0, d, alg, rg);
+        if (partial) fetch8<O, VEC>(r + w.row * ldr, c0, d, alr, rr);
+        if (x) fetch8<T, VEC>(x + w.row * ldx, c0, d, alx, rx);
+        uint32_t keep = gx ? keep8(ph((uint32_t)(c0 >> 3) + (threadIdx.x & 31), (uint32_t)w.row), thr) : 0;
         float u[8], v[8];
-        load_at<O, VEC>(g + row * ldg, cg * 8, d, u);
+        settle8<O, VEC>(rg, alg, buf, u);
         if (partial) {
-            load_at<O, VEC>(r + row * ldr, cg * 8, d, v);
+            settle8<O, VEC>(rr, alr, buf, v);
 #pragma unroll
             for (int k = 0; k < 8; k++) sum = __fmaf_rn(u[k], v[k], sum);
         }
         if (gr) {
 #pragma unroll
             for (int k = 0; k < 8; k++) v[k] = __fmul_rn(gamma, u[k]);
-            store_at<O, VEC>(gr + row * ldgr, cg * 8, d, v);
+            put8<O, VEC>(gr + w.row * ldgr, c0, d, algr, buf, v);
         }
         if (gx) {
-            uint32_t keep = keep8(ph((uint32_t)cg, (uint32_t)row), thr);
             if (x) {  // ReLU
-                load_at<T, VEC>(x + row * ldx, cg * 8, d, v);
+                settle8<T, VEC>(rx, alx, buf, v);
 #pragma unroll
                 for (int k = 0; k < 8; k++) keep &= ~((uint32_t)!(v[k] > 0.0f) << k);
             }
 #pragma unroll
             for (int k = 0; k < 8; k++) u[k] = (keep >> k) & 1u ? __fmul_rn(u[k], scale) : 0.0f;
-            store_at<T, VEC>(gx + row * ldgx, cg * 8, d, u);
+            put8<T, VEC>(gx + w.row * ldgx, c0, d, algx, buf, u);
         }
     }
     if (partial) {
@@ -146,11 +157,6 @@ __global__ void __launch_bounds__(256) dropout_gamma_kernel(const double *partia
     if (threadIdx.x == 0) *ggamma = (float)red[0];
 }
 
-template <typename T>
-bool row_vec(const T *p, long ld) {
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * sizeof(T) % 16 == 0;
-}
-
 template <typename F>
 void by_types(int dtype, int otype, F &&f) {
     auto with = [&](auto t) {
@@ -161,11 +167,6 @@ void by_types(int dtype, int otype, F &&f) {
     if (dtype == MNMT_F32) with(float{});
     else if (dtype == MNMT_BF16) with(__nv_bfloat16{});
     else with(__half{});
-}
-
-int grid_of(long groups) {
-    const long blocks = (groups + 255) / 256, cap = (long)8 * device_sm_count();
-    return (int)(blocks < 1 ? 1 : blocks < cap ? blocks : cap < DROPOUT_PARTIALS ? cap : DROPOUT_PARTIALS);
 }
 
 Philox generator(uint64_t seed, uint64_t offset) {
@@ -181,11 +182,9 @@ cudaError_t launch_dropout(const DropoutArgs &a, cudaStream_t st) {
         const T *x = static_cast<const T *>(a.x);
         const O *r = static_cast<const O *>(a.r);
         O *out = static_cast<O *>(a.out);
-        const bool vec = row_vec(x, a.ldx) && row_vec(out, a.ldo) && (!r || row_vec(r, a.ldr));
-        const int grid = grid_of((long)a.M * ((a.d + 7) / 8));
-        const Philox ph = generator(a.seed, a.offset);
-        if (vec) launch_pdl(dropout_kernel<T, O, true>, grid, 256, 0, st, x, a.ldx, r, a.ldr, a.gamma, a.thr, a.scale, ph, a.relu, a.M, a.d, out, a.ldo);
-        else launch_pdl(dropout_kernel<T, O, false>, grid, 256, 0, st, x, a.ldx, r, a.ldr, a.gamma, a.thr, a.scale, ph, a.relu, a.M, a.d, out, a.ldo);
+        const bool ax = row_aligned(x, a.ldx), ar = !r || row_aligned(r, a.ldr), ao = row_aligned(out, a.ldo);
+        launch_pdl(ax && ar && ao ? dropout_kernel<T, O, true> : dropout_kernel<T, O, false>, row_grid(a.M, a.d, device_sm_count()), 256, 0, st, x, a.ldx,
+                   ax, r, a.ldr, ar, a.gamma, a.thr, a.scale, generator(a.seed, a.offset), a.relu, a.M, a.d, out, a.ldo, ao);
     });
     return cudaGetLastError();
 }
@@ -199,16 +198,12 @@ cudaError_t launch_dropout_backward(const DropoutArgs &a, cudaStream_t st) {
         T *gx = static_cast<T *>(a.gx);
         O *gr = static_cast<O *>(a.gr);
         double *partial = a.ggamma ? static_cast<double *>(a.workspace) : nullptr;
-        const bool vec = row_vec(g, a.ldg) && (!x || row_vec(x, a.ldx)) && (!r || row_vec(r, a.ldr)) && (!gx || row_vec(gx, a.ldgx)) &&
-                         (!gr || row_vec(gr, a.ldgr));
-        const int grid = grid_of((long)a.M * ((a.d + 7) / 8));
-        const Philox ph = generator(a.seed, a.offset);
-        if (vec)
-            launch_pdl(dropout_backward_kernel<T, O, true>, grid, 256, 0, st, g, a.ldg, x, a.ldx, r, a.ldr, a.gamma, a.thr, a.scale, ph, a.M, a.d, gx,
-                       a.ldgx, gr, a.ldgr, partial);
-        else
-            launch_pdl(dropout_backward_kernel<T, O, false>, grid, 256, 0, st, g, a.ldg, x, a.ldx, r, a.ldr, a.gamma, a.thr, a.scale, ph, a.M, a.d, gx,
-                       a.ldgx, gr, a.ldgr, partial);
+        const bool ag = row_aligned(g, a.ldg), ax = !x || row_aligned(x, a.ldx), ar = !r || row_aligned(r, a.ldr);
+        const bool agx = !gx || row_aligned(gx, a.ldgx), agr = !gr || row_aligned(gr, a.ldgr);
+        const int blocks = row_grid(a.M, a.d, device_sm_count()), grid = blocks < DROPOUT_PARTIALS ? blocks : DROPOUT_PARTIALS;
+        launch_pdl(ag && ax && ar && agx && agr ? dropout_backward_kernel<T, O, true> : dropout_backward_kernel<T, O, false>, grid, 256, 0, st, g, a.ldg,
+                   ag, x, a.ldx, ax, r, a.ldr, ar, a.gamma, a.thr, a.scale, generator(a.seed, a.offset), a.M, a.d, gx, a.ldgx, agx, gr, a.ldgr, agr,
+                   partial);
         if (partial) launch_pdl(dropout_gamma_kernel, 1, 256, 0, st, (const double *)partial, grid, a.ggamma);
     });
     return cudaGetLastError();
