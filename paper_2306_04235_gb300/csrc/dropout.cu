@@ -13,6 +13,7 @@
 
 #include "fp4.cuh"
 #include "internal.h"
+#include "row_pass.cuh"
 
 namespace mnmt {
 namespace {
@@ -48,83 +49,86 @@ MNMT_DEV uint32_t keep8(const uint4 w, uint32_t thr) {
     return k;
 }
 
+// the E elements of a lane: one or two counters
+template <int E>
+MNMT_DEV uint32_t keep_lane(const Philox &ph, const RowAt &a, uint32_t thr) {
+    const uint32_t g = (uint32_t)a.c >> 3, row = (uint32_t)a.row;
+    uint32_t k = keep8(ph(g, row), thr);
+    if constexpr (E == 16) k |= keep8(ph(g + 1, row), thr) << 8;
+    return k;
+}
+
 // T: type of x and gx; O: type of out, r, g and gr
 template <typename T, typename O, bool VEC>
-__global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_kernel(const T *x, long ldx, bool alx, const O *r, long ldr, bool alr, float gamma,
-                                                                  uint32_t thr, float scale, Philox ph, int relu, int M, int d, O *out, long ldo,
-                                                                  bool alo) {
+__global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_kernel(const T *x, long ldx, int alx, const O *r, long ldr, int alr, float gamma, uint32_t thr,
+                                                                  float scale, Philox ph, int relu, int M, int d, O *out, long ldo, int alo, int lr) {
     pdl_grid_wait();
     MNMT_ROW_BUF(buf, VEC);
-    constexpr int U = 2;  // chunks in flight
-    for (Walk w(d); w.row < M;) {
-        Raw8<T> rx[U];
-        Raw8<O> rr[U];
-        long row[U];
-        int c0[U];
+    constexpr int E = row_elements(VEC);
+    for (Walk<E> w(M, d, lr); w.more(); w.next()) {
+        const RowAt a = w.at();
+        const bool ok = a.row < M;
+        Raw<T, E> rx;
+        Raw<O, E> rr;
+        fetch<T, VEC>(x + a.row * ldx, w, a, d, ok, alx, rx);
+        if (r) fetch<O, VEC>(r + a.row * ldr, w, a, d, ok, alr, rr);
+        const uint32_t keep = keep_lane<E>(ph, a, thr);
+        float v[E];
+        settle<T, VEC>(rx, w, alx, buf, v);
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            row[u] = w.row, c0[u] = w.chunk * ROW_CHUNK;
-            if (row[u] < M) {
-                fetch8<T, VEC>(x + row[u] * ldx, c0[u], d, alx, rx[u]);
-                if (r) fetch8<O, VEC>(r + row[u] * ldr, c0[u], d, alr, rr[u]);
-            }
-            w.next();
+        for (int k = 0; k < E; k++) {
+            const float y = relu && v[k] <= 0.0f ? 0.0f : v[k];  // a NaN stays
+            v[k] = (keep >> k) & 1u ? __fmul_rn(y, scale) : 0.0f;
         }
+        if (r) {
+            float s[E];
+            settle<O, VEC>(rr, w, alr, buf, s);
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            if (row[u] >= M) break;
-            const uint32_t keep = keep8(ph((uint32_t)(c0[u] >> 3) + (threadIdx.x & 31), (uint32_t)row[u]), thr);
-            float v[8], s[8];
-            settle8<T, VEC>(rx[u], alx, buf, v);
-            if (r) settle8<O, VEC>(rr[u], alr, buf, s);
-#pragma unroll
-            for (int k = 0; k < 8; k++) {
-                float y = relu && v[k] <= 0.0f ? 0.0f : v[k];  // a NaN stays
-                y = (keep >> k) & 1u ? __fmul_rn(y, scale) : 0.0f;
-                v[k] = r ? __fadd_rn(__fmul_rn(gamma, s[k]), y) : y;
-            }
-            put8<O, VEC>(out + row[u] * ldo, c0[u], d, alo, buf, v);
+            for (int k = 0; k < E; k++) v[k] = __fadd_rn(__fmul_rn(gamma, s[k]), v[k]);
         }
+        put<O, VEC>(out + a.row * ldo, w, a, d, ok, alo, buf, v);
     }
 }
 
 template <typename T, typename O, bool VEC>
-__global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_backward_kernel(const O *g, long ldg, bool alg, const T *x, long ldx, bool alx, const O *r,
-                                                                           long ldr, bool alr, float gamma, uint32_t thr, float scale, Philox ph, int M,
-                                                                           int d, T *gx, long ldgx, bool algx, O *gr, long ldgr, bool algr,
-                                                                           double *partial) {
+__global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_backward_kernel(const O *g, long ldg, int alg, const T *x, long ldx, int alx, const O *r,
+                                                                           long ldr, int alr, float gamma, uint32_t thr, float scale, Philox ph, int M,
+                                                                           int d, T *gx, long ldgx, int algx, O *gr, long ldgr, int algr,
+                                                                           double *partial, int lr) {
     pdl_grid_wait();
     MNMT_ROW_BUF(buf, VEC);
+    constexpr int E = 8;  // whatever the alignment, so that ggamma's sum has one order
     float sum = 0.0f;
-    for (Walk w(d); w.row < M; w.next()) {
-        const int c0 = w.chunk * ROW_CHUNK;
-        Raw8<O> rg, rr;
-        Raw8<T> rx;
-        fetch8<O, VEC>(g + w.row * ldg, c0, d, alg, rg);
-        if (partial) fetch8<O, VEC>(r + w.row * ldr, c0, d, alr, rr);
-        if (x) fetch8<T, VEC>(x + w.row * ldx, c0, d, alx, rx);
-        uint32_t keep = gx ? keep8(ph((uint32_t)(c0 >> 3) + (threadIdx.x & 31), (uint32_t)w.row), thr) : 0;
-        float u[8], v[8];
-        settle8<O, VEC>(rg, alg, buf, u);
+    for (Walk<E> w(M, d, lr); w.more(); w.next()) {
+        const RowAt a = w.at();
+        const bool ok = a.row < M;
+        Raw<O, E> rg, rr;
+        Raw<T, E> rx;
+        fetch<O, VEC>(g + a.row * ldg, w, a, d, ok, alg, rg);
+        if (partial) fetch<O, VEC>(r + a.row * ldr, w, a, d, ok, alr, rr);
+        if (x) fetch<T, VEC>(x + a.row * ldx, w, a, d, ok, alx, rx);
+        uint32_t keep = gx ? keep_lane<E>(ph, a, thr) : 0;
+        float u[E], v[E];
+        settle<O, VEC>(rg, w, alg, buf, u);
         if (partial) {
-            settle8<O, VEC>(rr, alr, buf, v);
+            settle<O, VEC>(rr, w, alr, buf, v);
 #pragma unroll
-            for (int k = 0; k < 8; k++) sum = __fmaf_rn(u[k], v[k], sum);
+            for (int k = 0; k < E; k++) sum = __fmaf_rn(u[k], v[k], sum);
         }
         if (gr) {
 #pragma unroll
-            for (int k = 0; k < 8; k++) v[k] = __fmul_rn(gamma, u[k]);
-            put8<O, VEC>(gr + w.row * ldgr, c0, d, algr, buf, v);
+            for (int k = 0; k < E; k++) v[k] = __fmul_rn(gamma, u[k]);
+            put<O, VEC>(gr + a.row * ldgr, w, a, d, ok, algr, buf, v);
         }
         if (gx) {
             if (x) {  // ReLU
-                settle8<T, VEC>(rx, alx, buf, v);
+                settle<T, VEC>(rx, w, alx, buf, v);
 #pragma unroll
-                for (int k = 0; k < 8; k++) keep &= ~((uint32_t)!(v[k] > 0.0f) << k);
+                for (int k = 0; k < E; k++) keep &= ~((uint32_t)!(v[k] > 0.0f) << k);
             }
 #pragma unroll
-            for (int k = 0; k < 8; k++) u[k] = (keep >> k) & 1u ? __fmul_rn(u[k], scale) : 0.0f;
-            put8<T, VEC>(gx + w.row * ldgx, c0, d, algx, buf, u);
+            for (int k = 0; k < E; k++) u[k] = (keep >> k) & 1u ? __fmul_rn(u[k], scale) : 0.0f;
+            put<T, VEC>(gx + a.row * ldgx, w, a, d, ok, algx, buf, u);
         }
     }
     if (partial) {
@@ -182,9 +186,11 @@ cudaError_t launch_dropout(const DropoutArgs &a, cudaStream_t st) {
         const T *x = static_cast<const T *>(a.x);
         const O *r = static_cast<const O *>(a.r);
         O *out = static_cast<O *>(a.out);
-        const bool ax = row_aligned(x, a.ldx), ar = !r || row_aligned(r, a.ldr), ao = row_aligned(out, a.ldo);
-        launch_pdl(ax && ar && ao ? dropout_kernel<T, O, true> : dropout_kernel<T, O, false>, row_grid(a.M, a.d, device_sm_count()), 256, 0, st, x, a.ldx,
-                   ax, r, a.ldr, ar, a.gamma, a.thr, a.scale, generator(a.seed, a.offset), a.relu, a.M, a.d, out, a.ldo, ao);
+        const int ax = row_alignment(x, a.ldx), ar = r ? row_alignment(r, a.ldr) : 2, ao = row_alignment(out, a.ldo);
+        const bool vec = ax == 2 && ar == 2 && ao == 2;
+        launch_pdl(vec ? dropout_kernel<T, O, true> : dropout_kernel<T, O, false>, row_grid(a.M, a.d, vec, device_sm_count()), 256, 0, st, x, a.ldx,
+                   ax, r, a.ldr, ar, a.gamma, a.thr, a.scale, generator(a.seed, a.offset), a.relu, a.M, a.d, out, a.ldo, ao,
+                   row_lanes(a.d, vec));
     });
     return cudaGetLastError();
 }
@@ -198,12 +204,13 @@ cudaError_t launch_dropout_backward(const DropoutArgs &a, cudaStream_t st) {
         T *gx = static_cast<T *>(a.gx);
         O *gr = static_cast<O *>(a.gr);
         double *partial = a.ggamma ? static_cast<double *>(a.workspace) : nullptr;
-        const bool ag = row_aligned(g, a.ldg), ax = !x || row_aligned(x, a.ldx), ar = !r || row_aligned(r, a.ldr);
-        const bool agx = !gx || row_aligned(gx, a.ldgx), agr = !gr || row_aligned(gr, a.ldgr);
-        const int blocks = row_grid(a.M, a.d, device_sm_count()), grid = blocks < DROPOUT_PARTIALS ? blocks : DROPOUT_PARTIALS;
-        launch_pdl(ag && ax && ar && agx && agr ? dropout_backward_kernel<T, O, true> : dropout_backward_kernel<T, O, false>, grid, 256, 0, st, g, a.ldg,
+        const int ag = row_alignment(g, a.ldg), ax = x ? row_alignment(x, a.ldx) : 2, ar = r ? row_alignment(r, a.ldr) : 2;
+        const int agx = gx ? row_alignment(gx, a.ldgx) : 2, agr = gr ? row_alignment(gr, a.ldgr) : 2;
+        const bool vec = ag == 2 && ax == 2 && ar == 2 && agx == 2 && agr == 2;
+        const int blocks = row_grid(a.M, a.d, false, device_sm_count()), grid = blocks < DROPOUT_PARTIALS ? blocks : DROPOUT_PARTIALS;
+        launch_pdl(vec ? dropout_backward_kernel<T, O, true> : dropout_backward_kernel<T, O, false>, grid, 256, 0, st, g, a.ldg,
                    ag, x, a.ldx, ax, r, a.ldr, ar, a.gamma, a.thr, a.scale, generator(a.seed, a.offset), a.M, a.d, gx, a.ldgx, agx, gr, a.ldgr, agr,
-                   partial);
+                   partial, row_lanes(a.d, false));
         if (partial) launch_pdl(dropout_gamma_kernel, 1, 256, 0, st, (const double *)partial, grid, a.ggamma);
     });
     return cudaGetLastError();

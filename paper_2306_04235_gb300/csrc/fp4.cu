@@ -5,79 +5,93 @@
 //   MX  e = max(floor(log2 a) - 2, -127), S = 2^e, r = 2^-e;
 //   NV  s = E4M3(fl(a fl(1 / fl(6 g)))), S = fl(s g), r = fl(1 / S) (0 where S = 0);
 //   q = E2M1(fl(x r)), value fl(q S), gradient |fl(x r)| <= 6 ? g : 0.
-// All three are one pass over the data, bound by its bytes.  A warp takes 256
-// consecutive elements of a row, eight per lane, so a block is four (MX) or two
-// (NV) neighbouring lanes and its maximum two or one shuffles.
+// All three are one pass over the data, bound by its bytes; a lane takes E = 16 or
+// 8 elements of a row (row_pass.cuh), so a block is one, two or four neighbouring
+// lanes.
 #include <type_traits>
 
 #include "fp4.cuh"
 #include "internal.h"
+#include "row_pass.cuh"
 
 namespace mnmt {
 namespace {
 
-template <bool NV>
-MNMT_DEV uint32_t block_amax(const float (&v)[8]) {
-    uint32_t m = 0;
+// the largest magnitude of the lane's block as bits; a NaN stays one
+template <bool NV, int E>
+MNMT_DEV uint32_t block_amax(const float (&v)[E]) {
+    float m = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-    if (!NV) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-    return m;
+    for (int i = 0; i < E; i += 2)
+        asm("{\n\t.reg .f32 a, b;\n\tabs.f32 a, %1;\n\tabs.f32 b, %2;\n\tmax.NaN.f32 %0, %0, a, b;\n\t}" : "+f"(m) : "f"(v[i]), "f"(v[i + 1]));
+    uint32_t u = __float_as_uint(m);
+#pragma unroll
+    for (int o = 1; o < fp4_block(NV) / E; o *= 2) u = max(u, __shfl_xor_sync(0xFFFFFFFFu, u, o));
+    return u;
 }
 
 // chunks in flight per warp
 template <typename T>
-constexpr int FLIGHT = sizeof(T) == 2 ? 4 : 2;
+constexpr int FLIGHT = sizeof(T) == 2 ? 2 : 1;
 
 // codes and scales (q.codes, q.scales) and values, each where its pointer is given
 template <typename T, bool NV, bool VEC>
-__global__ void __launch_bounds__(256, ROW_BLOCKS) fp4_quantize_kernel(const T *x, long ldx, bool alx, Fp4Args q, T *values, long ldv, bool alv) {
+__global__ void __launch_bounds__(256, ROW_BLOCKS) fp4_quantize_kernel(const T *x, long ldx, int alx, Fp4Args q, T *values, long ldv, int alv, int lr) {
     pdl_grid_wait();
     MNMT_ROW_BUF(buf, VEC);
-    constexpr int LPB = fp4_block(NV) / 8, U = FLIGHT<T>;  // lanes per block
+    constexpr int E = row_elements(VEC), LPB = fp4_block(NV) / E, U = FLIGHT<T>;  // lanes per block
     const int lane = threadIdx.x & 31;
     const int tiles_k = fp4_tiles_k(q.cols, NV);
     const size_t pitch = fp4_pitch(q.cols);
-    for (Walk w(q.cols); w.row < q.rows;) {
-        Raw8<T> raw[U];
-        long row[U];
-        int c0[U];
+    for (Walk<E> w(q.rows, q.cols, lr); w.more();) {
+        Raw<T, E> raw[U];
+        RowAt at[U];
+        bool more[U];
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            row[u] = w.row, c0[u] = w.chunk * ROW_CHUNK;
-            if (row[u] < q.rows) fetch8<T, VEC>(x + row[u] * ldx, c0[u], q.cols, alx, raw[u]);
+            at[u] = w.at(), more[u] = w.more();
+            if (more[u]) fetch<T, VEC>(x + at[u].row * ldx, w, at[u], q.cols, at[u].row < q.rows, alx, raw[u]);
             w.next();
         }
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            if (row[u] >= q.rows) break;
-            float v[8];
-            settle8<T, VEC>(raw[u], alx, buf, v);
+            if (!more[u]) break;
+            const RowAt &a = at[u];
+            const bool ok = a.row < q.rows;
+            float v[E];
+            settle<T, VEC>(raw[u], w, alx, buf, v);
             const Fp4Scale s = fp4_scale<NV>(block_amax<NV>(v), q.g, q.inv6g);
-            uint32_t codes = 0;
+            const bool bad = !(s.S == s.S);
+            uint32_t codes[E / 8];
 #pragma unroll
-            for (int i = 0; i < 4; i++) codes |= fp4_code2(__fmul_rn(v[2 * i], s.r), __fmul_rn(v[2 * i + 1], s.r)) << (8 * i);
-            if (!(s.S == s.S)) codes = 0;
+            for (int h = 0; h < E / 8; h++) {
+                uint32_t b[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) b[i] = fp4_code2(__fmul_rn(v[8 * h + 2 * i], s.r), __fmul_rn(v[8 * h + 2 * i + 1], s.r));
+                codes[h] = bad ? 0u : __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+            }
             if (values) {
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const float2 f = fp4_float2((codes >> (8 * i)) & 0xFFu);
+                for (int i = 0; i < E / 2; i++) {
+                    const float2 f = fp4_float2((codes[i >> 2] >> (8 * (i & 3))) & 0xFFu);
                     v[2 * i] = __fmul_rn(f.x, s.S);
                     v[2 * i + 1] = __fmul_rn(f.y, s.S);
                 }
-                put8<T, VEC>(values + row[u] * ldv, c0[u], q.cols, alv, buf, v);
+                put<T, VEC>(values + a.row * ldv, w, a, q.cols, ok, alv, buf, v);
             }
             if (q.codes) {
-                const int c = c0[u] + 8 * lane;
-                if ((size_t)(c >> 1) < pitch) *reinterpret_cast<uint32_t *>(q.codes + row[u] * pitch + (c >> 1)) = codes;
+                if (ok && (size_t)(a.c >> 1) < pitch) {
+                    uint8_t *p = q.codes + a.row * pitch + (a.c >> 1);
+                    if constexpr (E == 16) *reinterpret_cast<uint2 *>(p) = make_uint2(codes[0], codes[1]);
+                    else *reinterpret_cast<uint32_t *>(p) = codes[0];
+                }
                 // the scales of four blocks, a word of a tile
-                const int b = c / fp4_block(NV);
+                const int b = a.c / fp4_block(NV);
                 uint32_t word = s.byte << (8 * (b & 3));
                 word |= __shfl_xor_sync(0xFFFFFFFFu, word, LPB);
                 word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2 * LPB);
-                if (lane % (4 * LPB) == 0 && (b >> 2) < tiles_k)
-                    *reinterpret_cast<uint32_t *>(q.scales + fp4_scale_at((int)row[u], b, tiles_k)) = word;
+                if (ok && lane % (4 * LPB) == 0 && (b >> 2) < tiles_k)
+                    *reinterpret_cast<uint32_t *>(q.scales + fp4_scale_at((int)a.row, b, tiles_k)) = word;
             }
         }
     }
@@ -89,58 +103,64 @@ __global__ void __launch_bounds__(256, ROW_BLOCKS) fp4_quantize_kernel(const T *
 }
 
 template <typename T, bool NV, bool VEC>
-__global__ void __launch_bounds__(256, ROW_BLOCKS) fp4_dequantize_kernel(Fp4Args q, T *values, long ldv, bool alv) {
+__global__ void __launch_bounds__(256, ROW_BLOCKS) fp4_dequantize_kernel(Fp4Args q, T *values, long ldv, int alv, int lr) {
     pdl_grid_wait();
     MNMT_ROW_BUF(buf, VEC);
+    constexpr int E = row_elements(VEC), U = FLIGHT<T>;
     const int tiles_k = fp4_tiles_k(q.cols, NV);
     const size_t pitch = fp4_pitch(q.cols);
-    for (Walk w(q.cols); w.row < q.rows; w.next()) {
-        const int c0 = w.chunk * ROW_CHUNK, c = c0 + 8 * (int)(threadIdx.x & 31);
-        float v[8] = {};
-        if (c < q.cols) {
-            const uint32_t codes = *reinterpret_cast<const uint32_t *>(q.codes + w.row * pitch + (c >> 1));
-            const Fp4Scale s = fp4_scale_of<NV>(q.scales[fp4_scale_at((int)w.row, c / fp4_block(NV), tiles_k)], q.g);
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const float2 f = fp4_float2((codes >> (8 * i)) & 0xFFu);
-                v[2 * i] = __fmul_rn(f.x, s.S);
-                v[2 * i + 1] = __fmul_rn(f.y, s.S);
-            }
-        }
-        put8<T, VEC>(values + w.row * ldv, c0, q.cols, alv, buf, v);
-    }
-}
-
-template <typename T, bool NV, bool VEC>
-__global__ void __launch_bounds__(256, ROW_BLOCKS) fp4_quantize_backward_kernel(const T *x, long ldx, bool alx, const T *g, long ldg, bool alg, T *gx,
-                                                                                long ldgx, bool algx, int rows, int cols, float tg, float inv6g) {
-    pdl_grid_wait();
-    MNMT_ROW_BUF(buf, VEC);
-    constexpr int U = FLIGHT<T> / 2;
-    for (Walk w(cols); w.row < rows;) {
-        Raw8<T> rx[U], rg[U];
-        long row[U];
-        int c0[U];
+    for (Walk<E> w(q.rows, q.cols, lr); w.more();) {
+        RowAt at[U];
+        bool more[U], ok[U];
+        uint2 codes[U];
+        uint32_t byte[U];
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            row[u] = w.row, c0[u] = w.chunk * ROW_CHUNK;
-            if (row[u] < rows) {
-                fetch8<T, VEC>(x + row[u] * ldx, c0[u], cols, alx, rx[u]);
-                fetch8<T, VEC>(g + row[u] * ldg, c0[u], cols, alg, rg[u]);
+            at[u] = w.at(), more[u] = w.more(), ok[u] = at[u].row < q.rows;
+            codes[u] = make_uint2(0, 0), byte[u] = 0;
+            if (ok[u] && at[u].c < q.cols) {
+                const uint8_t *p = q.codes + at[u].row * pitch + (at[u].c >> 1);
+                if constexpr (E == 16) codes[u] = *reinterpret_cast<const uint2 *>(p);
+                else codes[u].x = *reinterpret_cast<const uint32_t *>(p);
+                byte[u] = q.scales[fp4_scale_at((int)at[u].row, at[u].c / fp4_block(NV), tiles_k)];
             }
             w.next();
         }
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            if (row[u] >= rows) break;
-            float v[8], d[8];
-            settle8<T, VEC>(rx[u], alx, buf, v);
-            settle8<T, VEC>(rg[u], alg, buf, d);
-            const Fp4Scale s = fp4_scale<NV>(block_amax<NV>(v), tg, inv6g);
+            if (!more[u]) break;
+            const Fp4Scale s = fp4_scale_of<NV>(byte[u], q.g);
+            float v[E];
 #pragma unroll
-            for (int i = 0; i < 8; i++) d[i] = fabsf(__fmul_rn(v[i], s.r)) <= 6.0f ? d[i] : 0.0f;
-            put8<T, VEC>(gx + row[u] * ldgx, c0[u], cols, algx, buf, d);
+            for (int i = 0; i < E / 2; i++) {
+                const float2 f = fp4_float2(((i < 4 ? codes[u].x : codes[u].y) >> (8 * (i & 3))) & 0xFFu);
+                v[2 * i] = __fmul_rn(f.x, s.S);
+                v[2 * i + 1] = __fmul_rn(f.y, s.S);
+            }
+            put<T, VEC>(values + at[u].row * ldv, w, at[u], q.cols, ok[u], alv, buf, v);
         }
+    }
+}
+
+template <typename T, bool NV, bool VEC>
+__global__ void __launch_bounds__(256, ROW_BLOCKS) fp4_quantize_backward_kernel(const T *x, long ldx, int alx, const T *g, long ldg, int alg, T *gx,
+                                                                                long ldgx, int algx, int rows, int cols, float tg, float inv6g, int lr) {
+    pdl_grid_wait();
+    MNMT_ROW_BUF(buf, VEC);
+    constexpr int E = row_elements(VEC);
+    for (Walk<E> w(rows, cols, lr); w.more(); w.next()) {
+        const RowAt a = w.at();
+        const bool ok = a.row < rows;
+        Raw<T, E> rx, rg;
+        fetch<T, VEC>(x + a.row * ldx, w, a, cols, ok, alx, rx);
+        fetch<T, VEC>(g + a.row * ldg, w, a, cols, ok, alg, rg);
+        float v[E], d[E];
+        settle<T, VEC>(rx, w, alx, buf, v);
+        const Fp4Scale s = fp4_scale<NV>(block_amax<NV>(v), tg, inv6g);
+        settle<T, VEC>(rg, w, alg, buf, d);
+#pragma unroll
+        for (int i = 0; i < E; i++) d[i] = fabsf(__fmul_rn(v[i], s.r)) <= 6.0f ? d[i] : 0.0f;
+        put<T, VEC>(gx + a.row * ldgx, w, a, cols, ok, algx, buf, d);
     }
 }
 
@@ -164,10 +184,10 @@ cudaError_t launch_fp4_quantize(const void *x, int dtype, long ldx, const Fp4Arg
         using T = decltype(t);
         const T *xp = static_cast<const T *>(x);
         T *vp = static_cast<T *>(values);
-        const bool ax = row_aligned(xp, ldx), av = !vp || row_aligned(vp, ldv);
-        by_form<T>(nv, ax && av, [&](auto n, auto v) {
-            launch_pdl(fp4_quantize_kernel<T, decltype(n)::value, decltype(v)::value>, row_grid(q.rows, q.cols, device_sm_count()), 256, 0, st, xp, ldx,
-                       ax, q, vp, ldv, av);
+        const int ax = row_alignment(xp, ldx), av = vp ? row_alignment(vp, ldv) : 2;
+        by_form<T>(nv, ax == 2 && av == 2, [&](auto n, auto v) {
+            launch_pdl(fp4_quantize_kernel<T, decltype(n)::value, decltype(v)::value>, row_grid(q.rows, q.cols, v.value, device_sm_count()), 256, 0, st, xp, ldx,
+                       ax, q, vp, ldv, av, row_lanes(q.cols, v.value));
         });
     });
     return cudaGetLastError();
@@ -177,10 +197,10 @@ cudaError_t launch_fp4_dequantize(const Fp4Args &q, bool nv, void *values, int d
     by_type(dtype, [&](auto t) {
         using T = decltype(t);
         T *vp = static_cast<T *>(values);
-        const bool av = row_aligned(vp, ldv);
-        by_form<T>(nv, av, [&](auto n, auto v) {
-            launch_pdl(fp4_dequantize_kernel<T, decltype(n)::value, decltype(v)::value>, row_grid(q.rows, q.cols, device_sm_count()), 256, 0, st, q, vp,
-                       ldv, av);
+        const int av = row_alignment(vp, ldv);
+        by_form<T>(nv, av == 2, [&](auto n, auto v) {
+            launch_pdl(fp4_dequantize_kernel<T, decltype(n)::value, decltype(v)::value>, row_grid(q.rows, q.cols, v.value, device_sm_count()), 256, 0, st, q, vp,
+                       ldv, av, row_lanes(q.cols, v.value));
         });
     });
     return cudaGetLastError();
@@ -192,10 +212,10 @@ cudaError_t launch_fp4_quantize_backward(const void *x, int dtype, long ldx, con
         using T = decltype(t);
         const T *xp = static_cast<const T *>(x), *gp = static_cast<const T *>(g);
         T *op = static_cast<T *>(gx);
-        const bool ax = row_aligned(xp, ldx), ag = row_aligned(gp, ldg), ao = row_aligned(op, ldgx);
-        by_form<T>(nv, ax && ag && ao, [&](auto n, auto v) {
-            launch_pdl(fp4_quantize_backward_kernel<T, decltype(n)::value, decltype(v)::value>, row_grid(rows, cols, device_sm_count()), 256, 0, st, xp,
-                       ldx, ax, gp, ldg, ag, op, ldgx, ao, rows, cols, tg, inv6g);
+        const int ax = row_alignment(xp, ldx), ag = row_alignment(gp, ldg), ao = row_alignment(op, ldgx);
+        by_form<T>(nv, ax == 2 && ag == 2 && ao == 2, [&](auto n, auto v) {
+            launch_pdl(fp4_quantize_backward_kernel<T, decltype(n)::value, decltype(v)::value>, row_grid(rows, cols, v.value, device_sm_count()), 256, 0, st, xp,
+                       ldx, ax, gp, ldg, ag, op, ldgx, ao, rows, cols, tg, inv6g, row_lanes(cols, v.value));
         });
     });
     return cudaGetLastError();

@@ -191,96 +191,4 @@ MNMT_DEV void store8(T *p, int n, const float (&v)[8]) {
     }
 }
 
-// ---------------------------------------------------------------------------
-// one pass over the rows of a matrix: a warp takes 256 consecutive elements of a
-// row at a time, eight per lane, several such chunks in flight
-// ---------------------------------------------------------------------------
-constexpr int ROW_CHUNK = 256;
-constexpr int ROW_BLOCKS = 4;  // blocks of 256 threads per SM (64 registers a thread)
-
-// the (row, chunk) pairs of a warp: chunk index fastest, advanced without divisions
-struct Walk {
-    long row, step_rows;
-    int chunk, step_chunks, chunks;
-    MNMT_DEV Walk(int cols) {
-        chunks = (cols + ROW_CHUNK - 1) / ROW_CHUNK;
-        const int w = (int)(blockIdx.x * blockDim.x + threadIdx.x) >> 5, n = (int)(gridDim.x * blockDim.x) >> 5;
-        row = w / chunks, chunk = w % chunks;
-        step_rows = n / chunks, step_chunks = n % chunks;
-    }
-    MNMT_DEV void next() {
-        row += step_rows;
-        chunk += step_chunks;
-        if (chunk >= chunks) chunk -= chunks, row++;
-    }
-};
-inline int row_grid(long rows, int cols, int sms) {
-    const long blocks = (rows * ((cols + ROW_CHUNK - 1) / ROW_CHUNK) + 7) / 8, cap = (long)ROW_BLOCKS * sms;
-    return (int)(blocks < 1 ? 1 : blocks < cap ? blocks : cap);
-}
-template <typename T>
-bool row_aligned(const T *p, long ld) {  // every row starts on 16 bytes
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * sizeof(T) % 16 == 0;
-}
-
-// Eight elements per lane of the chunk of a row from column c0 on.  Where the
-// matrix's rows are aligned (al; VEC: known to be) a lane loads its own eight; else
-// 32 lanes load 32 neighbours at a time, and settle8 / put8 turn them in shared
-// memory (buf: 264 words of the warp, element e at e + e / 32: no bank conflicts).
-template <typename T>
-struct alignas(16) Raw8 {
-    T e[8];
-};
-template <typename T, bool VEC>
-MNMT_DEV void fetch8(const T *row, int c0, int cols, bool al, Raw8<T> &r) {
-    const int lane = threadIdx.x & 31, c = c0 + 8 * lane;
-    if (VEC || al) {
-        if (c + 8 <= cols) {
-#pragma unroll
-            for (int i = 0; i < (int)(sizeof(T) / 2); i++) reinterpret_cast<uint4 *>(r.e)[i] = reinterpret_cast<const uint4 *>(row + c)[i];
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; k++) r.e[k] = c + k < cols ? row[c + k] : from_f32<T>(0.0f);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; j++) r.e[j] = c0 + 32 * j + lane < cols ? row[c0 + 32 * j + lane] : from_f32<T>(0.0f);
-    }
-}
-template <typename T, bool VEC>
-MNMT_DEV void settle8(const Raw8<T> &r, bool al, float *buf, float (&v)[8]) {
-    const int lane = threadIdx.x & 31;
-    if (VEC || al) {
-#pragma unroll
-        for (int k = 0; k < 8; k++) v[k] = to_f32(r.e[k]);
-    } else {
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 8; j++) buf[33 * j + lane] = to_f32(r.e[j]);
-        __syncwarp();
-#pragma unroll
-        for (int k = 0; k < 8; k++) v[k] = buf[8 * lane + (lane >> 2) + k];
-    }
-}
-template <typename T, bool VEC>
-MNMT_DEV void put8(T *row, int c0, int cols, bool al, float *buf, const float (&v)[8]) {
-    const int lane = threadIdx.x & 31, c = c0 + 8 * lane;
-    if (VEC || al) {
-        if (c + 8 <= cols) store8<T, true>(row + c, 8, v);
-        else store8<T, false>(row + c, cols - c, v);
-    } else {
-        __syncwarp();
-#pragma unroll
-        for (int k = 0; k < 8; k++) buf[8 * lane + (lane >> 2) + k] = v[k];
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 8; j++)
-            if (c0 + 32 * j + lane < cols) row[c0 + 32 * j + lane] = from_f32<T>(buf[33 * j + lane]);
-    }
-}
-// the warp's buffer for unaligned rows
-#define MNMT_ROW_BUF(buf, VEC)                    \
-    __shared__ float buf##_all[VEC ? 1 : 8 * 264]; \
-    float *buf = buf##_all + (VEC ? 0 : (threadIdx.x >> 5) * 264)
-
 }  // namespace mnmt
