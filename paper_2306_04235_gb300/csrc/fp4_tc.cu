@@ -265,15 +265,22 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
         uint8_t *stg = sm + L::OFF_STG + ew * F4_BLK;
         float *bias = reinterpret_cast<float *>(sm + L::OFF_COLS) + ew * CW;
         uint32_t lt = 0;
+        float next[NB];  // a lane's bias columns of the tile to come
+        auto fetch_bias = [&](long tile) {
+#pragma unroll
+            for (int b = 0; b < NB; b++) {
+                const int n = tile_n(tile) + cw + 32 * b + lane;
+                next[b] = o.bias && tile < tiles && n < N ? o.bias[n] : 0.0f;
+            }
+        };
+        fetch_bias(unit);
         for (long tile = unit; tile < tiles; tile += units, lt++) {
             const int buf = (int)(lt & 1);
             const int row0 = tile_m(tile) + (int)rank * F4_BM + 32 * q, col0 = tile_n(tile) + cw;
             __syncwarp();
 #pragma unroll
-            for (int b = 0; b < NB; b++) {
-                const int n = col0 + 32 * b + lane;
-                bias[32 * b + lane] = o.bias && n < N ? o.bias[n] : 0.0f;
-            }
+            for (int b = 0; b < NB; b++) bias[32 * b + lane] = next[b];
+            fetch_bias(tile + units);
             bool ok = *abort_flag == 0 && mbar_wait(accf_bar(buf), (lt >> 1) & 1);
             if (!ok && *abort_flag == 0) {
                 *abort_flag = 1;

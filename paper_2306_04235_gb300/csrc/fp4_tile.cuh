@@ -122,8 +122,12 @@ __device__ __forceinline__ void f4_stage32(uint8_t *blk, const float (&v)[32]) {
 // staging block (32 x 16-bit or 16 x fp32 columns) so that the stores write whole
 // 64-byte runs, eight rows at a time.
 __device__ __forceinline__ void f4_store_block(const F4Out &o, uint8_t *blk, const float (&v)[32], int row0, int col, int M, int N) {
-    const int lane = threadIdx.x & 31, c = lane & 3;
-    const bool f32 = o.type == MNMT_F32;
+    const int lane = threadIdx.x & 31, rl = lane >> 2, c = lane & 3;
+    const bool f32 = o.type == MNMT_F32, whole = o.vec && row0 + 32 <= M && col + 32 <= N;
+    const int es = f32 ? 4 : 2, per = 16 / es;
+    const long step = 8 * o.ldy * es;  // bytes between the rows that a lane stores
+    uint8_t *dst = static_cast<uint8_t *>(o.y) + ((row0 + rl) * o.ldy + col) * es + 16 * c;
+    const uint8_t *src = blk + rl * 64 + t2_chunk<64>(rl, c);  // rows 8 apart have the same swizzle
 #pragma unroll
     for (int h = 0; h < 2; h++) {
         if (h == 1 && !f32) break;
@@ -132,25 +136,28 @@ __device__ __forceinline__ void f4_store_block(const F4Out &o, uint8_t *blk, con
         else if (h == 0) f4_stage32<0>(blk, v);
         else f4_stage32<1>(blk, v);
         __syncwarp();
-        const int es = f32 ? 4 : 2, per = 16 / es, col0 = col + 16 * h + per * c, n = N - col0;
+        if (whole) {
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int r = 8 * i + (lane >> 2), row = row0 + r;
-            const uint4 w = *reinterpret_cast<const uint4 *>(blk + r * 64 + t2_chunk<64>(r, c));
-            if (row >= M || n <= 0) continue;
-            uint8_t *dst = static_cast<uint8_t *>(o.y) + ((long)row * o.ldy + col0) * es;
-            if (o.vec && n >= per) {
-                *reinterpret_cast<uint4 *>(dst) = w;
-            } else {
+            for (int i = 0; i < 4; i++) *reinterpret_cast<uint4 *>(dst + i * step + 64 * h) = *reinterpret_cast<const uint4 *>(src + 512 * i);
+        } else {
+            const int n = N - col - 16 * h - per * c;
+            for (int i = 0; i < 4; i++) {
+                if (row0 + rl + 8 * i >= M || n <= 0) continue;
+                const uint4 w = *reinterpret_cast<const uint4 *>(src + 512 * i);
+                uint8_t *d = dst + i * step + 64 * h;
+                if (o.vec && n >= per) {
+                    *reinterpret_cast<uint4 *>(d) = w;
+                    continue;
+                }
                 const uint32_t u[4] = {w.x, w.y, w.z, w.w};
                 if (f32) {
 #pragma unroll
                     for (int k = 0; k < 4; k++)
-                        if (k < n) reinterpret_cast<uint32_t *>(dst)[k] = u[k];
+                        if (k < n) reinterpret_cast<uint32_t *>(d)[k] = u[k];
                 } else {
 #pragma unroll
                     for (int k = 0; k < 8; k++)
-                        if (k < n) reinterpret_cast<uint16_t *>(dst)[k] = (uint16_t)(u[k >> 1] >> (16 * (k & 1)));
+                        if (k < n) reinterpret_cast<uint16_t *>(d)[k] = (uint16_t)(u[k >> 1] >> (16 * (k & 1)));
                 }
             }
         }
