@@ -583,7 +583,7 @@ Plan plan(int M, int N, int K, bool gx, bool gw) {
         Plan p = {};
         p.pair = pair;
         p.units = pair ? 76 : 152;
-        const int least = pair ? 8 : 4;  // stages of a part, at least
+        const int least = pair ? 8 : 16;  // stages of a part, at least: finishing split sums is one more launch
         double work = 0.0;
         for (int i = 0; i < 2; i++) {
             if (!want[i]) continue;
