@@ -13,7 +13,7 @@
 // fp4_backward_gemm, both products in one persistent launch (tensor cores): the
 // reduction index is the row of a stored operand, so the MMAs read W, X and (for
 // gW) G "MN-major" from tiles as they lie in memory: no transposed copies.  The
-// epilogue warps apply masks and store through shared memory (masks from the float
+// epilogue warps apply masks and store (masks from the float
 // originals there, a row per lane, waited for memory: gX of 16384 x 512 x 2048 130
 // us, without masks 64); two warps sum the bias gradient meanwhile.
 // fp4_backward_finish: where the reduction of a product was split (few tiles, long
@@ -534,7 +534,7 @@ __global__ void __launch_bounds__(256) fp4_backward_finish(FinishArgs a) {
         auto put = [&](auto t) {
             using T = decltype(t);
             T *o = static_cast<T *>(p.out.y) + row * p.out.ldy + c;
-            if (p.out.vec && n >= 8) store8<T, true>(o, 8, s);
+            if (p.out.al && n >= 8) store8<T, true>(o, 8, s);
             else store8<T, false>(o, n, s);
         };
         if (p.out.type == MNMT_F32) put(float{});
@@ -706,7 +706,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
         a.n++;
         r.rows = input ? M : N, r.cols = K, r.red = input ? N : M, r.a_mn = !input;
         r.out = input ? F4Out{b.gx, b.ldgx, b.xdtype, 0, 0, b.nv ? b.w.g : 1.0f, nullptr} : F4Out{b.gw, b.ldgw, MNMT_F32, 0, 0, b.nv ? b.x.g : 1.0f, nullptr};
-        r.out.vec = out_vec(r.out.y, r.out.ldy, r.out.type);
+        r.out.al = out_alignment(r.out.y, r.out.ldy, r.out.type);
         r.mask = p.m[input].mask, r.mp = s.mp;
         r.parts = pl.parts[!input], r.len = pl.len[!input];
         if (r.parts > 1) {

@@ -8,13 +8,14 @@
 // tiles of 256 codes) and the scales as they are stored: a 512-byte tile of 128
 // rows x 4 blocks goes to four TMEM columns with one tcgen05.cp.
 //
-// Persistent, 10 or 14 warps per CTA:
+// Persistent, 2 + BN / 8 warps per CTA:
 //   warp 0 lane 0   TMA producer: codes and scales of a k-block of 256 into a ring;
 //   warp 1 lane 0   copies a k-block's scales to TMEM (tcgen05.cp and .mma run in
 //                   the order in which they are issued, so one set of columns
 //                   serves every k-block), issues its four MMAs, frees the slot;
 //   the others      drain a finished accumulator (TMEM holds two), apply alpha,
-//                   bias and ReLU, round, and store through shared memory.
+//                   bias and ReLU, round, and store; 32 columns each: the chain of
+//                   one warp's instructions is what a small tile takes.
 // CG = 2: a pair of CTAs computes 256 x 192 tiles, each CTA half of the rows of
 // both operands; CG = 1: 128 x 128 or 128 x 64 tiles for smaller grids.
 // Every wait is bounded; one that runs out records MNMT_ETIMEOUT in *status, and
@@ -26,6 +27,7 @@
 #include "fp4_tile.cuh"
 #include "internal.h"
 #include "mbarrier.cuh"
+#include "routes.h"
 #include "tcgen05.cuh"
 
 namespace mnmt {
@@ -41,7 +43,7 @@ struct F4Layout {
     static constexpr uint32_t B_BYTES = BN / CG * 128;
     static constexpr uint32_t OFF_SFA = A_BYTES + B_BYTES, OFF_SFB = OFF_SFA + T * 512;
     static constexpr uint32_t STAGE = OFF_SFB + R * T * 512;
-    static constexpr int EPI = BN == 64 ? 8 : BN / 16, CW = 4 * BN / EPI;  // epilogue warps, columns of each (its 32 rows)
+    static constexpr int EPI = BN == 192 ? 12 : BN / 8, CW = 4 * BN / EPI;  // epilogue warps, columns of each (its 32 rows)
     static constexpr int THREADS = 64 + 32 * EPI;
     static constexpr uint32_t OFF_AFTER = EPI * (F4_BLK + CW * 4) + 512;  // staging, bias, barriers
     static constexpr int FIT = (int)((227 * 1024 - 1024 - OFF_AFTER) / STAGE);
@@ -389,13 +391,14 @@ cudaError_t fp4_init() {
 
 cudaError_t launch_fp4_product(const Fp4Args &x, const Fp4Args &w, bool nv, float alpha, const float *bias, int relu, void *y, int ydtype,
                                long ldy, int *status, cudaStream_t st) {
-    const F4Out o{y, ldy, ydtype, out_vec(y, ldy, ydtype), relu, alpha, bias};
+    const F4Out o{y, ldy, ydtype, out_alignment(y, ldy, ydtype), relu, alpha, bias};
     auto go = [&](auto n) {
         constexpr bool NV = decltype(n)::value;
-        const long mt = (x.rows + 127) / 128, sms = device_sm_count();
-        if (mt * ((w.rows + 63) / 64) <= sms) return f4_launch<1, 64, NV>(x, w, o, status, st);
-        if (mt * ((w.rows + 127) / 128) <= sms) return f4_launch<1, 128, NV>(x, w, o, status, st);
-        return f4_launch<2, 192, NV>(x, w, o, status, st);
+        switch (route_fp4_tiles(x.rows, w.rows, x.cols, device_sm_count())) {
+            case FP4_64: return f4_launch<1, 64, NV>(x, w, o, status, st);
+            case FP4_128: return f4_launch<1, 128, NV>(x, w, o, status, st);
+            default: return f4_launch<2, 192, NV>(x, w, o, status, st);
+        }
     };
     return nv ? go(std::true_type{}) : go(std::false_type{});
 }

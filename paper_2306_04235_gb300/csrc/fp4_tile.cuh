@@ -6,12 +6,13 @@
 #include "fp4.cuh"
 #include "internal.h"
 #include "mbarrier.cuh"
+#include "row_pass.cuh"
 #include "tcgen05.cuh"
 
 namespace mnmt {
 
 constexpr int F4_BM = 128;  // rows of a tile per CTA
-constexpr int F4_BLK = 2048;  // a warp's staging block: 32 rows of 64 bytes
+constexpr int F4_BLK = 1024;  // a warp's staging block, for outputs without alignment: 32 rows of 32 bytes
 
 // An epilogue warp has read an accumulator (tcgen05.wait::ld): the leader's MMAs
 // may overwrite it.  Relaxed: nothing in memory is handed over, and a release
@@ -82,84 +83,87 @@ struct F4Out {
     void *y;
     long ldy;
     int type;   // MNMT_F32 / BF16 / F16
-    int vec;    // 16-byte stores are aligned
+    int al;     // every row starts on 32 bytes (2), 16 bytes (1), less (0)
     int relu;
     float alpha;
     const float *bias;
 };
 
-// 32 outputs of a row, rounded, into staging blocks (row = lane): one of 32
-// 16-bit outputs, or half h of 32 fp32 ones
-__device__ __forceinline__ void f4_stage16(uint8_t *blk, const float (&v)[32], int type) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int c = 0; c < 4; c++) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const float lo = v[8 * c + 2 * i], hi = v[8 * c + 2 * i + 1];
-            if (type == MNMT_BF16) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-                w[i] = *reinterpret_cast<const uint32_t *>(&h);
-            } else {
-                const __half2 h = __floats2half2_rn(lo, hi);
-                w[i] = *reinterpret_cast<const uint32_t *>(&h);
-            }
-        }
-        *reinterpret_cast<uint4 *>(blk + lane * 64 + t2_chunk<64>(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+// outputs c .. c + 1 of a row as a word of type's 16 bits
+__device__ __forceinline__ uint32_t f4_pair(float lo, float hi, int type) {
+    if (type == MNMT_BF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
     }
-}
-template <int H>
-__device__ __forceinline__ void f4_stage32(uint8_t *blk, const float (&v)[32]) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int c = 0; c < 4; c++)
-        *reinterpret_cast<float4 *>(blk + lane * 64 + t2_chunk<64>(lane, c)) =
-            make_float4(v[16 * H + 4 * c], v[16 * H + 4 * c + 1], v[16 * H + 4 * c + 2], v[16 * H + 4 * c + 3]);
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// 32 columns of a warp's 32 rows (a row per lane) from column col on: through the
-// staging block (32 x 16-bit or 16 x fp32 columns) so that the stores write whole
-// 64-byte runs, eight rows at a time.
+// 32 columns of a warp's 32 rows (a row per lane) from column col on.  A lane
+// stores its row in whole 32-byte sectors; turning the block in shared memory for
+// longer runs costs more instructions than it saves (a tile of 128 x 128, K = 256:
+// 1.9 us).  Only what is unaligned or cut off at the matrix's edge is turned.
 __device__ __forceinline__ void f4_store_block(const F4Out &o, uint8_t *blk, const float (&v)[32], int row0, int col, int M, int N) {
-    const int lane = threadIdx.x & 31, rl = lane >> 2, c = lane & 3;
-    const bool f32 = o.type == MNMT_F32, whole = o.vec && row0 + 32 <= M && col + 32 <= N;
-    const int es = f32 ? 4 : 2, per = 16 / es;
-    const long step = 8 * o.ldy * es;  // bytes between the rows that a lane stores
-    uint8_t *dst = static_cast<uint8_t *>(o.y) + ((row0 + rl) * o.ldy + col) * es + 16 * c;
-    const uint8_t *src = blk + rl * 64 + t2_chunk<64>(rl, c);  // rows 8 apart have the same swizzle
+    const int lane = threadIdx.x & 31;
+    const bool f32 = o.type == MNMT_F32;
+    if (o.al && col + 32 <= N) {
+        if (row0 + lane >= M) return;
+        uint8_t *dst = static_cast<uint8_t *>(o.y) + ((row0 + lane) * o.ldy + col) * (f32 ? 4 : 2);
+        if (f32) {
+            uint32_t w[32];
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
-        if (h == 1 && !f32) break;
-        __syncwarp();  // the block has been read
-        if (!f32) f4_stage16(blk, v, o.type);
-        else if (h == 0) f4_stage32<0>(blk, v);
-        else f4_stage32<1>(blk, v);
-        __syncwarp();
-        if (whole) {
+            for (int i = 0; i < 32; i++) w[i] = __float_as_uint(v[i]);
+            if (o.al == 2) {
 #pragma unroll
-            for (int i = 0; i < 4; i++) *reinterpret_cast<uint4 *>(dst + i * step + 64 * h) = *reinterpret_cast<const uint4 *>(src + 512 * i);
-        } else {
-            const int n = N - col - 16 * h - per * c;
-            for (int i = 0; i < 4; i++) {
-                if (row0 + rl + 8 * i >= M || n <= 0) continue;
-                const uint4 w = *reinterpret_cast<const uint4 *>(src + 512 * i);
-                uint8_t *d = dst + i * step + 64 * h;
-                if (o.vec && n >= per) {
-                    *reinterpret_cast<uint4 *>(d) = w;
-                    continue;
-                }
-                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-                if (f32) {
+                for (int i = 0; i < 4; i++) st32(dst + 32 * i, w + 8 * i);
+            } else {
 #pragma unroll
-                    for (int k = 0; k < 4; k++)
-                        if (k < n) reinterpret_cast<uint32_t *>(d)[k] = u[k];
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; k++)
-                        if (k < n) reinterpret_cast<uint16_t *>(d)[k] = (uint16_t)(u[k >> 1] >> (16 * (k & 1)));
-                }
+                for (int i = 0; i < 8; i++) reinterpret_cast<uint4 *>(dst)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
             }
+        } else {
+            uint32_t w[16];
+            if (o.type == MNMT_BF16) {
+#pragma unroll
+                for (int i = 0; i < 16; i++) w[i] = f4_pair(v[2 * i], v[2 * i + 1], MNMT_BF16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; i++) w[i] = f4_pair(v[2 * i], v[2 * i + 1], MNMT_F16);
+            }
+            if (o.al == 2) {
+                st32(dst, w);
+                st32(dst + 32, w + 8);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; i++) reinterpret_cast<uint4 *>(dst)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+            }
+        }
+        return;
+    }
+    // slices of 8 fp32 or 16 16-bit columns, 32 bytes a row; neighbouring lanes store neighbouring columns
+    const int per = f32 ? 8 : 16;
+#pragma unroll
+    for (int h = 0; h < 4; h++) {
+        if (h >= 2 && !f32) break;
+        __syncwarp();  // the block has been read
+        uint4 *mine = reinterpret_cast<uint4 *>(blk + 32 * lane);
+        if (f32) {
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+                mine[i] = make_uint4(__float_as_uint(v[8 * h + 4 * i]), __float_as_uint(v[8 * h + 4 * i + 1]), __float_as_uint(v[8 * h + 4 * i + 2]),
+                                     __float_as_uint(v[8 * h + 4 * i + 3]));
+        } else if (h < 2) {
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+                mine[i] = make_uint4(f4_pair(v[16 * h + 8 * i], v[16 * h + 8 * i + 1], o.type), f4_pair(v[16 * h + 8 * i + 2], v[16 * h + 8 * i + 3], o.type),
+                                     f4_pair(v[16 * h + 8 * i + 4], v[16 * h + 8 * i + 5], o.type), f4_pair(v[16 * h + 8 * i + 6], v[16 * h + 8 * i + 7], o.type));
+        }
+        __syncwarp();
+        const int c = lane & (per - 1), n = col + per * h + c;
+        for (int r = lane / per; r < 32; r += 32 / per) {
+            if (row0 + r >= M || n >= N) continue;
+            const long at = (row0 + r) * o.ldy + n;
+            if (f32) static_cast<float *>(o.y)[at] = reinterpret_cast<const float *>(blk + 32 * r)[c];
+            else static_cast<uint16_t *>(o.y)[at] = reinterpret_cast<const uint16_t *>(blk + 32 * r)[c];
         }
     }
 }
@@ -173,9 +177,8 @@ inline bool encode(CUtensorMap *tm, CUtensorMapDataType type, const void *p, cuu
                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// whether every 16-byte store of the epilogue is aligned
-inline bool out_vec(const void *y, long ldy, int type) {
-    return (reinterpret_cast<uintptr_t>(y) & 15) == 0 && ldy * (type == MNMT_F32 ? 4 : 2) % 16 == 0;
+inline int out_alignment(const void *y, long ldy, int type) {
+    return type == MNMT_F32 ? row_alignment(static_cast<const float *>(y), ldy) : row_alignment(static_cast<const uint16_t *>(y), ldy);
 }
 
 // cluster and launch attributes of a tile kernel (programmatic launch outside stream captures, as launch_pdl)

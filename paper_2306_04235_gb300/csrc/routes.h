@@ -147,4 +147,13 @@ inline bool route_rows_variant(int nb, int hpc, int beam, int clusters, int fit)
     return clusters <= fit && ((nb <= 2 && hpc == 1) || beam >= 4);
 }
 
+// Output tiles of the product of 4-bit floating-point matrices: 256 x 192 on CTA
+// pairs, 128 x 128 or 128 x 64 on single CTAs.
+enum Fp4Tiles { FP4_PAIR, FP4_128, FP4_64 };
+inline Fp4Tiles route_fp4_tiles(int M, int N, int K, int sms) {
+    const long mt = (M + 127L) / 128, t64 = mt * ((N + 63L) / 64), t128 = mt * ((N + 127L) / 128);
+    if (t64 <= sms) return FP4_64;
+    return t128 <= 2L * sms || (t128 <= 4L * sms && K <= 2048) ? FP4_128 : FP4_PAIR;
+}
+
 }  // namespace mnmt
