@@ -121,6 +121,7 @@ constexpr int BW_BK = 64;  // reduction indices per stage
 // terms and added up in registers (16384 terms: 5e-7 off); 16-bit results, whose
 // rounding is 2^-9 or 2^-11, are not.
 constexpr int BW_CHUNK = 16;  // stages
+constexpr int BW_TILE = 12;  // what an item takes beside its stages, in stages
 constexpr int BW_EPI_WARPS = 8, BW_GB_WARPS = 2, BW_THREADS = 64 + 32 * (BW_EPI_WARPS + BW_GB_WARPS);
 constexpr int GB_ROWS = 128, GB_COLS = 256;  // rows and columns of G that a warp sums at a time
 
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
     // then have one item less take as many more of product 1 as fit that item's
     // time, then all of them take turns.
     const int heavy = (int)(n0 % units);
-    const long extra = heavy ? (long)(units - heavy) * (a.p[0].len / max(1, a.p[1].len)) : 0;
+    const long extra = heavy ? (long)(units - heavy) * ((a.p[0].len + BW_TILE) / (a.p[1].len + BW_TILE)) : 0;
     struct Range {
         long first, step, end;
     };
@@ -588,21 +589,24 @@ Plan plan(int M, int N, int K, bool gx, bool gw) {
         for (int i = 0; i < 2; i++) {
             if (!want[i]) continue;
             p.tiles[i] = (long)fp4_div_up(rows[i], pair ? 2 * F4_BM : F4_BM) * fp4_div_up(K, pair ? 256 : 64);
-            work += (double)p.tiles[i] * fp4_div_up(red[i], BW_BK);
+            work += (double)p.tiles[i] * (fp4_div_up(red[i], BW_BK) + BW_TILE);
         }
-        const double share = work / p.units;  // stages of a unit
+        const double share = work / p.units;  // of a unit, in stages
         const bool few = p.tiles[0] + p.tiles[1] < p.units;
         for (int i = 0; i < 2; i++) {
             // a reduction longer than a unit's share is split into parts of about that
             const int nkb = fp4_div_up(red[i], BW_BK);
-            double parts = want[i] && nkb > share ? nkb / (share > least ? share : least) + (few ? 0.0 : 0.99) : 1.0;
+            const double len = share - BW_TILE > least ? share - BW_TILE : least;
+            double parts = want[i] && nkb > len ? nkb / len + (few ? 0.0 : 0.99) : 1.0;
             if (parts > 64.0) parts = 64.0;
             p.len[i] = fp4_div_up(nkb, parts < 1.0 ? 1 : (int)parts);
             p.parts[i] = fp4_div_up(nkb, p.len[i]);
             p.items += p.tiles[i] * p.parts[i];
         }
         best = p;
-        if (pair && share >= 12) break;
+        // us, pairs / single CTAs: 512 x 2048 x 2048 (share 26) 33.8 / 28.5, 4096 x 2048 x 512
+        // (35) 31.3 / 45.0, 2048^3 (74) 42.2 / 78.3, 46 x 1024 x 256 (1) 15.4 / 10.2
+        if (pair && share >= 30) break;
     }
     return best;
 }

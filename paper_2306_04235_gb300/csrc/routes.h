@@ -149,11 +149,21 @@ inline bool route_rows_variant(int nb, int hpc, int beam, int clusters, int fit)
 
 // Output tiles of the product of 4-bit floating-point matrices: 256 x 192 on CTA
 // pairs, 128 x 128 or 128 x 64 on single CTAs.
+//   64 columns while there is an SM for every tile (1000 x 512 x 2048 5.0 us, 128
+//   columns 5.7), else by time, waves x (a + b k-blocks of 256) us, fitted to 588
+//   products of 20 to 9000 rows, 512 to 32000 columns and K of 256 to 8192 (us, 128
+//   columns / pairs):
+//     512 x 32000 x 512 13.6 / 14.5;  2048 x 8192 x 8192 54.6 / 44.6
+//     384 x 32000 x 512 10.3 / 14.7;  1600 x 1536 x 8192 17.5 / 13.0
+//     9000 x 8192 x 8192 238 / 182
 enum Fp4Tiles { FP4_PAIR, FP4_128, FP4_64 };
 inline Fp4Tiles route_fp4_tiles(int M, int N, int K, int sms) {
     const long mt = (M + 127L) / 128, t64 = mt * ((N + 63L) / 64), t128 = mt * ((N + 127L) / 128);
+    const long pairs = (M + 255L) / 256 * ((N + 191L) / 192), half = sms / 2;
     if (t64 <= sms) return FP4_64;
-    return t128 <= 2L * sms || (t128 <= 4L * sms && K <= 2048) ? FP4_128 : FP4_PAIR;
+    const double kb = (K + 255) / 256;
+    const double single = (double)((t128 + sms - 1) / sms) * (1.55 + 0.196 * kb), paired = (double)((pairs + half - 1) / half) * (2.5 + 0.2 * kb);
+    return single <= paired ? FP4_128 : FP4_PAIR;
 }
 
 }  // namespace mnmt
