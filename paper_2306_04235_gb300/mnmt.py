@@ -58,6 +58,8 @@ def lib_path() -> str:
 def lib():
     """Load libmnmt.so (building it first if its sources are newer)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             path = _build.build()
@@ -141,11 +143,11 @@ def _ptr(x):
     """Address of a numpy array, a torch tensor, or an integer address."""
     if x is None:
         return None
-    if isinstance(x, int):
-        return x
+    if hasattr(x, "data_ptr"):
+        return x.data_ptr()
     if isinstance(x, np.ndarray):
         return x.ctypes.data
-    return x.data_ptr()
+    return x
 
 
 def _stream_handle(stream):
