@@ -9,10 +9,12 @@
 // rows x 4 blocks goes to four TMEM columns with one tcgen05.cp.
 //
 // Persistent, 2 + BN / 8 warps per CTA:
-//   warp 0 lane 0   TMA producer: codes and scales of a k-block of 256 into a ring;
-//   warp 1 lane 0   copies a k-block's scales to TMEM (tcgen05.cp and .mma run in
-//                   the order in which they are issued, so one set of columns
-//                   serves every k-block), issues its four MMAs, frees the slot;
+//   warp 0          TMA producer: codes and scales of a k-block of 256 into a ring;
+//   warp 1          copies a k-block's scales to TMEM (copies and MMAs of one issuer
+//                   run in the order of issue; two sets of columns by turns all the
+//                   same, so that no copy touches what the k-block before it reads:
+//                   waiting for those MMAs instead costs 8192^3 192 us), issues its
+//                   four MMAs, frees the slot;
 //   the others      drain a finished accumulator (TMEM holds two), apply alpha,
 //                   bias and ReLU, round, and store; 32 columns each: the chain of
 //                   one warp's instructions is what a small tile takes.
@@ -54,9 +56,9 @@ struct F4Layout {
     static constexpr int NBARS = 2 * STAGES + 5;  // full, empty, acc_full[2], acc_empty[2], done
     static constexpr uint32_t OFF_MISC = OFF_BARS + NBARS * 8;
     static constexpr size_t SMEM = 1024 + OFF_MISC + 16;
-    static constexpr int COL_SFA = 2 * BN, COL_SFB = COL_SFA + 4 * T;  // TMEM columns
-    static constexpr int COLS = COL_SFB + 4 * R * T <= 256 ? 256 : 512;
-    static_assert(COL_SFB + 4 * R * T <= 512, "TMEM holds 512 columns");
+    static constexpr int COL_SFA = 2 * BN, COL_SFB = COL_SFA + 4 * T, SF = 4 * T + 4 * R * T;  // TMEM columns; two sets of scales
+    static constexpr int COLS = COL_SFA + 2 * SF <= 256 ? 256 : 512;
+    static_assert(COL_SFA + 2 * SF <= 512, "TMEM holds 512 columns");
     static_assert(STAGE % 1024 == 0, "swizzled tiles start on 1024 bytes");
     static_assert(OFF_MISC + 16 - OFF_STG <= OFF_AFTER, "barriers fit");
 };
@@ -227,16 +229,17 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
                 }
                 tc_fence_after();
                 const uint64_t off = (uint64_t)((s * L::STAGE) >> 4);
+                const uint32_t set = (seen & 1) * L::SF;
 #pragma unroll
                 for (int t = 0; t < T; t++) {
-                    f4_copy_scales_on<CG>(on, sfa + 4 * t, sa_desc + off + (uint64_t)(t * 32));
+                    f4_copy_scales_on<CG>(on, sfa + set + 4 * t, sa_desc + off + (uint64_t)(t * 32));
 #pragma unroll
-                    for (int r = 0; r < R; r++) f4_copy_scales_on<CG>(on, cfb + 4 * (R * t + r), sb_desc + off + (uint64_t)((r * T + t) * 32));
+                    for (int r = 0; r < R; r++) f4_copy_scales_on<CG>(on, cfb + set + 4 * (R * t + r), sb_desc + off + (uint64_t)((r * T + t) * 32));
                 }
                 auto mma = [&](int k) {
                     const int t = NV ? k : k >> 1, id = NV ? 0 : 2 * (k & 1);
                     f4_mma_on<CG, NV>(on, d, a_desc + off + (uint64_t)(2 * k), b_desc + off + (uint64_t)(2 * k), f4_idesc(CG * F4_BM, BN, NV, id),
-                                      sfa + 4 * t, sfb + 4 * R * t, (uint32_t)(kb | k));
+                                      sfa + set + 4 * t, sfb + set + 4 * R * t, (uint32_t)(kb | k));
                 };
                 if (kb < full) {
                     mma(0), mma(1), mma(2), mma(3);
