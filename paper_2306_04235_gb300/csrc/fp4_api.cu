@@ -8,6 +8,7 @@
 
 #include "fp4.cuh"
 #include "internal.h"
+#include "routes.h"
 
 using namespace mnmt;
 
@@ -148,7 +149,7 @@ extern "C" int mnmt_fp4_linear(const mnmt_fp4 *xq, const mnmt_fp4 *w, const void
     if (!aligned(bias, 4) || !aligned(status, 4)) return fail(MNMT_EINVAL, "fp4_linear: bias and status must be 4-byte aligned");
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const Fp4Args a = args_of(xq), b = args_of(w);
-    if (w->rows > 0 && fp4_small_fits(a.rows, a.cols))
+    if (w->rows > 0 && route_fp4_small(a.rows, b.rows, a.cols))
         return done(launch_fp4_small(a, b, is_nv(w), x, xdtype, ldx, a.g * b.g, bias, relu != 0, y, ydtype, ldy, st), "fp4_linear");
     if (x) {
         cudaError_t e = launch_fp4_quantize(x, xdtype, ldx, a, is_nv(xq), nullptr, 0, st);

@@ -234,7 +234,6 @@ cudaError_t launch_fp4_quantize_backward(const void *x, int dtype, long ldx, con
 cudaError_t launch_fp4_product(const Fp4Args &x, const Fp4Args &w, bool nv, float alpha, const float *bias, int relu,
                                void *y, int ydtype, long ldy, int *status, cudaStream_t st);
 // a few rows: quantisation (x non-null) and product in one launch
-bool fp4_small_fits(int M, int K);
 cudaError_t launch_fp4_small(const Fp4Args &x, const Fp4Args &w, bool nv, const void *xp, int xdtype, long ldx, float alpha,
                              const float *bias, int relu, void *y, int ydtype, long ldy, cudaStream_t st);
 cudaError_t fp4_init();  // set-up of the product kernels on the current device

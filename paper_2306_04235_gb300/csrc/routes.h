@@ -147,22 +147,34 @@ inline bool route_rows_variant(int nb, int hpc, int beam, int clusters, int fit)
     return clusters <= fit && ((nb <= 2 && hpc == 1) || beam >= 4);
 }
 
+// Does a product of 4-bit floating-point matrices run on the kernel for a few rows
+// (one launch with the quantisation) or as quantisation and tensor-core product?
+// x must fit its shared memory; then by time, us a call, few rows / two launches:
+//   2048 x 512: 8 rows 4.7 / 5.9;  32000 x 512: 1 row 6.8 / 7.9, 4 rows 11.2 / 7.9
+//   8192 x 2048: 1 row 6.9 / 8.8, 4 rows 11.9 / 8.8;  2048 x 8192: 1 row 8.0 / 12.0, 4 rows 15.1 / 12.0
+constexpr long FP4_SMALL_X = 32768;  // elements of x, rows padded to 32
+inline bool route_fp4_small(int M, int N, int K) {
+    if (M > 8 || (long)M * ((K + 31L) / 32 * 32) > FP4_SMALL_X) return false;
+    return M == 1 || (double)M * N * K <= 2.5e7;
+}
+
 // Output tiles of the product of 4-bit floating-point matrices: 256 x 192 on CTA
 // pairs, 128 x 128 or 128 x 64 on single CTAs.
 //   64 columns while there is an SM for every tile (1000 x 512 x 2048 5.0 us, 128
-//   columns 5.7), else by time, waves x (a + b k-blocks of 256) us, fitted to 588
-//   products of 20 to 9000 rows, 512 to 32000 columns and K of 256 to 8192 (us, 128
+//   columns 5.7), else by time, t + waves x (a + b k-blocks of 256) us, fitted to 510
+//   products of 40 to 16384 rows, 512 to 32000 columns and K of 256 to 8192 (us, 128
 //   columns / pairs):
 //     512 x 32000 x 512 13.6 / 14.5;  2048 x 8192 x 8192 54.6 / 44.6
 //     384 x 32000 x 512 10.3 / 14.7;  1600 x 1536 x 8192 17.5 / 13.0
-//     9000 x 8192 x 8192 238 / 182
+//     16384 x 8192 x 512 96 / 84;     9000 x 8192 x 8192 238 / 182
 enum Fp4Tiles { FP4_PAIR, FP4_128, FP4_64 };
 inline Fp4Tiles route_fp4_tiles(int M, int N, int K, int sms) {
     const long mt = (M + 127L) / 128, t64 = mt * ((N + 63L) / 64), t128 = mt * ((N + 127L) / 128);
     const long pairs = (M + 255L) / 256 * ((N + 191L) / 192), half = sms / 2;
     if (t64 <= sms) return FP4_64;
     const double kb = (K + 255) / 256;
-    const double single = (double)((t128 + sms - 1) / sms) * (1.55 + 0.196 * kb), paired = (double)((pairs + half - 1) / half) * (2.5 + 0.2 * kb);
+    const double single = 2.17 + (double)((t128 + sms - 1) / sms) * (1.46 + 0.207 * kb);
+    const double paired = 4.22 + (double)((pairs + half - 1) / half) * (2.0 + 0.203 * kb);
     return single <= paired ? FP4_128 : FP4_PAIR;
 }
 
