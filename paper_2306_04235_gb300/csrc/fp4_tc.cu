@@ -47,11 +47,12 @@ struct F4Layout {
     static constexpr uint32_t STAGE = OFF_SFB + R * T * 512;
     static constexpr int EPI = BN == 192 ? 12 : BN / 8, CW = 4 * BN / EPI;  // epilogue warps, columns of each (its 32 rows)
     static constexpr int THREADS = 64 + 32 * EPI;
-    static constexpr uint32_t OFF_AFTER = EPI * (F4_BLK + CW * 4) + 512;  // staging, bias, barriers
+    static constexpr uint32_t BLK = CG == 1 ? 4096 : F4_BLK;  // a warp's staging block
+    static constexpr uint32_t OFF_AFTER = EPI * (BLK + CW * 4) + 512;  // staging, bias, barriers
     static constexpr int FIT = (int)((227 * 1024 - 1024 - OFF_AFTER) / STAGE);
     static constexpr int STAGES = FIT > 8 ? 8 : FIT;
     static constexpr uint32_t OFF_STG = STAGES * STAGE;
-    static constexpr uint32_t OFF_COLS = OFF_STG + EPI * F4_BLK;  // [EPI][CW] fp32
+    static constexpr uint32_t OFF_COLS = OFF_STG + EPI * BLK;  // [EPI][CW] fp32
     static constexpr uint32_t OFF_BARS = OFF_COLS + EPI * CW * 4;
     static constexpr int NBARS = 2 * STAGES + 5;  // full, empty, acc_full[2], acc_empty[2], done
     static constexpr uint32_t OFF_MISC = OFF_BARS + NBARS * 8;
@@ -109,7 +110,7 @@ __device__ __forceinline__ void f4_copy_scales_on(uint32_t on, uint32_t taddr, u
 template <int CG, int BN, bool NV>
 __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
     fp4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmSA,
-             const __grid_constant__ CUtensorMap tmSB, F4Out o, int M, int N, int K, int *status) {
+             const __grid_constant__ CUtensorMap tmSB, const __grid_constant__ CUtensorMap tmY, F4Out o, int M, int N, int K, int *status) {
     pdl_grid_wait();
     using L = F4Layout<CG, BN, NV>;
     constexpr int STAGES = L::STAGES, T = L::T, R = L::R;
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
         // ---- epilogue: warp ew takes 32 of this CTA's rows, CW columns of the tile ----
         constexpr int CW = L::CW, NB = CW / 32;
         const int ew = warp - 2, q = warp & 3, cw = CW * (ew >> 2);
-        uint8_t *stg = sm + L::OFF_STG + ew * F4_BLK;
+        uint8_t *stg = sm + L::OFF_STG + ew * L::BLK;
         float *bias = reinterpret_cast<float *>(sm + L::OFF_COLS) + ew * CW;
         uint32_t lt = 0;
         float next[NB];  // a lane's bias columns of the tile to come
@@ -319,9 +320,33 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
                 if (o.relu)
 #pragma unroll
                     for (int i = 0; i < 32; i++) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v[i]));
-                f4_store_block(o, stg, v, row0, col0 + 32 * b, M, N);
+                if (CG == 2 || !o.al) {
+                    f4_store_block(o, stg, v, row0, col0 + 32 * b, M, N);
+                    continue;
+                }
+                if (lane == 0) t2_store_wait_read<0>();  // the last tile's block has been read
+                __syncwarp();
+                if (o.type == MNMT_F32) {
+#pragma unroll
+                    for (int c = 0; c < 8; c++)
+                        *reinterpret_cast<uint4 *>(stg + lane * 128 + t2_chunk<128>(lane, c)) =
+                            make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; c++)
+                        *reinterpret_cast<uint4 *>(stg + lane * 64 + t2_chunk<64>(lane, c)) =
+                            make_uint4(f4_pair(v[8 * c], v[8 * c + 1], o.type), f4_pair(v[8 * c + 2], v[8 * c + 3], o.type),
+                                       f4_pair(v[8 * c + 4], v[8 * c + 5], o.type), f4_pair(v[8 * c + 6], v[8 * c + 7], o.type));
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    t2_store(&tmY, col0 + 32 * b, row0, s_addr(stg));
+                    t2_store_commit();
+                }
             }
         }
+        if (CG == 1 && lane == 0) t2_store_wait();
     }
 
     // ---- teardown: every MMA and copy has completed before a CTA ends ----
@@ -370,14 +395,20 @@ cudaError_t f4_init() {
 template <int CG, int BN, bool NV>
 cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &o, int *status, cudaStream_t st) {
     const int M = x.rows, N = w.rows, K = x.cols;
-    CUtensorMap ta, tb, tsa, tsb;
+    CUtensorMap ta, tb, tsa, tsb, ty;
     if (!encode_codes(&ta, x, F4_BM) || !encode_codes(&tb, w, BN / CG) || !encode_scales(&tsa, x, NV) || !encode_scales(&tsb, w, NV))
+        return cudaErrorInvalidValue;
+    ty = ta;
+    const int es = o.type == MNMT_F32 ? 4 : 2;
+    if (CG == 1 && o.al &&
+        !encode(&ty, es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, o.y, N, M, (cuuint64_t)o.ldy * es, 32, 32,
+                es == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
         return cudaErrorInvalidValue;
     const long tiles = (long)((M + CG * F4_BM - 1) / (CG * F4_BM)) * ((N + BN - 1) / BN);
     const long fit = CG == 2 ? g_f4_pairs : device_sm_count();
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, (int)(tiles < fit ? tiles : fit), F4Layout<CG, BN, NV>::THREADS, F4Layout<CG, BN, NV>::SMEM, st, attr);
-    return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV>, ta, tb, tsa, tsb, o, M, N, K, status);
+    return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV>, ta, tb, tsa, tsb, ty, o, M, N, K, status);
 }
 
 }  // namespace
