@@ -131,11 +131,6 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
     if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
     const int mt = (M + CG * F4_BM - 1) / (CG * F4_BM), nt = (N + BN - 1) / BN;
-    const long tiles = (long)mt * nt;
-    // the dimension of fewer tiles runs fastest: the larger operand is then read
-    // by CTAs that run at the same time
-    auto tile_m = [&](long t) { return (int)(mt <= nt ? t % mt : t / nt) * CG * F4_BM; };
-    auto tile_n = [&](long t) { return (int)(mt <= nt ? t / mt : t % nt) * BN; };
     const int steps = (K + 63) / 64, full = steps / 4, nkb = (K + F4_BK - 1) / F4_BK, tiles_k = fp4_tiles_k(K, NV);
 
     if (threadIdx.x == 0) {
@@ -175,8 +170,8 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
         uint32_t s = 0, phase = 1;  // slot, and the parity its release completes
         bool failed = false;
         const uint32_t ring = s_addr(sm), lead = CG == 1 ? bars : t2_mapa(bars, 0);
-        for (long tile = unit; tile < tiles && !failed && !*abort_flag; tile += units) {
-            const int m0 = tile_m(tile) + (int)rank * F4_BM, nb = tile_n(tile), n0 = nb + (int)rank * (BN / CG);
+        for (F4Walk w(mt, nt, unit, units); w.more() && !failed && !*abort_flag; w.next()) {
+            const int m0 = w.m() * CG * F4_BM + (int)rank * F4_BM, nb = w.n() * BN, n0 = nb + (int)rank * (BN / CG);
             // scale tiles of the rows' tile rows (tiles past the row's end belong
             // to k-steps that are not issued)
             int sa = (m0 >> 7) * tiles_k, sb = (nb >> 7) * tiles_k;
@@ -208,21 +203,20 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
         const uint32_t ring = s_addr(sm);
         const uint64_t a_desc = sw128_desc(ring), b_desc = sw128_desc(ring + L::A_BYTES);
         const uint64_t sa_desc = f4_scale_desc(ring + L::OFF_SFA), sb_desc = f4_scale_desc(ring + L::OFF_SFB);
-        for (long tile = unit; tile < tiles && !failed; tile += units, lt++) {
-            const uint32_t buf = lt & 1;
+        // Through a shuffle: every lane has the same value, and says so.  (Operands that
+        // the compiler cannot see to be uniform, or a test per MMA for the last k-block,
+        // cost more than the MMA: 8192^3 191 -> 157 us.)
+        const uint32_t base = __shfl_sync(0xFFFFFFFFu, tbase, 0), sfa = base + L::COL_SFA, cfb = base + L::COL_SFB;
+        for (F4Walk w(mt, nt, unit, units); w.more() && !failed; w.next(), lt++) {
+            const uint32_t buf = lt & 1, d = base + buf * BN;
+            // scale columns of the tile's first row of W: every other tile of 64 or 192 columns
+            // starts in the middle of a row tile, two columns on
+            const uint32_t sfb = __shfl_sync(0xFFFFFFFFu, cfb + ((uint32_t)(w.n() * BN & 127) >> 5), 0);
             if (lt >= 2 && !mbar_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
                 failed = true;
                 break;
             }
             tc_fence_after();
-            // Through a shuffle: every lane has the same value, and says so.  (Operands
-            // that the compiler cannot see to be uniform, or a test per MMA for the
-            // last k-block, cost more than the MMA: 8192^3 191 -> 157 us.)
-            const uint32_t d = __shfl_sync(0xFFFFFFFFu, tbase + buf * BN, 0);
-            // scale columns of the tile's first row of W: a tile may start in the middle of a row tile, two columns on
-            const uint32_t sfa = __shfl_sync(0xFFFFFFFFu, tbase + L::COL_SFA, 0);
-            const uint32_t sfb = __shfl_sync(0xFFFFFFFFu, tbase + L::COL_SFB + ((uint32_t)(tile_n(tile) & 127) >> 5), 0);
-            const uint32_t cfb = __shfl_sync(0xFFFFFFFFu, tbase + L::COL_SFB, 0);
             for (int kb = 0; kb < nkb; kb++) {
                 if (!mbar_wait(full_bar(s), phase)) {
                     failed = true;
@@ -270,23 +264,26 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
         const int ew = warp - 2, q = warp & 3, cw = CW * (ew >> 2);
         uint8_t *stg = sm + L::OFF_STG + ew * L::BLK;
         float *bias = reinterpret_cast<float *>(sm + L::OFF_COLS) + ew * CW;
+        const unsigned long long alpha = f4_two(o.alpha, o.alpha);
         uint32_t lt = 0;
         float next[NB];  // a lane's bias columns of the tile to come
-        auto fetch_bias = [&](long tile) {
+        F4Walk w(mt, nt, unit, units);
+        auto fetch_bias = [&]() {
 #pragma unroll
             for (int b = 0; b < NB; b++) {
-                const int n = tile_n(tile) + cw + 32 * b + lane;
-                next[b] = o.bias && tile < tiles && n < N ? o.bias[n] : 0.0f;
+                const int n = w.n() * BN + cw + 32 * b + lane;
+                next[b] = o.bias && w.more() && n < N ? o.bias[n] : 0.0f;
             }
         };
-        fetch_bias(unit);
-        for (long tile = unit; tile < tiles; tile += units, lt++) {
+        fetch_bias();
+        for (; w.more(); lt++) {
             const int buf = (int)(lt & 1);
-            const int row0 = tile_m(tile) + (int)rank * F4_BM + 32 * q, col0 = tile_n(tile) + cw;
+            const int row0 = w.m() * CG * F4_BM + (int)rank * F4_BM + 32 * q, col0 = w.n() * BN + cw;
             __syncwarp();
 #pragma unroll
             for (int b = 0; b < NB; b++) bias[32 * b + lane] = next[b];
-            fetch_bias(tile + units);
+            w.next();
+            fetch_bias();
             bool ok = *abort_flag == 0 && mbar_wait(accf_bar(buf), (lt >> 1) & 1);
             if (!ok && *abort_flag == 0) {
                 *abort_flag = 1;
@@ -310,12 +307,11 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
 #pragma unroll
                 for (int i = 0; i < 32; i += 4) {
                     const float4 c = *reinterpret_cast<const float4 *>(bias + 32 * b + i);
-                    const float cc[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        const float a = __uint_as_float(r[b][i + k]);
-                        v[i + k] = __fadd_rn(NV ? __fmul_rn(a, o.alpha) : a, cc[k]);
-                    }
+                    unsigned long long x = f4_two(__uint_as_float(r[b][i]), __uint_as_float(r[b][i + 1]));
+                    unsigned long long y = f4_two(__uint_as_float(r[b][i + 2]), __uint_as_float(r[b][i + 3]));
+                    if (NV) x = f4_mul2(x, alpha), y = f4_mul2(y, alpha);
+                    f4_untwo(f4_add2(x, f4_two(c.x, c.y)), v[i], v[i + 1]);
+                    f4_untwo(f4_add2(y, f4_two(c.z, c.w)), v[i + 2], v[i + 3]);
                 }
                 if (o.relu)
 #pragma unroll

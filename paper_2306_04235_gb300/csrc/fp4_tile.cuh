@@ -89,6 +89,45 @@ struct F4Out {
     const float *bias;
 };
 
+// The tiles of a unit (CTA or pair), every units-th one, without divisions after
+// the first: the dimension of fewer tiles runs fastest, so that the larger operand
+// is read by units that run at the same time.
+struct F4Walk {
+    int fast, slow, f, end, df, ds;
+    bool m_fast;
+    __device__ __forceinline__ F4Walk(int mt, int nt, int unit, int units) {
+        m_fast = mt <= nt;
+        f = m_fast ? mt : nt, end = m_fast ? nt : mt;
+        fast = unit % f, slow = unit / f;
+        df = units % f, ds = units / f;
+    }
+    __device__ __forceinline__ bool more() const { return slow < end; }
+    __device__ __forceinline__ int m() const { return m_fast ? fast : slow; }
+    __device__ __forceinline__ int n() const { return m_fast ? slow : fast; }
+    __device__ __forceinline__ void next() {
+        fast += df, slow += ds;
+        if (fast >= f) fast -= f, slow++;
+    }
+};
+
+// two fp32 at a time: sums and products, each rounded (the pair instructions of this part)
+__device__ __forceinline__ unsigned long long f4_two(float lo, float hi) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void f4_untwo(unsigned long long v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ unsigned long long f4_add2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ unsigned long long f4_mul2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // outputs c .. c + 1 of a row as a word of type's 16 bits
 __device__ __forceinline__ uint32_t f4_pair(float lo, float hi, int type) {
     if (type == MNMT_BF16) {
