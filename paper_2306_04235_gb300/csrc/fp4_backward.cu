@@ -709,7 +709,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
         CUtensorMap *t = tm + 2 * a.n;
         a.n++;
         r.rows = input ? M : N, r.cols = K, r.red = input ? N : M, r.a_mn = !input;
-        r.out = input ? F4Out{b.gx, b.ldgx, b.xdtype, 0, 0, b.nv ? b.w.g : 1.0f, nullptr} : F4Out{b.gw, b.ldgw, MNMT_F32, 0, 0, b.nv ? b.x.g : 1.0f, nullptr};
+        r.out = input ? F4Out{b.gx, b.ldgx, b.xdtype, 0, 0, 0, b.nv ? b.w.g : 1.0f, nullptr} : F4Out{b.gw, b.ldgw, MNMT_F32, 0, 0, 0, b.nv ? b.x.g : 1.0f, nullptr};
         r.out.al = out_alignment(r.out.y, r.out.ldy, r.out.type);
         r.mask = p.m[input].mask, r.mp = s.mp;
         r.parts = pl.parts[!input], r.len = pl.len[!input];
@@ -720,7 +720,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
             q.out = r.out, q.mask = r.mask, q.mp = s.mp;
             const long n = ((long)r.rows * fp4_div_up(K, 8) + 255) / 256, most = 8L * device_sm_count();
             q.blocks = (int)(n < most ? n : most);
-            r.out = F4Out{partial, s.pk, MNMT_F32, 1, 0, 1.0f, nullptr};
+            r.out = F4Out{partial, s.pk, MNMT_F32, out_alignment(partial, s.pk, MNMT_F32), 0, 0, 1.0f, nullptr};
             r.mask = nullptr;
             partial += partial_bytes(pl, !input, r.rows, K);
         }

@@ -16,8 +16,7 @@
 //                   waiting for those MMAs instead costs 8192^3 192 us), issues its
 //                   four MMAs, frees the slot;
 //   the others      drain a finished accumulator (TMEM holds two), apply alpha,
-//                   bias and ReLU, round, and store; 32 columns each: the chain of
-//                   one warp's instructions is what a small tile takes.
+//                   bias and ReLU, round, and store by TMA or from registers.
 // CG = 2: a pair of CTAs computes 256 x 192 tiles, each CTA half of the rows of
 // both operands; CG = 1: 128 x 128 or 128 x 64 tiles for smaller grids.
 // Every wait is bounded; one that runs out records MNMT_ETIMEOUT in *status, and
@@ -47,7 +46,7 @@ struct F4Layout {
     static constexpr uint32_t STAGE = OFF_SFB + R * T * 512;
     static constexpr int EPI = BN == 192 ? 12 : BN / 8, CW = 4 * BN / EPI;  // epilogue warps, columns of each (its 32 rows)
     static constexpr int THREADS = 64 + 32 * EPI;
-    static constexpr uint32_t BLK = CG == 1 ? 4096 : F4_BLK;  // a warp's staging block
+    static constexpr uint32_t BLK = CG == 1 ? 4096 : 2048;  // a warp's staging block
     static constexpr uint32_t OFF_AFTER = EPI * (BLK + CW * 4) + 512;  // staging, bias, barriers
     static constexpr int FIT = (int)((227 * 1024 - 1024 - OFF_AFTER) / STAGE);
     static constexpr int STAGES = FIT > 8 ? 8 : FIT;
@@ -316,33 +315,45 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
                 if (o.relu)
 #pragma unroll
                     for (int i = 0; i < 32; i++) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v[i]));
-                if (CG == 2 || !o.al) {
+                if (!o.tma) {
                     f4_store_block(o, stg, v, row0, col0 + 32 * b, M, N);
                     continue;
                 }
-                if (lane == 0) t2_store_wait_read<0>();  // the last tile's block has been read
-                __syncwarp();
-                if (o.type == MNMT_F32) {
+                // by TMA, rows of RB bytes: 32 16-bit columns, or 32 (pairs: 16, twice) fp32 from C0 on
+                auto send = [&](auto rb, auto first) {
+                    constexpr int RB = decltype(rb)::value, C0 = decltype(first)::value;
+                    if (lane == 0) t2_store_wait_read<0>();  // the block's earlier store has read it
+                    __syncwarp();
+                    if (o.type == MNMT_F32) {
 #pragma unroll
-                    for (int c = 0; c < 8; c++)
-                        *reinterpret_cast<uint4 *>(stg + lane * 128 + t2_chunk<128>(lane, c)) =
-                            make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+                        for (int c = 0; c < RB / 16; c++)
+                            *reinterpret_cast<uint4 *>(stg + lane * RB + t2_chunk<RB>(lane, c)) =
+                                make_uint4(__float_as_uint(v[C0 + 4 * c]), __float_as_uint(v[C0 + 4 * c + 1]), __float_as_uint(v[C0 + 4 * c + 2]),
+                                           __float_as_uint(v[C0 + 4 * c + 3]));
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; c++)
+                            *reinterpret_cast<uint4 *>(stg + lane * 64 + t2_chunk<64>(lane, c)) =
+                                make_uint4(f4_pair(v[8 * c], v[8 * c + 1], o.type), f4_pair(v[8 * c + 2], v[8 * c + 3], o.type),
+                                           f4_pair(v[8 * c + 4], v[8 * c + 5], o.type), f4_pair(v[8 * c + 6], v[8 * c + 7], o.type));
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (col0 + 32 * b + C0 < N) t2_store(&tmY, col0 + 32 * b + C0, row0, s_addr(stg));
+                        t2_store_commit();
+                    }
+                };
+                using std::integral_constant;
+                if constexpr (CG == 1) {
+                    send(integral_constant<int, 128>{}, integral_constant<int, 0>{});
                 } else {
-#pragma unroll
-                    for (int c = 0; c < 4; c++)
-                        *reinterpret_cast<uint4 *>(stg + lane * 64 + t2_chunk<64>(lane, c)) =
-                            make_uint4(f4_pair(v[8 * c], v[8 * c + 1], o.type), f4_pair(v[8 * c + 2], v[8 * c + 3], o.type),
-                                       f4_pair(v[8 * c + 4], v[8 * c + 5], o.type), f4_pair(v[8 * c + 6], v[8 * c + 7], o.type));
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) {
-                    t2_store(&tmY, col0 + 32 * b, row0, s_addr(stg));
-                    t2_store_commit();
+                    send(integral_constant<int, 64>{}, integral_constant<int, 0>{});
+                    if (o.type == MNMT_F32) send(integral_constant<int, 64>{}, integral_constant<int, 16>{});
                 }
             }
         }
-        if (CG == 1 && lane == 0) t2_store_wait();
+        if (lane == 0) t2_store_wait();
     }
 
     // ---- teardown: every MMA and copy has completed before a CTA ends ----
@@ -389,16 +400,22 @@ cudaError_t f4_init() {
 }
 
 template <int CG, int BN, bool NV>
-cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &o, int *status, cudaStream_t st) {
+cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &out, int *status, cudaStream_t st) {
     const int M = x.rows, N = w.rows, K = x.cols;
     CUtensorMap ta, tb, tsa, tsb, ty;
     if (!encode_codes(&ta, x, F4_BM) || !encode_codes(&tb, w, BN / CG) || !encode_scales(&tsa, x, NV) || !encode_scales(&tsb, w, NV))
         return cudaErrorInvalidValue;
+    // Stores by TMA: a store of 32 bytes per lane takes 61 passes through the L1 data
+    // pipe, which bounds small tiles (us, from registers / TMA: 512 x 32000 x 512 to
+    // fp32 19.3 / 15.0; pairs, 16384 x 8192, K = 256 76 / 52, 2048 101 / 95), but pairs
+    // of long K are bound by the MMAs (8192^3 152 / 155, to fp32 164 / 176).
+    F4Out o = out;
+    o.tma = o.al && (CG == 1 || K <= 4096);
     ty = ta;
     const int es = o.type == MNMT_F32 ? 4 : 2;
-    if (CG == 1 && o.al &&
-        !encode(&ty, es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, o.y, N, M, (cuuint64_t)o.ldy * es, 32, 32,
-                es == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
+    const bool wide = CG == 1 && es == 4;  // rows of 128 bytes, else 64
+    if (o.tma && !encode(&ty, es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, o.y, N, M, (cuuint64_t)o.ldy * es,
+                         (wide ? 128 : 64) / es, 32, wide ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
         return cudaErrorInvalidValue;
     const long tiles = (long)((M + CG * F4_BM - 1) / (CG * F4_BM)) * ((N + BN - 1) / BN);
     const long fit = CG == 2 ? g_f4_pairs : device_sm_count();
@@ -421,7 +438,7 @@ cudaError_t fp4_init() {
 
 cudaError_t launch_fp4_product(const Fp4Args &x, const Fp4Args &w, bool nv, float alpha, const float *bias, int relu, void *y, int ydtype,
                                long ldy, int *status, cudaStream_t st) {
-    const F4Out o{y, ldy, ydtype, out_alignment(y, ldy, ydtype), relu, alpha, bias};
+    const F4Out o{y, ldy, ydtype, out_alignment(y, ldy, ydtype), 0, relu, alpha, bias};
     auto go = [&](auto n) {
         constexpr bool NV = decltype(n)::value;
         switch (route_fp4_tiles(x.rows, w.rows, x.cols, device_sm_count())) {

@@ -84,6 +84,7 @@ struct F4Out {
     long ldy;
     int type;   // MNMT_F32 / BF16 / F16
     int al;     // every row starts on 32 bytes (2), 16 bytes (1), less (0)
+    int tma;    // stores by TMA
     int relu;
     float alpha;
     const float *bias;
@@ -138,10 +139,9 @@ __device__ __forceinline__ uint32_t f4_pair(float lo, float hi, int type) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// 32 columns of a warp's 32 rows (a row per lane) from column col on.  A lane
-// stores its row in whole 32-byte sectors; turning the block in shared memory for
-// longer runs costs more instructions than it saves (a tile of 128 x 128, K = 256:
-// 1.9 us).  Only what is unaligned or cut off at the matrix's edge is turned.
+// 32 columns of a warp's 32 rows (a row per lane) from column col on, from
+// registers: a lane stores its row in whole 32-byte sectors.  What is unaligned or
+// cut off at the matrix's edge is turned in shared memory first (blk).
 __device__ __forceinline__ void f4_store_block(const F4Out &o, uint8_t *blk, const float (&v)[32], int row0, int col, int M, int N) {
     const int lane = threadIdx.x & 31;
     const bool f32 = o.type == MNMT_F32;

@@ -164,17 +164,17 @@ inline bool route_fp4_small(int M, int N, int K) {
 //   columns 5.7), else by time, t + waves x (a + b k-blocks of 256) us, fitted to 510
 //   products of 40 to 16384 rows, 512 to 32000 columns and K of 256 to 8192 (us, 128
 //   columns / pairs):
-//     512 x 32000 x 512 13.6 / 14.5;  2048 x 8192 x 8192 54.6 / 44.6
-//     384 x 32000 x 512 10.3 / 14.7;  1600 x 1536 x 8192 17.5 / 13.0
-//     16384 x 8192 x 512 96 / 84;     9000 x 8192 x 8192 238 / 182
+//     512 x 32000 x 512 9.9 / 11.5;  384 x 32000 x 512 8.1 / 11.5
+//     4096 x 8192 x 512 16 / 18.3;  16384 x 8192 x 512 52.4 / 56.4
+//     2100 x 8192 x 8192 72.2 / 51.1;  16384 x 8192 x 8192 439 / 292
 enum Fp4Tiles { FP4_PAIR, FP4_128, FP4_64 };
 inline Fp4Tiles route_fp4_tiles(int M, int N, int K, int sms) {
     const long mt = (M + 127L) / 128, t64 = mt * ((N + 63L) / 64), t128 = mt * ((N + 127L) / 128);
     const long pairs = (M + 255L) / 256 * ((N + 191L) / 192), half = sms / 2;
     if (t64 <= sms) return FP4_64;
     const double kb = (K + 255) / 256;
-    const double single = 2.17 + (double)((t128 + sms - 1) / sms) * (1.46 + 0.207 * kb);
-    const double paired = 4.22 + (double)((pairs + half - 1) / half) * (2.0 + 0.203 * kb);
+    const double single = 3.8 + (double)((t128 + sms - 1) / sms) * (0.47 + 0.305 * kb);
+    const double paired = 5.11 + (double)((pairs + half - 1) / half) * (1.01 + 0.272 * kb);
     return single <= paired ? FP4_128 : FP4_PAIR;
 }
 
