@@ -599,7 +599,9 @@ Plan plan(int M, int N, int K, bool gx, bool gw) {
             const double len = share - BW_TILE > least ? share - BW_TILE : least;
             double parts = want[i] && nkb > len ? nkb / len + (few ? 0.0 : 0.99) : 1.0;
             if (parts > 64.0) parts = 64.0;
-            p.len[i] = fp4_div_up(nkb, parts < 1.0 ? 1 : (int)parts);
+            if (p.tiles[i] * parts > p.units) parts = (double)p.units / p.tiles[i];  // no second round of parts
+            p.parts[i] = parts < 1.0 ? 1 : (int)parts;
+            p.len[i] = fp4_div_up(nkb, p.parts[i]);
             p.parts[i] = fp4_div_up(nkb, p.len[i]);
             p.items += p.tiles[i] * p.parts[i];
         }
