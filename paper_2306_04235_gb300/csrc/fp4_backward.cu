@@ -130,7 +130,7 @@ struct BwLayout {
     static constexpr uint32_t A_BYTES = F4_BM * BW_BK * 2;
     static constexpr uint32_t B_BYTES = BN / CG * BW_BK * 2;
     static constexpr uint32_t STAGE = A_BYTES + B_BYTES;
-    static constexpr uint32_t STG = BW_EPI_WARPS * F4_BLK;
+    static constexpr uint32_t STG = BW_EPI_WARPS * 4096;  // a warp's two blocks of 2 KB
     static constexpr int FIT = (int)((227 * 1024 - 1024 - STG - 512) / STAGE);
     static constexpr int STAGES = FIT > 8 ? 8 : FIT;
     static constexpr uint32_t OFF_STG = STAGES * STAGE;
@@ -236,8 +236,8 @@ __device__ __noinline__ void bias_gradient(const BwArgs &a, int w, int n) {
 // 11 sum the bias gradient.  An item is a part of a tile.
 template <int CG, int BN>
 __global__ void __launch_bounds__(BW_THREADS, 1)
-    fp4_backward_gemm(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0,
-                      const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1,
+    fp4_backward_gemm(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmY0,
+                      const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ CUtensorMap tmY1,
                       const __grid_constant__ BwArgs a, int *status) {
     pdl_grid_wait();
     using L = BwLayout<CG, BN>;
@@ -414,8 +414,8 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
         // ---- epilogue ----
         constexpr int NB = BN / 64;
         const int ew = warp - 2, q = warp & 3, cw = (BN / 2) * (ew >> 2);
-        uint8_t *stg = sm + L::OFF_STG + ew * F4_BLK;
-        uint32_t lt = 0;
+        uint8_t *stg = sm + L::OFF_STG + ew * 4096;
+        uint32_t lt = 0, sent = 0;
         for (int phase = 0; phase < 3; phase++) {
             const Range rg = range(phase);
             const BwProduct &p = a.p[phase > 0];
@@ -475,10 +475,12 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                     if (col0 + 32 * b >= p.cols) continue;
 #pragma unroll
                     for (int i = 0; i < 32; i++) acc[b][i] = (in[b] >> i) & 1u ? __fmul_rn(acc[b][i], p.out.alpha) : 0.0f;
-                    f4_store_block(o, stg, acc[b], row0, col0 + 32 * b, p.rows, p.cols);
+                    if (o.tma) f4_send_block<64, 2>(o, phase ? &tmY1 : &tmY0, stg, sent, acc[b], row0, col0 + 32 * b, p.cols);
+                    else f4_store_block(o, stg, acc[b], row0, col0 + 32 * b, p.rows, p.cols);
                 }
             }
         }
+        if (lane == 0) t2_store_wait();
     }
 
     // ---- teardown: every MMA and copy has completed before a CTA ends ----
@@ -641,7 +643,7 @@ Scratch scratch(int M, int N, int K) {
 }
 
 template <int CG, int BN>
-cudaError_t bw_launch(const CUtensorMap (&tm)[4], const BwArgs &a, long items, int *status, cudaStream_t st) {
+cudaError_t bw_launch(const CUtensorMap (&tm)[6], const BwArgs &a, long items, int *status, cudaStream_t st) {
     const long fit = CG == 2 ? g_bw_pairs : device_sm_count();
     // the bias gradient's warps take the whole GPU where the products do not
     const long gb = a.gb ? (long)fp4_div_up(a.N, GB_COLS) * fp4_div_up(a.M, GB_ROWS) / (CG * BW_GB_WARPS) : 0;
@@ -649,7 +651,7 @@ cudaError_t bw_launch(const CUtensorMap (&tm)[4], const BwArgs &a, long items, i
     if (items < 1) items = 1;
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, (int)(items < fit ? items : fit), BW_THREADS, BwLayout<CG, BN>::SMEM, st, attr);
-    return cudaLaunchKernelEx(&cfg, fp4_backward_gemm<CG, BN>, tm[0], tm[1], tm[2], tm[3], a, status);
+    return cudaLaunchKernelEx(&cfg, fp4_backward_gemm<CG, BN>, tm[0], tm[1], tm[2], tm[3], tm[4], tm[5], a, status);
 }
 
 }  // namespace
@@ -696,7 +698,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
     a.g = copy ? p.g16 : p.g, a.ldg = copy ? s.pn : b.ldg;
     a.gb = b.gb, a.gb_part = reinterpret_cast<float *>(ws + s.gb), a.gb_tickets = tickets;
     a.p[0].parts = a.p[1].parts = 1;
-    CUtensorMap tm[4];
+    CUtensorMap tm[6];
     memset(tm, 0, sizeof(tm));
     FinishArgs f;
     memset(&f, 0, sizeof(f));
@@ -708,7 +710,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
         const bool input = (i == 0) == input_first;
         if (input ? !b.gx : !b.gw) continue;
         BwProduct &r = a.p[a.n];
-        CUtensorMap *t = tm + 2 * a.n;
+        CUtensorMap *t = tm + 3 * a.n;
         a.n++;
         r.rows = input ? M : N, r.cols = K, r.red = input ? N : M, r.a_mn = !input;
         r.out = input ? F4Out{b.gx, b.ldgx, b.xdtype, 0, 0, 0, b.nv ? b.w.g : 1.0f, nullptr} : F4Out{b.gw, b.ldgw, MNMT_F32, 0, 0, 0, b.nv ? b.x.g : 1.0f, nullptr};
@@ -727,6 +729,8 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
             partial += partial_bytes(pl, !input, r.rows, K);
         }
         r.chunk = r.out.type == MNMT_F32 ? BW_CHUNK : 1 << 24;
+        r.out.tma = r.out.al && r.parts == 1;
+        if (r.out.tma && !encode_out<64>(t + 2, r.out, r.rows, K)) return cudaErrorInvalidValue;
         if (!encode_bf16(t, a.g, N, M, a.ldg, input ? F4_BM : 64) || !encode_bf16(t + 1, p.m[!input].values, K, input ? N : M, s.pk, 64))
             return cudaErrorInvalidValue;
     }

@@ -264,7 +264,7 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
         uint8_t *stg = sm + L::OFF_STG + ew * L::BLK;
         float *bias = reinterpret_cast<float *>(sm + L::OFF_COLS) + ew * CW;
         const unsigned long long alpha = f4_two(o.alpha, o.alpha);
-        uint32_t lt = 0;
+        uint32_t lt = 0, sent = 0;
         float next[NB];  // a lane's bias columns of the tile to come
         F4Walk w(mt, nt, unit, units);
         auto fetch_bias = [&]() {
@@ -315,42 +315,8 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
                 if (o.relu)
 #pragma unroll
                     for (int i = 0; i < 32; i++) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v[i]));
-                if (!o.tma) {
-                    f4_store_block(o, stg, v, row0, col0 + 32 * b, M, N);
-                    continue;
-                }
-                // by TMA, rows of RB bytes: 32 16-bit columns, or 32 (pairs: 16, twice) fp32 from C0 on
-                auto send = [&](auto rb, auto first) {
-                    constexpr int RB = decltype(rb)::value, C0 = decltype(first)::value;
-                    if (lane == 0) t2_store_wait_read<0>();  // the block's earlier store has read it
-                    __syncwarp();
-                    if (o.type == MNMT_F32) {
-#pragma unroll
-                        for (int c = 0; c < RB / 16; c++)
-                            *reinterpret_cast<uint4 *>(stg + lane * RB + t2_chunk<RB>(lane, c)) =
-                                make_uint4(__float_as_uint(v[C0 + 4 * c]), __float_as_uint(v[C0 + 4 * c + 1]), __float_as_uint(v[C0 + 4 * c + 2]),
-                                           __float_as_uint(v[C0 + 4 * c + 3]));
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 4; c++)
-                            *reinterpret_cast<uint4 *>(stg + lane * 64 + t2_chunk<64>(lane, c)) =
-                                make_uint4(f4_pair(v[8 * c], v[8 * c + 1], o.type), f4_pair(v[8 * c + 2], v[8 * c + 3], o.type),
-                                           f4_pair(v[8 * c + 4], v[8 * c + 5], o.type), f4_pair(v[8 * c + 6], v[8 * c + 7], o.type));
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (col0 + 32 * b + C0 < N) t2_store(&tmY, col0 + 32 * b + C0, row0, s_addr(stg));
-                        t2_store_commit();
-                    }
-                };
-                using std::integral_constant;
-                if constexpr (CG == 1) {
-                    send(integral_constant<int, 128>{}, integral_constant<int, 0>{});
-                } else {
-                    send(integral_constant<int, 64>{}, integral_constant<int, 0>{});
-                    if (o.type == MNMT_F32) send(integral_constant<int, 64>{}, integral_constant<int, 16>{});
-                }
+                if (o.tma) f4_send_block<L::BLK / 32, 1>(o, &tmY, stg, sent, v, row0, col0 + 32 * b, N);
+                else f4_store_block(o, stg, v, row0, col0 + 32 * b, M, N);
             }
         }
         if (lane == 0) t2_store_wait();
@@ -412,11 +378,7 @@ cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &out, int 
     F4Out o = out;
     o.tma = o.al && (CG == 1 || K <= 4096);
     ty = ta;
-    const int es = o.type == MNMT_F32 ? 4 : 2;
-    const bool wide = CG == 1 && es == 4;  // rows of 128 bytes, else 64
-    if (o.tma && !encode(&ty, es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, o.y, N, M, (cuuint64_t)o.ldy * es,
-                         (wide ? 128 : 64) / es, 32, wide ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
-        return cudaErrorInvalidValue;
+    if (o.tma && !encode_out<F4Layout<CG, BN, NV>::BLK / 32>(&ty, o, M, N)) return cudaErrorInvalidValue;
     const long tiles = (long)((M + CG * F4_BM - 1) / (CG * F4_BM)) * ((N + BN - 1) / BN);
     const long fit = CG == 2 ? g_f4_pairs : device_sm_count();
     cudaLaunchAttribute attr[2];

@@ -3,6 +3,8 @@
 // to memory, tensor maps.
 #pragma once
 
+#include <type_traits>
+
 #include "fp4.cuh"
 #include "internal.h"
 #include "mbarrier.cuh"
@@ -207,6 +209,42 @@ __device__ __forceinline__ void f4_store_block(const F4Out &o, uint8_t *blk, con
     }
 }
 
+// The same by TMA (o.tma): blocks of 32 rows x 64 bytes (fp32 with RB = 128: 128) of
+// tensor map tm, staged in BLOCKS blocks at stg by turns; `sent` counts them.
+template <int RB, int BLOCKS>
+__device__ __forceinline__ void f4_send_block(const F4Out &o, const CUtensorMap *tm, uint8_t *stg, uint32_t &sent, const float (&v)[32], int row0, int col,
+                                              int N) {
+    const int lane = threadIdx.x & 31;
+    auto send = [&](auto first) {
+        constexpr int C0 = decltype(first)::value;
+        uint8_t *blk = stg + (sent++ & (BLOCKS - 1)) * (32 * RB);
+        if (lane == 0) t2_store_wait_read<BLOCKS - 1>();  // the block's earlier store has read it
+        __syncwarp();
+        if (o.type == MNMT_F32) {
+#pragma unroll
+            for (int c = 0; c < RB / 16; c++)
+                *reinterpret_cast<uint4 *>(blk + lane * RB + t2_chunk<RB>(lane, c)) =
+                    make_uint4(__float_as_uint(v[C0 + 4 * c]), __float_as_uint(v[C0 + 4 * c + 1]), __float_as_uint(v[C0 + 4 * c + 2]),
+                               __float_as_uint(v[C0 + 4 * c + 3]));
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; c++)
+                *reinterpret_cast<uint4 *>(blk + lane * 64 + t2_chunk<64>(lane, c)) =
+                    make_uint4(f4_pair(v[8 * c], v[8 * c + 1], o.type), f4_pair(v[8 * c + 2], v[8 * c + 3], o.type),
+                               f4_pair(v[8 * c + 4], v[8 * c + 5], o.type), f4_pair(v[8 * c + 6], v[8 * c + 7], o.type));
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            if (col + C0 < N) t2_store(tm, col + C0, row0, s_addr(blk));
+            t2_store_commit();
+        }
+    };
+    send(std::integral_constant<int, 0>{});
+    if constexpr (RB == 64)
+        if (o.type == MNMT_F32) send(std::integral_constant<int, 16>{});
+}
+
 // two-dimensional tensor map: w x h elements, rows `stride` bytes apart, boxes of bw x bh
 inline bool encode(CUtensorMap *tm, CUtensorMapDataType type, const void *p, cuuint64_t w, cuuint64_t h, cuuint64_t stride, cuuint32_t bw, cuuint32_t bh,
             CUtensorMapSwizzle sw) {
@@ -214,6 +252,15 @@ inline bool encode(CUtensorMap *tm, CUtensorMapDataType type, const void *p, cuu
     cuuint32_t box[2] = {bw, bh}, estr[2] = {1, 1};
     return tma_encoder()(tm, type, 2, const_cast<void *>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// the map for f4_send_block<RB, ...>
+template <int RB>
+bool encode_out(CUtensorMap *tm, const F4Out &o, int rows, int cols) {
+    const bool f32 = o.type == MNMT_F32, wide = f32 && RB == 128;
+    const int es = f32 ? 4 : 2;
+    return encode(tm, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, o.y, cols, rows, (cuuint64_t)o.ldy * es,
+                  (wide ? 128 : 64) / es, 32, wide ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 inline int out_alignment(const void *y, long ldy, int type) {
