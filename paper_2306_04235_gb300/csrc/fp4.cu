@@ -38,6 +38,7 @@ constexpr int FLIGHT = sizeof(T) == 2 ? 2 : 1;
 template <typename T, bool NV, bool VEC>
 __global__ void __launch_bounds__(256, ROW_BLOCKS) fp4_quantize_kernel(const T *x, long ldx, int alx, Fp4Args q, T *values, long ldv, int alv, int lr) {
     pdl_grid_wait();
+    pdl_allow_next();  // a product that follows sets itself up meanwhile
     MNMT_ROW_BUF(buf, VEC);
     constexpr int E = row_elements(VEC), LPB = fp4_block(NV) / E, U = FLIGHT<T>;  // lanes per block
     const int lane = threadIdx.x & 31;

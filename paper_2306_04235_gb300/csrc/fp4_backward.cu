@@ -87,6 +87,7 @@ MNMT_DEV void prepare_rows(const PrepMatrix &m, int pk, int mp, int block) {
 template <bool NV>
 __global__ void __launch_bounds__(256) fp4_backward_prepare(PrepArgs a) {
     pdl_grid_wait();
+    pdl_allow_next();  // the products' kernel sets itself up meanwhile
     int block = blockIdx.x;
 #pragma unroll
     for (int i = 0; i < 2; i++) {
@@ -239,7 +240,6 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
     fp4_backward_gemm(const __grid_constant__ CUtensorMap tmA0, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmY0,
                       const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ CUtensorMap tmY1,
                       const __grid_constant__ BwArgs a, int *status) {
-    pdl_grid_wait();
     using L = BwLayout<CG, BN>;
     constexpr int STAGES = L::STAGES, BOXES = BN / CG / 64;
 
@@ -319,6 +319,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tbase = misc[0];
+    pdl_grid_wait();  // nothing before this reads or writes global memory
 
     uint32_t issued = 0;
     if (warp == 0 && lane == 0) {

@@ -110,7 +110,6 @@ template <int CG, int BN, bool NV>
 __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
     fp4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmSA,
              const __grid_constant__ CUtensorMap tmSB, const __grid_constant__ CUtensorMap tmY, F4Out o, int M, int N, int K, int *status) {
-    pdl_grid_wait();
     using L = F4Layout<CG, BN, NV>;
     constexpr int STAGES = L::STAGES, T = L::T, R = L::R;
 
@@ -161,6 +160,7 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tbase = misc[0];
+    pdl_grid_wait();  // nothing before this reads or writes global memory
 
     uint32_t issued = 0;
     if (warp == 0) {
