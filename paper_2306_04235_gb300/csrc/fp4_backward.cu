@@ -692,6 +692,12 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
     p.g16 = copy ? reinterpret_cast<__nv_bfloat16 *>(ws + s.g) : nullptr;
     p.tickets = tickets, p.n_tickets = s.strips;
     p.M = M, p.N = N, p.pk = s.pk, p.mp = s.mp, p.pn = s.pn;
+    const long cap = 8L * device_sm_count();
+    auto blocks = [&](long threads) { return (int)((threads + 255) / 256 < cap ? (threads + 255) / 256 : cap); };
+    for (PrepMatrix &m : p.m) m.blocks = m.values || m.mask ? blocks((long)m.q.rows * s.pk / 8) : 0;
+    const int rest = copy ? blocks((long)M * s.pn / 8) : 1;
+    launch_pdl(b.nv ? fp4_backward_prepare<true> : fp4_backward_prepare<false>, p.m[0].blocks + p.m[1].blocks + rest, 256, 0, st, p);
+    if ((err = cudaGetLastError()) != cudaSuccess) return err;
 
     BwArgs a;
     memset(&a, 0, sizeof(a));
@@ -736,12 +742,6 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
             return cudaErrorInvalidValue;
     }
 
-    const long cap = 8L * device_sm_count();
-    auto blocks = [&](long threads) { return (int)((threads + 255) / 256 < cap ? (threads + 255) / 256 : cap); };
-    for (PrepMatrix &m : p.m) m.blocks = m.values || m.mask ? blocks((long)m.q.rows * s.pk / 8) : 0;
-    const int rest = copy ? blocks((long)M * s.pn / 8) : 1;
-    launch_pdl(b.nv ? fp4_backward_prepare<true> : fp4_backward_prepare<false>, p.m[0].blocks + p.m[1].blocks + rest, 256, 0, st, p);
-    if ((err = cudaGetLastError()) != cudaSuccess) return err;
     err = pl.pair ? bw_launch<2, 256>(tm, a, pl.items, b.status, st) : bw_launch<1, 64>(tm, a, pl.items, b.status, st);
     if (err != cudaSuccess || !split) return err;
     launch_pdl(fp4_backward_finish, f.p[0].blocks + f.p[1].blocks, 256, 0, st, f);
