@@ -47,17 +47,30 @@ struct PrepArgs {
     int n_tickets, M, N, pk, mp, pn;
 };
 
-// eight elements of a row per thread and step
+// A thread's groups of eight columns, every step-th one of all rows', without
+// divisions after the first (with one per group the whole call took 27.9 us at
+// 512 x 2048 x 2048, without 27.0).
+struct GroupWalk {
+    int row, group, groups, dr, dg;
+    MNMT_DEV GroupWalk(int first, int step, int n) : groups(n) {
+        row = first / n, group = first % n;
+        dr = step / n, dg = step % n;
+    }
+    MNMT_DEV void next() {
+        row += dr, group += dg;
+        if (group >= groups) group -= groups, row++;
+    }
+};
+
 template <bool NV, typename T>
 MNMT_DEV void prepare_rows(const PrepMatrix &m, int pk, int mp, int block) {
-    const int groups = pk / 8, tiles_k = fp4_tiles_k(m.q.cols, NV);
+    const int tiles_k = fp4_tiles_k(m.q.cols, NV);
     const size_t pitch = fp4_pitch(m.q.cols);
-    const long total = (long)m.q.rows * groups, step = m.blocks * 256L;
     const T *orig = static_cast<const T *>(m.orig);
     const bool vec = ((reinterpret_cast<uintptr_t>(orig) | (uintptr_t)m.ldo * sizeof(T)) & 15) == 0;
 #pragma unroll 2
-    for (long i = block * 256L + threadIdx.x; i < total; i += step) {
-        const int row = (int)(i / groups), c = (int)(i - (long)row * groups) * 8;
+    for (GroupWalk w(block * 256 + threadIdx.x, m.blocks * 256, pk / 8); w.row < m.q.rows; w.next()) {
+        const int row = w.row, c = 8 * w.group;
         const uint32_t byte = m.q.scales[fp4_scale_at(row, c / fp4_block(NV), tiles_k)];
         if (m.values) {
             const uint32_t codes = *reinterpret_cast<const uint32_t *>(m.q.codes + row * pitch + (c >> 1));
@@ -103,9 +116,9 @@ __global__ void __launch_bounds__(256) fp4_backward_prepare(PrepArgs a) {
     const int first = block * 256 + threadIdx.x, step = ((int)gridDim.x - a.m[0].blocks - a.m[1].blocks) * 256;
     for (int i = first; i < a.n_tickets; i += step) a.tickets[i] = 0;
     if (!a.g16) return;
-    const int groups = a.pn / 8;
-    for (long i = first; i < (long)a.M * groups; i += step) {
-        const int r = (int)(i / groups), c = (int)(i - (long)r * groups) * 8;
+    for (GroupWalk w(first, step, a.pn / 8); w.row < a.M; w.next()) {
+        const long r = w.row;
+        const int c = 8 * w.group;
         float v[8];
         load8<__nv_bfloat16, false>(a.g + r * a.ldg + c, a.N - c, v);
         store8<__nv_bfloat16, true>(a.g16 + (size_t)r * a.pn + c, 8, v);
@@ -519,10 +532,10 @@ __global__ void __launch_bounds__(256) fp4_backward_finish(FinishArgs a) {
     pdl_grid_wait();
     const bool second = (int)blockIdx.x >= a.p[0].blocks;
     const FinishProduct &p = a.p[second];
-    const int groups = fp4_div_up(p.cols, 8);
-    const long total = (long)p.rows * groups, part = (long)p.rows * p.ld;
-    for (long i = ((int)blockIdx.x - (second ? a.p[0].blocks : 0)) * 256L + threadIdx.x; i < total; i += p.blocks * 256L) {
-        const int row = (int)(i / groups), c = (int)(i - (long)row * groups) * 8, n = p.cols - c;
+    const long part = (long)p.rows * p.ld;
+    const int first = ((int)blockIdx.x - (second ? a.p[0].blocks : 0)) * 256 + threadIdx.x;
+    for (GroupWalk w(first, p.blocks * 256, fp4_div_up(p.cols, 8)); w.row < p.rows; w.next()) {
+        const int row = w.row, c = 8 * w.group, n = p.cols - c;
         const float *src = p.sums + (long)row * p.ld + c;
         float s[8] = {};
 #pragma unroll 4
