@@ -137,7 +137,7 @@ constexpr int BW_BK = 64;  // reduction indices per stage
 constexpr int BW_CHUNK = 16;  // stages
 constexpr int BW_TILE = 12;  // what an item takes beside its stages, in stages
 constexpr int BW_EPI_WARPS = 8, BW_GB_WARPS = 2, BW_THREADS = 64 + 32 * (BW_EPI_WARPS + BW_GB_WARPS);
-constexpr int GB_ROWS = 128, GB_COLS = 256;  // rows and columns of G that a warp sums at a time
+constexpr int GB_COLS = 256, GB_FLIGHT = 16;  // columns of G that a warp sums at a time, rows that it loads at a time
 
 template <int CG, int BN>
 struct BwLayout {
@@ -168,9 +168,11 @@ struct BwProduct {
 struct BwArgs {
     BwProduct p[2];
     int n;  // products
-    // bias gradient: G, partial column sums [ceil(M / 128)][N], done per 256 columns; gb may be null
+    // bias gradient: G (readable up to column gcols), partial column sums
+    // [blocks of rows][N], done per 256 columns; gb may be null
     const __nv_bfloat16 *g;
     long ldg;
+    int gcols, gb_rows;  // rows: that a warp sums at a time
     float *gb, *gb_part;
     int *gb_tickets;
     int M, N;
@@ -189,29 +191,41 @@ __host__ __device__ constexpr uint32_t bw_idesc(int m, int n, bool a_mn) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-// The bias gradient by warps w of n: 128 rows x 256 columns at a time, eight
-// columns per lane; the warp that finishes the last row block of 256 columns adds
-// the blocks' sums in their order.
+// The bias gradient by warps w of n: gb_rows x 256 columns at a time, eight columns
+// per lane; the warp that finishes the last row block of 256 columns adds the
+// blocks' sums in their order.
 __device__ __noinline__ void bias_gradient(const BwArgs &a, int w, int n) {
     const int lane = threadIdx.x & 31;
-    const int strips = fp4_div_up(a.N, GB_COLS), blocks = fp4_div_up(a.M, GB_ROWS);
+    const int strips = fp4_div_up(a.N, GB_COLS), blocks = fp4_div_up(a.M, a.gb_rows);
     const bool vec = (reinterpret_cast<uintptr_t>(a.g) & 15) == 0 && a.ldg % 8 == 0;
     for (long i = w; i < (long)strips * blocks; i += n) {
         const int block = (int)(i / strips), strip = (int)(i - (long)block * strips), c = strip * GB_COLS + 8 * lane;
-        const int r1 = min(a.M, (block + 1) * GB_ROWS);
+        const int r0 = block * a.gb_rows, r1 = min(a.M, r0 + a.gb_rows);
         float s[8] = {};
         if (c < a.N) {
             const __nv_bfloat16 *p = a.g + c;
-            if (vec && c + 8 <= a.N) {
-#pragma unroll 8
-                for (int r = block * GB_ROWS; r < r1; r++) {
-                    float v[8];
-                    load8<__nv_bfloat16, true>(p + r * a.ldg, 8, v);
+            if (vec && c + 8 <= a.gcols) {
+                auto add = [&](int r, int n) {
+                    uint4 w[GB_FLIGHT];
 #pragma unroll
-                    for (int k = 0; k < 8; k++) s[k] = __fadd_rn(s[k], v[k]);
-                }
+                    for (int u = 0; u < GB_FLIGHT; u++)
+                        w[u] = u < n ? *reinterpret_cast<const uint4 *>(p + (r + u) * a.ldg) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int u = 0; u < GB_FLIGHT; u++) {
+                        const uint32_t x[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            s[2 * k] = __fadd_rn(s[2 * k], __uint_as_float(x[k] << 16));
+                            s[2 * k + 1] = __fadd_rn(s[2 * k + 1], __uint_as_float(x[k] & 0xFFFF0000u));
+                        }
+                    }
+                };
+                int r = r0;
+                for (; r + GB_FLIGHT <= r1; r += GB_FLIGHT) add(r, GB_FLIGHT);
+                if (r < r1) add(r, r1 - r);
             } else {
-                for (int r = block * GB_ROWS; r < r1; r++) {
+#pragma unroll 4
+                for (int r = r0; r < r1; r++) {
                     float v[8];
                     load8<__nv_bfloat16, false>(p + r * a.ldg, a.N - c, v);
 #pragma unroll
@@ -231,7 +245,7 @@ __device__ __noinline__ void bias_gradient(const BwArgs &a, int w, int n) {
             __threadfence();
             const float4 *in = reinterpret_cast<const float4 *>(a.gb_part + c);
             float4 lo = make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi = lo;
-#pragma unroll 4
+#pragma unroll 8
             for (int b = 0; b < blocks; b++) {
                 const float4 x = __ldcg(in + (size_t)b * strips * (GB_COLS / 4)), y = __ldcg(in + (size_t)b * strips * (GB_COLS / 4) + 1);
                 lo.x = __fadd_rn(lo.x, x.x), lo.y = __fadd_rn(lo.y, x.y), lo.z = __fadd_rn(lo.z, x.z), lo.w = __fadd_rn(lo.w, x.w);
@@ -630,6 +644,19 @@ Plan plan(int M, int N, int K, bool gx, bool gw) {
 }
 size_t partial_bytes(const Plan &p, int i, int rows, int K) { return p.parts[i] > 1 ? (size_t)p.parts[i] * rows * up8(K) * 4 : 0; }
 
+// Rows of G that a warp sums at a time.  It waits for memory once per GB_FLIGHT rows,
+// the last warp of 256 columns then once per eight partial sums: about sqrt(2 M)
+// rows make that shortest, more where the warps have more to do (two per SM beside the
+// products, ten without), at most 512 (sums of fp32).  With 128 rows for all, eight at a time: 1001 x 771 x 389 25.8 us (so: 14.4),
+// 16384 x 2048 x 512 83.8 (63.3).
+int gb_rows(int M, int N, bool products) {
+    if (M <= 64) return 64;  // nothing to join
+    const int per = 152 * (BW_GB_WARPS + (products ? 0 : BW_EPI_WARPS)) / fp4_div_up(N, GB_COLS);
+    int r = fp4_div_up(fp4_div_up(M, per > 1 ? per : 1), GB_FLIGHT) * GB_FLIGHT;
+    while ((long)r * r < 2L * M) r += GB_FLIGHT;
+    return r < 512 ? r : 512;
+}
+
 // scratch: W and X in bf16, their masks, a copy of G, sums of the bias gradient, of split products, tickets
 struct Scratch {
     size_t w, x, mw, mx, g, gb, partial, tickets, bytes;
@@ -644,7 +671,7 @@ Scratch scratch(int M, int N, int K) {
     s.mx = s.mw + (size_t)N * s.mp;
     s.g = s.mx + (size_t)M * s.mp;
     s.gb = s.g + up16((size_t)M * s.pn * 2);
-    s.partial = s.gb + (size_t)fp4_div_up(M, GB_ROWS) * s.strips * GB_COLS * 4;
+    s.partial = s.gb + (size_t)fp4_div_up(M, gb_rows(M, N, false)) * s.strips * GB_COLS * 4;
     size_t most = 0;
     for (int w = 1; w < 4; w++) {
         const Plan p = plan(M, N, K, w & 1, w & 2);
@@ -660,7 +687,7 @@ template <int CG, int BN>
 cudaError_t bw_launch(const CUtensorMap (&tm)[6], const BwArgs &a, long items, int *status, cudaStream_t st) {
     const long fit = CG == 2 ? g_bw_pairs : device_sm_count();
     // the bias gradient's warps take the whole GPU where the products do not
-    const long gb = a.gb ? (long)fp4_div_up(a.N, GB_COLS) * fp4_div_up(a.M, GB_ROWS) / (CG * BW_GB_WARPS) : 0;
+    const long gb = a.gb ? (long)fp4_div_up(a.N, GB_COLS) * fp4_div_up(a.M, a.gb_rows) / (CG * BW_GB_WARPS) : 0;
     if (items < gb) items = gb;
     if (items < 1) items = 1;
     cudaLaunchAttribute attr[2];
@@ -715,7 +742,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
     BwArgs a;
     memset(&a, 0, sizeof(a));
     a.M = M, a.N = N;
-    a.g = copy ? p.g16 : p.g, a.ldg = copy ? s.pn : b.ldg;
+    a.g = copy ? p.g16 : p.g, a.ldg = copy ? s.pn : b.ldg, a.gcols = copy ? s.pn : N, a.gb_rows = gb_rows(M, N, products);
     a.gb = b.gb, a.gb_part = reinterpret_cast<float *>(ws + s.gb), a.gb_tickets = tickets;
     a.p[0].parts = a.p[1].parts = 1;
     CUtensorMap tm[6];
