@@ -9,6 +9,10 @@
 // key = seed: 128 bits, a 16-bit field for each of eight neighbouring columns.
 // 16 bits, not 32, because ten rounds per four elements would take as long as
 // the elements' bytes; the keep probability is then a multiple of 2^-16.
+// Bound by memory where elements are wide (16384 x 2048 bf16 onto an fp32 residual
+// 55 us, 6.1 TB/s), by the generator's and the moves' instructions where they are
+// narrow or start anywhere (16384 x 2048 bf16 to bf16 33 us, 4.0 TB/s; backward of
+// 5003 x 1001 fp16 with all gradients 20 us, 3.9 TB/s).
 #include <type_traits>
 
 #include "fp4.cuh"

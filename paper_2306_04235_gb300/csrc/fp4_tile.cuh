@@ -14,11 +14,10 @@
 namespace mnmt {
 
 constexpr int F4_BM = 128;  // rows of a tile per CTA
-constexpr int F4_BLK = 1024;  // a warp's staging block, for outputs without alignment: 32 rows of 32 bytes
 
 // An epilogue warp has read an accumulator (tcgen05.wait::ld): the leader's MMAs
 // may overwrite it.  Relaxed: nothing in memory is handed over, and a release
-// would wait for the warp's own stores of the tile before (16384 x 8192 x 2048: 142 us).
+// would wait for the warp's own stores of the tile before (16384 x 8192 x 2048: 142 us, 109 so).
 template <int CG>
 __device__ __forceinline__ void f4_release(uint32_t bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(CG == 1 ? bar : t2_mapa(bar, 0)) : "memory");
@@ -143,7 +142,7 @@ __device__ __forceinline__ uint32_t f4_pair(float lo, float hi, int type) {
 
 // 32 columns of a warp's 32 rows (a row per lane) from column col on, from
 // registers: a lane stores its row in whole 32-byte sectors.  What is unaligned or
-// cut off at the matrix's edge is turned in shared memory first (blk).
+// cut off at the matrix's edge is turned in shared memory first (blk: 1 KB).
 __device__ __forceinline__ void f4_store_block(const F4Out &o, uint8_t *blk, const float (&v)[32], int row0, int col, int M, int N) {
     const int lane = threadIdx.x & 31;
     const bool f32 = o.type == MNMT_F32;
