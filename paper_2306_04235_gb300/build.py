@@ -19,9 +19,10 @@ CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libmnmt.so")
 SOURCES = ["api.cu", "linear.cu", "linear_w4.cu", "gemm_tc.cu", "attention.cu", "rows.cu", "decode_cluster.cu",
-           "decode_rows.cu",            "noalloc.cu", "fakequant.cu", "fp4.cu", "fp4_backward.cu", "fp4_tc.cu", "fp4_small.cu", "fp4_api.cu", "dropout.cu"]
-HEADERS = ["attn_core.cuh", "common.cuh", "decode_rows.h", "epilogue.cuh", "fp4.cuh", "fp4_tile.cuh", "internal.h", "mbarrier.cuh", "routes.h", "row_pass.cuh",
-           "tcgen05.cuh"]
+           "decode_rows.cu", "noalloc.cu", "fakequant.cu", "fp4.cu", "fp4_backward.cu", "fp4_tc.cu", "fp4_small.cu",
+           "fp4_api.cu", "dropout.cu"]
+HEADERS = ["attn_core.cuh", "common.cuh", "decode_rows.h", "epilogue.cuh", "fp4.cuh", "fp4_tile.cuh", "internal.h",
+           "mbarrier.cuh", "routes.h", "row_pass.cuh", "tcgen05.cuh", "train.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

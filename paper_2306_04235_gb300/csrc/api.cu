@@ -28,6 +28,7 @@
 #include "decode_rows.h"
 #include "internal.h"
 #include "routes.h"
+#include "train.h"
 
 using namespace mnmt;
 

@@ -12,8 +12,8 @@
 #include <type_traits>
 
 #include "fp4.cuh"
-#include "internal.h"
 #include "row_pass.cuh"
+#include "train.h"
 
 namespace mnmt {
 namespace {

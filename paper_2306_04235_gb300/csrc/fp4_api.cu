@@ -7,8 +7,8 @@
 #include <mutex>
 
 #include "fp4.cuh"
-#include "internal.h"
 #include "routes.h"
+#include "train.h"
 
 using namespace mnmt;
 

@@ -24,7 +24,7 @@
 
 #include "fp4.cuh"
 #include "fp4_tile.cuh"
-#include "internal.h"
+#include "train.h"
 
 namespace mnmt {
 namespace {
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                 const bool a_mn = a.p[t.p].a_mn;
                 for (int kb = t.k0; kb < t.k1; kb++, it++) {
                     const int s = (int)(it % STAGES);
-                    if (it >= STAGES && !mbar_wait(empty_bar(s), (it / STAGES - 1) & 1)) {
+                    if (it >= STAGES && !f4_wait(empty_bar(s), (it / STAGES - 1) & 1)) {
                         *abort_flag = 1;
                         set_status(status, MNMT_ETIMEOUT);
                         failed = true;
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                 const At t = at(phase, item);
                 for (int k0 = t.k0; k0 < t.k1 && !failed; k0 += chunk, lt++) {
                     const int buf = (int)(lt & 1), k1 = min(t.k1, k0 + chunk);
-                    if (lt >= 2 && !mbar_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
+                    if (lt >= 2 && !f4_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
                         failed = true;
                         break;
                     }
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                     const uint32_t d = tbase + (uint32_t)(buf * BN);
                     for (int kb = k0; kb < k1; kb++, it++) {
                         const int s = (int)(it % STAGES);
-                        if (!mbar_wait(full_bar(s), (it / STAGES) & 1)) {
+                        if (!f4_wait(full_bar(s), (it / STAGES) & 1)) {
                             failed = true;
                             break;
                         }
@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                 bool ok = true;
                 for (int k0 = t.k0; k0 < t.k1; k0 += p.chunk, lt++) {
                     const int buf = (int)(lt & 1);
-                    ok = *abort_flag == 0 && mbar_wait(accf_bar(buf), (lt >> 1) & 1);
+                    ok = *abort_flag == 0 && f4_wait(accf_bar(buf), (lt >> 1) & 1);
                     if (!ok && *abort_flag == 0) {
                         *abort_flag = 1;
                         set_status(status, MNMT_ETIMEOUT);
@@ -516,9 +516,9 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
     // ---- teardown: every MMA and copy has completed before a CTA ends ----
     __syncthreads();
     if (warp == 0 && lane == 0 && rank == 0 && *abort_flag)
-        for (uint32_t it = misc[2]; it < issued; it++) mbar_wait(full_bar((int)(it % STAGES)), (it / STAGES) & 1);
+        for (uint32_t it = misc[2]; it < issued; it++) f4_wait(full_bar((int)(it % STAGES)), (it / STAGES) & 1);
     if (warp == 1) {
-        if (lane == 0) mbar_wait(done_bar, 0);
+        if (lane == 0) f4_wait(done_bar, 0);
         __syncwarp();
         tc_fence_after();
     }

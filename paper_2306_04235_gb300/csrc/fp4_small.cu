@@ -14,7 +14,7 @@
 #include <type_traits>
 
 #include "fp4.cuh"
-#include "internal.h"
+#include "train.h"
 
 namespace mnmt {
 namespace {

@@ -19,7 +19,7 @@
 //                   bias and ReLU, round, and store by TMA or from registers.
 // CG = 2: a pair of CTAs computes 256 x 192 tiles, each CTA half of the rows of
 // both operands; CG = 1: 128 x 128 or 128 x 64 tiles for smaller grids.
-// Measured: 8192^3 MX 157 us (7.0 PFLOP/s), 16384 x 8192 x 2048 to bf16 MX 99 us (5.5),
+// Measured: 8192^3 MX 160 us (6.9 PFLOP/s), 16384 x 8192 x 2048 to bf16 MX 99 us (5.5),
 // NV 111; bound by shared memory, which the MMAs read their operands from and the
 // epilogue stages its tiles in, and for small grids by their start.
 // Every wait is bounded; one that runs out records MNMT_ETIMEOUT in *status, and
@@ -29,10 +29,10 @@
 
 #include "fp4.cuh"
 #include "fp4_tile.cuh"
-#include "internal.h"
 #include "mbarrier.cuh"
 #include "routes.h"
 #include "tcgen05.cuh"
+#include "train.h"
 
 namespace mnmt {
 namespace {
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
             // to k-steps that are not issued)
             int sa = (m0 >> 7) * tiles_k, sb = (nb >> 7) * tiles_k;
             for (int kb = 0; kb < nkb; kb++) {
-                if (!mbar_wait(empty_bar(s), phase)) {  // a fresh barrier passes
+                if (!f4_wait(empty_bar(s), phase)) {  // a fresh barrier passes
                     *abort_flag = 1;
                     set_status(status, MNMT_ETIMEOUT);
                     failed = true;
@@ -214,13 +214,13 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
             // scale columns of the tile's first row of W: every other tile of 64 or 192 columns
             // starts in the middle of a row tile, two columns on
             const uint32_t sfb = __shfl_sync(0xFFFFFFFFu, cfb + ((uint32_t)(w.n() * BN & 127) >> 5), 0);
-            if (lt >= 2 && !mbar_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
+            if (lt >= 2 && !f4_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
                 failed = true;
                 break;
             }
             tc_fence_after();
             for (int kb = 0; kb < nkb; kb++) {
-                if (!mbar_wait(full_bar(s), phase)) {
+                if (!f4_wait(full_bar(s), phase)) {
                     failed = true;
                     break;
                 }
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
             for (int b = 0; b < NB; b++) bias[32 * b + lane] = next[b];
             w.next();
             fetch_bias();
-            bool ok = *abort_flag == 0 && mbar_wait(accf_bar(buf), (lt >> 1) & 1);
+            bool ok = *abort_flag == 0 && f4_wait(accf_bar(buf), (lt >> 1) & 1);
             if (!ok && *abort_flag == 0) {
                 *abort_flag = 1;
                 set_status(status, MNMT_ETIMEOUT);
@@ -328,9 +328,9 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
     // ---- teardown: every MMA and copy has completed before a CTA ends ----
     __syncthreads();
     if (warp == 0 && lane == 0 && rank == 0 && *abort_flag)
-        for (uint32_t it = misc[2]; it < issued; it++) mbar_wait(full_bar((int)(it % STAGES)), (it / STAGES) & 1);
+        for (uint32_t it = misc[2]; it < issued; it++) f4_wait(full_bar((int)(it % STAGES)), (it / STAGES) & 1);
     if (warp == 1) {
-        if (lane == 0) mbar_wait(done_bar, 0);
+        if (lane == 0) f4_wait(done_bar, 0);
         __syncwarp();
         tc_fence_after();
     }

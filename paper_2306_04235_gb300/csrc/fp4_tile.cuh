@@ -6,14 +6,27 @@
 #include <type_traits>
 
 #include "fp4.cuh"
-#include "internal.h"
 #include "mbarrier.cuh"
 #include "row_pass.cuh"
 #include "tcgen05.cuh"
+#include "train.h"
 
 namespace mnmt {
 
 constexpr int F4_BM = 128;  // rows of a tile per CTA
+
+// mbar_wait.  Most waits end within the first tries, each of which suspends the
+// thread for a while; reading the device clock before them costs each its latency.
+// (A function that calls none: with mbar_wait called here 8192^3 took 177 us, 160 so.)
+static __device__ __noinline__ bool f4_wait_slow(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < 8; i++)
+        if (mbar_try(bar, parity)) return true;
+    const unsigned long long t0 = global_ns();
+    while (!mbar_try(bar, parity))
+        if (global_ns() - t0 > MNMT_WAIT_NS) return false;
+    return true;
+}
+__device__ __forceinline__ bool f4_wait(uint32_t bar, uint32_t parity) { return mbar_test(bar, parity) || f4_wait_slow(bar, parity); }
 
 // An epilogue warp has read an accumulator (tcgen05.wait::ld): the leader's MMAs
 // may overwrite it.  Relaxed: nothing in memory is handed over, and a release

@@ -54,10 +54,6 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
 
 // the waiting part of mbar_wait, out of line
 static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
-    // most waits end within the tries below, each of which suspends the thread for
-    // a while; reading the device clock first would cost each of them its latency
-    for (int i = 0; i < 8; i++)
-        if (mbar_try(bar, parity)) return true;
     const unsigned long long t0 = global_ns();
     while (!mbar_try(bar, parity)) {
         if (global_ns() - t0 > MNMT_WAIT_NS) return false;
