@@ -29,6 +29,8 @@
 namespace mnmt {
 namespace {
 
+__host__ __device__ constexpr int up32(int n) { return (n + 31) / 32 * 32; }
+
 // what is made of a packed matrix: its values in bf16 (without the tensor scale),
 // rows pk apart, and a bit per element, set where the float original lies within
 // the range of its block, rows of mp bytes; each may be null
@@ -498,15 +500,15 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
                     if (lane == 0) f4_release<CG>(acce_bar(buf));
                 }
                 if (!ok || row0 >= p.rows) continue;
-                F4Out o = p.out;
-                o.y = static_cast<uint8_t *>(o.y) + (p.parts > 1 ? (size_t)(t.k0 / p.len) * p.rows * o.ldy * 4 : 0);
+                // parts of a split product: 32 rows and more apart, all by TMA
+                const int part0 = p.parts > 1 ? t.k0 / p.len * up32(p.rows) : 0;
 #pragma unroll
                 for (int b = 0; b < NB; b++) {
                     if (col0 + 32 * b >= p.cols) continue;
 #pragma unroll
                     for (int i = 0; i < 32; i++) acc[b][i] = (in[b] >> i) & 1u ? __fmul_rn(acc[b][i], p.out.alpha) : 0.0f;
-                    if (o.tma) f4_send_block<64, 2>(o, phase ? &tmY1 : &tmY0, stg, sent, acc[b], row0, col0 + 32 * b, p.cols);
-                    else f4_store_block(o, stg, acc[b], row0, col0 + 32 * b, p.rows, p.cols);
+                    if (p.out.tma) f4_send_block<64, 2>(p.out, phase ? &tmY1 : &tmY0, stg, sent, acc[b], part0 + row0, col0 + 32 * b, p.cols);
+                    else f4_store_block<4096, false>(p.out, stg, acc[b], row0, col0 + 32 * b, p.rows, p.cols);
                 }
             }
         }
@@ -533,7 +535,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
 // the parts of split products
 // ---------------------------------------------------------------------------
 struct FinishProduct {
-    const float *sums;  // [parts][rows][ld]
+    const float *sums;  // [parts][rows in whole 32][ld]
     int parts, rows, cols, ld, blocks;
     F4Out out;
     const uint8_t *mask;
@@ -548,7 +550,7 @@ __global__ void __launch_bounds__(256) fp4_backward_finish(FinishArgs a) {
     pdl_grid_wait();
     const bool second = (int)blockIdx.x >= a.p[0].blocks;
     const FinishProduct &p = a.p[second];
-    const long part = (long)p.rows * p.ld;
+    const long part = (long)up32(p.rows) * p.ld;
     const int first = ((int)blockIdx.x - (second ? a.p[0].blocks : 0)) * 256 + threadIdx.x;
     for (GroupWalk w(first, p.blocks * 256, fp4_div_up(p.cols, 8)); w.row < p.rows; w.next()) {
         const int row = w.row, c = 8 * w.group, n = p.cols - c;
@@ -644,7 +646,7 @@ Plan plan(int M, int N, int K, bool gx, bool gw) {
     }
     return best;
 }
-size_t partial_bytes(const Plan &p, int i, int rows, int K) { return p.parts[i] > 1 ? (size_t)p.parts[i] * rows * up8(K) * 4 : 0; }
+size_t partial_bytes(const Plan &p, int i, int rows, int K) { return p.parts[i] > 1 ? (size_t)p.parts[i] * up32(rows) * up8(K) * 4 : 0; }
 
 // Rows of G that a warp sums at a time.  It waits for memory once per GB_FLIGHT rows,
 // the last warp of 256 columns then once per eight partial sums: about sqrt(2 M)
@@ -778,8 +780,8 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
             partial += partial_bytes(pl, !input, r.rows, K);
         }
         r.chunk = r.out.type == MNMT_F32 ? BW_CHUNK : 1 << 24;
-        r.out.tma = r.out.al && r.parts == 1;
-        if (r.out.tma && !encode_out<64>(t + 2, r.out, r.rows, K)) return cudaErrorInvalidValue;
+        r.out.tma = r.out.al > 0;
+        if (r.out.tma && !encode_out<64>(t + 2, r.out, r.parts > 1 ? r.parts * up32(r.rows) : r.rows, K)) return cudaErrorInvalidValue;
         if (!encode_bf16(t, a.g, N, M, a.ldg, input ? F4_BM : 64) || !encode_bf16(t + 1, p.m[!input].values, K, input ? N : M, s.pk, 64))
             return cudaErrorInvalidValue;
     }

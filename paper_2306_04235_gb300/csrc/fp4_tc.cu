@@ -109,7 +109,12 @@ __device__ __forceinline__ void f4_copy_scales_on(uint32_t on, uint32_t taddr, u
                      : "memory");
 }
 
-template <int CG, int BN, bool NV>
+// how a tile is stored: F4_BY_TMA where every row is aligned, else from registers;
+// pairs know it when they are compiled (for the registers: 16384 x 8192 x 2048
+// 92.5 us, 94.8 with both)
+enum { F4_EITHER, F4_BY_TMA, F4_BY_LANES };
+
+template <int CG, int BN, bool NV, int ST>
 __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
     fp4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmSA,
              const __grid_constant__ CUtensorMap tmSB, const __grid_constant__ CUtensorMap tmY, F4Out o, int M, int N, int K, int *status) {
@@ -318,8 +323,10 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
                 if (o.relu)
 #pragma unroll
                     for (int i = 0; i < 32; i++) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v[i]));
-                if (o.tma) f4_send_block<L::BLK / 32, 1>(o, &tmY, stg, sent, v, row0, col0 + 32 * b, N);
-                else f4_store_block(o, stg, v, row0, col0 + 32 * b, M, N);
+                const int col = col0 + 32 * b;
+                if (ST == F4_BY_TMA || (ST == F4_EITHER && o.tma)) f4_send_block<L::BLK / 32, 1>(o, &tmY, stg, sent, v, row0, col, N);
+                else if (ST == F4_BY_LANES && o.al && col + 32 <= N) f4_store_rows(o, v, row0, col, M);
+                else f4_store_block<L::BLK, CG == 2>(o, stg, v, row0, col, M, N);
             }
         }
         if (lane == 0) t2_store_wait();
@@ -356,14 +363,14 @@ bool encode_scales(CUtensorMap *tm, const Fp4Args &q, bool nv) {
     return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT32, q.scales, 128, n, 512, 128, nv ? 4 : 2, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-template <int CG, int BN, bool NV>
+template <int CG, int BN, bool NV, int ST = F4_EITHER>
 cudaError_t f4_init() {
-    cudaError_t err = cudaFuncSetAttribute(fp4_gemm<CG, BN, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F4Layout<CG, BN, NV>::SMEM);
+    cudaError_t err = cudaFuncSetAttribute(fp4_gemm<CG, BN, NV, ST>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F4Layout<CG, BN, NV>::SMEM);
     if (err != cudaSuccess || CG == 1) return err;
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, 64, F4Layout<CG, BN, NV>::THREADS, F4Layout<CG, BN, NV>::SMEM, nullptr, attr);
     int n = 0;
-    err = cudaOccupancyMaxActiveClusters(&n, fp4_gemm<CG, BN, NV>, &cfg);
+    err = cudaOccupancyMaxActiveClusters(&n, fp4_gemm<CG, BN, NV, ST>, &cfg);
     if (err == cudaSuccess && (g_f4_pairs == 0 || n < g_f4_pairs)) g_f4_pairs = n;
     return err;
 }
@@ -386,14 +393,18 @@ cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &out, int 
     const long fit = CG == 2 ? g_f4_pairs : device_sm_count();
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, (int)(tiles < fit ? tiles : fit), F4Layout<CG, BN, NV>::THREADS, F4Layout<CG, BN, NV>::SMEM, st, attr);
-    return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV>, ta, tb, tsa, tsb, ty, o, M, N, K, status);
+    auto launch = [&](auto st_kind) { return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV, decltype(st_kind)::value>, ta, tb, tsa, tsb, ty, o, M, N, K, status); };
+    if constexpr (CG == 1) return launch(std::integral_constant<int, F4_EITHER>{});
+    else return o.tma ? launch(std::integral_constant<int, F4_BY_TMA>{}) : launch(std::integral_constant<int, F4_BY_LANES>{});
 }
 
 }  // namespace
 
 cudaError_t fp4_init() {
-    cudaError_t err = f4_init<2, 192, false>();
-    if (err == cudaSuccess) err = f4_init<2, 192, true>();
+    cudaError_t err = f4_init<2, 192, false, F4_BY_TMA>();
+    if (err == cudaSuccess) err = f4_init<2, 192, true, F4_BY_TMA>();
+    if (err == cudaSuccess) err = f4_init<2, 192, false, F4_BY_LANES>();
+    if (err == cudaSuccess) err = f4_init<2, 192, true, F4_BY_LANES>();
     if (err == cudaSuccess) err = f4_init<1, 128, false>();
     if (err == cudaSuccess) err = f4_init<1, 128, true>();
     if (err == cudaSuccess) err = f4_init<1, 64, false>();

@@ -153,71 +153,99 @@ __device__ __forceinline__ uint32_t f4_pair(float lo, float hi, int type) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// `rows` rows of n bytes from a block as f4_store_block leaves it.  Out of line where
+// the kernel's loops need no registers across the call (single CTAs: 512 x 32001 x 512
+// 21.5 us, inline 24.8; gradients: 64 x 32000 x 511 84.6, 94.7), inline on pairs (16384 x
+// 8190 x 2048 122 us, out of line 157).
+__device__ __forceinline__ void f4_block_out(uint8_t *dst, long ld, uint32_t bits, const uint8_t *blk, bool f32, int n, int rows) {
+    const int lane = threadIdx.x & 31, rb = f32 ? 128 : 64;
+    auto store = [&](auto unit) {
+        using T = decltype(unit);
+        const int lanes = rb / (int)sizeof(T), at = lane % lanes * (int)sizeof(T);
+        if (at >= n) return;
+#pragma unroll 8
+        for (int r = lane / lanes; r < rows; r += 32 / lanes)
+            *reinterpret_cast<T *>(dst + r * ld + at) =
+                *reinterpret_cast<const T *>(blk + r * rb + (f32 ? t2_chunk<128>(r, at >> 4) : t2_chunk<64>(r, at >> 4)) + (at & 15));
+    };
+    if (bits % 8 == 0) store(uint2{});
+    else if (bits % 4 == 0) store(uint32_t{});
+    else store(uint16_t{});
+}
+static __device__ __noinline__ void f4_block_out_call(uint8_t *dst, long ld, uint32_t bits, const uint8_t *blk, bool f32, int n, int rows) {
+    f4_block_out(dst, ld, bits, blk, f32, n, rows);
+}
+
 // 32 columns of a warp's 32 rows (a row per lane) from column col on, from
-// registers: a lane stores its row in whole 32-byte sectors.  What is unaligned or
-// cut off at the matrix's edge is turned in shared memory first (blk: 1 KB).
+// registers: a lane stores its row in whole 32-byte sectors (o.al, all columns in the matrix).
+__device__ __forceinline__ void f4_store_rows(const F4Out &o, const float (&v)[32], int row0, int col, int M) {
+    const int lane = threadIdx.x & 31;
+    const bool f32 = o.type == MNMT_F32;
+    if (row0 + lane >= M) return;
+    uint8_t *dst = static_cast<uint8_t *>(o.y) + ((row0 + lane) * o.ldy + col) * (f32 ? 4 : 2);
+    if (f32) {
+        uint32_t w[32];
+#pragma unroll
+        for (int i = 0; i < 32; i++) w[i] = __float_as_uint(v[i]);
+        if (o.al == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) st32(dst + 32 * i, w + 8 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) reinterpret_cast<uint4 *>(dst)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        }
+    } else {
+        uint32_t w[16];
+        if (o.type == MNMT_BF16) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) w[i] = f4_pair(v[2 * i], v[2 * i + 1], MNMT_BF16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; i++) w[i] = f4_pair(v[2 * i], v[2 * i + 1], MNMT_F16);
+        }
+        if (o.al == 2) {
+            st32(dst, w);
+            st32(dst + 32, w + 8);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) reinterpret_cast<uint4 *>(dst)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        }
+    }
+}
+
+// The same of any alignment and cut off at the matrix's edge, turned in shared memory
+// first (blk: BLK bytes, 32 rows of 16-bit outputs or more), so that lanes next to
+// each other store what is next to each other in a row, 8, 4 or 2 bytes each as the
+// rows are aligned (4052 x 25146 x 115 to fp32 110 us; in pieces of 32 bytes of a
+// row 232).
+template <int BLK, bool INLINE>
 __device__ __forceinline__ void f4_store_block(const F4Out &o, uint8_t *blk, const float (&v)[32], int row0, int col, int M, int N) {
     const int lane = threadIdx.x & 31;
     const bool f32 = o.type == MNMT_F32;
-    if (o.al && col + 32 <= N) {
-        if (row0 + lane >= M) return;
-        uint8_t *dst = static_cast<uint8_t *>(o.y) + ((row0 + lane) * o.ldy + col) * (f32 ? 4 : 2);
-        if (f32) {
-            uint32_t w[32];
-#pragma unroll
-            for (int i = 0; i < 32; i++) w[i] = __float_as_uint(v[i]);
-            if (o.al == 2) {
-#pragma unroll
-                for (int i = 0; i < 4; i++) st32(dst + 32 * i, w + 8 * i);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; i++) reinterpret_cast<uint4 *>(dst)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-            }
-        } else {
-            uint32_t w[16];
-            if (o.type == MNMT_BF16) {
-#pragma unroll
-                for (int i = 0; i < 16; i++) w[i] = f4_pair(v[2 * i], v[2 * i + 1], MNMT_BF16);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; i++) w[i] = f4_pair(v[2 * i], v[2 * i + 1], MNMT_F16);
-            }
-            if (o.al == 2) {
-                st32(dst, w);
-                st32(dst + 32, w + 8);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; i++) reinterpret_cast<uint4 *>(dst)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-            }
-        }
-        return;
-    }
-    // slices of 8 fp32 or 16 16-bit columns, 32 bytes a row; neighbouring lanes store neighbouring columns
-    const int per = f32 ? 8 : 16;
-#pragma unroll
-    for (int h = 0; h < 4; h++) {
-        if (h >= 2 && !f32) break;
+    const int es = f32 ? 4 : 2, rb = 32 * es, pass = BLK / rb < 32 ? BLK / rb : 32;  // bytes of a row; rows at a time
+    const int n = (N - col < 32 ? N - col : 32) * es;                               // bytes to store of each
+    uint8_t *dst = static_cast<uint8_t *>(o.y) + (row0 * o.ldy + col) * es;
+    const long ld = o.ldy * es;
+    const uint32_t bits = (uint32_t)reinterpret_cast<uintptr_t>(o.y) | (uint32_t)ld | (uint32_t)n;
+    for (int r0 = 0; r0 < 32; r0 += pass) {
         __syncwarp();  // the block has been read
-        uint4 *mine = reinterpret_cast<uint4 *>(blk + 32 * lane);
-        if (f32) {
+        if (lane >= r0 && lane < r0 + pass) {
+            if (f32) {
 #pragma unroll
-            for (int i = 0; i < 2; i++)
-                mine[i] = make_uint4(__float_as_uint(v[8 * h + 4 * i]), __float_as_uint(v[8 * h + 4 * i + 1]), __float_as_uint(v[8 * h + 4 * i + 2]),
-                                     __float_as_uint(v[8 * h + 4 * i + 3]));
-        } else if (h < 2) {
+                for (int c = 0; c < 8; c++)
+                    *reinterpret_cast<uint4 *>(blk + (lane - r0) * 128 + t2_chunk<128>(lane - r0, c)) =
+                        make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+            } else {
 #pragma unroll
-            for (int i = 0; i < 2; i++)
-                mine[i] = make_uint4(f4_pair(v[16 * h + 8 * i], v[16 * h + 8 * i + 1], o.type), f4_pair(v[16 * h + 8 * i + 2], v[16 * h + 8 * i + 3], o.type),
-                                     f4_pair(v[16 * h + 8 * i + 4], v[16 * h + 8 * i + 5], o.type), f4_pair(v[16 * h + 8 * i + 6], v[16 * h + 8 * i + 7], o.type));
+                for (int c = 0; c < 4; c++)
+                    *reinterpret_cast<uint4 *>(blk + (lane - r0) * 64 + t2_chunk<64>(lane - r0, c)) =
+                        make_uint4(f4_pair(v[8 * c], v[8 * c + 1], o.type), f4_pair(v[8 * c + 2], v[8 * c + 3], o.type),
+                                   f4_pair(v[8 * c + 4], v[8 * c + 5], o.type), f4_pair(v[8 * c + 6], v[8 * c + 7], o.type));
+            }
         }
         __syncwarp();
-        const int c = lane & (per - 1), n = col + per * h + c;
-        for (int r = lane / per; r < 32; r += 32 / per) {
-            if (row0 + r >= M || n >= N) continue;
-            const long at = (row0 + r) * o.ldy + n;
-            if (f32) static_cast<float *>(o.y)[at] = reinterpret_cast<const float *>(blk + 32 * r)[c];
-            else static_cast<uint16_t *>(o.y)[at] = reinterpret_cast<const uint16_t *>(blk + 32 * r)[c];
-        }
+        if constexpr (INLINE) f4_block_out(dst + r0 * ld, ld, bits, blk, f32, n, min(pass, M - row0 - r0));
+        else f4_block_out_call(dst + r0 * ld, ld, bits, blk, f32, n, min(pass, M - row0 - r0));
     }
 }
 
