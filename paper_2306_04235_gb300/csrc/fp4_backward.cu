@@ -780,8 +780,9 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
             partial += partial_bytes(pl, !input, r.rows, K);
         }
         r.chunk = r.out.type == MNMT_F32 ? BW_CHUNK : 1 << 24;
-        r.out.tma = r.out.al > 0;
-        if (r.out.tma && !encode_out<64>(t + 2, r.out, r.parts > 1 ? r.parts * up32(r.rows) : r.rows, K)) return cudaErrorInvalidValue;
+        const int width = r.parts > 1 ? s.pk : K;
+        r.out.tma = tma_output(r.out, width);
+        if (r.out.tma && !encode_out<64>(t + 2, r.out, r.parts > 1 ? r.parts * up32(r.rows) : r.rows, width)) return cudaErrorInvalidValue;
         if (!encode_bf16(t, a.g, N, M, a.ldg, input ? F4_BM : 64) || !encode_bf16(t + 1, p.m[!input].values, K, input ? N : M, s.pk, 64))
             return cudaErrorInvalidValue;
     }

@@ -109,7 +109,7 @@ __device__ __forceinline__ void f4_copy_scales_on(uint32_t on, uint32_t taddr, u
                      : "memory");
 }
 
-// how a tile is stored: F4_BY_TMA where every row is aligned, else from registers;
+// how a tile is stored, F4_BY_TMA where f4_launch says so, else from registers;
 // pairs know it when they are compiled (for the registers: 16384 x 8192 x 2048
 // 92.5 us, 94.8 with both)
 enum { F4_EITHER, F4_BY_TMA, F4_BY_LANES };
@@ -386,7 +386,7 @@ cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &out, int 
     // fp32 19.3 / 15.0; pairs, 16384 x 8192, K = 256 76 / 52, 2048 101 / 95), but pairs
     // of long K are bound by the MMAs (8192^3 152 / 155, to fp32 164 / 176).
     F4Out o = out;
-    o.tma = o.al && (CG == 1 || K <= 4096);
+    o.tma = tma_output(o, N) && (CG == 1 || K <= 4096);
     ty = ta;
     if (o.tma && !encode_out<F4Layout<CG, BN, NV>::BLK / 32>(&ty, o, M, N)) return cudaErrorInvalidValue;
     const long tiles = (long)((M + CG * F4_BM - 1) / (CG * F4_BM)) * ((N + BN - 1) / BN);

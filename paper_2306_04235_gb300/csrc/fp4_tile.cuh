@@ -294,6 +294,10 @@ inline bool encode(CUtensorMap *tm, CUtensorMapDataType type, const void *p, cuu
                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Whether rows of cols elements can be stored by TMA: it stores 16 bytes at a time, so
+// a row that ends within 16 bytes would take what lies beside it along.
+inline bool tma_output(const F4Out &o, int cols) { return o.al && (long)cols * (o.type == MNMT_F32 ? 4 : 2) % 16 == 0; }
+
 // the map for f4_send_block<RB, ...>
 template <int RB>
 bool encode_out(CUtensorMap *tm, const F4Out &o, int rows, int cols) {
