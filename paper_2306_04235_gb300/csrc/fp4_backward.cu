@@ -451,6 +451,12 @@ __global__ void __launch_bounds__(BW_THREADS, 1)
         for (int phase = 0; phase < 3; phase++) {
             const Range rg = range(phase);
             const BwProduct &p = a.p[phase > 0];
+            if (!p.out.tma) {
+                // f4_store_block writes the staging blocks without asking, and stores by TMA
+                // of the product before may still be reading them
+                if (lane == 0) t2_store_wait_read<0>();
+                __syncwarp();
+            }
             for (long item = rg.first; item < rg.end; item += rg.step) {
                 const At t = at(phase, item);
                 const int row0 = t.m + (int)rank * F4_BM + 32 * q, col0 = t.n + cw;
