@@ -479,7 +479,8 @@ int mnmt_dropout(const void *x, int32_t dtype, int64_t ldx, const void *r, int64
                  void *cuda_stream);
 
 /* Its backward pass for the gradient g [M][d] of out (type otype):
- *   gx = keep and (relu: x > 0) ? fl(g s) : 0   type dtype (x is read only if relu)
+ *   gx = keep and (relu: x > 0) ? fl(g s) : 0   type dtype (x is read only if relu,
+ *                                               and only for gx)
  *   gr = fl(gamma g)                            type otype
  *   *ggamma = sum g r                           fp32, summed in a fixed order
  * Each output may be NULL; ggamma needs r and workspace (MNMT_DROPOUT_WORKSPACE

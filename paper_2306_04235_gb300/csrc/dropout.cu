@@ -203,8 +203,8 @@ cudaError_t launch_dropout_backward(const DropoutArgs &a, cudaStream_t st) {
     by_types(a.dtype, a.otype, [&](auto t, auto o) {
         using T = decltype(t);
         using O = decltype(o);
-        const O *g = static_cast<const O *>(a.g), *r = a.ggamma ? static_cast<const O *>(a.r) : nullptr;
-        const T *x = a.relu ? static_cast<const T *>(a.x) : nullptr;
+        const O *g = static_cast<const O *>(a.g), *r = static_cast<const O *>(a.backward_r());
+        const T *x = static_cast<const T *>(a.backward_x());
         T *gx = static_cast<T *>(a.gx);
         O *gr = static_cast<O *>(a.gr);
         double *partial = a.ggamma ? static_cast<double *>(a.workspace) : nullptr;

@@ -37,6 +37,9 @@ struct DropoutArgs {
     long ldo, ldgx, ldgr;
     float *ggamma;
     void *workspace;
+    // what a backward pass reads beside g: x where ReLU decides about gx, r for the gain (their types are given then only)
+    const void *backward_x() const { return relu && gx ? x : nullptr; }
+    const void *backward_r() const { return ggamma ? r : nullptr; }
 };
 cudaError_t launch_dropout(const DropoutArgs &a, cudaStream_t st);
 cudaError_t launch_dropout_backward(const DropoutArgs &a, cudaStream_t st);
