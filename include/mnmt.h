@@ -423,7 +423,8 @@ size_t mnmt_fp4_scale_bytes(int32_t rows, int32_t cols, int32_t format);
 
 /* Quantises x [q->rows][q->cols] of type dtype in one pass into q's codes and
  * scales (both given, or both NULL) and into `values` (the value of each code,
- * rounded to dtype; may be NULL, may be x).  At least one of the two outputs. */
+ * rounded to dtype; may be NULL, may be x with ldv = ldx).  At least one of the two
+ * outputs. */
 int mnmt_fp4_quantize(const mnmt_fp4 *q, const void *x, int32_t dtype, int64_t ldx, void *values, int64_t ldv,
                       void *cuda_stream);
 
@@ -433,7 +434,7 @@ int mnmt_fp4_dequantize(const mnmt_fp4 *q, void *values, int32_t dtype, int64_t 
 /* Straight-through gradient of the values of mnmt_fp4_quantize: gx = g where
  * |fl(x r)| <= 6 (r as above, found again from x), 0 where the code was held at
  * 6 and in blocks with an infinity or a NaN.  x, g and gx of type dtype; of q only
- * rows, cols, format and tensor_scale are used.  gx may be x or g. */
+ * rows, cols, format and tensor_scale are used.  gx may be x or g, with their stride. */
 int mnmt_fp4_quantize_backward(const mnmt_fp4 *q, const void *x, int32_t dtype, int64_t ldx, const void *g, int64_t ldg,
                                void *gx, int64_t ldgx, void *cuda_stream);
 
@@ -473,7 +474,8 @@ int mnmt_fp4_linear_backward(const mnmt_fp4 *xq, const mnmt_fp4 *wq, const void 
  * t = rne(65536 p) and s = fl(65536 / (65536 - t)); p = 1 drops everything.  p in
  * [0, 1].  No mask is stored: calls with one (seed, offset) draw the same numbers,
  * so a program gives each dropout of each step an offset of its own.  x of type
- * dtype; r and out of type otype.  out may be x (if the types are equal) or r. */
+ * dtype; r and out of type otype.  out may be x (if the types are equal) or r, with the
+ * same stride. */
 int mnmt_dropout(const void *x, int32_t dtype, int64_t ldx, const void *r, int64_t ldr, float gamma, float p, uint64_t seed,
                  uint64_t offset, int32_t relu, int32_t M, int32_t d, void *out, int32_t otype, int64_t ldo,
                  void *cuda_stream);
@@ -484,8 +486,8 @@ int mnmt_dropout(const void *x, int32_t dtype, int64_t ldx, const void *r, int64
  *   gr = fl(gamma g)                            type otype
  *   *ggamma = sum g r                           fp32, summed in a fixed order
  * Each output may be NULL; ggamma needs r and workspace (MNMT_DROPOUT_WORKSPACE
- * bytes of device scratch, 8-byte aligned).  gx may be x or g, gr may be g (gx and gr are
- * then not the same). */
+ * bytes of device scratch, 8-byte aligned).  gx may be x or g, gr may be g, with the same
+ * stride (gx and gr are then not the same). */
 #define MNMT_DROPOUT_WORKSPACE 16384
 int mnmt_dropout_backward(const void *g, int32_t otype, int64_t ldg, const void *x, int32_t dtype, int64_t ldx, const void *r,
                           int64_t ldr, float gamma, float p, uint64_t seed, uint64_t offset, int32_t relu, int32_t M,

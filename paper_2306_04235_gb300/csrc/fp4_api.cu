@@ -38,6 +38,10 @@ bool matrix_ok(const void *p, int32_t dtype, int64_t ld, int32_t cols) {
     return e && p && aligned(p, e) && ld >= cols && ld <= ((int64_t)1 << 40);
 }
 
+// Whether `out` may be written while `in` is read: apart, or in place with one row
+// stride.  With two, a warp would write over rows that others have yet to read.
+bool in_place_ok(const void *out, int64_t ldo, const void *in, int64_t ldi, int32_t rows) { return out != in || !out || ldo == ldi || rows <= 1; }
+
 // one-time set-up of the product kernels, apart from the library's own so that
 // programs that only translate do not load them
 int fp4_ready() {
@@ -108,6 +112,7 @@ extern "C" int mnmt_fp4_quantize(const mnmt_fp4 *q, const void *x, int32_t dtype
     if (!q->codes != !q->scales || (!q->codes && !values)) return fail(MNMT_EINVAL, "fp4_quantize: codes and scales, values or all three");
     if (!matrix_ok(x, dtype, ldx, q->cols) || (values && !matrix_ok(values, dtype, ldv, q->cols)))
         return fail(MNMT_EINVAL, "fp4_quantize: bad pointer or row stride");
+    if (!in_place_ok(values, ldv, x, ldx, q->rows)) return fail(MNMT_EINVAL, "fp4_quantize: in place needs one row stride");
     return done(launch_fp4_quantize(x, dtype, ldx, args_of(q), is_nv(q), values, ldv, static_cast<cudaStream_t>(cuda_stream)), "fp4_quantize");
 }
 
@@ -130,6 +135,8 @@ extern "C" int mnmt_fp4_quantize_backward(const mnmt_fp4 *q, const void *x, int3
     if (q->rows == 0) return MNMT_OK;
     if (!matrix_ok(x, dtype, ldx, q->cols) || !matrix_ok(g, dtype, ldg, q->cols) || !matrix_ok(gx, dtype, ldgx, q->cols))
         return fail(MNMT_EINVAL, "fp4_quantize_backward: bad pointer or row stride");
+    if (!in_place_ok(gx, ldgx, x, ldx, q->rows) || !in_place_ok(gx, ldgx, g, ldg, q->rows))
+        return fail(MNMT_EINVAL, "fp4_quantize_backward: in place needs one row stride");
     const Fp4Args a = args_of(q);
     return done(launch_fp4_quantize_backward(x, dtype, ldx, g, ldg, gx, ldgx, q->rows, q->cols, is_nv(q), a.g, a.inv6g,
                                              static_cast<cudaStream_t>(cuda_stream)),
@@ -211,7 +218,8 @@ extern "C" int mnmt_dropout(const void *x, int32_t dtype, int64_t ldx, const voi
     if (M == 0) return MNMT_OK;
     if (!matrix_ok(x, dtype, ldx, d) || !matrix_ok(out, otype, ldo, d) || (r && !matrix_ok(r, otype, ldr, d)))
         return fail(MNMT_EINVAL, "dropout: bad pointer or row stride");
-    if (out == x && (dtype != otype || ldo != ldx)) return fail(MNMT_EINVAL, "dropout: in place needs one type and stride");
+    if ((out == x && (dtype != otype || ldo != ldx)) || !in_place_ok(out, ldo, r, ldr, M))
+        return fail(MNMT_EINVAL, "dropout: in place needs one type and stride");
     a.x = x, a.ldx = ldx, a.dtype = dtype;
     a.r = r, a.ldr = ldr, a.gamma = gamma;
     a.out = out, a.ldo = ldo, a.otype = otype;
@@ -236,7 +244,9 @@ extern "C" int mnmt_dropout_backward(const void *g, int32_t otype, int64_t ldg, 
     if (ggamma && (!aligned(ggamma, 4) || !workspace || !aligned(workspace, 8)))
         return fail(MNMT_EINVAL, "dropout_backward: ggamma needs an 8-byte aligned workspace");
     if (gx && gx == gr) return fail(MNMT_EINVAL, "dropout_backward: gx and gr are one buffer");
-    if (M > 0 && gx && gx == g && (dtype != otype || ldgx != ldg)) return fail(MNMT_EINVAL, "dropout_backward: in place needs one type and stride");
+    if ((M > 0 && gx && gx == g && (dtype != otype || ldgx != ldg)) || (relu && !in_place_ok(gx, ldgx, x, ldx, M)) ||
+        !in_place_ok(gr, ldgr, g, ldg, M))
+        return fail(MNMT_EINVAL, "dropout_backward: in place needs one type and stride");
     a.g = g, a.ldg = ldg, a.otype = otype;
     a.x = x, a.ldx = ldx, a.dtype = gx ? dtype : MNMT_F32;
     a.r = r, a.ldr = ldr, a.gamma = gamma;
