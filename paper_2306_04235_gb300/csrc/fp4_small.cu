@@ -183,8 +183,13 @@ __global__ void __launch_bounds__(SM_WARPS * 32) fp4_small_kernel(SmallArgs a) {
                         d = __dp4a((int)xw[i], (int)mg[i], d);
                         e = __dp4a((int)xw[i], (int)t[i], e);
                     }
-                    // scaled by one factor after the other: their product may leave fp32 where the sum is zero
-                    acc[m] = __fmaf_rn(__fmul_rn((float)(d - e), sx[m * nb + s * NS + k]), sw[k], acc[m]);
+                    // Scaled by one factor after the other: their product may leave fp32 where the
+                    // sum is zero.  The smaller first: a whole number of at least 2^-129 is exact, and
+                    // infinite only where both scales are so large that the sum is (a NaN stays).
+                    // E4M3 scales reach neither end.
+                    const float f = sx[m * nb + s * NS + k], g = sw[k];
+                    const bool up = !NV && f > g;
+                    acc[m] = __fmaf_rn(__fmul_rn((float)(d - e), up ? g : f), up ? f : g, acc[m]);
                 }
             }
         }
