@@ -135,10 +135,10 @@ __global__ void __launch_bounds__(256) fp4_backward_prepare(PrepArgs a) {
 constexpr int BW_BK = 64;  // reduction indices per stage
 // The tensor core's fp32 accumulator drops bits at every MMA (its relative error
 // grows by about 3e-8 per MMA of 16 terms, always towards zero: 3e-5 measured
-// after 16384 terms).  fp32 results are therefore accumulated there over 1024
-// terms and added up in registers (16384 terms: 5e-7 off); 16-bit results, whose
-// rounding is 2^-9 or 2^-11, are not.
-constexpr int BW_CHUNK = 16;  // stages
+// after 16384 terms).  Results are therefore accumulated there over a number of terms
+// and added up in registers: fp32 over 1024 (16384 terms: 5e-7 off), 16-bit ones, whose
+// rounding is 2^-9 or 2^-12, over 8192 (2^-16).
+constexpr int BW_CHUNK = 16, BW_CHUNK16 = 128;  // stages
 constexpr int BW_TILE = 12;  // what an item takes beside its stages, in stages
 constexpr int BW_EPI_WARPS = 8, BW_GB_WARPS = 2, BW_THREADS = 64 + 32 * (BW_EPI_WARPS + BW_GB_WARPS);
 constexpr int GB_COLS = 256, GB_FLIGHT = 16;  // columns of G that a warp sums at a time, rows that it loads at a time
@@ -788,7 +788,7 @@ cudaError_t launch_fp4_linear_backward(const Fp4BackwardArgs &b, cudaStream_t st
             r.mask = nullptr;
             partial += partial_bytes(pl, !input, r.rows, K);
         }
-        r.chunk = r.out.type == MNMT_F32 ? BW_CHUNK : 1 << 24;
+        r.chunk = r.out.type == MNMT_F32 ? BW_CHUNK : BW_CHUNK16;
         const int width = r.parts > 1 ? s.pk : K;
         r.out.tma = tma_output(r.out, width);
         if (r.out.tma && !encode_out<64>(t + 2, r.out, r.parts > 1 ? r.parts * up32(r.rows) : r.rows, width)) return cudaErrorInvalidValue;

@@ -1,0 +1,47 @@
+"""Sums of many terms of one sign in the 4-bit floating-point operators: what the tensor
+core's truncating accumulator loses must not grow with their length."""
+import pytest
+
+from paper_2306_04235_gb300 import mnmt
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": (mnmt.F32, torch.float32, 2.0 ** -24), "bf16": (mnmt.BF16, torch.bfloat16, 2.0 ** -8), "f16": (mnmt.F16, torch.float16, 2.0 ** -11)}
+
+
+def empty(rows, cols, fmt=mnmt.FP4_MX, g=1.0):
+    return mnmt.Fp4(rows, cols, fmt, g, torch.empty((rows, mnmt.mnmt_fp4_pitch(cols)), dtype=torch.uint8, device="cuda"),
+                    torch.empty(mnmt.mnmt_fp4_scale_bytes(rows, cols, fmt), dtype=torch.uint8, device="cuda"))
+
+
+def values(q):
+    v = torch.empty((q.rows, q.cols), device="cuda")
+    mnmt.mnmt_fp4_dequantize(q, v, mnmt.F32, q.cols)
+    return v
+
+
+@pytest.mark.parametrize("out", ["bf16", "f16"])
+def test_input_gradient_over_many_outputs(out):
+    """gX in 16 bits of a layer so wide that its sums would fill the accumulator: 40 tiles of 256 x 256 on 76 pairs, which
+    are not split.  An MMA of 16 terms loses at most 2^-24 of the sum on average, and at most 512 of them follow each
+    other: a bias of at most 2^-15 of the sum (all terms have one sign), beside the output's rounding."""
+    M, N, K = 2560, 131072, 1024
+    ty, dt, unit = TYPES[out]
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    G = (torch.rand((M, N), generator=gen, device="cuda", dtype=torch.float32) + 0.5).mul_(2.0 ** -8).to(torch.bfloat16)
+    w = torch.rand((N, K), generator=gen, device="cuda") + 0.25
+    wq, xq = empty(N, K), empty(M, K)
+    mnmt.mnmt_fp4_quantize(wq, w, mnmt.F32, K)
+    mnmt.mnmt_fp4_quantize(xq, torch.zeros((M, K), device="cuda"), mnmt.F32, K)
+    ws = torch.empty(mnmt.mnmt_fp4_linear_backward_workspace(M, N, K), dtype=torch.uint8, device="cuda")
+    gx = torch.empty((M, K), dtype=dt, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    mnmt.mnmt_fp4_linear_backward(xq, wq, G, N, None, ty, K, None, mnmt.F32, K, ws, gx, K, status=status)
+    rows = torch.arange(0, M, 10, device="cuda")
+    want = G[rows].double() @ values(wq).double()
+    rel = (gx[rows].double() - want) / want
+    assert int(status.item()) == 0
+    assert float(rel.abs().max()) <= unit + 2.0 ** -15
+    # the roundings of 262144 outputs cancel
+    assert abs(float(rel.mean())) <= 2.0 ** -15
