@@ -8,14 +8,14 @@
 // tiles of 256 codes) and the scales as they are stored: a 512-byte tile of 128
 // rows x 4 blocks goes to four TMEM columns with one tcgen05.cp.
 //
-// Persistent, 2 + BN / 8 warps per CTA:
+// Persistent, 10 to 18 warps per CTA:
 //   warp 0          TMA producer: codes and scales of a k-block of 256 into a ring;
 //   warp 1          copies a k-block's scales to TMEM (copies and MMAs of one issuer
 //                   run in the order of issue; two sets of columns by turns all the
 //                   same, so that no copy touches what the k-block before it reads:
 //                   waiting for those MMAs instead costs 8192^3 192 us), issues its
 //                   four MMAs, frees the slot;
-//   the others      drain a finished accumulator (TMEM holds two), apply alpha,
+//   the others      drain a finished accumulator (TMEM holds two; long sums take several), apply alpha,
 //                   bias and ReLU, round, and store by TMA or from registers.
 // CG = 2: a pair of CTAs computes 256 x 192 tiles, each CTA half of the rows of
 // both operands; CG = 1: 128 x 128 or 128 x 64 tiles for smaller grids.
@@ -38,6 +38,12 @@ namespace mnmt {
 namespace {
 
 constexpr int F4_BK = 256;  // codes per k-block: 128 bytes
+// The tensor core's fp32 accumulator truncates at every MMA of 64 terms (NV, terms of one
+// sign: 6e-8 of the sum lost after 4096 terms, 5.5e-7 after 8192, 2.5e-6 after 16384,
+// 8.6e-5 after 262144).  fp32 results therefore leave it every 8192 terms and are added
+// up in registers, 16-bit ones, whose rounding is 2^-9 or 2^-12, every 65536 (2e-5).
+// (Every 4096 took 8192^3 to fp32 from 173 us to 182, 2100 x 8192 x 8192 from 59 to 65.)
+constexpr int F4_CHUNK = 32, F4_CHUNK16 = 256;  // k-blocks
 
 template <int CG, int BN, bool NV>
 struct F4Layout {
@@ -114,10 +120,12 @@ __device__ __forceinline__ void f4_copy_scales_on(uint32_t on, uint32_t taddr, u
 // 92.5 us, 94.8 with both)
 enum { F4_EITHER, F4_BY_TMA, F4_BY_LANES };
 
-template <int CG, int BN, bool NV, int ST>
+// LONG: a sum takes several accumulators, chunk k-blocks each (compiled apart: pairs have
+// no registers left for it)
+template <int CG, int BN, bool NV, int ST, bool LONG>
 __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
     fp4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmSA,
-             const __grid_constant__ CUtensorMap tmSB, const __grid_constant__ CUtensorMap tmY, F4Out o, int M, int N, int K, int *status) {
+             const __grid_constant__ CUtensorMap tmSB, const __grid_constant__ CUtensorMap tmY, F4Out o, int M, int N, int K, int chunk, int *status) {
     using L = F4Layout<CG, BN, NV>;
     constexpr int STAGES = L::STAGES, T = L::T, R = L::R;
 
@@ -214,47 +222,52 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
         // the compiler cannot see to be uniform, or a test per MMA for the last k-block,
         // cost more than the MMA: 8192^3 191 -> 157 us.)
         const uint32_t base = __shfl_sync(0xFFFFFFFFu, tbase, 0), sfa = base + L::COL_SFA, cfb = base + L::COL_SFB;
-        for (F4Walk w(mt, nt, unit, units); w.more() && !failed; w.next(), lt++) {
-            const uint32_t buf = lt & 1, d = base + buf * BN;
+        for (F4Walk w(mt, nt, unit, units); w.more() && !failed; w.next()) {
             // scale columns of the tile's first row of W: every other tile of 64 or 192 columns
             // starts in the middle of a row tile, two columns on
             const uint32_t sfb = __shfl_sync(0xFFFFFFFFu, cfb + ((uint32_t)(w.n() * BN & 127) >> 5), 0);
-            if (lt >= 2 && !f4_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
-                failed = true;
-                break;
-            }
-            tc_fence_after();
-            for (int kb = 0; kb < nkb; kb++) {
-                if (!f4_wait(full_bar(s), phase)) {
+            int k0 = 0;
+            do {
+                const uint32_t buf = lt & 1, d = base + buf * BN;
+                const int k1 = LONG ? min(nkb, k0 + chunk) : nkb;
+                if (lt >= 2 && !f4_wait(acce_bar(buf), (lt / 2 - 1) & 1)) {
                     failed = true;
                     break;
                 }
                 tc_fence_after();
-                const uint64_t off = (uint64_t)((s * L::STAGE) >> 4);
-                const uint32_t set = (seen & 1) * L::SF;
+                for (int kb = k0; kb < k1; kb++) {
+                    if (!f4_wait(full_bar(s), phase)) {
+                        failed = true;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint64_t off = (uint64_t)((s * L::STAGE) >> 4);
+                    const uint32_t set = (seen & 1) * L::SF;
 #pragma unroll
-                for (int t = 0; t < T; t++) {
-                    f4_copy_scales_on<CG>(on, sfa + set + 4 * t, sa_desc + off + (uint64_t)(t * 32));
+                    for (int t = 0; t < T; t++) {
+                        f4_copy_scales_on<CG>(on, sfa + set + 4 * t, sa_desc + off + (uint64_t)(t * 32));
 #pragma unroll
-                    for (int r = 0; r < R; r++) f4_copy_scales_on<CG>(on, cfb + set + 4 * (R * t + r), sb_desc + off + (uint64_t)((r * T + t) * 32));
+                        for (int r = 0; r < R; r++) f4_copy_scales_on<CG>(on, cfb + set + 4 * (R * t + r), sb_desc + off + (uint64_t)((r * T + t) * 32));
+                    }
+                    auto mma = [&](int k) {
+                        const int t = NV ? k : k >> 1, id = NV ? 0 : 2 * (k & 1);
+                        f4_mma_on<CG, NV>(on, d, a_desc + off + (uint64_t)(2 * k), b_desc + off + (uint64_t)(2 * k), f4_idesc(CG * F4_BM, BN, NV, id),
+                                          sfa + set + 4 * t, sfb + set + 4 * R * t, (uint32_t)((kb - k0) | k));
+                    };
+                    if (kb < full) {
+                        mma(0), mma(1), mma(2), mma(3);
+                    } else {
+                        mma(0);
+                        if (steps - 4 * kb > 1) mma(1);
+                        if (steps - 4 * kb > 2) mma(2);
+                    }
+                    f4_commit_on<CG>(on, empty_bar(s));
+                    seen++;
+                    if (++s == STAGES) s = 0, phase ^= 1;
                 }
-                auto mma = [&](int k) {
-                    const int t = NV ? k : k >> 1, id = NV ? 0 : 2 * (k & 1);
-                    f4_mma_on<CG, NV>(on, d, a_desc + off + (uint64_t)(2 * k), b_desc + off + (uint64_t)(2 * k), f4_idesc(CG * F4_BM, BN, NV, id),
-                                      sfa + set + 4 * t, sfb + set + 4 * R * t, (uint32_t)(kb | k));
-                };
-                if (kb < full) {
-                    mma(0), mma(1), mma(2), mma(3);
-                } else {
-                    mma(0);
-                    if (steps - 4 * kb > 1) mma(1);
-                    if (steps - 4 * kb > 2) mma(2);
-                }
-                f4_commit_on<CG>(on, empty_bar(s));
-                seen++;
-                if (++s == STAGES) s = 0, phase ^= 1;
-            }
-            if (!failed) f4_commit_on<CG>(on, accf_bar(buf));
+                if (!failed) f4_commit_on<CG>(on, accf_bar(buf));
+                k0 = k1, lt++;
+            } while (LONG && k0 < nkb && !failed);
         }
         if (failed) {
             *abort_flag = 1;
@@ -283,29 +296,48 @@ __global__ void __launch_bounds__((F4Layout<CG, BN, NV>::THREADS), 1)
             }
         };
         fetch_bias();
-        for (; w.more(); lt++) {
-            const int buf = (int)(lt & 1);
+        while (w.more()) {
             const int row0 = w.m() * CG * F4_BM + (int)rank * F4_BM + 32 * q, col0 = w.n() * BN + cw;
             __syncwarp();
 #pragma unroll
             for (int b = 0; b < NB; b++) bias[32 * b + lane] = next[b];
             w.next();
             fetch_bias();
-            bool ok = *abort_flag == 0 && f4_wait(accf_bar(buf), (lt >> 1) & 1);
-            if (!ok && *abort_flag == 0) {
-                *abort_flag = 1;
-                set_status(status, MNMT_ETIMEOUT);
-            }
-            tc_fence_after();
-            ok = __all_sync(0xFFFFFFFFu, ok && *abort_flag == 0);
-            const uint32_t taddr = tbase + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * BN + cw);
+            bool ok;
             uint32_t r[NB][32];
+            int k0 = 0;
+            do {
+                const int buf = (int)(lt & 1);
+                ok = *abort_flag == 0 && f4_wait(accf_bar(buf), (lt >> 1) & 1);
+                if (!ok && *abort_flag == 0) {
+                    *abort_flag = 1;
+                    set_status(status, MNMT_ETIMEOUT);
+                }
+                tc_fence_after();
+                ok = __all_sync(0xFFFFFFFFu, ok && *abort_flag == 0);
+                const uint32_t taddr = tbase + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * BN + cw);
+                if (!LONG || k0 == 0) {
 #pragma unroll
-            for (int b = 0; b < NB; b++) tmem_ld32(taddr + 32 * b, r[b]);
-            tmem_wait_ld();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) f4_release<CG>(acce_bar(buf));  // this warp is done with the accumulator buffer
+                    for (int b = 0; b < NB; b++) tmem_ld32(taddr + 32 * b, r[b]);
+                    tmem_wait_ld();
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 2 * NB; b++) {
+                        uint32_t more[16];
+                        tmem_ld16(taddr + 16 * b, more);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; i++) {
+                            uint32_t &sum = r[b >> 1][16 * (b & 1) + i];
+                            sum = __float_as_uint(__fadd_rn(__uint_as_float(sum), __uint_as_float(more[i])));
+                        }
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) f4_release<CG>(acce_bar(buf));  // this warp is done with the accumulator buffer
+                k0 += chunk, lt++;
+            } while (LONG && k0 < nkb);
             if (!ok || row0 >= M) continue;
 #pragma unroll
             for (int b = 0; b < NB; b++) {
@@ -363,14 +395,14 @@ bool encode_scales(CUtensorMap *tm, const Fp4Args &q, bool nv) {
     return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT32, q.scales, 128, n, 512, 128, nv ? 4 : 2, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-template <int CG, int BN, bool NV, int ST = F4_EITHER>
+template <int CG, int BN, bool NV, int ST = F4_EITHER, bool LONG = false>
 cudaError_t f4_init() {
-    cudaError_t err = cudaFuncSetAttribute(fp4_gemm<CG, BN, NV, ST>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F4Layout<CG, BN, NV>::SMEM);
+    cudaError_t err = cudaFuncSetAttribute(fp4_gemm<CG, BN, NV, ST, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F4Layout<CG, BN, NV>::SMEM);
     if (err != cudaSuccess || CG == 1) return err;
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, 64, F4Layout<CG, BN, NV>::THREADS, F4Layout<CG, BN, NV>::SMEM, nullptr, attr);
     int n = 0;
-    err = cudaOccupancyMaxActiveClusters(&n, fp4_gemm<CG, BN, NV, ST>, &cfg);
+    err = cudaOccupancyMaxActiveClusters(&n, fp4_gemm<CG, BN, NV, ST, LONG>, &cfg);
     if (err == cudaSuccess && (g_f4_pairs == 0 || n < g_f4_pairs)) g_f4_pairs = n;
     return err;
 }
@@ -393,23 +425,34 @@ cudaError_t f4_launch(const Fp4Args &x, const Fp4Args &w, const F4Out &out, int 
     const long fit = CG == 2 ? g_f4_pairs : device_sm_count();
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = f4_config(CG, (int)(tiles < fit ? tiles : fit), F4Layout<CG, BN, NV>::THREADS, F4Layout<CG, BN, NV>::SMEM, st, attr);
-    auto launch = [&](auto st_kind) { return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV, decltype(st_kind)::value>, ta, tb, tsa, tsb, ty, o, M, N, K, status); };
-    if constexpr (CG == 1) return launch(std::integral_constant<int, F4_EITHER>{});
-    else return o.tma ? launch(std::integral_constant<int, F4_BY_TMA>{}) : launch(std::integral_constant<int, F4_BY_LANES>{});
+    const int chunk = o.type == MNMT_F32 ? F4_CHUNK : F4_CHUNK16;
+    const bool more = K > chunk * F4_BK;
+    auto launch = [&](auto st_kind, auto is_long) {
+        return cudaLaunchKernelEx(&cfg, fp4_gemm<CG, BN, NV, decltype(st_kind)::value, decltype(is_long)::value>, ta, tb, tsa, tsb, ty, o, M, N, K, chunk, status);
+    };
+    using Either = std::integral_constant<int, F4_EITHER>;
+    using Lanes = std::integral_constant<int, F4_BY_LANES>;
+    if constexpr (CG == 1) return more ? launch(Either{}, std::true_type{}) : launch(Either{}, std::false_type{});
+    else if (o.tma) return launch(std::integral_constant<int, F4_BY_TMA>{}, std::false_type{});  // K <= 4096
+    else return more ? launch(Lanes{}, std::true_type{}) : launch(Lanes{}, std::false_type{});
 }
 
 }  // namespace
 
-cudaError_t fp4_init() {
-    cudaError_t err = f4_init<2, 192, false, F4_BY_TMA>();
-    if (err == cudaSuccess) err = f4_init<2, 192, true, F4_BY_TMA>();
-    if (err == cudaSuccess) err = f4_init<2, 192, false, F4_BY_LANES>();
-    if (err == cudaSuccess) err = f4_init<2, 192, true, F4_BY_LANES>();
-    if (err == cudaSuccess) err = f4_init<1, 128, false>();
-    if (err == cudaSuccess) err = f4_init<1, 128, true>();
-    if (err == cudaSuccess) err = f4_init<1, 64, false>();
-    if (err == cudaSuccess) err = f4_init<1, 64, true>();
+template <bool NV>
+static cudaError_t init_all() {
+    cudaError_t err = f4_init<2, 192, NV, F4_BY_TMA>();
+    if (err == cudaSuccess) err = f4_init<2, 192, NV, F4_BY_LANES>();
+    if (err == cudaSuccess) err = f4_init<2, 192, NV, F4_BY_LANES, true>();
+    if (err == cudaSuccess) err = f4_init<1, 128, NV>();
+    if (err == cudaSuccess) err = f4_init<1, 128, NV, F4_EITHER, true>();
+    if (err == cudaSuccess) err = f4_init<1, 64, NV>();
+    if (err == cudaSuccess) err = f4_init<1, 64, NV, F4_EITHER, true>();
     return err;
+}
+cudaError_t fp4_init() {
+    const cudaError_t err = init_all<false>();
+    return err == cudaSuccess ? init_all<true>() : err;
 }
 
 cudaError_t launch_fp4_product(const Fp4Args &x, const Fp4Args &w, bool nv, float alpha, const float *bias, int relu, void *y, int ydtype,

@@ -45,3 +45,39 @@ def test_input_gradient_over_many_outputs(out):
     assert float(rel.abs().max()) <= unit + 2.0 ** -15
     # the roundings of 262144 outputs cancel
     assert abs(float(rel.mean())) <= 2.0 ** -15
+
+
+@pytest.mark.parametrize("fmt,g", [(mnmt.FP4_MX, 1.0), (mnmt.FP4_NV, 2.0 ** -9)])
+@pytest.mark.parametrize("M,N,K", [(16, 128, 262144), (128, 19200, 65536), (300, 20000, 65536), (17, 40, 4160)])
+@pytest.mark.parametrize("out", ["f32", "f16"])
+def test_linear_of_long_rows(M, N, K, out, fmt, g):
+    """Each kind of tile (128 x 64, 128 x 128, pairs).  At most 128 MMAs of 64 terms follow each other in the accumulator
+    for fp32 outputs and 1024 for 16-bit ones, each losing 2^-25 of the sum on average (half a last bit), at most 2^-24;
+    the few sums taken out are added in fp32: a bias of 2^-18 or 2^-14 of the sum, beside the output's rounding.  Every third block or so of
+    W has one large element, so that block scales (and with them the bits of the terms) differ."""
+    ty, dt, unit = TYPES[out]
+    lost = 2.0 ** -18 if out == "f32" else 2.0 ** -14
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    x = torch.rand((M, K), generator=gen, device="cuda") + 0.25
+    w = torch.rand((N, K), generator=gen, device="cuda").mul_(0.5).add_(0.1)
+    w[:, ::96] *= 7
+    xq, wq = empty(M, K, fmt, g), empty(N, K, fmt, g)
+    mnmt.mnmt_fp4_quantize(xq, x, mnmt.F32, K)
+    mnmt.mnmt_fp4_quantize(wq, w, mnmt.F32, K)
+    del x, w
+    scale = 2.0 ** -6 if out == "f16" else 1.0  # of x, by way of its scales: sums within fp16's range
+    if out == "f16":
+        if fmt == mnmt.FP4_NV:
+            xq.tensor_scale = g * scale
+        else:
+            s = xq.buffers[1]
+            s.copy_(torch.where(s > 0, s.int() - 6, 0).to(torch.uint8))
+    y = torch.empty((M, N), dtype=dt, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    mnmt.mnmt_fp4_linear(xq, wq, None, 0, 0, None, False, y, ty, N, status)
+    cols = torch.arange(0, N, max(1, N // 500), device="cuda")
+    want = values(xq).double() @ values(wq)[cols].double().t()
+    rel = (y[:, cols].double() - want) / want
+    assert int(status.item()) == 0 and float(want.min()) > 0
+    assert float(rel.abs().max()) <= unit + 2 * lost
+    assert abs(float(rel.mean())) <= lost + unit / rel.numel() ** 0.5
