@@ -62,6 +62,10 @@ MNMT_DEV uint32_t keep_lane(const Philox &ph, const RowAt &a, uint32_t thr) {
     return k;
 }
 
+// Steps of eight products that a lane's part of ggamma stays in fp32: a chain of 512
+// additions whatever the matrix, and one in 64 bits for it.
+constexpr int GAMMA_STEPS = 64;
+
 // T: type of x and gx; O: type of out, r, g and gr
 template <typename T, typename O, bool VEC>
 __global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_kernel(const T *x, long ldx, int alx, const O *r, long ldr, int alr, float gamma, uint32_t thr,
@@ -102,7 +106,10 @@ __global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_backward_kernel(const
     pdl_grid_wait();
     MNMT_ROW_BUF(buf, VEC);
     constexpr int E = 8;  // whatever the alignment, so that ggamma's sum has one order
-    float sum = 0.0f;
+    __shared__ double totals[256];  // a lane's sum but for the last steps (in shared memory for the registers)
+    if (partial) totals[threadIdx.x] = 0.0;
+    float sum = 0.0f;  // of at most GAMMA_STEPS steps
+    int steps = GAMMA_STEPS;
     for (Walk<E> w(M, d, lr); w.more(); w.next()) {
         const RowAt a = w.at();
         const bool ok = a.row < M;
@@ -118,6 +125,7 @@ __global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_backward_kernel(const
             settle<O, VEC>(rr, w, alr, buf, v);
 #pragma unroll
             for (int k = 0; k < E; k++) sum = __fmaf_rn(u[k], v[k], sum);
+            if (--steps == 0) totals[threadIdx.x] += sum, sum = 0.0f, steps = GAMMA_STEPS;
         }
         if (gr) {
 #pragma unroll
@@ -138,7 +146,7 @@ __global__ void __launch_bounds__(256, ROW_BLOCKS) dropout_backward_kernel(const
     if (partial) {
         // the block's sum, always in the same order
         __shared__ double red[8];
-        double s = sum;
+        double s = totals[threadIdx.x] + sum;
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
         if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
         __syncthreads();
