@@ -142,6 +142,7 @@ constexpr int BW_CHUNK = 16, BW_CHUNK16 = 128;  // stages
 constexpr int BW_TILE = 12;  // what an item takes beside its stages, in stages
 constexpr int BW_EPI_WARPS = 8, BW_GB_WARPS = 2, BW_THREADS = 64 + 32 * (BW_EPI_WARPS + BW_GB_WARPS);
 constexpr int GB_COLS = 256, GB_FLIGHT = 16;  // columns of G that a warp sums at a time, rows that it loads at a time
+constexpr int GB_JOIN = 512;  // blocks' sums added in fp32, above that in 64 bits (for all: 1 us of every call)
 
 template <int CG, int BN>
 struct BwLayout {
@@ -197,7 +198,8 @@ __host__ __device__ constexpr uint32_t bw_idesc(int m, int n, bool a_mn) {
 
 // The bias gradient by warps w of n: gb_rows x 256 columns at a time, eight columns
 // per lane; the warp that finishes the last row block of 256 columns adds the
-// blocks' sums in their order.
+// blocks' sums in their order.  A term passes through at most 512 + 512 additions in
+// fp32, whatever M is.
 __device__ __noinline__ void bias_gradient(const BwArgs &a, int w, int n) {
     const int lane = threadIdx.x & 31;
     const int strips = fp4_div_up(a.N, GB_COLS), blocks = fp4_div_up(a.M, a.gb_rows);
@@ -248,14 +250,24 @@ __device__ __noinline__ void bias_gradient(const BwArgs &a, int w, int n) {
             if (__shfl_sync(0xFFFFFFFFu, old, 0) != blocks - 1) continue;
             __threadfence();
             const float4 *in = reinterpret_cast<const float4 *>(a.gb_part + c);
-            float4 lo = make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi = lo;
+            double sum[8] = {};
+            for (int b0 = 0; b0 < blocks; b0 += GB_JOIN) {
+                const int b1 = min(blocks, b0 + GB_JOIN);
+                float4 lo = make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi = lo;
 #pragma unroll 8
-            for (int b = 0; b < blocks; b++) {
-                const float4 x = __ldcg(in + (size_t)b * strips * (GB_COLS / 4)), y = __ldcg(in + (size_t)b * strips * (GB_COLS / 4) + 1);
-                lo.x = __fadd_rn(lo.x, x.x), lo.y = __fadd_rn(lo.y, x.y), lo.z = __fadd_rn(lo.z, x.z), lo.w = __fadd_rn(lo.w, x.w);
-                hi.x = __fadd_rn(hi.x, y.x), hi.y = __fadd_rn(hi.y, y.y), hi.z = __fadd_rn(hi.z, y.z), hi.w = __fadd_rn(hi.w, y.w);
+                for (int b = b0; b < b1; b++) {
+                    const float4 x = __ldcg(in + (size_t)b * strips * (GB_COLS / 4)), y = __ldcg(in + (size_t)b * strips * (GB_COLS / 4) + 1);
+                    lo.x = __fadd_rn(lo.x, x.x), lo.y = __fadd_rn(lo.y, x.y), lo.z = __fadd_rn(lo.z, x.z), lo.w = __fadd_rn(lo.w, x.w);
+                    hi.x = __fadd_rn(hi.x, y.x), hi.y = __fadd_rn(hi.y, y.y), hi.z = __fadd_rn(hi.z, y.z), hi.w = __fadd_rn(hi.w, y.w);
+                }
+                s[0] = lo.x, s[1] = lo.y, s[2] = lo.z, s[3] = lo.w, s[4] = hi.x, s[5] = hi.y, s[6] = hi.z, s[7] = hi.w;
+                if (blocks <= GB_JOIN) break;
+#pragma unroll
+                for (int k = 0; k < 8; k++) sum[k] += s[k];
             }
-            s[0] = lo.x, s[1] = lo.y, s[2] = lo.z, s[3] = lo.w, s[4] = hi.x, s[5] = hi.y, s[6] = hi.z, s[7] = hi.w;
+            if (blocks > GB_JOIN)
+#pragma unroll
+                for (int k = 0; k < 8; k++) s[k] = (float)sum[k];
         }
 #pragma unroll
         for (int k = 0; k < 8; k++)

@@ -81,3 +81,25 @@ def test_linear_of_long_rows(M, N, K, out, fmt, g):
     assert int(status.item()) == 0 and float(want.min()) > 0
     assert float(rel.abs().max()) <= unit + 2 * lost
     assert abs(float(rel.mean())) <= lost + unit / rel.numel() ** 0.5
+
+
+@pytest.mark.parametrize("products", [True, False])
+@pytest.mark.parametrize("M,N", [(1 << 22, 8), ((1 << 22) - 511, 7)])
+def test_bias_gradient_of_many_rows(M, N, products):
+    """Columns of ones with 1 + 7/128 in every 512th row: sums of 512 rows are exact, and a chain of thousands of them
+    rounds each the same way.  At most 512 + 512 additions in fp32, 64 bits above, one rounding: 2^-24 (1024 + 2)."""
+    K = 8
+    G = torch.ones((M, N), dtype=torch.bfloat16, device="cuda")
+    G[::512] = 1 + 7 / 128
+    xq, wq = empty(M, K), empty(N, K)
+    mnmt.mnmt_fp4_quantize(xq, torch.ones((M, K), dtype=torch.bfloat16, device="cuda"), mnmt.BF16, K)
+    mnmt.mnmt_fp4_quantize(wq, torch.ones((N, K), device="cuda"), mnmt.F32, K)
+    ws = torch.empty(mnmt.mnmt_fp4_linear_backward_workspace(M, N, K), dtype=torch.uint8, device="cuda")
+    gx = torch.empty((M, K), dtype=torch.bfloat16, device="cuda") if products else None
+    gw = torch.empty((N, K), device="cuda") if products else None
+    gb = torch.empty(N, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    mnmt.mnmt_fp4_linear_backward(xq, wq, G, N, None, mnmt.BF16, K, None, mnmt.F32, K, ws, gx, K, gw, K, gb, status)
+    want = G.double().sum(0)
+    assert int(status.item()) == 0
+    assert ((gb.double() - want).abs() <= 2.0 ** -24 * 1026 * want).all()
