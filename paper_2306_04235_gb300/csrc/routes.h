@@ -149,13 +149,22 @@ inline bool route_rows_variant(int nb, int hpc, int beam, int clusters, int fit)
 
 // Does a product of 4-bit floating-point matrices run on the kernel for a few rows
 // (one launch with the quantisation) or as quantisation and tensor-core product?
-// x must fit its shared memory; then by time, us a call, few rows / two launches:
-//   2048 x 512: 8 rows 4.7 / 5.9;  32000 x 512: 1 row 6.8 / 7.9, 4 rows 11.2 / 7.9
-//   8192 x 2048: 1 row 6.9 / 8.8, 4 rows 11.9 / 8.8;  2048 x 8192: 1 row 8.0 / 12.0, 4 rows 15.1 / 12.0
+// x must fit its shared memory; then by time, us a call back to back with x to be
+// quantised, few rows / two launches (MX):
+//   2048 x 512: 1 row 2.8 / 5.5, 8 rows 4.7 / 5.8;  32000 x 512: 1 row 6.6 / 7.7, 4 rows 11.2 / 7.9
+//   8192 x 2048: 1 row 6.8 / 9.4, 4 rows 11.9 / 8.8;  2048 x 8192: 1 row 7.9 / 13.8, 4 rows 15.1 / 12.0
+// Every block quantises all of x, which costs more rows of long K more than it saves:
+//   512 x 2048: 8 rows 7.2 / 6.8;  512 x 4096: 8 rows 11.6 / 8.6;  512 x 8192: 4 rows 12.6 / 12.1
+//   512 x 16384: 2 rows 16.0 / 19.1
+// One row is up to 8 % slower than two launches at the largest sizes measured (8192 x 32768
+// 70 / 65, 128000 x 4096 105 / 103), faster at the others (32000 x 8192 54 / 61, 64 x 32768 22 / 33).
+// With x packed already the other form is one launch too, and often the faster one (8 x 512 x
+// 512 3.9 / 3.0); the route is the same all the same, so that a packed operand gives
+// the bits of the call that packs it.
 constexpr long FP4_SMALL_X = 32768;  // elements of x, rows padded to 32
 inline bool route_fp4_small(int M, int N, int K) {
     if (M > 8 || (long)M * ((K + 31L) / 32 * 32) > FP4_SMALL_X) return false;
-    return M == 1 || (double)M * N * K <= 2.5e7;
+    return M == 1 || ((double)M * N * K <= 2.5e7 && (M == 2 || (long)M * K <= 12288));
 }
 
 // Output tiles of the product of 4-bit floating-point matrices: 256 x 192 on CTA
