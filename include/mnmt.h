@@ -440,7 +440,9 @@ int mnmt_fp4_quantize_backward(const mnmt_fp4 *q, const void *x, int32_t dtype, 
 
 /* Linear on 4-bit floating-point operands:
  *   y[m][n] = act(alpha sum_k X[m][k] W[n][k] + bias[n])
- * with X, W the codes times their block scales (products exact, sums in fp32),
+ * with X, W the codes times their block scales (products exact, sums in fp32; the tensor
+ * cores' truncate, for at most 8192 terms before they are added up, 65536 where the output
+ * has 16 bits: up to 6e-7 and 2e-5 of a sum of one sign),
  * alpha = fl(g_x g_w) for NV and 1 for MX, bias [N] fp32 or NULL, act = ReLU if
  * relu != 0, y rounded once to ydtype.  X is quantised from x (type xdtype) into
  * xq's buffers, which hold it afterwards (for the backward pass); with x = NULL
@@ -455,11 +457,13 @@ int mnmt_fp4_linear(const mnmt_fp4 *xq, const mnmt_fp4 *w, const void *x, int32_
  *   gw[n][k] = in_w alpha_x sum_m G[m][n] X[m][k]      fp32
  *   gb[n]    = sum_m G[m][n]                           fp32
  * (alpha_w, alpha_x: the tensor scales for NV, else 1; products exact, sums in
- * fp32 in a fixed order).  in_x, in_w: the straight-through masks, |fl(x r)| <= 6,
+ * fp32 in a fixed order, the tensor cores' for at most 1024 terms before they are added up,
+ * 8192 where gx has 16 bits).  in_x, in_w: the straight-through masks, |fl(x r)| <= 6,
  * from the float originals x [M][K] and w [N][K] (types xdtype and wdtype) and the
  * scales of xq and wq; a NULL original means no mask.  gx, gw and gb may each be
  * NULL.  workspace: mnmt_fp4_linear_backward_workspace(M, N, K) bytes of device
- * scratch, 16-byte aligned. */
+ * scratch, 16-byte aligned.  *status as in mnmt_fp4_linear; after MNMT_ETIMEOUT the
+ * gradients are not valid. */
 size_t mnmt_fp4_linear_backward_workspace(int32_t M, int32_t N, int32_t K);
 int mnmt_fp4_linear_backward(const mnmt_fp4 *xq, const mnmt_fp4 *wq, const void *G, int64_t ldg, const void *x,
                              int32_t xdtype, int64_t ldx, const void *w, int32_t wdtype, int64_t ldw, void *workspace,

@@ -10,9 +10,9 @@
 // 16 bits, not 32, because ten rounds per four elements would take as long as
 // the elements' bytes; the keep probability is then a multiple of 2^-16.
 // Bound by memory where elements are wide (16384 x 2048 bf16 onto an fp32 residual
-// 55 us, 6.1 TB/s), by the generator's and the moves' instructions where they are
-// narrow or start anywhere (16384 x 2048 bf16 to bf16 33 us, 4.0 TB/s; backward of
-// 5003 x 1001 fp16 with all gradients 20 us, 3.9 TB/s).
+// 55 us, 6.1 TB/s), by latency where they are narrow (one step of a warp in flight:
+// 16384 x 2048 bf16 to bf16 30 to 33 us, 4.0 to 4.5 TB/s, issue 56 %; backward with ReLU 47)
+// or start anywhere (backward of 5003 x 1001 fp16 with all gradients 20 us, 3.9 TB/s).
 #include <type_traits>
 
 #include "fp4.cuh"

@@ -7,8 +7,8 @@
 //   q = E2M1(fl(x r)), value fl(q S), gradient |fl(x r)| <= 6 ? g : 0.
 // All three are one pass over the data, bound by its bytes; a lane takes E = 16 or
 // 8 elements of a row (row_pass.cuh), so a block is one, two or four neighbouring
-// lanes.  16384 x 2048 bf16, codes and values: 27 us, 5.6 TB/s; the gradient of
-// 8000 x 509 fp32 10 us, 4.8 TB/s.
+// lanes.  16384 x 2048 bf16, codes and values: 27 us, 5.6 TB/s (codes alone 18, rows of
+// 2047 69); the gradient of 8000 x 509 fp32 10 us, 4.8 TB/s.
 #include <type_traits>
 
 #include "fp4.cuh"

@@ -16,10 +16,11 @@
 // epilogue warps apply masks and store (masks from the float
 // originals there, a row per lane, waited for memory: gX of 16384 x 512 x 2048 130
 // us, 65 with bits); two warps sum the bias gradient meanwhile.  16384 x 8192 x 2048:
-// 594 us, 1.85 PFLOP/s; with preparation 635, against 565 at the measured rate of bf16.
+// 594 us, 1.85 PFLOP/s; with preparation 635, in a row 650 to 700 under the power cap,
+// against 565 at the measured rate of bf16 (645 at the sustained one).
 // fp4_backward_finish: where the reduction of a product was split (few tiles, long
 // sums), adds the parts' sums in their order and applies masks (memory; 512 x 2048 x
-// 2048 27 us in all, 46 x 1024 x 256 9.3: three and two short launches).
+// 2048 27 to 30 us in all, 46 x 1024 x 256 9.3 to 9.8: three and two short launches).
 #include <type_traits>
 
 #include "fp4.cuh"

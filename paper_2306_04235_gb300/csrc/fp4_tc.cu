@@ -15,13 +15,15 @@
 //                   same, so that no copy touches what the k-block before it reads:
 //                   waiting for those MMAs instead costs 8192^3 192 us), issues its
 //                   four MMAs, frees the slot;
-//   the others      drain a finished accumulator (TMEM holds two; long sums take several), apply alpha,
-//                   bias and ReLU, round, and store by TMA or from registers.
+//   the others      drain a finished accumulator (TMEM holds two; long sums take
+//                   several), apply alpha, bias and ReLU, round, and store by TMA or
+//                   from registers.
 // CG = 2: a pair of CTAs computes 256 x 192 tiles, each CTA half of the rows of
 // both operands; CG = 1: 128 x 128 or 128 x 64 tiles for smaller grids.
-// Measured: 8192^3 MX 160 us (6.9 PFLOP/s), 16384 x 8192 x 2048 to bf16 MX 99 us (5.5),
-// NV 111; bound by shared memory, which the MMAs read their operands from and the
-// epilogue stages its tiles in, and for small grids by their start.
+// Measured to bf16, back to back: 8192^3 MX 152 us (7.2 PFLOP/s), NV 173; 16384 x 8192 x
+// 2048 MX 93 us (5.9), NV 104 (after a flush of L2 160, 177, 98, 110).  With K of 2048 a
+// tile's drain stands against eight k-blocks only (tensor pipe active 59 %); small grids
+// are bound by their start.
 // Every wait is bounded; one that runs out records MNMT_ETIMEOUT in *status, and
 // the CTA stops issuing work, waits (bounded) for what it has in flight, frees
 // its TMEM and returns.
@@ -117,7 +119,7 @@ __device__ __forceinline__ void f4_copy_scales_on(uint32_t on, uint32_t taddr, u
 
 // how a tile is stored, F4_BY_TMA where f4_launch says so, else from registers;
 // pairs know it when they are compiled (for the registers: 16384 x 8192 x 2048
-// 92.5 us, 94.8 with both)
+// back to back 92.5 us, 94.8 with both)
 enum { F4_EITHER, F4_BY_TMA, F4_BY_LANES };
 
 // LONG: a sum takes several accumulators, chunk k-blocks each (compiled apart: pairs have

@@ -170,9 +170,9 @@ inline bool route_fp4_small(int M, int N, int K) {
 // Output tiles of the product of 4-bit floating-point matrices: 256 x 192 on CTA
 // pairs, 128 x 128 or 128 x 64 on single CTAs.
 //   64 columns while there is an SM for every tile (1000 x 512 x 2048 5.0 us, 128
-//   columns 5.7), else by time, t + waves x (a + b k-blocks of 256) us, fitted to 510
-//   products of 40 to 16384 rows, 512 to 32000 columns and K of 256 to 8192 (us, 128
-//   columns / pairs):
+//   columns 5.7), else by time, t + waves x (a + b k-blocks of 256) us, fitted to
+//   510 products of 40 to 16384 rows, 512 to 32000 columns and K of 256 to 8192, of which
+//   the host test keeps a third (us, 128 columns / pairs):
 //     512 x 32000 x 512 9.9 / 11.5;  384 x 32000 x 512 8.1 / 11.5
 //     4096 x 8192 x 512 16 / 18.3;  16384 x 8192 x 512 52.4 / 56.4
 //     2100 x 8192 x 8192 72.2 / 51.1;  16384 x 8192 x 8192 439 / 292
