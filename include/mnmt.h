@@ -498,6 +498,87 @@ int mnmt_dropout_backward(const void *g, int32_t otype, int64_t ldg, const void 
                           int32_t d, void *gx, int64_t ldgx, void *gr, int64_t ldgr, float *ggamma, void *workspace,
                           void *cuda_stream);
 
+/* Softmax attention of a batch of sequences of different lengths, without padding
+ * rows between them (or with them, where lengths are given apart from starts):
+ *   o[i][h] = sum_j P_ij v[j][h'],  P_ij = exp(s_ij - lse_i),  lse_i = log sum_j exp(s_ij),
+ *   s_ij = scale q[i][h] . k[j][h'],  h' = h / (q_heads / kv_heads)
+ * over the keys j of the query's own sequence; causal: the last query sees all keys, each
+ * one before it a key less (query i of n_q sees key j <= i + n_k - n_q).  A query that
+ * sees no key has o = 0 and lse = -inf.  What a query does not see (other sequences, later
+ * keys, rows of no sequence) does not enter its result, infinities and NaN included.
+ * Rows: sequence b has the query rows q_start[b] .. q_start[b] + q_len[b] - 1, in memory
+ *   order without overlap; q_len NULL: up to q_start[b + 1] - 1 (q_start then has
+ *   n_seqs + 1 entries, else n_seqs).  Keys alike with k_start and k_len; with k_len the
+ *   key rows of sequences may come in any order and be shared, but not in
+ *   mnmt_attention_backward.  Lengths may be zero.  Device arrays; what they name beyond
+ *   q_rows and k_rows is left out.
+ * q_rows, k_rows: rows in memory of q and o, and of k and v.  Output rows that belong to
+ *   no sequence are left as they are.
+ * d_head: a multiple of 8 up to 128.  dtype (MNMT_BF16 or MNMT_F16): of every operand
+ *   below but lse.  scale in (0, 2^60].
+ * Scores, weights' sums and results are summed in fp32; the weights (and in the backward
+ * pass P and dS) are rounded to dtype in front of the second product, results once. */
+typedef struct {
+    int32_t n_seqs, q_rows, k_rows, q_heads, kv_heads, d_head, dtype, causal;
+    float scale;
+    const int32_t *q_start, *q_len, *k_start, *k_len;
+} mnmt_attention_shape;
+
+/* Rows of heads: element e of head h of row t is data[t * row + h * head + e].  data
+ * 16-byte aligned, strides multiples of 8 elements (a row's of one row, a head's of one
+ * head are not looked at); a head per row or a row per head. */
+typedef struct {
+    void *data;
+    int64_t row, head;
+} mnmt_heads;
+
+/* Forward: o, and lse [q_heads][q_rows] (fp32, may be NULL).  o is no input.  workspace:
+ * mnmt_attention_forward_workspace(shape) bytes of device scratch, 16-byte aligned
+ * (sizes need none of the shape's arrays; 0: invalid shape).  *status (device int32, may
+ * be NULL) receives MNMT_ETIMEOUT if a bounded wait of a kernel gave up. */
+size_t mnmt_attention_forward_workspace(const mnmt_attention_shape *shape);
+int mnmt_attention_forward(const mnmt_attention_shape *shape, const mnmt_heads *q, const mnmt_heads *k, const mnmt_heads *v,
+                           const mnmt_heads *o, float *lse, void *workspace, int32_t *status, void *cuda_stream);
+
+/* Its gradients for the gradient g of o, from the forward pass's inputs, o and lse:
+ *   dv[j] = sum_i P_ij g[i],  dS_ij = P_ij (g[i] . v[j] - g[i] . o[i]),
+ *   dq[i] = scale sum_j dS_ij k[j],  dk[j] = scale sum_i dS_ij q[i]
+ * (dk, dv: over the query heads that share the key head).  Sums in a fixed order.  The
+ * gradients have the operands' type; none of their buffers is an input. */
+size_t mnmt_attention_backward_workspace(const mnmt_attention_shape *shape);
+int mnmt_attention_backward(const mnmt_attention_shape *shape, const mnmt_heads *q, const mnmt_heads *k, const mnmt_heads *v,
+                            const mnmt_heads *o, const float *lse, const mnmt_heads *g, const mnmt_heads *dq,
+                            const mnmt_heads *dk, const mnmt_heads *dv, void *workspace, int32_t *status,
+                            void *cuda_stream);
+
+/* The same for one query per sequence (decoding against a cache): row b of q and o
+ * belongs to sequence b (q_rows = n_seqs; q_start, q_len and causal are not looked at) and
+ * sees all of its k_len[b] keys from row k_start[b] on. */
+size_t mnmt_attention_token_workspace(const mnmt_attention_shape *shape);
+int mnmt_attention_token(const mnmt_attention_shape *shape, const mnmt_heads *q, const mnmt_heads *k, const mnmt_heads *v,
+                         const mnmt_heads *o, float *lse, void *workspace, int32_t *status, void *cuda_stream);
+
+/* Embedding of T tokens from a floating-point table [V][d] (type dtype, row stride ldt):
+ *   out[t] = fl(fl(scale table[ids[t]]) + pe[pos[t]])
+ * rounded once to otype; pe [P][d] fp32 or NULL (nothing is added), pos [T] or NULL (row t
+ * is position t).  A token id outside [0, V) or a position outside [0, P) gives a row of
+ * zeros and MNMT_EINVAL in *status (device int32, may be NULL). */
+int mnmt_embed(const int32_t *ids, int32_t T, const void *table, int32_t dtype, int64_t ldt, int32_t V, int32_t d, float scale,
+               const int32_t *pos, const float *pe, int64_t ldpe, int32_t P, void *out, int32_t otype, int64_t ldo,
+               int32_t *status, void *cuda_stream);
+
+/* Its gradient for the gradient g [T][d] (type gtype) of out:
+ *   gtable[v] = fl(scale sum of g[t] over the tokens t with ids[t] = v)
+ * in fp32 and a fixed order, rounded once to otype; accumulate: added to what gtable
+ * holds, and rows that no token names are not touched (else they are zero).  Tokens pad_id
+ * (-1: none) take no gradient; ids outside [0, V) neither, with MNMT_EINVAL in *status.
+ * workspace: mnmt_embed_backward_workspace(T, V, d) bytes of device scratch, 16-byte
+ * aligned (0: invalid sizes). */
+size_t mnmt_embed_backward_workspace(int32_t T, int32_t V, int32_t d);
+int mnmt_embed_backward(const int32_t *ids, int32_t T, const void *g, int32_t gtype, int64_t ldg, float scale, int32_t pad_id,
+                        int32_t V, int32_t d, void *gtable, int32_t otype, int64_t ldt, int32_t accumulate, void *workspace,
+                        int32_t *status, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,214 @@
+// seq_attn.cuh -- softmax attention over sequences whose rows lie one after
+// another (include/mnmt.h, mnmt_attention_forward / _backward / _token): the
+// shapes its kernels share and the plain loops over one row's own keys.
+//
+//   s_ij = scale q_i . k_j,  P_ij = exp(s_ij - lse_i),  o_i = sum_j P_ij v_j
+//   lse_i = log sum_j exp(s_ij)
+//   D_i = do_i . o_i,  dS_ij = P_ij (do_i . v_j - D_i)
+//   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij do_i
+//
+// The keys that a query sees are one interval of key rows, and the queries that
+// see a key one interval of query rows; a mask is a pair of row numbers.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "fp4.cuh"
+#include "train.h"
+
+namespace mnmt {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+struct Span {
+    int lo, hi;  // rows lo .. hi - 1; empty where hi <= lo
+};
+
+// the sequence that row may belong to: the last of n that starts at or before it, -1 if none
+MNMT_DEV int seq_of(const int *start, int n, int row) {
+    int lo = 0, hi = n;  // starts before lo are <= row, from hi on > row
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (__ldg(start + mid) <= row) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo - 1;
+}
+
+// rows of sequence b, whatever the arrays hold within 0 .. rows
+MNMT_DEV Span seq_rows(const int *start, const int *len, int b, int rows) {
+    const int s = __ldg(start + b);
+    const long e = len ? (long)s + max(__ldg(len + b), 0) : (long)__ldg(start + b + 1);
+    Span r;
+    r.lo = min(max(s, 0), rows);
+    r.hi = (int)(e < r.lo ? r.lo : e > rows ? rows : e);
+    return r;
+}
+
+// the keys that query row sees (in: whether it belongs to a sequence at all)
+MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, bool &in) {
+    const int b = row < a.q_rows ? seq_of(a.q_start, a.n_seqs, row) : -1;
+    in = false;
+    if (b < 0) return Span{0, 0};
+    const Span q = seq_rows(a.q_start, a.q_len, b, a.q_rows);
+    if (row >= q.hi) return Span{0, 0};
+    in = true;
+    Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
+    if (a.causal) k.hi = min(k.hi, k.hi - (q.hi - 1 - row));  // the last query sees all keys
+    if (k.hi < k.lo) k.hi = k.lo;
+    return k;
+}
+
+// the queries that see key row
+MNMT_DEV Span queries_of_key(const SeqAttn &a, int row, bool &in) {
+    const int b = row < a.k_rows ? seq_of(a.k_start, a.n_seqs, row) : -1;
+    in = false;
+    if (b < 0) return Span{0, 0};
+    const Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
+    if (row >= k.hi) return Span{0, 0};
+    in = true;
+    Span q = seq_rows(a.q_start, a.q_len, b, a.q_rows);
+    if (a.causal) q.lo = max(q.lo, q.hi - (k.hi - row));
+    if (q.hi < q.lo) q.hi = q.lo;
+    return q;
+}
+
+MNMT_DEV float warp_sum_f(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+
+// 2^x to within 2 ulp, 0 below -126
+MNMT_DEV float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// dot product of dh elements (a multiple of 8) of two rows on 16 bytes
+template <typename T>
+MNMT_DEV float row_dot(const T *x, const T *y, int dh) {
+    float s = 0.0f;
+    for (int c = 0; c < dh; c += 8) {
+        float u[8], v[8];
+        load8<T, true>(x + c, 8, u);
+        load8<T, true>(y + c, 8, v);
+#pragma unroll
+        for (int i = 0; i < 8; i++) s = fmaf(u[i], v[i], s);
+    }
+    return s;
+}
+
+// four elements of a row, 8-byte aligned
+template <typename T>
+MNMT_DEV void load4(const T *p, float (&v)[4]) {
+    const uint2 w = *reinterpret_cast<const uint2 *>(p);
+    if constexpr (std::is_same_v<T, __half>) {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&w.x)), b = __half22float2(*reinterpret_cast<const __half2 *>(&w.y));
+        v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+    } else {
+        v[0] = __uint_as_float(w.x << 16), v[1] = __uint_as_float(w.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(w.y << 16), v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+    }
+}
+template <typename T>
+MNMT_DEV void store4(T *p, const float (&v)[4]) {
+    uint2 w;
+    T *t = reinterpret_cast<T *>(&w);
+#pragma unroll
+    for (int i = 0; i < 4; i++) t[i] = from_f32<T>(v[i]);
+    *reinterpret_cast<uint2 *>(p) = w;
+}
+
+// One query row by a warp: lane l holds elements 4 l .. 4 l + 3 of the sum (dh <= 128).
+// m: the largest score times log2 e, l: sum of 2^(s - m), over keys k.lo .. k.hi - 1.
+struct RowSum {
+    float m, l, acc[4];
+};
+template <typename T>
+__device__ __noinline__ RowSum attn_row(const T *q, const T *k, long ldk, const T *v, long ldv, Span s, int dh, float c) {
+    const int lane = threadIdx.x & 31;
+    RowSum r{-INFINITY, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+    for (int j0 = s.lo; j0 < s.hi; j0 += 32) {
+        const int j = j0 + lane;
+        const bool on = j < s.hi;
+        const float x = on ? row_dot(q, k + j * ldk, dh) * c : -INFINITY;
+        const float mn = fmaxf(r.m, warp_max_f(x)), mu = mn == -INFINITY ? 0.0f : mn;
+        const float p = on ? exp2_fast(x - mu) : 0.0f, alpha = exp2_fast(r.m - mu);
+        r.m = mn;
+        r.l = fmaf(r.l, alpha, warp_sum_f(p));
+#pragma unroll
+        for (int i = 0; i < 4; i++) r.acc[i] *= alpha;
+        const int n = min(32, s.hi - j0);
+        for (int t = 0; t < n; t++) {
+            const float pt = __shfl_sync(0xFFFFFFFFu, p, t);
+            if (4 * lane < dh) {
+                float w[4];
+                load4(v + (j0 + t) * ldv + 4 * lane, w);
+#pragma unroll
+                for (int i = 0; i < 4; i++) r.acc[i] = fmaf(pt, w[i], r.acc[i]);
+            }
+        }
+    }
+    return r;
+}
+// log-sum-exp of a row
+MNMT_DEV float row_lse(float m, float l) { return fmaf(m, LN2, logf(l)); }
+
+// dq of one query row (without the scale): lane l holds elements 4 l .. 4 l + 3
+template <typename T>
+__device__ __noinline__ float4 attn_row_dq(const T *q, const T *g, float lse2, float delta, const T *k, long ldk, const T *v, long ldv, Span s, int dh,
+                                           float c) {
+    const int lane = threadIdx.x & 31;
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j0 = s.lo; j0 < s.hi; j0 += 32) {
+        const int j = j0 + lane;
+        float ds = 0.0f;
+        if (j < s.hi) {
+            const float p = exp2_fast(fmaf(row_dot(q, k + j * ldk, dh), c, -lse2));
+            ds = p * (row_dot(g, v + j * ldv, dh) - delta);
+        }
+        const int n = min(32, s.hi - j0);
+        for (int t = 0; t < n; t++) {
+            const float d = __shfl_sync(0xFFFFFFFFu, ds, t);
+            if (4 * lane < dh) {
+                float w[4];
+                load4(k + (j0 + t) * ldk + 4 * lane, w);
+#pragma unroll
+                for (int i = 0; i < 4; i++) acc[i] = fmaf(d, w[i], acc[i]);
+            }
+        }
+    }
+    return make_float4(acc[0], acc[1], acc[2], acc[3]);
+}
+
+// dk (without the scale) and dv of one key row from one query head, added to dk and dv
+template <typename T>
+__device__ __noinline__ void attn_row_dkv(const T *k, const T *v, const T *q, long ldq, const T *g, long ldg, const float *lse, const float *delta, Span s,
+                                          int dh, float c, float (&dk)[4], float (&dv)[4]) {
+    const int lane = threadIdx.x & 31;
+    for (int i0 = s.lo; i0 < s.hi; i0 += 32) {
+        const int i = i0 + lane;
+        float p = 0.0f, ds = 0.0f;
+        if (i < s.hi) {
+            p = exp2_fast(fmaf(row_dot(q + i * ldq, k, dh), c, -lse[i] * LOG2E));
+            ds = p * (row_dot(g + i * ldg, v, dh) - delta[i]);
+        }
+        const int n = min(32, s.hi - i0);
+        for (int t = 0; t < n; t++) {
+            const float pt = __shfl_sync(0xFFFFFFFFu, p, t), dt = __shfl_sync(0xFFFFFFFFu, ds, t);
+            if (4 * lane < dh) {
+                float w[4], u[4];
+                load4(q + (i0 + t) * ldq + 4 * lane, w);
+                load4(g + (i0 + t) * ldg + 4 * lane, u);
+#pragma unroll
+                for (int e = 0; e < 4; e++) dk[e] = fmaf(dt, w[e], dk[e]), dv[e] = fmaf(pt, u[e], dv[e]);
+            }
+        }
+    }
+}
+
+}  // namespace mnmt

@@ -1,5 +1,5 @@
-// train.h -- launches of the operators on microscaled 4-bit floating point (fp4.cuh)
-// and of dropout.
+// train.h -- launches of the operators on microscaled 4-bit floating point (fp4.cuh),
+// of dropout, of attention over sequences (seq_attn.cuh) and of the embedding.
 #pragma once
 
 #include "internal.h"
@@ -43,5 +43,50 @@ struct DropoutArgs {
 };
 cudaError_t launch_dropout(const DropoutArgs &a, cudaStream_t st);
 cudaError_t launch_dropout_backward(const DropoutArgs &a, cudaStream_t st);
+
+// element (row, head, e) of an attention operand is at p + row * ld + head * hd + e
+struct HeadRows {
+    void *p;
+    long ld, hd;
+};
+// attention over sequences (seq_attn.cuh); sequence b has query rows from q_start[b] on, q_len[b] of them
+// (q_len null: up to q_start[b + 1]), keys alike
+struct SeqAttn {
+    int n_seqs, q_rows, k_rows, hq, hkv, dh, dtype, causal;
+    float scale;
+    const int *q_start, *q_len, *k_start, *k_len;
+    HeadRows q, k, v, o;
+    float *lse;  // [hq][q_rows], natural logarithm
+    HeadRows g, dq, dk, dv;  // backward: output gradient, results
+    void *workspace;
+    int *status;
+    __host__ __device__ int group() const { return hq / hkv; }
+};
+size_t seq_attn_forward_workspace(const SeqAttn &a);
+size_t seq_attn_backward_workspace(const SeqAttn &a);
+size_t seq_attn_token_workspace(const SeqAttn &a);
+cudaError_t launch_seq_attn_forward(const SeqAttn &a, cudaStream_t st);
+cudaError_t launch_seq_attn_backward(const SeqAttn &a, cudaStream_t st);
+cudaError_t launch_seq_attn_token(const SeqAttn &a, cudaStream_t st);
+
+struct EmbedRowsArgs {
+    const int32_t *ids, *pos;  // [T]; pos null: row t is position t
+    int T, V, d, P;
+    const void *table;         // backward: the gradient of the rows [T][d]
+    int dtype;
+    long ld;
+    float scale;
+    const float *pe;           // null: none
+    long ldpe;
+    void *out;                 // backward: the gradient of the table [V][d]
+    int otype;
+    long ldo;
+    int pad_id, accumulate;    // backward
+    void *workspace;
+    int *status;
+};
+cudaError_t launch_embed_rows(const EmbedRowsArgs &a, cudaStream_t st);
+cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &a, cudaStream_t st);
+size_t embed_rows_backward_workspace(int T, int V, int d);
 
 }  // namespace mnmt

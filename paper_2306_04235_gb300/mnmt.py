@@ -51,6 +51,36 @@ class Fp4(C.Structure):
         self.buffers = codes, scales
 
 
+class AttentionShape(C.Structure):
+    """A batch of sequences and its heads (mnmt_attention_shape): starts and lengths are device buffers, kept alive by
+    this object."""
+    _fields_ = [(n, C.c_int32) for n in ["n_seqs", "q_rows", "k_rows", "q_heads", "kv_heads", "d_head", "dtype", "causal"]] + \
+        [("scale", C.c_float)] + [(n, C.c_void_p) for n in ["q_start", "q_len", "k_start", "k_len"]]
+
+    def __init__(self, n_seqs, q_rows, k_rows, q_heads, kv_heads, d_head, dtype, causal, scale, q_start, k_start, q_len=None,
+                 k_len=None):
+        super().__init__(n_seqs, q_rows, k_rows, q_heads, kv_heads, d_head, dtype, int(causal), scale, _ptr(q_start), _ptr(q_len),
+                         _ptr(k_start), _ptr(k_len))
+        self.buffers = q_start, q_len, k_start, k_len
+
+
+class Heads(C.Structure):
+    """Rows of heads (mnmt_heads): the buffer and its row and head strides in elements."""
+    _fields_ = [("data", C.c_void_p), ("row", C.c_int64), ("head", C.c_int64)]
+
+    def __init__(self, data, row, head):
+        super().__init__(_ptr(data), row, head)
+        self.buffer = data
+
+
+def heads(x) -> Heads:
+    """The Heads of a tensor [rows][heads][d] whose elements of a head lie one after another."""
+    row, head, one = x.stride()
+    if one != 1 and x.shape[2] > 1:
+        raise ValueError("heads: elements of a head must lie one after another")
+    return Heads(x, row, head)
+
+
 def lib_path() -> str:
     return _build.LIB
 
@@ -116,6 +146,17 @@ def _declare(L):
     L.mnmt_dropout.argtypes = [p, i32, i64, p, i64, f, f, u64, u64, i32, i32, i32, p, i32, i64, p]
     L.mnmt_dropout_backward.argtypes = [p, i32, i64, p, i32, i64, p, i64, f, f, u64, u64, i32, i32, i32, p, i64, p, i64,
                                         p, p, p]
+    shape, hd = C.POINTER(AttentionShape), C.POINTER(Heads)
+    for n in ["forward", "backward", "token"]:
+        size = getattr(L, f"mnmt_attention_{n}_workspace")
+        size.argtypes, size.restype = [shape], sz
+    L.mnmt_attention_forward.argtypes = L.mnmt_attention_token.argtypes = [shape, hd, hd, hd, hd, p, p, p, p]
+    L.mnmt_attention_backward.argtypes = [shape, hd, hd, hd, hd, p, hd, hd, hd, hd, p, p, p]
+    L.mnmt_embed.argtypes = [p, i32, p, i32, i64, i32, i32, f, p, p, i64, i32, p, i32, i64, p, p]
+    L.mnmt_embed_backward_workspace.argtypes = [i32, i32, i32]; L.mnmt_embed_backward_workspace.restype = sz
+    L.mnmt_embed_backward.argtypes = [p, i32, p, i32, i64, f, i32, i32, i32, p, i32, i64, i32, p, p, p]
+    for n in ["mnmt_attention_forward", "mnmt_attention_backward", "mnmt_attention_token", "mnmt_embed", "mnmt_embed_backward"]:
+        getattr(L, n).restype = C.c_int
     for n in ["mnmt_fp4_quantize", "mnmt_fp4_dequantize", "mnmt_fp4_quantize_backward", "mnmt_fp4_linear",
               "mnmt_fp4_linear_backward", "mnmt_dropout", "mnmt_dropout_backward"]:
         getattr(L, n).restype = C.c_int
@@ -360,6 +401,50 @@ def mnmt_dropout_backward(g, otype, ldg, x, dtype, ldx, r, ldr, gamma, p, seed, 
     _chk(lib().mnmt_dropout_backward(_ptr(g), otype, ldg, _ptr(x), dtype, ldx, _ptr(r), ldr, gamma, p, seed, offset,
                                      int(relu), M, d, _ptr(gx), ldgx, _ptr(gr), ldgr, _ptr(ggamma), _ptr(workspace),
                                      _stream_handle(stream)))
+
+
+def mnmt_attention_forward_workspace(shape: AttentionShape) -> int:
+    return lib().mnmt_attention_forward_workspace(shape)
+
+
+def mnmt_attention_backward_workspace(shape: AttentionShape) -> int:
+    return lib().mnmt_attention_backward_workspace(shape)
+
+
+def mnmt_attention_token_workspace(shape: AttentionShape) -> int:
+    return lib().mnmt_attention_token_workspace(shape)
+
+
+def mnmt_attention_forward(shape: AttentionShape, q: Heads, k: Heads, v: Heads, o: Heads, lse, workspace, status=None, stream=None):
+    """Softmax attention of a batch of sequences into o and (where given) lse [q_heads][q_rows]."""
+    _chk(lib().mnmt_attention_forward(shape, q, k, v, o, _ptr(lse), _ptr(workspace), _ptr(status), _stream_handle(stream)))
+
+
+def mnmt_attention_backward(shape: AttentionShape, q: Heads, k: Heads, v: Heads, o: Heads, lse, g: Heads, dq: Heads, dk: Heads, dv: Heads,
+                            workspace, status=None, stream=None):
+    """Gradients dq, dk and dv of mnmt_attention_forward for the gradient g of o."""
+    _chk(lib().mnmt_attention_backward(shape, q, k, v, o, _ptr(lse), g, dq, dk, dv, _ptr(workspace), _ptr(status), _stream_handle(stream)))
+
+
+def mnmt_attention_token(shape: AttentionShape, q: Heads, k: Heads, v: Heads, o: Heads, lse, workspace, status=None, stream=None):
+    """Attention of one query per sequence against a cache of keys and values."""
+    _chk(lib().mnmt_attention_token(shape, q, k, v, o, _ptr(lse), _ptr(workspace), _ptr(status), _stream_handle(stream)))
+
+
+def mnmt_embed(ids, T, table, dtype, ldt, V, d, scale, out, otype, ldo, pos=None, pe=None, ldpe=0, P=0, status=None, stream=None):
+    """out[t] = scale table[ids[t]] + pe[pos[t]] (pe None: nothing added, pos None: position t)."""
+    _chk(lib().mnmt_embed(_ptr(ids), T, _ptr(table), dtype, ldt, V, d, scale, _ptr(pos), _ptr(pe), ldpe, P, _ptr(out), otype, ldo,
+                          _ptr(status), _stream_handle(stream)))
+
+
+def mnmt_embed_backward_workspace(T: int, V: int, d: int) -> int:
+    return lib().mnmt_embed_backward_workspace(T, V, d)
+
+
+def mnmt_embed_backward(ids, T, g, gtype, ldg, scale, pad_id, V, d, gtable, otype, ldt, accumulate, workspace, status=None, stream=None):
+    """Gradient of mnmt_embed's table for the gradient g of its output."""
+    _chk(lib().mnmt_embed_backward(_ptr(ids), T, _ptr(g), gtype, ldg, scale, pad_id, V, d, _ptr(gtable), otype, ldt, int(accumulate),
+                                   _ptr(workspace), _ptr(status), _stream_handle(stream)))
 
 
 def mnmt_codes_to_f16(src, dst, n, stream=None):
