@@ -3,6 +3,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <mutex>
 
 #include "train.h"
 
@@ -31,6 +32,22 @@ bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 bool matrix_ok(const void *p, int32_t dtype, int64_t ld, int32_t cols) {
     const int e = type_size(dtype);
     return e && p && aligned(p, e) && ld >= cols && ld <= MAX_LD;
+}
+
+// one-time set-up of the attention kernels on the current device
+int seq_ready() {
+    if (int rc = ensure_device()) return rc;
+    static std::mutex mu;
+    static bool ready[64] = {false};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return fail(MNMT_ECUDA, "attention: no usable current device");
+    std::lock_guard<std::mutex> lk(mu);
+    if (!ready[dev]) {
+        const cudaError_t e = seq_attn_init();
+        if (e != cudaSuccess) return fail(MNMT_ECUDA, "attention kernel set-up failed: %s", cudaGetErrorString(e));
+        ready[dev] = true;
+    }
+    return MNMT_OK;
 }
 
 // 0 if the shape is valid; with a shape alone (sizes of workspaces) nothing of its arrays is looked at
@@ -124,7 +141,7 @@ extern "C" int mnmt_attention_forward(const mnmt_attention_shape *shape, const m
                                       float *lse, void *workspace, int32_t *status, void *cuda_stream) {
     SeqAttn a;
     int rc = check_forward("attention_forward", shape, q, k, v, o, lse, workspace, status, false, a);
-    if (rc || (rc = ensure_device())) return rc;
+    if (rc || (rc = seq_ready())) return rc;
     if (a.n_seqs == 0 || a.q_rows == 0) return MNMT_OK;
     return done(launch_seq_attn_forward(a, static_cast<cudaStream_t>(cuda_stream)), "attention_forward");
 }
@@ -133,7 +150,7 @@ extern "C" int mnmt_attention_token(const mnmt_attention_shape *shape, const mnm
                                     float *lse, void *workspace, int32_t *status, void *cuda_stream) {
     SeqAttn a;
     int rc = check_forward("attention_token", shape, q, k, v, o, lse, workspace, status, true, a);
-    if (rc || (rc = ensure_device())) return rc;
+    if (rc || (rc = seq_ready())) return rc;
     if (a.n_seqs == 0) return MNMT_OK;
     return done(launch_seq_attn_token(a, static_cast<cudaStream_t>(cuda_stream)), "attention_token");
 }
@@ -156,7 +173,7 @@ extern "C" int mnmt_attention_backward(const mnmt_attention_shape *shape, const 
         for (int j = 0; j < i; j++)
             if (same(*out[i], *out[j])) return fail(MNMT_EINVAL, "%s: two gradients in one buffer", call);
     }
-    if ((rc = ensure_device())) return rc;
+    if ((rc = seq_ready())) return rc;
     if (a.n_seqs == 0 || (a.q_rows == 0 && a.k_rows == 0)) return MNMT_OK;
     return done(launch_seq_attn_backward(a, static_cast<cudaStream_t>(cuda_stream)), call);
 }

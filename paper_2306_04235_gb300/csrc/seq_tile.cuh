@@ -1,0 +1,120 @@
+// seq_tile.cuh -- tiles of 128 rows of one head, as the tcgen05 kernels of
+// attention over sequences move and multiply them.
+//
+// A tile in shared memory: DH / 64 boxes of 128 rows x 64 elements (128 bytes),
+// 128-byte swizzle, as TMA leaves them (heads of fewer than 64 or 128 elements are
+// filled up with zeros).  Read with K-major rows it is an operand whose sum runs
+// over the head's elements; read MN-major, one whose sum runs over the rows.
+#pragma once
+
+#include "fp4_tile.cuh"
+#include "seq_attn.cuh"
+
+namespace mnmt {
+
+constexpr int SQ_ROWS = 128;                 // rows of a tile
+constexpr int SQ_BOX = SQ_ROWS * 128;        // bytes of a box
+template <int DH>
+__host__ __device__ constexpr int sq_bytes() { return DH / 64 * SQ_BOX; }
+
+// dimensions {element, head, row}: the coordinates of a box may start at a negative row or end past the last (zeros)
+inline bool sq_map(CUtensorMap *tm, const HeadRows &x, int rows, int heads, int dh) {
+    cuuint64_t dims[3] = {(cuuint64_t)dh, (cuuint64_t)heads, (cuuint64_t)rows}, strides[2] = {(cuuint64_t)x.hd * 2, (cuuint64_t)x.ld * 2};
+    cuuint32_t box[3] = {64, 1, SQ_ROWS}, estr[3] = {1, 1, 1};
+    return tma_encoder()(tm, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, x.p, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// the tile from row on of a head (one thread): completes on bar, which expects sq_bytes<DH>()
+template <int DH>
+__device__ __forceinline__ void sq_load(uint32_t dst, const CUtensorMap *tm, int head, int row, uint32_t bar) {
+    mbar_expect_tx(bar, sq_bytes<DH>());
+#pragma unroll
+    for (int b = 0; b < DH / 64; b++)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst + b * SQ_BOX),
+            "l"(reinterpret_cast<uint64_t>(tm)), "r"(64 * b), "r"(head), "r"(row), "r"(bar)
+            : "memory");
+}
+
+// descriptors of 16 reduction indices: K-major step k of the head's elements, MN-major step k of the rows
+__device__ __forceinline__ uint64_t sq_k(uint32_t tile, int k) { return sw128_desc(tile + (k >> 2) * SQ_BOX + (k & 3) * 32); }
+__device__ __forceinline__ uint64_t sq_mn(uint32_t tile, int k) {
+    return (uint64_t)(((tile + k * 2048) >> 4) & 0x3FFFu) | ((uint64_t)(SQ_BOX >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+           ((uint64_t)2 << 61);
+}
+// kind::f16, D fp32 of 128 x n; bf: bf16 operands; b_mn: B is MN-major
+__host__ __device__ constexpr uint32_t sq_idesc(int n, bool bf, bool b_mn) {
+    return (1u << 4) | ((bf ? 1u : 0u) << 7) | ((bf ? 1u : 0u) << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+// A from tensor memory: lane = row, a column holds two elements
+__device__ __forceinline__ void mma_f16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+        "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <bool BF>
+__device__ __forceinline__ uint32_t sq_pack(float lo, float hi) {
+    uint32_t r;
+    if constexpr (BF) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ unsigned long long sq_fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// the 32 lanes' bits of columns lo .. hi - 1 of a block of 32
+__device__ __forceinline__ uint32_t sq_bits(int lo, int hi) {
+    const uint32_t up = hi >= 32 ? 0xFFFFFFFFu : hi <= 0 ? 0u : (1u << hi) - 1u;
+    return lo >= 32 ? 0u : lo <= 0 ? up : up & ~((1u << lo) - 1u);
+}
+
+// A column range of a row stored from fp32: COLS elements from element c0 on, those below dh, in 16-byte pieces
+template <bool BF, int COLS>
+__device__ __forceinline__ void sq_store(void *row, int c0, int dh, const float (&v)[COLS]) {
+#pragma unroll
+    for (int c = 0; c < COLS; c += 8)
+        if (c0 + c < dh)
+            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(row) + c0 + c) =
+                make_uint4(sq_pack<BF>(v[c], v[c + 1]), sq_pack<BF>(v[c + 2], v[c + 3]), sq_pack<BF>(v[c + 4], v[c + 5]), sq_pack<BF>(v[c + 6], v[c + 7]));
+}
+
+// Waits of a kernel's roles: a wait that gives up sets `failed` in shared memory and the
+// status, and every role leaves its loop at its next wait.
+struct SqWaits {
+    volatile int *failed;
+    int *status;
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
+        if (mbar_test(bar, parity)) return true;
+        return slow(bar, parity);
+    }
+    __device__ __noinline__ bool slow(uint32_t bar, uint32_t parity) const {
+        for (int i = 0; i < 8; i++)
+            if (mbar_try(bar, parity)) return true;
+        const unsigned long long t0 = global_ns();
+        while (!mbar_try(bar, parity))
+            if (*failed || global_ns() - t0 > MNMT_WAIT_NS) {
+                *failed = 1;
+                set_status(status, MNMT_ETIMEOUT);
+                return false;
+            }
+        return true;
+    }
+};
+
+}  // namespace mnmt
