@@ -43,7 +43,8 @@ int seq_ready() {
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return fail(MNMT_ECUDA, "attention: no usable current device");
     std::lock_guard<std::mutex> lk(mu);
     if (!ready[dev]) {
-        const cudaError_t e = seq_attn_init();
+        cudaError_t e = seq_attn_init();
+        if (e == cudaSuccess) e = seq_attn_backward_init();
         if (e != cudaSuccess) return fail(MNMT_ECUDA, "attention kernel set-up failed: %s", cudaGetErrorString(e));
         ready[dev] = true;
     }

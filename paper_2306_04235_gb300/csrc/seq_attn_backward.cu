@@ -1,78 +1,551 @@
-// seq_attn_backward.cu -- gradients of attention over sequences (seq_attn.cuh): D,
-// then a warp per query row for dq and a warp per key row for dk and dv.
-#include "seq_attn.cuh"
+// seq_attn_backward.cu -- gradients of attention over sequences (seq_attn.cuh), in two
+// kernels, each of which computes the scores again and adds up in TMEM, in a fixed order:
+//   dq:      128 query rows of a head walk the keys that they see:
+//            S = Q K^T, dP = G V^T, dS = P (dP - D), dQ += dS K; D = sum g o on the way in
+//   dk, dv:  128 key rows of a key head walk the queries that see them, head by head:
+//            S^T = K Q^T, dP^T = V G^T, dV += P^T G, dK += dS^T Q
+// (seven products instead of the five of one kernel that adds to dQ from everywhere,
+// whose sums would depend on the order of arrival).
+// One CTA per SM, eight warps of two threads per row.  P and dS go to TMEM in the
+// operands' type, as the A operand of the second products.  While the threads work on
+// one of S and dP the tensor core is on the products that follow the other:
+//   dk, dv:  dV(j), S(j+1) once P(j) is written, dK(j), dP(j+1) once dS(j) is
+//   dq:      S(j+1), dP(j+1) once S(j), dP(j) are in registers, dQ(j) once dS(j) is written
+// A walk goes backwards from the last row that is seen, as in the forward pass, and rows
+// whose result is not finite are computed again over their own queries or keys alone.
+#include "seq_tile.cuh"
 
 namespace mnmt {
 namespace {
 
-template <typename T>
-__global__ void __launch_bounds__(256) seq_attn_delta_kernel(SeqAttn a, float *delta) {
-    pdl_grid_wait();
-    const long w = (long)blockIdx.x * 256 + threadIdx.x;
-    if (w >= (long)a.q_rows * a.hq) return;
-    const int row = (int)(w / a.hq), h = (int)(w % a.hq);
-    delta[(long)h * a.q_rows + row] =
-        row_dot(static_cast<const T *>(a.o.p) + row * a.o.ld + h * a.o.hd, static_cast<const T *>(a.g.p) + row * a.g.ld + h * a.g.hd, a.dh);
+constexpr int BW_THREADS = 320;  // eight warps on the elements, a TMA warp, an MMA warp
+
+__device__ __forceinline__ void elements_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// A thread's 64 columns (of a row's 128) from TMEM
+__device__ __forceinline__ void load64(uint32_t taddr, uint32_t (&r)[2][32]) {
+    tmem_ld32(taddr, r[0]);
+    tmem_ld32(taddr + 32, r[1]);
+    tmem_wait_ld();
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) seq_attn_dq_rows_kernel(SeqAttn a, float c, const float *delta) {
-    pdl_grid_wait();
-    const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 5;
-    if (w >= (long)a.q_rows * a.hq) return;
-    const int row = (int)(w / a.hq), h = (int)(w % a.hq), hk = h / a.group(), lane = threadIdx.x & 31;
-    bool in;
-    const Span s = keys_of_query(a, row, in);
-    if (!in) return;
-    const long at = (long)h * a.q_rows + row;
-    const float4 d = attn_row_dq(static_cast<const T *>(a.q.p) + row * a.q.ld + h * a.q.hd, static_cast<const T *>(a.g.p) + row * a.g.ld + h * a.g.hd,
-                                 a.lse[at] * LOG2E, delta[at], static_cast<const T *>(a.k.p) + hk * a.k.hd, a.k.ld,
-                                 static_cast<const T *>(a.v.p) + hk * a.v.hd, a.v.ld, s, a.dh, c);
-    const float o[4] = {d.x * a.scale, d.y * a.scale, d.z * a.scale, d.w * a.scale};
-    if (4 * lane < a.dh) store4(static_cast<T *>(a.dq.p) + row * a.dq.ld + h * a.dq.hd + 4 * lane, o);
-}
+// --------------------------------------------------------------------------- dq
+template <int DH>
+struct DqLayout {
+    static constexpr int STAGES = 2, TILE = sq_bytes<DH>();
+    static constexpr int OFF_G = TILE, OFF_K = 2 * TILE, OFF_V = OFF_K + STAGES * TILE, SMEM = OFF_V + STAGES * TILE + 1024;
+    static constexpr int T_DP = 128, T_DS = 256, T_DQ = 320;  // columns of dP, dS and dQ behind S
+};
 
-template <typename T>
-__global__ void __launch_bounds__(256) seq_attn_dkv_rows_kernel(SeqAttn a, float c, const float *delta) {
+template <int DH, bool BF>
+__global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
+                                                                    const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
+                                                                    const SeqAttn a, const float c, float *delta) {
+    using L = DqLayout<DH>;
+    using T = std::conditional_t<BF, __nv_bfloat16, __half>;
+    constexpr int ST = L::STAGES;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[4 * ST + 6];
+    __shared__ uint32_t tslot;
+    __shared__ int failed, span[2][4];
+    __shared__ float part[2][SQ_ROWS];
+    __shared__ uint8_t odd_rows[2][SQ_ROWS];
+    const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
+    const auto k_full = [&](int s) { return bar0 + 8 * s; };
+    const auto k_free = [&](int s) { return bar0 + 8 * (ST + s); };
+    const auto v_full = [&](int s) { return bar0 + 8 * (2 * ST + s); };
+    const auto v_free = [&](int s) { return bar0 + 8 * (3 * ST + s); };
+    const uint32_t q_full = bar0 + 8 * (4 * ST), sp_full = q_full + 8, sp_free = q_full + 16, ds_full = q_full + 24, ds_free = q_full + 32,
+                   dq_full = q_full + 40;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int h = blockIdx.x % a.hq, hk = h / a.group(), tile = (int)(gridDim.x / a.hq) - 1 - (int)(blockIdx.x / a.hq);
+    const int half = warp >> 2, rt = (int)threadIdx.x & 127, row = tile * SQ_ROWS + rt;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < ST; s++) mbar_init(k_full(s), 1), mbar_init(k_free(s), 1), mbar_init(v_full(s), 1), mbar_init(v_free(s), 1);
+        mbar_init(q_full, 2), mbar_init(sp_full, 1), mbar_init(sp_free, 8), mbar_init(ds_full, 8), mbar_init(ds_free, 1), mbar_init(dq_full, 1);
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) tmem_alloc<512>(s_addr(&tslot));
     pdl_grid_wait();
-    const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 5;
-    if (w >= (long)a.k_rows * a.hkv) return;
-    const int row = (int)(w / a.hkv), hk = (int)(w % a.hkv), lane = threadIdx.x & 31;
-    bool in;
-    const Span s = queries_of_key(a, row, in);
-    if (!in) return;
-    float dk[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int h = hk * a.group(); h < (hk + 1) * a.group(); h++)
-        attn_row_dkv(static_cast<const T *>(a.k.p) + row * a.k.ld + hk * a.k.hd, static_cast<const T *>(a.v.p) + row * a.v.ld + hk * a.v.hd,
-                     static_cast<const T *>(a.q.p) + h * a.q.hd, a.q.ld, static_cast<const T *>(a.g.p) + h * a.g.hd, a.g.ld,
-                     a.lse + (long)h * a.q_rows, delta + (long)h * a.q_rows, s, a.dh, c, dk, dv);
+    Span keys{0, 0};
+    bool in = false;
+    if (warp < 8) {
+        keys = keys_of_query(a, row, in);
+        const bool some = keys.hi > keys.lo;
+        const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? keys.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? keys.hi : 0);
+        if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tS = tslot, tP = tS + L::T_DP, tD = tS + L::T_DS, tO = tS + L::T_DQ;
+    const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
+    const int nt = end > first ? (end - first + SQ_ROWS - 1) / SQ_ROWS : 0;
+    const SqWaits wait{&failed, a.status};
+
+    if (warp == 8) {
+        if (lane == 0 && nt) {
+            sq_load<DH>(sm, &tq, h, tile * SQ_ROWS, q_full);
+            sq_load<DH>(sm + L::OFF_G, &tg, h, tile * SQ_ROWS, q_full);
+            int j = 0;
+            for (; j < nt; j++) {
+                const int s = j % ST, at = end - SQ_ROWS * (j + 1);
+                const uint32_t ph = (uint32_t)(j / ST - 1) & 1;
+                if (j >= ST && !wait(k_free(s), ph)) break;
+                sq_load<DH>(sm + L::OFF_K + s * L::TILE, &tk, hk, at, k_full(s));
+                if (j >= ST && !wait(v_free(s), ph)) {
+                    wait(k_full(s), (uint32_t)(j / ST) & 1);  // in flight
+                    break;
+                }
+                sq_load<DH>(sm + L::OFF_V + s * L::TILE, &tv, hk, at, v_full(s));
+            }
+            if (failed) {  // copies in flight land before the block ends
+                wait(q_full, 0);
+                for (int i = max(0, j - ST); i < j; i++) wait(k_full(i % ST), (uint32_t)(i / ST) & 1), wait(v_full(i % ST), (uint32_t)(i / ST) & 1);
+            }
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && nt) {
+            bool ok = wait(q_full, 0);
+            for (int j = 0; j <= nt && ok; j++) {
+                if (j < nt) {  // S(j), dP(j)
+                    const int s = j % ST;
+                    const uint32_t ph = (uint32_t)(j / ST) & 1;
+                    if (j && !(ok = wait(sp_free, (uint32_t)(j - 1) & 1))) break;
+                    if (!(ok = wait(k_full(s), ph) && wait(v_full(s), ph))) break;
+                    tc_fence_after();
 #pragma unroll
-    for (int i = 0; i < 4; i++) dk[i] *= a.scale;
-    if (4 * lane < a.dh) {
-        store4(static_cast<T *>(a.dk.p) + row * a.dk.ld + hk * a.dk.hd + 4 * lane, dk);
-        store4(static_cast<T *>(a.dv.p) + row * a.dv.ld + hk * a.dv.hd + 4 * lane, dv);
+                    for (int k = 0; k < DH / 16; k++) mma_f16(tS, sq_k(sm, k), sq_k(sm + L::OFF_K + s * L::TILE, k), sq_idesc(128, BF, false), k > 0);
+#pragma unroll
+                    for (int k = 0; k < DH / 16; k++)
+                        mma_f16(tP, sq_k(sm + L::OFF_G, k), sq_k(sm + L::OFF_V + s * L::TILE, k), sq_idesc(128, BF, false), k > 0);
+                    mma_commit(v_free(s));
+                    mma_commit(sp_full);
+                }
+                if (j > 0) {  // dQ(j - 1)
+                    const int i = j - 1, s = i % ST;
+                    if (!(ok = wait(ds_full, (uint32_t)i & 1))) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 0; k < SQ_ROWS / 16; k++)
+                        mma_f16_ta(tO, tD + 8 * k, sq_mn(sm + L::OFF_K + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(i | k));
+                    mma_commit(k_free(s));
+                    mma_commit(ds_free);
+                }
+            }
+            mma_commit(dq_full);
+            wait(dq_full, 0);
+        }
+        pdl_allow_next();
+    } else {
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const long at_row = (long)h * a.q_rows + row;
+        // D: each of a row's two threads takes half of the head
+        float dot = 0.0f;
+        if (in) {
+            const int c0 = half * (DH / 2), n = min(DH / 2, a.dh - c0);
+            if (n > 0)
+                dot = row_dot(static_cast<const T *>(a.o.p) + row * a.o.ld + h * a.o.hd + c0, static_cast<const T *>(a.g.p) + row * a.g.ld + h * a.g.hd + c0,
+                              n);
+        }
+        part[half][rt] = dot;
+        elements_sync();
+        const float D = part[0][rt] + part[1][rt];
+        if (in && half == 0) delta[at_row] = D;
+        const bool none = keys.hi <= keys.lo;
+        const float lse2 = none ? 0.0f : a.lse[at_row] * LOG2E;
+        const unsigned long long c2 = f4_two(c, c), l2 = f4_two(-lse2, -lse2), d2 = f4_two(-D, -D);
+        bool ok = true;
+        for (int j = 0; j < nt; j++) {
+            if (!(ok = wait(sp_full, (uint32_t)j & 1))) break;
+            tc_fence_after();
+            uint32_t s[2][32], p[2][32];
+            tmem_ld32(tS + lanes + 64 * half, s[0]);
+            tmem_ld32(tS + lanes + 64 * half + 32, s[1]);
+            tmem_ld32(tP + lanes + 64 * half, p[0]);
+            tmem_ld32(tP + lanes + 64 * half + 32, p[1]);
+            tmem_wait_ld();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sp_free);
+            const int at = end - SQ_ROWS * (j + 1) + 64 * half, lo = keys.lo - at, hi = keys.hi - at;
+            const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= 64);
+            if (j && !(ok = wait(ds_free, (uint32_t)(j - 1) & 1))) break;
+#pragma unroll
+            for (int b = 0; b < 2; b++) {
+                const uint32_t see = all ? 0xFFFFFFFFu : sq_bits(lo - 32 * b, hi - 32 * b);
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    float x, y, u, v;
+                    f4_untwo(sq_fma2(f4_two(__uint_as_float(s[b][2 * i]), __uint_as_float(s[b][2 * i + 1])), c2, l2), x, y);
+                    const unsigned long long t = f4_add2(f4_two(__uint_as_float(p[b][2 * i]), __uint_as_float(p[b][2 * i + 1])), d2);
+                    f4_untwo(f4_mul2(f4_two(exp2_fast(x), exp2_fast(y)), t), u, v);
+                    if (!all) u = (see >> (2 * i)) & 1u ? u : 0.0f, v = (see >> (2 * i + 1)) & 1u ? v : 0.0f;
+                    w[i] = sq_pack<BF>(u, v);
+                }
+                tmem_st16(tD + lanes + 32 * half + 16 * b, w);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_full);
+        }
+        if (nt) ok = wait(dq_full, 0) && ok;
+        tc_fence_after();
+        bool odd = false;
+        if (ok) {
+            T *o = static_cast<T *>(a.dq.p) + row * a.dq.ld + h * a.dq.hd;
+#pragma unroll
+            for (int b = 0; b < DH / 64; b++) {
+                const int c0 = half * (DH / 2) + 32 * b;
+                uint32_t w[32];
+                float v[32];
+                if (nt) tmem_ld32(tO + lanes + c0, w);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; i++) {
+                    const float x = nt && !none ? __uint_as_float(w[i]) : 0.0f;
+                    odd |= !(fabsf(x) < INFINITY);
+                    v[i] = x * a.scale;
+                }
+                if (in) sq_store<BF>(o, c0, a.dh, v);
+            }
+        }
+        odd_rows[half][rt] = odd;
+        elements_sync();
+        odd = ok && in && (odd_rows[0][rt] || odd_rows[1][rt]);
+        // the rows of a warp and its partner by turns
+        for (uint32_t again = __ballot_sync(0xFFFFFFFFu, odd && (rt & 1) == half); again; again &= again - 1) {
+            const int src = __ffs(again) - 1, rr = __shfl_sync(0xFFFFFFFFu, row, src);
+            const Span sp{__shfl_sync(0xFFFFFFFFu, keys.lo, src), __shfl_sync(0xFFFFFFFFu, keys.hi, src)};
+            const float4 d = attn_row_dq(static_cast<const T *>(a.q.p) + rr * a.q.ld + h * a.q.hd, static_cast<const T *>(a.g.p) + rr * a.g.ld + h * a.g.hd,
+                                         __shfl_sync(0xFFFFFFFFu, lse2, src), __shfl_sync(0xFFFFFFFFu, D, src), static_cast<const T *>(a.k.p) + hk * a.k.hd,
+                                         a.k.ld, static_cast<const T *>(a.v.p) + hk * a.v.hd, a.v.ld, sp, a.dh, c);
+            const float v[4] = {d.x * a.scale, d.y * a.scale, d.z * a.scale, d.w * a.scale};
+            if (4 * lane < a.dh) store4(static_cast<T *>(a.dq.p) + rr * a.dq.ld + h * a.dq.hd + 4 * lane, v);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) tmem_free<512>(tslot);
+}
+
+// --------------------------------------------------------------------------- dk, dv
+template <int DH>
+struct DkvLayout {
+    static constexpr int STAGES = DH == 64 ? 3 : 2, TILE = sq_bytes<DH>();
+    // K and V, stages of Q and G, stages of -lse log2 e and -D of 128 queries
+    static constexpr int OFF_V = TILE, OFF_Q = 2 * TILE, OFF_G = OFF_Q + STAGES * TILE, OFF_N = OFF_G + STAGES * TILE, SMEM = OFF_N + STAGES * 1024 + 1024;
+    static constexpr int T_DP = 128, T_DV = 256, T_DK = 256 + DH;
+};
+
+template <int DH, bool BF>
+__global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
+                                                                     const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
+                                                                     const SeqAttn a, const float c, const float *delta) {
+    using L = DkvLayout<DH>;
+    using T = std::conditional_t<BF, __nv_bfloat16, __half>;
+    constexpr int ST = L::STAGES;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[4 * ST + 6];
+    __shared__ uint32_t tslot;
+    __shared__ int failed, span[2][4];
+    __shared__ uint8_t odd_rows[2][SQ_ROWS];
+    const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
+    uint8_t *smp = raw + (sm - s_addr(raw));
+    const auto q_full = [&](int s) { return bar0 + 8 * s; };
+    const auto q_free = [&](int s) { return bar0 + 8 * (ST + s); };
+    const auto g_full = [&](int s) { return bar0 + 8 * (2 * ST + s); };
+    const auto g_free = [&](int s) { return bar0 + 8 * (3 * ST + s); };
+    const uint32_t kv_full = bar0 + 8 * (4 * ST), s_full = kv_full + 8, dp_full = kv_full + 16, p_full = kv_full + 24, ds_full = kv_full + 32,
+                   out_full = kv_full + 40;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int hk = blockIdx.x % a.hkv, tile = (int)(blockIdx.x / a.hkv);
+    const int h0 = hk * a.group(), heads = a.group();
+    const int half = warp >> 2, rt = (int)threadIdx.x & 127, row = tile * SQ_ROWS + rt;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < ST; s++) mbar_init(q_full(s), 2), mbar_init(q_free(s), 1), mbar_init(g_full(s), 1), mbar_init(g_free(s), 1);
+        mbar_init(kv_full, 2), mbar_init(s_full, 1), mbar_init(dp_full, 1), mbar_init(p_full, 8), mbar_init(ds_full, 8), mbar_init(out_full, 1);
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) tmem_alloc<512>(s_addr(&tslot));
+    pdl_grid_wait();
+    Span qs{0, 0};
+    bool in = false;
+    if (warp < 8) {
+        qs = queries_of_key(a, row, in);
+        const bool some = qs.hi > qs.lo;
+        const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? qs.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? qs.hi : 0);
+        if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tS = tslot, tP = tS + L::T_DP, tV = tS + L::T_DV, tK = tS + L::T_DK;
+    const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
+    const int nt = end > first ? (end - first + SQ_ROWS - 1) / SQ_ROWS : 0, n = nt * heads;  // tiles of one head, of all
+    const SqWaits wait{&failed, a.status};
+
+    if (warp == 8) {
+        if (nt) {
+            if (lane == 0) {
+                sq_load<DH>(sm, &tk, hk, tile * SQ_ROWS, kv_full);
+                sq_load<DH>(sm + L::OFF_V, &tv, hk, tile * SQ_ROWS, kv_full);
+            }
+            int j = 0, h = h0, t = 0;
+            bool ok = true;
+            for (; j < n; j++) {
+                const int s = j % ST, at = end - SQ_ROWS * (t + 1);
+                const uint32_t ph = (uint32_t)(j / ST - 1) & 1;
+                if (j >= ST) ok = wait(q_free(s), ph);
+                if (!__all_sync(0xFFFFFFFFu, ok)) break;
+                if (lane == 0) sq_load<DH>(sm + L::OFF_Q + s * L::TILE, &tq, h, at, q_full(s));
+                // -lse log2 e and -D of the tile's queries
+                float *num = reinterpret_cast<float *>(smp + L::OFF_N + s * 1024);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int r = at + 32 * i + lane;
+                    const bool on = r >= 0 && r < a.q_rows;
+                    num[32 * i + lane] = on ? -LOG2E * __ldg(a.lse + (long)h * a.q_rows + r) : 0.0f;
+                    num[128 + 32 * i + lane] = on ? -delta[(long)h * a.q_rows + r] : 0.0f;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_full(s));
+                if (j >= ST) ok = wait(g_free(s), ph);
+                if (!__all_sync(0xFFFFFFFFu, ok)) {
+                    wait(q_full(s), (uint32_t)(j / ST) & 1);  // in flight
+                    break;
+                }
+                if (lane == 0) sq_load<DH>(sm + L::OFF_G + s * L::TILE, &tg, h, at, g_full(s));
+                if (++t == nt) t = 0, h++;
+            }
+            if (failed) {  // copies in flight land before the block ends
+                wait(kv_full, 0);
+                for (int i = max(0, j - ST); i < j; i++) wait(q_full(i % ST), (uint32_t)(i / ST) & 1), wait(g_full(i % ST), (uint32_t)(i / ST) & 1);
+            }
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && nt) {
+            bool ok = wait(kv_full, 0);
+            const auto scores = [&](int j) {  // S^T(j)
+                const int s = j % ST;
+                if (!wait(q_full(s), (uint32_t)(j / ST) & 1)) return false;
+                tc_fence_after();
+#pragma unroll
+                for (int k = 0; k < DH / 16; k++) mma_f16(tS, sq_k(sm, k), sq_k(sm + L::OFF_Q + s * L::TILE, k), sq_idesc(128, BF, false), k > 0);
+                mma_commit(s_full);
+                return true;
+            };
+            const auto weights = [&](int j) {  // dP^T(j)
+                const int s = j % ST;
+                if (!wait(g_full(s), (uint32_t)(j / ST) & 1)) return false;
+                tc_fence_after();
+#pragma unroll
+                for (int k = 0; k < DH / 16; k++)
+                    mma_f16(tP, sq_k(sm + L::OFF_V, k), sq_k(sm + L::OFF_G + s * L::TILE, k), sq_idesc(128, BF, false), k > 0);
+                mma_commit(dp_full);
+                return true;
+            };
+            ok = ok && scores(0) && weights(0);
+            for (int j = 0; j < n && ok; j++) {
+                const int s = j % ST;
+                if (!(ok = wait(p_full, (uint32_t)j & 1))) break;
+                tc_fence_after();
+#pragma unroll
+                for (int k = 0; k < SQ_ROWS / 16; k++)  // a row's two threads write 32 columns each, 64 apart
+                    mma_f16_ta(tV, tS + 8 * (k & 3) + 64 * (k >> 2), sq_mn(sm + L::OFF_G + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                mma_commit(g_free(s));
+                if (j + 1 < n && !(ok = scores(j + 1))) break;
+                if (!(ok = wait(ds_full, (uint32_t)j & 1))) break;
+                tc_fence_after();
+#pragma unroll
+                for (int k = 0; k < SQ_ROWS / 16; k++)
+                    mma_f16_ta(tK, tP + 8 * (k & 3) + 64 * (k >> 2), sq_mn(sm + L::OFF_Q + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                mma_commit(q_free(s));
+                if (j + 1 < n && !(ok = weights(j + 1))) break;
+            }
+            mma_commit(out_full);
+            wait(out_full, 0);
+        }
+        pdl_allow_next();
+    } else {
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const unsigned long long c2 = f4_two(c, c);
+        bool ok = true;
+        for (int j = 0, t = 0; j < n; j++) {
+            const int s = j % ST, at = end - SQ_ROWS * (t + 1) + 64 * half, lo = qs.lo - at, hi = qs.hi - at;
+            if (++t == nt) t = 0;
+            const float4 *num = reinterpret_cast<const float4 *>(smp + L::OFF_N + s * 1024) + 16 * half;
+            const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= 64);
+            const uint32_t see[2] = {all ? 0xFFFFFFFFu : sq_bits(lo, hi), all ? 0xFFFFFFFFu : sq_bits(lo - 32, hi - 32)};
+            // the producer's numbers are visible with the tile that they came with
+            if (!(ok = wait(s_full, (uint32_t)j & 1) && wait(q_full(s), (uint32_t)(j / ST) & 1))) break;
+            tc_fence_after();
+            uint32_t r[2][32];
+            load64(tS + lanes + 64 * half, r);
+#pragma unroll
+            for (int b = 0; b < 2; b++) {
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float4 x = num[8 * b + i];
+                    float p[4];
+                    f4_untwo(sq_fma2(f4_two(__uint_as_float(r[b][4 * i]), __uint_as_float(r[b][4 * i + 1])), c2, f4_two(x.x, x.y)), p[0], p[1]);
+                    f4_untwo(sq_fma2(f4_two(__uint_as_float(r[b][4 * i + 2]), __uint_as_float(r[b][4 * i + 3])), c2, f4_two(x.z, x.w)), p[2], p[3]);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        p[e] = exp2_fast(p[e]);
+                        if (!all) p[e] = (see[b] >> (4 * i + e)) & 1u ? p[e] : 0.0f;
+                        r[b][4 * i + e] = __float_as_uint(p[e]);
+                    }
+                    w[2 * i] = sq_pack<BF>(p[0], p[1]), w[2 * i + 1] = sq_pack<BF>(p[2], p[3]);
+                }
+                tmem_st16(tS + lanes + 64 * half + 16 * b, w);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full);
+            if (!(ok = wait(dp_full, (uint32_t)j & 1))) break;
+            tc_fence_after();
+            uint32_t q[2][32];
+            load64(tP + lanes + 64 * half, q);
+#pragma unroll
+            for (int b = 0; b < 2; b++) {
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float4 x = num[32 + 8 * b + i];
+                    float d[4];
+                    f4_untwo(f4_mul2(f4_two(__uint_as_float(r[b][4 * i]), __uint_as_float(r[b][4 * i + 1])),
+                                     f4_add2(f4_two(__uint_as_float(q[b][4 * i]), __uint_as_float(q[b][4 * i + 1])), f4_two(x.x, x.y))),
+                             d[0], d[1]);
+                    f4_untwo(f4_mul2(f4_two(__uint_as_float(r[b][4 * i + 2]), __uint_as_float(r[b][4 * i + 3])),
+                                     f4_add2(f4_two(__uint_as_float(q[b][4 * i + 2]), __uint_as_float(q[b][4 * i + 3])), f4_two(x.z, x.w))),
+                             d[2], d[3]);
+                    if (!all) {
+#pragma unroll
+                        for (int e = 0; e < 4; e++) d[e] = (see[b] >> (4 * i + e)) & 1u ? d[e] : 0.0f;
+                    }
+                    w[2 * i] = sq_pack<BF>(d[0], d[1]), w[2 * i + 1] = sq_pack<BF>(d[2], d[3]);
+                }
+                tmem_st16(tP + lanes + 64 * half + 16 * b, w);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_full);
+        }
+        if (nt) ok = wait(out_full, 0) && ok;
+        tc_fence_after();
+        // a row's two threads: dv, dk
+        bool odd = false;
+        if (ok) {
+            const HeadRows &x = half ? a.dk : a.dv;
+            const float f = half ? a.scale : 1.0f;
+            T *o = static_cast<T *>(x.p) + row * x.ld + hk * x.hd;
+#pragma unroll
+            for (int b = 0; b < DH / 32; b++) {
+                uint32_t w[32];
+                float v[32];
+                if (nt) tmem_ld32((half ? tK : tV) + lanes + 32 * b, w);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; i++) {
+                    const float y = nt && qs.hi > qs.lo ? __uint_as_float(w[i]) : 0.0f;
+                    odd |= !(fabsf(y) < INFINITY);
+                    v[i] = y * f;
+                }
+                if (in) sq_store<BF>(o, 32 * b, a.dh, v);
+            }
+        }
+        odd_rows[half][rt] = odd;
+        elements_sync();
+        odd = ok && in && (odd_rows[0][rt] || odd_rows[1][rt]);
+        for (uint32_t again = __ballot_sync(0xFFFFFFFFu, odd && (rt & 1) == half); again; again &= again - 1) {
+            const int src = __ffs(again) - 1, rr = __shfl_sync(0xFFFFFFFFu, row, src);
+            const Span sp{__shfl_sync(0xFFFFFFFFu, qs.lo, src), __shfl_sync(0xFFFFFFFFu, qs.hi, src)};
+            float dk[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int h = h0; h < h0 + heads; h++)
+                attn_row_dkv(static_cast<const T *>(a.k.p) + rr * a.k.ld + hk * a.k.hd, static_cast<const T *>(a.v.p) + rr * a.v.ld + hk * a.v.hd,
+                             static_cast<const T *>(a.q.p) + h * a.q.hd, a.q.ld, static_cast<const T *>(a.g.p) + h * a.g.hd, a.g.ld,
+                             a.lse + (long)h * a.q_rows, delta + (long)h * a.q_rows, sp, a.dh, c, dk, dv);
+#pragma unroll
+            for (int i = 0; i < 4; i++) dk[i] *= a.scale;
+            if (4 * lane < a.dh) {
+                store4(static_cast<T *>(a.dk.p) + rr * a.dk.ld + hk * a.dk.hd + 4 * lane, dk);
+                store4(static_cast<T *>(a.dv.p) + rr * a.dv.ld + hk * a.dv.hd + 4 * lane, dv);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) tmem_free<512>(tslot);
+}
+
+// Where there are no queries or no keys at all, gradients of rows in sequences are zero.
+template <typename T>
+__global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
+    pdl_grid_wait();
+    const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 5;
+    const int lane = threadIdx.x & 31;
+    const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    bool in;
+    if (a.k_rows == 0) {
+        if (w >= a.q_rows) return;
+        keys_of_query(a, (int)w, in);
+        for (int h = 0; in && 4 * lane < a.dh && h < a.hq; h++) store4(static_cast<T *>(a.dq.p) + w * a.dq.ld + h * a.dq.hd + 4 * lane, z);
+    } else {
+        if (w >= a.k_rows) return;
+        queries_of_key(a, (int)w, in);
+        for (int h = 0; in && 4 * lane < a.dh && h < a.hkv; h++) {
+            store4(static_cast<T *>(a.dk.p) + w * a.dk.ld + h * a.dk.hd + 4 * lane, z);
+            store4(static_cast<T *>(a.dv.p) + w * a.dv.ld + h * a.dv.hd + 4 * lane, z);
+        }
     }
 }
 
-template <typename T>
-cudaError_t backward(const SeqAttn &a, cudaStream_t st) {
+template <int DH, bool BF>
+cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
+    CUtensorMap tq, tk, tv, tg;
+    if (!sq_map(&tq, a.q, a.q_rows, a.hq, a.dh) || !sq_map(&tg, a.g, a.q_rows, a.hq, a.dh) || !sq_map(&tk, a.k, a.k_rows, a.hkv, a.dh) ||
+        !sq_map(&tv, a.v, a.k_rows, a.hkv, a.dh))
+        return cudaErrorInvalidValue;
     float *delta = static_cast<float *>(a.workspace);
     const float c = a.scale * LOG2E;
-    const long q = (long)a.q_rows * a.hq, k = (long)a.k_rows * a.hkv;
-    if (q) {
-        launch_pdl(seq_attn_delta_kernel<T>, (unsigned)((q + 255) / 256), 256, 0, st, a, delta);
-        launch_pdl(seq_attn_dq_rows_kernel<T>, (unsigned)((q + 7) / 8), 256, 0, st, a, c, (const float *)delta);
-    }
-    if (k) launch_pdl(seq_attn_dkv_rows_kernel<T>, (unsigned)((k + 7) / 8), 256, 0, st, a, c, (const float *)delta);
-    return cudaGetLastError();
+    const unsigned qt = (unsigned)((a.q_rows + SQ_ROWS - 1) / SQ_ROWS), kt = (unsigned)((a.k_rows + SQ_ROWS - 1) / SQ_ROWS);
+    const cudaError_t e = launch_pdl(seq_attn_dq_kernel<DH, BF>, qt * a.hq, BW_THREADS, DqLayout<DH>::SMEM, st, tq, tg, tk, tv, a, c, delta);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(seq_attn_dkv_kernel<DH, BF>, kt * a.hkv, BW_THREADS, DkvLayout<DH>::SMEM, st, tk, tv, tq, tg, a, c, (const float *)delta);
+}
+
+template <int DH, bool BF>
+cudaError_t tile_init() {
+    const cudaError_t e = cudaFuncSetAttribute(seq_attn_dq_kernel<DH, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<DH>::SMEM);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(seq_attn_dkv_kernel<DH, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, DkvLayout<DH>::SMEM);
 }
 
 }  // namespace
 
+cudaError_t seq_attn_backward_init() {
+    cudaError_t e = tile_init<64, true>();
+    if (e == cudaSuccess) e = tile_init<64, false>();
+    if (e == cudaSuccess) e = tile_init<128, true>();
+    if (e == cudaSuccess) e = tile_init<128, false>();
+    return e;
+}
+
 size_t seq_attn_backward_workspace(const SeqAttn &a) { return ((size_t)a.hq * a.q_rows * 4 + 31) / 16 * 16; }
 
 cudaError_t launch_seq_attn_backward(const SeqAttn &a, cudaStream_t st) {
-    return a.dtype == MNMT_BF16 ? backward<__nv_bfloat16>(a, st) : backward<__half>(a, st);
+    const bool bf = a.dtype == MNMT_BF16;
+    if (a.q_rows == 0 || a.k_rows == 0)
+        return launch_pdl(bf ? seq_attn_zero_kernel<__nv_bfloat16> : seq_attn_zero_kernel<__half>, (unsigned)((a.q_rows + a.k_rows + 7) / 8), 256, 0, st, a);
+    if (a.dh <= 64) return bf ? tile_backward<64, true>(a, st) : tile_backward<64, false>(a, st);
+    return bf ? tile_backward<128, true>(a, st) : tile_backward<128, false>(a, st);
 }
 
 }  // namespace mnmt

@@ -62,7 +62,8 @@ struct SeqAttn {
     int *status;
     __host__ __device__ int group() const { return hq / hkv; }
 };
-cudaError_t seq_attn_init();  // set-up of its kernels on the current device
+cudaError_t seq_attn_init();  // set-up of the kernels on the current device
+cudaError_t seq_attn_backward_init();
 size_t seq_attn_forward_workspace(const SeqAttn &a);
 size_t seq_attn_backward_workspace(const SeqAttn &a);
 size_t seq_attn_token_workspace(const SeqAttn &a);
