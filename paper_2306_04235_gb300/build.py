@@ -20,7 +20,7 @@ OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libmnmt.so")
 SOURCES = ["api.cu", "linear.cu", "linear_w4.cu", "gemm_tc.cu", "attention.cu", "rows.cu", "decode_cluster.cu",
            "decode_rows.cu", "noalloc.cu", "fakequant.cu", "fp4.cu", "fp4_backward.cu", "fp4_tc.cu", "fp4_small.cu",
-           "fp4_api.cu", "dropout.cu", "seq_attn.cu", "seq_attn_backward.cu", "seq_api.cu", "embed_rows.cu"]
+           "fp4_api.cu", "dropout.cu", "seq_attn.cu", "seq_attn_backward.cu", "seq_attn_token.cu", "seq_api.cu", "embed_rows.cu"]
 HEADERS = ["attn_core.cuh", "common.cuh", "decode_rows.h", "epilogue.cuh", "fp4.cuh", "fp4_tile.cuh", "internal.h",
            "mbarrier.cuh", "routes.h", "row_pass.cuh", "seq_attn.cuh", "seq_tile.cuh", "tcgen05.cuh", "train.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

@@ -45,6 +45,7 @@ int seq_ready() {
     if (!ready[dev]) {
         cudaError_t e = seq_attn_init();
         if (e == cudaSuccess) e = seq_attn_backward_init();
+        if (e == cudaSuccess) e = seq_attn_token_init();
         if (e != cudaSuccess) return fail(MNMT_ECUDA, "attention kernel set-up failed: %s", cudaGetErrorString(e));
         ready[dev] = true;
     }

@@ -64,6 +64,7 @@ struct SeqAttn {
 };
 cudaError_t seq_attn_init();  // set-up of the kernels on the current device
 cudaError_t seq_attn_backward_init();
+cudaError_t seq_attn_token_init();
 size_t seq_attn_forward_workspace(const SeqAttn &a);
 size_t seq_attn_backward_workspace(const SeqAttn &a);
 size_t seq_attn_token_workspace(const SeqAttn &a);
