@@ -40,35 +40,337 @@ __global__ void __launch_bounds__(256, ROW_BLOCKS) embed_rows_kernel(EmbedRowsAr
     }
 }
 
-// A warp per row of the table: all tokens that name it, in their order.
-template <typename T, typename O>
-__global__ void __launch_bounds__(256) embed_rows_backward_kernel(EmbedRowsArgs a) {
-    pdl_grid_wait();
-    const int lane = threadIdx.x & 31;
-    const long id = ((long)blockIdx.x * 256 + threadIdx.x) >> 5;
-    if (id == 0 && a.status)
-        for (int t = lane; t < a.T; t += 32)
-            if (a.ids[t] < 0 || a.ids[t] >= a.V) set_status(a.status, MNMT_EINVAL);
-    if (id >= a.V) return;
-    O *out = static_cast<O *>(a.out) + id * a.ldo;
-    const T *g = static_cast<const T *>(a.table);
-    for (int c0 = 0; c0 < a.d; c0 += 256) {
-        float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        for (int t0 = 0; t0 < a.T; t0 += 32) {
-            uint32_t m = __ballot_sync(0xFFFFFFFFu, t0 + lane < a.T && a.ids[t0 + lane] == id && id != a.pad_id);
-            for (; m; m &= m - 1) {
-                const T *row = g + (t0 + __ffs(m) - 1) * a.ld;
+// --------------------------------------------------------------------------- the table's gradient
+constexpr int EB_COLS = 256;  // columns of a warp: eight a lane
+
+// A lane's eight of the warp's columns from c0 on: side by side where rows are 16-byte
+// aligned (VEC), else 32 apart, so that lanes next to each other load what is.
+template <bool VEC>
+struct LaneCols {
+    int c0, d;
+    MNMT_DEV int at(int k) const { return VEC ? c0 + 8 * (threadIdx.x & 31) + k : c0 + 32 * k + (threadIdx.x & 31); }
+    template <typename T>
+    MNMT_DEV void load(const T *row, float (&v)[8]) const {
+        if (VEC && at(0) + 8 <= d) {
+            load8<T, true>(row + at(0), 8, v);
+        } else {
 #pragma unroll
-                for (int k = 0; k < 8; k++)
-                    if (c0 + 32 * k + lane < a.d) s[k] += to_f32(row[c0 + 32 * k + lane]);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < 8; k++) {
-            const int c = c0 + 32 * k + lane;
-            if (c < a.d) out[c] = from_f32<O>(__fadd_rn(a.accumulate ? to_f32(out[c]) : 0.0f, __fmul_rn(s[k], a.scale)));
+            for (int k = 0; k < 8; k++) v[k] = at(k) < d ? to_f32(row[at(k)]) : 0.0f;
         }
     }
+    template <typename O>
+    MNMT_DEV void store(O *row, const float (&v)[8]) const {
+        if (VEC && at(0) + 8 <= d) {
+            store8<O, true>(row + at(0), 8, v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                if (at(k) < d) row[at(k)] = from_f32<O>(v[k]);
+        }
+    }
+    // the row of a token's gradient from the sum of its g
+    template <typename O>
+    MNMT_DEV void finish(O *row, float (&s)[8], float scale, bool accumulate) const {
+        float old[8];
+        if (accumulate) load(row, old);
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            s[k] = __fmul_rn(s[k], scale);
+            if (accumulate) s[k] = __fadd_rn(old[k], s[k]);
+        }
+        store(row, s);
+    }
+};
+
+// s += the rows of g that lanes of `mask` hold the numbers of, in lane order, several in flight
+template <typename T, bool VEC>
+MNMT_DEV void add_rows(const T *g, long ld, int t, uint32_t mask, const LaneCols<VEC> &cols, float (&s)[8]) {
+    constexpr int N = 8;
+    while (mask) {
+        float v[N][8];
+        bool on[N];
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            on[i] = mask != 0;
+            const int row = __shfl_sync(0xFFFFFFFFu, t, on[i] ? __ffs(mask) - 1 : 0);
+            if (on[i]) cols.load(g + row * ld, v[i]);
+            mask &= mask - 1;
+        }
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            if (on[i]) {
+#pragma unroll
+                for (int k = 0; k < 8; k++) s[k] += v[i][k];
+            }
+    }
+}
+
+// Few tokens, one launch.  Block (x, y) has the rows of the table that are x modulo the
+// number of row sets (frequent tokens have low numbers: they spread over the blocks) and
+// 256 columns.  Each warp looks through its eighth of the tokens and lists those of the
+// block's rows; rows that many tokens name are added up by all warps, each over its own
+// list, the others by a warp each over all lists: in the tokens' order both.
+constexpr int EF_TOKENS = 4096, EF_ROWS = 4096;  // at most: tokens, rows of a block
+constexpr int EF_MANY = 32;                      // tokens of a row from which all warps work on it
+template <typename T, typename O, bool VEC>
+__global__ void __launch_bounds__(256) embed_few_kernel(EmbedRowsArgs a) {
+    __shared__ uint16_t list[EF_TOKENS], slot[EF_TOKENS];
+    __shared__ uint32_t count[EF_ROWS / 2];  // of two rows each
+    __shared__ int found[8], many[EF_TOKENS / EF_MANY + 1], n_many;
+    __shared__ float part[8][EB_COLS];
+    pdl_grid_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sets = gridDim.x, x = blockIdx.x;
+    const int rows = (a.V - x + sets - 1) / sets;
+    const LaneCols<VEC> cols{(int)blockIdx.y * EB_COLS, a.d};
+    const T *g = static_cast<const T *>(a.table);
+    O *out = static_cast<O *>(a.out);
+    for (int i = threadIdx.x; i < (rows + 1) / 2; i += 256) count[i] = 0;
+    if (threadIdx.x == 0) n_many = 0;
+    __syncthreads();
+    const int per = (a.T + 7) / 8, t0 = warp * per, t1 = min(a.T, t0 + per);
+    int n = 0;
+    for (int t = t0; t < t1; t += 32) {
+        const int id = t + lane < t1 ? a.ids[t + lane] : -1;
+        const bool bad = t + lane < t1 && (id < 0 || id >= a.V);
+        if (bad && x == 0 && blockIdx.y == 0) set_status(a.status, MNMT_EINVAL);
+        const bool mine = id >= 0 && id < a.V && id != a.pad_id && id % sets == x;
+        const uint32_t m = __ballot_sync(0xFFFFFFFFu, mine);
+        if (mine) {
+            const int at = t0 + n + __popc(m & ((1u << lane) - 1u)), r = id / sets;
+            list[at] = (uint16_t)(t + lane), slot[at] = (uint16_t)r;
+            atomicAdd(&count[r >> 1], r & 1 ? 65536u : 1u);
+        }
+        n += __popc(m);
+    }
+    if (lane == 0) found[warp] = n;
+    __syncthreads();
+    const auto of = [&](int r) { return (count[r >> 1] >> (r & 1 ? 16 : 0)) & 0xFFFFu; };
+    // a warp's list: s += its tokens of row r
+    const auto add_list = [&](int w, int r, float(&s)[8]) {
+        const int first = w * per, end = first + found[w];
+        for (int i = first; i < end; i += 32) {
+            const bool on = i + lane < end && slot[i + lane] == r;
+            add_rows<T, VEC>(g, a.ld, on ? list[i + lane] : 0, __ballot_sync(0xFFFFFFFFu, on), cols, s);
+        }
+    };
+    for (int r = warp; r < rows; r += 8) {
+        const int c = of(r);
+        if (c >= EF_MANY) {
+            if (lane == 0) many[atomicAdd(&n_many, 1)] = r;  // in any order: each row's sum is its own
+        } else if (c || !a.accumulate) {
+            float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (c)
+                for (int w = 0; w < 8; w++) add_list(w, r, s);
+            cols.finish(out + ((long)r * sets + x) * a.ldo, s, a.scale, a.accumulate);
+        }
+    }
+    __syncthreads();
+    for (int i = 0; i < n_many; i++) {
+        float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        add_list(warp, many[i], s);
+#pragma unroll
+        for (int k = 0; k < 8; k++) part[warp][32 * k + lane] = s[k];
+        __syncthreads();
+        if (warp == 0) {
+            for (int w = 1; w < 8; w++)
+#pragma unroll
+                for (int k = 0; k < 8; k++) s[k] += part[w][32 * k + lane];
+            cols.finish(out + ((long)many[i] * sets + x) * a.ldo, s, a.scale, a.accumulate);
+        }
+        __syncthreads();
+    }
+}
+
+// Many tokens: sorted by their number (stable), in chunks of 32 a warp adds up; rows
+// whose tokens lie in several chunks are joined from the chunks' sums.
+struct SortBufs {
+    int *key[2], *idx[2];
+};
+
+// Stable sort of the tokens by one cluster, eight bits a pass: counts per warp, an
+// exclusive sum over (digit, CTA, warp), then every token to its place.  Tokens
+// without a gradient take the number V, behind all others.
+constexpr int ES_THREADS = 1024, ES_WARPS = 32, ES_CLUSTER = 8;
+MNMT_DEV void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__global__ void __launch_bounds__(ES_THREADS) embed_sort_kernel(const int *ids, int T, int V, int pad_id, int passes, SortBufs b, int *status) {
+    __shared__ int cnt[ES_WARPS][256], tot[256], base[256], wsum[8];
+    pdl_grid_wait();
+    pdl_allow_next();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = threadIdx.x;
+    const int ctas = gridDim.x, rank = blockIdx.x;  // the grid is one cluster
+    const long per = ((long)T + ctas * ES_WARPS * 32 - 1) / (ctas * ES_WARPS * 32) * 32;  // tokens of a warp
+    const long first = (rank * ES_WARPS + warp) * per, end = min((long)T, first + per);
+    for (int pass = 0; pass < passes; pass++) {
+        const int *key = b.key[(pass & 1) ^ 1], *idx = b.idx[(pass & 1) ^ 1];
+        int *okey = b.key[pass & 1], *oidx = b.idx[pass & 1];
+        const auto load = [&](long t, bool report) {
+            if (pass) return t < end ? key[t] : 0;
+            const int id = t < end ? ids[t] : 0;
+            const bool bad = id < 0 || id >= V;
+            if (bad && report) set_status(status, MNMT_EINVAL);
+            return bad || id == pad_id ? V : id;
+        };
+        const int shift = 8 * pass;
+        for (int i = d; i < ES_WARPS * 256; i += ES_THREADS) cnt[i >> 8][i & 255] = 0;
+        __syncthreads();
+        for (long t = first; t < end; t += 32) {
+            const uint32_t live = __ballot_sync(0xFFFFFFFFu, t + lane < end);
+            const int dig = t + lane < end ? (load(t + lane, true) >> shift) & 255 : 256;
+            const uint32_t same = __match_any_sync(0xFFFFFFFFu, dig) & live;
+            if (dig < 256 && lane == __ffs(same) - 1) cnt[warp][dig] += __popc(same);
+            __syncwarp();
+        }
+        __syncthreads();
+        if (d < 256) {
+            int s = 0;
+            for (int w = 0; w < ES_WARPS; w++) {
+                const int c = cnt[w][d];
+                cnt[w][d] = s;
+                s += c;
+            }
+            tot[d] = s;
+        }
+        cluster_sync_all();
+        int before = 0, all = 0, x = 0;
+        if (d < 256) {
+            const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&tot[d]);
+            for (int c = 0; c < ctas; c++) {
+                uint32_t at;
+                int v;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(mine), "r"(c));
+                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+                if (c < rank) before += v;
+                all += v;
+            }
+            x = all;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+                if (lane >= o) x += y;
+            }
+            if (lane == 31) wsum[warp] = x;
+        }
+        __syncthreads();
+        if (d < 256) {
+            for (int w = 0; w < warp; w++) x += wsum[w];
+            base[d] = x - all + before;
+        }
+        __syncthreads();
+        for (long t = first; t < end; t += 32) {
+            const bool on = t + lane < end;
+            const uint32_t live = __ballot_sync(0xFFFFFFFFu, on);
+            const int k = load(t + lane, false), dig = on ? (k >> shift) & 255 : 256;
+            const uint32_t same = __match_any_sync(0xFFFFFFFFu, dig) & live;
+            if (on) {
+                const int to = base[dig] + cnt[warp][dig] + __popc(same & ((1u << lane) - 1u));
+                okey[to] = k, oidx[to] = pass ? idx[t + lane] : (int)(t + lane);
+            }
+            __syncwarp();
+            if (on && lane == __ffs(same) - 1) cnt[warp][dig] += __popc(same);
+            __syncwarp();
+        }
+        cluster_sync_all();  // every token is in its place, every CTA's counts have been read
+    }
+}
+
+// Rows that no token names are zero.  Needs the ids alone: runs beside the sort.
+constexpr int EZ_BITS = 1 << 17;
+template <typename O, bool VEC>
+__global__ void __launch_bounds__(512) embed_zero_kernel(EmbedRowsArgs a) {
+    __shared__ uint32_t named[EZ_BITS / 32];
+    pdl_allow_next();
+    const int warp = threadIdx.x >> 5;
+    const int per = (a.V + (int)gridDim.x - 1) / (int)gridDim.x, v0 = (int)min((long)a.V, (long)blockIdx.x * per), v1 = min(a.V, v0 + per);
+    O *out = static_cast<O *>(a.out);
+    const float z[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    for (int f = v0; f < v1; f += EZ_BITS) {
+        const int e = min(v1, f + EZ_BITS);
+        __syncthreads();
+        for (int i = threadIdx.x; i < (e - f + 31) / 32; i += 512) named[i] = 0;
+        __syncthreads();
+#pragma unroll 8
+        for (int t = threadIdx.x; t < a.T; t += 512) {
+            const int id = a.ids[t];
+            if (id >= f && id < e && id != a.pad_id) atomicOr(&named[(id - f) >> 5], 1u << ((id - f) & 31));
+        }
+        __syncthreads();
+        for (int v = f + warp; v < e; v += 16)
+            if (!((named[(v - f) >> 5] >> ((v - f) & 31)) & 1u))
+                for (LaneCols<VEC> cols{0, a.d}; cols.c0 < a.d; cols.c0 += EB_COLS) cols.store(out + (long)v * a.ldo, z);
+    }
+    pdl_grid_wait();  // the sort's end is this kernel's too
+}
+
+// A warp per chunk of 32 sorted tokens and 256 columns.  A row whose tokens all lie in
+// the chunk is finished here; the sum of one that came from the chunk before, or goes on
+// into the next, is left in slot 2 chunk (it starts at the chunk's first token) or + 1.
+template <typename T, typename O, bool VEC>
+__global__ void __launch_bounds__(256) embed_sum_kernel(EmbedRowsArgs a, const int *key, const int *idx, float *parts) {
+    pdl_grid_wait();
+    const int lane = threadIdx.x & 31, cb = (a.d + EB_COLS - 1) / EB_COLS;
+    const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 5, chunk = w / cb, p0 = 32 * chunk;
+    if (p0 >= a.T) return;
+    const LaneCols<VEC> cols{(int)(w % cb) * EB_COLS, a.d};
+    const bool on = p0 + lane < a.T;
+    const int k = on ? key[p0 + lane] : a.V, t = on ? idx[p0 + lane] : 0;
+    const int prev = p0 ? key[p0 - 1] : -1, next = p0 + 32 < a.T ? key[p0 + 32] : a.V;
+    const int left = __shfl_up_sync(0xFFFFFFFFu, k, 1);
+    uint32_t heads = __ballot_sync(0xFFFFFFFFu, lane == 0 || k != left);  // first tokens of rows
+    while (heads) {
+        const int i = __ffs(heads) - 1;
+        heads &= heads - 1;
+        const int j = heads ? __ffs(heads) - 1 : 32, v = __shfl_sync(0xFFFFFFFFu, k, i);
+        if (v >= a.V) break;
+        float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        add_rows<T, VEC>(static_cast<const T *>(a.table), a.ld, t, (j == 32 ? 0xFFFFFFFFu : (1u << j) - 1u) & ~((1u << i) - 1u), cols, s);
+        if ((i > 0 || prev != v) && (j < 32 || next != v)) {
+            cols.finish(static_cast<O *>(a.out) + (long)v * a.ldo, s, a.scale, a.accumulate);
+        } else {
+            float *p = parts + (2 * chunk + (i > 0)) * (long)(cb * EB_COLS) + cols.c0;
+            reinterpret_cast<float4 *>(p)[2 * lane] = make_float4(s[0], s[1], s[2], s[3]);
+            reinterpret_cast<float4 *>(p)[2 * lane + 1] = make_float4(s[4], s[5], s[6], s[7]);
+        }
+    }
+}
+
+// A block per chunk and 256 columns: the row that begins in the chunk and goes on into
+// the next ones, if there is one.  Each warp adds an eighth of its chunks.
+template <typename O, bool VEC>
+__global__ void __launch_bounds__(256) embed_join_kernel(EmbedRowsArgs a, const int *key, const float *parts) {
+    __shared__ float part[8][EB_COLS];
+    pdl_grid_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cb = (a.d + EB_COLS - 1) / EB_COLS;
+    const long chunk = blockIdx.x / cb, p0 = 32 * chunk;
+    if (p0 + 32 >= a.T) return;
+    const int v = key[p0 + 31];
+    if (v >= a.V || key[p0 + 32] != v) return;
+    const bool from_first = key[p0] == v;
+    if (from_first && p0 > 0 && key[p0 - 1] == v) return;  // it began before
+    const LaneCols<VEC> cols{(int)(blockIdx.x % cb) * EB_COLS, a.d};
+    long lo = p0 + 32, hi = a.T;  // past its last token
+    while (lo < hi) {
+        const long mid = (lo + hi) >> 1;
+        if (key[mid] <= v) lo = mid + 1;
+        else hi = mid;
+    }
+    const long last = (lo - 1) / 32, n = last - chunk + 1, per = (n + 7) / 8;
+    float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+    for (long c = chunk + warp * per; c <= min(last, chunk + (warp + 1) * per - 1); c++) {
+        const float4 *p = reinterpret_cast<const float4 *>(parts + (2 * c + (c == chunk && !from_first)) * (long)(cb * EB_COLS) + cols.c0);
+        const float4 x = p[2 * lane], y = p[2 * lane + 1];
+        s[0] += x.x, s[1] += x.y, s[2] += x.z, s[3] += x.w, s[4] += y.x, s[5] += y.y, s[6] += y.z, s[7] += y.w;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; k++) part[warp][32 * k + lane] = s[k];
+    __syncthreads();
+    if (warp) return;
+    for (int w = 1; w < 8; w++)
+#pragma unroll
+        for (int k = 0; k < 8; k++) s[k] += part[w][32 * k + lane];
+    cols.finish(static_cast<O *>(a.out) + (long)v * a.ldo, s, a.scale, a.accumulate);
 }
 
 template <typename F>
@@ -98,13 +400,64 @@ cudaError_t launch_embed_rows(const EmbedRowsArgs &a, cudaStream_t st) {
     return cudaGetLastError();
 }
 
-size_t embed_rows_backward_workspace(int, int, int) { return 16; }
+namespace {
+// row sets of embed_few_kernel: four blocks per SM over all columns, no more than rows
+int few_sets(int V, int d) {
+    const int cb = (d + EB_COLS - 1) / EB_COLS, sets = (4 * 152 + cb - 1) / cb;
+    return sets < V ? sets : V;
+}
+bool few_tokens(int T, int V, int d) { return T <= EF_TOKENS && (V + few_sets(V, d) - 1) / few_sets(V, d) <= EF_ROWS && (d + EB_COLS - 1) / EB_COLS <= 65535; }
+size_t sort_ints(int T) { return ((size_t)T + 3) / 4 * 4; }
+size_t sum_parts(int T, int d) { return 2 * (((size_t)T + 31) / 32) * ((size_t)(d + EB_COLS - 1) / EB_COLS * EB_COLS); }
+}  // namespace
+
+size_t embed_rows_backward_workspace(int T, int V, int d) { return few_tokens(T, V, d) ? 16 : 16 * sort_ints(T) + 4 * sum_parts(T, d); }
 
 cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &a, cudaStream_t st) {
+    cudaError_t err = cudaSuccess;
     by_types(a.dtype, a.otype, [&](auto t, auto o) {
-        launch_pdl(embed_rows_backward_kernel<decltype(t), decltype(o)>, (unsigned)((a.V + 7) / 8), 256, 0, st, a);
+        using T = decltype(t);
+        using O = decltype(o);
+        const bool vec = row_alignment(static_cast<const T *>(a.table), a.T ? a.ld : 0) && row_alignment(static_cast<const O *>(a.out), a.ldo);
+        const unsigned cb = (unsigned)((a.d + EB_COLS - 1) / EB_COLS);
+        if (few_tokens(a.T, a.V, a.d)) {
+            err = launch_pdl(vec ? embed_few_kernel<T, O, true> : embed_few_kernel<T, O, false>, dim3((unsigned)few_sets(a.V, a.d), cb), 256, 0, st, a);
+            return;
+        }
+        const long chunks = ((long)a.T + 31) / 32;
+        if (chunks * cb > 0x7FFFFFFFL) {
+            err = cudaErrorInvalidValue;
+            return;
+        }
+        SortBufs b;
+        int *p = static_cast<int *>(a.workspace);
+        for (int i = 0; i < 2; i++) b.key[i] = p + 2 * i * sort_ints(a.T), b.idx[i] = b.key[i] + sort_ints(a.T);
+        float *parts = reinterpret_cast<float *>(p + 4 * sort_ints(a.T));
+        int passes = 1;
+        while ((a.V >> (8 * passes)) != 0) passes++;
+        cudaLaunchConfig_t cfg = {};
+        int ctas = 1;
+        while (ctas < ES_CLUSTER && a.T > 1024 * ctas) ctas *= 2;
+        cfg.gridDim = dim3(ctas);
+        cfg.blockDim = dim3(ES_THREADS);
+        cfg.stream = st;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)ctas, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(st, &cs) != cudaSuccess) cs = cudaStreamCaptureStatusNone;
+        cfg.attrs = attr;
+        cfg.numAttrs = cs == cudaStreamCaptureStatusActive ? 1 : 2;
+        if ((err = cudaLaunchKernelEx(&cfg, embed_sort_kernel, a.ids, a.T, a.V, a.pad_id, passes, b, a.status)) != cudaSuccess) return;
+        if (!a.accumulate && (err = launch_pdl(vec ? embed_zero_kernel<O, true> : embed_zero_kernel<O, false>, 2 * 152, 512, 0, st, a)) != cudaSuccess) return;
+        const int *key = b.key[(passes - 1) & 1], *idx = b.idx[(passes - 1) & 1];
+        err = launch_pdl(vec ? embed_sum_kernel<T, O, true> : embed_sum_kernel<T, O, false>, (unsigned)((chunks * cb + 7) / 8), 256, 0, st, a, key, idx, parts);
+        if (err == cudaSuccess)
+            err = launch_pdl(vec ? embed_join_kernel<O, true> : embed_join_kernel<O, false>, (unsigned)(chunks * cb), 256, 0, st, a, key, (const float *)parts);
     });
-    return cudaGetLastError();
+    return err;
 }
 
 }  // namespace mnmt
