@@ -68,15 +68,22 @@ struct LaneCols {
                 if (at(k) < d) row[at(k)] = from_f32<O>(v[k]);
         }
     }
-    // the row of a token's gradient from the sum of its g
+    // the row of a token's gradient from the sum of its g (wide: rows start on 32 bytes)
     template <typename O>
-    MNMT_DEV void finish(O *row, float (&s)[8], float scale, bool accumulate) const {
+    MNMT_DEV void finish(O *row, float (&s)[8], float scale, bool accumulate, bool wide) const {
         float old[8];
         if (accumulate) load(row, old);
 #pragma unroll
         for (int k = 0; k < 8; k++) {
             s[k] = __fmul_rn(s[k], scale);
             if (accumulate) s[k] = __fadd_rn(old[k], s[k]);
+        }
+        if (VEC && sizeof(O) == 4 && wide && at(0) + 8 <= d) {
+            uint32_t w[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) w[k] = __float_as_uint(s[k]);
+            st32(row + at(0), w);
+            return;
         }
         store(row, s);
     }
@@ -161,7 +168,7 @@ __global__ void __launch_bounds__(256) embed_few_kernel(EmbedRowsArgs a) {
             float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
             if (c)
                 for (int w = 0; w < 8; w++) add_list(w, r, s);
-            cols.finish(out + ((long)r * sets + x) * a.ldo, s, a.scale, a.accumulate);
+            cols.finish(out + ((long)r * sets + x) * a.ldo, s, a.scale, a.accumulate, a.wide);
         }
     }
     __syncthreads();
@@ -175,7 +182,7 @@ __global__ void __launch_bounds__(256) embed_few_kernel(EmbedRowsArgs a) {
             for (int w = 1; w < 8; w++)
 #pragma unroll
                 for (int k = 0; k < 8; k++) s[k] += part[w][32 * k + lane];
-            cols.finish(out + ((long)many[i] * sets + x) * a.ldo, s, a.scale, a.accumulate);
+            cols.finish(out + ((long)many[i] * sets + x) * a.ldo, s, a.scale, a.accumulate, a.wide);
         }
         __syncthreads();
     }
@@ -275,30 +282,36 @@ __global__ void __launch_bounds__(ES_THREADS) embed_sort_kernel(const int *ids, 
     }
 }
 
-// Rows that no token names are zero.  Needs the ids alone: runs beside the sort.
-constexpr int EZ_BITS = 1 << 17;
-template <typename O, bool VEC>
-__global__ void __launch_bounds__(512) embed_zero_kernel(EmbedRowsArgs a) {
+// Rows that no token names are zero.  Needs the ids alone: runs beside the sort.  A block
+// has the rows that are its number modulo the blocks (those of frequent tokens have low numbers).
+constexpr int EZ_BITS = 1 << 17, EZ_THREADS = 512;
+template <typename O>
+__global__ void __launch_bounds__(EZ_THREADS) embed_zero_kernel(EmbedRowsArgs a, bool vec) {
     __shared__ uint32_t named[EZ_BITS / 32];
     pdl_allow_next();
-    const int warp = threadIdx.x >> 5;
-    const int per = (a.V + (int)gridDim.x - 1) / (int)gridDim.x, v0 = (int)min((long)a.V, (long)blockIdx.x * per), v1 = min(a.V, v0 + per);
-    O *out = static_cast<O *>(a.out);
-    const float z[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    for (int f = v0; f < v1; f += EZ_BITS) {
-        const int e = min(v1, f + EZ_BITS);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sets = gridDim.x, x = blockIdx.x;
+    const int rows = x < a.V ? (a.V - x + sets - 1) / sets : 0;
+    const long whole = vec ? (long)a.d * sizeof(O) / 16 : 0;  // 16-byte pieces of a row
+    for (int f = 0; f < rows; f += EZ_BITS) {
+        const int n = min(EZ_BITS, rows - f);
         __syncthreads();
-        for (int i = threadIdx.x; i < (e - f + 31) / 32; i += 512) named[i] = 0;
+        for (int i = threadIdx.x; i < (n + 31) / 32; i += EZ_THREADS) named[i] = 0;
         __syncthreads();
 #pragma unroll 8
-        for (int t = threadIdx.x; t < a.T; t += 512) {
+        for (int t = threadIdx.x; t < a.T; t += EZ_THREADS) {
             const int id = a.ids[t];
-            if (id >= f && id < e && id != a.pad_id) atomicOr(&named[(id - f) >> 5], 1u << ((id - f) & 31));
+            if (id >= 0 && id < a.V && id != a.pad_id && id % sets == x) {
+                const int r = id / sets - f;
+                if (r >= 0 && r < n) atomicOr(&named[r >> 5], 1u << (r & 31));
+            }
         }
         __syncthreads();
-        for (int v = f + warp; v < e; v += 16)
-            if (!((named[(v - f) >> 5] >> ((v - f) & 31)) & 1u))
-                for (LaneCols<VEC> cols{0, a.d}; cols.c0 < a.d; cols.c0 += EB_COLS) cols.store(out + (long)v * a.ldo, z);
+        for (int r = warp; r < n; r += EZ_THREADS / 32)
+            if (!((named[r >> 5] >> (r & 31)) & 1u)) {
+                O *row = static_cast<O *>(a.out) + ((long)(f + r) * sets + x) * a.ldo;
+                for (long i = lane; i < whole; i += 32) reinterpret_cast<uint4 *>(row)[i] = make_uint4(0, 0, 0, 0);
+                for (long i = whole * (16 / sizeof(O)) + lane; i < a.d; i += 32) row[i] = from_f32<O>(0.0f);
+            }
     }
     pdl_grid_wait();  // the sort's end is this kernel's too
 }
@@ -317,22 +330,46 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedRowsArgs a, const i
     const int k = on ? key[p0 + lane] : a.V, t = on ? idx[p0 + lane] : 0;
     const int prev = p0 ? key[p0 - 1] : -1, next = p0 + 32 < a.T ? key[p0 + 32] : a.V;
     const int left = __shfl_up_sync(0xFFFFFFFFu, k, 1);
-    uint32_t heads = __ballot_sync(0xFFFFFFFFu, lane == 0 || k != left);  // first tokens of rows
-    while (heads) {
-        const int i = __ffs(heads) - 1;
-        heads &= heads - 1;
-        const int j = heads ? __ffs(heads) - 1 : 32, v = __shfl_sync(0xFFFFFFFFu, k, i);
-        if (v >= a.V) break;
-        float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        add_rows<T, VEC>(static_cast<const T *>(a.table), a.ld, t, (j == 32 ? 0xFFFFFFFFu : (1u << j) - 1u) & ~((1u << i) - 1u), cols, s);
-        if ((i > 0 || prev != v) && (j < 32 || next != v)) {
-            cols.finish(static_cast<O *>(a.out) + (long)v * a.ldo, s, a.scale, a.accumulate);
-        } else {
-            float *p = parts + (2 * chunk + (i > 0)) * (long)(cb * EB_COLS) + cols.c0;
-            reinterpret_cast<float4 *>(p)[2 * lane] = make_float4(s[0], s[1], s[2], s[3]);
-            reinterpret_cast<float4 *>(p)[2 * lane + 1] = make_float4(s[4], s[5], s[6], s[7]);
+    const uint32_t heads = __ballot_sync(0xFFFFFFFFu, lane > 0 && k != left);  // first tokens of further rows
+    const T *g = static_cast<const T *>(a.table);
+    float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    int from = 0;
+    const auto flush = [&](int to) {  // tokens from .. to - 1 are one row's
+        const int v = __shfl_sync(0xFFFFFFFFu, k, from);
+        if (v < a.V) {
+            if ((from > 0 || prev != v) && (to < 32 || next != v)) {
+                cols.finish(static_cast<O *>(a.out) + (long)v * a.ldo, s, a.scale, a.accumulate, a.wide);
+            } else {
+                float *p = parts + (2 * chunk + (from > 0)) * (long)(cb * EB_COLS) + cols.c0;
+                reinterpret_cast<float4 *>(p)[2 * lane] = make_float4(s[0], s[1], s[2], s[3]);
+                reinterpret_cast<float4 *>(p)[2 * lane + 1] = make_float4(s[4], s[5], s[6], s[7]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) s[e] = 0.0f;
+        from = to;
+    };
+    for (int i0 = 0; i0 < 32; i0 += 8) {  // eight rows in flight, whosever they are
+        float v[8][8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const bool some = __shfl_sync(0xFFFFFFFFu, k, i0 + i) < a.V;
+            const long row = __shfl_sync(0xFFFFFFFFu, t, i0 + i);
+            if (some) {
+                cols.load(g + row * a.ld, v[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[i][e] = 0.0f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if ((heads >> (i0 + i)) & 1u) flush(i0 + i);
+#pragma unroll
+            for (int e = 0; e < 8; e++) s[e] += v[i][e];
         }
     }
+    flush(32);
 }
 
 // A block per chunk and 256 columns: the row that begins in the chunk and goes on into
@@ -349,13 +386,17 @@ __global__ void __launch_bounds__(256) embed_join_kernel(EmbedRowsArgs a, const 
     const bool from_first = key[p0] == v;
     if (from_first && p0 > 0 && key[p0 - 1] == v) return;  // it began before
     const LaneCols<VEC> cols{(int)(blockIdx.x % cb) * EB_COLS, a.d};
-    long lo = p0 + 32, hi = a.T;  // past its last token
-    while (lo < hi) {
-        const long mid = (lo + hi) >> 1;
-        if (key[mid] <= v) lo = mid + 1;
-        else hi = mid;
+    // its last chunk: 32 chunks at a time, those that end with it
+    long last = chunk;
+    for (;;) {
+        const long c = last + 1 + lane;
+        const uint32_t full = __ballot_sync(0xFFFFFFFFu, 32 * c + 31 < a.T && key[32 * c + 31] == v);
+        const int m = full == 0xFFFFFFFFu ? 32 : __ffs(~full) - 1;
+        last += m;
+        if (m < 32) break;
     }
-    const long last = (lo - 1) / 32, n = last - chunk + 1, per = (n + 7) / 8;
+    if (32 * (last + 1) < a.T && key[32 * (last + 1)] == v) last++;
+    const long n = last - chunk + 1, per = (n + 7) / 8;
     float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
     for (long c = chunk + warp * per; c <= min(last, chunk + (warp + 1) * per - 1); c++) {
@@ -370,7 +411,7 @@ __global__ void __launch_bounds__(256) embed_join_kernel(EmbedRowsArgs a, const 
     for (int w = 1; w < 8; w++)
 #pragma unroll
         for (int k = 0; k < 8; k++) s[k] += part[w][32 * k + lane];
-    cols.finish(static_cast<O *>(a.out) + (long)v * a.ldo, s, a.scale, a.accumulate);
+    cols.finish(static_cast<O *>(a.out) + (long)v * a.ldo, s, a.scale, a.accumulate, a.wide);
 }
 
 template <typename F>
@@ -413,13 +454,15 @@ size_t sum_parts(int T, int d) { return 2 * (((size_t)T + 31) / 32) * ((size_t)(
 
 size_t embed_rows_backward_workspace(int T, int V, int d) { return few_tokens(T, V, d) ? 16 : 16 * sort_ints(T) + 4 * sum_parts(T, d); }
 
-cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &a, cudaStream_t st) {
+cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &args, cudaStream_t st) {
     cudaError_t err = cudaSuccess;
+    EmbedRowsArgs a = args;
     by_types(a.dtype, a.otype, [&](auto t, auto o) {
         using T = decltype(t);
         using O = decltype(o);
         const bool vec = row_alignment(static_cast<const T *>(a.table), a.T ? a.ld : 0) && row_alignment(static_cast<const O *>(a.out), a.ldo);
         const unsigned cb = (unsigned)((a.d + EB_COLS - 1) / EB_COLS);
+        a.wide = row_alignment(static_cast<const O *>(a.out), a.ldo) == 2;
         if (few_tokens(a.T, a.V, a.d)) {
             err = launch_pdl(vec ? embed_few_kernel<T, O, true> : embed_few_kernel<T, O, false>, dim3((unsigned)few_sets(a.V, a.d), cb), 256, 0, st, a);
             return;
@@ -451,7 +494,7 @@ cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &a, cudaStream_t st) 
         cfg.attrs = attr;
         cfg.numAttrs = cs == cudaStreamCaptureStatusActive ? 1 : 2;
         if ((err = cudaLaunchKernelEx(&cfg, embed_sort_kernel, a.ids, a.T, a.V, a.pad_id, passes, b, a.status)) != cudaSuccess) return;
-        if (!a.accumulate && (err = launch_pdl(vec ? embed_zero_kernel<O, true> : embed_zero_kernel<O, false>, 2 * 152, 512, 0, st, a)) != cudaSuccess) return;
+        if (!a.accumulate && (err = launch_pdl(embed_zero_kernel<O>, 2 * 152, EZ_THREADS, 0, st, a, row_alignment(static_cast<const O *>(a.out), a.ldo) > 0)) != cudaSuccess) return;
         const int *key = b.key[(passes - 1) & 1], *idx = b.idx[(passes - 1) & 1];
         err = launch_pdl(vec ? embed_sum_kernel<T, O, true> : embed_sum_kernel<T, O, false>, (unsigned)((chunks * cb + 7) / 8), 256, 0, st, a, key, idx, parts);
         if (err == cudaSuccess)

@@ -11,6 +11,8 @@
 // one of S and dP the tensor core is on the products that follow the other:
 //   dk, dv:  dV(j), S(j+1) once P(j) is written, dK(j), dP(j+1) once dS(j) is
 //   dq:      S(j+1), dP(j+1) once S(j), dP(j) are in registers, dQ(j) once dS(j) is written
+// Where tiles of keys are few and their walks long (shared key heads), a cluster of up to
+// eight CTAs divides a walk's steps and adds up its sums through distributed shared memory.
 // A walk goes backwards from the last row that is seen, as in the forward pass, and rows
 // whose result is not finite are computed again over their own queries or keys alone.
 #include "seq_tile.cuh"
@@ -244,7 +246,7 @@ struct DkvLayout {
 template <int DH, bool BF>
 __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                                                                      const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
-                                                                     const SeqAttn a, const float c, const float *delta) {
+                                                                     const SeqAttn a, const float c, const float *delta, const int ctas) {
     using L = DkvLayout<DH>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
     constexpr int ST = L::STAGES;
@@ -262,7 +264,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
     const uint32_t kv_full = bar0 + 8 * (4 * ST), s_full = kv_full + 8, dp_full = kv_full + 16, p_full = kv_full + 24, ds_full = kv_full + 32,
                    out_full = kv_full + 40;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int hk = blockIdx.x % a.hkv, tile = (int)(blockIdx.x / a.hkv);
+    const int share = (int)blockIdx.x % ctas, unit = (int)blockIdx.x / ctas, hk = unit % a.hkv, tile = unit / a.hkv;
     const int h0 = hk * a.group(), heads = a.group();
     const int half = warp >> 2, rt = (int)threadIdx.x & 127, row = tile * SQ_ROWS + rt;
     if (threadIdx.x == 0) {
@@ -286,16 +288,19 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
     tc_fence_after();
     const uint32_t tS = tslot, tP = tS + L::T_DP, tV = tS + L::T_DV, tK = tS + L::T_DK;
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
-    const int nt = end > first ? (end - first + SQ_ROWS - 1) / SQ_ROWS : 0, n = nt * heads;  // tiles of one head, of all
+    const int nt = end > first ? (end - first + SQ_ROWS - 1) / SQ_ROWS : 0;  // tiles of one head
+    // this CTA's steps of the walk over all heads: n of them from step0 on
+    const int step0 = (int)((long)nt * heads * share / ctas), n = (int)((long)nt * heads * (share + 1) / ctas) - step0;
+    const int head0 = nt ? step0 / nt : 0, t0 = step0 - head0 * nt;
     const SqWaits wait{&failed, a.status};
 
     if (warp == 8) {
-        if (nt) {
+        if (n) {
             if (lane == 0) {
                 sq_load<DH>(sm, &tk, hk, tile * SQ_ROWS, kv_full);
                 sq_load<DH>(sm + L::OFF_V, &tv, hk, tile * SQ_ROWS, kv_full);
             }
-            int j = 0, h = h0, t = 0;
+            int j = 0, h = h0 + head0, t = t0;
             bool ok = true;
             for (; j < n; j++) {
                 const int s = j % ST, at = end - SQ_ROWS * (t + 1);
@@ -328,7 +333,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
             }
         }
     } else if (warp == 9) {
-        if (lane == 0 && nt) {
+        if (lane == 0 && n) {
             bool ok = wait(kv_full, 0);
             const auto scores = [&](int j) {  // S^T(j)
                 const int s = j % ST;
@@ -375,7 +380,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const unsigned long long c2 = f4_two(c, c);
         bool ok = true;
-        for (int j = 0, t = 0; j < n; j++) {
+        for (int j = 0, t = t0; j < n; j++) {
             const int s = j % ST, at = end - SQ_ROWS * (t + 1) + 64 * half, lo = qs.lo - at, hi = qs.hi - at;
             if (++t == nt) t = 0;
             const float4 *num = reinterpret_cast<const float4 *>(smp + L::OFF_N + s * 1024) + 16 * half;
@@ -439,27 +444,68 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
             __syncwarp();
             if (lane == 0) mbar_arrive(ds_full);
         }
-        if (nt) ok = wait(out_full, 0) && ok;
+        if (n) ok = wait(out_full, 0) && ok;
         tc_fence_after();
         // a row's two threads: dv, dk
+        const HeadRows &x = half ? a.dk : a.dv;
+        const float f = half ? a.scale : 1.0f;
+        T *o = static_cast<T *>(x.p) + row * x.ld + hk * x.hd;
         bool odd = false;
-        if (ok) {
-            const HeadRows &x = half ? a.dk : a.dv;
-            const float f = half ? a.scale : 1.0f;
-            T *o = static_cast<T *>(x.p) + row * x.ld + hk * x.hd;
+        int c0 = 0, c1 = DH;  // the columns that this CTA stores
+        if (ctas == 1) {
+            if (ok) {
+#pragma unroll
+                for (int b = 0; b < DH / 32; b++) {
+                    uint32_t w[32];
+                    float v[32];
+                    if (n) tmem_ld32((half ? tK : tV) + lanes + 32 * b, w);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; i++) {
+                        const float y = n && qs.hi > qs.lo ? __uint_as_float(w[i]) : 0.0f;
+                        odd |= !(fabsf(y) < INFINITY);
+                        v[i] = y * f;
+                    }
+                    if (in) sq_store<BF>(o, 32 * b, a.dh, v);
+                }
+            }
+        } else {
+            // sums of this CTA's steps to shared memory, where the ring was: four columns of a row side by side
+            float4 *mine = reinterpret_cast<float4 *>(smp + L::OFF_Q) + half * (DH / 4) * SQ_ROWS + rt;
 #pragma unroll
             for (int b = 0; b < DH / 32; b++) {
                 uint32_t w[32];
-                float v[32];
-                if (nt) tmem_ld32((half ? tK : tV) + lanes + 32 * b, w);
+                if (n) tmem_ld32((half ? tK : tV) + lanes + 32 * b, w);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; i++) {
-                    const float y = nt && qs.hi > qs.lo ? __uint_as_float(w[i]) : 0.0f;
-                    odd |= !(fabsf(y) < INFINITY);
-                    v[i] = y * f;
+                for (int i = 0; i < 8; i++)
+                    mine[(8 * b + i) * SQ_ROWS] = n ? make_float4(__uint_as_float(w[4 * i]), __uint_as_float(w[4 * i + 1]), __uint_as_float(w[4 * i + 2]),
+                                                                  __uint_as_float(w[4 * i + 3]))
+                                                    : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+            __syncwarp();
+            sq_cluster_sync();
+            // every CTA of the cluster adds up a share of the columns, in the order of the CTAs
+            c0 = DH / ctas * share, c1 = c0 + DH / ctas;
+            if (ok) {
+                const uint32_t at = s_addr(mine);
+#pragma unroll 2
+                for (int col = c0; col < c1; col += 8) {
+                    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+                    for (int r = 0; r < ctas; r++) {
+                        const uint32_t from = t2_mapa(at + (col / 4) * (SQ_ROWS * 16), r);
+                        const float4 y = sq_remote(from), z = sq_remote(from + SQ_ROWS * 16);
+                        v[0] += y.x, v[1] += y.y, v[2] += y.z, v[3] += y.w, v[4] += z.x, v[5] += z.y, v[6] += z.z, v[7] += z.w;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        if (qs.hi <= qs.lo) v[i] = 0.0f;
+                        odd |= !(fabsf(v[i]) < INFINITY);
+                        v[i] *= f;
+                    }
+                    if (in) sq_store<BF>(o, col, a.dh, v);
                 }
-                if (in) sq_store<BF>(o, 32 * b, a.dh, v);
             }
         }
         odd_rows[half][rt] = odd;
@@ -475,11 +521,19 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
                              a.lse + (long)h * a.q_rows, delta + (long)h * a.q_rows, sp, a.dh, c, dk, dv);
 #pragma unroll
             for (int i = 0; i < 4; i++) dk[i] *= a.scale;
-            if (4 * lane < a.dh) {
+            if (4 * lane >= c0 && 4 * lane < c1 && 4 * lane < a.dh) {
                 store4(static_cast<T *>(a.dk.p) + rr * a.dk.ld + hk * a.dk.hd + 4 * lane, dk);
                 store4(static_cast<T *>(a.dv.p) + rr * a.dv.ld + hk * a.dv.hd + 4 * lane, dv);
             }
         }
+    }
+    if (ctas > 1) {
+        if (warp >= 8) {
+            __syncwarp();
+            sq_cluster_sync();
+        }
+        __syncwarp();
+        sq_cluster_sync();  // no CTA leaves while others read its sums
     }
     tc_fence_before();
     __syncthreads();
@@ -508,6 +562,15 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     }
 }
 
+// CTAs that share the walk of a tile of keys: until the card is filled three times over (walks
+// differ in length), as long as each still has two steps of the longest walk there may be
+int dkv_ctas(long tiles, const SeqAttn &a) {
+    const long steps = (a.q_rows + SQ_ROWS - 1L) / SQ_ROWS * a.group();
+    int p = 1;
+    while (p < 8 && tiles * a.hkv * p < 3L * 152 && steps >= 4 * p) p *= 2;
+    return p;
+}
+
 template <int DH, bool BF>
 cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
     CUtensorMap tq, tk, tv, tg;
@@ -519,7 +582,9 @@ cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
     const unsigned qt = (unsigned)((a.q_rows + SQ_ROWS - 1) / SQ_ROWS), kt = (unsigned)((a.k_rows + SQ_ROWS - 1) / SQ_ROWS);
     const cudaError_t e = launch_pdl(seq_attn_dq_kernel<DH, BF>, qt * a.hq, BW_THREADS, DqLayout<DH>::SMEM, st, tq, tg, tk, tv, a, c, delta);
     if (e != cudaSuccess) return e;
-    return launch_pdl(seq_attn_dkv_kernel<DH, BF>, kt * a.hkv, BW_THREADS, DkvLayout<DH>::SMEM, st, tk, tv, tq, tg, a, c, (const float *)delta);
+    const int ctas = dkv_ctas(kt, a);
+    return sq_launch(seq_attn_dkv_kernel<DH, BF>, kt * a.hkv * ctas, ctas, BW_THREADS, DkvLayout<DH>::SMEM, st, tk, tv, tq, tg, a, c, (const float *)delta,
+                     ctas);
 }
 
 template <int DH, bool BF>

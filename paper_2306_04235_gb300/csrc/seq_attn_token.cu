@@ -217,7 +217,7 @@ __device__ __forceinline__ void run_out(const SeqAttn &a, const Unit &u, bool no
 
 // Tiles before each sequence's, in units of one head: pre[0 .. n_seqs].  All threads of the block.
 template <int DH>
-__device__ void tile_prefix(const SeqAttn &a, int *pre) {
+__device__ __forceinline__ void tile_prefix(const SeqAttn &a, int *pre) {
     __shared__ int sums[32];
     constexpr int KT = tk_keys<DH>();
     const int n = a.n_seqs, per = (n + (int)blockDim.x - 1) / (int)blockDim.x, from = (int)threadIdx.x * per, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -272,6 +272,9 @@ __global__ void __launch_bounds__(32 * TK_WARPS, TK_BLOCKS) seq_attn_token_kerne
     int *pre = reinterpret_cast<int *>(ring_all + TK_SMEM);
     tile_prefix<DH>(a, pre);
     const int per = a.hkv * chunks, rows = min(16, a.group());
+    int *pre_out = reinterpret_cast<int *>(static_cast<float *>(a.workspace) + 2 * (size_t)TK_GRID * TK_WARPS * tk_slot<DH>(rows));
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b <= a.n_seqs; b += 32 * TK_WARPS) pre_out[b] = pre[b];
     const long total = (long)pre[a.n_seqs] * per, run = run_tiles(total, (int)gridDim.x * TK_WARPS), t0 = w * run, t1 = min(total, t0 + run);
     float *slot = static_cast<float *>(a.workspace) + 2 * w * tk_slot<DH>(rows);
     for (long t = t0; t < t1;) {
@@ -307,29 +310,28 @@ __global__ void __launch_bounds__(32 * TK_WARPS, TK_BLOCKS) seq_attn_token_kerne
     pdl_allow_next();
 }
 
-// A warp per unit and row: the runs of a unit that was cut, added in their order; zeros where there is no key.
+// A block per unit and row: the runs of a unit that was cut, a quarter of them a warp,
+// added in their order; zeros where there is no key.  pre: as the first kernel left it.
+constexpr int TJ_WARPS = 4;
 template <int DH, bool BF>
-__global__ void __launch_bounds__(256) seq_attn_token_join_kernel(const SeqAttn a, const int chunks, const int warps) {
+__global__ void __launch_bounds__(32 * TJ_WARPS) seq_attn_token_join_kernel(const SeqAttn a, const int chunks, const int warps, const int *pre) {
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
-    extern __shared__ __align__(16) int pre[];
-    tile_prefix<DH>(a, pre);  // lengths are the caller's, not the first kernel's
+    constexpr int E = DH / 32;  // columns of a lane
+    __shared__ float sums[TJ_WARPS][DH + 1];
     pdl_grid_wait();
-    const int per = a.hkv * chunks, rows = min(16, a.group()), lane = threadIdx.x & 31;
-    const long total = (long)pre[a.n_seqs] * per, run = run_tiles(total, warps), units = (long)a.n_seqs * per;
-    const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 5, un = w / rows;
-    const int row = (int)(w % rows);
-    if (un >= units) return;
+    const int per = a.hkv * chunks, rows = min(16, a.group()), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long un = blockIdx.x / rows;
+    const int row = (int)(blockIdx.x % rows);
     const Unit u = unit_of(a, chunks, un);
     if (row >= u.n) return;
-    const int nb = pre[u.b + 1] - pre[u.b];
-    const long ut = (long)pre[u.b] * per + (un - (long)u.b * per) * nb, ue = ut + nb;
+    const int p0 = pre[u.b], nb = pre[u.b + 1] - p0;
+    const long total = (long)pre[a.n_seqs] * per, run = run_tiles(total, warps);
+    const long ut = (long)p0 * per + (un - (long)u.b * per) * nb, ue = ut + nb;
     T *o = static_cast<T *>(a.o.p) + u.b * a.o.ld + (u.h + row) * a.o.hd;
     float *lse = a.lse ? a.lse + (long)(u.h + row) * a.q_rows + u.b : nullptr;
-    constexpr int E = DH / 32;  // columns of a lane
     if (nb == 0) {
-        for (int i = 0; i < E; i++)
-            if (E * lane + i < a.dh) o[E * lane + i] = from_f32<T>(0.0f);
-        if (lane == 0 && lse) *lse = -INFINITY;
+        if ((int)threadIdx.x < a.dh) o[threadIdx.x] = from_f32<T>(0.0f);
+        if (threadIdx.x == 0 && lse) *lse = -INFINITY;
         return;
     }
     const long wa = ut / run, wb = (ue - 1) / run;
@@ -342,22 +344,31 @@ __global__ void __launch_bounds__(256) seq_attn_token_join_kernel(const SeqAttn 
     for (long x = wa + lane; x <= wb; x += 32) m = fmaxf(m, part(x)[rows * DH + 2 * row]);
     m = warp_max_f(m);
     const float mu = m == -INFINITY ? 0.0f : m;
+    const long share = (wb - wa + TJ_WARPS) / TJ_WARPS, xa = wa + warp * share, xb = min(wb, xa + share - 1);
     float l = 0.0f, acc[E];
 #pragma unroll
     for (int i = 0; i < E; i++) acc[i] = 0.0f;
-#pragma unroll 4
-    for (long x = wa; x <= wb; x++) {
+#pragma unroll 8
+    for (long x = xa; x <= xb; x++) {
         const float *p = part(x);
         const float2 ml = *reinterpret_cast<const float2 *>(p + rows * DH + 2 * row);
         const float f = exp2_fast(ml.x - mu);
         l = fmaf(ml.y, f, l);
 #pragma unroll
-        for (int i = 0; i < E; i++) acc[i] = fmaf(p[row * DH + E * lane + i], f, acc[i]);
+        for (int i = 0; i < E; i++) acc[i] = fmaf(p[row * DH + 32 * i + lane], f, acc[i]);
     }
 #pragma unroll
-    for (int i = 0; i < E; i++)
-        if (E * lane + i < a.dh) o[E * lane + i] = from_f32<T>(acc[i] / l);
-    if (lane == 0 && lse) *lse = row_lse(m, l);
+    for (int i = 0; i < E; i++) sums[warp][32 * i + lane] = acc[i];
+    if (lane == 0) sums[warp][DH] = l;
+    __syncthreads();
+    l = 0.0f;
+    for (int w = 0; w < TJ_WARPS; w++) l += sums[w][DH];
+    if ((int)threadIdx.x < a.dh) {
+        float x = 0.0f;
+        for (int w = 0; w < TJ_WARPS; w++) x += sums[w][threadIdx.x];
+        o[threadIdx.x] = from_f32<T>(x / l);
+    }
+    if (threadIdx.x == 0 && lse) *lse = row_lse(m, l);
 }
 
 int token_chunks(const SeqAttn &a) { return (a.group() + 15) / 16; }
@@ -376,8 +387,9 @@ cudaError_t token(const SeqAttn &a, cudaStream_t st) {
     const size_t pre = ((size_t)a.n_seqs + 1) * 4;
     const cudaError_t e = launch_pdl(seq_attn_token_kernel<DH, BF>, blocks, 32 * TK_WARPS, TK_SMEM + pre, st, a, c, chunks, 1);
     if (e != cudaSuccess) return e;
-    const long rows = units * (a.group() < 16 ? a.group() : 16);
-    return launch_pdl(seq_attn_token_join_kernel<DH, BF>, (unsigned)((rows + 7) / 8), 256, pre, st, a, chunks, blocks * TK_WARPS);
+    const int rows = a.group() < 16 ? a.group() : 16;
+    const int *left = reinterpret_cast<const int *>(static_cast<const float *>(a.workspace) + 2 * (size_t)TK_GRID * TK_WARPS * tk_slot<DH>(rows));
+    return launch_pdl(seq_attn_token_join_kernel<DH, BF>, (unsigned)(units * rows), 32 * TJ_WARPS, 0, st, a, chunks, blocks * TK_WARPS, left);
 }
 
 template <int DH, bool BF>
@@ -399,7 +411,7 @@ cudaError_t seq_attn_token_init() {
 size_t seq_attn_token_workspace(const SeqAttn &a) {
     if (!token_split(a)) return 16;
     const int rows = a.group() < 16 ? a.group() : 16;
-    return 2 * (size_t)TK_GRID * TK_WARPS * (a.dh <= 64 ? tk_slot<64>(rows) : tk_slot<128>(rows)) * 4;
+    return 2 * (size_t)TK_GRID * TK_WARPS * (a.dh <= 64 ? tk_slot<64>(rows) : tk_slot<128>(rows)) * 4 + ((size_t)a.n_seqs + 1) * 4;
 }
 
 cudaError_t launch_seq_attn_token(const SeqAttn &a, cudaStream_t st) {

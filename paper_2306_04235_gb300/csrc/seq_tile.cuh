@@ -94,6 +94,43 @@ __device__ __forceinline__ void sq_store(void *row, int c0, int dh, const float 
                 make_uint4(sq_pack<BF>(v[c], v[c + 1]), sq_pack<BF>(v[c + 2], v[c + 3]), sq_pack<BF>(v[c + 4], v[c + 5]), sq_pack<BF>(v[c + 6], v[c + 7]));
 }
 
+// all threads of the cluster, whole warps
+__device__ __forceinline__ void sq_cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float4 sq_remote(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// launch_pdl in clusters of `ctas`
+template <typename... KArgs, typename... Args>
+cudaError_t sq_launch(void (*kernel)(KArgs...), unsigned grid, int ctas, int threads, size_t smem, cudaStream_t st, Args &&...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (ctas > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)ctas;
+        attr[n].val.clusterDim.y = 1;
+        attr[n++].val.clusterDim.z = 1;
+    }
+    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &cs) != cudaSuccess) cs = cudaStreamCaptureStatusNone;
+    if (cs != cudaStreamCaptureStatusActive) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args &&>(args)...);
+}
+
 // Waits of a kernel's roles: a wait that gives up sets `failed` in shared memory and the
 // status, and every role leaves its loop at its next wait.
 struct SqWaits {

@@ -85,6 +85,7 @@ struct EmbedRowsArgs {
     int otype;
     long ldo;
     int pad_id, accumulate;    // backward
+    int wide;                  // backward: rows of out start on 32 bytes
     void *workspace;
     int *status;
 };
