@@ -58,6 +58,24 @@ struct LaneCols {
             for (int k = 0; k < 8; k++) v[k] = at(k) < d ? to_f32(row[at(k)]) : 0.0f;
         }
     }
+    // the same as words, to be converted when they are added
+    template <typename T>
+    MNMT_DEV void fetch8(const T *row, Raw<T, 8> &r) const {
+        constexpr int NW = sizeof(T) * 2;
+        if (VEC && at(0) + 8 <= d) {
+#pragma unroll
+            for (int i = 0; i < NW / 4; i++) {
+                const uint4 v = reinterpret_cast<const uint4 *>(row + at(0))[i];
+                r.w[4 * i] = v.x, r.w[4 * i + 1] = v.y, r.w[4 * i + 2] = v.z, r.w[4 * i + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NW; i++) r.w[i] = 0;
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                if (at(k) < d) r.w[k * NW / 8] |= bits_of(row[at(k)]) << (sizeof(T) == 2 ? 16 * (k & 1) : 0);
+        }
+    }
     template <typename O>
     MNMT_DEV void store(O *row, const float (&v)[8]) const {
         if (VEC && at(0) + 8 <= d) {
@@ -243,11 +261,12 @@ __global__ void __launch_bounds__(ES_THREADS) embed_sort_kernel(const int *ids, 
         int before = 0, all = 0, x = 0;
         if (d < 256) {
             const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&tot[d]);
+#pragma unroll 8
             for (int c = 0; c < ctas; c++) {
                 uint32_t at;
                 int v;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(mine), "r"(c));
-                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(mine), "r"(c));
+                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at));
                 if (c < rank) before += v;
                 all += v;
             }
@@ -284,31 +303,34 @@ __global__ void __launch_bounds__(ES_THREADS) embed_sort_kernel(const int *ids, 
 
 // Rows that no token names are zero.  Needs the ids alone: runs beside the sort.  A block
 // has the rows that are its number modulo the blocks (those of frequent tokens have low numbers).
-constexpr int EZ_BITS = 1 << 17, EZ_THREADS = 512;
+constexpr int EZ_BITS = 1 << 16, EZ_THREADS = 256, EZ_SETS = 4 * 152;
 template <typename O>
 __global__ void __launch_bounds__(EZ_THREADS) embed_zero_kernel(EmbedRowsArgs a, bool vec) {
     __shared__ uint32_t named[EZ_BITS / 32];
     pdl_allow_next();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sets = gridDim.x, x = blockIdx.x;
-    const int rows = x < a.V ? (a.V - x + sets - 1) / sets : 0;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, x = blockIdx.x;
+    const int rows = x < a.V ? (a.V - x + EZ_SETS - 1) / EZ_SETS : 0;
     const long whole = vec ? (long)a.d * sizeof(O) / 16 : 0;  // 16-byte pieces of a row
+    const int quads = (reinterpret_cast<uintptr_t>(a.ids) & 15) ? 0 : a.T / 4;
     for (int f = 0; f < rows; f += EZ_BITS) {
         const int n = min(EZ_BITS, rows - f);
         __syncthreads();
         for (int i = threadIdx.x; i < (n + 31) / 32; i += EZ_THREADS) named[i] = 0;
         __syncthreads();
+        const auto name = [&](int id) {
+            const int r = id / EZ_SETS - f;
+            if (id >= 0 && id < a.V && id != a.pad_id && id % EZ_SETS == x && r >= 0 && r < n) atomicOr(&named[r >> 5], 1u << (r & 31));
+        };
 #pragma unroll 8
-        for (int t = threadIdx.x; t < a.T; t += EZ_THREADS) {
-            const int id = a.ids[t];
-            if (id >= 0 && id < a.V && id != a.pad_id && id % sets == x) {
-                const int r = id / sets - f;
-                if (r >= 0 && r < n) atomicOr(&named[r >> 5], 1u << (r & 31));
-            }
+        for (int i = threadIdx.x; i < quads; i += EZ_THREADS) {
+            const int4 q = reinterpret_cast<const int4 *>(a.ids)[i];
+            name(q.x), name(q.y), name(q.z), name(q.w);
         }
+        for (int t = 4 * quads + threadIdx.x; t < a.T; t += EZ_THREADS) name(a.ids[t]);
         __syncthreads();
         for (int r = warp; r < n; r += EZ_THREADS / 32)
             if (!((named[r >> 5] >> (r & 31)) & 1u)) {
-                O *row = static_cast<O *>(a.out) + ((long)(f + r) * sets + x) * a.ldo;
+                O *row = static_cast<O *>(a.out) + ((long)(f + r) * EZ_SETS + x) * a.ldo;
                 for (long i = lane; i < whole; i += 32) reinterpret_cast<uint4 *>(row)[i] = make_uint4(0, 0, 0, 0);
                 for (long i = whole * (16 / sizeof(O)) + lane; i < a.d; i += 32) row[i] = from_f32<O>(0.0f);
             }
@@ -350,68 +372,95 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedRowsArgs a, const i
         from = to;
     };
     for (int i0 = 0; i0 < 32; i0 += 8) {  // eight rows in flight, whosever they are
-        float v[8][8];
+        Raw<T, 8> v[8];
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const bool some = __shfl_sync(0xFFFFFFFFu, k, i0 + i) < a.V;
             const long row = __shfl_sync(0xFFFFFFFFu, t, i0 + i);
             if (some) {
-                cols.load(g + row * a.ld, v[i]);
+                cols.fetch8(g + row * a.ld, v[i]);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; e++) v[i][e] = 0.0f;
+                for (uint32_t &w : v[i].w) w = 0;
             }
         }
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             if ((heads >> (i0 + i)) & 1u) flush(i0 + i);
 #pragma unroll
-            for (int e = 0; e < 8; e++) s[e] += v[i][e];
+            for (int e = 0; e < 8; e++) s[e] += raw_at(v[i], e);
         }
     }
     flush(32);
 }
 
-// A block per chunk and 256 columns: the row that begins in the chunk and goes on into
-// the next ones, if there is one.  Each warp adds an eighth of its chunks.
+// A block per 8 chunks and 256 columns: the rows that begin in one of the chunks and go on
+// into the next, a warp each; those of many chunks by all warps, an eighth of them each.
+constexpr int EJ_MANY = 16;
 template <typename O, bool VEC>
 __global__ void __launch_bounds__(256) embed_join_kernel(EmbedRowsArgs a, const int *key, const float *parts) {
     __shared__ float part[8][EB_COLS];
+    __shared__ long chunks[8];
     pdl_grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cb = (a.d + EB_COLS - 1) / EB_COLS;
-    const long chunk = blockIdx.x / cb, p0 = 32 * chunk;
-    if (p0 + 32 >= a.T) return;
-    const int v = key[p0 + 31];
-    if (v >= a.V || key[p0 + 32] != v) return;
-    const bool from_first = key[p0] == v;
-    if (from_first && p0 > 0 && key[p0 - 1] == v) return;  // it began before
+    const long chunk = (long)(blockIdx.x / cb) * 8 + warp, q0 = 32 * chunk;
     const LaneCols<VEC> cols{(int)(blockIdx.x % cb) * EB_COLS, a.d};
-    // its last chunk: 32 chunks at a time, those that end with it
-    long last = chunk;
-    for (;;) {
-        const long c = last + 1 + lane;
-        const uint32_t full = __ballot_sync(0xFFFFFFFFu, 32 * c + 31 < a.T && key[32 * c + 31] == v);
-        const int m = full == 0xFFFFFFFFu ? 32 : __ffs(~full) - 1;
-        last += m;
-        if (m < 32) break;
+    // the warp's chunk: its last row, whether that goes on and whether it began here
+    int row = a.V;
+    bool from_first = false, begins = false;
+    if (q0 + 32 < a.T) {
+        const int first = key[q0], next = key[q0 + 32], prev = q0 ? key[q0 - 1] : -1;
+        row = key[q0 + 31];
+        from_first = first == row;
+        begins = row < a.V && next == row && !(from_first && prev == row);
     }
-    if (32 * (last + 1) < a.T && key[32 * (last + 1)] == v) last++;
-    const long n = last - chunk + 1, per = (n + 7) / 8;
-    float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    long n = 0;  // its chunks: 32 at a time, those that end with it
+    if (begins) {
+        long last = chunk;
+        for (;;) {
+            const long c = last + 1 + lane;
+            const uint32_t full = __ballot_sync(0xFFFFFFFFu, 32 * c + 31 < a.T && key[32 * c + 31] == row);
+            const int m = full == 0xFFFFFFFFu ? 32 : __ffs(~full) - 1;
+            last += m;
+            if (m < 32) break;
+        }
+        if (32 * (last + 1) < a.T && key[32 * (last + 1)] == row) last++;
+        n = last - chunk + 1;
+    }
+    // the sums of chunks c0 .. c1 - 1 of a row that begins in chunk c
+    const auto add = [&](long c, bool whole, long c0, long c1, float(&s)[8]) {
 #pragma unroll 8
-    for (long c = chunk + warp * per; c <= min(last, chunk + (warp + 1) * per - 1); c++) {
-        const float4 *p = reinterpret_cast<const float4 *>(parts + (2 * c + (c == chunk && !from_first)) * (long)(cb * EB_COLS) + cols.c0);
-        const float4 x = p[2 * lane], y = p[2 * lane + 1];
-        s[0] += x.x, s[1] += x.y, s[2] += x.z, s[3] += x.w, s[4] += y.x, s[5] += y.y, s[6] += y.z, s[7] += y.w;
+        for (long i = c0; i < c1; i++) {
+            const float4 *p = reinterpret_cast<const float4 *>(parts + (2 * i + (i == c && !whole)) * (long)(cb * EB_COLS) + cols.c0);
+            const float4 x = p[2 * lane], y = p[2 * lane + 1];
+            s[0] += x.x, s[1] += x.y, s[2] += x.z, s[3] += x.w, s[4] += y.x, s[5] += y.y, s[6] += y.z, s[7] += y.w;
+        }
+    };
+    if (n && n < EJ_MANY) {
+        float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        add(chunk, from_first, chunk, chunk + n, s);
+        cols.finish(static_cast<O *>(a.out) + (long)row * a.ldo, s, a.scale, a.accumulate, a.wide);
     }
-#pragma unroll
-    for (int k = 0; k < 8; k++) part[warp][32 * k + lane] = s[k];
+    if (lane == 0) chunks[warp] = n < EJ_MANY ? 0 : from_first ? n : -n;
     __syncthreads();
-    if (warp) return;
-    for (int w = 1; w < 8; w++)
+    for (int w = 0; w < 8; w++) {
+        if (chunks[w] == 0) continue;  // alike in all threads
+        const long c = chunk - warp + w, m = chunks[w] < 0 ? -chunks[w] : chunks[w], per = (m + 7) / 8;
+        float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        add(c, chunks[w] > 0, min(c + m, c + warp * per), min(c + m, c + (warp + 1) * per), s);
+        __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 8; k++) s[k] += part[w][32 * k + lane];
-    cols.finish(static_cast<O *>(a.out) + (long)v * a.ldo, s, a.scale, a.accumulate, a.wide);
+        for (int k = 0; k < 8; k++) part[warp][32 * k + lane] = s[k];
+        __syncthreads();
+        if (warp == w) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) s[k] = part[0][32 * k + lane];
+            for (int x = 1; x < 8; x++)
+#pragma unroll
+                for (int k = 0; k < 8; k++) s[k] += part[x][32 * k + lane];
+            cols.finish(static_cast<O *>(a.out) + (long)row * a.ldo, s, a.scale, a.accumulate, a.wide);
+        }
+    }
 }
 
 template <typename F>
@@ -494,11 +543,12 @@ cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &args, cudaStream_t s
         cfg.attrs = attr;
         cfg.numAttrs = cs == cudaStreamCaptureStatusActive ? 1 : 2;
         if ((err = cudaLaunchKernelEx(&cfg, embed_sort_kernel, a.ids, a.T, a.V, a.pad_id, passes, b, a.status)) != cudaSuccess) return;
-        if (!a.accumulate && (err = launch_pdl(embed_zero_kernel<O>, 2 * 152, EZ_THREADS, 0, st, a, row_alignment(static_cast<const O *>(a.out), a.ldo) > 0)) != cudaSuccess) return;
+        const bool ovec = row_alignment(static_cast<const O *>(a.out), a.ldo) > 0;
+        if (!a.accumulate && (err = launch_pdl(embed_zero_kernel<O>, EZ_SETS, EZ_THREADS, 0, st, a, ovec)) != cudaSuccess) return;
         const int *key = b.key[(passes - 1) & 1], *idx = b.idx[(passes - 1) & 1];
         err = launch_pdl(vec ? embed_sum_kernel<T, O, true> : embed_sum_kernel<T, O, false>, (unsigned)((chunks * cb + 7) / 8), 256, 0, st, a, key, idx, parts);
         if (err == cudaSuccess)
-            err = launch_pdl(vec ? embed_join_kernel<O, true> : embed_join_kernel<O, false>, (unsigned)(chunks * cb), 256, 0, st, a, key, (const float *)parts);
+            err = launch_pdl(vec ? embed_join_kernel<O, true> : embed_join_kernel<O, false>, (unsigned)((chunks + 7) / 8 * cb), 256, 0, st, a, key, (const float *)parts);
     });
     return err;
 }

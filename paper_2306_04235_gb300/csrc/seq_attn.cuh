@@ -47,9 +47,8 @@ MNMT_DEV Span seq_rows(const int *start, const int *len, int b, int rows) {
     return r;
 }
 
-// the keys that query row sees (in: whether it belongs to a sequence at all)
-MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, bool &in) {
-    const int b = row < a.q_rows ? seq_of(a.q_start, a.n_seqs, row) : -1;
+// the keys that query row sees (b: as seq_of; in: whether it belongs to a sequence at all)
+MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, int b, bool &in) {
     in = false;
     if (b < 0) return Span{0, 0};
     const Span q = seq_rows(a.q_start, a.q_len, b, a.q_rows);
@@ -62,8 +61,7 @@ MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, bool &in) {
 }
 
 // the queries that see key row
-MNMT_DEV Span queries_of_key(const SeqAttn &a, int row, bool &in) {
-    const int b = row < a.k_rows ? seq_of(a.k_start, a.n_seqs, row) : -1;
+MNMT_DEV Span queries_of_key(const SeqAttn &a, int row, int b, bool &in) {
     in = false;
     if (b < 0) return Span{0, 0};
     const Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
@@ -73,6 +71,44 @@ MNMT_DEV Span queries_of_key(const SeqAttn &a, int row, bool &in) {
     if (a.causal) q.lo = max(q.lo, q.hi - (k.hi - row));
     if (q.hi < q.lo) q.hi = q.lo;
     return q;
+}
+
+// The sequences of 32 rows, row0 + lane, by a whole warp: 256 starts are compared with the
+// first row at a time (their loads in flight together), the next 32 starts serve the others.
+MNMT_DEV int seq_of_lane(const int *start, int n, int row0) {
+    const int lane = threadIdx.x & 31, row = row0 + lane;
+    int lo = 0, hi = n;  // of the starts, lo at least and hi at most are <= row0
+    while (lo < hi) {
+        const int step = (hi - lo + 255) >> 8;
+        bool below[8];
+#pragma unroll
+        for (int x = 0; x < 8; x++) {
+            const int i = lo + (8 * lane + x + 1) * step - 1;
+            below[x] = i < hi && __ldg(start + min(i, n - 1)) <= row0;
+        }
+        int c = 0;
+#pragma unroll
+        for (int x = 0; x < 8; x++) c += __popc(__ballot_sync(0xFFFFFFFFu, below[x]));
+        lo += step * c;
+        hi = min(hi, lo + step - 1);
+    }
+    const int w = lo + lane < n ? __ldg(start + lo + lane) : 0x7FFFFFFF;
+    int k = 0;  // of them are <= row
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1)
+        if (__shfl_sync(0xFFFFFFFFu, w, k + s - 1) <= row) k += s;
+    // 31 or more (sequences without rows): each lane for itself
+    return __any_sync(0xFFFFFFFFu, k == 31) ? seq_of(start, n, row) : lo + k - 1;
+}
+
+// the keys that query row0 + lane sees, and the queries that see key row0 + lane; whole warps
+MNMT_DEV Span keys_of_lane(const SeqAttn &a, int row0, bool &in) {
+    const int row = row0 + (threadIdx.x & 31), b = row0 < a.q_rows ? seq_of_lane(a.q_start, a.n_seqs, row0) : -1;
+    return keys_of_query(a, row, row < a.q_rows ? b : -1, in);
+}
+MNMT_DEV Span queries_of_lane(const SeqAttn &a, int row0, bool &in) {
+    const int row = row0 + (threadIdx.x & 31), b = row0 < a.k_rows ? seq_of_lane(a.k_start, a.n_seqs, row0) : -1;
+    return queries_of_key(a, row, row < a.k_rows ? b : -1, in);
 }
 
 MNMT_DEV float warp_sum_f(float v) {

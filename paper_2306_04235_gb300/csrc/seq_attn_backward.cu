@@ -24,26 +24,27 @@ constexpr int BW_THREADS = 320;  // eight warps on the elements, a TMA warp, an 
 
 __device__ __forceinline__ void elements_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-// A thread's 64 columns (of a row's 128) from TMEM
-__device__ __forceinline__ void load64(uint32_t taddr, uint32_t (&r)[2][32]) {
-    tmem_ld32(taddr, r[0]);
-    tmem_ld32(taddr + 32, r[1]);
+// A thread's W / 2 columns (of a row's W) from TMEM
+template <int W>
+__device__ __forceinline__ void load_half(uint32_t taddr, uint32_t (&r)[W / 64][32]) {
+#pragma unroll
+    for (int b = 0; b < W / 64; b++) tmem_ld32(taddr + 32 * b, r[b]);
     tmem_wait_ld();
 }
 
 // --------------------------------------------------------------------------- dq
-template <int DH>
+template <int DH, int W>
 struct DqLayout {
-    static constexpr int STAGES = 2, TILE = sq_bytes<DH>();
-    static constexpr int OFF_G = TILE, OFF_K = 2 * TILE, OFF_V = OFF_K + STAGES * TILE, SMEM = OFF_V + STAGES * TILE + 1024;
-    static constexpr int T_DP = 128, T_DS = 256, T_DQ = 320;  // columns of dP, dS and dQ behind S
+    static constexpr int STAGES = 2, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, W>();
+    static constexpr int OFF_G = QT, OFF_K = 2 * QT, OFF_V = OFF_K + STAGES * TILE, SMEM = OFF_V + STAGES * TILE + 1024;
+    static constexpr int T_DP = W, T_DS = 2 * W, T_DQ = 2 * W + W / 2, COLS = pow2_cols(T_DQ + DH);  // columns of dP, dS and dQ behind S
 };
 
-template <int DH, bool BF>
-__global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
+template <int DH, bool BF, int W>
+__global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_attn_dq_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
                                                                     const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                                                                     const SeqAttn a, const float c, float *delta) {
-    using L = DqLayout<DH>;
+    using L = DqLayout<DH, W>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
     constexpr int ST = L::STAGES;
     extern __shared__ uint8_t raw[];
@@ -53,6 +54,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
     __shared__ float part[2][SQ_ROWS];
     __shared__ uint8_t odd_rows[2][SQ_ROWS];
     const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
+    uint8_t *smp = raw + (sm - s_addr(raw));
     const auto k_full = [&](int s) { return bar0 + 8 * s; };
     const auto k_free = [&](int s) { return bar0 + 8 * (ST + s); };
     const auto v_full = [&](int s) { return bar0 + 8 * (2 * ST + s); };
@@ -68,12 +70,12 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 9) tmem_alloc<512>(s_addr(&tslot));
+    if (warp == 9) tmem_alloc<L::COLS>(s_addr(&tslot));
     pdl_grid_wait();
     Span keys{0, 0};
     bool in = false;
     if (warp < 8) {
-        keys = keys_of_query(a, row, in);
+        keys = keys_of_lane(a, row - lane, in);
         const bool some = keys.hi > keys.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? keys.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? keys.hi : 0);
         if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi;
@@ -83,7 +85,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
     tc_fence_after();
     const uint32_t tS = tslot, tP = tS + L::T_DP, tD = tS + L::T_DS, tO = tS + L::T_DQ;
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
-    const int nt = end > first ? (end - first + SQ_ROWS - 1) / SQ_ROWS : 0;
+    const int nt = end > first ? (end - first + W - 1) / W : 0;
     const SqWaits wait{&failed, a.status};
 
     if (warp == 8) {
@@ -92,15 +94,15 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
             sq_load<DH>(sm + L::OFF_G, &tg, h, tile * SQ_ROWS, q_full);
             int j = 0;
             for (; j < nt; j++) {
-                const int s = j % ST, at = end - SQ_ROWS * (j + 1);
+                const int s = j % ST, at = end - W * (j + 1);
                 const uint32_t ph = (uint32_t)(j / ST - 1) & 1;
                 if (j >= ST && !wait(k_free(s), ph)) break;
-                sq_load<DH>(sm + L::OFF_K + s * L::TILE, &tk, hk, at, k_full(s));
+                sq_load<DH, W>(sm + L::OFF_K + s * L::TILE, &tk, hk, at, k_full(s));
                 if (j >= ST && !wait(v_free(s), ph)) {
                     wait(k_full(s), (uint32_t)(j / ST) & 1);  // in flight
                     break;
                 }
-                sq_load<DH>(sm + L::OFF_V + s * L::TILE, &tv, hk, at, v_full(s));
+                sq_load<DH, W>(sm + L::OFF_V + s * L::TILE, &tv, hk, at, v_full(s));
             }
             if (failed) {  // copies in flight land before the block ends
                 wait(q_full, 0);
@@ -118,10 +120,10 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
                     if (!(ok = wait(k_full(s), ph) && wait(v_full(s), ph))) break;
                     tc_fence_after();
 #pragma unroll
-                    for (int k = 0; k < DH / 16; k++) mma_f16(tS, sq_k(sm, k), sq_k(sm + L::OFF_K + s * L::TILE, k), sq_idesc(128, BF, false), k > 0);
+                    for (int k = 0; k < DH / 16; k++) mma_f16(tS, sq_k(sm, k), sq_k<W>(sm + L::OFF_K + s * L::TILE, k), sq_idesc(W, BF, false), k > 0);
 #pragma unroll
                     for (int k = 0; k < DH / 16; k++)
-                        mma_f16(tP, sq_k(sm + L::OFF_G, k), sq_k(sm + L::OFF_V + s * L::TILE, k), sq_idesc(128, BF, false), k > 0);
+                        mma_f16(tP, sq_k(sm + L::OFF_G, k), sq_k<W>(sm + L::OFF_V + s * L::TILE, k), sq_idesc(W, BF, false), k > 0);
                     mma_commit(v_free(s));
                     mma_commit(sp_full);
                 }
@@ -130,8 +132,8 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
                     if (!(ok = wait(ds_full, (uint32_t)i & 1))) break;
                     tc_fence_after();
 #pragma unroll
-                    for (int k = 0; k < SQ_ROWS / 16; k++)
-                        mma_f16_ta(tO, tD + 8 * k, sq_mn(sm + L::OFF_K + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(i | k));
+                    for (int k = 0; k < W / 16; k++)
+                        mma_f16_ta(tO, tD + 8 * k, sq_mn<W>(sm + L::OFF_K + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(i | k));
                     mma_commit(k_free(s));
                     mma_commit(ds_free);
                 }
@@ -162,24 +164,29 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
         for (int j = 0; j < nt; j++) {
             if (!(ok = wait(sp_full, (uint32_t)j & 1))) break;
             tc_fence_after();
-            uint32_t s[2][32], p[2][32];
-            tmem_ld32(tS + lanes + 64 * half, s[0]);
-            tmem_ld32(tS + lanes + 64 * half + 32, s[1]);
-            tmem_ld32(tP + lanes + 64 * half, p[0]);
-            tmem_ld32(tP + lanes + 64 * half + 32, p[1]);
-            tmem_wait_ld();
+            const int at = end - W * (j + 1) + W / 2 * half, lo = keys.lo - at, hi = keys.hi - at;
+            const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= W / 2), some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
+            uint32_t s[W / 64][32], p[W / 64][32];
+            if (some) {
+#pragma unroll
+                for (int b = 0; b < W / 64; b++) {
+                    tmem_ld32(tS + lanes + W / 2 * half + 32 * b, s[b]);
+                    tmem_ld32(tP + lanes + W / 2 * half + 32 * b, p[b]);
+                }
+                tmem_wait_ld();
+            }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(sp_free);
-            const int at = end - SQ_ROWS * (j + 1) + 64 * half, lo = keys.lo - at, hi = keys.hi - at;
-            const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= 64);
             if (j && !(ok = wait(ds_free, (uint32_t)(j - 1) & 1))) break;
 #pragma unroll
-            for (int b = 0; b < 2; b++) {
+            for (int b = 0; b < W / 64; b++) {
                 const uint32_t see = all ? 0xFFFFFFFFu : sq_bits(lo - 32 * b, hi - 32 * b);
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
+                    w[i] = 0;
+                    if (!some) continue;
                     float x, y, u, v;
                     f4_untwo(sq_fma2(f4_two(__uint_as_float(s[b][2 * i]), __uint_as_float(s[b][2 * i + 1])), c2, l2), x, y);
                     const unsigned long long t = f4_add2(f4_two(__uint_as_float(p[b][2 * i]), __uint_as_float(p[b][2 * i + 1])), d2);
@@ -187,7 +194,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
                     if (!all) u = (see >> (2 * i)) & 1u ? u : 0.0f, v = (see >> (2 * i + 1)) & 1u ? v : 0.0f;
                     w[i] = sq_pack<BF>(u, v);
                 }
-                tmem_st16(tD + lanes + 32 * half + 16 * b, w);
+                tmem_st16(tD + lanes + W / 4 * half + 16 * b, w);
             }
             tmem_wait_st();
             tc_fence_before();
@@ -198,22 +205,22 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
         tc_fence_after();
         bool odd = false;
         if (ok) {
-            T *o = static_cast<T *>(a.dq.p) + row * a.dq.ld + h * a.dq.hd;
+            uint32_t out[DH / 4];
 #pragma unroll
             for (int b = 0; b < DH / 64; b++) {
-                const int c0 = half * (DH / 2) + 32 * b;
                 uint32_t w[32];
-                float v[32];
-                if (nt) tmem_ld32(tO + lanes + c0, w);
+                if (nt) tmem_ld32(tO + lanes + half * (DH / 2) + 32 * b, w);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; i++) {
-                    const float x = nt && !none ? __uint_as_float(w[i]) : 0.0f;
-                    odd |= !(fabsf(x) < INFINITY);
-                    v[i] = x * a.scale;
+                for (int i = 0; i < 16; i++) {
+                    const float x = nt && !none ? __uint_as_float(w[2 * i]) : 0.0f, y = nt && !none ? __uint_as_float(w[2 * i + 1]) : 0.0f;
+                    odd |= !(fabsf(x) < INFINITY) || !(fabsf(y) < INFINITY);
+                    out[16 * b + i] = sq_pack<BF>(x * a.scale, y * a.scale);
                 }
-                if (in) sq_store<BF>(o, c0, a.dh, v);
             }
+            // the queries have been multiplied: their rows are free
+            sq_store_rows<DH / 2>(smp + warp * (32 * DH), out, static_cast<uint16_t *>(a.dq.p) + (long)(row - lane) * a.dq.ld + h * a.dq.hd + half * (DH / 2),
+                                  a.dq.ld, __ballot_sync(0xFFFFFFFFu, in), a.dh - half * (DH / 2));
         }
         odd_rows[half][rt] = odd;
         elements_sync();
@@ -231,23 +238,24 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dq_kernel(const __grid
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) tmem_free<512>(tslot);
+    if (warp == 9) tmem_free<L::COLS>(tslot);
 }
 
 // --------------------------------------------------------------------------- dk, dv
-template <int DH>
+template <int DH, int W>
 struct DkvLayout {
-    static constexpr int STAGES = DH == 64 ? 3 : 2, TILE = sq_bytes<DH>();
-    // K and V, stages of Q and G, stages of -lse log2 e and -D of 128 queries
-    static constexpr int OFF_V = TILE, OFF_Q = 2 * TILE, OFF_G = OFF_Q + STAGES * TILE, OFF_N = OFF_G + STAGES * TILE, SMEM = OFF_N + STAGES * 1024 + 1024;
-    static constexpr int T_DP = 128, T_DV = 256, T_DK = 256 + DH;
+    static constexpr int STAGES = DH == 64 ? 3 : 2, KT = sq_bytes<DH>(), TILE = sq_bytes<DH, W>(), NUM = 8 * W;
+    // K and V, stages of Q and G, stages of -lse log2 e and -D of W queries
+    static constexpr int OFF_V = KT, OFF_Q = 2 * KT, OFF_G = OFF_Q + STAGES * TILE, OFF_N = OFF_G + STAGES * TILE, SMEM = OFF_N + STAGES * NUM + 1024;
+    static constexpr int T_DP = W, T_DV = 2 * W, T_DK = 2 * W + DH, COLS = pow2_cols(2 * W + 2 * DH);
+    static_assert(OFF_N >= 2 * SQ_ROWS * DH * 4, "a CTA's sums for its cluster");
 };
 
-template <int DH, bool BF>
-__global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
+template <int DH, bool BF, int W>
+__global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_attn_dkv_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                                                                      const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
                                                                      const SeqAttn a, const float c, const float *delta, const int ctas) {
-    using L = DkvLayout<DH>;
+    using L = DkvLayout<DH, W>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
     constexpr int ST = L::STAGES;
     extern __shared__ uint8_t raw[];
@@ -273,12 +281,12 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 9) tmem_alloc<512>(s_addr(&tslot));
+    if (warp == 9) tmem_alloc<L::COLS>(s_addr(&tslot));
     pdl_grid_wait();
     Span qs{0, 0};
     bool in = false;
     if (warp < 8) {
-        qs = queries_of_key(a, row, in);
+        qs = queries_of_lane(a, row - lane, in);
         const bool some = qs.hi > qs.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? qs.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? qs.hi : 0);
         if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi;
@@ -288,7 +296,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
     tc_fence_after();
     const uint32_t tS = tslot, tP = tS + L::T_DP, tV = tS + L::T_DV, tK = tS + L::T_DK;
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
-    const int nt = end > first ? (end - first + SQ_ROWS - 1) / SQ_ROWS : 0;  // tiles of one head
+    const int nt = end > first ? (end - first + W - 1) / W : 0;  // tiles of one head
     // this CTA's steps of the walk over all heads: n of them from step0 on
     const int step0 = (int)((long)nt * heads * share / ctas), n = (int)((long)nt * heads * (share + 1) / ctas) - step0;
     const int head0 = nt ? step0 / nt : 0, t0 = step0 - head0 * nt;
@@ -303,19 +311,19 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
             int j = 0, h = h0 + head0, t = t0;
             bool ok = true;
             for (; j < n; j++) {
-                const int s = j % ST, at = end - SQ_ROWS * (t + 1);
+                const int s = j % ST, at = end - W * (t + 1);
                 const uint32_t ph = (uint32_t)(j / ST - 1) & 1;
                 if (j >= ST) ok = wait(q_free(s), ph);
                 if (!__all_sync(0xFFFFFFFFu, ok)) break;
-                if (lane == 0) sq_load<DH>(sm + L::OFF_Q + s * L::TILE, &tq, h, at, q_full(s));
+                if (lane == 0) sq_load<DH, W>(sm + L::OFF_Q + s * L::TILE, &tq, h, at, q_full(s));
                 // -lse log2 e and -D of the tile's queries
-                float *num = reinterpret_cast<float *>(smp + L::OFF_N + s * 1024);
+                float *num = reinterpret_cast<float *>(smp + L::OFF_N + s * L::NUM);
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
+                for (int i = 0; i < W / 32; i++) {
                     const int r = at + 32 * i + lane;
                     const bool on = r >= 0 && r < a.q_rows;
                     num[32 * i + lane] = on ? -LOG2E * __ldg(a.lse + (long)h * a.q_rows + r) : 0.0f;
-                    num[128 + 32 * i + lane] = on ? -delta[(long)h * a.q_rows + r] : 0.0f;
+                    num[W + 32 * i + lane] = on ? -delta[(long)h * a.q_rows + r] : 0.0f;
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full(s));
@@ -324,7 +332,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
                     wait(q_full(s), (uint32_t)(j / ST) & 1);  // in flight
                     break;
                 }
-                if (lane == 0) sq_load<DH>(sm + L::OFF_G + s * L::TILE, &tg, h, at, g_full(s));
+                if (lane == 0) sq_load<DH, W>(sm + L::OFF_G + s * L::TILE, &tg, h, at, g_full(s));
                 if (++t == nt) t = 0, h++;
             }
             if (failed) {  // copies in flight land before the block ends
@@ -340,7 +348,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
                 if (!wait(q_full(s), (uint32_t)(j / ST) & 1)) return false;
                 tc_fence_after();
 #pragma unroll
-                for (int k = 0; k < DH / 16; k++) mma_f16(tS, sq_k(sm, k), sq_k(sm + L::OFF_Q + s * L::TILE, k), sq_idesc(128, BF, false), k > 0);
+                for (int k = 0; k < DH / 16; k++) mma_f16(tS, sq_k(sm, k), sq_k<W>(sm + L::OFF_Q + s * L::TILE, k), sq_idesc(W, BF, false), k > 0);
                 mma_commit(s_full);
                 return true;
             };
@@ -350,7 +358,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < DH / 16; k++)
-                    mma_f16(tP, sq_k(sm + L::OFF_V, k), sq_k(sm + L::OFF_G + s * L::TILE, k), sq_idesc(128, BF, false), k > 0);
+                    mma_f16(tP, sq_k(sm + L::OFF_V, k), sq_k<W>(sm + L::OFF_G + s * L::TILE, k), sq_idesc(W, BF, false), k > 0);
                 mma_commit(dp_full);
                 return true;
             };
@@ -360,15 +368,15 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
                 if (!(ok = wait(p_full, (uint32_t)j & 1))) break;
                 tc_fence_after();
 #pragma unroll
-                for (int k = 0; k < SQ_ROWS / 16; k++)  // a row's two threads write 32 columns each, 64 apart
-                    mma_f16_ta(tV, tS + 8 * (k & 3) + 64 * (k >> 2), sq_mn(sm + L::OFF_G + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                for (int k = 0; k < W / 16; k++)  // a row's two threads write W / 4 columns each, W / 2 apart
+                    mma_f16_ta(tV, tS + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), sq_mn<W>(sm + L::OFF_G + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
                 mma_commit(g_free(s));
                 if (j + 1 < n && !(ok = scores(j + 1))) break;
                 if (!(ok = wait(ds_full, (uint32_t)j & 1))) break;
                 tc_fence_after();
 #pragma unroll
-                for (int k = 0; k < SQ_ROWS / 16; k++)
-                    mma_f16_ta(tK, tP + 8 * (k & 3) + 64 * (k >> 2), sq_mn(sm + L::OFF_Q + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                for (int k = 0; k < W / 16; k++)
+                    mma_f16_ta(tK, tP + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), sq_mn<W>(sm + L::OFF_Q + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
                 mma_commit(q_free(s));
                 if (j + 1 < n && !(ok = weights(j + 1))) break;
             }
@@ -381,21 +389,25 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
         const unsigned long long c2 = f4_two(c, c);
         bool ok = true;
         for (int j = 0, t = t0; j < n; j++) {
-            const int s = j % ST, at = end - SQ_ROWS * (t + 1) + 64 * half, lo = qs.lo - at, hi = qs.hi - at;
+            const int s = j % ST, at = end - W * (t + 1) + W / 2 * half, lo = qs.lo - at, hi = qs.hi - at;
             if (++t == nt) t = 0;
-            const float4 *num = reinterpret_cast<const float4 *>(smp + L::OFF_N + s * 1024) + 16 * half;
-            const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= 64);
-            const uint32_t see[2] = {all ? 0xFFFFFFFFu : sq_bits(lo, hi), all ? 0xFFFFFFFFu : sq_bits(lo - 32, hi - 32)};
+            const float4 *num = reinterpret_cast<const float4 *>(smp + L::OFF_N + s * L::NUM) + W / 8 * half;
+            const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= W / 2), some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
+            uint32_t see[W / 64];
+#pragma unroll
+            for (int b = 0; b < W / 64; b++) see[b] = all ? 0xFFFFFFFFu : sq_bits(lo - 32 * b, hi - 32 * b);
             // the producer's numbers are visible with the tile that they came with
             if (!(ok = wait(s_full, (uint32_t)j & 1) && wait(q_full(s), (uint32_t)(j / ST) & 1))) break;
             tc_fence_after();
-            uint32_t r[2][32];
-            load64(tS + lanes + 64 * half, r);
+            uint32_t r[W / 64][32];
+            if (some) load_half<W>(tS + lanes + W / 2 * half, r);
 #pragma unroll
-            for (int b = 0; b < 2; b++) {
+            for (int b = 0; b < W / 64; b++) {
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
+                    w[2 * i] = w[2 * i + 1] = 0;
+                    if (!some) continue;
                     const float4 x = num[8 * b + i];
                     float p[4];
                     f4_untwo(sq_fma2(f4_two(__uint_as_float(r[b][4 * i]), __uint_as_float(r[b][4 * i + 1])), c2, f4_two(x.x, x.y)), p[0], p[1]);
@@ -408,7 +420,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
                     }
                     w[2 * i] = sq_pack<BF>(p[0], p[1]), w[2 * i + 1] = sq_pack<BF>(p[2], p[3]);
                 }
-                tmem_st16(tS + lanes + 64 * half + 16 * b, w);
+                tmem_st16(tS + lanes + W / 2 * half + 16 * b, w);
             }
             tmem_wait_st();
             tc_fence_before();
@@ -416,14 +428,16 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
             if (lane == 0) mbar_arrive(p_full);
             if (!(ok = wait(dp_full, (uint32_t)j & 1))) break;
             tc_fence_after();
-            uint32_t q[2][32];
-            load64(tP + lanes + 64 * half, q);
+            uint32_t q[W / 64][32];
+            if (some) load_half<W>(tP + lanes + W / 2 * half, q);
 #pragma unroll
-            for (int b = 0; b < 2; b++) {
+            for (int b = 0; b < W / 64; b++) {
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const float4 x = num[32 + 8 * b + i];
+                    w[2 * i] = w[2 * i + 1] = 0;
+                    if (!some) continue;
+                    const float4 x = num[W / 4 + 8 * b + i];
                     float d[4];
                     f4_untwo(f4_mul2(f4_two(__uint_as_float(r[b][4 * i]), __uint_as_float(r[b][4 * i + 1])),
                                      f4_add2(f4_two(__uint_as_float(q[b][4 * i]), __uint_as_float(q[b][4 * i + 1])), f4_two(x.x, x.y))),
@@ -437,7 +451,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
                     }
                     w[2 * i] = sq_pack<BF>(d[0], d[1]), w[2 * i + 1] = sq_pack<BF>(d[2], d[3]);
                 }
-                tmem_st16(tP + lanes + 64 * half + 16 * b, w);
+                tmem_st16(tP + lanes + W / 2 * half + 16 * b, w);
             }
             tmem_wait_st();
             tc_fence_before();
@@ -454,24 +468,26 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
         int c0 = 0, c1 = DH;  // the columns that this CTA stores
         if (ctas == 1) {
             if (ok) {
+                uint32_t out[DH / 2];
 #pragma unroll
                 for (int b = 0; b < DH / 32; b++) {
                     uint32_t w[32];
-                    float v[32];
                     if (n) tmem_ld32((half ? tK : tV) + lanes + 32 * b, w);
                     tmem_wait_ld();
+                    const bool any = n && qs.hi > qs.lo;
 #pragma unroll
-                    for (int i = 0; i < 32; i++) {
-                        const float y = n && qs.hi > qs.lo ? __uint_as_float(w[i]) : 0.0f;
-                        odd |= !(fabsf(y) < INFINITY);
-                        v[i] = y * f;
+                    for (int i = 0; i < 16; i++) {
+                        const float y = any ? __uint_as_float(w[2 * i]) : 0.0f, z = any ? __uint_as_float(w[2 * i + 1]) : 0.0f;
+                        odd |= !(fabsf(y) < INFINITY) || !(fabsf(z) < INFINITY);
+                        out[16 * b + i] = sq_pack<BF>(y * f, z * f);
                     }
-                    if (in) sq_store<BF>(o, 32 * b, a.dh, v);
                 }
+                // the keys and values have been multiplied: their rows are free
+                sq_store_rows<DH>(smp + warp * (64 * DH), out, reinterpret_cast<uint16_t *>(o) - lane * x.ld, x.ld, __ballot_sync(0xFFFFFFFFu, in), a.dh);
             }
         } else {
-            // sums of this CTA's steps to shared memory, where the ring was: four columns of a row side by side
-            float4 *mine = reinterpret_cast<float4 *>(smp + L::OFF_Q) + half * (DH / 4) * SQ_ROWS + rt;
+            // sums of this CTA's steps to shared memory, where the tiles were: four columns of a row side by side
+            float4 *mine = reinterpret_cast<float4 *>(smp) + half * (DH / 4) * SQ_ROWS + rt;
 #pragma unroll
             for (int b = 0; b < DH / 32; b++) {
                 uint32_t w[32];
@@ -537,7 +553,7 @@ __global__ void __launch_bounds__(BW_THREADS, 1) seq_attn_dkv_kernel(const __gri
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) tmem_free<512>(tslot);
+    if (warp == 9) tmem_free<L::COLS>(tslot);
 }
 
 // Where there are no queries or no keys at all, gradients of rows in sequences are zero.
@@ -550,11 +566,11 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     bool in;
     if (a.k_rows == 0) {
         if (w >= a.q_rows) return;
-        keys_of_query(a, (int)w, in);
+        keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hq; h++) store4(static_cast<T *>(a.dq.p) + w * a.dq.ld + h * a.dq.hd + 4 * lane, z);
     } else {
         if (w >= a.k_rows) return;
-        queries_of_key(a, (int)w, in);
+        queries_of_key(a, (int)w, seq_of(a.k_start, a.n_seqs, (int)w), in);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hkv; h++) {
             store4(static_cast<T *>(a.dk.p) + w * a.dk.ld + h * a.dk.hd + 4 * lane, z);
             store4(static_cast<T *>(a.dv.p) + w * a.dv.ld + h * a.dv.hd + 4 * lane, z);
@@ -571,35 +587,42 @@ int dkv_ctas(long tiles, const SeqAttn &a) {
     return p;
 }
 
-template <int DH, bool BF>
+template <int DH, bool BF, int W>
 cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
-    CUtensorMap tq, tk, tv, tg;
-    if (!sq_map(&tq, a.q, a.q_rows, a.hq, a.dh) || !sq_map(&tg, a.g, a.q_rows, a.hq, a.dh) || !sq_map(&tk, a.k, a.k_rows, a.hkv, a.dh) ||
-        !sq_map(&tv, a.v, a.k_rows, a.hkv, a.dh))
+    // whole tiles of the rows that stay, tiles of W rows of those that are walked
+    CUtensorMap tq, tk, tv, tg, wq, wk, wv, wg;
+    if (!sq_map(&tq, a.q, a.q_rows, a.hq, a.dh, SQ_ROWS) || !sq_map(&tg, a.g, a.q_rows, a.hq, a.dh, SQ_ROWS) ||
+        !sq_map(&tk, a.k, a.k_rows, a.hkv, a.dh, SQ_ROWS) || !sq_map(&tv, a.v, a.k_rows, a.hkv, a.dh, SQ_ROWS))
         return cudaErrorInvalidValue;
+    if (W == SQ_ROWS) {
+        wq = tq, wk = tk, wv = tv, wg = tg;
+    } else if (!sq_map(&wq, a.q, a.q_rows, a.hq, a.dh, W) || !sq_map(&wg, a.g, a.q_rows, a.hq, a.dh, W) || !sq_map(&wk, a.k, a.k_rows, a.hkv, a.dh, W) ||
+               !sq_map(&wv, a.v, a.k_rows, a.hkv, a.dh, W)) {
+        return cudaErrorInvalidValue;
+    }
     float *delta = static_cast<float *>(a.workspace);
     const float c = a.scale * LOG2E;
     const unsigned qt = (unsigned)((a.q_rows + SQ_ROWS - 1) / SQ_ROWS), kt = (unsigned)((a.k_rows + SQ_ROWS - 1) / SQ_ROWS);
-    const cudaError_t e = launch_pdl(seq_attn_dq_kernel<DH, BF>, qt * a.hq, BW_THREADS, DqLayout<DH>::SMEM, st, tq, tg, tk, tv, a, c, delta);
+    const cudaError_t e = launch_pdl(seq_attn_dq_kernel<DH, BF, W>, qt * a.hq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta);
     if (e != cudaSuccess) return e;
     const int ctas = dkv_ctas(kt, a);
-    return sq_launch(seq_attn_dkv_kernel<DH, BF>, kt * a.hkv * ctas, ctas, BW_THREADS, DkvLayout<DH>::SMEM, st, tk, tv, tq, tg, a, c, (const float *)delta,
-                     ctas);
+    return sq_launch(seq_attn_dkv_kernel<DH, BF, W>, kt * a.hkv * ctas, ctas, BW_THREADS, DkvLayout<DH, W>::SMEM, st, tk, tv, wq, wg, a, c,
+                     (const float *)delta, ctas);
 }
 
-template <int DH, bool BF>
+template <int DH, bool BF, int W>
 cudaError_t tile_init() {
-    const cudaError_t e = cudaFuncSetAttribute(seq_attn_dq_kernel<DH, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<DH>::SMEM);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(seq_attn_dkv_kernel<DH, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, DkvLayout<DH>::SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(seq_attn_dq_kernel<DH, BF, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<DH, W>::SMEM);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(seq_attn_dkv_kernel<DH, BF, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, DkvLayout<DH, W>::SMEM);
 }
 
 }  // namespace
 
 cudaError_t seq_attn_backward_init() {
-    cudaError_t e = tile_init<64, true>();
-    if (e == cudaSuccess) e = tile_init<64, false>();
-    if (e == cudaSuccess) e = tile_init<128, true>();
-    if (e == cudaSuccess) e = tile_init<128, false>();
+    cudaError_t e = tile_init<64, true, 64>();
+    if (e == cudaSuccess) e = tile_init<64, false, 64>();
+    if (e == cudaSuccess) e = tile_init<128, true, 128>();
+    if (e == cudaSuccess) e = tile_init<128, false, 128>();
     return e;
 }
 
@@ -609,8 +632,8 @@ cudaError_t launch_seq_attn_backward(const SeqAttn &a, cudaStream_t st) {
     const bool bf = a.dtype == MNMT_BF16;
     if (a.q_rows == 0 || a.k_rows == 0)
         return launch_pdl(bf ? seq_attn_zero_kernel<__nv_bfloat16> : seq_attn_zero_kernel<__half>, (unsigned)((a.q_rows + a.k_rows + 7) / 8), 256, 0, st, a);
-    if (a.dh <= 64) return bf ? tile_backward<64, true>(a, st) : tile_backward<64, false>(a, st);
-    return bf ? tile_backward<128, true>(a, st) : tile_backward<128, false>(a, st);
+    if (a.dh > 64) return bf ? tile_backward<128, true, 128>(a, st) : tile_backward<128, false, 128>(a, st);
+    return bf ? tile_backward<64, true, 64>(a, st) : tile_backward<64, false, 64>(a, st);
 }
 
 }  // namespace mnmt

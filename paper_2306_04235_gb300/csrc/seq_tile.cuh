@@ -12,35 +12,36 @@
 
 namespace mnmt {
 
-constexpr int SQ_ROWS = 128;                 // rows of a tile
-constexpr int SQ_BOX = SQ_ROWS * 128;        // bytes of a box
-template <int DH>
-__host__ __device__ constexpr int sq_bytes() { return DH / 64 * SQ_BOX; }
+constexpr int SQ_ROWS = 128;  // rows of a tile
+template <int DH, int ROWS = SQ_ROWS>
+__host__ __device__ constexpr int sq_bytes() { return DH / 64 * ROWS * 128; }
 
 // dimensions {element, head, row}: the coordinates of a box may start at a negative row or end past the last (zeros)
-inline bool sq_map(CUtensorMap *tm, const HeadRows &x, int rows, int heads, int dh) {
+inline bool sq_map(CUtensorMap *tm, const HeadRows &x, int rows, int heads, int dh, int box_rows) {
     cuuint64_t dims[3] = {(cuuint64_t)dh, (cuuint64_t)heads, (cuuint64_t)rows}, strides[2] = {(cuuint64_t)x.hd * 2, (cuuint64_t)x.ld * 2};
-    cuuint32_t box[3] = {64, 1, SQ_ROWS}, estr[3] = {1, 1, 1};
+    cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows}, estr[3] = {1, 1, 1};
     return tma_encoder()(tm, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, x.p, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // the tile from row on of a head (one thread): completes on bar, which expects sq_bytes<DH>()
-template <int DH>
+template <int DH, int ROWS = SQ_ROWS>
 __device__ __forceinline__ void sq_load(uint32_t dst, const CUtensorMap *tm, int head, int row, uint32_t bar) {
-    mbar_expect_tx(bar, sq_bytes<DH>());
+    mbar_expect_tx(bar, sq_bytes<DH, ROWS>());
 #pragma unroll
     for (int b = 0; b < DH / 64; b++)
         asm volatile(
-            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst + b * SQ_BOX),
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst + b * ROWS * 128),
             "l"(reinterpret_cast<uint64_t>(tm)), "r"(64 * b), "r"(head), "r"(row), "r"(bar)
             : "memory");
 }
 
 // descriptors of 16 reduction indices: K-major step k of the head's elements, MN-major step k of the rows
-__device__ __forceinline__ uint64_t sq_k(uint32_t tile, int k) { return sw128_desc(tile + (k >> 2) * SQ_BOX + (k & 3) * 32); }
+template <int ROWS = SQ_ROWS>
+__device__ __forceinline__ uint64_t sq_k(uint32_t tile, int k) { return sw128_desc(tile + (k >> 2) * (ROWS * 128) + (k & 3) * 32); }
+template <int ROWS = SQ_ROWS>
 __device__ __forceinline__ uint64_t sq_mn(uint32_t tile, int k) {
-    return (uint64_t)(((tile + k * 2048) >> 4) & 0x3FFFu) | ((uint64_t)(SQ_BOX >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+    return (uint64_t)(((tile + k * 2048) >> 4) & 0x3FFFu) | ((uint64_t)((ROWS * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
            ((uint64_t)2 << 61);
 }
 // kind::f16, D fp32 of 128 x n; bf: bf16 operands; b_mn: B is MN-major
@@ -92,6 +93,30 @@ __device__ __forceinline__ void sq_store(void *row, int c0, int dh, const float 
         if (c0 + c < dh)
             *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(row) + c0 + c) =
                 make_uint4(sq_pack<BF>(v[c], v[c + 1]), sq_pack<BF>(v[c + 2], v[c + 3]), sq_pack<BF>(v[c + 4], v[c + 5]), sq_pack<BF>(v[c + 6], v[c + 7]));
+}
+
+// COLS elements (16-bit, packed two to a word) of a warp's 32 rows, a row per lane, stored through
+// `stage` (32 rows of 2 COLS bytes of the warp's own, 16-byte pieces at piece ^ row) so that
+// lanes next to each other store what is next to each other (a row's pieces from its own lane:
+// an instruction to 32 rows, and twice the time of the rest of a short sequence's epilogue).
+// live: the rows to store; n: elements of a row, a multiple of 8.
+template <int COLS>
+__device__ __forceinline__ void sq_store_rows(uint8_t *stage, const uint32_t (&w)[COLS / 2], uint16_t *row0, long ld, uint32_t live, int n) {
+    constexpr int P = COLS / 8;  // pieces of a row
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int c = 0; c < P; c++)
+        *reinterpret_cast<uint4 *>(stage + lane * (16 * P) + 16 * ((c & ~7) | ((c ^ lane) & (P < 8 ? P - 1 : 7)))) =
+            make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+        const int r = i * (32 / P) + lane / P, c = lane % P;
+        if (((live >> r) & 1u) && 8 * c < n)
+            *reinterpret_cast<uint4 *>(row0 + r * ld + 8 * c) =
+                *reinterpret_cast<const uint4 *>(stage + r * (16 * P) + 16 * ((c & ~7) | ((c ^ r) & (P < 8 ? P - 1 : 7))));
+    }
+    __syncwarp();
 }
 
 // all threads of the cluster, whole warps
