@@ -23,9 +23,10 @@ constexpr int FW_THREADS = 192;  // four softmax warps, a TMA warp, an MMA warp
 // KT: keys of a tile; BLOCKS: CTAs per SM
 template <int DH, int KT>
 struct FwLayout {
-    static constexpr int STAGES = DH == 64 ? 2 : 1, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, KT>();
+    static constexpr int STAGES = 2, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, KT>();
     static constexpr int OFF_K = QT, OFF_V = OFF_K + STAGES * TILE, SMEM = OFF_V + STAGES * TILE + 1024;
-    static constexpr int COLS = pow2_cols(KT + DH), BLOCKS = 512 / COLS;
+    static constexpr bool APART = DH + KT > 128;  // P beside S
+    static constexpr int T_P = APART ? KT : 0, T_O = KT + (APART ? KT / 2 : 0), COLS = pow2_cols(T_O + DH), BLOCKS = 512 / COLS;
 };
 constexpr float FW_SLACK = 8.0f;  // how far, in powers of two, a score may exceed m
 
@@ -36,17 +37,17 @@ __device__ __forceinline__ void hide(uint32_t (&r)[32], uint32_t see) {
 }
 __device__ __forceinline__ void max32(const uint32_t (&r)[32], float (&mx)[4]) {
 #pragma unroll
-    for (int i = 0; i < 32; i++) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(r[i]));
+    for (int i = 0; i < 32; i += 2) mx[i / 2 & 3] = fmaxf(fmaxf(mx[i / 2 & 3], __uint_as_float(r[i])), __uint_as_float(r[i + 1]));
 }
 // their weights 2^(c s - m), packed; sums in ls
 template <bool BF>
-__device__ __forceinline__ void weigh(const uint32_t (&r)[32], unsigned long long c2, unsigned long long m2, float (&ls)[2], uint32_t (&p)[16]) {
+__device__ __forceinline__ void weigh(const uint32_t (&r)[32], unsigned long long c2, unsigned long long m2, unsigned long long &ls, uint32_t (&p)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; i++) {
         float x, y;
         f4_untwo(sq_fma2(f4_two(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), c2, m2), x, y);
         x = exp2_fast(x), y = exp2_fast(y);
-        ls[0] += x, ls[1] += y;
+        ls = f4_add2(ls, f4_two(x, y));
         p[i] = sq_pack<BF>(x, y);
     }
 }
@@ -59,7 +60,7 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
     constexpr int ST = L::STAGES;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[4 * ST + 4];
+    __shared__ __align__(8) uint64_t bars[4 * ST + 6];
     __shared__ uint32_t tslot;
     __shared__ int failed, span[2][4];
     const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
@@ -68,13 +69,15 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
     const auto k_free = [&](int s) { return bar0 + 8 * (ST + s); };
     const auto v_full = [&](int s) { return bar0 + 8 * (2 * ST + s); };
     const auto v_free = [&](int s) { return bar0 + 8 * (3 * ST + s); };
-    const uint32_t q_full = bar0 + 8 * (4 * ST), s_full = q_full + 8, p_full = q_full + 16, o_full = q_full + 24;
+    const uint32_t q_full = bar0 + 8 * (4 * ST), s_full = q_full + 8, p_full = q_full + 16, o_full = q_full + 24, s_read = q_full + 32,
+                   pv_done = q_full + 40;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int h = blockIdx.x % a.hq, tile = (int)(gridDim.x / a.hq) - 1 - (int)(blockIdx.x / a.hq);  // the last rows (causal: the longest) first
     const int row = tile * SQ_ROWS + (int)threadIdx.x;
     if (threadIdx.x == 128) {
         for (int s = 0; s < ST; s++) mbar_init(k_full(s), 1), mbar_init(k_free(s), 1), mbar_init(v_full(s), 1), mbar_init(v_free(s), 1);
-        mbar_init(q_full, 1), mbar_init(s_full, 1), mbar_init(p_full, 4), mbar_init(o_full, 1);
+        mbar_init(q_full, 1), mbar_init(s_full, 1), mbar_init(p_full, 4), mbar_init(o_full, 1), mbar_init(s_read, 4),
+            mbar_init(pv_done, 1);
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -92,7 +95,7 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tS = tslot, tO = tslot + KT;
+    const uint32_t tS = tslot, tP = tslot + L::T_P, tO = tslot + L::T_O;
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
     const int nt = end > first ? (end - first + KT - 1) / KT : 0;
     const SqWaits wait{&failed, a.status};
@@ -119,30 +122,36 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
         }
     } else if (warp == 5) {
         if (lane == 0 && nt) {
-            bool ok = wait(q_full, 0);
-            for (int j = 0; j < nt && ok; j++) {
+            const auto scores = [&](int j) {  // S(j)
                 const int s = j % ST;
-                const uint32_t ph = (uint32_t)(j / ST) & 1;
-                if (!(ok = wait(k_full(s), ph))) break;
+                if (!wait(k_full(s), (uint32_t)(j / ST) & 1)) return false;
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < DH / 16; k++)
                     mma_f16(tS, sq_k(sm, k), sq_k<KT>(sm + L::OFF_K + s * L::TILE, k), sq_idesc(KT, BF, false), k > 0);
                 mma_commit(k_free(s));
                 mma_commit(s_full);
-                if (!(ok = wait(p_full, (uint32_t)j & 1) && wait(v_full(s), ph))) break;
+                return true;
+            };
+            bool ok = wait(q_full, 0) && scores(0);
+            for (int j = 0; j < nt && ok; j++) {
+                const int s = j % ST;
+                if (L::APART && j + 1 < nt && !(ok = wait(s_read, (uint32_t)j & 1) && scores(j + 1))) break;
+                if (!(ok = wait(p_full, (uint32_t)j & 1) && wait(v_full(s), (uint32_t)(j / ST) & 1))) break;
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < KT / 16; k++)
-                    mma_f16_ta(tO, tS + 8 * k, sq_mn<KT>(sm + L::OFF_V + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                    mma_f16_ta(tO, tP + 8 * k, sq_mn<KT>(sm + L::OFF_V + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
                 mma_commit(v_free(s));
+                if (L::APART) mma_commit(pv_done);
+                if (!L::APART && j + 1 < nt && !(ok = scores(j + 1))) break;  // MMAs keep their order: P(j) has been read
             }
             mma_commit(o_full);
             wait(o_full, 0);
         }
         pdl_allow_next();
     } else {
-        constexpr bool HOLD = L::BLOCKS <= 2;  // registers for a row of scores; else they are read twice
+        constexpr bool HOLD = L::APART;  // registers for a row of scores; else they are read twice
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
         float m = -INFINITY, l = 0.0f;  // m: of c s
         bool ok = true;
@@ -151,14 +160,21 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
             tc_fence_after();
             const int at = end - KT * (j + 1), lo = keys.lo - at, hi = keys.hi - at;
             const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= KT);
-            if (!__any_sync(0xFFFFFFFFu, hi > 0 && lo < KT)) {  // no row of the warp sees a key of the tile
-                const uint32_t zeros[16] = {};
-#pragma unroll
-                for (int b = 0; b < KT / 32; b++) tmem_st16(tS + lanes + 16 * b, zeros);
+            // the products of P(j - 1) are in O, and P is free (over S: S(j) came after them)
+            const auto last_done = [&] { return !L::APART || j == 0 || wait(pv_done, (uint32_t)(j - 1) & 1); };
+            const auto p_ready = [&] {
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full);
+            };
+            if (!__any_sync(0xFFFFFFFFu, hi > 0 && lo < KT)) {  // no row of the warp sees a key of the tile
+                if (L::APART && lane == 0) mbar_arrive(s_read);
+                if (!(ok = last_done())) break;
+                const uint32_t zeros[16] = {};
+#pragma unroll
+                for (int b = 0; b < KT / 32; b++) tmem_st16(tP + lanes + 16 * b, zeros);
+                p_ready();
                 continue;
             }
             uint32_t r[HOLD ? KT / 32 : 1][32];
@@ -167,6 +183,11 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
 #pragma unroll
                 for (int b = 0; b < KT / 32; b++) tmem_ld32(tS + lanes + 32 * b, r[b]);
                 tmem_wait_ld();
+                if (L::APART) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(s_read);
+                }
                 if (!all) {
 #pragma unroll
                     for (int b = 0; b < KT / 32; b++) hide(r[b], sq_bits(lo - 32 * b, hi - 32 * b));
@@ -183,6 +204,8 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
                 }
             }
             const float top = c * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            if (!(ok = last_done())) break;
+            tc_fence_after();
             // the first scores, or scores that 2^8 does not hold
             if (__any_sync(0xFFFFFFFFu, top > m + FW_SLACK)) {
                 const float mn = top > m + FW_SLACK ? top : m;
@@ -203,7 +226,7 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
             }
             const float mu = m == -INFINITY ? 0.0f : m;  // no score yet: 2^-inf
             const unsigned long long c2 = f4_two(c, c), m2 = f4_two(-mu, -mu);
-            float ls[2] = {0.0f, 0.0f};
+            unsigned long long ls = f4_two(0.0f, 0.0f);
 #pragma unroll
             for (int b = 0; b < KT / 32; b++) {
                 uint32_t p[16];
@@ -215,13 +238,12 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
                     if (!all) hide(r[0], sq_bits(lo - 32 * b, hi - 32 * b));
                     weigh<BF>(r[0], c2, m2, ls, p);
                 }
-                tmem_st16(tS + lanes + 16 * b, p);  // over scores that were read
+                tmem_st16(tP + lanes + 16 * b, p);  // over S: scores that were read
             }
-            l += ls[0] + ls[1];
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full);
+            float la, lb;
+            f4_untwo(ls, la, lb);
+            l += la + lb;
+            p_ready();
         }
         ok = wait(nt ? o_full : q_full, 0) && ok;
         tc_fence_after();
@@ -306,7 +328,7 @@ cudaError_t tile_init() {
 cudaError_t seq_attn_init() {
     cudaError_t e = tile_init<64, 64>();
     if (e == cudaSuccess) e = tile_init<64, 128>();
-    if (e == cudaSuccess) e = tile_init<128, 128>();
+    if (e == cudaSuccess) e = tile_init<128, 64>();
     return e;
 }
 
@@ -315,7 +337,7 @@ size_t seq_attn_forward_workspace(const SeqAttn &) { return 16; }
 cudaError_t launch_seq_attn_forward(const SeqAttn &a, cudaStream_t st) {
     const bool bf = a.dtype == MNMT_BF16;
     if (a.k_rows == 0) return launch_pdl(bf ? seq_attn_zero_kernel<__nv_bfloat16> : seq_attn_zero_kernel<__half>, (unsigned)((a.q_rows + 7) / 8), 256, 0, st, a);
-    if (a.dh > 64) return bf ? tile_forward<128, true, 128>(a, st) : tile_forward<128, false, 128>(a, st);
+    if (a.dh > 64) return bf ? tile_forward<128, true, 64>(a, st) : tile_forward<128, false, 64>(a, st);
     // Tiles of 64 keys, four CTAs per SM, where sequences are short: 64 x 200 rows of 8 heads 25 us (128 keys: 29),
     // one of 46 rows 5.3 (5.9).  Not where CTAs are few (4 x 512: 13.8, 128 keys 10.9) or walks long (8192
     // causal rows 186, 112: all CTAs are on the card at once, and SMs with long walks are waited for).
