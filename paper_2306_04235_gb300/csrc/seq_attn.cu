@@ -20,13 +20,13 @@ namespace mnmt {
 namespace {
 
 constexpr int FW_THREADS = 192;  // four softmax warps, a TMA warp, an MMA warp
-// KT: keys of a tile; BLOCKS: CTAs per SM
-template <int DH, int KT>
+constexpr int KT = 64;           // keys of a tile
+// BUFS: tiles of scores in TMEM; BLOCKS: CTAs per SM
+template <int DH>
 struct FwLayout {
-    static constexpr int STAGES = 2, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, KT>();
+    static constexpr int STAGES = DH == 64 ? 4 : 2, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, KT>();
     static constexpr int OFF_K = QT, OFF_V = OFF_K + STAGES * TILE, SMEM = OFF_V + STAGES * TILE + 1024;
-    static constexpr bool APART = DH + KT > 128;  // P beside S
-    static constexpr int T_P = APART ? KT : 0, T_O = KT + (APART ? KT / 2 : 0), COLS = pow2_cols(T_O + DH), BLOCKS = 512 / COLS;
+    static constexpr int BUFS = DH == 64 ? 3 : 2, T_O = BUFS * KT, COLS = pow2_cols(T_O + DH), BLOCKS = 512 / COLS;
 };
 constexpr float FW_SLACK = 8.0f;  // how far, in powers of two, a score may exceed m
 
@@ -52,15 +52,15 @@ __device__ __forceinline__ void weigh(const uint32_t (&r)[32], unsigned long lon
     }
 }
 
-template <int DH, bool BF, int KT>
-__global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
+template <int DH, bool BF>
+__global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     seq_attn_forward_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                             const SeqAttn a, const float c) {
-    using L = FwLayout<DH, KT>;
+    using L = FwLayout<DH>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
-    constexpr int ST = L::STAGES;
+    constexpr int ST = L::STAGES, BUFS = L::BUFS;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[4 * ST + 6];
+    __shared__ __align__(8) uint64_t bars[4 * ST + 4 + 2 * BUFS];
     __shared__ uint32_t tslot;
     __shared__ int failed, span[2][4];
     const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
@@ -69,15 +69,15 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
     const auto k_free = [&](int s) { return bar0 + 8 * (ST + s); };
     const auto v_full = [&](int s) { return bar0 + 8 * (2 * ST + s); };
     const auto v_free = [&](int s) { return bar0 + 8 * (3 * ST + s); };
-    const uint32_t q_full = bar0 + 8 * (4 * ST), s_full = q_full + 8, p_full = q_full + 16, o_full = q_full + 24, s_read = q_full + 32,
-                   pv_done = q_full + 40;
+    const uint32_t q_full = bar0 + 8 * (4 * ST), o_full = q_full + 8, pv_done = q_full + 16, s_full = q_full + 32,
+                   p_full = s_full + 8 * BUFS;  // two of pv_done by turns, BUFS of s_full and p_full (a warp may be a tile ahead)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int h = blockIdx.x % a.hq, tile = (int)(gridDim.x / a.hq) - 1 - (int)(blockIdx.x / a.hq);  // the last rows (causal: the longest) first
     const int row = tile * SQ_ROWS + (int)threadIdx.x;
     if (threadIdx.x == 128) {
         for (int s = 0; s < ST; s++) mbar_init(k_full(s), 1), mbar_init(k_free(s), 1), mbar_init(v_full(s), 1), mbar_init(v_free(s), 1);
-        mbar_init(q_full, 1), mbar_init(s_full, 1), mbar_init(p_full, 4), mbar_init(o_full, 1), mbar_init(s_read, 4),
-            mbar_init(pv_done, 1);
+        for (int b = 0; b < BUFS; b++) mbar_init(s_full + 8 * b, 1), mbar_init(p_full + 8 * b, 4);
+        mbar_init(q_full, 1), mbar_init(o_full, 1), mbar_init(pv_done, 1), mbar_init(pv_done + 8, 1);
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tS = tslot, tP = tslot + L::T_P, tO = tslot + L::T_O;
+    const uint32_t tS = tslot, tO = tslot + L::T_O;  // P(j) takes the first half of S(j)'s columns
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
     const int nt = end > first ? (end - first + KT - 1) / KT : 0;
     const SqWaits wait{&failed, a.status};
@@ -121,91 +121,74 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
             }
         }
     } else if (warp == 5) {
-        if (lane == 0 && nt) {
+        if (nt) {
+            const uint32_t on = elect_one();
+            const uint64_t qd = sq_k(sm), kd = sq_k(sm + L::OFF_K), vd = sq_mn<KT>(sm + L::OFF_V);
             const auto scores = [&](int j) {  // S(j)
                 const int s = j % ST;
                 if (!wait(k_full(s), (uint32_t)(j / ST) & 1)) return false;
                 tc_fence_after();
+                const uint64_t b = kd + (uint64_t)(s * (L::TILE >> 4));
+                const uint32_t d = tS + j % BUFS * KT;
 #pragma unroll
-                for (int k = 0; k < DH / 16; k++)
-                    mma_f16(tS, sq_k(sm, k), sq_k<KT>(sm + L::OFF_K + s * L::TILE, k), sq_idesc(KT, BF, false), k > 0);
-                mma_commit(k_free(s));
-                mma_commit(s_full);
+                for (int k = 0; k < DH / 16; k++) sq_mma(on, d, qd + sq_k_step(k), b + sq_k_step<KT>(k), sq_idesc(KT, BF, false), k > 0);
+                f4_commit_on<1>(on, k_free(s));
+                f4_commit_on<1>(on, s_full + 8 * (j % BUFS));
                 return true;
             };
-            bool ok = wait(q_full, 0) && scores(0);
+            bool ok = wait(q_full, 0);
+            for (int j = 0; j < BUFS && j < nt && ok; j++) ok = scores(j);
             for (int j = 0; j < nt && ok; j++) {
                 const int s = j % ST;
-                if (L::APART && j + 1 < nt && !(ok = wait(s_read, (uint32_t)j & 1) && scores(j + 1))) break;
-                if (!(ok = wait(p_full, (uint32_t)j & 1) && wait(v_full(s), (uint32_t)(j / ST) & 1))) break;
+                if (!(ok = wait(p_full + 8 * (j % BUFS), (uint32_t)(j / BUFS) & 1) && wait(v_full(s), (uint32_t)(j / ST) & 1))) break;
                 tc_fence_after();
+                const uint64_t b = vd + (uint64_t)(s * (L::TILE >> 4));
+                const uint32_t p = tS + j % BUFS * KT;
 #pragma unroll
-                for (int k = 0; k < KT / 16; k++)
-                    mma_f16_ta(tO, tP + 8 * k, sq_mn<KT>(sm + L::OFF_V + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
-                mma_commit(v_free(s));
-                if (L::APART) mma_commit(pv_done);
-                if (!L::APART && j + 1 < nt && !(ok = scores(j + 1))) break;  // MMAs keep their order: P(j) has been read
+                for (int k = 0; k < KT / 16; k++) sq_mma_ta(on, tO, p + 8 * k, b + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                f4_commit_on<1>(on, v_free(s));
+                f4_commit_on<1>(on, pv_done + 8 * (j & 1));
+                if (j + BUFS < nt && !(ok = scores(j + BUFS))) break;  // MMAs keep their order: P(j) has been read
             }
-            mma_commit(o_full);
+            f4_commit_on<1>(on, o_full);
             wait(o_full, 0);
         }
         pdl_allow_next();
     } else {
-        constexpr bool HOLD = L::APART;  // registers for a row of scores; else they are read twice
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
         float m = -INFINITY, l = 0.0f;  // m: of c s
         bool ok = true;
         for (int j = 0; j < nt; j++) {
-            if (!(ok = wait(s_full, (uint32_t)j & 1))) break;
+            if (!(ok = wait(s_full + 8 * (j % BUFS), (uint32_t)(j / BUFS) & 1))) break;
             tc_fence_after();
+            const uint32_t tP = tS + j % BUFS * KT + lanes;
             const int at = end - KT * (j + 1), lo = keys.lo - at, hi = keys.hi - at;
             const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= KT);
-            // the products of P(j - 1) are in O, and P is free (over S: S(j) came after them)
-            const auto last_done = [&] { return !L::APART || j == 0 || wait(pv_done, (uint32_t)(j - 1) & 1); };
             const auto p_ready = [&] {
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full);
+                if (lane == 0) mbar_arrive(p_full + 8 * (j % BUFS));
             };
             if (!__any_sync(0xFFFFFFFFu, hi > 0 && lo < KT)) {  // no row of the warp sees a key of the tile
-                if (L::APART && lane == 0) mbar_arrive(s_read);
-                if (!(ok = last_done())) break;
                 const uint32_t zeros[16] = {};
 #pragma unroll
-                for (int b = 0; b < KT / 32; b++) tmem_st16(tP + lanes + 16 * b, zeros);
+                for (int b = 0; b < KT / 32; b++) tmem_st16(tP + 16 * b, zeros);
                 p_ready();
                 continue;
             }
-            uint32_t r[HOLD ? KT / 32 : 1][32];
+            uint32_t r[KT / 32][32];
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            if constexpr (HOLD) {
 #pragma unroll
-                for (int b = 0; b < KT / 32; b++) tmem_ld32(tS + lanes + 32 * b, r[b]);
-                tmem_wait_ld();
-                if (L::APART) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(s_read);
-                }
-                if (!all) {
+            for (int b = 0; b < KT / 32; b++) tmem_ld32(tP + 32 * b, r[b]);
+            tmem_wait_ld();
+            if (!all) {
 #pragma unroll
-                    for (int b = 0; b < KT / 32; b++) hide(r[b], sq_bits(lo - 32 * b, hi - 32 * b));
-                }
-#pragma unroll
-                for (int b = 0; b < KT / 32; b++) max32(r[b], mx);
-            } else {
-#pragma unroll
-                for (int b = 0; b < KT / 32; b++) {
-                    tmem_ld32(tS + lanes + 32 * b, r[0]);
-                    tmem_wait_ld();
-                    if (!all) hide(r[0], sq_bits(lo - 32 * b, hi - 32 * b));
-                    max32(r[0], mx);
-                }
+                for (int b = 0; b < KT / 32; b++) hide(r[b], sq_bits(lo - 32 * b, hi - 32 * b));
             }
+#pragma unroll
+            for (int b = 0; b < KT / 32; b++) max32(r[b], mx);
             const float top = c * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-            if (!(ok = last_done())) break;
-            tc_fence_after();
             // the first scores, or scores that 2^8 does not hold
             if (__any_sync(0xFFFFFFFFu, top > m + FW_SLACK)) {
                 const float mn = top > m + FW_SLACK ? top : m;
@@ -213,6 +196,10 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
                 m = mn;
                 l *= f;
                 if (j > 0 && __any_sync(0xFFFFFFFFu, f != 1.0f)) {
+                    // P V up to the tile before is in O.  (Not every turn is waited for: those two before are over, as S(j)
+                    // was multiplied after them.)
+                    if (!(ok = wait(pv_done + 8 * ((j - 1) & 1), (uint32_t)((j - 1) >> 1) & 1))) break;
+                    tc_fence_after();
 #pragma unroll
                     for (int b = 0; b < DH / 16; b++) {
                         uint32_t o[16];
@@ -230,15 +217,8 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH, KT>::BLOCKS)
 #pragma unroll
             for (int b = 0; b < KT / 32; b++) {
                 uint32_t p[16];
-                if constexpr (HOLD) {
-                    weigh<BF>(r[b], c2, m2, ls, p);
-                } else {
-                    tmem_ld32(tS + lanes + 32 * b, r[0]);
-                    tmem_wait_ld();
-                    if (!all) hide(r[0], sq_bits(lo - 32 * b, hi - 32 * b));
-                    weigh<BF>(r[0], c2, m2, ls, p);
-                }
-                tmem_st16(tP + lanes + 16 * b, p);  // over S: scores that were read
+                weigh<BF>(r[b], c2, m2, ls, p);
+                tmem_st16(tP + 16 * b, p);  // over scores that were read
             }
             float la, lb;
             f4_untwo(ls, la, lb);
@@ -307,28 +287,27 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     }
 }
 
-template <int DH, bool BF, int KT>
+template <int DH, bool BF>
 cudaError_t tile_forward(const SeqAttn &a, cudaStream_t st) {
     CUtensorMap tq, tk, tv;
     if (!sq_map(&tq, a.q, a.q_rows, a.hq, a.dh, SQ_ROWS) || !sq_map(&tk, a.k, a.k_rows, a.hkv, a.dh, KT) || !sq_map(&tv, a.v, a.k_rows, a.hkv, a.dh, KT))
         return cudaErrorInvalidValue;
     const unsigned grid = (unsigned)((a.q_rows + SQ_ROWS - 1) / SQ_ROWS) * (unsigned)a.hq;
-    return launch_pdl(seq_attn_forward_kernel<DH, BF, KT>, grid, FW_THREADS, FwLayout<DH, KT>::SMEM, st, tq, tk, tv, a, a.scale * LOG2E);
+    return launch_pdl(seq_attn_forward_kernel<DH, BF>, grid, FW_THREADS, FwLayout<DH>::SMEM, st, tq, tk, tv, a, a.scale * LOG2E);
 }
 
-template <int DH, int KT>
+template <int DH, bool BF>
 cudaError_t tile_init() {
-    const cudaError_t e = cudaFuncSetAttribute(seq_attn_forward_kernel<DH, true, KT>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwLayout<DH, KT>::SMEM);
-    return e != cudaSuccess ? e
-                            : cudaFuncSetAttribute(seq_attn_forward_kernel<DH, false, KT>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwLayout<DH, KT>::SMEM);
+    return cudaFuncSetAttribute(seq_attn_forward_kernel<DH, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwLayout<DH>::SMEM);
 }
 
 }  // namespace
 
 cudaError_t seq_attn_init() {
-    cudaError_t e = tile_init<64, 64>();
-    if (e == cudaSuccess) e = tile_init<64, 128>();
-    if (e == cudaSuccess) e = tile_init<128, 64>();
+    cudaError_t e = tile_init<64, true>();
+    if (e == cudaSuccess) e = tile_init<64, false>();
+    if (e == cudaSuccess) e = tile_init<128, true>();
+    if (e == cudaSuccess) e = tile_init<128, false>();
     return e;
 }
 
@@ -337,13 +316,8 @@ size_t seq_attn_forward_workspace(const SeqAttn &) { return 16; }
 cudaError_t launch_seq_attn_forward(const SeqAttn &a, cudaStream_t st) {
     const bool bf = a.dtype == MNMT_BF16;
     if (a.k_rows == 0) return launch_pdl(bf ? seq_attn_zero_kernel<__nv_bfloat16> : seq_attn_zero_kernel<__half>, (unsigned)((a.q_rows + 7) / 8), 256, 0, st, a);
-    if (a.dh > 64) return bf ? tile_forward<128, true, 64>(a, st) : tile_forward<128, false, 64>(a, st);
-    // Tiles of 64 keys, four CTAs per SM, where sequences are short: 64 x 200 rows of 8 heads 25 us (128 keys: 29),
-    // one of 46 rows 5.3 (5.9).  Not where CTAs are few (4 x 512: 13.8, 128 keys 10.9) or walks long (8192
-    // causal rows 186, 112: all CTAs are on the card at once, and SMs with long walks are waited for).
-    const long keys = a.n_seqs ? a.k_rows / a.n_seqs : 0, ctas = (a.q_rows + SQ_ROWS - 1L) / SQ_ROWS * a.hq;
-    if (keys <= 64 || (keys < 1024 && ctas > 2 * 152)) return bf ? tile_forward<64, true, 64>(a, st) : tile_forward<64, false, 64>(a, st);
-    return bf ? tile_forward<64, true, 128>(a, st) : tile_forward<64, false, 128>(a, st);
+    if (a.dh <= 64) return bf ? tile_forward<64, true>(a, st) : tile_forward<64, false>(a, st);
+    return bf ? tile_forward<128, true>(a, st) : tile_forward<128, false>(a, st);
 }
 
 }  // namespace mnmt

@@ -110,35 +110,37 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             }
         }
     } else if (warp == 9) {
-        if (lane == 0 && nt) {
+        if (nt) {
+            const uint32_t on = elect_one();
+            const uint64_t qd = sq_k(sm), gd = sq_k(sm + L::OFF_G), kd = sq_k(sm + L::OFF_K), vd = sq_k(sm + L::OFF_V), kt = sq_mn<W>(sm + L::OFF_K);
             bool ok = wait(q_full, 0);
             for (int j = 0; j <= nt && ok; j++) {
                 if (j < nt) {  // S(j), dP(j)
                     const int s = j % ST;
+                    const uint64_t off = (uint64_t)(s * (L::TILE >> 4));
                     const uint32_t ph = (uint32_t)(j / ST) & 1;
                     if (j && !(ok = wait(sp_free, (uint32_t)(j - 1) & 1))) break;
                     if (!(ok = wait(k_full(s), ph) && wait(v_full(s), ph))) break;
                     tc_fence_after();
 #pragma unroll
-                    for (int k = 0; k < DH / 16; k++) mma_f16(tS, sq_k(sm, k), sq_k<W>(sm + L::OFF_K + s * L::TILE, k), sq_idesc(W, BF, false), k > 0);
+                    for (int k = 0; k < DH / 16; k++) sq_mma(on, tS, qd + sq_k_step(k), kd + off + sq_k_step<W>(k), sq_idesc(W, BF, false), k > 0);
 #pragma unroll
-                    for (int k = 0; k < DH / 16; k++)
-                        mma_f16(tP, sq_k(sm + L::OFF_G, k), sq_k<W>(sm + L::OFF_V + s * L::TILE, k), sq_idesc(W, BF, false), k > 0);
-                    mma_commit(v_free(s));
-                    mma_commit(sp_full);
+                    for (int k = 0; k < DH / 16; k++) sq_mma(on, tP, gd + sq_k_step(k), vd + off + sq_k_step<W>(k), sq_idesc(W, BF, false), k > 0);
+                    f4_commit_on<1>(on, v_free(s));
+                    f4_commit_on<1>(on, sp_full);
                 }
                 if (j > 0) {  // dQ(j - 1)
                     const int i = j - 1, s = i % ST;
                     if (!(ok = wait(ds_full, (uint32_t)i & 1))) break;
                     tc_fence_after();
+                    const uint64_t b = kt + (uint64_t)(s * (L::TILE >> 4));
 #pragma unroll
-                    for (int k = 0; k < W / 16; k++)
-                        mma_f16_ta(tO, tD + 8 * k, sq_mn<W>(sm + L::OFF_K + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(i | k));
-                    mma_commit(k_free(s));
-                    mma_commit(ds_free);
+                    for (int k = 0; k < W / 16; k++) sq_mma_ta(on, tO, tD + 8 * k, b + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(i | k));
+                    f4_commit_on<1>(on, k_free(s));
+                    f4_commit_on<1>(on, ds_free);
                 }
             }
-            mma_commit(dq_full);
+            f4_commit_on<1>(on, dq_full);
             wait(dq_full, 0);
         }
         pdl_allow_next();
@@ -341,46 +343,51 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             }
         }
     } else if (warp == 9) {
-        if (lane == 0 && n) {
-            bool ok = wait(kv_full, 0);
+        if (n) {
+            const uint32_t on = elect_one();
+            const uint64_t kd = sq_k(sm), vd = sq_k(sm + L::OFF_V), qd = sq_k(sm + L::OFF_Q), gd = sq_k(sm + L::OFF_G);
+            const uint64_t qt = sq_mn<W>(sm + L::OFF_Q), gt = sq_mn<W>(sm + L::OFF_G);
             const auto scores = [&](int j) {  // S^T(j)
                 const int s = j % ST;
                 if (!wait(q_full(s), (uint32_t)(j / ST) & 1)) return false;
                 tc_fence_after();
+                const uint64_t b = qd + (uint64_t)(s * (L::TILE >> 4));
 #pragma unroll
-                for (int k = 0; k < DH / 16; k++) mma_f16(tS, sq_k(sm, k), sq_k<W>(sm + L::OFF_Q + s * L::TILE, k), sq_idesc(W, BF, false), k > 0);
-                mma_commit(s_full);
+                for (int k = 0; k < DH / 16; k++) sq_mma(on, tS, kd + sq_k_step(k), b + sq_k_step<W>(k), sq_idesc(W, BF, false), k > 0);
+                f4_commit_on<1>(on, s_full);
                 return true;
             };
             const auto weights = [&](int j) {  // dP^T(j)
                 const int s = j % ST;
                 if (!wait(g_full(s), (uint32_t)(j / ST) & 1)) return false;
                 tc_fence_after();
+                const uint64_t b = gd + (uint64_t)(s * (L::TILE >> 4));
 #pragma unroll
-                for (int k = 0; k < DH / 16; k++)
-                    mma_f16(tP, sq_k(sm + L::OFF_V, k), sq_k<W>(sm + L::OFF_G + s * L::TILE, k), sq_idesc(W, BF, false), k > 0);
-                mma_commit(dp_full);
+                for (int k = 0; k < DH / 16; k++) sq_mma(on, tP, vd + sq_k_step(k), b + sq_k_step<W>(k), sq_idesc(W, BF, false), k > 0);
+                f4_commit_on<1>(on, dp_full);
                 return true;
             };
-            ok = ok && scores(0) && weights(0);
+            bool ok = wait(kv_full, 0) && scores(0) && weights(0);
             for (int j = 0; j < n && ok; j++) {
                 const int s = j % ST;
+                const uint64_t off = (uint64_t)(s * (L::TILE >> 4));
                 if (!(ok = wait(p_full, (uint32_t)j & 1))) break;
                 tc_fence_after();
+                // a row's two threads write W / 4 columns each, W / 2 apart
 #pragma unroll
-                for (int k = 0; k < W / 16; k++)  // a row's two threads write W / 4 columns each, W / 2 apart
-                    mma_f16_ta(tV, tS + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), sq_mn<W>(sm + L::OFF_G + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
-                mma_commit(g_free(s));
+                for (int k = 0; k < W / 16; k++)
+                    sq_mma_ta(on, tV, tS + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), gt + off + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                f4_commit_on<1>(on, g_free(s));
                 if (j + 1 < n && !(ok = scores(j + 1))) break;
                 if (!(ok = wait(ds_full, (uint32_t)j & 1))) break;
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < W / 16; k++)
-                    mma_f16_ta(tK, tP + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), sq_mn<W>(sm + L::OFF_Q + s * L::TILE, k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
-                mma_commit(q_free(s));
+                    sq_mma_ta(on, tK, tP + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), qt + off + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                f4_commit_on<1>(on, q_free(s));
                 if (j + 1 < n && !(ok = weights(j + 1))) break;
             }
-            mma_commit(out_full);
+            f4_commit_on<1>(on, out_full);
             wait(out_full, 0);
         }
         pdl_allow_next();

@@ -36,25 +36,39 @@ __device__ __forceinline__ void sq_load(uint32_t dst, const CUtensorMap *tm, int
             : "memory");
 }
 
-// descriptors of 16 reduction indices: K-major step k of the head's elements, MN-major step k of the rows
+// Descriptor of a tile and what step k of 16 reduction indices adds to it: K-major (the sum
+// runs over the head's elements) and MN-major (over the tile's rows)
+__device__ __forceinline__ uint64_t sq_k(uint32_t tile) { return sw128_desc(tile); }
 template <int ROWS = SQ_ROWS>
-__device__ __forceinline__ uint64_t sq_k(uint32_t tile, int k) { return sw128_desc(tile + (k >> 2) * (ROWS * 128) + (k & 3) * 32); }
+__host__ __device__ constexpr uint64_t sq_k_step(int k) { return (uint64_t)(((k >> 2) * (ROWS * 128) + (k & 3) * 32) >> 4); }
 template <int ROWS = SQ_ROWS>
-__device__ __forceinline__ uint64_t sq_mn(uint32_t tile, int k) {
-    return (uint64_t)(((tile + k * 2048) >> 4) & 0x3FFFu) | ((uint64_t)((ROWS * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
-           ((uint64_t)2 << 61);
+__device__ __forceinline__ uint64_t sq_mn(uint32_t tile) {
+    return (uint64_t)((tile >> 4) & 0x3FFFu) | ((uint64_t)((ROWS * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
+__host__ __device__ constexpr uint64_t sq_mn_step(int k) { return (uint64_t)(k * 2048 >> 4); }
 // kind::f16, D fp32 of 128 x n; bf: bf16 operands; b_mn: B is MN-major
 __host__ __device__ constexpr uint32_t sq_idesc(int n, bool bf, bool b_mn) {
     return (1u << 4) | ((bf ? 1u : 0u) << 7) | ((bf ? 1u : 0u) << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
-// A from tensor memory: lane = row, a column holds two elements
-__device__ __forceinline__ void mma_f16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// MMAs and commits of a converged warp, by one lane (on; see elect_one): issued under a branch on
+// the lane they took 100 to 130 cycles each, and set the pace of every kernel here.
+__device__ __forceinline__ void sq_mma(uint32_t on, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(on)
+        : "memory");
+}
+// A from tensor memory: lane = row, a column holds two elements
+__device__ __forceinline__ void sq_mma_ta(uint32_t on, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(on)
         : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
