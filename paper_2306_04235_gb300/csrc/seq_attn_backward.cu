@@ -181,22 +181,32 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             __syncwarp();
             if (lane == 0) mbar_arrive(sp_free);
             if (j && !(ok = wait(ds_free, (uint32_t)(j - 1) & 1))) break;
+            // dS of the 32 b columns: without the masks where the warp's rows see all of them
+            const auto ds = [&](auto whole) {
 #pragma unroll
-            for (int b = 0; b < W / 64; b++) {
-                const uint32_t see = all ? 0xFFFFFFFFu : sq_bits(lo - 32 * b, hi - 32 * b);
-                uint32_t w[16];
+                for (int b = 0; b < W / 64; b++) {
+                    const uint32_t see = sq_bits(lo - 32 * b, hi - 32 * b);
+                    uint32_t w[16];
 #pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    w[i] = 0;
-                    if (!some) continue;
-                    float x, y, u, v;
-                    f4_untwo(sq_fma2(f4_two(__uint_as_float(s[b][2 * i]), __uint_as_float(s[b][2 * i + 1])), c2, l2), x, y);
-                    const unsigned long long t = f4_add2(f4_two(__uint_as_float(p[b][2 * i]), __uint_as_float(p[b][2 * i + 1])), d2);
-                    f4_untwo(f4_mul2(f4_two(exp2_fast(x), exp2_fast(y)), t), u, v);
-                    if (!all) u = (see >> (2 * i)) & 1u ? u : 0.0f, v = (see >> (2 * i + 1)) & 1u ? v : 0.0f;
-                    w[i] = sq_pack<BF>(u, v);
+                    for (int i = 0; i < 16; i++) {
+                        float x, y, u, v;
+                        f4_untwo(sq_fma2(f4_two(__uint_as_float(s[b][2 * i]), __uint_as_float(s[b][2 * i + 1])), c2, l2), x, y);
+                        const unsigned long long t = f4_add2(f4_two(__uint_as_float(p[b][2 * i]), __uint_as_float(p[b][2 * i + 1])), d2);
+                        f4_untwo(f4_mul2(f4_two(exp2_fast(x), exp2_fast(y)), t), u, v);
+                        if (!decltype(whole)::value) u = (see >> (2 * i)) & 1u ? u : 0.0f, v = (see >> (2 * i + 1)) & 1u ? v : 0.0f;
+                        w[i] = sq_pack<BF>(u, v);
+                    }
+                    tmem_st16(tD + lanes + W / 4 * half + 16 * b, w);
                 }
-                tmem_st16(tD + lanes + W / 4 * half + 16 * b, w);
+            };
+            if (all) {
+                ds(std::true_type{});
+            } else if (some) {
+                ds(std::false_type{});
+            } else {
+                const uint32_t zeros[16] = {};
+#pragma unroll
+                for (int b = 0; b < W / 64; b++) tmem_st16(tD + lanes + W / 4 * half + 16 * b, zeros);
             }
             tmem_wait_st();
             tc_fence_before();
@@ -400,70 +410,87 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             if (++t == nt) t = 0;
             const float4 *num = reinterpret_cast<const float4 *>(smp + L::OFF_N + s * L::NUM) + W / 8 * half;
             const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= W / 2), some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
-            uint32_t see[W / 64];
-#pragma unroll
-            for (int b = 0; b < W / 64; b++) see[b] = all ? 0xFFFFFFFFu : sq_bits(lo - 32 * b, hi - 32 * b);
             // the producer's numbers are visible with the tile that they came with
             if (!(ok = wait(s_full, (uint32_t)j & 1) && wait(q_full(s), (uint32_t)(j / ST) & 1))) break;
             tc_fence_after();
+            // Two passes over a thread's columns, P and dS, without the masks where the warp's rows see all of them
             uint32_t r[W / 64][32];
-            if (some) load_half<W>(tS + lanes + W / 2 * half, r);
+            const uint32_t zeros[16] = {};
+            const auto weights = [&](auto whole) {
+                load_half<W>(tS + lanes + W / 2 * half, r);
 #pragma unroll
-            for (int b = 0; b < W / 64; b++) {
-                uint32_t w[16];
+                for (int b = 0; b < W / 64; b++) {
+                    const uint32_t see = sq_bits(lo - 32 * b, hi - 32 * b);
+                    uint32_t w[16];
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    w[2 * i] = w[2 * i + 1] = 0;
-                    if (!some) continue;
-                    const float4 x = num[8 * b + i];
-                    float p[4];
-                    f4_untwo(sq_fma2(f4_two(__uint_as_float(r[b][4 * i]), __uint_as_float(r[b][4 * i + 1])), c2, f4_two(x.x, x.y)), p[0], p[1]);
-                    f4_untwo(sq_fma2(f4_two(__uint_as_float(r[b][4 * i + 2]), __uint_as_float(r[b][4 * i + 3])), c2, f4_two(x.z, x.w)), p[2], p[3]);
+                    for (int i = 0; i < 8; i++) {
+                        const float4 x = num[8 * b + i];
+                        float p[4];
+                        f4_untwo(sq_fma2(f4_two(__uint_as_float(r[b][4 * i]), __uint_as_float(r[b][4 * i + 1])), c2, f4_two(x.x, x.y)), p[0], p[1]);
+                        f4_untwo(sq_fma2(f4_two(__uint_as_float(r[b][4 * i + 2]), __uint_as_float(r[b][4 * i + 3])), c2, f4_two(x.z, x.w)), p[2], p[3]);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        p[e] = exp2_fast(p[e]);
-                        if (!all) p[e] = (see[b] >> (4 * i + e)) & 1u ? p[e] : 0.0f;
-                        r[b][4 * i + e] = __float_as_uint(p[e]);
+                        for (int e = 0; e < 4; e++) {
+                            p[e] = exp2_fast(p[e]);
+                            if (!decltype(whole)::value) p[e] = (see >> (4 * i + e)) & 1u ? p[e] : 0.0f;
+                            r[b][4 * i + e] = __float_as_uint(p[e]);
+                        }
+                        w[2 * i] = sq_pack<BF>(p[0], p[1]), w[2 * i + 1] = sq_pack<BF>(p[2], p[3]);
                     }
-                    w[2 * i] = sq_pack<BF>(p[0], p[1]), w[2 * i + 1] = sq_pack<BF>(p[2], p[3]);
+                    tmem_st16(tS + lanes + W / 2 * half + 16 * b, w);
                 }
-                tmem_st16(tS + lanes + W / 2 * half + 16 * b, w);
+            };
+            const auto gradients = [&](auto whole) {
+                uint32_t q[W / 64][32];
+                load_half<W>(tP + lanes + W / 2 * half, q);
+#pragma unroll
+                for (int b = 0; b < W / 64; b++) {
+                    const uint32_t see = sq_bits(lo - 32 * b, hi - 32 * b);
+                    uint32_t w[16];
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const float4 x = num[W / 4 + 8 * b + i];
+                        float d[4];
+                        f4_untwo(f4_mul2(f4_two(__uint_as_float(r[b][4 * i]), __uint_as_float(r[b][4 * i + 1])),
+                                         f4_add2(f4_two(__uint_as_float(q[b][4 * i]), __uint_as_float(q[b][4 * i + 1])), f4_two(x.x, x.y))),
+                                 d[0], d[1]);
+                        f4_untwo(f4_mul2(f4_two(__uint_as_float(r[b][4 * i + 2]), __uint_as_float(r[b][4 * i + 3])),
+                                         f4_add2(f4_two(__uint_as_float(q[b][4 * i + 2]), __uint_as_float(q[b][4 * i + 3])), f4_two(x.z, x.w))),
+                                 d[2], d[3]);
+                        if (!decltype(whole)::value) {
+#pragma unroll
+                            for (int e = 0; e < 4; e++) d[e] = (see >> (4 * i + e)) & 1u ? d[e] : 0.0f;
+                        }
+                        w[2 * i] = sq_pack<BF>(d[0], d[1]), w[2 * i + 1] = sq_pack<BF>(d[2], d[3]);
+                    }
+                    tmem_st16(tP + lanes + W / 2 * half + 16 * b, w);
+                }
+            };
+            const auto written = [&](uint32_t bar) {
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar);
+            };
+            if (all) {
+                weights(std::true_type{});
+            } else if (some) {
+                weights(std::false_type{});
+            } else {
+#pragma unroll
+                for (int b = 0; b < W / 64; b++) tmem_st16(tS + lanes + W / 2 * half + 16 * b, zeros);
             }
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full);
+            written(p_full);
             if (!(ok = wait(dp_full, (uint32_t)j & 1))) break;
             tc_fence_after();
-            uint32_t q[W / 64][32];
-            if (some) load_half<W>(tP + lanes + W / 2 * half, q);
+            if (all) {
+                gradients(std::true_type{});
+            } else if (some) {
+                gradients(std::false_type{});
+            } else {
 #pragma unroll
-            for (int b = 0; b < W / 64; b++) {
-                uint32_t w[16];
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    w[2 * i] = w[2 * i + 1] = 0;
-                    if (!some) continue;
-                    const float4 x = num[W / 4 + 8 * b + i];
-                    float d[4];
-                    f4_untwo(f4_mul2(f4_two(__uint_as_float(r[b][4 * i]), __uint_as_float(r[b][4 * i + 1])),
-                                     f4_add2(f4_two(__uint_as_float(q[b][4 * i]), __uint_as_float(q[b][4 * i + 1])), f4_two(x.x, x.y))),
-                             d[0], d[1]);
-                    f4_untwo(f4_mul2(f4_two(__uint_as_float(r[b][4 * i + 2]), __uint_as_float(r[b][4 * i + 3])),
-                                     f4_add2(f4_two(__uint_as_float(q[b][4 * i + 2]), __uint_as_float(q[b][4 * i + 3])), f4_two(x.z, x.w))),
-                             d[2], d[3]);
-                    if (!all) {
-#pragma unroll
-                        for (int e = 0; e < 4; e++) d[e] = (see[b] >> (4 * i + e)) & 1u ? d[e] : 0.0f;
-                    }
-                    w[2 * i] = sq_pack<BF>(d[0], d[1]), w[2 * i + 1] = sq_pack<BF>(d[2], d[3]);
-                }
-                tmem_st16(tP + lanes + W / 2 * half + 16 * b, w);
+                for (int b = 0; b < W / 64; b++) tmem_st16(tP + lanes + W / 2 * half + 16 * b, zeros);
             }
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ds_full);
+            written(ds_full);
         }
         if (n) ok = wait(out_full, 0) && ok;
         tc_fence_after();
