@@ -26,6 +26,7 @@ template <int DH>
 struct FwLayout {
     static constexpr int STAGES = DH == 64 ? 4 : 2, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, KT>();
     static constexpr int OFF_K = QT, OFF_V = OFF_K + STAGES * TILE, SMEM = OFF_V + STAGES * TILE + 1024;
+    static_assert(2 * STAGES * TILE >= 4 * SQ_INTS, "starts and lengths before keys and values");
     static constexpr int BUFS = DH == 64 ? 3 : 2, T_O = BUFS * KT, COLS = pow2_cols(T_O + DH), BLOCKS = 512 / COLS;
 };
 constexpr float FW_SLACK = 8.0f;  // how far, in powers of two, a score may exceed m
@@ -84,14 +85,16 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     if (warp == 5) tmem_alloc<L::COLS>(s_addr(&tslot));
     pdl_grid_wait();
     if (threadIdx.x == 128) sq_load<DH>(sm, &tq, h, tile * SQ_ROWS, q_full);
+    const SeqAttn ix = seq_shared(a, reinterpret_cast<int *>(smp + L::OFF_K), FW_THREADS);  // where keys and values come later
     Span keys{0, 0};
     bool in = false;
     if (warp < 4) {
-        keys = keys_of_lane(a, row - lane, in);
+        keys = keys_of_query(ix, row, in);
         const bool some = keys.hi > keys.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? keys.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? keys.hi : 0);
         if (lane == 0) span[0][warp] = lo, span[1][warp] = hi;
     }
+    sq_before_copies();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -278,7 +281,7 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     const int lane = threadIdx.x & 31;
     bool in;
     if (w >= a.q_rows) return;
-    keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in);
+    keys_of_query(a, (int)w, in);
     if (!in) return;
     const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int h = 0; h < a.hq; h++) {

@@ -32,11 +32,32 @@ __device__ __forceinline__ void load_half(uint32_t taddr, uint32_t (&r)[W / 64][
     tmem_wait_ld();
 }
 
+// sum of eight products of 16-bit elements
+template <typename T>
+__device__ __forceinline__ float dot8(const uint4 &x, const uint4 &y) {
+    const uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {y.x, y.y, y.z, y.w};
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (std::is_same_v<T, __half>) {
+            const float2 u = __half22float2(*reinterpret_cast<const __half2 *>(&a[i])), v = __half22float2(*reinterpret_cast<const __half2 *>(&b[i]));
+            s = fmaf(u.x, v.x, fmaf(u.y, v.y, s));
+        } else {
+            s = fmaf(__uint_as_float(a[i] << 16), __uint_as_float(b[i] << 16),
+                     fmaf(__uint_as_float(a[i] & 0xFFFF0000u), __uint_as_float(b[i] & 0xFFFF0000u), s));
+        }
+    }
+    return s;
+}
+
 // --------------------------------------------------------------------------- dq
 template <int DH, int W>
 struct DqLayout {
-    static constexpr int STAGES = 2, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, W>();
-    static constexpr int OFF_G = QT, OFF_K = 2 * QT, OFF_V = OFF_K + STAGES * TILE, SMEM = OFF_V + STAGES * TILE + 1024;
+    // a stage of K more than of V: it is held until dQ of its tile, and its successor needs a microsecond to come
+    // (two stages: the MMA warp waited 1300 cycles a tile for K)
+    static constexpr int VS = DH == 64 ? 3 : 2, KS = VS + 1, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, W>();
+    static constexpr int OFF_G = QT, OFF_K = 2 * QT, OFF_V = OFF_K + KS * TILE, SMEM = OFF_V + VS * TILE + 1024;
+    static_assert((KS + VS) * TILE >= 4 * SQ_INTS, "starts and lengths before keys and values");
     static constexpr int T_DP = W, T_DS = 2 * W, T_DQ = 2 * W + W / 2, COLS = pow2_cols(T_DQ + DH);  // columns of dP, dS and dQ behind S
 };
 
@@ -46,40 +67,63 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
                                                                     const SeqAttn a, const float c, float *delta) {
     using L = DqLayout<DH, W>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
-    constexpr int ST = L::STAGES;
+    constexpr int KS = L::KS, VS = L::VS;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[4 * ST + 6];
+    __shared__ __align__(8) uint64_t bars[2 * KS + 2 * VS + 6];
     __shared__ uint32_t tslot;
     __shared__ int failed, span[2][4];
-    __shared__ float part[2][SQ_ROWS];
+    __shared__ float dots[SQ_ROWS];
     __shared__ uint8_t odd_rows[2][SQ_ROWS];
     const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
     uint8_t *smp = raw + (sm - s_addr(raw));
     const auto k_full = [&](int s) { return bar0 + 8 * s; };
-    const auto k_free = [&](int s) { return bar0 + 8 * (ST + s); };
-    const auto v_full = [&](int s) { return bar0 + 8 * (2 * ST + s); };
-    const auto v_free = [&](int s) { return bar0 + 8 * (3 * ST + s); };
-    const uint32_t q_full = bar0 + 8 * (4 * ST), sp_full = q_full + 8, sp_free = q_full + 16, ds_full = q_full + 24, ds_free = q_full + 32,
+    const auto k_free = [&](int s) { return bar0 + 8 * (KS + s); };
+    const auto v_full = [&](int s) { return bar0 + 8 * (2 * KS + s); };
+    const auto v_free = [&](int s) { return bar0 + 8 * (2 * KS + VS + s); };
+    const uint32_t q_full = bar0 + 8 * (2 * KS + 2 * VS), sp_full = q_full + 8, sp_free = q_full + 16, ds_full = q_full + 24, ds_free = q_full + 32,
                    dq_full = q_full + 40;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int h = blockIdx.x % a.hq, hk = h / a.group(), tile = (int)(gridDim.x / a.hq) - 1 - (int)(blockIdx.x / a.hq);
     const int half = warp >> 2, rt = (int)threadIdx.x & 127, row = tile * SQ_ROWS + rt;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < ST; s++) mbar_init(k_full(s), 1), mbar_init(k_free(s), 1), mbar_init(v_full(s), 1), mbar_init(v_free(s), 1);
+        for (int s = 0; s < KS; s++) mbar_init(k_full(s), 1), mbar_init(k_free(s), 1);
+        for (int s = 0; s < VS; s++) mbar_init(v_full(s), 1), mbar_init(v_free(s), 1);
         mbar_init(q_full, 2), mbar_init(sp_full, 1), mbar_init(sp_free, 8), mbar_init(ds_full, 8), mbar_init(ds_free, 1), mbar_init(dq_full, 1);
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) tmem_alloc<L::COLS>(s_addr(&tslot));
     pdl_grid_wait();
+    // D of the tile's rows, 16 a warp, DH / 8 lanes a row; the loads are in flight while the starts come
+    constexpr int PC = DH / 8, NR = 16 * PC / 32;  // 16-byte pieces of a row, rows of a lane
+    uint4 ov[NR], gv[NR];
+    if (warp < 8) {
+        const int c = 8 * (lane % PC);
+#pragma unroll
+        for (int i = 0; i < NR; i++) {
+            const int r = tile * SQ_ROWS + 16 * warp + i * (32 / PC) + lane / PC;
+            const bool on = r < a.q_rows && c < a.dh;
+            ov[i] = on ? *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.o.p) + r * a.o.ld + h * a.o.hd + c) : make_uint4(0, 0, 0, 0);
+            gv[i] = on ? *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.g.p) + r * a.g.ld + h * a.g.hd + c) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    const SeqAttn ix = seq_shared(a, reinterpret_cast<int *>(smp + L::OFF_K), BW_THREADS);  // where keys and values come later
     Span keys{0, 0};
     bool in = false;
     if (warp < 8) {
-        keys = keys_of_lane(a, row - lane, in);
+        keys = keys_of_query(ix, row, in);
         const bool some = keys.hi > keys.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? keys.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? keys.hi : 0);
         if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi;
+#pragma unroll
+        for (int i = 0; i < NR; i++) {
+            float dot = dot8<T>(ov[i], gv[i]);
+#pragma unroll
+            for (int o = PC / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
+            if (lane % PC == 0) dots[16 * warp + i * (32 / PC) + lane / PC] = dot;
+        }
     }
+    sq_before_copies();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -92,21 +136,25 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         if (lane == 0 && nt) {
             sq_load<DH>(sm, &tq, h, tile * SQ_ROWS, q_full);
             sq_load<DH>(sm + L::OFF_G, &tg, h, tile * SQ_ROWS, q_full);
-            int j = 0;
-            for (; j < nt; j++) {
-                const int s = j % ST, at = end - W * (j + 1);
-                const uint32_t ph = (uint32_t)(j / ST - 1) & 1;
-                if (j >= ST && !wait(k_free(s), ph)) break;
-                sq_load<DH, W>(sm + L::OFF_K + s * L::TILE, &tk, hk, at, k_full(s));
-                if (j >= ST && !wait(v_free(s), ph)) {
-                    wait(k_full(s), (uint32_t)(j / ST) & 1);  // in flight
+            int jk = 0, jv = 0;  // loads issued
+            // K(0), then V(j) and K(j + KS - VS) by turns: each waits for what the tensor core is done with first
+            for (; jv < nt; jv++) {
+                if (jv >= VS && !wait(v_free(jv % VS), (uint32_t)(jv / VS - 1) & 1)) break;
+                for (; jk <= jv; jk++) sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, end - W * (jk + 1), k_full(jk % KS));  // the first
+                sq_load<DH, W>(sm + L::OFF_V + jv % VS * L::TILE, &tv, hk, end - W * (jv + 1), v_full(jv % VS));
+                for (; jk < nt && jk <= jv + KS - VS; jk++) {
+                    if (jk >= KS && !wait(k_free(jk % KS), (uint32_t)(jk / KS - 1) & 1)) break;
+                    sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, end - W * (jk + 1), k_full(jk % KS));
+                }
+                if (failed) {
+                    jv++;
                     break;
                 }
-                sq_load<DH, W>(sm + L::OFF_V + s * L::TILE, &tv, hk, at, v_full(s));
             }
             if (failed) {  // copies in flight land before the block ends
                 wait(q_full, 0);
-                for (int i = max(0, j - ST); i < j; i++) wait(k_full(i % ST), (uint32_t)(i / ST) & 1), wait(v_full(i % ST), (uint32_t)(i / ST) & 1);
+                for (int i = max(0, jk - KS); i < jk; i++) wait(k_full(i % KS), (uint32_t)(i / KS) & 1);
+                for (int i = max(0, jv - VS); i < jv; i++) wait(v_full(i % VS), (uint32_t)(i / VS) & 1);
             }
         }
     } else if (warp == 9) {
@@ -116,21 +164,22 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             bool ok = wait(q_full, 0);
             for (int j = 0; j <= nt && ok; j++) {
                 if (j < nt) {  // S(j), dP(j)
-                    const int s = j % ST;
-                    const uint64_t off = (uint64_t)(s * (L::TILE >> 4));
-                    const uint32_t ph = (uint32_t)(j / ST) & 1;
+                    const int s = j % KS, sv = j % VS;
+                    const uint64_t koff = (uint64_t)(s * (L::TILE >> 4)), voff = (uint64_t)(sv * (L::TILE >> 4));
                     if (j && !(ok = wait(sp_free, (uint32_t)(j - 1) & 1))) break;
-                    if (!(ok = wait(k_full(s), ph) && wait(v_full(s), ph))) break;
+                    if (!(ok = wait(k_full(s), (uint32_t)(j / KS) & 1))) break;
                     tc_fence_after();
 #pragma unroll
-                    for (int k = 0; k < DH / 16; k++) sq_mma(on, tS, qd + sq_k_step(k), kd + off + sq_k_step<W>(k), sq_idesc(W, BF, false), k > 0);
+                    for (int k = 0; k < DH / 16; k++) sq_mma(on, tS, qd + sq_k_step(k), kd + koff + sq_k_step<W>(k), sq_idesc(W, BF, false), k > 0);
+                    if (!(ok = wait(v_full(sv), (uint32_t)(j / VS) & 1))) break;
+                    tc_fence_after();
 #pragma unroll
-                    for (int k = 0; k < DH / 16; k++) sq_mma(on, tP, gd + sq_k_step(k), vd + off + sq_k_step<W>(k), sq_idesc(W, BF, false), k > 0);
-                    f4_commit_on<1>(on, v_free(s));
+                    for (int k = 0; k < DH / 16; k++) sq_mma(on, tP, gd + sq_k_step(k), vd + voff + sq_k_step<W>(k), sq_idesc(W, BF, false), k > 0);
+                    f4_commit_on<1>(on, v_free(sv));
                     f4_commit_on<1>(on, sp_full);
                 }
                 if (j > 0) {  // dQ(j - 1)
-                    const int i = j - 1, s = i % ST;
+                    const int i = j - 1, s = i % KS;
                     if (!(ok = wait(ds_full, (uint32_t)i & 1))) break;
                     tc_fence_after();
                     const uint64_t b = kt + (uint64_t)(s * (L::TILE >> 4));
@@ -147,17 +196,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     } else {
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const long at_row = (long)h * a.q_rows + row;
-        // D: each of a row's two threads takes half of the head
-        float dot = 0.0f;
-        if (in) {
-            const int c0 = half * (DH / 2), n = min(DH / 2, a.dh - c0);
-            if (n > 0)
-                dot = row_dot(static_cast<const T *>(a.o.p) + row * a.o.ld + h * a.o.hd + c0, static_cast<const T *>(a.g.p) + row * a.g.ld + h * a.g.hd + c0,
-                              n);
-        }
-        part[half][rt] = dot;
-        elements_sync();
-        const float D = part[0][rt] + part[1][rt];
+        const float D = dots[rt];
         if (in && half == 0) delta[at_row] = D;
         const bool none = keys.hi <= keys.lo;
         const float lse2 = none ? 0.0f : a.lse[at_row] * LOG2E;
@@ -256,9 +295,12 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
 // --------------------------------------------------------------------------- dk, dv
 template <int DH, int W>
 struct DkvLayout {
-    static constexpr int STAGES = DH == 64 ? 3 : 2, KT = sq_bytes<DH>(), TILE = sq_bytes<DH, W>(), NUM = 8 * W;
-    // K and V, stages of Q and G, stages of -lse log2 e and -D of W queries
-    static constexpr int OFF_V = KT, OFF_Q = 2 * KT, OFF_G = OFF_Q + STAGES * TILE, OFF_N = OFF_G + STAGES * TILE, SMEM = OFF_N + STAGES * NUM + 1024;
+    // a stage of Q more than of G: it is held until dK of its tile, which comes last
+    static constexpr int GS = DH == 64 ? 3 : 2, QS = GS + 1, KT = sq_bytes<DH>(), TILE = sq_bytes<DH, W>(), NUM = 8 * W;
+    // K and V, stages of Q and G, two of -lse log2 e and -D of W queries, barriers and the rest (no room for more with heads of 128)
+    static constexpr int OFF_V = KT, OFF_Q = 2 * KT, OFF_G = OFF_Q + QS * TILE, OFF_N = OFF_G + GS * TILE, OFF_R = OFF_N + 2 * NUM;
+    static constexpr int SMEM = OFF_R + 8 * (2 * QS + 2 * GS + 10) + 48 + 2 * SQ_ROWS;
+    static_assert((QS + GS) * TILE >= 4 * SQ_INTS, "starts and lengths before queries");
     static constexpr int T_DP = W, T_DV = 2 * W, T_DK = 2 * W + DH, COLS = pow2_cols(2 * W + 2 * DH);
     static_assert(OFF_N >= 2 * SQ_ROWS * DH * 4, "a CTA's sums for its cluster");
 };
@@ -269,45 +311,52 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                                                                      const SeqAttn a, const float c, const float *delta, const int ctas) {
     using L = DkvLayout<DH, W>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
-    constexpr int ST = L::STAGES;
-    extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[4 * ST + 6];
-    __shared__ uint32_t tslot;
-    __shared__ int failed, span[2][4];
-    __shared__ uint8_t odd_rows[2][SQ_ROWS];
-    const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
-    uint8_t *smp = raw + (sm - s_addr(raw));
+    constexpr int QS = L::QS, GS = L::GS;
+    extern __shared__ __align__(1024) uint8_t smp[];  // nothing else is in shared memory
+    const uint32_t sm = s_addr(smp), bar0 = sm + L::OFF_R;
+    int *rest = reinterpret_cast<int *>(smp + L::OFF_R + 8 * (2 * QS + 2 * GS + 10));
+    uint32_t &tslot = *reinterpret_cast<uint32_t *>(rest);
+    int &failed = rest[1], *span_lo = rest + 2, *span_hi = rest + 6;
+    uint8_t *odd_rows = reinterpret_cast<uint8_t *>(rest + 12);
     const auto q_full = [&](int s) { return bar0 + 8 * s; };
-    const auto q_free = [&](int s) { return bar0 + 8 * (ST + s); };
-    const auto g_full = [&](int s) { return bar0 + 8 * (2 * ST + s); };
-    const auto g_free = [&](int s) { return bar0 + 8 * (3 * ST + s); };
-    const uint32_t kv_full = bar0 + 8 * (4 * ST), s_full = kv_full + 8, dp_full = kv_full + 16, p_full = kv_full + 24, ds_full = kv_full + 32,
-                   out_full = kv_full + 40;
+    const auto q_free = [&](int s) { return bar0 + 8 * (QS + s); };
+    const auto g_full = [&](int s) { return bar0 + 8 * (2 * QS + s); };
+    const auto g_free = [&](int s) { return bar0 + 8 * (2 * QS + GS + s); };
+    const uint32_t kv_full = bar0 + 8 * (2 * QS + 2 * GS), s_full = kv_full + 8, dp_full = kv_full + 16, p_full = kv_full + 24, ds_full = kv_full + 32,
+                   out_full = kv_full + 40, n_full = kv_full + 48, n_free = kv_full + 64;  // the last: two each
+    if (sm & 1023u) {  // alike in all threads of all CTAs
+        if (threadIdx.x == 0) set_status(a.status, MNMT_ECUDA);
+        return;
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int share = (int)blockIdx.x % ctas, unit = (int)blockIdx.x / ctas, hk = unit % a.hkv, tile = unit / a.hkv;
     const int h0 = hk * a.group(), heads = a.group();
     const int half = warp >> 2, rt = (int)threadIdx.x & 127, row = tile * SQ_ROWS + rt;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < ST; s++) mbar_init(q_full(s), 2), mbar_init(q_free(s), 1), mbar_init(g_full(s), 1), mbar_init(g_free(s), 1);
+        for (int s = 0; s < QS; s++) mbar_init(q_full(s), 1), mbar_init(q_free(s), 1);
+        for (int s = 0; s < GS; s++) mbar_init(g_full(s), 1), mbar_init(g_free(s), 1);
+        mbar_init(n_full, 1), mbar_init(n_full + 8, 1), mbar_init(n_free, 8), mbar_init(n_free + 8, 8);
         mbar_init(kv_full, 2), mbar_init(s_full, 1), mbar_init(dp_full, 1), mbar_init(p_full, 8), mbar_init(ds_full, 8), mbar_init(out_full, 1);
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) tmem_alloc<L::COLS>(s_addr(&tslot));
     pdl_grid_wait();
+    const SeqAttn ix = seq_shared(a, reinterpret_cast<int *>(smp + L::OFF_Q), BW_THREADS);  // where queries come later
     Span qs{0, 0};
     bool in = false;
     if (warp < 8) {
-        qs = queries_of_lane(a, row - lane, in);
+        qs = queries_of_key(ix, row, in);
         const bool some = qs.hi > qs.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? qs.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? qs.hi : 0);
-        if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi;
+        if (lane == 0 && half == 0) span_lo[warp] = lo, span_hi[warp] = hi;
     }
+    sq_before_copies();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tS = tslot, tP = tS + L::T_DP, tV = tS + L::T_DV, tK = tS + L::T_DK;
-    const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
+    const int first = min(min(span_lo[0], span_lo[1]), min(span_lo[2], span_lo[3])), end = max(max(span_hi[0], span_hi[1]), max(span_hi[2], span_hi[3]));
     const int nt = end > first ? (end - first + W - 1) / W : 0;  // tiles of one head
     // this CTA's steps of the walk over all heads: n of them from step0 on
     const int step0 = (int)((long)nt * heads * share / ctas), n = (int)((long)nt * heads * (share + 1) / ctas) - step0;
@@ -320,36 +369,48 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                 sq_load<DH>(sm, &tk, hk, tile * SQ_ROWS, kv_full);
                 sq_load<DH>(sm + L::OFF_V, &tv, hk, tile * SQ_ROWS, kv_full);
             }
-            int j = 0, h = h0 + head0, t = t0;
+            // Q(0), then G(j), Q(j + QS - GS) and the numbers of tile j's queries by turns
+            int jq = 0, jg = 0, hq = h0 + head0, tq_ = t0, hg = hq, tg_ = t0;
             bool ok = true;
-            for (; j < n; j++) {
-                const int s = j % ST, at = end - W * (t + 1);
-                const uint32_t ph = (uint32_t)(j / ST - 1) & 1;
-                if (j >= ST) ok = wait(q_free(s), ph);
-                if (!__all_sync(0xFFFFFFFFu, ok)) break;
-                if (lane == 0) sq_load<DH, W>(sm + L::OFF_Q + s * L::TILE, &tq, h, at, q_full(s));
-                // -lse log2 e and -D of the tile's queries
-                float *num = reinterpret_cast<float *>(smp + L::OFF_N + s * L::NUM);
+            const auto next_q = [&] {
+                const int s = jq % QS;
+                if (jq >= QS) ok = __all_sync(0xFFFFFFFFu, wait(q_free(s), (uint32_t)(jq / QS - 1) & 1));
+                if (!ok) return;
+                if (lane == 0) sq_load<DH, W>(sm + L::OFF_Q + s * L::TILE, &tq, hq, end - W * (tq_ + 1), q_full(s));
+                if (++tq_ == nt) tq_ = 0, hq++;
+                jq++;
+            };
+            next_q();
+            while (ok && jg < n) {
+                const int s = jg % GS, at = end - W * (tg_ + 1);
+                if (jg >= GS) ok = __all_sync(0xFFFFFFFFu, wait(g_free(s), (uint32_t)(jg / GS - 1) & 1));
+                if (!ok) break;
+                if (lane == 0) sq_load<DH, W>(sm + L::OFF_G + s * L::TILE, &tg, hg, at, g_full(s));
+                // -lse log2 e and -D
+                float x[2][W / 32];
 #pragma unroll
                 for (int i = 0; i < W / 32; i++) {
                     const int r = at + 32 * i + lane;
                     const bool on = r >= 0 && r < a.q_rows;
-                    num[32 * i + lane] = on ? -LOG2E * __ldg(a.lse + (long)h * a.q_rows + r) : 0.0f;
-                    num[W + 32 * i + lane] = on ? -delta[(long)h * a.q_rows + r] : 0.0f;
+                    x[0][i] = on ? -LOG2E * __ldg(a.lse + (long)hg * a.q_rows + r) : 0.0f;
+                    x[1][i] = on ? -delta[(long)hg * a.q_rows + r] : 0.0f;
                 }
+                if (++tg_ == nt) tg_ = 0, hg++;
+                const int b = jg & 1, turn = jg >> 1;
+                jg++;
+                while (ok && jq < n && jq < jg + QS - GS) next_q();
+                if (ok && turn) ok = __all_sync(0xFFFFFFFFu, wait(n_free + 8 * b, (uint32_t)(turn - 1) & 1));
+                if (!ok) break;
+                float *num = reinterpret_cast<float *>(smp + L::OFF_N + b * L::NUM);
+#pragma unroll
+                for (int i = 0; i < W / 32; i++) num[32 * i + lane] = x[0][i], num[W + 32 * i + lane] = x[1][i];
                 __syncwarp();
-                if (lane == 0) mbar_arrive(q_full(s));
-                if (j >= ST) ok = wait(g_free(s), ph);
-                if (!__all_sync(0xFFFFFFFFu, ok)) {
-                    wait(q_full(s), (uint32_t)(j / ST) & 1);  // in flight
-                    break;
-                }
-                if (lane == 0) sq_load<DH, W>(sm + L::OFF_G + s * L::TILE, &tg, h, at, g_full(s));
-                if (++t == nt) t = 0, h++;
+                if (lane == 0) mbar_arrive(n_full + 8 * b);
             }
             if (failed) {  // copies in flight land before the block ends
                 wait(kv_full, 0);
-                for (int i = max(0, j - ST); i < j; i++) wait(q_full(i % ST), (uint32_t)(i / ST) & 1), wait(g_full(i % ST), (uint32_t)(i / ST) & 1);
+                for (int i = max(0, jq - QS); i < jq; i++) wait(q_full(i % QS), (uint32_t)(i / QS) & 1);
+                for (int i = max(0, jg - GS); i < jg; i++) wait(g_full(i % GS), (uint32_t)(i / GS) & 1);
             }
         }
     } else if (warp == 9) {
@@ -358,8 +419,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             const uint64_t kd = sq_k(sm), vd = sq_k(sm + L::OFF_V), qd = sq_k(sm + L::OFF_Q), gd = sq_k(sm + L::OFF_G);
             const uint64_t qt = sq_mn<W>(sm + L::OFF_Q), gt = sq_mn<W>(sm + L::OFF_G);
             const auto scores = [&](int j) {  // S^T(j)
-                const int s = j % ST;
-                if (!wait(q_full(s), (uint32_t)(j / ST) & 1)) return false;
+                const int s = j % QS;
+                if (!wait(q_full(s), (uint32_t)(j / QS) & 1)) return false;
                 tc_fence_after();
                 const uint64_t b = qd + (uint64_t)(s * (L::TILE >> 4));
 #pragma unroll
@@ -368,8 +429,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                 return true;
             };
             const auto weights = [&](int j) {  // dP^T(j)
-                const int s = j % ST;
-                if (!wait(g_full(s), (uint32_t)(j / ST) & 1)) return false;
+                const int s = j % GS;
+                if (!wait(g_full(s), (uint32_t)(j / GS) & 1)) return false;
                 tc_fence_after();
                 const uint64_t b = gd + (uint64_t)(s * (L::TILE >> 4));
 #pragma unroll
@@ -379,22 +440,22 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             };
             bool ok = wait(kv_full, 0) && scores(0) && weights(0);
             for (int j = 0; j < n && ok; j++) {
-                const int s = j % ST;
-                const uint64_t off = (uint64_t)(s * (L::TILE >> 4));
+                const int sq = j % QS, sg = j % GS;
+                const uint64_t qoff = (uint64_t)(sq * (L::TILE >> 4)), goff = (uint64_t)(sg * (L::TILE >> 4));
                 if (!(ok = wait(p_full, (uint32_t)j & 1))) break;
                 tc_fence_after();
                 // a row's two threads write W / 4 columns each, W / 2 apart
 #pragma unroll
                 for (int k = 0; k < W / 16; k++)
-                    sq_mma_ta(on, tV, tS + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), gt + off + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
-                f4_commit_on<1>(on, g_free(s));
+                    sq_mma_ta(on, tV, tS + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), gt + goff + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                f4_commit_on<1>(on, g_free(sg));
                 if (j + 1 < n && !(ok = scores(j + 1))) break;
                 if (!(ok = wait(ds_full, (uint32_t)j & 1))) break;
                 tc_fence_after();
 #pragma unroll
                 for (int k = 0; k < W / 16; k++)
-                    sq_mma_ta(on, tK, tP + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), qt + off + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
-                f4_commit_on<1>(on, q_free(s));
+                    sq_mma_ta(on, tK, tP + 8 * (k % (W / 32)) + W / 2 * (k / (W / 32)), qt + qoff + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
+                f4_commit_on<1>(on, q_free(sq));
                 if (j + 1 < n && !(ok = weights(j + 1))) break;
             }
             f4_commit_on<1>(on, out_full);
@@ -406,12 +467,11 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
         const unsigned long long c2 = f4_two(c, c);
         bool ok = true;
         for (int j = 0, t = t0; j < n; j++) {
-            const int s = j % ST, at = end - W * (t + 1) + W / 2 * half, lo = qs.lo - at, hi = qs.hi - at;
+            const int at = end - W * (t + 1) + W / 2 * half, lo = qs.lo - at, hi = qs.hi - at;
             if (++t == nt) t = 0;
-            const float4 *num = reinterpret_cast<const float4 *>(smp + L::OFF_N + s * L::NUM) + W / 8 * half;
+            const float4 *num = reinterpret_cast<const float4 *>(smp + L::OFF_N + (j & 1) * L::NUM) + W / 8 * half;
             const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= W / 2), some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
-            // the producer's numbers are visible with the tile that they came with
-            if (!(ok = wait(s_full, (uint32_t)j & 1) && wait(q_full(s), (uint32_t)(j / ST) & 1))) break;
+            if (!(ok = wait(s_full, (uint32_t)j & 1) && wait(n_full + 8 * (j & 1), (uint32_t)(j >> 1) & 1))) break;
             tc_fence_after();
             // Two passes over a thread's columns, P and dS, without the masks where the warp's rows see all of them
             uint32_t r[W / 64][32];
@@ -491,6 +551,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                 for (int b = 0; b < W / 64; b++) tmem_st16(tP + lanes + W / 2 * half + 16 * b, zeros);
             }
             written(ds_full);
+            if (lane == 0) mbar_arrive(n_free + 8 * (j & 1));
         }
         if (n) ok = wait(out_full, 0) && ok;
         tc_fence_after();
@@ -558,9 +619,9 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                 }
             }
         }
-        odd_rows[half][rt] = odd;
+        odd_rows[half * SQ_ROWS + rt] = odd;
         elements_sync();
-        odd = ok && in && (odd_rows[0][rt] || odd_rows[1][rt]);
+        odd = ok && in && (odd_rows[rt] || odd_rows[SQ_ROWS + rt]);
         for (uint32_t again = __ballot_sync(0xFFFFFFFFu, odd && (rt & 1) == half); again; again &= again - 1) {
             const int src = __ffs(again) - 1, rr = __shfl_sync(0xFFFFFFFFu, row, src);
             const Span sp{__shfl_sync(0xFFFFFFFFu, qs.lo, src), __shfl_sync(0xFFFFFFFFu, qs.hi, src)};
@@ -600,11 +661,11 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     bool in;
     if (a.k_rows == 0) {
         if (w >= a.q_rows) return;
-        keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in);
+        keys_of_query(a, (int)w, in);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hq; h++) store4(static_cast<T *>(a.dq.p) + w * a.dq.ld + h * a.dq.hd + 4 * lane, z);
     } else {
         if (w >= a.k_rows) return;
-        queries_of_key(a, (int)w, seq_of(a.k_start, a.n_seqs, (int)w), in);
+        queries_of_key(a, (int)w, in);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hkv; h++) {
             store4(static_cast<T *>(a.dk.p) + w * a.dk.ld + h * a.dk.hd + 4 * lane, z);
             store4(static_cast<T *>(a.dv.p) + w * a.dv.ld + h * a.dv.hd + 4 * lane, z);

@@ -169,6 +169,9 @@ cudaError_t sq_launch(void (*kernel)(KArgs...), unsigned grid, int ctas, int thr
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args &&>(args)...);
 }
 
+// what was written to or read from shared memory comes before copies into it by TMA (all threads, before a barrier)
+__device__ __forceinline__ void sq_before_copies() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // Waits of a kernel's roles: a wait that gives up sets `failed` in shared memory and the
 // status, and every role leaves its loop at its next wait.
 struct SqWaits {
