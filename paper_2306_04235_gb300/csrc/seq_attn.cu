@@ -21,12 +21,14 @@ namespace {
 
 constexpr int FW_THREADS = 192;  // four softmax warps, a TMA warp, an MMA warp
 constexpr int KT = 64;           // keys of a tile
-// BUFS: tiles of scores in TMEM; BLOCKS: CTAs per SM
 template <int DH>
 struct FwLayout {
-    static constexpr int STAGES = DH == 64 ? 4 : 2, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, KT>();
-    static constexpr int OFF_K = QT, OFF_V = OFF_K + STAGES * TILE, SMEM = OFF_V + STAGES * TILE + 1024;
+    // tiles of keys and values, of queries
+    static constexpr int STAGES = DH == 64 ? 4 : 2, QS = DH == 64 ? 2 : 1, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, KT>();
+    static constexpr int OFF_K = QS * QT, OFF_V = OFF_K + STAGES * TILE, SMEM = OFF_V + STAGES * TILE + 1024;
     static_assert(2 * STAGES * TILE >= 4 * SQ_INTS, "starts and lengths before keys and values");
+    static_assert(OFF_V + STAGES * TILE >= SQ_ROWS * (DH * 4 + 8), "a CTA's sums for its cluster");
+    // tiles of scores in TMEM, columns of O behind them; CTAs per SM
     static constexpr int BUFS = DH == 64 ? 3 : 2, T_O = BUFS * KT, COLS = pow2_cols(T_O + DH), BLOCKS = 512 / COLS;
 };
 constexpr float FW_SLACK = 8.0f;  // how far, in powers of two, a score may exceed m
@@ -53,15 +55,100 @@ __device__ __forceinline__ void weigh(const uint32_t (&r)[32], unsigned long lon
     }
 }
 
+// Rows of `again`, a lane's row each, computed again over their own keys; columns c0 .. c1 - 1 are stored
+template <typename T>
+__device__ __noinline__ void forward_again(const SeqAttn &a, uint32_t again, int row, int h, Span keys, float c, int c0, int c1) {
+    const int lane = threadIdx.x & 31, hk = h / a.group();
+    for (; again; again &= again - 1) {
+        const int src = __ffs(again) - 1, rr = __shfl_sync(0xFFFFFFFFu, row, src);
+        const Span s{__shfl_sync(0xFFFFFFFFu, keys.lo, src), __shfl_sync(0xFFFFFFFFu, keys.hi, src)};
+        const RowSum x = attn_row(static_cast<const T *>(a.q.p) + rr * a.q.ld + h * a.q.hd, static_cast<const T *>(a.k.p) + hk * a.k.hd, a.k.ld,
+                                  static_cast<const T *>(a.v.p) + hk * a.v.hd, a.v.ld, s, a.dh, c);
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] = x.acc[i] / x.l;
+        if (4 * lane >= c0 && 4 * lane < c1 && 4 * lane < a.dh) store4(static_cast<T *>(a.o.p) + rr * a.o.ld + h * a.o.hd + 4 * lane, v);
+    }
+}
+
+// The end of a CTA whose cluster divides a head's walk: its softmax warps meet the others' here once
+template <int DH, bool BF>
+__device__ __noinline__ void forward_join(const SeqAttn &a, uint8_t *smp, int ctas, int share, int row, int h0, bool in, Span keys, float c, float m, float l,
+                                          bool ok, uint32_t tO, int nt) {
+    using T = std::conditional_t<BF, __nv_bfloat16, __half>;
+    const bool none = keys.hi <= keys.lo;
+    // This CTA's sums, four columns of a row side by side, and its m and l, where queries and keys were
+    float4 *mine = reinterpret_cast<float4 *>(smp) + threadIdx.x;
+    float2 *ml = reinterpret_cast<float2 *>(smp + SQ_ROWS * DH * 4) + threadIdx.x;
+#pragma unroll
+    for (int b = 0; b < DH / 32; b++) {
+        uint32_t w[32];
+        if (nt) tmem_ld32(tO + 32 * b, w);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            mine[(8 * b + i) * SQ_ROWS] = nt ? make_float4(__uint_as_float(w[4 * i]), __uint_as_float(w[4 * i + 1]), __uint_as_float(w[4 * i + 2]),
+                                                           __uint_as_float(w[4 * i + 3]))
+                                             : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    *ml = make_float2(m, l);
+    __syncwarp();
+    sq_cluster_sync();
+    // every CTA joins a share of the columns, in the order of the CTAs
+    const int c0 = DH / ctas * share, c1 = c0 + DH / ctas;
+    const uint32_t at = s_addr(mine), at_ml = s_addr(ml);
+    float w[8], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 8; r++) {
+        if (r >= ctas) continue;
+        const float2 x = sq_remote2(t2_mapa(at_ml, r));
+        top = fmaxf(top, x.x);
+        w[r] = x.x;
+    }
+    const float mu = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int r = 0; r < 8; r++) {
+        if (r >= ctas) continue;
+        w[r] = exp2_fast(w[r] - mu);
+        sum = fmaf(sq_remote2(t2_mapa(at_ml, r)).y, w[r], sum);
+    }
+    const float inv = none ? 0.0f : 1.0f / sum;
+    bool odd = false;
+    if (ok) {
+        T *o = static_cast<T *>(a.o.p) + row * a.o.ld + h0 * a.o.hd;
+#pragma unroll 1
+        for (int col = c0; col < c1; col += 8) {
+            float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int r = 0; r < 8; r++) {
+                if (r >= ctas) continue;
+                const uint32_t from = t2_mapa(at + (col / 4) * (SQ_ROWS * 16), r);
+                const float4 y = sq_remote(from), z = sq_remote(from + SQ_ROWS * 16);
+                v[0] = fmaf(y.x, w[r], v[0]), v[1] = fmaf(y.y, w[r], v[1]), v[2] = fmaf(y.z, w[r], v[2]), v[3] = fmaf(y.w, w[r], v[3]);
+                v[4] = fmaf(z.x, w[r], v[4]), v[5] = fmaf(z.y, w[r], v[5]), v[6] = fmaf(z.z, w[r], v[6]), v[7] = fmaf(z.w, w[r], v[7]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                odd |= !(fabsf(v[i]) < INFINITY);
+                v[i] = none ? 0.0f : v[i] * inv;
+            }
+            if (in) sq_store<BF>(o, col, a.dh, v);
+        }
+        if (in && a.lse && share == 0) a.lse[(long)h0 * a.q_rows + row] = none ? -INFINITY : row_lse(top, sum);
+    }
+    __syncwarp();
+    forward_again<T>(a, __ballot_sync(0xFFFFFFFFu, ok && in && !none && odd && fabsf(sum) < INFINITY), row, h0, keys, c, c0, c1);
+}
+
 template <int DH, bool BF>
 __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     seq_attn_forward_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
-                            const SeqAttn a, const float c) {
+                            const __grid_constant__ SeqAttn a, const float c, const int heads, const int ctas) {
     using L = FwLayout<DH>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
-    constexpr int ST = L::STAGES, BUFS = L::BUFS;
+    constexpr int ST = L::STAGES, BUFS = L::BUFS, QS = L::QS;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[4 * ST + 4 + 2 * BUFS];
+    __shared__ __align__(8) uint64_t bars[4 * ST + 2 * QS + 5 + 2 * BUFS];
     __shared__ uint32_t tslot;
     __shared__ int failed, span[2][4];
     const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
@@ -70,26 +157,31 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     const auto k_free = [&](int s) { return bar0 + 8 * (ST + s); };
     const auto v_full = [&](int s) { return bar0 + 8 * (2 * ST + s); };
     const auto v_free = [&](int s) { return bar0 + 8 * (3 * ST + s); };
-    const uint32_t q_full = bar0 + 8 * (4 * ST), o_full = q_full + 8, pv_done = q_full + 16, s_full = q_full + 32,
+    const auto q_full = [&](int s) { return bar0 + 8 * (4 * ST + s); };
+    const auto q_free = [&](int s) { return bar0 + 8 * (4 * ST + QS + s); };
+    const uint32_t o_full = bar0 + 8 * (4 * ST + 2 * QS), o_free = o_full + 8, pv_done = o_full + 16, done = o_full + 32, s_full = o_full + 40,
                    p_full = s_full + 8 * BUFS;  // two of pv_done by turns, BUFS of s_full and p_full (a warp may be a tile ahead)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int h = blockIdx.x % a.hq, tile = (int)(gridDim.x / a.hq) - 1 - (int)(blockIdx.x / a.hq);  // the last rows (causal: the longest) first
-    const int row = tile * SQ_ROWS + (int)threadIdx.x;
+    // heads h0 .. h0 + nh - 1 of a tile of rows, the last rows (causal: the longest walks) first
+    // (ctas > 1: a cluster divides the walk of one head)
+    const int groups = (a.hq + heads - 1) / heads, share = (int)blockIdx.x % ctas, unit = (int)blockIdx.x / ctas;
+    const int h0 = unit % groups * heads, nh = min(heads, a.hq - h0);
+    const int tile = (int)gridDim.x / ctas / groups - 1 - unit / groups, row = tile * SQ_ROWS + (int)threadIdx.x;
     if (threadIdx.x == 128) {
         for (int s = 0; s < ST; s++) mbar_init(k_full(s), 1), mbar_init(k_free(s), 1), mbar_init(v_full(s), 1), mbar_init(v_free(s), 1);
+        for (int s = 0; s < QS; s++) mbar_init(q_full(s), 1), mbar_init(q_free(s), 4);
         for (int b = 0; b < BUFS; b++) mbar_init(s_full + 8 * b, 1), mbar_init(p_full + 8 * b, 4);
-        mbar_init(q_full, 1), mbar_init(o_full, 1), mbar_init(pv_done, 1), mbar_init(pv_done + 8, 1);
+        mbar_init(o_full, 1), mbar_init(o_free, 4), mbar_init(pv_done, 1), mbar_init(pv_done + 8, 1), mbar_init(done, 1);
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 5) tmem_alloc<L::COLS>(s_addr(&tslot));
     pdl_grid_wait();
-    if (threadIdx.x == 128) sq_load<DH>(sm, &tq, h, tile * SQ_ROWS, q_full);
     const SeqAttn ix = seq_shared(a, reinterpret_cast<int *>(smp + L::OFF_K), FW_THREADS);  // where keys and values come later
     Span keys{0, 0};
     bool in = false;
     if (warp < 4) {
-        keys = keys_of_query(ix, row, in);
+        keys = keys_of_lane(ix, row - lane, in);
         const bool some = keys.hi > keys.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? keys.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? keys.hi : 0);
         if (lane == 0) span[0][warp] = lo, span[1][warp] = hi;
@@ -100,26 +192,43 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     tc_fence_after();
     const uint32_t tS = tslot, tO = tslot + L::T_O;  // P(j) takes the first half of S(j)'s columns
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
-    const int nt = end > first ? (end - first + KT - 1) / KT : 0;
+    // this CTA's tiles of a head, nt of them from t0 on; of all heads
+    const int all_t = end > first ? (end - first + KT - 1) / KT : 0, t0 = (int)((long)all_t * share / ctas), nt = (int)((long)all_t * (share + 1) / ctas) - t0;
+    const int n = nt * nh;
     const SqWaits wait{&failed, a.status};
 
     if (warp == 4) {
         if (lane == 0) {
-            const int hk = h / a.group();
-            int j = 0;
-            for (; j < nt; j++) {
-                const int s = j % ST, at = end - KT * (j + 1);
-                const uint32_t ph = (uint32_t)(j / ST - 1) & 1;
-                if (j >= ST && !wait(k_free(s), ph)) break;
-                sq_load<DH, KT>(sm + L::OFF_K + s * L::TILE, &tk, hk, at, k_full(s));
-                if (j >= ST && !wait(v_free(s), ph)) {
-                    wait(k_full(s), (uint32_t)(j / ST) & 1);  // in flight
-                    break;
+            int j = 0, nq = 1;  // tiles of keys and values, and tiles of queries, whose copies were issued
+            sq_load<DH>(sm, &tq, h0, tile * SQ_ROWS, q_full(0));
+            bool ok = true;
+            for (int it = 0; it < nh && nt && ok; it++) {
+                const int hk = (h0 + it) / a.group();
+                for (int t = 0; t < nt && ok; t++, j++) {
+                    const int s = j % ST, at = end - KT * (t0 + t + 1);
+                    const uint32_t ph = (uint32_t)(j / ST - 1) & 1;
+                    if (j >= ST && !(ok = wait(k_free(s), ph))) break;
+                    sq_load<DH, KT>(sm + L::OFF_K + s * L::TILE, &tk, hk, at, k_full(s));
+                    if (j >= ST && !(ok = wait(v_free(s), ph))) {
+                        wait(k_full(s), (uint32_t)(j / ST) & 1);  // in flight
+                        break;
+                    }
+                    sq_load<DH, KT>(sm + L::OFF_V + s * L::TILE, &tv, hk, at, v_full(s));
+                    // the next head's queries, once the results of the head that had their place are stored
+                    if (t == min(1, nt - 1) && QS > 1 && nq < nh) {
+                        if (nq >= QS && !(ok = wait(q_free(nq % QS), (uint32_t)(nq / QS - 1) & 1))) continue;
+                        sq_load<DH>(sm + nq % QS * L::QT, &tq, h0 + nq, tile * SQ_ROWS, q_full(nq % QS));
+                        nq++;
+                    }
                 }
-                sq_load<DH, KT>(sm + L::OFF_V + s * L::TILE, &tv, hk, at, v_full(s));
+                if (QS == 1 && ok && nq < nh) {
+                    if (!(ok = wait(q_free(0), (uint32_t)it & 1))) break;
+                    sq_load<DH>(sm, &tq, h0 + nq, tile * SQ_ROWS, q_full(0));
+                    nq++;
+                }
             }
             if (failed || nt == 0) {  // copies in flight land before the block ends
-                wait(q_full, 0);
+                for (int i = max(0, nq - QS); i < nq; i++) wait(q_full(i % QS), (uint32_t)(i / QS) & 1);
                 for (int i = max(0, j - ST); i < j; i++) wait(k_full(i % ST), (uint32_t)(i / ST) & 1), wait(v_full(i % ST), (uint32_t)(i / ST) & 1);
             }
         }
@@ -127,146 +236,165 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
         if (nt) {
             const uint32_t on = elect_one();
             const uint64_t qd = sq_k(sm), kd = sq_k(sm + L::OFF_K), vd = sq_mn<KT>(sm + L::OFF_V);
-            const auto scores = [&](int j) {  // S(j)
-                const int s = j % ST;
-                if (!wait(k_full(s), (uint32_t)(j / ST) & 1)) return false;
+            int next = 0, nit = 0, nst = 0;  // the next scores: number, head and tile of it
+            const auto scores = [&] {
+                const int s = next % ST;
+                if (nst == 0 && !wait(q_full(nit % QS), (uint32_t)(nit / QS) & 1)) return false;
+                if (!wait(k_full(s), (uint32_t)(next / ST) & 1)) return false;
                 tc_fence_after();
-                const uint64_t b = kd + (uint64_t)(s * (L::TILE >> 4));
-                const uint32_t d = tS + j % BUFS * KT;
+                const uint64_t a = qd + (uint64_t)(nit % QS * (L::QT >> 4)), b = kd + (uint64_t)(s * (L::TILE >> 4));
+                const uint32_t d = tS + next % BUFS * KT;
 #pragma unroll
-                for (int k = 0; k < DH / 16; k++) sq_mma(on, d, qd + sq_k_step(k), b + sq_k_step<KT>(k), sq_idesc(KT, BF, false), k > 0);
+                for (int k = 0; k < DH / 16; k++) sq_mma(on, d, a + sq_k_step(k), b + sq_k_step<KT>(k), sq_idesc(KT, BF, false), k > 0);
                 f4_commit_on<1>(on, k_free(s));
-                f4_commit_on<1>(on, s_full + 8 * (j % BUFS));
+                f4_commit_on<1>(on, s_full + 8 * (next % BUFS));
+                next++;
+                if (++nst == nt) nst = 0, nit++;
                 return true;
             };
-            bool ok = wait(q_full, 0);
-            for (int j = 0; j < BUFS && j < nt && ok; j++) ok = scores(j);
-            for (int j = 0; j < nt && ok; j++) {
-                const int s = j % ST;
-                if (!(ok = wait(p_full + 8 * (j % BUFS), (uint32_t)(j / BUFS) & 1) && wait(v_full(s), (uint32_t)(j / ST) & 1))) break;
-                tc_fence_after();
-                const uint64_t b = vd + (uint64_t)(s * (L::TILE >> 4));
-                const uint32_t p = tS + j % BUFS * KT;
+            bool ok = true;
+            for (int it = 0, j = 0; it < nh && ok; it++)
+                for (int t = 0; t < nt && ok; t++, j++) {
+                    // Scores up to BUFS tiles ahead (MMAs keep their order: P(j - 1), whose place S(j + BUFS - 1) takes, has been
+                    // read).  The next head's only if its queries are there: they may wait for what this head has yet to do.
+                    while (ok && next < n && next < j + BUFS &&
+                           (next == j || nst > 0 || (nit <= it + QS - 1 && __all_sync(0xFFFFFFFFu, mbar_test(q_full(nit % QS), (uint32_t)(nit / QS) & 1)))))
+                        ok = scores();
+                    if (ok && t == 0 && it > 0) ok = wait(o_free, (uint32_t)(it - 1) & 1);  // the last head's O has been read
+                    const int s = j % ST;
+                    if (!ok || !(ok = wait(p_full + 8 * (j % BUFS), (uint32_t)(j / BUFS) & 1) && wait(v_full(s), (uint32_t)(j / ST) & 1))) break;
+                    tc_fence_after();
+                    const uint64_t b = vd + (uint64_t)(s * (L::TILE >> 4));
+                    const uint32_t p = tS + j % BUFS * KT;
 #pragma unroll
-                for (int k = 0; k < KT / 16; k++) sq_mma_ta(on, tO, p + 8 * k, b + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
-                f4_commit_on<1>(on, v_free(s));
-                f4_commit_on<1>(on, pv_done + 8 * (j & 1));
-                if (j + BUFS < nt && !(ok = scores(j + BUFS))) break;  // MMAs keep their order: P(j) has been read
-            }
-            f4_commit_on<1>(on, o_full);
-            wait(o_full, 0);
+                    for (int k = 0; k < KT / 16; k++) sq_mma_ta(on, tO, p + 8 * k, b + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(t | k));
+                    f4_commit_on<1>(on, v_free(s));
+                    f4_commit_on<1>(on, pv_done + 8 * (j & 1));
+                    if (t == nt - 1) f4_commit_on<1>(on, o_full);
+                }
+            f4_commit_on<1>(on, done);
+            wait(done, 0);
         }
         pdl_allow_next();
     } else {
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        float m = -INFINITY, l = 0.0f;  // m: of c s
         bool ok = true;
-        for (int j = 0; j < nt; j++) {
-            if (!(ok = wait(s_full + 8 * (j % BUFS), (uint32_t)(j / BUFS) & 1))) break;
-            tc_fence_after();
-            const uint32_t tP = tS + j % BUFS * KT + lanes;
-            const int at = end - KT * (j + 1), lo = keys.lo - at, hi = keys.hi - at;
-            const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= KT);
-            const auto p_ready = [&] {
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + 8 * (j % BUFS));
-            };
-            if (!__any_sync(0xFFFFFFFFu, hi > 0 && lo < KT)) {  // no row of the warp sees a key of the tile
-                const uint32_t zeros[16] = {};
+        float m = -INFINITY, l = 0.0f;  // m: of c s
+        const bool none = keys.hi <= keys.lo;  // no key: zeros; a sum of nothing but zeros is not a number, as 0 / 0
+        for (int it = 0, j = 0; it < nh && ok; it++) {
+            const int h = h0 + it;
+            m = -INFINITY, l = 0.0f;
+            for (int t = 0; t < nt; t++, j++) {
+                if (!(ok = wait(s_full + 8 * (j % BUFS), (uint32_t)(j / BUFS) & 1))) break;
+                tc_fence_after();
+                const uint32_t tP = tS + j % BUFS * KT + lanes;
+                const int at = end - KT * (t0 + t + 1), lo = keys.lo - at, hi = keys.hi - at;
+                const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= KT);
+                const auto p_ready = [&] {
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full + 8 * (j % BUFS));
+                };
+                if (!__any_sync(0xFFFFFFFFu, hi > 0 && lo < KT)) {  // no row of the warp sees a key of the tile
+                    const uint32_t zeros[16] = {};
 #pragma unroll
-                for (int b = 0; b < KT / 32; b++) tmem_st16(tP + 16 * b, zeros);
-                p_ready();
-                continue;
-            }
-            uint32_t r[KT / 32][32];
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    for (int b = 0; b < KT / 32; b++) tmem_st16(tP + 16 * b, zeros);
+                    p_ready();
+                    continue;
+                }
+                uint32_t r[KT / 32][32];
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int b = 0; b < KT / 32; b++) tmem_ld32(tP + 32 * b, r[b]);
-            tmem_wait_ld();
-            if (!all) {
+                for (int b = 0; b < KT / 32; b++) tmem_ld32(tP + 32 * b, r[b]);
+                tmem_wait_ld();
+                if (!all) {
 #pragma unroll
-                for (int b = 0; b < KT / 32; b++) hide(r[b], sq_bits(lo - 32 * b, hi - 32 * b));
-            }
+                    for (int b = 0; b < KT / 32; b++) hide(r[b], sq_bits(lo - 32 * b, hi - 32 * b));
+                }
 #pragma unroll
-            for (int b = 0; b < KT / 32; b++) max32(r[b], mx);
-            const float top = c * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-            // the first scores, or scores that 2^8 does not hold
-            if (__any_sync(0xFFFFFFFFu, top > m + FW_SLACK)) {
-                const float mn = top > m + FW_SLACK ? top : m;
-                const float f = m == -INFINITY ? 1.0f : exp2_fast(m - mn);  // nothing was added yet: 0 stays 0
-                m = mn;
-                l *= f;
-                if (j > 0 && __any_sync(0xFFFFFFFFu, f != 1.0f)) {
-                    // P V up to the tile before is in O.  (Not every turn is waited for: those two before are over, as S(j)
-                    // was multiplied after them.)
-                    if (!(ok = wait(pv_done + 8 * ((j - 1) & 1), (uint32_t)((j - 1) >> 1) & 1))) break;
-                    tc_fence_after();
+                for (int b = 0; b < KT / 32; b++) max32(r[b], mx);
+                const float top = c * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                // the first scores, or scores that 2^8 does not hold
+                if (__any_sync(0xFFFFFFFFu, top > m + FW_SLACK)) {
+                    const float mn = top > m + FW_SLACK ? top : m;
+                    const float f = m == -INFINITY ? 1.0f : exp2_fast(m - mn);  // nothing was added yet: 0 stays 0
+                    m = mn;
+                    l *= f;
+                    if (t > 0 && __any_sync(0xFFFFFFFFu, f != 1.0f)) {
+                        // P V up to the tile before is in O.  (Not every turn is waited for: those two before are over, as S(j)
+                        // was multiplied after them.)
+                        if (!(ok = wait(pv_done + 8 * ((j - 1) & 1), (uint32_t)((j - 1) >> 1) & 1))) break;
+                        tc_fence_after();
 #pragma unroll
-                    for (int b = 0; b < DH / 16; b++) {
-                        uint32_t o[16];
-                        tmem_ld16(tO + lanes + 16 * b, o);
-                        tmem_wait_ld();
+                        for (int b = 0; b < DH / 16; b++) {
+                            uint32_t o[16];
+                            tmem_ld16(tO + lanes + 16 * b, o);
+                            tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 16; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        tmem_st16(tO + lanes + 16 * b, o);
+                            for (int i = 0; i < 16; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st16(tO + lanes + 16 * b, o);
+                        }
                     }
                 }
-            }
-            const float mu = m == -INFINITY ? 0.0f : m;  // no score yet: 2^-inf
-            const unsigned long long c2 = f4_two(c, c), m2 = f4_two(-mu, -mu);
-            unsigned long long ls = f4_two(0.0f, 0.0f);
+                const float mu = m == -INFINITY ? 0.0f : m;  // no score yet: 2^-inf
+                const unsigned long long c2 = f4_two(c, c), m2 = f4_two(-mu, -mu);
+                unsigned long long ls = f4_two(0.0f, 0.0f);
 #pragma unroll
-            for (int b = 0; b < KT / 32; b++) {
-                uint32_t p[16];
-                weigh<BF>(r[b], c2, m2, ls, p);
-                tmem_st16(tP + 16 * b, p);  // over scores that were read
+                for (int b = 0; b < KT / 32; b++) {
+                    uint32_t p[16];
+                    weigh<BF>(r[b], c2, m2, ls, p);
+                    tmem_st16(tP + 16 * b, p);  // over scores that were read
+                }
+                float la, lb;
+                f4_untwo(ls, la, lb);
+                l += la + lb;
+                p_ready();
             }
-            float la, lb;
-            f4_untwo(ls, la, lb);
-            l += la + lb;
-            p_ready();
-        }
-        ok = wait(nt ? o_full : q_full, 0) && ok;
-        tc_fence_after();
-        // no tile and no key: zeros; a sum of nothing but zeros is not a number, as 0 / 0
-        const bool none = keys.hi <= keys.lo;
-        const float inv = none ? 0.0f : 1.0f / l;
-        bool odd = false;
-        if (ok) {
+            if (ok) ok = nt ? wait(o_full, (uint32_t)it & 1) : wait(q_full(0), 0);
+            if (!ok) break;
+            tc_fence_after();
+            if (ctas > 1) break;  // one head, joined below
+            const float inv = none ? 0.0f : 1.0f / l;
             uint32_t out[DH / 2];
+            const unsigned long long i2 = f4_two(inv, inv), z2 = f4_two(0.0f, 0.0f);
+            unsigned long long nans = z2;  // sums of 0 x: not zero where an x is not finite
 #pragma unroll
             for (int b = 0; b < DH / 32; b++) {
                 uint32_t w[32];
                 if (nt) tmem_ld32(tO + lanes + 32 * b, w);
                 tmem_wait_ld();
-                float v[32];
 #pragma unroll
-                for (int i = 0; i < 32; i++) {
-                    const float x = nt ? __uint_as_float(w[i]) : 0.0f;
-                    odd |= !(fabsf(x) < INFINITY);
-                    v[i] = none ? 0.0f : x * inv;
+                for (int i = 0; i < 16; i++) {
+                    const unsigned long long x = nt ? f4_two(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])) : z2;
+                    float u, v;
+                    nans = sq_fma2(x, z2, nans);
+                    f4_untwo(f4_mul2(x, i2), u, v);
+                    out[16 * b + i] = none ? 0u : sq_pack<BF>(u, v);
                 }
-#pragma unroll
-                for (int i = 0; i < 16; i++) out[16 * b + i] = sq_pack<BF>(v[2 * i], v[2 * i + 1]);
             }
+            float na, nb;
+            f4_untwo(nans, na, nb);
+            const bool odd = !(na + nb == 0.0f);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(o_free);
             // the queries have been multiplied: their rows are free
-            sq_store_rows<DH>(smp + warp * (64 * DH), out, static_cast<uint16_t *>(a.o.p) + (long)(row - lane) * a.o.ld + h * a.o.hd, a.o.ld,
+            sq_store_rows<DH>(smp + it % QS * L::QT + warp * (64 * DH), out, static_cast<uint16_t *>(a.o.p) + (long)(row - lane) * a.o.ld + h * a.o.hd, a.o.ld,
                               __ballot_sync(0xFFFFFFFFu, in), a.dh);
+            sq_before_copies();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_free(it % QS));
             if (in && a.lse) a.lse[(long)h * a.q_rows + row] = none ? -INFINITY : row_lse(m, l);
-            const int hk = h / a.group();
-            for (uint32_t again = __ballot_sync(0xFFFFFFFFu, in && !none && odd && fabsf(l) < INFINITY); again; again &= again - 1) {
-                const int src = __ffs(again) - 1, rr = __shfl_sync(0xFFFFFFFFu, row, src);
-                const Span s{__shfl_sync(0xFFFFFFFFu, keys.lo, src), __shfl_sync(0xFFFFFFFFu, keys.hi, src)};
-                const RowSum x = attn_row(static_cast<const T *>(a.q.p) + rr * a.q.ld + h * a.q.hd, static_cast<const T *>(a.k.p) + hk * a.k.hd, a.k.ld,
-                                          static_cast<const T *>(a.v.p) + hk * a.v.hd, a.v.ld, s, a.dh, c);
-                float v[4];
-#pragma unroll
-                for (int i = 0; i < 4; i++) v[i] = x.acc[i] / x.l;
-                if (4 * lane < a.dh) store4(static_cast<T *>(a.o.p) + rr * a.o.ld + h * a.o.hd + 4 * lane, v);
-            }
+            const uint32_t again = __ballot_sync(0xFFFFFFFFu, in && !none && odd && fabsf(l) < INFINITY);
+            if (again) forward_again<T>(a, again, row, h, keys, c, 0, DH);
         }
+        if (ctas > 1) forward_join<DH, BF>(a, smp, ctas, share, row, h0, in, keys, c, m, l, ok, tO + lanes, nt);
+    }
+    if (ctas > 1) {
+        __syncwarp();
+        if (warp >= 4) sq_cluster_sync();
+        sq_cluster_sync();  // no CTA leaves while others read its sums
     }
     tc_fence_before();
     __syncthreads();
@@ -281,7 +409,7 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     const int lane = threadIdx.x & 31;
     bool in;
     if (w >= a.q_rows) return;
-    keys_of_query(a, (int)w, in);
+    keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in);
     if (!in) return;
     const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int h = 0; h < a.hq; h++) {
@@ -290,13 +418,30 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     }
 }
 
+// Heads that a CTA takes one after another: many short sequences, whose lookups and starts then
+// count once for several heads
+int forward_heads(long items, const SeqAttn &a) {
+    const long keys = a.n_seqs ? a.k_rows / a.n_seqs : 0, h = (items + 2 * 152 - 1) / (2 * 152);
+    return keys >= 256 ? 1 : (int)(h < 4 ? h : 4);
+}
+// CTAs that share the walk of a head: few tiles of rows, each with four tiles of keys at least.  Causal walks, which differ
+// in length, gain until there are two CTAs for every SM (4096 rows of 8 heads 44 -> 35 us), others until there is one
+// (64 rows on 8192 keys of 8 heads 80 -> 16; 2048 rows not causal 24 -> 26).
+int forward_ctas(long items, const SeqAttn &a) {
+    const long keys = a.n_seqs ? a.k_rows / a.n_seqs : 0;
+    int p = 1;
+    while (p < 8 && items * p < (a.causal ? 2 * 152 : 76) && keys >= 4L * KT * 2 * p) p *= 2;
+    return p;
+}
+
 template <int DH, bool BF>
 cudaError_t tile_forward(const SeqAttn &a, cudaStream_t st) {
     CUtensorMap tq, tk, tv;
     if (!sq_map(&tq, a.q, a.q_rows, a.hq, a.dh, SQ_ROWS) || !sq_map(&tk, a.k, a.k_rows, a.hkv, a.dh, KT) || !sq_map(&tv, a.v, a.k_rows, a.hkv, a.dh, KT))
         return cudaErrorInvalidValue;
-    const unsigned grid = (unsigned)((a.q_rows + SQ_ROWS - 1) / SQ_ROWS) * (unsigned)a.hq;
-    return launch_pdl(seq_attn_forward_kernel<DH, BF>, grid, FW_THREADS, FwLayout<DH>::SMEM, st, tq, tk, tv, a, a.scale * LOG2E);
+    const int tiles = (a.q_rows + SQ_ROWS - 1) / SQ_ROWS, heads = forward_heads((long)tiles * a.hq, a), ctas = forward_ctas((long)tiles * a.hq, a);
+    const unsigned grid = (unsigned)tiles * (unsigned)((a.hq + heads - 1) / heads) * (unsigned)ctas;
+    return sq_launch(seq_attn_forward_kernel<DH, BF>, grid, ctas, FW_THREADS, FwLayout<DH>::SMEM, st, tq, tk, tv, a, a.scale * LOG2E, heads, ctas);
 }
 
 template <int DH, bool BF>

@@ -32,6 +32,31 @@ __device__ __forceinline__ void load_half(uint32_t taddr, uint32_t (&r)[W / 64][
     tmem_wait_ld();
 }
 
+// Columns c0 .. c1 - 1 of a row's sums of all CTAs of a cluster, added in the order of the CTAs, times f and
+// stored to row o; at: this CTA's sums of the row.  live: 0 for a row that has none.  Whether one is not finite.
+template <bool BF>
+__device__ __forceinline__ bool sq_join(uint32_t at, int c0, int c1, int ctas, float live, float f, bool in, void *o, int dh) {
+    bool odd = false;
+#pragma unroll 2
+    for (int col = c0; col < c1; col += 8) {
+        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int r = 0; r < ctas; r++) {
+            const uint32_t from = t2_mapa(at + (col / 4) * (SQ_ROWS * 16), r);
+            const float4 y = sq_remote(from), z = sq_remote(from + SQ_ROWS * 16);
+            v[0] += y.x, v[1] += y.y, v[2] += y.z, v[3] += y.w, v[4] += z.x, v[5] += z.y, v[6] += z.z, v[7] += z.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (live == 0.0f) v[i] = 0.0f;
+            odd |= !(fabsf(v[i]) < INFINITY);
+            v[i] *= f;
+        }
+        if (in) sq_store<BF>(o, col, dh, v);
+    }
+    return odd;
+}
+
 // sum of eight products of 16-bit elements
 template <typename T>
 __device__ __forceinline__ float dot8(const uint4 &x, const uint4 &y) {
@@ -64,7 +89,7 @@ struct DqLayout {
 template <int DH, bool BF, int W>
 __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_attn_dq_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
                                                                     const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
-                                                                    const SeqAttn a, const float c, float *delta) {
+                                                                    const __grid_constant__ SeqAttn a, const float c, float *delta, const int ctas) {
     using L = DqLayout<DH, W>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
     constexpr int KS = L::KS, VS = L::VS;
@@ -83,7 +108,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     const uint32_t q_full = bar0 + 8 * (2 * KS + 2 * VS), sp_full = q_full + 8, sp_free = q_full + 16, ds_full = q_full + 24, ds_free = q_full + 32,
                    dq_full = q_full + 40;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int h = blockIdx.x % a.hq, hk = h / a.group(), tile = (int)(gridDim.x / a.hq) - 1 - (int)(blockIdx.x / a.hq);
+    const int share = (int)blockIdx.x % ctas, unit = (int)blockIdx.x / ctas, h = unit % a.hq, hk = h / a.group();
+    const int tile = (int)gridDim.x / ctas / a.hq - 1 - unit / a.hq;
     const int half = warp >> 2, rt = (int)threadIdx.x & 127, row = tile * SQ_ROWS + rt;
     if (threadIdx.x == 0) {
         for (int s = 0; s < KS; s++) mbar_init(k_full(s), 1), mbar_init(k_free(s), 1);
@@ -111,7 +137,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     Span keys{0, 0};
     bool in = false;
     if (warp < 8) {
-        keys = keys_of_query(ix, row, in);
+        keys = keys_of_lane(ix, row - lane, in);
         const bool some = keys.hi > keys.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? keys.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? keys.hi : 0);
         if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi;
@@ -129,7 +155,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     tc_fence_after();
     const uint32_t tS = tslot, tP = tS + L::T_DP, tD = tS + L::T_DS, tO = tS + L::T_DQ;
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
-    const int nt = end > first ? (end - first + W - 1) / W : 0;
+    // this CTA's tiles, nt of them from t0 on
+    const int all_t = end > first ? (end - first + W - 1) / W : 0, t0 = (int)((long)all_t * share / ctas), nt = (int)((long)all_t * (share + 1) / ctas) - t0;
     const SqWaits wait{&failed, a.status};
 
     if (warp == 8) {
@@ -140,11 +167,11 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             // K(0), then V(j) and K(j + KS - VS) by turns: each waits for what the tensor core is done with first
             for (; jv < nt; jv++) {
                 if (jv >= VS && !wait(v_free(jv % VS), (uint32_t)(jv / VS - 1) & 1)) break;
-                for (; jk <= jv; jk++) sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, end - W * (jk + 1), k_full(jk % KS));  // the first
-                sq_load<DH, W>(sm + L::OFF_V + jv % VS * L::TILE, &tv, hk, end - W * (jv + 1), v_full(jv % VS));
+                for (; jk <= jv; jk++) sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, end - W * (t0 + jk + 1), k_full(jk % KS));  // the first
+                sq_load<DH, W>(sm + L::OFF_V + jv % VS * L::TILE, &tv, hk, end - W * (t0 + jv + 1), v_full(jv % VS));
                 for (; jk < nt && jk <= jv + KS - VS; jk++) {
                     if (jk >= KS && !wait(k_free(jk % KS), (uint32_t)(jk / KS - 1) & 1)) break;
-                    sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, end - W * (jk + 1), k_full(jk % KS));
+                    sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, end - W * (t0 + jk + 1), k_full(jk % KS));
                 }
                 if (failed) {
                     jv++;
@@ -197,7 +224,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const long at_row = (long)h * a.q_rows + row;
         const float D = dots[rt];
-        if (in && half == 0) delta[at_row] = D;
+        if (in && half == 0 && share == 0) delta[at_row] = D;
         const bool none = keys.hi <= keys.lo;
         const float lse2 = none ? 0.0f : a.lse[at_row] * LOG2E;
         const unsigned long long c2 = f4_two(c, c), l2 = f4_two(-lse2, -lse2), d2 = f4_two(-D, -D);
@@ -205,7 +232,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         for (int j = 0; j < nt; j++) {
             if (!(ok = wait(sp_full, (uint32_t)j & 1))) break;
             tc_fence_after();
-            const int at = end - W * (j + 1) + W / 2 * half, lo = keys.lo - at, hi = keys.hi - at;
+            const int at = end - W * (t0 + j + 1) + W / 2 * half, lo = keys.lo - at, hi = keys.hi - at;
             const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= W / 2), some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
             uint32_t s[W / 64][32], p[W / 64][32];
             if (some) {
@@ -255,7 +282,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         if (nt) ok = wait(dq_full, 0) && ok;
         tc_fence_after();
         bool odd = false;
-        if (ok) {
+        int c0 = 0, c1 = DH;  // the columns that this CTA stores
+        if (ctas == 1 && ok) {
             uint32_t out[DH / 4];
 #pragma unroll
             for (int b = 0; b < DH / 64; b++) {
@@ -272,6 +300,26 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             // the queries have been multiplied: their rows are free
             sq_store_rows<DH / 2>(smp + warp * (32 * DH), out, static_cast<uint16_t *>(a.dq.p) + (long)(row - lane) * a.dq.ld + h * a.dq.hd + half * (DH / 2),
                                   a.dq.ld, __ballot_sync(0xFFFFFFFFu, in), a.dh - half * (DH / 2));
+        } else if (ctas > 1) {
+            // sums of this CTA's tiles to shared memory, where queries and gradients were: four columns of a row side by side
+            float4 *sums = reinterpret_cast<float4 *>(smp) + rt, *mine = sums + half * (DH / 8) * SQ_ROWS;
+#pragma unroll
+            for (int b = 0; b < DH / 64; b++) {
+                uint32_t w[32];
+                if (nt) tmem_ld32(tO + lanes + half * (DH / 2) + 32 * b, w);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    mine[(8 * b + i) * SQ_ROWS] = nt ? make_float4(__uint_as_float(w[4 * i]), __uint_as_float(w[4 * i + 1]), __uint_as_float(w[4 * i + 2]),
+                                                                  __uint_as_float(w[4 * i + 3]))
+                                                    : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+            __syncwarp();
+            sq_cluster_sync();
+            // every CTA of the cluster adds up a share of the columns, in the order of the CTAs
+            c0 = DH / ctas * share, c1 = c0 + DH / ctas;
+            if (ok && half == 0)
+                odd = sq_join<BF>(s_addr(sums), c0, c1, ctas, none ? 0.0f : 1.0f, a.scale, in, static_cast<T *>(a.dq.p) + row * a.dq.ld + h * a.dq.hd, a.dh);
         }
         odd_rows[half][rt] = odd;
         elements_sync();
@@ -284,8 +332,13 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
                                          __shfl_sync(0xFFFFFFFFu, lse2, src), __shfl_sync(0xFFFFFFFFu, D, src), static_cast<const T *>(a.k.p) + hk * a.k.hd,
                                          a.k.ld, static_cast<const T *>(a.v.p) + hk * a.v.hd, a.v.ld, sp, a.dh, c);
             const float v[4] = {d.x * a.scale, d.y * a.scale, d.z * a.scale, d.w * a.scale};
-            if (4 * lane < a.dh) store4(static_cast<T *>(a.dq.p) + rr * a.dq.ld + h * a.dq.hd + 4 * lane, v);
+            if (4 * lane >= c0 && 4 * lane < c1 && 4 * lane < a.dh) store4(static_cast<T *>(a.dq.p) + rr * a.dq.ld + h * a.dq.hd + 4 * lane, v);
         }
+    }
+    if (ctas > 1) {
+        __syncwarp();
+        if (warp >= 8) sq_cluster_sync();
+        sq_cluster_sync();  // no CTA leaves while others read its sums
     }
     tc_fence_before();
     __syncthreads();
@@ -308,7 +361,7 @@ struct DkvLayout {
 template <int DH, bool BF, int W>
 __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_attn_dkv_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                                                                      const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
-                                                                     const SeqAttn a, const float c, const float *delta, const int ctas) {
+                                                                     const __grid_constant__ SeqAttn a, const float c, const float *delta, const int ctas) {
     using L = DkvLayout<DH, W>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
     constexpr int QS = L::QS, GS = L::GS;
@@ -346,7 +399,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
     Span qs{0, 0};
     bool in = false;
     if (warp < 8) {
-        qs = queries_of_key(ix, row, in);
+        qs = queries_of_lane(ix, row - lane, in);
         const bool some = qs.hi > qs.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? qs.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? qs.hi : 0);
         if (lane == 0 && half == 0) span_lo[warp] = lo, span_hi[warp] = hi;
@@ -598,26 +651,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             sq_cluster_sync();
             // every CTA of the cluster adds up a share of the columns, in the order of the CTAs
             c0 = DH / ctas * share, c1 = c0 + DH / ctas;
-            if (ok) {
-                const uint32_t at = s_addr(mine);
-#pragma unroll 2
-                for (int col = c0; col < c1; col += 8) {
-                    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-                    for (int r = 0; r < ctas; r++) {
-                        const uint32_t from = t2_mapa(at + (col / 4) * (SQ_ROWS * 16), r);
-                        const float4 y = sq_remote(from), z = sq_remote(from + SQ_ROWS * 16);
-                        v[0] += y.x, v[1] += y.y, v[2] += y.z, v[3] += y.w, v[4] += z.x, v[5] += z.y, v[6] += z.z, v[7] += z.w;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        if (qs.hi <= qs.lo) v[i] = 0.0f;
-                        odd |= !(fabsf(v[i]) < INFINITY);
-                        v[i] *= f;
-                    }
-                    if (in) sq_store<BF>(o, col, a.dh, v);
-                }
-            }
+            if (ok) odd = sq_join<BF>(s_addr(mine), c0, c1, ctas, qs.hi > qs.lo ? 1.0f : 0.0f, f, in, o, a.dh);
         }
         odd_rows[half * SQ_ROWS + rt] = odd;
         elements_sync();
@@ -661,11 +695,11 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     bool in;
     if (a.k_rows == 0) {
         if (w >= a.q_rows) return;
-        keys_of_query(a, (int)w, in);
+        keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hq; h++) store4(static_cast<T *>(a.dq.p) + w * a.dq.ld + h * a.dq.hd + 4 * lane, z);
     } else {
         if (w >= a.k_rows) return;
-        queries_of_key(a, (int)w, in);
+        queries_of_key(a, (int)w, seq_of(a.k_start, a.n_seqs, (int)w), in);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hkv; h++) {
             store4(static_cast<T *>(a.dk.p) + w * a.dk.ld + h * a.dk.hd + 4 * lane, z);
             store4(static_cast<T *>(a.dv.p) + w * a.dv.ld + h * a.dv.hd + 4 * lane, z);
@@ -679,6 +713,14 @@ int dkv_ctas(long tiles, const SeqAttn &a) {
     const long steps = (a.q_rows + SQ_ROWS - 1L) / SQ_ROWS * a.group();
     int p = 1;
     while (p < 8 && tiles * a.hkv * p < 3L * 152 && steps >= 4 * p) p *= 2;
+    return p;
+}
+
+// CTAs that share the walk of a tile of queries: few tiles, each with four tiles of keys at least
+int dq_ctas(long tiles, const SeqAttn &a, int w, int blocks) {
+    const long keys = a.n_seqs ? a.k_rows / a.n_seqs : 0;
+    int p = 1;
+    while (p < 8 && tiles * a.hq * p < 152L * blocks && keys >= 8L * w * p) p *= 2;
     return p;
 }
 
@@ -698,7 +740,8 @@ cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
     float *delta = static_cast<float *>(a.workspace);
     const float c = a.scale * LOG2E;
     const unsigned qt = (unsigned)((a.q_rows + SQ_ROWS - 1) / SQ_ROWS), kt = (unsigned)((a.k_rows + SQ_ROWS - 1) / SQ_ROWS);
-    const cudaError_t e = launch_pdl(seq_attn_dq_kernel<DH, BF, W>, qt * a.hq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta);
+    const int cq = dq_ctas(qt, a, W, 512 / DqLayout<DH, W>::COLS);
+    const cudaError_t e = sq_launch(seq_attn_dq_kernel<DH, BF, W>, qt * a.hq * cq, cq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta, cq);
     if (e != cudaSuccess) return e;
     const int ctas = dkv_ctas(kt, a);
     return sq_launch(seq_attn_dkv_kernel<DH, BF, W>, kt * a.hkv * ctas, ctas, BW_THREADS, DkvLayout<DH, W>::SMEM, st, tk, tv, wq, wg, a, c,

@@ -137,6 +137,13 @@ SIZES = [
     ([2] * 200, None, 2, 2, 64, BF, True, "rows"),
     ([1000], None, 2, 2, 64, BF, True, "rows"),
     ([640], [1400], 2, 1, 128, BF, False, "rows"),
+    # few rows beside many keys: the walks are shared by clusters
+    ([17], [4500], 3, 1, 64, BF, True, "rows"),
+    ([200], [5000], 2, 1, 128, FP, False, "rows"),
+    ([1], [2500], 2, 2, 128, BF, False, "wide"),
+    ([3000], [2], 2, 2, 64, BF, True, "rows"),
+    ([1500, 10], [1500, 2200], 1, 1, 40, BF, True, "heads"),
+    ([2100], None, 1, 1, 64, FP, True, "fused"),
 ]
 
 
