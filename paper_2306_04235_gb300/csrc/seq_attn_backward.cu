@@ -707,21 +707,31 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     }
 }
 
-// CTAs that share the walk of a tile of keys: until the card is filled three times over (walks
-// differ in length), as long as each still has two steps of the longest walk there may be
-int dkv_ctas(long tiles, const SeqAttn &a) {
-    const long steps = (a.q_rows + SQ_ROWS - 1L) / SQ_ROWS * a.group();
-    int p = 1;
-    while (p < 8 && tiles * a.hkv * p < 3L * 152 && steps >= 4 * p) p *= 2;
-    return p;
+// CTAs that share the walks of `units` tiles, `slots` of them on the card at a time: one to eight, by a model of the time in us
+// fitted to measured calls (1 to 8 sequences of 46 to 8192 rows, heads of 64 and 128, one to 16 heads a key head).  A CTA
+// takes 8 us beside its steps, a cluster as many more as it has CTAs; a step of 64 takes 0.95 where two CTAs share an SM, one of
+// 128 alone 1.45.  In one round the longest walk counts; in more, the sum of the work and half of the longest walk.
+// (4096 causal rows of 8 heads of 64: two CTAs 90 us, one 110; 2048 rows of 16 heads of 128 on 2 key heads: four 103, two 147,
+// eight 146; 2048 rows of 8 heads of 128: one 58, two 63, four 83.)
+int walk_ctas(long units, long slots, double longest, double mean, int w) {
+    const double step = w == 64 ? 0.95 : 1.45;
+    int best = 1;
+    double least = 0.0;
+    for (int p = 1; p <= 8 && (p == 1 || longest >= 2.0 * p); p *= 2) {
+        const double beside = 8.0 + (p > 1 ? p : 0), chain = beside + longest / p * step, n = (double)units * p;
+        const double t = n <= slots ? chain : (n * beside + units * mean * step) / slots + chain / 2;
+        if (p == 1 || t < least) best = p, least = t;
+    }
+    return best;
 }
-
-// CTAs that share the walk of a tile of queries: few tiles, each with four tiles of keys at least
+// steps of a walk over rows of n sequences, at most and on average
+int dkv_ctas(long tiles, const SeqAttn &a, int w, int blocks) {
+    const double steps = ((double)a.q_rows / ((double)a.n_seqs * w) + 1) * a.group();
+    return walk_ctas(tiles * a.hkv, 152L * blocks, steps, a.causal ? steps / 2 : steps, w);
+}
 int dq_ctas(long tiles, const SeqAttn &a, int w, int blocks) {
-    const long keys = a.n_seqs ? a.k_rows / a.n_seqs : 0;
-    int p = 1;
-    while (p < 8 && tiles * a.hq * p < 152L * blocks && keys >= 8L * w * p) p *= 2;
-    return p;
+    const double steps = (double)a.k_rows / ((double)a.n_seqs * w) + 1;
+    return walk_ctas(tiles * a.hq, 152L * blocks, steps, a.causal ? steps / 2 : steps, w);
 }
 
 template <int DH, bool BF, int W>
@@ -743,7 +753,7 @@ cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
     const int cq = dq_ctas(qt, a, W, 512 / DqLayout<DH, W>::COLS);
     const cudaError_t e = sq_launch(seq_attn_dq_kernel<DH, BF, W>, qt * a.hq * cq, cq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta, cq);
     if (e != cudaSuccess) return e;
-    const int ctas = dkv_ctas(kt, a);
+    const int ctas = dkv_ctas(kt, a, W, 512 / DkvLayout<DH, W>::COLS);
     return sq_launch(seq_attn_dkv_kernel<DH, BF, W>, kt * a.hkv * ctas, ctas, BW_THREADS, DkvLayout<DH, W>::SMEM, st, tk, tv, wq, wg, a, c,
                      (const float *)delta, ctas);
 }
