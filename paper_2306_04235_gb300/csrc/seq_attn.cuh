@@ -61,13 +61,14 @@ MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, int b, bool &in) {
     return k;
 }
 
-// the queries that see key row
-MNMT_DEV Span queries_of_key(const SeqAttn &a, int row, int b, bool &in) {
-    in = false;
+// the queries that see key row (one: they see no other key)
+MNMT_DEV Span queries_of_key(const SeqAttn &a, int row, int b, bool &in, bool &one) {
+    in = one = false;
     if (b < 0) return Span{0, 0};
     const Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
     if (row >= k.hi) return Span{0, 0};
     in = true;
+    one = k.hi - k.lo == 1;
     Span q = seq_rows(a.q_start, a.q_len, b, a.q_rows);
     if (a.causal) q.lo = max(q.lo, q.hi - (k.hi - row));
     if (q.hi < q.lo) q.hi = q.lo;
@@ -121,9 +122,9 @@ MNMT_DEV Span keys_of_lane(const SeqAttn &a, int row0, bool &in) {
     const int row = row0 + (threadIdx.x & 31), b = row0 < a.q_rows ? seq_of_lane(a.q_start, a.n_seqs, row0) : -1;
     return keys_of_query(a, row, row < a.q_rows ? b : -1, in);
 }
-MNMT_DEV Span queries_of_lane(const SeqAttn &a, int row0, bool &in) {
+MNMT_DEV Span queries_of_lane(const SeqAttn &a, int row0, bool &in, bool &one) {
     const int row = row0 + (threadIdx.x & 31), b = row0 < a.k_rows ? seq_of_lane(a.k_start, a.n_seqs, row0) : -1;
-    return queries_of_key(a, row, row < a.k_rows ? b : -1, in);
+    return queries_of_key(a, row, row < a.k_rows ? b : -1, in, one);
 }
 
 MNMT_DEV float warp_sum_f(float v) {

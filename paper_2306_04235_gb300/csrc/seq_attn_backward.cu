@@ -226,6 +226,9 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         const float D = dots[rt];
         if (in && half == 0 && share == 0) delta[at_row] = D;
         const bool none = keys.hi <= keys.lo;
+        // a query's only key has the weight 1 and dS = 0, where dP - D would leave what their two sums are rounded by (0, not
+        // nothing: what is not a number stays so)
+        const float f = keys.hi - keys.lo == 1 ? 0.0f : a.scale;
         const float lse2 = none ? 0.0f : a.lse[at_row] * LOG2E;
         const unsigned long long c2 = f4_two(c, c), l2 = f4_two(-lse2, -lse2), d2 = f4_two(-D, -D);
         bool ok = true;
@@ -294,7 +297,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
                 for (int i = 0; i < 16; i++) {
                     const float x = nt && !none ? __uint_as_float(w[2 * i]) : 0.0f, y = nt && !none ? __uint_as_float(w[2 * i + 1]) : 0.0f;
                     odd |= !(fabsf(x) < INFINITY) || !(fabsf(y) < INFINITY);
-                    out[16 * b + i] = sq_pack<BF>(x * a.scale, y * a.scale);
+                    out[16 * b + i] = sq_pack<BF>(x * f, y * f);
                 }
             }
             // the queries have been multiplied: their rows are free
@@ -319,7 +322,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             // every CTA of the cluster adds up a share of the columns, in the order of the CTAs
             c0 = DH / ctas * share, c1 = c0 + DH / ctas;
             if (ok && half == 0)
-                odd = sq_join<BF>(s_addr(sums), c0, c1, ctas, none ? 0.0f : 1.0f, a.scale, in, static_cast<T *>(a.dq.p) + row * a.dq.ld + h * a.dq.hd, a.dh);
+                odd = sq_join<BF>(s_addr(sums), c0, c1, ctas, none ? 0.0f : 1.0f, f, in, static_cast<T *>(a.dq.p) + row * a.dq.ld + h * a.dq.hd, a.dh);
         }
         odd_rows[half][rt] = odd;
         elements_sync();
@@ -331,7 +334,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             const float4 d = attn_row_dq(static_cast<const T *>(a.q.p) + rr * a.q.ld + h * a.q.hd, static_cast<const T *>(a.g.p) + rr * a.g.ld + h * a.g.hd,
                                          __shfl_sync(0xFFFFFFFFu, lse2, src), __shfl_sync(0xFFFFFFFFu, D, src), static_cast<const T *>(a.k.p) + hk * a.k.hd,
                                          a.k.ld, static_cast<const T *>(a.v.p) + hk * a.v.hd, a.v.ld, sp, a.dh, c);
-            const float v[4] = {d.x * a.scale, d.y * a.scale, d.z * a.scale, d.w * a.scale};
+            const float fs = __shfl_sync(0xFFFFFFFFu, f, src), v[4] = {d.x * fs, d.y * fs, d.z * fs, d.w * fs};
             if (4 * lane >= c0 && 4 * lane < c1 && 4 * lane < a.dh) store4(static_cast<T *>(a.dq.p) + rr * a.dq.ld + h * a.dq.hd + 4 * lane, v);
         }
     }
@@ -397,9 +400,9 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
     pdl_grid_wait();
     const SeqAttn ix = seq_shared(a, reinterpret_cast<int *>(smp + L::OFF_Q), BW_THREADS);  // where queries come later
     Span qs{0, 0};
-    bool in = false;
+    bool in = false, one = false;
     if (warp < 8) {
-        qs = queries_of_lane(ix, row - lane, in);
+        qs = queries_of_lane(ix, row - lane, in, one);
         const bool some = qs.hi > qs.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? qs.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? qs.hi : 0);
         if (lane == 0 && half == 0) span_lo[warp] = lo, span_hi[warp] = hi;
@@ -610,7 +613,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
         tc_fence_after();
         // a row's two threads: dv, dk
         const HeadRows &x = half ? a.dk : a.dv;
-        const float f = half ? a.scale : 1.0f;
+        const float fk = one ? 0.0f : a.scale, f = half ? fk : 1.0f;  // as in the dq kernel
         T *o = static_cast<T *>(x.p) + row * x.ld + hk * x.hd;
         bool odd = false;
         int c0 = 0, c1 = DH;  // the columns that this CTA stores
@@ -665,7 +668,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                              static_cast<const T *>(a.q.p) + h * a.q.hd, a.q.ld, static_cast<const T *>(a.g.p) + h * a.g.hd, a.g.ld,
                              a.lse + (long)h * a.q_rows, delta + (long)h * a.q_rows, sp, a.dh, c, dk, dv);
 #pragma unroll
-            for (int i = 0; i < 4; i++) dk[i] *= a.scale;
+            for (int i = 0; i < 4; i++) dk[i] *= __shfl_sync(0xFFFFFFFFu, fk, src);
             if (4 * lane >= c0 && 4 * lane < c1 && 4 * lane < a.dh) {
                 store4(static_cast<T *>(a.dk.p) + rr * a.dk.ld + hk * a.dk.hd + 4 * lane, dk);
                 store4(static_cast<T *>(a.dv.p) + rr * a.dv.ld + hk * a.dv.hd + 4 * lane, dv);
@@ -692,14 +695,14 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 5;
     const int lane = threadIdx.x & 31;
     const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    bool in;
+    bool in, one;
     if (a.k_rows == 0) {
         if (w >= a.q_rows) return;
         keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hq; h++) store4(static_cast<T *>(a.dq.p) + w * a.dq.ld + h * a.dq.hd + 4 * lane, z);
     } else {
         if (w >= a.k_rows) return;
-        queries_of_key(a, (int)w, seq_of(a.k_start, a.n_seqs, (int)w), in);
+        queries_of_key(a, (int)w, seq_of(a.k_start, a.n_seqs, (int)w), in, one);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hkv; h++) {
             store4(static_cast<T *>(a.dk.p) + w * a.dk.ld + h * a.dk.hd + 4 * lane, z);
             store4(static_cast<T *>(a.dv.p) + w * a.dv.ld + h * a.dv.hd + 4 * lane, z);

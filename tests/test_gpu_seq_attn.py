@@ -261,6 +261,28 @@ def test_nothing_to_do():
         b.check_backward()
 
 
+def test_one_key():
+    """A query that sees one key has the weight 1 whatever its score: no gradient reaches q, nor k where all queries of
+    a sequence are such; exactly, not within rounding.  What is not a number stays so."""
+    for qn, kn, causal in [([70, 300, 5], [1, 1, 1], False), ([1] * 40, None, True), ([2000], [1], False)]:
+        b = batch(qn, kn, 4, 2, 64, BF, causal, "rows")
+        b.forward()
+        b.backward()
+        b.check_backward()
+        assert not bool(b.dq.any()) and not bool(b.dk.any()) and bool(b.dv.any())
+    b = batch([300], None, 2, 1, 128, FP, True, "rows")
+    b.forward()
+    b.backward()
+    b.check_backward()
+    assert not bool(b.dq[0].any()) and bool(b.dq[1].any())
+    b = batch([70, 300], [1, 1], 1, 1, 64, BF, False, "rows")
+    b.forward()
+    b.g[10, 0, 3] = torch.nan
+    b.backward()
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(b.dq[10]).all()) and bool(torch.isnan(b.dk[0]).all()) and not bool(b.dq[11:].any()) and not bool(b.dk[1].any())
+
+
 def test_without_lse():
     b = batch([70, 200], None, 2, 1, 64, FP, True, "rows")
     b.forward(lse=False)
