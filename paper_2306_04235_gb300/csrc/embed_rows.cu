@@ -526,7 +526,7 @@ cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &args, cudaStream_t s
         for (int i = 0; i < 2; i++) b.key[i] = p + 2 * i * sort_ints(a.T), b.idx[i] = b.key[i] + sort_ints(a.T);
         float *parts = reinterpret_cast<float *>(p + 4 * sort_ints(a.T));
         int passes = 1;
-        while ((a.V >> (8 * passes)) != 0) passes++;
+        while (passes < 4 && (a.V >> (8 * passes)) != 0) passes++;
         cudaLaunchConfig_t cfg = {};
         int ctas = 1;
         while (ctas < ES_CLUSTER && a.T > 1024 * ctas) ctas *= 2;

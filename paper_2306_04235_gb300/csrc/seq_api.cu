@@ -62,6 +62,9 @@ int check_shape(const char *call, const mnmt_attention_shape *s, SeqAttn &a, boo
     if (s->d_head < 8 || s->d_head > 128 || s->d_head % 8) return fail(MNMT_EINVAL, "%s: head size %d is no multiple of 8 up to 128", call, s->d_head);
     if (s->dtype != MNMT_BF16 && s->dtype != MNMT_F16) return fail(MNMT_EINVAL, "%s: type %d is neither bf16 nor fp16", call, s->dtype);
     if (!(s->scale > 0.0f && s->scale <= 0x1p60f)) return fail(MNMT_EINVAL, "%s: scale %g outside (0, 2^60]", call, s->scale);
+    // blocks of a launch: tiles of 128 rows x heads x the CTAs that may share a walk (one query per sequence: units and rows)
+    const int64_t most = 0x7FFFFFFF, tiles = token ? s->n_seqs : ((int64_t)(s->q_rows > s->k_rows ? s->q_rows : s->k_rows) + 127) / 128 * 8;
+    if (tiles * s->q_heads > most) return fail(MNMT_EINVAL, "%s: %d rows of %d heads are more than a launch takes", call, s->q_rows, s->q_heads);
     if (token && s->q_rows != s->n_seqs) return fail(MNMT_EINVAL, "%s: %d query rows for %d sequences", call, s->q_rows, s->n_seqs);
     if (arrays && s->n_seqs > 0 && ((!token && !s->q_start) || !s->k_start)) return fail(MNMT_EINVAL, "%s: null starts of the sequences", call);
     if (!aligned(s->q_start, 4) || !aligned(s->q_len, 4) || !aligned(s->k_start, 4) || !aligned(s->k_len, 4))

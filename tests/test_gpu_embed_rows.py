@@ -144,6 +144,27 @@ def test_embed_backward_one_token_everywhere():
     assert bool(((out.cpu().double() - want).abs() <= bound).all())
 
 
+def test_embed_backward_large_numbers():
+    """Numbers of tokens that take four passes of the sort, rows behind 2^32 bytes, added to what is there."""
+    V, d, T = (1 << 28) + 77, 8, 9000
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    ids = torch.randint(0, V, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    ids[::50] = V - 1
+    ids[1::70] = 3
+    _, g = matrix(T, d, F32, seed=9)
+    out = torch.zeros((V, d), dtype=BF, device="cuda")
+    ws = torch.empty(mnmt.mnmt_embed_backward_workspace(T, V, d), dtype=torch.uint8, device="cuda")
+    mnmt.mnmt_embed_backward(ids, T, g, mnmt.F32, d, 1.0, -1, V, d, out, mnmt.BF16, d, True, ws)
+    torch.cuda.synchronize()
+    names, back = torch.unique(ids.long(), return_inverse=True)
+    want = torch.zeros((len(names), d), dtype=torch.float64, device="cuda").index_add_(0, back, g.double())
+    mag = torch.zeros_like(want).index_add_(0, back, g.double().abs())
+    got = out[names].double()
+    assert bool(((got - want).abs() <= 2.0 ** -8 * want.abs() + T * 2.0 ** -24 * mag).all())
+    out[names] = 0
+    assert not bool(out.any())
+
+
 def test_embed_backward_bad_ids():
     ids = torch.tensor([3, -1, 49, 50, 2 ** 31 - 1, -2 ** 31, 3, 0], dtype=torch.int32, device="cuda")
     _, g = matrix(8, 64, F32, seed=7)

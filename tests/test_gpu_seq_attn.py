@@ -261,6 +261,64 @@ def test_nothing_to_do():
         b.check_backward()
 
 
+@pytest.mark.parametrize("lens", [[3, 0, 1, 2, 5] * 260, [0] * 40 + [70] + [0] * 100 + [1] * 3 + [0] * 33 + [90], [0] * 1500 + [40] + [0] * 70])
+def test_many_sequences(lens):
+    """More sequences than are looked up in shared memory, and long runs of sequences without rows."""
+    b = batch(lens, None, 2, 1, 32, BF, True, "rows")
+    b.forward()
+    b.check_forward()
+    b.backward()
+    b.check_backward()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_what_is_not_seen_does_not_enter_shared_walks(bad):
+    """The same where clusters share a walk: the keys of one sequence, or its queries, hold what is no number."""
+    for qn, kn, spoil in [([17, 30], [4000, 1000], "kv"), ([3000, 900], [20, 30], "qg")]:
+        b, clean = (Batch(starts(qn), starts(kn), 2, 1, 64, BF, False, seed=4) for _ in range(2))
+        for x, at in [(b.k, kn), (b.v, kn)] if spoil == "kv" else [(b.q, qn), (b.g, qn)]:
+            x[at[0]:, :, 7] = bad
+        for x in (b, clean):
+            x.forward()
+            x.backward()
+        torch.cuda.synchronize()
+        o, lse, bo, bl = clean.case().forward()
+        check("o", b.o[:qn[0]], o[:qn[0]], bo[:qn[0]])
+        check("lse", b.lse[:, :qn[0]], lse[:, :qn[0]], bl[:, :qn[0]])
+        for name, got, (want, bound), n in zip(("dq", "dk", "dv"), (b.dq, b.dk, b.dv), clean.case().backward(clean.g, clean.o), (qn[0], kn[0], kn[0])):
+            check(name, got[:n], want[:n], bound[:n])
+
+
+@pytest.mark.parametrize("call", ["forward", "token"])
+def test_offsets_past_32_bits(call):
+    """Keys behind 2^32 bytes and 2^31 elements of a cache, at the end of its rows."""
+    rows, d = (1 << 31) // 128 + 1000, 128
+    far = rows - 600
+    if call == "token":
+        b = Batch([0, 1, 2], [far, 5], 2, 1, d, BF, False, k_len=[600, 300], k_rows=8)
+    else:
+        b = Batch([0, 70, 100], [far, 5], 2, 1, d, BF, True, k_len=[600, 300], k_rows=8)
+    kv = torch.zeros((2, rows, 1, d), dtype=BF, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for at, n in ((far, 600), (5, 300)):
+        kv[:, at:at + n] = torch.randn((2, n, 1, d), generator=g, device="cuda").to(BF)
+    b.k, b.v = kv[0], kv[1]
+    getattr(b, call)()
+    torch.cuda.synchronize()
+    near = Case(b.q, torch.cat([b.k[far:], b.k[5:305]]), torch.cat([b.v[far:], b.v[5:305]]), b.scale, b.causal, b.lists[0], [0, 600], None, [600, 300], 2)
+    o, lse, bo, bl = near.forward()
+    check("o", b.o, o, bo)
+    check("lse", b.lse, lse, bl)
+
+
+def test_many_heads_of_short_sequences():
+    """Enough tiles that a CTA takes several heads, in groups that do not divide them."""
+    for d, hq, hkv in ((64, 7, 7), (128, 6, 2), (64, 10, 5)):
+        b = batch([90, 128, 30, 77, 1, 50] * 24, None, hq, hkv, d, BF, True, "fused")
+        b.forward()
+        b.check_forward()
+
+
 def test_one_key():
     """A query that sees one key has the weight 1 whatever its score: no gradient reaches q, nor k where all queries of
     a sequence are such; exactly, not within rounding.  What is not a number stays so."""
@@ -431,6 +489,14 @@ def test_token_is_the_last_row_of_the_prompt():
     _, _, bo, bl = t.case().forward()
     assert bool(((t.o.cpu().double() - b.o[[199, 276]].cpu().double()).abs() <= 2 * bo).all())
     assert bool(((t.lse - b.lse[:, [199, 276]]).cpu().abs() <= 2 * bl).all())
+
+
+def test_token_many_sequences():
+    """More units than are cut: a warp each."""
+    n = [(37 * i) % 90 for i in range(700)]
+    b = tokens(n, 90, 8, 4, 64, BF)
+    b.token()
+    b.check_forward()
 
 
 def test_token_graph():
