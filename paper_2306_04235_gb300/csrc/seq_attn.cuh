@@ -98,23 +98,21 @@ MNMT_DEV SeqAttn seq_shared(const SeqAttn &a, int *buf, int threads) {
     return s;
 }
 // The sequences of 32 rows, row0 + lane, by a whole warp.  Of up to 1024 starts the first row
-// takes two comparisons (every 32nd start, then 32 of them), the rows behind it the next 32
-// starts; more, or rows of more sequences, are searched lane by lane.  Short code counts here:
-// it runs once a block, from a cold instruction cache (unrolled searches took 2.3 us).
+// takes two comparisons (every 32nd start, then 32 of them); the rows behind it count the
+// starts among them, as bits of a word.  More starts, or sequences without rows, are searched
+// lane by lane.  Few instructions count here: they run once a block, from a cold cache (with
+// searches by shuffles 1.2 us).
 MNMT_DEV int seq_of_lane(const int *start, int n, int row0) {
-    const int lane = threadIdx.x & 31, row = row0 + lane;
+    const int lane = threadIdx.x & 31;
     if (n <= SQ_SEQS) {
         const auto at = [&](int i) { return i < n ? start[i] : 0x7FFFFFFF; };
-        const int block = __popc(__ballot_sync(0xFFFFFFFFu, at(32 * lane) <= row0));  // starts 0, 32, .. that are <= row0
-        const int lo = block ? 32 * (block - 1) + __popc(__ballot_sync(0xFFFFFFFFu, at(32 * (block - 1) + lane) <= row0)) : 0;
-        const int w = at(lo + lane);
-        int k = 0;  // of them are <= row
-#pragma unroll
-        for (int s = 16; s > 0; s >>= 1)
-            if (__shfl_sync(0xFFFFFFFFu, w, k + s - 1) <= row) k += s;
-        if (!__any_sync(0xFFFFFFFFu, k == 31)) return lo + k - 1;
+        const int block = 32 * max(0, __popc(__ballot_sync(0xFFFFFFFFu, at(32 * lane) <= row0)) - 1);  // starts 0, 32, .. that are <= row0
+        const int lo = block + __popc(__ballot_sync(0xFFFFFFFFu, at(block + lane) <= row0));
+        const int d = at(lo + lane) - row0;  // > 0: the next 32 starts
+        const uint32_t among = __reduce_or_sync(0xFFFFFFFFu, d < 32 ? 1u << d : 0u);
+        if (__popc(among) == __popc(__ballot_sync(0xFFFFFFFFu, d < 32))) return lo - 1 + __popc(among & (0xFFFFFFFFu >> (31 - lane)));
     }
-    return seq_of(start, n, row);
+    return seq_of(start, n, row0 + lane);
 }
 
 // the keys that query row0 + lane sees, and the queries that see key row0 + lane; whole warps
