@@ -310,18 +310,18 @@ __global__ void __launch_bounds__(32 * TK_WARPS, TK_BLOCKS) seq_attn_token_kerne
     pdl_allow_next();
 }
 
-// A block per unit and row: the runs of a unit that was cut, a quarter of them a warp,
+// A block per unit, row and COLS columns: the runs of a unit that was cut, an equal part of them a warp,
 // added in their order; zeros where there is no key.  pre: as the first kernel left it.
-constexpr int TJ_WARPS = 4;
-template <int DH, bool BF>
+template <int DH, bool BF, int TJ_WARPS, int COLS>
 __global__ void __launch_bounds__(32 * TJ_WARPS) seq_attn_token_join_kernel(const SeqAttn a, const int chunks, const int warps, const int *pre) {
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
-    constexpr int E = DH / 32;  // columns of a lane
-    __shared__ float sums[TJ_WARPS][DH + 1];
+    constexpr int E = COLS / 32, CB = DH / COLS;  // columns of a lane, blocks of a row
+    __shared__ float sums[TJ_WARPS][COLS + 1], tops[TJ_WARPS];
     pdl_grid_wait();
     const int per = a.hkv * chunks, rows = min(16, a.group()), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long un = blockIdx.x / rows;
-    const int row = (int)(blockIdx.x % rows);
+    const long un = blockIdx.x / (rows * CB);
+    const int row = (int)(blockIdx.x / CB % rows), c0 = (int)(blockIdx.x % CB) * COLS, col = c0 + (int)threadIdx.x;
+    const bool mine = (int)threadIdx.x < COLS && col < a.dh;
     const Unit u = unit_of(a, chunks, un);
     if (row >= u.n) return;
     const int p0 = pre[u.b], nb = pre[u.b + 1] - p0;
@@ -330,8 +330,8 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) seq_attn_token_join_kernel(cons
     T *o = static_cast<T *>(a.o.p) + u.b * a.o.ld + (u.h + row) * a.o.hd;
     float *lse = a.lse ? a.lse + (long)(u.h + row) * a.q_rows + u.b : nullptr;
     if (nb == 0) {
-        if ((int)threadIdx.x < a.dh) o[threadIdx.x] = from_f32<T>(0.0f);
-        if (threadIdx.x == 0 && lse) *lse = -INFINITY;
+        if (mine) o[col] = from_f32<T>(0.0f);
+        if (col == 0 && lse) *lse = -INFINITY;
         return;
     }
     const long wa = ut / run, wb = (ue - 1) / run;
@@ -340,11 +340,14 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) seq_attn_token_join_kernel(cons
     const size_t size = tk_slot<DH>(rows);
     const auto part = [&](long x) { return ws + (2 * x + (x == wa && x * run < ut ? 1 : 0)) * size; };
     // the largest maximum, then the sums
-    float m = -INFINITY;
-    for (long x = wa + lane; x <= wb; x += 32) m = fmaxf(m, part(x)[rows * DH + 2 * row]);
-    m = warp_max_f(m);
-    const float mu = m == -INFINITY ? 0.0f : m;
     const long share = (wb - wa + TJ_WARPS) / TJ_WARPS, xa = wa + warp * share, xb = min(wb, xa + share - 1);
+    float m = -INFINITY;
+    for (long x = xa + lane; x <= xb; x += 32) m = fmaxf(m, part(x)[rows * DH + 2 * row]);
+    m = warp_max_f(m);
+    if (lane == 0) tops[warp] = m;
+    __syncthreads();
+    for (int w = 0; w < TJ_WARPS; w++) m = fmaxf(m, tops[w]);
+    const float mu = m == -INFINITY ? 0.0f : m;
     float l = 0.0f, acc[E];
 #pragma unroll
     for (int i = 0; i < E; i++) acc[i] = 0.0f;
@@ -355,20 +358,20 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) seq_attn_token_join_kernel(cons
         const float f = exp2_fast(ml.x - mu);
         l = fmaf(ml.y, f, l);
 #pragma unroll
-        for (int i = 0; i < E; i++) acc[i] = fmaf(p[row * DH + 32 * i + lane], f, acc[i]);
+        for (int i = 0; i < E; i++) acc[i] = fmaf(p[row * DH + c0 + 32 * i + lane], f, acc[i]);
     }
 #pragma unroll
     for (int i = 0; i < E; i++) sums[warp][32 * i + lane] = acc[i];
-    if (lane == 0) sums[warp][DH] = l;
+    if (lane == 0) sums[warp][COLS] = l;
     __syncthreads();
     l = 0.0f;
-    for (int w = 0; w < TJ_WARPS; w++) l += sums[w][DH];
-    if ((int)threadIdx.x < a.dh) {
+    for (int w = 0; w < TJ_WARPS; w++) l += sums[w][COLS];
+    if (mine) {
         float x = 0.0f;
         for (int w = 0; w < TJ_WARPS; w++) x += sums[w][threadIdx.x];
-        o[threadIdx.x] = from_f32<T>(x / l);
+        o[col] = from_f32<T>(x / l);
     }
-    if (threadIdx.x == 0 && lse) *lse = row_lse(m, l);
+    if (col == 0 && lse) *lse = row_lse(m, l);
 }
 
 int token_chunks(const SeqAttn &a) { return (a.group() + 15) / 16; }
@@ -389,7 +392,15 @@ cudaError_t token(const SeqAttn &a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     const int rows = a.group() < 16 ? a.group() : 16;
     const int *left = reinterpret_cast<const int *>(static_cast<const float *>(a.workspace) + 2 * (size_t)TK_GRID * TK_WARPS * tk_slot<DH>(rows));
-    return launch_pdl(seq_attn_token_join_kernel<DH, BF>, (unsigned)(units * rows), 32 * TJ_WARPS, 0, st, a, chunks, blocks * TK_WARPS, left);
+    // A unit of hundreds of runs: sixteen warps for 32 columns (32768 keys of 2 x 128: 15 us, four warps a row 46).  Else
+    // four a row, as most blocks have little to do.
+    const auto join = [&](auto w, auto cols) {
+        constexpr int WARPS = decltype(w)::value, COLS = decltype(cols)::value;
+        return launch_pdl(seq_attn_token_join_kernel<DH, BF, WARPS, COLS>, (unsigned)(units * rows * (DH / COLS)), 32 * WARPS, 0, st, a, chunks,
+                          blocks * TK_WARPS, left);
+    };
+    return units <= 32 ? join(std::integral_constant<int, 16>{}, std::integral_constant<int, 32>{})
+                       : join(std::integral_constant<int, 4>{}, std::integral_constant<int, DH>{});
 }
 
 template <int DH, bool BF>
