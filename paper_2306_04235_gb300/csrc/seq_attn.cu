@@ -140,10 +140,12 @@ __device__ __noinline__ void forward_join(const SeqAttn &a, uint8_t *smp, int ct
     forward_again<T>(a, __ballot_sync(0xFFFFFFFFu, ok && in && !none && odd && fabsf(sum) < INFINITY), row, h0, keys, c, c0, c1);
 }
 
-template <int DH, bool BF>
+// MANY: a CTA takes several heads one after another; else one, whose walk a cluster may divide
+template <int DH, bool BF, bool MANY>
 __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     seq_attn_forward_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
-                            const __grid_constant__ SeqAttn a, const float c, const int heads, const int ctas) {
+                            const __grid_constant__ SeqAttn a, const float c, const int several) {
+    const int heads = MANY ? several : 1, ctas = MANY ? 1 : several;
     using L = FwLayout<DH>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
     constexpr int ST = L::STAGES, BUFS = L::BUFS, QS = L::QS;
@@ -165,7 +167,7 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     // heads h0 .. h0 + nh - 1 of a tile of rows, the last rows (causal: the longest walks) first
     // (ctas > 1: a cluster divides the walk of one head)
     const int groups = (a.hq + heads - 1) / heads, share = (int)blockIdx.x % ctas, unit = (int)blockIdx.x / ctas;
-    const int h0 = unit % groups * heads, nh = min(heads, a.hq - h0);
+    const int h0 = unit % groups * heads, nh = MANY ? min(heads, a.hq - h0) : 1;
     const int tile = (int)gridDim.x / ctas / groups - 1 - unit / groups, row = tile * SQ_ROWS + (int)threadIdx.x;
     if (threadIdx.x == 128) {
         for (int s = 0; s < ST; s++) mbar_init(k_full(s), 1), mbar_init(k_free(s), 1), mbar_init(v_full(s), 1), mbar_init(v_free(s), 1);
@@ -354,7 +356,7 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
             if (ok) ok = nt ? wait(o_full, (uint32_t)it & 1) : wait(q_full(0), 0);
             if (!ok) break;
             tc_fence_after();
-            if (ctas > 1) break;  // one head, joined below
+            if (!MANY && ctas > 1) break;  // one head, joined below
             const float inv = none ? 0.0f : 1.0f / l;
             uint32_t out[DH / 2];
             const unsigned long long i2 = f4_two(inv, inv), z2 = f4_two(0.0f, 0.0f);
@@ -389,9 +391,9 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
             const uint32_t again = __ballot_sync(0xFFFFFFFFu, in && !none && odd && fabsf(l) < INFINITY);
             if (again) forward_again<T>(a, again, row, h, keys, c, 0, DH);
         }
-        if (ctas > 1) forward_join<DH, BF>(a, smp, ctas, share, row, h0, in, keys, c, m, l, ok, tO + lanes, nt);
+        if (!MANY && ctas > 1) forward_join<DH, BF>(a, smp, ctas, share, row, h0, in, keys, c, m, l, ok, tO + lanes, nt);
     }
-    if (ctas > 1) {
+    if (!MANY && ctas > 1) {
         __syncwarp();
         if (warp >= 4) sq_cluster_sync();
         sq_cluster_sync();  // no CTA leaves while others read its sums
@@ -440,13 +442,15 @@ cudaError_t tile_forward(const SeqAttn &a, cudaStream_t st) {
     if (!sq_map(&tq, a.q, a.q_rows, a.hq, a.dh, SQ_ROWS) || !sq_map(&tk, a.k, a.k_rows, a.hkv, a.dh, KT) || !sq_map(&tv, a.v, a.k_rows, a.hkv, a.dh, KT))
         return cudaErrorInvalidValue;
     const int tiles = (a.q_rows + SQ_ROWS - 1) / SQ_ROWS, heads = forward_heads((long)tiles * a.hq, a), ctas = forward_ctas((long)tiles * a.hq, a);
-    const unsigned grid = (unsigned)tiles * (unsigned)((a.hq + heads - 1) / heads) * (unsigned)ctas;
-    return sq_launch(seq_attn_forward_kernel<DH, BF>, grid, ctas, FW_THREADS, FwLayout<DH>::SMEM, st, tq, tk, tv, a, a.scale * LOG2E, heads, ctas);
+    const unsigned grid = (unsigned)tiles * (unsigned)((a.hq + heads - 1) / heads) * (unsigned)ctas;  // heads: short sequences, ctas: long ones
+    if (heads > 1) return sq_launch(seq_attn_forward_kernel<DH, BF, true>, grid, 1, FW_THREADS, FwLayout<DH>::SMEM, st, tq, tk, tv, a, a.scale * LOG2E, heads);
+    return sq_launch(seq_attn_forward_kernel<DH, BF, false>, grid, ctas, FW_THREADS, FwLayout<DH>::SMEM, st, tq, tk, tv, a, a.scale * LOG2E, ctas);
 }
 
 template <int DH, bool BF>
 cudaError_t tile_init() {
-    return cudaFuncSetAttribute(seq_attn_forward_kernel<DH, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwLayout<DH>::SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(seq_attn_forward_kernel<DH, BF, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwLayout<DH>::SMEM);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(seq_attn_forward_kernel<DH, BF, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwLayout<DH>::SMEM);
 }
 
 }  // namespace
