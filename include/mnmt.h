@@ -517,7 +517,9 @@ int mnmt_dropout_backward(const void *g, int32_t otype, int64_t ldg, const void 
  * d_head: a multiple of 8 up to 128.  dtype (MNMT_BF16 or MNMT_F16): of every operand
  *   below but lse.  scale in (0, 2^60].
  * Scores, weights' sums and results are summed in fp32; the weights (and in the backward
- * pass P and dS) are rounded to dtype in front of the second product, results once. */
+ * pass P and dS) are rounded to dtype in front of the second product, results once.  (fp16
+ * holds dS down to 2^-24: gradients in fp16 want a loss scale.)  A query's only key takes no
+ * gradient, and gives q none.  A sequence that holds what is not finite is slower. */
 typedef struct {
     int32_t n_seqs, q_rows, k_rows, q_heads, kv_heads, d_head, dtype, causal;
     float scale;
@@ -534,7 +536,7 @@ typedef struct {
 
 /* Forward: o, and lse [q_heads][q_rows] (fp32, may be NULL).  o is no input.  workspace:
  * mnmt_attention_forward_workspace(shape) bytes of device scratch, 16-byte aligned
- * (sizes need none of the shape's arrays; 0: invalid shape).  *status (device int32, may
+ * (a few; sizes need none of the shape's arrays; 0: invalid shape).  *status (device int32, may
  * be NULL) receives MNMT_ETIMEOUT if a bounded wait of a kernel gave up. */
 size_t mnmt_attention_forward_workspace(const mnmt_attention_shape *shape);
 int mnmt_attention_forward(const mnmt_attention_shape *shape, const mnmt_heads *q, const mnmt_heads *k, const mnmt_heads *v,

@@ -1,19 +1,29 @@
 // seq_attn.cu -- attention over sequences, forward (seq_attn.cuh).
 //
-// A CTA takes 128 query rows of one head, whatever sequences they belong to: the
-// keys that a row sees are an interval of key rows, and the tile walks 128 keys at
-// a time through the union of its rows' intervals, from its end backwards, so that
-// no tile reaches past the last key that a row sees (what lies there, unwritten
-// rows for instance, would meet zero weights, and zero times NaN is NaN).
+// A CTA takes 128 query rows of one head, whatever sequences they belong to (tiles of a
+// sequence each would leave half of their rows empty at 90 rows a sentence): the keys that
+// a row sees are an interval of key rows, and the tile walks 64 keys at a time through the
+// union of its rows' intervals, from its end backwards, so that no tile reaches past the
+// last key that a row sees (what lies there, unwritten rows for instance, would meet zero
+// weights, and zero times NaN is NaN).
 //   S = Q K^T (TMEM), one thread per row: P = 2^(c s - m), c = scale log2 e, with the
 //   running maximum m and sum l; P over S in TMEM, in the operands' type; O += P V.
 // m is moved, and O scaled, only where a score exceeds it by 2^8 (the sum and the
 // result carry the same factor, so any m near the maximum serves).
-// Two CTAs per SM, so that the tensor core works for one while the other's threads
-// take powers.
+// Two CTAs per SM; three tiles of scores in TMEM (heads up to 64; two above), so that the
+// tensor core is tiles ahead of the threads that take powers: tiles of 128 keys with one
+// buffer waited 1750 of 3200 cycles a tile for it (8192 rows of 8 heads of 64 225 us, 158 so).
+// MMAs are issued by a converged warp (sq_mma): under a branch on the lane the issue of a
+// tile took 1250 cycles and set the pace (2 x 6000..8192 rows of 16 heads of 128 352 us, 309).
 // Where O of a row is not finite though its sum is, an infinity or a NaN of a key
 // that the row does not see may have come in: such rows are computed again over
 // their own keys alone (attn_row).
+//
+// Bound by: heads of 128, the tensor core and its operands (8192 rows of 16 heads, 4 key
+// heads, causal 193 us, 1.42 PFLOP/s, pipe active 60 %: S of 64 keys reads 6 KB of shared memory
+// for 32 cycles of products, and 168 registers leave no more CTAs); heads of 64, issue (0.87 PFLOP/s; 8192 rows not causal);
+// short sequences, a chain of latencies (128 targets of 20..160 rows against 20..128 keys, 8 heads of 64: 19 us for
+// 6.5 us of bytes: start 1, starts 0.6, search 0.6, first tile 1.4, 0.7 a tile, 1.8 the end of a head).
 #include "seq_tile.cuh"
 
 namespace mnmt {

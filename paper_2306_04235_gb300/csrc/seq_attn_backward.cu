@@ -6,7 +6,8 @@
 //            S^T = K Q^T, dP^T = V G^T, dV += P^T G, dK += dS^T Q
 // (seven products instead of the five of one kernel that adds to dQ from everywhere,
 // whose sums would depend on the order of arrival).
-// One CTA per SM, eight warps of two threads per row.  P and dS go to TMEM in the
+// One CTA per SM (tiles of 128 walked rows) or two (heads up to 64, tiles of 64: sentences, which share tiles, leave less of
+// them empty, 67 -> 48 us for the batch below), eight warps of two threads per row.  P and dS go to TMEM in the
 // operands' type, as the A operand of the second products.  While the threads work on
 // one of S and dP the tensor core is on the products that follow the other:
 //   dk, dv:  dV(j), S(j+1) once P(j) is written, dK(j), dP(j+1) once dS(j) is
@@ -15,6 +16,11 @@
 // eight CTAs divides a walk's steps and adds up its sums through distributed shared memory.
 // A walk goes backwards from the last row that is seen, as in the forward pass, and rows
 // whose result is not finite are computed again over their own queries or keys alone.
+//
+// Bound by: long walks, the tensor core, fed in turns with the threads (8192 rows of 16 heads of 128 on 4 key heads, not
+// causal 1284 us: 1.07 PFLOP/s of the formula's five products, 1.50 of the seven; pipe active 49 % in dq, whose threads take
+// 1400 of 2600 cycles a tile); sentences, a chain of latencies in front of 2 to 3 tiles a CTA (128 x 20..128 rows of 8 heads
+// of 64, causal 42 us for 11 us of bytes).
 #include "seq_tile.cuh"
 
 namespace mnmt {
@@ -83,7 +89,8 @@ struct DqLayout {
     static constexpr int VS = DH == 64 ? 3 : 2, KS = VS + 1, QT = sq_bytes<DH>(), TILE = sq_bytes<DH, W>();
     static constexpr int OFF_G = QT, OFF_K = 2 * QT, OFF_V = OFF_K + KS * TILE, SMEM = OFF_V + VS * TILE + 1024;
     static_assert((KS + VS) * TILE >= 4 * SQ_INTS, "starts and lengths before keys and values");
-    static constexpr int T_DP = W, T_DS = 2 * W, T_DQ = 2 * W + W / 2, COLS = pow2_cols(T_DQ + DH);  // columns of dP, dS and dQ behind S
+    // columns of dP, dS, what it was rounded by, and dQ behind S
+    static constexpr int T_DP = W, T_DS = 2 * W, T_DL = T_DS + W / 2, T_DQ = T_DL + W / 2, COLS = pow2_cols(T_DQ + DH);
 };
 
 template <int DH, bool BF, int W>
@@ -92,6 +99,10 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
                                                                     const __grid_constant__ SeqAttn a, const float c, float *delta, const int ctas) {
     using L = DqLayout<DH, W>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
+    // With bf16 and heads up to 64 dS goes in two parts, rounded and what that left, as the tensor core has room there (12 %
+    // busy with sentences), and dk and dv take a D that the rows' sums correct: on the batch of sentences gradients were off by up to
+    // 2.6e-3 of their norm, 2.4e-3 so (1.7e-3 is the results' own rounding), for 2 of 40 us.
+    constexpr bool FINE = BF && DH == 64;
     constexpr int KS = L::KS, VS = L::VS;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[2 * KS + 2 * VS + 6];
@@ -153,7 +164,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tS = tslot, tP = tS + L::T_DP, tD = tS + L::T_DS, tO = tS + L::T_DQ;
+    const uint32_t tS = tslot, tP = tS + L::T_DP, tD = tS + L::T_DS, tL = tS + L::T_DL, tO = tS + L::T_DQ;
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
     // this CTA's tiles, nt of them from t0 on
     const int all_t = end > first ? (end - first + W - 1) / W : 0, t0 = (int)((long)all_t * share / ctas), nt = (int)((long)all_t * (share + 1) / ctas) - t0;
@@ -212,6 +223,10 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
                     const uint64_t b = kt + (uint64_t)(s * (L::TILE >> 4));
 #pragma unroll
                     for (int k = 0; k < W / 16; k++) sq_mma_ta(on, tO, tD + 8 * k, b + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(i | k));
+                    if constexpr (FINE) {
+#pragma unroll
+                        for (int k = 0; k < W / 16; k++) sq_mma_ta(on, tO, tL + 8 * k, b + sq_mn_step(k), sq_idesc(DH, BF, true), 1);
+                    }
                     f4_commit_on<1>(on, k_free(s));
                     f4_commit_on<1>(on, ds_free);
                 }
@@ -224,7 +239,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const long at_row = (long)h * a.q_rows + row;
         const float D = dots[rt];
-        if (in && half == 0 && share == 0) delta[at_row] = D;
+        if (!FINE && in && half == 0 && share == 0) delta[at_row] = D;
+        unsigned long long rest = f4_two(0.0f, 0.0f);  // sum of dS
         const bool none = keys.hi <= keys.lo;
         // a query's only key has the weight 1 and dS = 0, where dP - D would leave what their two sums are rounded by (0, not
         // nothing: what is not a number stays so)
@@ -255,17 +271,26 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
 #pragma unroll
                 for (int b = 0; b < W / 64; b++) {
                     const uint32_t see = sq_bits(lo - 32 * b, hi - 32 * b);
-                    uint32_t w[16];
 #pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        float x, y, u, v;
-                        f4_untwo(sq_fma2(f4_two(__uint_as_float(s[b][2 * i]), __uint_as_float(s[b][2 * i + 1])), c2, l2), x, y);
-                        const unsigned long long t = f4_add2(f4_two(__uint_as_float(p[b][2 * i]), __uint_as_float(p[b][2 * i + 1])), d2);
-                        f4_untwo(f4_mul2(f4_two(exp2_fast(x), exp2_fast(y)), t), u, v);
-                        if (!decltype(whole)::value) u = (see >> (2 * i)) & 1u ? u : 0.0f, v = (see >> (2 * i + 1)) & 1u ? v : 0.0f;
-                        w[i] = sq_pack<BF>(u, v);
+                    for (int i0 = 0; i0 < 16; i0 += 8) {
+                        uint32_t w[8], wl[8];
+#pragma unroll
+                        for (int k = 0; k < 8; k++) {
+                            const int i = i0 + k;
+                            float x, y, u, v;
+                            f4_untwo(sq_fma2(f4_two(__uint_as_float(s[b][2 * i]), __uint_as_float(s[b][2 * i + 1])), c2, l2), x, y);
+                            const unsigned long long t = f4_add2(f4_two(__uint_as_float(p[b][2 * i]), __uint_as_float(p[b][2 * i + 1])), d2);
+                            f4_untwo(f4_mul2(f4_two(exp2_fast(x), exp2_fast(y)), t), u, v);
+                            if (!decltype(whole)::value) u = (see >> (2 * i)) & 1u ? u : 0.0f, v = (see >> (2 * i + 1)) & 1u ? v : 0.0f;
+                            w[k] = sq_pack<BF>(u, v);
+                            if constexpr (FINE) {
+                                rest = f4_add2(rest, f4_two(u, v));
+                                wl[k] = sq_pack<BF>(u - __uint_as_float(w[k] << 16), v - __uint_as_float(w[k] & 0xFFFF0000u));
+                            }
+                        }
+                        tmem_st8(tD + lanes + W / 4 * half + 16 * b + i0, w);
+                        if constexpr (FINE) tmem_st8(tL + lanes + W / 4 * half + 16 * b + i0, wl);
                     }
-                    tmem_st16(tD + lanes + W / 4 * half + 16 * b, w);
                 }
             };
             if (all) {
@@ -275,7 +300,10 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             } else {
                 const uint32_t zeros[16] = {};
 #pragma unroll
-                for (int b = 0; b < W / 64; b++) tmem_st16(tD + lanes + W / 4 * half + 16 * b, zeros);
+                for (int b = 0; b < W / 64; b++) {
+                    tmem_st16(tD + lanes + W / 4 * half + 16 * b, zeros);
+                    if constexpr (FINE) tmem_st16(tL + lanes + W / 4 * half + 16 * b, zeros);
+                }
             }
             tmem_wait_st();
             tc_fence_before();
@@ -284,6 +312,16 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         }
         if (nt) ok = wait(dq_full, 0) && ok;
         tc_fence_after();
+        if constexpr (FINE) {
+            // A row's dS add up to zero but for what D is off by (o is rounded): D + that is what dk and dv take.  (Where a
+            // cluster shares the row, no CTA has the sum.)
+            float ra, rb;
+            f4_untwo(rest, ra, rb);
+            elements_sync();
+            if (half) dots[rt] = ra + rb;
+            elements_sync();
+            if (in && half == 0 && share == 0) delta[at_row] = ctas == 1 && !none ? D + (ra + rb + dots[rt]) : D;
+        }
         bool odd = false;
         int c0 = 0, c1 = DH;  // the columns that this CTA stores
         if (ctas == 1 && ok) {
