@@ -18,9 +18,10 @@
 // whose result is not finite are computed again over their own queries or keys alone.
 //
 // Bound by: long walks, the tensor core, fed in turns with the threads (8192 rows of 16 heads of 128 on 4 key heads, not
-// causal 1284 us: 1.07 PFLOP/s of the formula's five products, 1.50 of the seven; pipe active 49 % in dq, whose threads take
+// causal 1259 us: 1.09 PFLOP/s of the formula's five products, 1.53 of the seven; pipe active 49 % in dq, whose threads take
 // 1400 of 2600 cycles a tile); sentences, a chain of latencies in front of 2 to 3 tiles a CTA (128 x 20..128 rows of 8 heads
-// of 64, causal 42 us for 11 us of bytes).
+// of 64, causal 41 us for 11 us of bytes; several heads a CTA, one after another, as the forward pass takes them, measured the
+// same: the CTA beside it fills the starts as well).
 #include "seq_tile.cuh"
 
 namespace mnmt {
@@ -92,6 +93,21 @@ struct DqLayout {
     // columns of dP, dS, what it was rounded by, and dQ behind S
     static constexpr int T_DP = W, T_DS = 2 * W, T_DL = T_DS + W / 2, T_DQ = T_DL + W / 2, COLS = pow2_cols(T_DQ + DH);
 };
+
+// Rows of `again`, a lane's row each, computed again over their own keys; columns c0 .. c1 - 1 are stored
+template <typename T>
+__device__ __noinline__ void dq_again(const SeqAttn &a, uint32_t again, int row, int h, Span keys, float lse2, float D, float f, float c, int c0, int c1) {
+    const int lane = threadIdx.x & 31, hk = h / a.group();
+    for (; again; again &= again - 1) {
+        const int src = __ffs(again) - 1, rr = __shfl_sync(0xFFFFFFFFu, row, src);
+        const Span sp{__shfl_sync(0xFFFFFFFFu, keys.lo, src), __shfl_sync(0xFFFFFFFFu, keys.hi, src)};
+        const float4 d = attn_row_dq(static_cast<const T *>(a.q.p) + rr * a.q.ld + h * a.q.hd, static_cast<const T *>(a.g.p) + rr * a.g.ld + h * a.g.hd,
+                                     __shfl_sync(0xFFFFFFFFu, lse2, src), __shfl_sync(0xFFFFFFFFu, D, src), static_cast<const T *>(a.k.p) + hk * a.k.hd,
+                                     a.k.ld, static_cast<const T *>(a.v.p) + hk * a.v.hd, a.v.ld, sp, a.dh, c);
+        const float fs = __shfl_sync(0xFFFFFFFFu, f, src), v[4] = {d.x * fs, d.y * fs, d.z * fs, d.w * fs};
+        if (4 * lane >= c0 && 4 * lane < c1 && 4 * lane < a.dh) store4(static_cast<T *>(a.dq.p) + rr * a.dq.ld + h * a.dq.hd + 4 * lane, v);
+    }
+}
 
 template <int DH, bool BF, int W>
 __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_attn_dq_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
@@ -253,7 +269,9 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             tc_fence_after();
             const int at = end - W * (t0 + j + 1) + W / 2 * half, lo = keys.lo - at, hi = keys.hi - at;
             const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= W / 2), some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
-            uint32_t s[W / 64][32], p[W / 64][32];
+            // (a value where there is none to read, or the registers count as used from one turn of the loop to the next:
+            // up to 160 bytes of spills; 3 x 2500..4095 rows of 16 heads of 128 400 us, so 387)
+            uint32_t s[W / 64][32] = {}, p[W / 64][32] = {};
             if (some) {
 #pragma unroll
                 for (int b = 0; b < W / 64; b++) {
@@ -273,7 +291,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
                     const uint32_t see = sq_bits(lo - 32 * b, hi - 32 * b);
 #pragma unroll
                     for (int i0 = 0; i0 < 16; i0 += 8) {
-                        uint32_t w[8], wl[8];
+                        uint32_t w[8];
+                        [[maybe_unused]] uint32_t wl[8];
 #pragma unroll
                         for (int k = 0; k < 8; k++) {
                             const int i = i0 + k;
@@ -328,7 +347,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             uint32_t out[DH / 4];
 #pragma unroll
             for (int b = 0; b < DH / 64; b++) {
-                uint32_t w[32];
+                uint32_t w[32] = {};
                 if (nt) tmem_ld32(tO + lanes + half * (DH / 2) + 32 * b, w);
                 tmem_wait_ld();
 #pragma unroll
@@ -346,7 +365,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             float4 *sums = reinterpret_cast<float4 *>(smp) + rt, *mine = sums + half * (DH / 8) * SQ_ROWS;
 #pragma unroll
             for (int b = 0; b < DH / 64; b++) {
-                uint32_t w[32];
+                uint32_t w[32] = {};
                 if (nt) tmem_ld32(tO + lanes + half * (DH / 2) + 32 * b, w);
                 tmem_wait_ld();
 #pragma unroll
@@ -366,15 +385,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         elements_sync();
         odd = ok && in && (odd_rows[0][rt] || odd_rows[1][rt]);
         // the rows of a warp and its partner by turns
-        for (uint32_t again = __ballot_sync(0xFFFFFFFFu, odd && (rt & 1) == half); again; again &= again - 1) {
-            const int src = __ffs(again) - 1, rr = __shfl_sync(0xFFFFFFFFu, row, src);
-            const Span sp{__shfl_sync(0xFFFFFFFFu, keys.lo, src), __shfl_sync(0xFFFFFFFFu, keys.hi, src)};
-            const float4 d = attn_row_dq(static_cast<const T *>(a.q.p) + rr * a.q.ld + h * a.q.hd, static_cast<const T *>(a.g.p) + rr * a.g.ld + h * a.g.hd,
-                                         __shfl_sync(0xFFFFFFFFu, lse2, src), __shfl_sync(0xFFFFFFFFu, D, src), static_cast<const T *>(a.k.p) + hk * a.k.hd,
-                                         a.k.ld, static_cast<const T *>(a.v.p) + hk * a.v.hd, a.v.ld, sp, a.dh, c);
-            const float fs = __shfl_sync(0xFFFFFFFFu, f, src), v[4] = {d.x * fs, d.y * fs, d.z * fs, d.w * fs};
-            if (4 * lane >= c0 && 4 * lane < c1 && 4 * lane < a.dh) store4(static_cast<T *>(a.dq.p) + rr * a.dq.ld + h * a.dq.hd + 4 * lane, v);
-        }
+        const uint32_t again = __ballot_sync(0xFFFFFFFFu, odd && (rt & 1) == half);
+        if (again) dq_again<T>(a, again, row, h, keys, lse2, D, f, c, c0, c1);
     }
     if (ctas > 1) {
         __syncwarp();
@@ -398,6 +410,27 @@ struct DkvLayout {
     static constexpr int T_DP = W, T_DV = 2 * W, T_DK = 2 * W + DH, COLS = pow2_cols(2 * W + 2 * DH);
     static_assert(OFF_N >= 2 * SQ_ROWS * DH * 4, "a CTA's sums for its cluster");
 };
+
+// As dq_again, dk and dv over the queries of all heads of key head hk
+template <typename T>
+__device__ __noinline__ void dkv_again(const SeqAttn &a, uint32_t again, int row, int hk, Span qs, float fk, float c, const float *delta, int c0, int c1) {
+    const int lane = threadIdx.x & 31;
+    for (; again; again &= again - 1) {
+        const int src = __ffs(again) - 1, rr = __shfl_sync(0xFFFFFFFFu, row, src);
+        const Span sp{__shfl_sync(0xFFFFFFFFu, qs.lo, src), __shfl_sync(0xFFFFFFFFu, qs.hi, src)};
+        float dk[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int h = hk * a.group(); h < (hk + 1) * a.group(); h++)
+            attn_row_dkv(static_cast<const T *>(a.k.p) + rr * a.k.ld + hk * a.k.hd, static_cast<const T *>(a.v.p) + rr * a.v.ld + hk * a.v.hd,
+                         static_cast<const T *>(a.q.p) + h * a.q.hd, a.q.ld, static_cast<const T *>(a.g.p) + h * a.g.hd, a.g.ld,
+                         a.lse + (long)h * a.q_rows, delta + (long)h * a.q_rows, sp, a.dh, c, dk, dv);
+#pragma unroll
+        for (int i = 0; i < 4; i++) dk[i] *= __shfl_sync(0xFFFFFFFFu, fk, src);
+        if (4 * lane >= c0 && 4 * lane < c1 && 4 * lane < a.dh) {
+            store4(static_cast<T *>(a.dk.p) + rr * a.dk.ld + hk * a.dk.hd + 4 * lane, dk);
+            store4(static_cast<T *>(a.dv.p) + rr * a.dv.ld + hk * a.dv.hd + 4 * lane, dv);
+        }
+    }
+}
 
 template <int DH, bool BF, int W>
 __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_attn_dkv_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
@@ -568,7 +601,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             if (!(ok = wait(s_full, (uint32_t)j & 1) && wait(n_full + 8 * (j & 1), (uint32_t)(j >> 1) & 1))) break;
             tc_fence_after();
             // Two passes over a thread's columns, P and dS, without the masks where the warp's rows see all of them
-            uint32_t r[W / 64][32];
+            uint32_t r[W / 64][32] = {};  // as in the dq kernel
             const uint32_t zeros[16] = {};
             const auto weights = [&](auto whole) {
                 load_half<W>(tS + lanes + W / 2 * half, r);
@@ -660,7 +693,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                 uint32_t out[DH / 2];
 #pragma unroll
                 for (int b = 0; b < DH / 32; b++) {
-                    uint32_t w[32];
+                    uint32_t w[32] = {};
                     if (n) tmem_ld32((half ? tK : tV) + lanes + 32 * b, w);
                     tmem_wait_ld();
                     const bool any = n && qs.hi > qs.lo;
@@ -679,7 +712,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             float4 *mine = reinterpret_cast<float4 *>(smp) + half * (DH / 4) * SQ_ROWS + rt;
 #pragma unroll
             for (int b = 0; b < DH / 32; b++) {
-                uint32_t w[32];
+                uint32_t w[32] = {};
                 if (n) tmem_ld32((half ? tK : tV) + lanes + 32 * b, w);
                 tmem_wait_ld();
 #pragma unroll
@@ -697,21 +730,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
         odd_rows[half * SQ_ROWS + rt] = odd;
         elements_sync();
         odd = ok && in && (odd_rows[rt] || odd_rows[SQ_ROWS + rt]);
-        for (uint32_t again = __ballot_sync(0xFFFFFFFFu, odd && (rt & 1) == half); again; again &= again - 1) {
-            const int src = __ffs(again) - 1, rr = __shfl_sync(0xFFFFFFFFu, row, src);
-            const Span sp{__shfl_sync(0xFFFFFFFFu, qs.lo, src), __shfl_sync(0xFFFFFFFFu, qs.hi, src)};
-            float dk[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (int h = h0; h < h0 + heads; h++)
-                attn_row_dkv(static_cast<const T *>(a.k.p) + rr * a.k.ld + hk * a.k.hd, static_cast<const T *>(a.v.p) + rr * a.v.ld + hk * a.v.hd,
-                             static_cast<const T *>(a.q.p) + h * a.q.hd, a.q.ld, static_cast<const T *>(a.g.p) + h * a.g.hd, a.g.ld,
-                             a.lse + (long)h * a.q_rows, delta + (long)h * a.q_rows, sp, a.dh, c, dk, dv);
-#pragma unroll
-            for (int i = 0; i < 4; i++) dk[i] *= __shfl_sync(0xFFFFFFFFu, fk, src);
-            if (4 * lane >= c0 && 4 * lane < c1 && 4 * lane < a.dh) {
-                store4(static_cast<T *>(a.dk.p) + rr * a.dk.ld + hk * a.dk.hd + 4 * lane, dk);
-                store4(static_cast<T *>(a.dv.p) + rr * a.dv.ld + hk * a.dv.hd + 4 * lane, dv);
-            }
-        }
+        const uint32_t again = __ballot_sync(0xFFFFFFFFu, odd && (rt & 1) == half);
+        if (again) dkv_again<T>(a, again, row, hk, qs, fk, c, delta, c0, c1);
     }
     if (ctas > 1) {
         if (warp >= 8) {
