@@ -218,16 +218,14 @@ __device__ __forceinline__ void run_out(const SeqAttn &a, const Unit &u, bool no
     }
 }
 
-// Tiles before each sequence's, in units of one head: pre[0 .. n_seqs].  All threads of the block.
-template <int DH>
-__device__ __forceinline__ void tile_prefix(const SeqAttn &a, int *pre) {
+// Pieces of 2^piece keys before each sequence's, in units of one head: pre[0 .. n_seqs].  All threads of the block.
+__device__ __forceinline__ void tile_prefix(const SeqAttn &a, int piece, int *pre) {
     __shared__ int sums[32];
-    constexpr int KT = tk_keys<DH>();
     const int n = a.n_seqs, per = (n + (int)blockDim.x - 1) / (int)blockDim.x, from = (int)threadIdx.x * per, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int s = 0;
     for (int b = from; b < min(n, from + per); b++) {
         const Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
-        const int t = (k.hi - k.lo + KT - 1) / KT;
+        const int t = (k.hi - k.lo + (1 << piece) - 1) >> piece;
         pre[b + 1] = t;
         s += t;
     }
@@ -250,7 +248,7 @@ __device__ __forceinline__ void tile_prefix(const SeqAttn &a, int *pre) {
 __device__ __forceinline__ long run_tiles(long total, int warps) { return max((long)TK_MIN_RUN, (total + warps - 1) / warps); }
 
 template <int DH, bool BF>
-__global__ void __launch_bounds__(32 * TK_WARPS, TK_BLOCKS) seq_attn_token_kernel(const SeqAttn a, const float c, const int chunks, const int split) {
+__global__ void __launch_bounds__(32 * TK_WARPS, TK_BLOCKS) seq_attn_token_kernel(const SeqAttn a, const float c, const int chunks, const int split) {  // split: log2 of a piece's keys, 0: whole units
     extern __shared__ __align__(128) uint8_t ring_all[];
     pdl_grid_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -273,7 +271,7 @@ __global__ void __launch_bounds__(32 * TK_WARPS, TK_BLOCKS) seq_attn_token_kerne
         return;
     }
     int *pre = reinterpret_cast<int *>(ring_all + TK_SMEM);
-    tile_prefix<DH>(a, pre);
+    tile_prefix(a, split, pre);
     const int per = a.hkv * chunks, rows = min(16, a.group());
     int *pre_out = reinterpret_cast<int *>(static_cast<float *>(a.workspace) + 2 * (size_t)TK_GRID * TK_WARPS * tk_slot<DH>(rows));
     if (blockIdx.x == 0)
@@ -293,7 +291,7 @@ __global__ void __launch_bounds__(32 * TK_WARPS, TK_BLOCKS) seq_attn_token_kerne
         const Unit u = unit_of(a, chunks, (long)lo * per + x);
         const Span k = seq_rows(a.k_start, a.k_len, u.b, a.k_rows);
         const long te = min(t1, ue);
-        const Span part{k.lo + (int)(t - ut) * tk_keys<DH>(), min(k.hi, k.lo + (int)(te - ut) * tk_keys<DH>())};
+        const Span part{k.lo + (int)((t - ut) << split), (int)min((long)k.hi, k.lo + ((te - ut) << split))};
         run_keys<DH, BF>(a, u, part, c, ring, r);
         if (t == ut && te == ue) {
             run_out<DH, BF>(a, u, false, r);
@@ -383,6 +381,15 @@ bool token_split(const SeqAttn &a) {
     return (long)a.n_seqs * a.hkv * token_chunks(a) < 2L * TK_GRID * TK_WARPS && a.k_rows >= TK_SPLIT_ROWS;
 }
 
+// log2 of the keys of a piece that a unit is cut into: a tile, but as many as keep the number of all sequences' pieces within 31
+// bits, however many of them share a long cache's rows
+template <int DH>
+int token_piece(const SeqAttn &a) {
+    int piece = 4;
+    while (1 << piece < tk_keys<DH>() || a.n_seqs * (((long)a.k_rows >> piece) + 1) > 0x7FFFFFFFL) piece++;
+    return piece;
+}
+
 template <int DH, bool BF>
 cudaError_t token(const SeqAttn &a, cudaStream_t st) {
     const int chunks = token_chunks(a), split = token_split(a);
@@ -391,7 +398,7 @@ cudaError_t token(const SeqAttn &a, cudaStream_t st) {
     if (!split) return launch_pdl(seq_attn_token_kernel<DH, BF>, (unsigned)((units + TK_WARPS - 1) / TK_WARPS), 32 * TK_WARPS, TK_SMEM, st, a, c, chunks, 0);
     const int blocks = TK_GRID;
     const size_t pre = ((size_t)a.n_seqs + 1) * 4;
-    const cudaError_t e = launch_pdl(seq_attn_token_kernel<DH, BF>, blocks, 32 * TK_WARPS, TK_SMEM + pre, st, a, c, chunks, 1);
+    const cudaError_t e = launch_pdl(seq_attn_token_kernel<DH, BF>, blocks, 32 * TK_WARPS, TK_SMEM + pre, st, a, c, chunks, token_piece<DH>(a));
     if (e != cudaSuccess) return e;
     const int rows = a.group() < 16 ? a.group() : 16;
     const int *left = reinterpret_cast<const int *>(static_cast<const float *>(a.workspace) + 2 * (size_t)TK_GRID * TK_WARPS * tk_slot<DH>(rows));

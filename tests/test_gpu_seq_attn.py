@@ -499,6 +499,58 @@ def test_token_many_sequences():
     b.check_forward()
 
 
+def shared_cache(lens, first, q, k, v):
+    """One head of 8, fp16, against a cache whose rows sequences share."""
+    B, rows = len(lens), k.shape[0]
+    s = mnmt.AttentionShape(B, B, rows, 1, 1, 8, mnmt.F16, False, 8 ** -0.5, None, dev(first), k_len=dev(lens))
+    ws = torch.full((mnmt.mnmt_attention_token_workspace(s),), 0xFF, dtype=torch.uint8, device="cuda")
+    o, lse = torch.full_like(q, SENTINEL), torch.full((1, B), SENTINEL, device="cuda")
+    mnmt.mnmt_attention_token(s, mnmt.heads(q), mnmt.heads(k), mnmt.heads(v), mnmt.heads(o), lse, ws)
+    torch.cuda.synchronize()
+    return o[:, 0], lse[0]
+
+
+def test_token_many_long_caches():
+    """Room for more than 2^31 tiles of 32 keys, few of them used: units are cut into larger pieces."""
+    B, rows = 2100, 1 << 25
+    g, r = torch.Generator(device="cuda").manual_seed(5), torch.Generator().manual_seed(6)
+    k, v = ((torch.randn((rows, 1, 8), generator=g, device="cuda") * 0.5).to(FP) for _ in range(2))
+    q = torch.randn((B, 1, 8), generator=g, device="cuda").to(FP)
+    lens = torch.randint(0, 9000, (B,), generator=r).tolist()
+    first = torch.randint(0, rows, (B,), generator=r).tolist()
+    lens[7], lens[14], first[21] = 0, 1, rows - 100  # the last ends behind the cache
+    lens[21] = 500
+    o, lse = shared_cache(lens, first, q, k, v)
+    for b in [7, 14, 21, *range(0, B, 70)]:
+        end = min(rows, first[b] + lens[b])
+        if end <= first[b]:
+            assert float(o[b].abs().max()) == 0.0 and float(lse[b]) == -float("inf")
+            continue
+        x = (k[first[b]:end, 0].double() * q[b, 0].double()).sum(1) * 8 ** -0.5
+        w = torch.softmax(x, 0)[:, None] * v[first[b]:end, 0].double()
+        want, mag = w.sum(0), w.abs().sum(0)
+        # scores: exact products, ten fp32 steps of 2^-24 of values below 32, which a power turns into a relative 10 * 32 * 2^-24
+        # < 2^-15, in numerator and denominator; a weight's rounding 2^-11; n sums in fp32 in each, truncated in one of them (2^-23);
+        # the result's rounding
+        n = end - first[b]
+        assert bool((abs(o[b].double() - want) <= mag * (2.0 ** -14 + 2.0 ** -11 + 3 * n * 2.0 ** -24) + want.abs() * 2.0 ** -11 + 2.0 ** -25).all())
+        assert abs(float(lse[b]) - float(torch.logsumexp(x, 0))) <= 2.0 ** -15 + n * 2.0 ** -24 + 32 * 2.0 ** -23
+
+
+def test_token_more_than_31_bits_of_tiles():
+    """Sequences that share all rows of a long cache: 2^31 tiles of 32 keys and more."""
+    B, rows = 2100, 1 << 25
+    g = torch.Generator(device="cuda").manual_seed(5)
+    k = (torch.randn((rows, 1, 8), generator=g, device="cuda") * 0.5).to(FP)
+    q = torch.randn((1, 1, 8), generator=g, device="cuda").to(FP)
+    o, lse = shared_cache([rows] * B, [0] * B, q.expand(B, 1, 8).contiguous(), k, torch.ones_like(k))
+    # a lane adds up to 2^22 terms (half an ulp each: 2^-2 of the sum), the tensor core 2^21 truncated ones (2^-2): a mean of ones
+    # between 0.75 / 1.25 and 1.25 / 0.75, and log 0.75 in the log-sum-exp
+    assert 0.59 < float(o.min()) and float(o.max()) < 1.68
+    want = float(torch.logsumexp((k[:, 0].double() * q[0, 0].double()).sum(1) * 8 ** -0.5, 0))
+    assert float((lse - want).abs().max()) < 0.3
+
+
 def test_token_graph():
     """A captured step, replayed while the cache fills."""
     b = tokens([10, 200, 1], 512, 4, 2, 64, BF)
