@@ -109,7 +109,8 @@ __device__ __noinline__ void dq_again(const SeqAttn &a, uint32_t again, int row,
     }
 }
 
-template <int DH, bool BF, int W>
+// FEW: sequences of few keys, see `twice`
+template <int DH, bool BF, int W, bool FEW>
 __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_attn_dq_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
                                                                     const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                                                                     const __grid_constant__ SeqAttn a, const float c, float *delta, const int ctas) {
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[2 * KS + 2 * VS + 6];
     __shared__ uint32_t tslot;
-    __shared__ int failed, span[2][4];
+    __shared__ int failed, span[4][4];
     __shared__ float dots[SQ_ROWS];
     __shared__ uint8_t odd_rows[2][SQ_ROWS];
     const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
@@ -167,7 +168,9 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         keys = keys_of_lane(ix, row - lane, in);
         const bool some = keys.hi > keys.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? keys.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? keys.hi : 0);
-        if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi;
+        const int seen = __reduce_add_sync(0xFFFFFFFFu, some ? min(keys.hi - keys.lo, 1 << 16) : 0);
+        const uint32_t see = __ballot_sync(0xFFFFFFFFu, some);
+        if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi, span[2][warp] = seen, span[3][warp] = __popc(see);
 #pragma unroll
         for (int i = 0; i < NR; i++) {
             float dot = dot8<T>(ov[i], gv[i]);
@@ -184,6 +187,11 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
     // this CTA's tiles, nt of them from t0 on
     const int all_t = end > first ? (end - first + W - 1) / W : 0, t0 = (int)((long)all_t * share / ctas), nt = (int)((long)all_t * (share + 1) / ctas) - t0;
+    // Where rows see few keys, D from the rounded o is off by what weighs most in dq and dk (sequences of 2 or 3: 3.7e-3 of dq's
+    // norm, 1.7e-3 its own rounding; of 10: 2.4e-3; of 40: 2.0e-3).  There the tiles are walked twice, at first for
+    // the sum of dS, which is zero but for that.  (In a kernel of its own: the code alone cost long walks 2 %.)
+    const bool twice = FEW && ctas == 1 && span[2][0] + span[2][1] + span[2][2] + span[2][3] <= 16 * (span[3][0] + span[3][1] + span[3][2] + span[3][3]);
+    const int n1 = twice ? nt : 0, n = n1 + nt;  // steps of the first walk, of both
     const SqWaits wait{&failed, a.status};
 
     if (warp == 8) {
@@ -191,14 +199,15 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             sq_load<DH>(sm, &tq, h, tile * SQ_ROWS, q_full);
             sq_load<DH>(sm + L::OFF_G, &tg, h, tile * SQ_ROWS, q_full);
             int jk = 0, jv = 0;  // loads issued
+            const auto at = [&](int j) { return end - W * (t0 + (j < nt ? j : j - nt) + 1); };  // rows of step j's tile
             // K(0), then V(j) and K(j + KS - VS) by turns: each waits for what the tensor core is done with first
-            for (; jv < nt; jv++) {
+            for (; jv < n; jv++) {
                 if (jv >= VS && !wait(v_free(jv % VS), (uint32_t)(jv / VS - 1) & 1)) break;
-                for (; jk <= jv; jk++) sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, end - W * (t0 + jk + 1), k_full(jk % KS));  // the first
-                sq_load<DH, W>(sm + L::OFF_V + jv % VS * L::TILE, &tv, hk, end - W * (t0 + jv + 1), v_full(jv % VS));
-                for (; jk < nt && jk <= jv + KS - VS; jk++) {
+                for (; jk <= jv; jk++) sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, at(jk), k_full(jk % KS));  // the first
+                sq_load<DH, W>(sm + L::OFF_V + jv % VS * L::TILE, &tv, hk, at(jv), v_full(jv % VS));
+                for (; jk < n && jk <= jv + KS - VS; jk++) {
                     if (jk >= KS && !wait(k_free(jk % KS), (uint32_t)(jk / KS - 1) & 1)) break;
-                    sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, end - W * (t0 + jk + 1), k_full(jk % KS));
+                    sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, at(jk), k_full(jk % KS));
                 }
                 if (failed) {
                     jv++;
@@ -216,8 +225,8 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             const uint32_t on = elect_one();
             const uint64_t qd = sq_k(sm), gd = sq_k(sm + L::OFF_G), kd = sq_k(sm + L::OFF_K), vd = sq_k(sm + L::OFF_V), kt = sq_mn<W>(sm + L::OFF_K);
             bool ok = wait(q_full, 0);
-            for (int j = 0; j <= nt && ok; j++) {
-                if (j < nt) {  // S(j), dP(j)
+            for (int j = 0; j <= n && ok; j++) {
+                if (j < n) {  // S(j), dP(j)
                     const int s = j % KS, sv = j % VS;
                     const uint64_t koff = (uint64_t)(s * (L::TILE >> 4)), voff = (uint64_t)(sv * (L::TILE >> 4));
                     if (j && !(ok = wait(sp_free, (uint32_t)(j - 1) & 1))) break;
@@ -231,9 +240,10 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
                     for (int k = 0; k < DH / 16; k++) sq_mma(on, tP, gd + sq_k_step(k), vd + voff + sq_k_step<W>(k), sq_idesc(W, BF, false), k > 0);
                     f4_commit_on<1>(on, v_free(sv));
                     f4_commit_on<1>(on, sp_full);
+                    if (j < n1) f4_commit_on<1>(on, k_free(s));
                 }
-                if (j > 0) {  // dQ(j - 1)
-                    const int i = j - 1, s = i % KS;
+                if (j > n1) {  // dQ(j - 1)
+                    const int i = j - 1 - n1, s = (j - 1) % KS;
                     if (!(ok = wait(ds_full, (uint32_t)i & 1))) break;
                     tc_fence_after();
                     const uint64_t b = kt + (uint64_t)(s * (L::TILE >> 4));
@@ -254,18 +264,63 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     } else {
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const long at_row = (long)h * a.q_rows + row;
-        const float D = dots[rt];
-        if (!FINE && in && half == 0 && share == 0) delta[at_row] = D;
+        float D = dots[rt];
+        if (!FINE && !twice && in && half == 0 && share == 0) delta[at_row] = D;
         unsigned long long rest = f4_two(0.0f, 0.0f);  // sum of dS
         const bool none = keys.hi <= keys.lo;
         // a query's only key has the weight 1 and dS = 0, where dP - D would leave what their two sums are rounded by (0, not
         // nothing: what is not a number stays so)
         const float f = keys.hi - keys.lo == 1 ? 0.0f : a.scale;
         const float lse2 = none ? 0.0f : a.lse[at_row] * LOG2E;
-        const unsigned long long c2 = f4_two(c, c), l2 = f4_two(-lse2, -lse2), d2 = f4_two(-D, -D);
+        const unsigned long long c2 = f4_two(c, c), l2 = f4_two(-lse2, -lse2);
         bool ok = true;
-        for (int j = 0; j < nt; j++) {
-            if (!(ok = wait(sp_full, (uint32_t)j & 1))) break;
+        if (twice) {
+            const unsigned long long d2 = f4_two(-D, -D);
+            for (int j = 0; j < nt; j++) {
+                if (!(ok = wait(sp_full, (uint32_t)j & 1))) break;
+                tc_fence_after();
+                const int at = end - W * (t0 + j + 1) + W / 2 * half, lo = keys.lo - at, hi = keys.hi - at;
+                const bool some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
+                uint32_t s[W / 64][32] = {}, p[W / 64][32] = {};
+                if (some) {
+#pragma unroll
+                    for (int b = 0; b < W / 64; b++) {
+                        tmem_ld32(tS + lanes + W / 2 * half + 32 * b, s[b]);
+                        tmem_ld32(tP + lanes + W / 2 * half + 32 * b, p[b]);
+                    }
+                    tmem_wait_ld();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sp_free);
+                if (!some) continue;
+#pragma unroll
+                for (int b = 0; b < W / 64; b++) {
+                    const uint32_t see = sq_bits(lo - 32 * b, hi - 32 * b);
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        float x, y, u, v;
+                        f4_untwo(sq_fma2(f4_two(__uint_as_float(s[b][2 * i]), __uint_as_float(s[b][2 * i + 1])), c2, l2), x, y);
+                        const unsigned long long t = f4_add2(f4_two(__uint_as_float(p[b][2 * i]), __uint_as_float(p[b][2 * i + 1])), d2);
+                        f4_untwo(f4_mul2(f4_two(exp2_fast(x), exp2_fast(y)), t), u, v);
+                        rest = f4_add2(rest, f4_two((see >> (2 * i)) & 1u ? u : 0.0f, (see >> (2 * i + 1)) & 1u ? v : 0.0f));
+                    }
+                }
+            }
+            // a row's two halves (every warp comes here, whether its waits were in vain or not)
+            float ra, rb;
+            f4_untwo(rest, ra, rb);
+            elements_sync();
+            if (half) dots[rt] = ra + rb;
+            elements_sync();
+            if (!half) dots[rt] = D + (ra + rb + dots[rt]);
+            elements_sync();
+            D = dots[rt];
+            if (in && half == 0) delta[at_row] = D;
+        }
+        const unsigned long long d2 = f4_two(-D, -D);
+        for (int j = 0; j < nt && ok; j++) {
+            if (!(ok = wait(sp_full, (uint32_t)(n1 + j) & 1))) break;
             tc_fence_after();
             const int at = end - W * (t0 + j + 1) + W / 2 * half, lo = keys.lo - at, hi = keys.hi - at;
             const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= W / 2), some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
@@ -331,7 +386,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         }
         if (nt) ok = wait(dq_full, 0) && ok;
         tc_fence_after();
-        if constexpr (FINE) {
+        if (FINE && !twice) {
             // A row's dS add up to zero but for what D is off by (o is rounded): D + that is what dk and dv take.  (Where a
             // cluster shares the row, no CTA has the sum.)
             float ra, rb;
@@ -812,7 +867,8 @@ cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
     const float c = a.scale * LOG2E;
     const unsigned qt = (unsigned)((a.q_rows + SQ_ROWS - 1) / SQ_ROWS), kt = (unsigned)((a.k_rows + SQ_ROWS - 1) / SQ_ROWS);
     const int cq = dq_ctas(qt, a, W, 512 / DqLayout<DH, W>::COLS);
-    const cudaError_t e = sq_launch(seq_attn_dq_kernel<DH, BF, W>, qt * a.hq * cq, cq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta, cq);
+    const bool few = a.k_rows <= 64L * a.n_seqs;
+    const cudaError_t e = sq_launch(few ? seq_attn_dq_kernel<DH, BF, W, true> : seq_attn_dq_kernel<DH, BF, W, false>, qt * a.hq * cq, cq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta, cq);
     if (e != cudaSuccess) return e;
     const int ctas = dkv_ctas(kt, a, W, 512 / DkvLayout<DH, W>::COLS);
     return sq_launch(seq_attn_dkv_kernel<DH, BF, W>, kt * a.hkv * ctas, ctas, BW_THREADS, DkvLayout<DH, W>::SMEM, st, tk, tv, wq, wg, a, c,
@@ -821,7 +877,8 @@ cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
 
 template <int DH, bool BF, int W>
 cudaError_t tile_init() {
-    const cudaError_t e = cudaFuncSetAttribute(seq_attn_dq_kernel<DH, BF, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<DH, W>::SMEM);
+    cudaError_t e = cudaFuncSetAttribute(seq_attn_dq_kernel<DH, BF, W, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<DH, W>::SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(seq_attn_dq_kernel<DH, BF, W, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<DH, W>::SMEM);
     return e != cudaSuccess ? e : cudaFuncSetAttribute(seq_attn_dkv_kernel<DH, BF, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, DkvLayout<DH, W>::SMEM);
 }
 

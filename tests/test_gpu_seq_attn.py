@@ -341,6 +341,26 @@ def test_one_key():
     assert bool(torch.isnan(b.dq[10]).all()) and bool(torch.isnan(b.dk[0]).all()) and not bool(b.dq[11:].any()) and not bool(b.dk[1].any())
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d", [64, 40, 128])
+@pytest.mark.parametrize("qn,kn,causal", [([2, 3] * 60, None, True), ([3, 2, 1, 0, 4] * 30, None, False), ([12] * 50, None, True),
+                                          ([40, 0, 60, 3] * 9, [2, 5, 0, 4] * 9, False)])
+def test_gradients_of_few_keys(qn, kn, causal, d, dtype):
+    """Few keys a row: the gradients are as near the true ones as their roundings, not as what o's rounding leaves of D."""
+    b = batch(qn, kn, 4, 2, d, dtype, causal, "rows", seed=3)
+    b.forward()
+    b.backward()
+    b.check_backward()
+    for name, got, (want, _) in zip(("dq", "dk", "dv"), (b.dq, b.dk, b.dv), b.case().backward(b.g, b.o)):
+        live = ~torch.isnan(want)
+        # Rounding x of a binade [1, 2) is off by at most half a step h, h / sqrt 3 as a root of a mean square; that of x is
+        # sqrt(3 / (2 ln 2)) = 1.47 there (as many in each part of a logarithm): 0.39 h of the norm.  A result and the P or dS that it
+        # sums: 0.39 sqrt 2 = 0.56 h, over hundreds of them; 0.7 leaves room for other spreads (at most 0.58 each where all begin
+        # a binade).  D from the rounded o comes on top: 0.8 h in all for sequences of 2 and 3.
+        far = ((got.cpu().double() - want)[live] ** 2).sum().sqrt() / (want[live] ** 2).sum().sqrt()
+        assert float(far) <= 0.7 * torch.finfo(dtype).eps / 2, (name, float(far))
+
+
 def test_without_lse():
     b = batch([70, 200], None, 2, 1, 64, FP, True, "rows")
     b.forward(lse=False)
