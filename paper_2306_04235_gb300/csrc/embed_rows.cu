@@ -308,12 +308,14 @@ __global__ void __launch_bounds__(ES_THREADS) embed_sort_kernel(const int *ids, 
     }
 }
 
-// Rows that no token names are zero.  Needs the ids alone: runs beside the sort.  A block
-// has the rows that are its number modulo the blocks (those of frequent tokens have low numbers).
+// Rows that no token names are zero.  Needs the ids alone: runs beside the sort, which lets it
+// start only when what was in the stream before is done; alone (no tokens), it waits for that itself.
+// A block has the rows that are its number modulo the blocks (those of frequent tokens have low numbers).
 constexpr int EZ_BITS = 1 << 16, EZ_THREADS = 256, EZ_SETS = 4 * 152;
 template <typename O>
 __global__ void __launch_bounds__(EZ_THREADS) embed_zero_kernel(EmbedRowsArgs a, bool vec) {
     __shared__ uint32_t named[EZ_BITS / 32];
+    if (a.T == 0) pdl_grid_wait();
     pdl_allow_next();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, x = blockIdx.x;
     const int rows = x < a.V ? (a.V - x + EZ_SETS - 1) / EZ_SETS : 0;
@@ -508,7 +510,9 @@ size_t sort_ints(int T) { return ((size_t)T + 3) / 4 * 4; }
 size_t sum_parts(int T, int d) { return 2 * (((size_t)T + 31) / 32) * ((size_t)(d + EB_COLS - 1) / EB_COLS * EB_COLS); }
 }  // namespace
 
-size_t embed_rows_backward_workspace(int T, int V, int d) { return few_tokens(T, V, d) ? 16 : 16 * sort_ints(T) + 4 * sum_parts(T, d); }
+size_t embed_rows_backward_workspace(int T, int V, int d) {
+    return T == 0 || few_tokens(T, V, d) ? 16 : 16 * sort_ints(T) + 4 * sum_parts(T, d);
+}
 
 cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &args, cudaStream_t st) {
     cudaError_t err = cudaSuccess;
@@ -521,6 +525,11 @@ cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &args, cudaStream_t s
         a.wide = row_alignment(static_cast<const O *>(a.out), a.ldo) == 2;
         if (few_tokens(a.T, a.V, a.d)) {
             err = launch_pdl(vec ? embed_few_kernel<T, O, true> : embed_few_kernel<T, O, false>, dim3((unsigned)few_sets(a.V, a.d), cb), 256, 0, st, a);
+            return;
+        }
+        const bool ovec = row_alignment(static_cast<const O *>(a.out), a.ldo) > 0;
+        if (a.T == 0) {  // nothing to sort or add; a table of that size is zeroed by as many blocks as beside the sort
+            if (!a.accumulate) err = launch_pdl(embed_zero_kernel<O>, EZ_SETS, EZ_THREADS, 0, st, a, ovec);
             return;
         }
         const long chunks = ((long)a.T + 31) / 32;
@@ -550,7 +559,6 @@ cudaError_t launch_embed_rows_backward(const EmbedRowsArgs &args, cudaStream_t s
         cfg.attrs = attr;
         cfg.numAttrs = cs == cudaStreamCaptureStatusActive ? 1 : 2;
         if ((err = cudaLaunchKernelEx(&cfg, embed_sort_kernel, a.ids, a.T, a.V, a.pad_id, passes, b, a.status)) != cudaSuccess) return;
-        const bool ovec = row_alignment(static_cast<const O *>(a.out), a.ldo) > 0;
         if (!a.accumulate && (err = launch_pdl(embed_zero_kernel<O>, EZ_SETS, EZ_THREADS, 0, st, a, ovec)) != cudaSuccess) return;
         const int *key = b.key[(passes - 1) & 1], *idx = b.idx[(passes - 1) & 1];
         err = launch_pdl(vec ? embed_sum_kernel<T, O, true> : embed_sum_kernel<T, O, false>, (unsigned)((chunks * cb + 7) / 8), 256, 0, st, a, key, idx, parts);
