@@ -332,8 +332,10 @@ int mnmt_codes_to_f16(const int8_t *src, uint16_t *dst, size_t n, void *cuda_str
  * block waits on a shared-memory transaction barrier that nothing completes.
  * The wait gives up after one second (the limit of every such wait in
  * mnmt_linear_tc), the kernel records MNMT_ETIMEOUT in *status (device int32,
- * required) and returns; no fault is raised and the context stays usable.
- * Returns once the kernel is queued. */
+ * required) and returns; no fault is raised and the context stays usable.  A
+ * second block does the same with the waits of mnmt_attention_forward and
+ * _backward, and records MNMT_ECUDA where lanes of a warp came apart.
+ * Returns once the kernels are queued. */
 int mnmt_wait_timeout_selftest(int32_t *status, void *cuda_stream);
 
 /* Output-vocabulary projection fused with greedy selection (App. D): for each

@@ -1893,6 +1893,7 @@ extern "C" int mnmt_wait_timeout_selftest(int32_t *status, void *cuda_stream) {
     if (rc) return rc;
     if (!status) return fail(MNMT_EINVAL, "wait_timeout_selftest: status is required");
     cudaError_t err = launch_wait_timeout_selftest(status, static_cast<cudaStream_t>(cuda_stream));
+    if (err == cudaSuccess) err = launch_seq_wait_selftest(status, static_cast<cudaStream_t>(cuda_stream));
     if (err != cudaSuccess) return fail(MNMT_ECUDA, "wait_timeout_selftest launch: %s", cudaGetErrorString(err));
     return MNMT_OK;
 }

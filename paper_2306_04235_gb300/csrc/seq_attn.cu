@@ -219,29 +219,29 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
                 for (int t = 0; t < nt && ok; t++, j++) {
                     const int s = j % ST, at = end - KT * (t0 + t + 1);
                     const uint32_t ph = (uint32_t)(j / ST - 1) & 1;
-                    if (j >= ST && !(ok = wait(k_free(s), ph))) break;
+                    if (j >= ST && !(ok = wait.one(k_free(s), ph))) break;
                     sq_load<DH, KT>(sm + L::OFF_K + s * L::TILE, &tk, hk, at, k_full(s));
-                    if (j >= ST && !(ok = wait(v_free(s), ph))) {
-                        wait(k_full(s), (uint32_t)(j / ST) & 1);  // in flight
+                    if (j >= ST && !(ok = wait.one(v_free(s), ph))) {
+                        wait.one(k_full(s), (uint32_t)(j / ST) & 1);  // in flight
                         break;
                     }
                     sq_load<DH, KT>(sm + L::OFF_V + s * L::TILE, &tv, hk, at, v_full(s));
                     // the next head's queries, once the results of the head that had their place are stored
                     if (t == min(1, nt - 1) && QS > 1 && nq < nh) {
-                        if (nq >= QS && !(ok = wait(q_free(nq % QS), (uint32_t)(nq / QS - 1) & 1))) continue;
+                        if (nq >= QS && !(ok = wait.one(q_free(nq % QS), (uint32_t)(nq / QS - 1) & 1))) continue;
                         sq_load<DH>(sm + nq % QS * L::QT, &tq, h0 + nq, tile * SQ_ROWS, q_full(nq % QS));
                         nq++;
                     }
                 }
                 if (QS == 1 && ok && nq < nh) {
-                    if (!(ok = wait(q_free(0), (uint32_t)it & 1))) break;
+                    if (!(ok = wait.one(q_free(0), (uint32_t)it & 1))) break;
                     sq_load<DH>(sm, &tq, h0 + nq, tile * SQ_ROWS, q_full(0));
                     nq++;
                 }
             }
             if (failed || nt == 0) {  // copies in flight land before the block ends
-                for (int i = max(0, nq - QS); i < nq; i++) wait(q_full(i % QS), (uint32_t)(i / QS) & 1);
-                for (int i = max(0, j - ST); i < j; i++) wait(k_full(i % ST), (uint32_t)(i / ST) & 1), wait(v_full(i % ST), (uint32_t)(i / ST) & 1);
+                for (int i = max(0, nq - QS); i < nq; i++) wait.one(q_full(i % QS), (uint32_t)(i / QS) & 1);
+                for (int i = max(0, j - ST); i < j; i++) wait.one(k_full(i % ST), (uint32_t)(i / ST) & 1), wait.one(v_full(i % ST), (uint32_t)(i / ST) & 1);
             }
         }
     } else if (warp == 5) {
@@ -413,6 +413,26 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     if (warp == 5) tmem_free<L::COLS>(tslot);
 }
 
+// The give-up of SqWaits, for mnmt_wait_timeout_selftest: a warp half of whose lanes would see
+// their phase end, one none of whose lanes do, and one whose lanes all do, which the others' giving up does not touch.
+__global__ void __launch_bounds__(96) seq_wait_selftest_kernel(int *status) {
+    __shared__ __align__(8) uint64_t bars[2];
+    __shared__ int failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t never = s_addr(bars), ended = never + 8;
+    if (threadIdx.x == 0) {
+        mbar_init(never, 1), mbar_init(ended, 1);
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        mbar_arrive(ended);
+    }
+    __syncthreads();
+    const SqWaits wait{&failed, status};
+    const bool ok = wait(warp == 2 || (warp == 0 && lane < 16) ? ended : never, 0);
+    const uint32_t all = __ballot_sync(0xFFFFFFFFu, ok);
+    if (lane == 0 && (all != (warp == 2 ? 0xFFFFFFFFu : 0u) || wait.one(never, 0) || !wait.one(ended, 0) || !failed)) atomicExch(status, MNMT_ECUDA);
+}
+
 // Where there are no keys at all, rows of sequences are zeros.
 template <typename T>
 __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
@@ -471,6 +491,11 @@ cudaError_t seq_attn_init() {
     if (e == cudaSuccess) e = tile_init<128, true>();
     if (e == cudaSuccess) e = tile_init<128, false>();
     return e;
+}
+
+cudaError_t launch_seq_wait_selftest(int *status, cudaStream_t st) {
+    seq_wait_selftest_kernel<<<1, 96, 0, st>>>(status);
+    return cudaGetLastError();
 }
 
 size_t seq_attn_forward_workspace(const SeqAttn &) { return 16; }

@@ -202,11 +202,11 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             const auto at = [&](int j) { return end - W * (t0 + (j < nt ? j : j - nt) + 1); };  // rows of step j's tile
             // K(0), then V(j) and K(j + KS - VS) by turns: each waits for what the tensor core is done with first
             for (; jv < n; jv++) {
-                if (jv >= VS && !wait(v_free(jv % VS), (uint32_t)(jv / VS - 1) & 1)) break;
+                if (jv >= VS && !wait.one(v_free(jv % VS), (uint32_t)(jv / VS - 1) & 1)) break;
                 for (; jk <= jv; jk++) sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, at(jk), k_full(jk % KS));  // the first
                 sq_load<DH, W>(sm + L::OFF_V + jv % VS * L::TILE, &tv, hk, at(jv), v_full(jv % VS));
                 for (; jk < n && jk <= jv + KS - VS; jk++) {
-                    if (jk >= KS && !wait(k_free(jk % KS), (uint32_t)(jk / KS - 1) & 1)) break;
+                    if (jk >= KS && !wait.one(k_free(jk % KS), (uint32_t)(jk / KS - 1) & 1)) break;
                     sq_load<DH, W>(sm + L::OFF_K + jk % KS * L::TILE, &tk, hk, at(jk), k_full(jk % KS));
                 }
                 if (failed) {
@@ -215,9 +215,9 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
                 }
             }
             if (failed) {  // copies in flight land before the block ends
-                wait(q_full, 0);
-                for (int i = max(0, jk - KS); i < jk; i++) wait(k_full(i % KS), (uint32_t)(i / KS) & 1);
-                for (int i = max(0, jv - VS); i < jv; i++) wait(v_full(i % VS), (uint32_t)(i / VS) & 1);
+                wait.one(q_full, 0);
+                for (int i = max(0, jk - KS); i < jk; i++) wait.one(k_full(i % KS), (uint32_t)(i / KS) & 1);
+                for (int i = max(0, jv - VS); i < jv; i++) wait.one(v_full(i % VS), (uint32_t)(i / VS) & 1);
             }
         }
     } else if (warp == 9) {
@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             bool ok = true;
             const auto next_q = [&] {
                 const int s = jq % QS;
-                if (jq >= QS) ok = __all_sync(0xFFFFFFFFu, wait(q_free(s), (uint32_t)(jq / QS - 1) & 1));
+                if (jq >= QS) ok = wait(q_free(s), (uint32_t)(jq / QS - 1) & 1);
                 if (!ok) return;
                 if (lane == 0) sq_load<DH, W>(sm + L::OFF_Q + s * L::TILE, &tq, hq, end - W * (tq_ + 1), q_full(s));
                 if (++tq_ == nt) tq_ = 0, hq++;
@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             next_q();
             while (ok && jg < n) {
                 const int s = jg % GS, at = end - W * (tg_ + 1);
-                if (jg >= GS) ok = __all_sync(0xFFFFFFFFu, wait(g_free(s), (uint32_t)(jg / GS - 1) & 1));
+                if (jg >= GS) ok = wait(g_free(s), (uint32_t)(jg / GS - 1) & 1);
                 if (!ok) break;
                 if (lane == 0) sq_load<DH, W>(sm + L::OFF_G + s * L::TILE, &tg, hg, at, g_full(s));
                 // -lse log2 e and -D
@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                 const int b = jg & 1, turn = jg >> 1;
                 jg++;
                 while (ok && jq < n && jq < jg + QS - GS) next_q();
-                if (ok && turn) ok = __all_sync(0xFFFFFFFFu, wait(n_free + 8 * b, (uint32_t)(turn - 1) & 1));
+                if (ok && turn) ok = wait(n_free + 8 * b, (uint32_t)(turn - 1) & 1);
                 if (!ok) break;
                 float *num = reinterpret_cast<float *>(smp + L::OFF_N + b * L::NUM);
 #pragma unroll
@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                 __syncwarp();
                 if (lane == 0) mbar_arrive(n_full + 8 * b);
             }
-            if (failed) {  // copies in flight land before the block ends
+            if (wait.given_up()) {  // copies in flight land before the block ends
                 wait(kv_full, 0);
                 for (int i = max(0, jq - QS); i < jq; i++) wait(q_full(i % QS), (uint32_t)(i / QS) & 1);
                 for (int i = max(0, jg - GS); i < jg; i++) wait(g_full(i % GS), (uint32_t)(i / GS) & 1);

@@ -182,27 +182,64 @@ cudaError_t sq_launch(void (*kernel)(KArgs...), unsigned grid, int ctas, int thr
 // what was written to or read from shared memory comes before copies into it by TMA (all threads, before a barrier)
 __device__ __forceinline__ void sq_before_copies() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// mbar_try of a whole warp: the vote on its own predicate, so that all lanes have the same answer
+__device__ __forceinline__ bool sq_try_all(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "vote.sync.all.pred p, p, 0xFFFFFFFF;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+
 // Waits of a kernel's roles: a wait that gives up sets `failed` in shared memory and the
-// status, and every role leaves its loop at its next wait.
+// status, and every role leaves its loop at its next wait.  What comes behind a warp's wait takes
+// whole warps (tcgen05.ld and st, votes), so its lanes give up as one, by votes: looking
+// for themselves, one might see the phase end that another had just given up.
+static __device__ __noinline__ bool sq_wait_warp(volatile int *failed, int *status, uint32_t bar, uint32_t parity) {
+    unsigned long long t0 = 0;
+    for (int i = 0;; i++) {
+        if (sq_try_all(bar, parity)) return true;
+        if (i < 8) continue;
+        if (i == 8) t0 = global_ns();
+        if (__any_sync(0xFFFFFFFFu, *failed || global_ns() - t0 > MNMT_WAIT_NS)) break;
+    }
+    if ((threadIdx.x & 31) == 0) {
+        *failed = 1;
+        set_status(status, MNMT_ETIMEOUT);
+    }
+    return false;
+}
+static __device__ __noinline__ bool sq_wait_one(volatile int *failed, int *status, uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < 8; i++)
+        if (mbar_try(bar, parity)) return true;
+    const unsigned long long t0 = global_ns();
+    while (!mbar_try(bar, parity))
+        if (*failed || global_ns() - t0 > MNMT_WAIT_NS) {
+            *failed = 1;
+            set_status(status, MNMT_ETIMEOUT);
+            return false;
+        }
+    return true;
+}
 struct SqWaits {
     volatile int *failed;
     int *status;
+    // A whole warp: alike in all lanes.  The first look may suspend the warp for a while: one that
+    // never does sent most waits into the call (3 x 2500..4095 rows of 16 heads of 128, gradients: 400 us, 366 so).
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
-        if (mbar_test(bar, parity)) return true;
-        return slow(bar, parity);
+        return sq_try_all(bar, parity) || sq_wait_warp(failed, status, bar, parity);
     }
-    __device__ __noinline__ bool slow(uint32_t bar, uint32_t parity) const {
-        for (int i = 0; i < 8; i++)
-            if (mbar_try(bar, parity)) return true;
-        const unsigned long long t0 = global_ns();
-        while (!mbar_try(bar, parity))
-            if (*failed || global_ns() - t0 > MNMT_WAIT_NS) {
-                *failed = 1;
-                set_status(status, MNMT_ETIMEOUT);
-                return false;
-            }
-        return true;
+    // one lane
+    __device__ __forceinline__ bool one(uint32_t bar, uint32_t parity) const {
+        return mbar_test(bar, parity) || sq_wait_one(failed, status, bar, parity);
     }
+    // whether a role has given up: alike in all lanes of a warp
+    __device__ __forceinline__ bool given_up() const { return __any_sync(0xFFFFFFFFu, *failed); }
 };
 
 }  // namespace mnmt

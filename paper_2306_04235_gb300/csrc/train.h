@@ -65,6 +65,7 @@ struct SeqAttn {
 cudaError_t seq_attn_init();  // set-up of the kernels on the current device
 cudaError_t seq_attn_backward_init();
 cudaError_t seq_attn_token_init();
+cudaError_t launch_seq_wait_selftest(int *status, cudaStream_t st);
 size_t seq_attn_forward_workspace(const SeqAttn &a);
 size_t seq_attn_backward_workspace(const SeqAttn &a);
 size_t seq_attn_token_workspace(const SeqAttn &a);
