@@ -549,7 +549,8 @@ int mnmt_attention_forward(const mnmt_attention_shape *shape, const mnmt_heads *
  *   dq[i] = scale sum_j dS_ij k[j],  dk[j] = scale sum_i dS_ij q[i]
  * (dk, dv: over the query heads that share the key head).  Sums in a fixed order.  The
  * gradients have the operands' type; none of their buffers is an input.  (g[i] . o[i], which is
- * sum_j P_ij g[i] . v[j], is taken from that sum where few keys make o's rounding count.) */
+ * sum_j P_ij g[i] . v[j], is taken from that sum in sequences whose queries see 10 keys or fewer on
+ * average, of those that see any, where o's rounding counts most; and for dk with bf16 and heads up to 64.) */
 size_t mnmt_attention_backward_workspace(const mnmt_attention_shape *shape);
 int mnmt_attention_backward(const mnmt_attention_shape *shape, const mnmt_heads *q, const mnmt_heads *k, const mnmt_heads *v,
                             const mnmt_heads *o, const float *lse, const mnmt_heads *g, const mnmt_heads *dq,

@@ -191,9 +191,9 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     pdl_grid_wait();
     const SeqAttn ix = seq_shared(a, reinterpret_cast<int *>(smp + L::OFF_K), FW_THREADS);  // where keys and values come later
     Span keys{0, 0};
-    bool in = false;
+    bool in = false, few;
     if (warp < 4) {
-        keys = keys_of_lane(ix, row - lane, in);
+        keys = keys_of_lane(ix, row - lane, in, few);
         const bool some = keys.hi > keys.lo;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? keys.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? keys.hi : 0);
         if (lane == 0) span[0][warp] = lo, span[1][warp] = hi;
@@ -439,9 +439,9 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     pdl_grid_wait();
     const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 5;
     const int lane = threadIdx.x & 31;
-    bool in;
+    bool in, few;
     if (w >= a.q_rows) return;
-    keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in);
+    keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in, few);
     if (!in) return;
     const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int h = 0; h < a.hq; h++) {

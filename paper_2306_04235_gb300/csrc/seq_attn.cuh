@@ -48,14 +48,17 @@ MNMT_DEV Span seq_rows(const int *start, const int *len, int b, int rows) {
     return r;
 }
 
-// the keys that query row sees (b: as seq_of; in: whether it belongs to a sequence at all)
-MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, int b, bool &in) {
-    in = false;
+// the keys that query row sees (b: as seq_of; in: whether it belongs to a sequence at all; few: whether the rows of its
+// sequence that see a key see 10 of them or fewer on average)
+MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, int b, bool &in, bool &few) {
+    in = few = false;
     if (b < 0) return Span{0, 0};
     const Span q = seq_rows(a.q_start, a.q_len, b, a.q_rows);
     if (row >= q.hi) return Span{0, 0};
     in = true;
     Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
+    const int nk = k.hi - k.lo;
+    few = nk <= 20 && 2 * nk - (a.causal ? min(q.hi - q.lo, nk) - 1 : 0) <= 20;
     if (a.causal) k.hi = min(k.hi, k.hi - (q.hi - 1 - row));  // the last query sees all keys
     if (k.hi < k.lo) k.hi = k.lo;
     return k;
@@ -116,9 +119,9 @@ MNMT_DEV int seq_of_lane(const int *start, int n, int row0) {
 }
 
 // the keys that query row0 + lane sees, and the queries that see key row0 + lane; whole warps
-MNMT_DEV Span keys_of_lane(const SeqAttn &a, int row0, bool &in) {
+MNMT_DEV Span keys_of_lane(const SeqAttn &a, int row0, bool &in, bool &few) {
     const int row = row0 + (threadIdx.x & 31), b = row0 < a.q_rows ? seq_of_lane(a.q_start, a.n_seqs, row0) : -1;
-    return keys_of_query(a, row, row < a.q_rows ? b : -1, in);
+    return keys_of_query(a, row, row < a.q_rows ? b : -1, in, few);
 }
 MNMT_DEV Span queries_of_lane(const SeqAttn &a, int row0, bool &in, bool &one) {
     const int row = row0 + (threadIdx.x & 31), b = row0 < a.k_rows ? seq_of_lane(a.k_start, a.n_seqs, row0) : -1;

@@ -109,8 +109,49 @@ __device__ __noinline__ void dq_again(const SeqAttn &a, uint32_t again, int row,
     }
 }
 
-// FEW: sequences of few keys, see `twice`
-template <int DH, bool BF, int W, bool FEW>
+// The first walk, for rows of sequences of few keys, over n tiles: the sum of dS with D from the rounded o; lo .. hi - 1: the
+// row's keys as seen from a thread's columns of the first tile (none: hi <= lo).  16 columns at a time in a loop that stays one:
+// its code lies between the start and the walk of every CTA, and four times as much of it cost those without such rows 1 %.
+struct FirstWalk {
+    float rest;
+    bool ok;
+};
+template <int W>
+__device__ __forceinline__ FirstWalk dq_first_walk(const SqWaits &wait, uint32_t sp_full, uint32_t sp_free, uint32_t scores, uint32_t weights, int lo, int hi,
+                                                   int n, float c, float lse2, float D) {
+    const unsigned long long c2 = f4_two(c, c), l2 = f4_two(-lse2, -lse2), d2 = f4_two(-D, -D);
+    unsigned long long rest = f4_two(0.0f, 0.0f);
+    for (int j = 0; j < n; j++, lo += W, hi += W) {
+        if (!wait(sp_full, (uint32_t)j & 1)) return FirstWalk{0.0f, false};
+        tc_fence_after();
+        if (__any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2 && lo < hi)) {
+#pragma unroll 1
+            for (int b = 0; b < W / 2; b += 16) {
+                uint32_t s[16], p[16];
+                tmem_ld16(scores + b, s);
+                tmem_ld16(weights + b, p);
+                tmem_wait_ld();
+                const uint32_t see = sq_bits(lo - b, hi - b);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    float x, y, u, v;
+                    f4_untwo(sq_fma2(f4_two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, l2), x, y);
+                    const unsigned long long t = f4_add2(f4_two(__uint_as_float(p[2 * i]), __uint_as_float(p[2 * i + 1])), d2);
+                    f4_untwo(f4_mul2(f4_two(exp2_fast(x), exp2_fast(y)), t), u, v);
+                    rest = f4_add2(rest, f4_two((see >> (2 * i)) & 1u ? u : 0.0f, (see >> (2 * i + 1)) & 1u ? v : 0.0f));
+                }
+            }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(sp_free);
+    }
+    float ra, rb;
+    f4_untwo(rest, ra, rb);
+    return FirstWalk{ra + rb, true};
+}
+
+template <int DH, bool BF, int W>
 __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_attn_dq_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
                                                                     const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                                                                     const __grid_constant__ SeqAttn a, const float c, float *delta, const int ctas) {
@@ -163,14 +204,14 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     }
     const SeqAttn ix = seq_shared(a, reinterpret_cast<int *>(smp + L::OFF_K), BW_THREADS);  // where keys and values come later
     Span keys{0, 0};
-    bool in = false;
+    bool in = false, few = false;
     if (warp < 8) {
-        keys = keys_of_lane(ix, row - lane, in);
+        keys = keys_of_lane(ix, row - lane, in, few);
         const bool some = keys.hi > keys.lo;
+        few &= some;
         const int lo = __reduce_min_sync(0xFFFFFFFFu, some ? keys.lo : 0x7FFFFFFF), hi = __reduce_max_sync(0xFFFFFFFFu, some ? keys.hi : 0);
-        const int seen = __reduce_add_sync(0xFFFFFFFFu, some ? min(keys.hi - keys.lo, 1 << 16) : 0);
-        const uint32_t see = __ballot_sync(0xFFFFFFFFu, some);
-        if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi, span[2][warp] = seen, span[3][warp] = __popc(see);
+        const int few_lo = __reduce_min_sync(0xFFFFFFFFu, few ? keys.lo : 0x7FFFFFFF), few_hi = __reduce_max_sync(0xFFFFFFFFu, few ? keys.hi : 0);
+        if (lane == 0 && half == 0) span[0][warp] = lo, span[1][warp] = hi, span[2][warp] = few_lo, span[3][warp] = few_hi;
 #pragma unroll
         for (int i = 0; i < NR; i++) {
             float dot = dot8<T>(ov[i], gv[i]);
@@ -187,19 +228,20 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     const int first = min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])), end = max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3]));
     // this CTA's tiles, nt of them from t0 on
     const int all_t = end > first ? (end - first + W - 1) / W : 0, t0 = (int)((long)all_t * share / ctas), nt = (int)((long)all_t * (share + 1) / ctas) - t0;
-    // Where rows see few keys, D from the rounded o is off by what weighs most in dq and dk (sequences of 2 or 3: 3.7e-3 of dq's
-    // norm, 1.7e-3 its own rounding; of 10: 2.4e-3; of 40: 2.0e-3).  There the tiles are walked twice, at first for
-    // the sum of dS, which is zero but for that.  (In a kernel of its own: the code alone cost long walks 2 %.)
-    const bool twice = FEW && ctas == 1 && span[2][0] + span[2][1] + span[2][2] + span[2][3] <= 16 * (span[3][0] + span[3][1] + span[3][2] + span[3][3]);
-    const int n1 = twice ? nt : 0, n = n1 + nt;  // steps of the first walk, of both
+    // Where a sequence's rows see few keys (10 on average or fewer), D from the rounded o is off by what weighs most in dq and dk
+    // (sequences of 2 or 3: 3.7e-3 of dq's norm, 1.7e-3 its own rounding; of 10: 2.4e-3; of 40: 2.0e-3).  The tiles that hold
+    // such rows' keys, n1 of them from f0 on, are walked before the others for the sum of dS, which is zero but for that; where a
+    // cluster shares the rows, by each of its CTAs.  (Up to 16 keys: 128 x 20..128 causal rows of 8 heads of 64 40.8 us, so 39.1.)
+    const int few_lo = min(min(span[2][0], span[2][1]), min(span[2][2], span[2][3])), few_hi = max(max(span[3][0], span[3][1]), max(span[3][2], span[3][3]));
+    const int f0 = (end - few_hi) / W, n1 = few_hi > few_lo ? (end - few_lo - 1) / W - f0 + 1 : 0, n = n1 + nt;  // steps of both walks
     const SqWaits wait{&failed, a.status};
 
     if (warp == 8) {
-        if (lane == 0 && nt) {
+        if (lane == 0 && n) {
             sq_load<DH>(sm, &tq, h, tile * SQ_ROWS, q_full);
             sq_load<DH>(sm + L::OFF_G, &tg, h, tile * SQ_ROWS, q_full);
             int jk = 0, jv = 0;  // loads issued
-            const auto at = [&](int j) { return end - W * (t0 + (j < nt ? j : j - nt) + 1); };  // rows of step j's tile
+            const auto at = [&](int j) { return end - W * ((j < n1 ? f0 + j : t0 + j - n1) + 1); };  // rows of step j's tile
             // K(0), then V(j) and K(j + KS - VS) by turns: each waits for what the tensor core is done with first
             for (; jv < n; jv++) {
                 if (jv >= VS && !wait.one(v_free(jv % VS), (uint32_t)(jv / VS - 1) & 1)) break;
@@ -221,7 +263,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             }
         }
     } else if (warp == 9) {
-        if (nt) {
+        if (n) {
             const uint32_t on = elect_one();
             const uint64_t qd = sq_k(sm), gd = sq_k(sm + L::OFF_G), kd = sq_k(sm + L::OFF_K), vd = sq_k(sm + L::OFF_V), kt = sq_mn<W>(sm + L::OFF_K);
             bool ok = wait(q_full, 0);
@@ -263,62 +305,27 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         pdl_allow_next();
     } else {
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const long at_row = (long)h * a.q_rows + row;
-        float D = dots[rt];
-        if (!FINE && !twice && in && half == 0 && share == 0) delta[at_row] = D;
-        unsigned long long rest = f4_two(0.0f, 0.0f);  // sum of dS
         const bool none = keys.hi <= keys.lo;
-        // a query's only key has the weight 1 and dS = 0, where dP - D would leave what their two sums are rounded by (0, not
-        // nothing: what is not a number stays so)
-        const float f = keys.hi - keys.lo == 1 ? 0.0f : a.scale;
-        const float lse2 = none ? 0.0f : a.lse[at_row] * LOG2E;
-        const unsigned long long c2 = f4_two(c, c), l2 = f4_two(-lse2, -lse2);
+        float D = dots[rt];
         bool ok = true;
-        if (twice) {
-            const unsigned long long d2 = f4_two(-D, -D);
-            for (int j = 0; j < nt; j++) {
-                if (!(ok = wait(sp_full, (uint32_t)j & 1))) break;
-                tc_fence_after();
-                const int at = end - W * (t0 + j + 1) + W / 2 * half, lo = keys.lo - at, hi = keys.hi - at;
-                const bool some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
-                uint32_t s[W / 64][32] = {}, p[W / 64][32] = {};
-                if (some) {
-#pragma unroll
-                    for (int b = 0; b < W / 64; b++) {
-                        tmem_ld32(tS + lanes + W / 2 * half + 32 * b, s[b]);
-                        tmem_ld32(tP + lanes + W / 2 * half + 32 * b, p[b]);
-                    }
-                    tmem_wait_ld();
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(sp_free);
-                if (!some) continue;
-#pragma unroll
-                for (int b = 0; b < W / 64; b++) {
-                    const uint32_t see = sq_bits(lo - 32 * b, hi - 32 * b);
-#pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        float x, y, u, v;
-                        f4_untwo(sq_fma2(f4_two(__uint_as_float(s[b][2 * i]), __uint_as_float(s[b][2 * i + 1])), c2, l2), x, y);
-                        const unsigned long long t = f4_add2(f4_two(__uint_as_float(p[b][2 * i]), __uint_as_float(p[b][2 * i + 1])), d2);
-                        f4_untwo(f4_mul2(f4_two(exp2_fast(x), exp2_fast(y)), t), u, v);
-                        rest = f4_add2(rest, f4_two((see >> (2 * i)) & 1u ? u : 0.0f, (see >> (2 * i + 1)) & 1u ? v : 0.0f));
-                    }
-                }
-            }
+        if (n1) {
+            const int at = end - W * (f0 + 1) + W / 2 * half;
+            const FirstWalk x = dq_first_walk<W>(wait, sp_full, sp_free, tS + lanes + W / 2 * half, tP + lanes + W / 2 * half, few ? keys.lo - at : 0,
+                                                 few ? keys.hi - at : 0, n1, c, none ? 0.0f : a.lse[(long)h * a.q_rows + row] * LOG2E, D);
+            ok = x.ok;
             // a row's two halves (every warp comes here, whether its waits were in vain or not)
-            float ra, rb;
-            f4_untwo(rest, ra, rb);
             elements_sync();
-            if (half) dots[rt] = ra + rb;
+            if (half) dots[rt] = x.rest;
             elements_sync();
-            if (!half) dots[rt] = D + (ra + rb + dots[rt]);
+            if (!half) dots[rt] = D + (x.rest + dots[rt]);
             elements_sync();
             D = dots[rt];
-            if (in && half == 0) delta[at_row] = D;
         }
-        const unsigned long long d2 = f4_two(-D, -D);
+        const long at_row = (long)h * a.q_rows + row;
+        if (!FINE && in && half == 0 && share == 0) delta[at_row] = D;
+        unsigned long long rest = f4_two(0.0f, 0.0f);  // sum of dS
+        const float lse2 = none ? 0.0f : a.lse[at_row] * LOG2E;
+        const unsigned long long c2 = f4_two(c, c), l2 = f4_two(-lse2, -lse2), d2 = f4_two(-D, -D);
         for (int j = 0; j < nt && ok; j++) {
             if (!(ok = wait(sp_full, (uint32_t)(n1 + j) & 1))) break;
             tc_fence_after();
@@ -384,18 +391,23 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             __syncwarp();
             if (lane == 0) mbar_arrive(ds_full);
         }
-        if (nt) ok = wait(dq_full, 0) && ok;
+        if (n) ok = wait(dq_full, 0) && ok;
         tc_fence_after();
-        if (FINE && !twice) {
+        float *rests = reinterpret_cast<float *>(smp + L::OFF_K);  // where keys were, of a row's two halves
+        if (FINE) {
             // A row's dS add up to zero but for what D is off by (o is rounded): D + that is what dk and dv take.  (Where a
-            // cluster shares the row, no CTA has the sum.)
+            // cluster shares the row, its CTAs' sums are added below.)
             float ra, rb;
             f4_untwo(rest, ra, rb);
             elements_sync();
-            if (half) dots[rt] = ra + rb;
+            if (ctas > 1) rests[2 * rt + half] = ra + rb;
+            else if (half) dots[rt] = ra + rb;
             elements_sync();
-            if (in && half == 0 && share == 0) delta[at_row] = ctas == 1 && !none ? D + (ra + rb + dots[rt]) : D;
+            if (ctas == 1 && in && half == 0) delta[at_row] = none ? D : D + (ra + rb + dots[rt]);
         }
+        // a query's only key has the weight 1 and dS = 0, where dP - D would leave what their two sums are rounded by (0, not
+        // nothing: what is not a number stays so)
+        const float f = keys.hi - keys.lo == 1 ? 0.0f : a.scale;
         bool odd = false;
         int c0 = 0, c1 = DH;  // the columns that this CTA stores
         if (ctas == 1 && ok) {
@@ -431,6 +443,14 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             }
             __syncwarp();
             sq_cluster_sync();
+            if (FINE && share == 0 && half == 0) {
+                float r = 0.0f;
+                for (int i = 0; i < ctas; i++) {
+                    const float2 x = sq_remote2(t2_mapa(s_addr(rests + 2 * rt), i));
+                    r += x.x + x.y;
+                }
+                if (in) delta[at_row] = none ? D : D + r;
+            }
             // every CTA of the cluster adds up a share of the columns, in the order of the CTAs
             c0 = DH / ctas * share, c1 = c0 + DH / ctas;
             if (ok && half == 0)
@@ -808,10 +828,10 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 5;
     const int lane = threadIdx.x & 31;
     const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    bool in, one;
+    bool in, one, few;
     if (a.k_rows == 0) {
         if (w >= a.q_rows) return;
-        keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in);
+        keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in, few);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hq; h++) store4(static_cast<T *>(a.dq.p) + w * a.dq.ld + h * a.dq.hd + 4 * lane, z);
     } else {
         if (w >= a.k_rows) return;
@@ -867,8 +887,7 @@ cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
     const float c = a.scale * LOG2E;
     const unsigned qt = (unsigned)((a.q_rows + SQ_ROWS - 1) / SQ_ROWS), kt = (unsigned)((a.k_rows + SQ_ROWS - 1) / SQ_ROWS);
     const int cq = dq_ctas(qt, a, W, 512 / DqLayout<DH, W>::COLS);
-    const bool few = a.k_rows <= 64L * a.n_seqs;
-    const cudaError_t e = sq_launch(few ? seq_attn_dq_kernel<DH, BF, W, true> : seq_attn_dq_kernel<DH, BF, W, false>, qt * a.hq * cq, cq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta, cq);
+    const cudaError_t e = sq_launch(seq_attn_dq_kernel<DH, BF, W>, qt * a.hq * cq, cq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta, cq);
     if (e != cudaSuccess) return e;
     const int ctas = dkv_ctas(kt, a, W, 512 / DkvLayout<DH, W>::COLS);
     return sq_launch(seq_attn_dkv_kernel<DH, BF, W>, kt * a.hkv * ctas, ctas, BW_THREADS, DkvLayout<DH, W>::SMEM, st, tk, tv, wq, wg, a, c,
@@ -877,8 +896,7 @@ cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
 
 template <int DH, bool BF, int W>
 cudaError_t tile_init() {
-    cudaError_t e = cudaFuncSetAttribute(seq_attn_dq_kernel<DH, BF, W, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<DH, W>::SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(seq_attn_dq_kernel<DH, BF, W, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<DH, W>::SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(seq_attn_dq_kernel<DH, BF, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<DH, W>::SMEM);
     return e != cudaSuccess ? e : cudaFuncSetAttribute(seq_attn_dkv_kernel<DH, BF, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, DkvLayout<DH, W>::SMEM);
 }
 
