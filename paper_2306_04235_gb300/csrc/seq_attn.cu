@@ -9,7 +9,9 @@
 //   S = Q K^T (TMEM), one thread per row: P = 2^(c s - m), c = scale log2 e, with the
 //   running maximum m and sum l; P over S in TMEM, in the operands' type; O += P V.
 // m is moved, and O scaled, only where a score exceeds it by 2^8 (the sum and the
-// result carry the same factor, so any m near the maximum serves).
+// result carry the same factor, so any m near the maximum serves).  For fp16 m is 7 less, so that
+// weights reach 2^15: those below 2^-25 of the largest would leave O but not l (32767 keys at 2^-25.2
+// of one: o 8.5e-4 low, 4e-6 so, of which one step is 4.9e-4).
 // Two CTAs per SM; three tiles of scores in TMEM (heads up to 64; two above), so that the
 // tensor core is tiles ahead of the threads that take powers: tiles of 128 keys with one
 // buffer waited 1750 of 3200 cycles a tile for it (8192 rows of 8 heads of 64 225 us, 158 so).
@@ -41,7 +43,7 @@ struct FwLayout {
     // tiles of scores in TMEM, columns of O behind them; CTAs per SM
     static constexpr int BUFS = DH == 64 ? 3 : 2, T_O = BUFS * KT, COLS = pow2_cols(T_O + DH), BLOCKS = 512 / COLS;
 };
-constexpr float FW_SLACK = 8.0f;  // how far, in powers of two, a score may exceed m
+constexpr float FW_SLACK = 8.0f;  // how far, in powers of two, a score may exceed m and its type's lift
 
 // 32 scores of a row from TMEM, -inf where the row does not see the key (see: bits of the 32)
 __device__ __forceinline__ void hide(uint32_t (&r)[32], uint32_t see) {
@@ -291,7 +293,7 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
     } else {
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
         bool ok = true;
-        float m = -INFINITY, l = 0.0f;  // m: of c s
+        float m = -INFINITY, l = 0.0f;  // m: of c s, less the lift
         const bool none = keys.hi <= keys.lo;  // no key: zeros; a sum of nothing but zeros is not a number, as 0 / 0
         for (int it = 0, j = 0; it < nh && ok; it++) {
             const int h = h0 + it;
@@ -328,8 +330,9 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
                 for (int b = 0; b < KT / 32; b++) max32(r[b], mx);
                 const float top = c * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 // the first scores, or scores that 2^8 does not hold
-                if (__any_sync(0xFFFFFFFFu, top > m + FW_SLACK)) {
-                    const float mn = top > m + FW_SLACK ? top : m;
+                constexpr float LIFT = weight_lift<BF>();
+                if (__any_sync(0xFFFFFFFFu, top > m + (LIFT + FW_SLACK))) {
+                    const float mn = top > m + (LIFT + FW_SLACK) ? top - LIFT : m;
                     const float f = m == -INFINITY ? 1.0f : exp2_fast(m - mn);  // nothing was added yet: 0 stays 0
                     m = mn;
                     l *= f;

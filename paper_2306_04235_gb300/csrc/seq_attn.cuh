@@ -134,6 +134,11 @@ MNMT_DEV float warp_sum_f(float v) {
     return v;
 }
 
+// How far below a row's largest score its weights' reference lies, in powers of two: fp16 weights are
+// taken 2^7 larger, as far as 65504 allows beside a slack of 2^8, and reach as much further down.
+template <bool BF>
+__host__ __device__ constexpr float weight_lift() { return BF ? 0.0f : 7.0f; }
+
 // 2^x to within 2 ulp, 0 below -126
 MNMT_DEV float exp2_fast(float x) {
     float y;

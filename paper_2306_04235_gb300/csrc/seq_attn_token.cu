@@ -26,7 +26,7 @@ constexpr int TK_BLOCKS = 2;          // per SM
 constexpr int TK_GRID = 152 * TK_BLOCKS;  // blocks that cut units (a constant: sizes of workspaces are asked for without a device)
 constexpr int TK_MIN_RUN = 4;         // tiles of a run at least
 constexpr int TK_SPLIT_ROWS = 512;    // key rows in memory from which a cut is worth a second launch
-constexpr float TK_SLACK = 8.0f;      // how far, in powers of two, a score may exceed m
+constexpr float TK_SLACK = 8.0f;      // how far, in powers of two, a score may exceed m and its type's lift (weight_lift)
 template <int DH>
 __host__ __device__ constexpr int tk_keys() { return TK_STAGE / (4 * DH); }  // keys of a tile
 
@@ -161,8 +161,9 @@ __device__ __forceinline__ void run_keys(const SeqAttn &a, const Unit &u, Span k
             for (int j = 0; j < KT / 8; j++) top = fmaxf(top, fmaxf(s[j][2 * x], s[j][2 * x + 1]));
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = c * fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            if (__any_sync(0xFFFFFFFFu, top > r.m[x] + TK_SLACK)) {
-                const float mn = top > r.m[x] + TK_SLACK ? top : r.m[x], f = r.m[x] == -INFINITY ? 1.0f : exp2_fast(r.m[x] - mn);
+            constexpr float LIFT = weight_lift<BF>();
+            if (__any_sync(0xFFFFFFFFu, top > r.m[x] + (LIFT + TK_SLACK))) {
+                const float mn = top > r.m[x] + (LIFT + TK_SLACK) ? top - LIFT : r.m[x], f = r.m[x] == -INFINITY ? 1.0f : exp2_fast(r.m[x] - mn);
                 r.m[x] = mn;
                 r.l[x] *= f;
 #pragma unroll
