@@ -519,8 +519,9 @@ int mnmt_dropout_backward(const void *g, int32_t otype, int64_t ldg, const void 
  * d_head: a multiple of 8 up to 128.  dtype (MNMT_BF16 or MNMT_F16): of every operand
  *   below but lse.  scale in (0, 2^60].
  * Scores, weights' sums and results are summed in fp32; the weights (and in the backward
- * pass P and dS) are rounded to dtype in front of the second product, results once.  (fp16
- * holds dS down to 2^-24: gradients in fp16 want a loss scale.)  A query's only key takes no
+ * pass P and dS) are rounded to dtype in front of the second product, results once.  (In fp16
+ * they are scaled to its range by powers of two meanwhile; gradients below 2^-14 are still rounded
+ * to multiples of 2^-24 as results, and want a loss scale.)  A query's only key takes no
  * gradient, and gives q none.  A sequence that holds what is not finite is slower. */
 typedef struct {
     int32_t n_seqs, q_rows, k_rows, q_heads, kv_heads, d_head, dtype, causal;

@@ -14,6 +14,10 @@
 //   dq:      S(j+1), dP(j+1) once S(j), dP(j) are in registers, dQ(j) once dS(j) is written
 // Where tiles of keys are few and their walks long (shared key heads), a cluster of up to
 // eight CTAs divides a walk's steps and adds up its sums through distributed shared memory.
+// fp16 holds little below 2^-14, so P and dS go to TMEM times powers of two, which their exponents take in and results
+// lose again: P of dv 2^15; dS in dq, per row, and in dk, per walk, as the largest |g| that it meets comes to 16..32 (where
+// |dP| then reaches 65504, sums are infinite and are computed again).  Unscaled, 2048 keys with g of 1e-3 left dq of heads of 64 off by
+// 2.7e-3 of its norm, 5.1e-4 so (its own rounding 4.7e-4).
 // A walk goes backwards from the last row that is seen, as in the forward pass, and rows
 // whose result is not finite are computed again over their own queries or keys alone.
 //
@@ -81,6 +85,12 @@ __device__ __forceinline__ float dot8(const uint4 &x, const uint4 &y) {
     }
     return s;
 }
+
+// log2 of the power that takes a largest |g| of `top` to 16..32 (0 and what is not finite: as it is)
+__device__ __forceinline__ int gain_of(float top) { return top > 0.0f && top < INFINITY ? 4 - ((int)(__float_as_uint(top) >> 23) - 127) : 0; }
+constexpr int GAIN_ROWS = 32;      // query rows of a largest |g| that the dq kernel leaves
+constexpr float P_GAIN = 15.0f;    // log2 of the power of P in dk, dv
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 .. 127
 
 // --------------------------------------------------------------------------- dq
 template <int DH, int W>
@@ -154,7 +164,7 @@ __device__ __forceinline__ FirstWalk dq_first_walk(const SqWaits &wait, uint32_t
 template <int DH, bool BF, int W>
 __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_attn_dq_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
                                                                     const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
-                                                                    const __grid_constant__ SeqAttn a, const float c, float *delta, const int ctas) {
+                                                                    const __grid_constant__ SeqAttn a, const float c, float *delta, float *tops, const int ctas) {
     using L = DqLayout<DH, W>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
     // With bf16 and heads up to 64 dS goes in two parts, rounded and what that left, as the tensor core has room there (12 %
@@ -167,6 +177,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
     __shared__ uint32_t tslot;
     __shared__ int failed, span[4][4];
     __shared__ float dots[SQ_ROWS];
+    __shared__ uint16_t g_top[BF ? 1 : SQ_ROWS];  // largest |g| of a row
     __shared__ uint8_t odd_rows[2][SQ_ROWS];
     const uint32_t sm = (s_addr(raw) + 1023u) & ~1023u, bar0 = s_addr(bars);
     uint8_t *smp = raw + (sm - s_addr(raw));
@@ -218,6 +229,13 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
 #pragma unroll
             for (int o = PC / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
             if (lane % PC == 0) dots[16 * warp + i * (32 / PC) + lane / PC] = dot;
+            if constexpr (!BF) {
+                const auto abs2 = [](uint32_t x) { return __habs2(*reinterpret_cast<const __half2 *>(&x)); };
+                __half2 t = __hmax2(__hmax2(abs2(gv[i].x), abs2(gv[i].y)), __hmax2(abs2(gv[i].z), abs2(gv[i].w)));
+#pragma unroll
+                for (int o = PC / 2; o > 0; o >>= 1) t = __hmax2(t, __shfl_xor_sync(0xFFFFFFFFu, t, o));
+                if (lane % PC == 0) g_top[16 * warp + i * (32 / PC) + lane / PC] = __half_as_ushort(__hmax(__low2half(t), __high2half(t)));
+            }
         }
     }
     sq_before_copies();
@@ -323,9 +341,19 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         }
         const long at_row = (long)h * a.q_rows + row;
         if (!FINE && in && half == 0 && share == 0) delta[at_row] = D;
+        int gain = 0;  // log2 of what dS is multiplied by
+        if constexpr (!BF) {
+            const float top = __half2float(__ushort_as_half(g_top[rt]));
+            gain = gain_of(top);
+            if (half == 0 && share == 0) {
+                const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(in && !none && top < INFINITY ? top : 0.0f));
+                if (lane == 0 && row < a.q_rows) tops[(long)h * ((a.q_rows + GAIN_ROWS - 1) / GAIN_ROWS) + row / GAIN_ROWS] = __uint_as_float(most);
+            }
+        }
         unsigned long long rest = f4_two(0.0f, 0.0f);  // sum of dS
         const float lse2 = none ? 0.0f : a.lse[at_row] * LOG2E;
-        const unsigned long long c2 = f4_two(c, c), l2 = f4_two(-lse2, -lse2), d2 = f4_two(-D, -D);
+        const float l = (float)gain - lse2;
+        const unsigned long long c2 = f4_two(c, c), l2 = f4_two(l, l), d2 = f4_two(-D, -D);
         for (int j = 0; j < nt && ok; j++) {
             if (!(ok = wait(sp_full, (uint32_t)(n1 + j) & 1))) break;
             tc_fence_after();
@@ -407,7 +435,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
         }
         // a query's only key has the weight 1 and dS = 0, where dP - D would leave what their two sums are rounded by (0, not
         // nothing: what is not a number stays so)
-        const float f = keys.hi - keys.lo == 1 ? 0.0f : a.scale;
+        const float f = keys.hi - keys.lo == 1 ? 0.0f : a.scale, fo = BF ? f : f * pow2(-gain);
         bool odd = false;
         int c0 = 0, c1 = DH;  // the columns that this CTA stores
         if (ctas == 1 && ok) {
@@ -421,7 +449,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
                 for (int i = 0; i < 16; i++) {
                     const float x = nt && !none ? __uint_as_float(w[2 * i]) : 0.0f, y = nt && !none ? __uint_as_float(w[2 * i + 1]) : 0.0f;
                     odd |= !(fabsf(x) < INFINITY) || !(fabsf(y) < INFINITY);
-                    out[16 * b + i] = sq_pack<BF>(x * f, y * f);
+                    out[16 * b + i] = sq_pack<BF>(x * fo, y * fo);
                 }
             }
             // the queries have been multiplied: their rows are free
@@ -454,7 +482,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             // every CTA of the cluster adds up a share of the columns, in the order of the CTAs
             c0 = DH / ctas * share, c1 = c0 + DH / ctas;
             if (ok && half == 0)
-                odd = sq_join<BF>(s_addr(sums), c0, c1, ctas, none ? 0.0f : 1.0f, f, in, static_cast<T *>(a.dq.p) + row * a.dq.ld + h * a.dq.hd, a.dh);
+                odd = sq_join<BF>(s_addr(sums), c0, c1, ctas, none ? 0.0f : 1.0f, fo, in, static_cast<T *>(a.dq.p) + row * a.dq.ld + h * a.dq.hd, a.dh);
         }
         odd_rows[half][rt] = odd;
         elements_sync();
@@ -510,7 +538,7 @@ __device__ __noinline__ void dkv_again(const SeqAttn &a, uint32_t again, int row
 template <int DH, bool BF, int W>
 __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_attn_dkv_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                                                                      const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tg,
-                                                                     const __grid_constant__ SeqAttn a, const float c, const float *delta, const int ctas) {
+                                                                     const __grid_constant__ SeqAttn a, const float c, const float *delta, const float *tops, const int ctas) {
     using L = DkvLayout<DH, W>;
     using T = std::conditional_t<BF, __nv_bfloat16, __half>;
     constexpr int QS = L::QS, GS = L::GS;
@@ -519,6 +547,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
     int *rest = reinterpret_cast<int *>(smp + L::OFF_R + 8 * (2 * QS + 2 * GS + 10));
     uint32_t &tslot = *reinterpret_cast<uint32_t *>(rest);
     int &failed = rest[1], *span_lo = rest + 2, *span_hi = rest + 6;
+    volatile int &gain = rest[10];  // log2 of what dS is multiplied by, from the first numbers of queries on
     uint8_t *odd_rows = reinterpret_cast<uint8_t *>(rest + 12);
     const auto q_full = [&](int s) { return bar0 + 8 * s; };
     const auto q_free = [&](int s) { return bar0 + 8 * (QS + s); };
@@ -566,6 +595,21 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
     const SqWaits wait{&failed, a.status};
 
     if (warp == 8) {
+        // From the largest |g| of the rows and heads of the whole walk, whoever shares it.  (The first head's first are on their
+        // way from the start: most sentences have no others.)
+        const int per = (a.q_rows + GAIN_ROWS - 1) / GAIN_ROWS, tops0 = first / GAIN_ROWS, n_tops = nt ? (end - 1) / GAIN_ROWS - tops0 + 1 : 0;
+        const uint32_t *top_of = reinterpret_cast<const uint32_t *>(tops) + (long)h0 * per + tops0;
+        [[maybe_unused]] const uint32_t top0 = !BF && lane < n_tops ? top_of[lane] : 0;
+        [[maybe_unused]] const auto find_gain = [&] {
+            uint32_t top = top0;
+            for (int i = lane; i < n_tops; i += 32)
+#pragma unroll 4
+                for (int h = i < 32 ? 1 : 0; h < heads; h++) top = max(top, top_of[(long)h * per + i]);
+            const int e = gain_of(__uint_as_float(__reduce_max_sync(0xFFFFFFFFu, top)));
+            if (lane == 0) gain = e;
+            return e;
+        };
+        if (!BF && nt && !n) find_gain();  // no step of the walk, but a share of the columns
         if (n) {
             if (lane == 0) {
                 sq_load<DH>(sm, &tk, hk, tile * SQ_ROWS, kv_full);
@@ -573,6 +617,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             }
             // Q(0), then G(j), Q(j + QS - GS) and the numbers of tile j's queries by turns
             int jq = 0, jg = 0, hq = h0 + head0, tq_ = t0, hg = hq, tg_ = t0;
+            [[maybe_unused]] float lift = 1.0f;
             bool ok = true;
             const auto next_q = [&] {
                 const int s = jq % QS;
@@ -603,6 +648,11 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                 while (ok && jq < n && jq < jg + QS - GS) next_q();
                 if (ok && turn) ok = wait(n_free + 8 * b, (uint32_t)(turn - 1) & 1);
                 if (!ok) break;
+                if constexpr (!BF) {  // P and dS times their powers (here: the numbers have had time to come)
+                    if (jg == 1) lift = pow2(find_gain() - (int)P_GAIN);
+#pragma unroll
+                    for (int i = 0; i < W / 32; i++) x[0][i] += P_GAIN, x[1][i] *= lift;
+                }
                 float *num = reinterpret_cast<float *>(smp + L::OFF_N + b * L::NUM);
 #pragma unroll
                 for (int i = 0; i < W / 32; i++) num[32 * i + lane] = x[0][i], num[W + 32 * i + lane] = x[1][i];
@@ -702,6 +752,9 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                 }
             };
             const auto gradients = [&](auto whole) {
+                [[maybe_unused]] const float lift = BF ? 1.0f : pow2(gain - (int)P_GAIN);
+                [[maybe_unused]] const unsigned long long lift2 = f4_two(lift, lift);
+                const auto less_d = [&](unsigned long long dp, unsigned long long d) { return BF ? f4_add2(dp, d) : sq_fma2(dp, lift2, d); };
                 uint32_t q[W / 64][32];
                 load_half<W>(tP + lanes + W / 2 * half, q);
 #pragma unroll
@@ -713,10 +766,10 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
                         const float4 x = num[W / 4 + 8 * b + i];
                         float d[4];
                         f4_untwo(f4_mul2(f4_two(__uint_as_float(r[b][4 * i]), __uint_as_float(r[b][4 * i + 1])),
-                                         f4_add2(f4_two(__uint_as_float(q[b][4 * i]), __uint_as_float(q[b][4 * i + 1])), f4_two(x.x, x.y))),
+                                         less_d(f4_two(__uint_as_float(q[b][4 * i]), __uint_as_float(q[b][4 * i + 1])), f4_two(x.x, x.y))),
                                  d[0], d[1]);
                         f4_untwo(f4_mul2(f4_two(__uint_as_float(r[b][4 * i + 2]), __uint_as_float(r[b][4 * i + 3])),
-                                         f4_add2(f4_two(__uint_as_float(q[b][4 * i + 2]), __uint_as_float(q[b][4 * i + 3])), f4_two(x.z, x.w))),
+                                         less_d(f4_two(__uint_as_float(q[b][4 * i + 2]), __uint_as_float(q[b][4 * i + 3])), f4_two(x.z, x.w))),
                                  d[2], d[3]);
                         if (!decltype(whole)::value) {
 #pragma unroll
@@ -759,12 +812,14 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
         tc_fence_after();
         // a row's two threads: dv, dk
         const HeadRows &x = half ? a.dk : a.dv;
-        const float fk = one ? 0.0f : a.scale, f = half ? fk : 1.0f;  // as in the dq kernel
+        const float fk = one ? 0.0f : a.scale;  // as in the dq kernel
+        const auto factor = [&] { return half ? BF || !nt ? fk : fk * pow2(-gain) : BF ? 1.0f : pow2(-(int)P_GAIN); };
         T *o = static_cast<T *>(x.p) + row * x.ld + hk * x.hd;
         bool odd = false;
         int c0 = 0, c1 = DH;  // the columns that this CTA stores
         if (ctas == 1) {
             if (ok) {
+                const float f = factor();
                 uint32_t out[DH / 2];
 #pragma unroll
                 for (int b = 0; b < DH / 32; b++) {
@@ -800,7 +855,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DkvLayout<DH, W>::COLS) seq_
             sq_cluster_sync();
             // every CTA of the cluster adds up a share of the columns, in the order of the CTAs
             c0 = DH / ctas * share, c1 = c0 + DH / ctas;
-            if (ok) odd = sq_join<BF>(s_addr(mine), c0, c1, ctas, qs.hi > qs.lo ? 1.0f : 0.0f, f, in, o, a.dh);
+            if (ok) odd = sq_join<BF>(s_addr(mine), c0, c1, ctas, qs.hi > qs.lo ? 1.0f : 0.0f, factor(), in, o, a.dh);
         }
         odd_rows[half * SQ_ROWS + rt] = odd;
         elements_sync();
@@ -883,15 +938,15 @@ cudaError_t tile_backward(const SeqAttn &a, cudaStream_t st) {
                !sq_map(&wv, a.v, a.k_rows, a.hkv, a.dh, W)) {
         return cudaErrorInvalidValue;
     }
-    float *delta = static_cast<float *>(a.workspace);
+    float *delta = static_cast<float *>(a.workspace), *tops = delta + (size_t)a.hq * a.q_rows;
     const float c = a.scale * LOG2E;
     const unsigned qt = (unsigned)((a.q_rows + SQ_ROWS - 1) / SQ_ROWS), kt = (unsigned)((a.k_rows + SQ_ROWS - 1) / SQ_ROWS);
     const int cq = dq_ctas(qt, a, W, 512 / DqLayout<DH, W>::COLS);
-    const cudaError_t e = sq_launch(seq_attn_dq_kernel<DH, BF, W>, qt * a.hq * cq, cq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta, cq);
+    const cudaError_t e = sq_launch(seq_attn_dq_kernel<DH, BF, W>, qt * a.hq * cq, cq, BW_THREADS, DqLayout<DH, W>::SMEM, st, tq, tg, wk, wv, a, c, delta, tops, cq);
     if (e != cudaSuccess) return e;
     const int ctas = dkv_ctas(kt, a, W, 512 / DkvLayout<DH, W>::COLS);
     return sq_launch(seq_attn_dkv_kernel<DH, BF, W>, kt * a.hkv * ctas, ctas, BW_THREADS, DkvLayout<DH, W>::SMEM, st, tk, tv, wq, wg, a, c,
-                     (const float *)delta, ctas);
+                     (const float *)delta, (const float *)tops, ctas);
 }
 
 template <int DH, bool BF, int W>
@@ -910,7 +965,11 @@ cudaError_t seq_attn_backward_init() {
     return e;
 }
 
-size_t seq_attn_backward_workspace(const SeqAttn &a) { return ((size_t)a.hq * a.q_rows * 4 + 31) / 16 * 16; }
+// D of every row and head; fp16: and the largest |g| of every GAIN_ROWS rows and head
+size_t seq_attn_backward_workspace(const SeqAttn &a) {
+    const size_t n = a.q_rows, tops = a.dtype == MNMT_F16 ? (n + GAIN_ROWS - 1) / GAIN_ROWS : 0;
+    return ((size_t)a.hq * (n + tops) * 4 + 31) / 16 * 16;
+}
 
 cudaError_t launch_seq_attn_backward(const SeqAttn &a, cudaStream_t st) {
     const bool bf = a.dtype == MNMT_BF16;
