@@ -509,11 +509,11 @@ int mnmt_dropout_backward(const void *g, int32_t otype, int64_t ldg, const void 
  * sees no key has o = 0 and lse = -inf.  What a query does not see (other sequences, later
  * keys, rows of no sequence) does not enter its result, infinities and NaN included.
  * Rows: sequence b has the query rows q_start[b] .. q_start[b] + q_len[b] - 1, in memory
- *   order without overlap; q_len NULL: up to q_start[b + 1] - 1 (q_start then has
- *   n_seqs + 1 entries, else n_seqs).  Keys alike with k_start and k_len; with k_len the
- *   key rows of sequences may come in any order and be shared, but not in
- *   mnmt_attention_backward.  Lengths may be zero.  Device arrays; what they name beyond
- *   q_rows and k_rows is left out.
+ *   order without overlap (one without rows may start at or among another's); q_len NULL:
+ *   up to q_start[b + 1] - 1 (q_start then has n_seqs + 1 entries, else n_seqs).  Keys alike
+ *   with k_start and k_len; with k_len the key rows of sequences may come in any order and
+ *   be shared, but not in mnmt_attention_backward.  Lengths may be zero.  Device arrays;
+ *   what they name beyond q_rows and k_rows is left out.
  * q_rows, k_rows: rows in memory of q and o, and of k and v.  Output rows that belong to
  *   no sequence are left as they are.
  * d_head: a multiple of 8 up to 128.  dtype (MNMT_BF16 or MNMT_F16): of every operand

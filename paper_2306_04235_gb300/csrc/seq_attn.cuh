@@ -48,13 +48,22 @@ MNMT_DEV Span seq_rows(const int *start, const int *len, int b, int rows) {
     return r;
 }
 
+// Row's sequence and its rows: b, as seq_of gave it, or one before it where b and those between have no rows (with lengths
+// given, a sequence without rows may start at or among another's).  Whether row is one of them.
+MNMT_DEV bool rows_around(const int *start, const int *len, int rows, int row, int &b, Span &s) {
+    s = seq_rows(start, len, b, rows);
+    if (len)
+        while (row >= s.hi && b > 0 && len[b] <= 0) s = seq_rows(start, len, --b, rows);
+    return row < s.hi;
+}
+
 // the keys that query row sees (b: as seq_of; in: whether it belongs to a sequence at all; few: whether the rows of its
 // sequence that see a key see 10 of them or fewer on average)
 MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, int b, bool &in, bool &few) {
     in = few = false;
     if (b < 0) return Span{0, 0};
-    const Span q = seq_rows(a.q_start, a.q_len, b, a.q_rows);
-    if (row >= q.hi) return Span{0, 0};
+    Span q;
+    if (!rows_around(a.q_start, a.q_len, a.q_rows, row, b, q)) return Span{0, 0};
     in = true;
     Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
     const int nk = k.hi - k.lo;
@@ -68,8 +77,8 @@ MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, int b, bool &in, bool &fe
 MNMT_DEV Span queries_of_key(const SeqAttn &a, int row, int b, bool &in, bool &one) {
     in = one = false;
     if (b < 0) return Span{0, 0};
-    const Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
-    if (row >= k.hi) return Span{0, 0};
+    Span k;
+    if (!rows_around(a.k_start, a.k_len, a.k_rows, row, b, k)) return Span{0, 0};
     in = true;
     one = k.hi - k.lo == 1;
     Span q = seq_rows(a.q_start, a.q_len, b, a.q_rows);
