@@ -177,19 +177,27 @@ __device__ __forceinline__ void run_keys(const SeqAttn &a, const Unit &u, Span k
                 r.l[x] += s[j][2 * x] + s[j][2 * x + 1];
             }
         }
+        uint32_t p[KT / 16][4];
 #pragma unroll
-        for (int k = 0; k < KT / 16; k++) {
-            const uint32_t p[4] = {pack2<BF>(s[2 * k][0], s[2 * k][1]), pack2<BF>(s[2 * k][2], s[2 * k][3]), pack2<BF>(s[2 * k + 1][0], s[2 * k + 1][1]),
-                                   pack2<BF>(s[2 * k + 1][2], s[2 * k + 1][3])};
-            const int rr = 16 * k + (lane & 15);
+        for (int k = 0; k < KT / 16; k++)
 #pragma unroll
-            for (int n = 0; n < DH / 8; n += 2) {
-                const int x = n + (lane >> 4);
+            for (int e = 0; e < 4; e++) p[k][e] = pack2<BF>(s[2 * k + (e >> 1)][2 * (e & 1)], s[2 * k + (e >> 1)][2 * (e & 1) + 1]);
+        // A tile's products from zero, then added: the tensor core truncates what it adds, which over a long walk
+        // made sums small (65536 keys 4e-4 of o, 2^20 keys 7e-3; so 1e-6).
+#pragma unroll
+        for (int n = 0; n < DH / 8; n += 2) {
+            const int x = n + (lane >> 4);
+            float y[2][4] = {};
+#pragma unroll
+            for (int k = 0; k < KT / 16; k++) {
+                const int rr = 16 * k + (lane & 15);
                 uint32_t b[4];
                 ldsm4_t(st + V_OFF + rr * (DH * 2) + 16 * ((x & ~7) | ((x ^ rr) & 7)), b);
-                mma16<BF>(r.o[n], p, b[0], b[1]);
-                mma16<BF>(r.o[n + 1], p, b[2], b[3]);
+                mma16<BF>(y[0], p[k], b[0], b[1]);
+                mma16<BF>(y[1], p[k], b[2], b[3]);
             }
+#pragma unroll
+            for (int e = 0; e < 4; e++) r.o[n][e] += y[0][e], r.o[n + 1][e] += y[1][e];
         }
         __syncwarp();  // the stage has been read
     }
