@@ -15,7 +15,7 @@
 // Where tiles of keys are few and their walks long (shared key heads), a cluster of up to
 // eight CTAs divides a walk's steps and adds up its sums through distributed shared memory.
 // fp16 holds little below 2^-14, so P and dS go to TMEM times powers of two, which their exponents take in and results
-// lose again: P of dv 2^15; dS in dq, per row, and in dk, per walk, as the largest |g| that it meets comes to 16..32 (where
+// lose again: P of dv 2^15; dS in dq, per row, and in dk, per walk, as the largest |g| that it meets comes to 16..32 if it is smaller (where
 // |dP| then reaches 65504, sums are infinite and are computed again).  Unscaled, 2048 keys with g of 1e-3 left dq of heads of 64 off by
 // 2.7e-3 of its norm, 5.1e-4 so (its own rounding 4.7e-4).
 // A walk goes backwards from the last row that is seen, as in the forward pass, and rows
@@ -86,8 +86,9 @@ __device__ __forceinline__ float dot8(const uint4 &x, const uint4 &y) {
     return s;
 }
 
-// log2 of the power that takes a largest |g| of `top` to 16..32 (0 and what is not finite: as it is)
-__device__ __forceinline__ int gain_of(float top) { return top > 0.0f && top < INFINITY ? 4 - ((int)(__float_as_uint(top) >> 23) - 127) : 0; }
+// log2 of the power that takes a largest |g| of `top` to 16..32 (larger ones, 0 and what is not finite: as it is; a power below 1 would
+// take small dS to steps above 2^-24)
+__device__ __forceinline__ int gain_of(float top) { return top > 0.0f ? max(0, 4 - ((int)(__float_as_uint(top) >> 23) - 127)) : 0; }
 constexpr int GAIN_ROWS = 32;      // query rows of a largest |g| that the dq kernel leaves
 constexpr float P_GAIN = 15.0f;    // log2 of the power of P in dk, dv
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 .. 127

@@ -78,6 +78,19 @@ def test_unlike_rows_and_sequences(d):
         hold(b, slice(s, s + m))
 
 
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("size", [1.0, 30.0, 1000.0])
+def test_small_dS_of_large_gradients(size, d):
+    """Every element within the plain form's bounds, in which dS is rounded by 2^-25 at most where it is small, whatever the size of
+    g: sentences beside long sequences, whose last queries leave little of dS for the first keys."""
+    lens = [23, 294, 3, 21, 30, 6, 285, 192, 1]
+    b = Batch(starts(lens), starts(lens), 1, 1, d, FP, True, seed=20, spread=2.0)
+    b.g.mul_(size)
+    run(b)
+    b.check_forward()
+    b.check_backward()
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_what_does_not_fit_is_computed_again(d):
     """dP far above what the size of g lets expect (values of 2000, g along them: dP of 64 x 2000 x 2, a quarter of which
