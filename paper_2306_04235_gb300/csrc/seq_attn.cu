@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
             int next = 0, nit = 0, nst = 0;  // the next scores: number, head and tile of it
             const auto scores = [&] {
                 const int s = next % ST;
-                if (nst == 0 && !wait(q_full(nit % QS), (uint32_t)(nit / QS) & 1)) return false;
+                if ((MANY ? nst : next) == 0 && !wait(q_full(nit % QS), (uint32_t)(nit / QS) & 1)) return false;
                 if (!wait(k_full(s), (uint32_t)(next / ST) & 1)) return false;
                 tc_fence_after();
                 const uint64_t a = qd + (uint64_t)(nit % QS * (L::QT >> 4)), b = kd + (uint64_t)(s * (L::TILE >> 4));
@@ -263,29 +263,47 @@ __global__ void __launch_bounds__(FW_THREADS, FwLayout<DH>::BLOCKS)
                 f4_commit_on<1>(on, k_free(s));
                 f4_commit_on<1>(on, s_full + 8 * (next % BUFS));
                 next++;
-                if (++nst == nt) nst = 0, nit++;
+                if (MANY && ++nst == nt) nst = 0, nit++;
                 return true;
             };
             bool ok = true;
-            for (int it = 0, j = 0; it < nh && ok; it++)
-                for (int t = 0; t < nt && ok; t++, j++) {
-                    // Scores up to BUFS tiles ahead (MMAs keep their order: P(j - 1), whose place S(j + BUFS - 1) takes, has been
-                    // read).  The next head's only if its queries are there: they may wait for what this head has yet to do.
-                    while (ok && next < n && next < j + BUFS &&
-                           (next == j || nst > 0 || (nit <= it + QS - 1 && __all_sync(0xFFFFFFFFu, mbar_test(q_full(nit % QS), (uint32_t)(nit / QS) & 1)))))
-                        ok = scores();
-                    if (ok && t == 0 && it > 0) ok = wait(o_free, (uint32_t)(it - 1) & 1);  // the last head's O has been read
+            if constexpr (MANY) {
+                for (int it = 0, j = 0; it < nh && ok; it++)
+                    for (int t = 0; t < nt && ok; t++, j++) {
+                        // Scores up to BUFS tiles ahead (MMAs keep their order: P(j - 1), whose place S(j + BUFS - 1) takes, has been
+                        // read).  The next head's only if its queries are there: they may wait for what this head has yet to do.
+                        while (ok && next < n && next < j + BUFS &&
+                               (next == j || nst > 0 || (nit <= it + QS - 1 && __all_sync(0xFFFFFFFFu, mbar_test(q_full(nit % QS), (uint32_t)(nit / QS) & 1)))))
+                            ok = scores();
+                        if (ok && t == 0 && it > 0) ok = wait(o_free, (uint32_t)(it - 1) & 1);  // the last head's O has been read
+                        const int s = j % ST;
+                        if (!ok || !(ok = wait(p_full + 8 * (j % BUFS), (uint32_t)(j / BUFS) & 1) && wait(v_full(s), (uint32_t)(j / ST) & 1))) break;
+                        tc_fence_after();
+                        const uint64_t b = vd + (uint64_t)(s * (L::TILE >> 4));
+                        const uint32_t p = tS + j % BUFS * KT;
+#pragma unroll
+                        for (int k = 0; k < KT / 16; k++) sq_mma_ta(on, tO, p + 8 * k, b + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(t | k));
+                        f4_commit_on<1>(on, v_free(s));
+                        f4_commit_on<1>(on, pv_done + 8 * (j & 1));
+                        if (t == nt - 1) f4_commit_on<1>(on, o_full);
+                    }
+            } else {
+                // one head: no question of whose queries are there (asked before every tile, 8192 rows of 8 heads of 64 took 179 us, 163 so)
+                for (int j = 0; j < BUFS && j < nt && ok; j++) ok = scores();
+                for (int j = 0; j < nt && ok; j++) {
                     const int s = j % ST;
-                    if (!ok || !(ok = wait(p_full + 8 * (j % BUFS), (uint32_t)(j / BUFS) & 1) && wait(v_full(s), (uint32_t)(j / ST) & 1))) break;
+                    if (!(ok = wait(p_full + 8 * (j % BUFS), (uint32_t)(j / BUFS) & 1) && wait(v_full(s), (uint32_t)(j / ST) & 1))) break;
                     tc_fence_after();
                     const uint64_t b = vd + (uint64_t)(s * (L::TILE >> 4));
                     const uint32_t p = tS + j % BUFS * KT;
 #pragma unroll
-                    for (int k = 0; k < KT / 16; k++) sq_mma_ta(on, tO, p + 8 * k, b + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(t | k));
+                    for (int k = 0; k < KT / 16; k++) sq_mma_ta(on, tO, p + 8 * k, b + sq_mn_step(k), sq_idesc(DH, BF, true), (uint32_t)(j | k));
                     f4_commit_on<1>(on, v_free(s));
                     f4_commit_on<1>(on, pv_done + 8 * (j & 1));
-                    if (t == nt - 1) f4_commit_on<1>(on, o_full);
+                    if (j + BUFS < nt && !(ok = scores())) break;  // MMAs keep their order: P(j) has been read
                 }
+                f4_commit_on<1>(on, o_full);
+            }
             f4_commit_on<1>(on, done);
             wait(done, 0);
         }
