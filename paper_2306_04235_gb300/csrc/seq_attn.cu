@@ -14,16 +14,16 @@
 // of one: o 8.5e-4 low, 4e-6 so, of which one step is 4.9e-4).
 // Two CTAs per SM; three tiles of scores in TMEM (heads up to 64; two above), so that the
 // tensor core is tiles ahead of the threads that take powers: tiles of 128 keys with one
-// buffer waited 1750 of 3200 cycles a tile for it (8192 rows of 8 heads of 64 225 us, 158 so).
-// MMAs are issued by a converged warp (sq_mma): under a branch on the lane the issue of a
-// tile took 1250 cycles and set the pace (2 x 6000..8192 rows of 16 heads of 128 352 us, 309).
+// buffer waited 1750 of 3200 cycles a tile for it, before MMAs were issued by a converged warp
+// (sq_mma); under a branch on the lane the issue of a tile took 1250 cycles and set the pace (2 x
+// 6000..8192 rows of 16 heads of 128 352 us, 309 then).  Tiles of 128 keys were not measured again since.
 // Where O of a row is not finite though its sum is, an infinity or a NaN of a key
 // that the row does not see may have come in: such rows are computed again over
 // their own keys alone (attn_row).
 //
 // Bound by: heads of 128, the tensor core and its operands (8192 rows of 16 heads, 4 key
-// heads, causal 193 us, 1.42 PFLOP/s, pipe active 60 %: S of 64 keys reads 6 KB of shared memory
-// for 32 cycles of products, and 168 registers leave no more CTAs); heads of 64, issue (0.87 PFLOP/s; 8192 rows not causal);
+// heads, causal 191 us, 1.43 PFLOP/s, pipe active 63 %: S of 64 keys reads 6 KB of shared memory
+// for 32 cycles of products, and 168 registers leave no more CTAs); heads of 64, issue (0.84 PFLOP/s; 8192 rows of 8 heads, not causal, 163 us);
 // short sequences, a chain of latencies (128 targets of 20..160 rows against 20..128 keys, 8 heads of 64: 19 us for
 // 6.5 us of bytes: start 1, starts 0.6, search 0.6, first tile 1.4, 0.7 a tile, 1.8 the end of a head).
 #include "seq_tile.cuh"
@@ -478,8 +478,9 @@ int forward_heads(long items, const SeqAttn &a) {
     return keys >= 256 ? 1 : (int)(h < 4 ? h : 4);
 }
 // CTAs that share the walk of a head: few tiles of rows, each with four tiles of keys at least.  Causal walks, which differ
-// in length, gain until there are two CTAs for every SM (4096 rows of 8 heads 44 -> 35 us), others until there is one
-// (64 rows on 8192 keys of 8 heads 80 -> 16; 2048 rows not causal 24 -> 26).
+// in length, gain until there are two CTAs for every SM (4096 rows of 8 heads 44 -> 35 us at the time, 34 now), others until there is
+// one (64 rows on 8192 keys of 8 heads 80 -> 16, 14 now; 2048 rows not causal 24 -> 26, so alone, 20 now).  (Rows in memory over
+// sequences stand for their lengths, here and in forward_heads: a long sequence among many short ones is walked as they are.)
 int forward_ctas(long items, const SeqAttn &a) {
     const long keys = a.n_seqs ? a.k_rows / a.n_seqs : 0;
     int p = 1;

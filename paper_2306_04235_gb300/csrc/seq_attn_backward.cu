@@ -22,9 +22,9 @@
 // whose result is not finite are computed again over their own queries or keys alone.
 //
 // Bound by: long walks, the tensor core, fed in turns with the threads (8192 rows of 16 heads of 128 on 4 key heads, not
-// causal 1259 us: 1.09 PFLOP/s of the formula's five products, 1.53 of the seven; pipe active 49 % in dq, whose threads take
-// 1400 of 2600 cycles a tile); sentences, a chain of latencies in front of 2 to 3 tiles a CTA (128 x 20..128 rows of 8 heads
-// of 64, causal 41 us for 11 us of bytes; several heads a CTA, one after another, as the forward pass takes them, measured the
+// causal 1190 to 1210 us: 1.14 PFLOP/s of the formula's five products, 1.59 of the seven; pipe active 53 % in dq, 69 % in dk, dv,
+// 4096 causal rows); sentences, a chain of latencies in front of 2 to 3 tiles a CTA (128 x 20..128 rows of 8 heads
+// of 64, causal 39.6 us for 11 us of bytes; several heads a CTA, one after another, as the forward pass takes them, measured the
 // same: the CTA beside it fills the starts as well).
 #include "seq_tile.cuh"
 
@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(BW_THREADS, 512 / DqLayout<DH, W>::COLS) seq_a
             const int at = end - W * (t0 + j + 1) + W / 2 * half, lo = keys.lo - at, hi = keys.hi - at;
             const bool all = __all_sync(0xFFFFFFFFu, lo <= 0 && hi >= W / 2), some = __any_sync(0xFFFFFFFFu, hi > 0 && lo < W / 2);
             // (a value where there is none to read, or the registers count as used from one turn of the loop to the next:
-            // up to 160 bytes of spills; 3 x 2500..4095 rows of 16 heads of 128 400 us, so 387)
+            // up to 160 bytes of spills, 8 so; 3 x 2500..4095 rows of 16 heads of 128 400 us, 387 at the time)
             uint32_t s[W / 64][32] = {}, p[W / 64][32] = {};
             if (some) {
 #pragma unroll
@@ -903,8 +903,9 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
 // fitted to measured calls (1 to 8 sequences of 46 to 8192 rows, heads of 64 and 128, one to 16 heads a key head).  A CTA
 // takes 8 us beside its steps, a cluster as many more as it has CTAs; a step of 64 takes 0.95 where two CTAs share an SM, one of
 // 128 alone 1.45.  In one round the longest walk counts; in more, the sum of the work and half of the longest walk.
-// (4096 causal rows of 8 heads of 64: two CTAs 90 us, one 110; 2048 rows of 16 heads of 128 on 2 key heads: four 103, two 147,
-// eight 146; 2048 rows of 8 heads of 128: one 58, two 63, four 83.)
+// (At the time of the fit: 4096 causal rows of 8 heads of 64: two CTAs 90 us, one 110; 2048 rows of 16 heads of 128 on 2 key heads: four 103,
+// two 147, eight 146; 2048 rows of 8 heads of 128: one 58, two 63, four 83.  These take 95, 76 and 49 now, by the choices that it makes.
+// Rows in memory over sequences stand for their lengths: a long sequence among many short ones is walked as they are.)
 int walk_ctas(long units, long slots, double longest, double mean, int w) {
     const double step = w == 64 ? 0.95 : 1.45;
     int best = 1;

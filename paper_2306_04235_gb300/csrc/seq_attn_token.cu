@@ -11,9 +11,9 @@
 // Few long sequences (units = sequences x key heads x groups of 16 heads below two
 // per warp of the card): all tiles of all units are cut into equal runs, one per warp,
 // whatever unit they belong to; units that were cut are joined by a second kernel in
-// the order of their runs.  Many: a warp per unit, one launch.
-// 12 sequences of 9000..32768 keys of 4 heads of 128: 93 us, 5.9 TB/s (87 % of measured), of which the join 9; 512 of 80..160
-// keys of 8 heads of 64: 24 us, 5.2 TB/s (3.4 rounds of warps); 4 of 30..34 keys: 3 us, a launch.  Bound by bytes in
+// the order of their runs.  Many: a warp per unit, one launch, however long a single unit is.
+// 12 sequences of 9000..32768 keys of 4 heads of 128: 93 us, 5.9 TB/s (86 % of measured), of which the join 9; 512 of 80..160
+// keys of 8 heads of 64: 24.6 us, 5.2 TB/s (3.4 rounds of warps); 4 of 30..34 keys: 3.2 us, a launch.  Bound by bytes in
 // flight: 192 KB of rings per SM; rings of half the stages and twice the warps were no faster (23.7 and 94 us).
 #include "seq_attn.cuh"
 
@@ -424,7 +424,7 @@ cudaError_t token(const SeqAttn &a, cudaStream_t st) {
 
 template <int DH, bool BF>
 cudaError_t token_init() {
-    // the ring, and starts of up to 2 x 2 x 4 x 152 sequences
+    // the ring, and the pieces before each of fewer than 2 TK_GRID TK_WARPS sequences
     return cudaFuncSetAttribute(seq_attn_token_kernel<DH, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, TK_SMEM + 15 * 1024);
 }
 
