@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     const int lane = threadIdx.x & 31;
     bool in, few;
     if (w >= a.q_rows) return;
-    keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in, few);
+    keys_of_query(a, (int)w, last_with_rows(a.q_len, seq_of(a.q_start, a.n_seqs, (int)w)), in, few);
     if (!in) return;
     const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int h = 0; h < a.hq; h++) {

@@ -48,22 +48,40 @@ MNMT_DEV Span seq_rows(const int *start, const int *len, int b, int rows) {
     return r;
 }
 
-// Row's sequence and its rows: b, as seq_of gave it, or one before it where b and those between have no rows (with lengths
-// given, a sequence without rows may start at or among another's).  Whether row is one of them.
-MNMT_DEV bool rows_around(const int *start, const int *len, int rows, int row, int &b, Span &s) {
-    s = seq_rows(start, len, b, rows);
-    if (len)
-        while (row >= s.hi && b > 0 && len[b] <= 0) s = seq_rows(start, len, --b, rows);
-    return row < s.hi;
+// b, or the last sequence before it that has rows where it has none (with lengths given, a sequence without rows may start at or
+// among another's; 0 if there is none).  Whole warps, 256 lengths at a look: rows behind the last sequence of a batch with room for
+// more go back over all that are not used (128 sentences in a batch for 1000, forward: step by step 64 us, so 20).
+MNMT_DEV int last_with_rows(const int *len, int b) {
+    if (!len) return b;
+    const int lane = threadIdx.x & 31;
+    bool need = b > 0 && len[b] <= 0;
+    for (uint32_t todo; (todo = __ballot_sync(0xFFFFFFFFu, need)) != 0;) {
+        const int from = __shfl_sync(0xFFFFFFFFu, b, __ffs(todo) - 1);
+        int x = from, at = -1;  // no rows from x to from
+        while (x > 0 && at < 0) {
+            bool some[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) some[i] = len[max(x - 1 - 32 * i - lane, 0)] > 0 && x - 1 - 32 * i - lane >= 0;
+#pragma unroll
+            for (int i = 7; i >= 0; i--) {
+                const uint32_t m = __ballot_sync(0xFFFFFFFFu, some[i]);
+                if (m) at = x - 32 * i - __ffs(m);
+            }
+            x -= 256;
+        }
+        at = max(at, 0);
+        if (need && b <= from && b > at) b = at, need = false;
+    }
+    return b;
 }
 
-// the keys that query row sees (b: as seq_of; in: whether it belongs to a sequence at all; few: whether the rows of its
+// the keys that query row sees (b: as last_with_rows after seq_of; in: whether it belongs to a sequence at all; few: whether the rows of its
 // sequence that see a key see 10 of them or fewer on average)
 MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, int b, bool &in, bool &few) {
     in = few = false;
     if (b < 0) return Span{0, 0};
-    Span q;
-    if (!rows_around(a.q_start, a.q_len, a.q_rows, row, b, q)) return Span{0, 0};
+    const Span q = seq_rows(a.q_start, a.q_len, b, a.q_rows);
+    if (row >= q.hi) return Span{0, 0};
     in = true;
     Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
     const int nk = k.hi - k.lo;
@@ -77,8 +95,8 @@ MNMT_DEV Span keys_of_query(const SeqAttn &a, int row, int b, bool &in, bool &fe
 MNMT_DEV Span queries_of_key(const SeqAttn &a, int row, int b, bool &in, bool &one) {
     in = one = false;
     if (b < 0) return Span{0, 0};
-    Span k;
-    if (!rows_around(a.k_start, a.k_len, a.k_rows, row, b, k)) return Span{0, 0};
+    const Span k = seq_rows(a.k_start, a.k_len, b, a.k_rows);
+    if (row >= k.hi) return Span{0, 0};
     in = true;
     one = k.hi - k.lo == 1;
     Span q = seq_rows(a.q_start, a.q_len, b, a.q_rows);
@@ -129,11 +147,11 @@ MNMT_DEV int seq_of_lane(const int *start, int n, int row0) {
 
 // the keys that query row0 + lane sees, and the queries that see key row0 + lane; whole warps
 MNMT_DEV Span keys_of_lane(const SeqAttn &a, int row0, bool &in, bool &few) {
-    const int row = row0 + (threadIdx.x & 31), b = row0 < a.q_rows ? seq_of_lane(a.q_start, a.n_seqs, row0) : -1;
+    const int row = row0 + (threadIdx.x & 31), b = row0 < a.q_rows ? last_with_rows(a.q_len, seq_of_lane(a.q_start, a.n_seqs, row0)) : -1;
     return keys_of_query(a, row, row < a.q_rows ? b : -1, in, few);
 }
 MNMT_DEV Span queries_of_lane(const SeqAttn &a, int row0, bool &in, bool &one) {
-    const int row = row0 + (threadIdx.x & 31), b = row0 < a.k_rows ? seq_of_lane(a.k_start, a.n_seqs, row0) : -1;
+    const int row = row0 + (threadIdx.x & 31), b = row0 < a.k_rows ? last_with_rows(a.k_len, seq_of_lane(a.k_start, a.n_seqs, row0)) : -1;
     return queries_of_key(a, row, row < a.k_rows ? b : -1, in, one);
 }
 

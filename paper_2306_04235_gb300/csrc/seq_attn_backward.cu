@@ -887,11 +887,11 @@ __global__ void __launch_bounds__(256) seq_attn_zero_kernel(SeqAttn a) {
     bool in, one, few;
     if (a.k_rows == 0) {
         if (w >= a.q_rows) return;
-        keys_of_query(a, (int)w, seq_of(a.q_start, a.n_seqs, (int)w), in, few);
+        keys_of_query(a, (int)w, last_with_rows(a.q_len, seq_of(a.q_start, a.n_seqs, (int)w)), in, few);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hq; h++) store4(static_cast<T *>(a.dq.p) + w * a.dq.ld + h * a.dq.hd + 4 * lane, z);
     } else {
         if (w >= a.k_rows) return;
-        queries_of_key(a, (int)w, seq_of(a.k_start, a.n_seqs, (int)w), in, one);
+        queries_of_key(a, (int)w, last_with_rows(a.k_len, seq_of(a.k_start, a.n_seqs, (int)w)), in, one);
         for (int h = 0; in && 4 * lane < a.dh && h < a.hkv; h++) {
             store4(static_cast<T *>(a.dk.p) + w * a.dk.ld + h * a.dk.hd + 4 * lane, z);
             store4(static_cast<T *>(a.dv.p) + w * a.dv.ld + h * a.dv.hd + 4 * lane, z);

@@ -31,6 +31,28 @@ def test_empty_sequences(q_at, qn, k_at, kn, rows, causal, d, dtype):
     b.check_backward()
 
 
+@pytest.mark.parametrize("used,room", [(5, 64), (9, 10), (3, 1000), (7, 3000), (0, 50), (1, 9)])
+def test_a_batch_with_room(used, room):
+    """Few of many sequences in use, the others of length 0 behind the last row, at row 0, or anywhere; rows behind them."""
+    n = [(17 * i) % 60 + 1 for i in range(used)]
+    at = [sum(n[:i]) for i in range(used)]
+    T = sum(n)
+    for rest in ([T] * (room - used), [T + i // 40 for i in range(room - used)]):
+        b = Batch(at + rest, at + rest, 2, 1, 64, BF, True, q_len=n + [0] * (room - used), k_len=n + [0] * (room - used), q_rows=T + 300, k_rows=T + 300, seed=5)
+        b.forward()
+        b.check_forward()
+        b.backward()
+        b.check_backward()
+    if used:  # in front of all, and between
+        at2, n2 = [0] * 8 + at, [0] * 8 + n
+        at2[9:9], n2[9:9] = [at2[8]] * 11, [0] * 11
+        b = Batch(at2, at2, 2, 1, 128, FP, False, q_len=n2, k_len=n2, q_rows=T + 300, k_rows=T + 300, seed=6)
+        b.forward()
+        b.check_forward()
+        b.backward()
+        b.check_backward()
+
+
 @pytest.mark.parametrize("where", ["at", "inside", "many"])
 def test_among_many(where):
     """The same where more sequences are searched than shared memory holds, and in runs of hundreds without rows."""
